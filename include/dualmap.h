@@ -562,6 +562,185 @@ DM_API dm_status dm_export_prefix_tree(dm_handle *h, uint64_t *keys_host, uint64
 DM_API dm_status dm_potc_max_loads(uint32_t n_bins, uint64_t m_balls, uint32_t d, uint32_t trials, uint64_t seed,
                                    uint32_t *max_load_dev, void *stream);
 
+/* ---------------------------------------------------------------------------
+ * An instance's prefix cache (the key-value cache whose hits the router
+ * counts, Sec. 3.1 and App. A.3.2; the paper leaves it to the serving
+ * engine): keys and values in pages of B tokens, sequences that share the
+ * pages of a common prefix, and attention that reads a shared prefix once.
+ *
+ * These calls take no handle: dm_cache names the caller's device memory, and
+ * every call enqueues its work on `stream` (a cudaStream_t, NULL = legacy
+ * default stream) and returns.  Calls on one dm_cache share its bookkeeping
+ * and its work buffer, so the caller orders them (one stream, or events).
+ * Arguments that the host can check return an error and change nothing.
+ * What only the device can check (ids, lengths, free pages) is recorded in
+ * *status: the call that found it changes nothing, and the calls after it do
+ * nothing, until dm_cache_last_error has read and cleared the status. */
+
+typedef enum { DM_BF16 = 0, DM_F16 = 1 } dm_dtype;
+
+/* Order of a page's values: [head][token][dim] or [token][head][dim]. */
+typedef enum { DM_PAGES_HEADS = 0, DM_PAGES_TOKENS = 1 } dm_page_layout;
+
+/* The cache.  Sequence s (0 .. max_seqs-1) holds lengths[s] tokens; token p
+ * is slot p % page_tokens of page tables[s * max_blocks + p / page_tokens].
+ * refs[p] counts the sequences that hold page p; 0 = free.  A page that is
+ * held more than once is full, and nothing writes it.  A cache without
+ * sequences has lengths and refs of zero. */
+typedef struct {
+    void *k, *v;              /* layer 0's page 0; 16-byte aligned */
+    uint32_t dtype;           /* dm_dtype */
+    uint32_t layout;          /* dm_page_layout */
+    uint32_t layers;          /* >= 1 */
+    uint32_t pages;           /* 1 .. 2^30 */
+    uint32_t page_tokens;     /* B: 4, 8, 16, 32 or 64, as dm_config.block_tokens */
+    uint32_t kv_heads;        /* 1 .. 65535 */
+    uint32_t head_dim;        /* D: 64 or 128 */
+    uint32_t max_seqs;        /* rows of tables, >= 1 */
+    uint32_t max_blocks;      /* columns of tables, >= 1; max_blocks * B < 2^31 */
+    uint32_t reserved0;       /* must be 0 */
+    uint64_t layer_stride;    /* elements from a layer to the next; a multiple of 8 */
+    uint64_t page_stride;     /* elements from a page to the next; a multiple of 8, >= kv_heads * B * D */
+    int32_t *tables;          /* max_seqs x max_blocks */
+    int32_t *lengths;         /* max_seqs */
+    int32_t *refs;            /* pages; 16-byte aligned */
+    uint32_t *status;         /* one word, 0 at the start */
+    void *work;               /* dm_cache_work_bytes bytes, 16-byte aligned */
+    uint64_t work_bytes;
+} dm_cache;
+
+/* Size of dm_cache.work for a cache of this shape; 0 for an invalid one. */
+DM_API uint64_t dm_cache_work_bytes(const dm_cache *c);
+
+/* Synchronise `stream`, return the status that was recorded first (DM_OK if
+ * none) and clear it. */
+DM_API dm_status dm_cache_last_error(const dm_cache *c, void *stream);
+
+/* Sequence seqs[i] grows by add[i] >= 0 tokens (i < n, device arrays; every
+ * sequence once).  The blocks it lacks get the free pages with the lowest
+ * ids, in the order of i and then of blocks.  Nothing is written to the
+ * pages.  Recorded: DM_ERR_INVALID_ARG (an id out of range or twice, a
+ * negative count), DM_ERR_CAPACITY (too few free pages, or more than
+ * max_blocks blocks).  Asynchronous. */
+DM_API dm_status dm_cache_extend(const dm_cache *c, const int32_t *seqs, const int32_t *add, uint32_t n,
+                                 void *stream);
+
+/* The empty sequence children[i] becomes a copy of the first len[i] tokens of
+ * parents[i]: it holds the parent's full pages (counted in refs), and the
+ * len[i] % B tokens of a last page that is not full are copied, in every
+ * layer, to the free page with the lowest id (in the order of i).  A parent
+ * may be named many times, a child once.  Recorded: DM_ERR_INVALID_ARG (an
+ * id out of range, a child twice or not empty, len[i] < 0 or above the
+ * parent's length), DM_ERR_CAPACITY (too few free pages).  Asynchronous. */
+DM_API dm_status dm_cache_fork(const dm_cache *c, const int32_t *parents, const int32_t *children,
+                               const int32_t *len, uint32_t n, void *stream);
+
+/* Sequences seqs[0 .. n) give up their pages and become empty; a page that
+ * no sequence holds any more is free.  An empty sequence stays empty; the
+ * rows of `tables` keep their entries.  Recorded: DM_ERR_INVALID_ARG (an id
+ * out of range).  Asynchronous. */
+DM_API dm_status dm_cache_free(const dm_cache *c, const int32_t *seqs, uint32_t n, void *stream);
+
+/* Move the pages in use to the lowest ids: with `live` of them, the k-th
+ * page in use at or above id `live` moves to the k-th free id below it, in
+ * every layer.  tables_out and refs_out (device, the shapes of tables and
+ * refs, refs_out 16-byte aligned) receive the new bookkeeping, for the
+ * blocks that sequences hold; either may be the array that it replaces,
+ * where NULL means that array.  With arrays of their own the old ones stay
+ * right until a moved page's old place is given out again, so work on other
+ * streams that still reads through them is not disturbed.  *moved (device,
+ * may be NULL) receives the number of pages moved.  Asynchronous. */
+DM_API dm_status dm_cache_compact(const dm_cache *c, int32_t *tables_out, int32_t *refs_out, uint32_t *moved,
+                                  void *stream);
+
+/* New tokens' queries, keys and values of one layer (dm_cache_append).
+ * Sequence seqs[i]'s new tokens are rows offsets[i] .. offsets[i+1]) of q, k
+ * and v, and its last offsets[i+1] - offsets[i] tokens: position lengths -
+ * new + j.  Element (t, h, d) of q is q[t * q_token + h * q_head + d], and so
+ * for the others; strides are in elements and multiples of 8, pointers
+ * 16-byte aligned. */
+typedef struct {
+    const int32_t *seqs;      /* n */
+    const int32_t *offsets;   /* n + 1, not decreasing, within 0 .. tokens */
+    uint32_t n;
+    uint32_t tokens;          /* rows of q, k and v */
+    uint32_t layer;
+    uint32_t q_heads;         /* a multiple of kv_heads, or 0: no queries */
+    const void *q, *k, *v;
+    void *q_out;              /* may be q with q's strides; may overlap nothing else */
+    uint64_t q_token, q_head, k_token, k_head, v_token, v_head, q_out_token, q_out_head;
+    const void *q_weight, *k_weight;   /* D each, of the cache's type; NULL: no norm */
+    const float *cos, *sin;   /* rope_rows x rope_dim/2, 16-byte aligned; NULL with rope_dim 0 */
+    uint32_t rope_rows;       /* positions 0 .. rope_rows-1 */
+    uint32_t rope_dim;        /* dims that turn, from 0 on: a multiple of 16, <= D; 0: none */
+    uint32_t interleaved;     /* 1: dims 2j and 2j+1 turn together, 0: j and j + rope_dim/2 */
+    float eps;                /* of the norm, >= 0 */
+} dm_append_args;
+
+/* q_out = rotate(norm(q)), and rotate(norm(k)) and v stored at their tokens'
+ * slots: norm(x) = x / sqrt(mean(x^2) + eps) * weight over a head's D values,
+ * rotate turns the pair (a, b) of frequency j at position p to (a cos - b
+ * sin, b cos + a sin) with cos[p][j] and sin[p][j].  Computed in 32 bits and
+ * rounded once.  Rows outside offsets[0] .. offsets[n] are not touched.
+ * Recorded: DM_ERR_INVALID_ARG (an id, offset or page out of range, more new
+ * tokens than the sequence has, a position beyond rope_rows); which of the
+ * call's other rows are then stored is not specified.  Asynchronous. */
+DM_API dm_status dm_cache_append(const dm_cache *c, const dm_append_args *a, void *stream);
+
+/* The sequences that one attention step reads (dm_cache_plan).  seqs and
+ * offsets as in dm_append_args.  Group g is the sequences i in
+ * group_offsets[g] .. group_offsets[g+1]) of the step; all of them start with
+ * the same group_prefix[g] tokens (a multiple of B, 0 = nothing shared) in
+ * the same pages, and their new tokens come after it. */
+typedef struct {
+    const int32_t *seqs;
+    const int32_t *offsets;
+    uint32_t n;
+    uint32_t tokens;          /* rows of q */
+    uint32_t q_heads;         /* a multiple of kv_heads */
+    uint32_t groups;          /* 0: none */
+    const int32_t *group_offsets;   /* groups + 1, not decreasing, within 0 .. n */
+    const int32_t *group_prefix;    /* groups */
+    void *work;               /* dm_plan_bytes bytes, 256-byte aligned */
+    uint64_t work_bytes;
+} dm_plan;
+
+/* Size of dm_plan.work for a step of this shape; 0 for an invalid one. */
+DM_API uint64_t dm_plan_bytes(const dm_cache *c, uint32_t n, uint32_t groups, uint32_t tokens, uint32_t q_heads);
+
+/* Divide a step's attention over the GPU, from lengths as they are: once per
+ * step, for all its layers.  A group's prefix is read once for all its
+ * sequences where each of them has fewer than 128 query rows (new tokens x
+ * query heads per key head); otherwise each sequence reads it by itself.
+ * The plan holds until lengths or tables change.  Recorded:
+ * DM_ERR_INVALID_ARG (an id, offset or group out of range, a prefix that is
+ * no multiple of B, that reaches into the new tokens of a sequence, or whose
+ * pages differ), and the plan is then empty.  Asynchronous. */
+DM_API dm_status dm_cache_plan(const dm_cache *c, const dm_plan *p, void *stream);
+
+/* One layer's attention of a planned step (dm_cache_attend).  Strides and
+ * alignment as in dm_append_args. */
+typedef struct {
+    uint32_t layer;
+    float scale;              /* of the scores, finite and > 0 */
+    const void *q;
+    void *o;                  /* may not overlap q */
+    float *lse;               /* tokens x q_heads, or NULL */
+    uint64_t q_token, q_head, o_token, o_head;
+} dm_attend_args;
+
+/* o[t, h] = sum over p <= pos(t) of softmax(scale q[t, h] . k[p])[p] v[p], with
+ * the keys and values of head h / (q_heads / kv_heads); *lse receives the
+ * natural logarithm of the softmax's sum.  A token at a negative position
+ * (a sequence shorter than its new tokens) sees nothing: zeros, and an lse
+ * of minus infinity.  Slots behind a sequence's end are not read, whatever
+ * they hold.  Scores, maxima, sums and the output are held in 32 bits; the
+ * weights are rounded to the cache's type for the product with v.  Rows
+ * outside offsets[0] .. offsets[n] are not touched.  Uses the plan's work
+ * buffer, so layers of one plan run one after another.  Recorded:
+ * DM_ERR_TIMEOUT (a wait in the kernel gave up).  Asynchronous. */
+DM_API dm_status dm_cache_attend(const dm_cache *c, const dm_plan *p, const dm_attend_args *a, void *stream);
+
 /* Testing only (no paper counterpart): after this call the library's
  * (n + 1)-th device allocation, counted over every handle of the process,
  * fails as if the device were out of memory (without calling the CUDA

@@ -21,7 +21,8 @@ LIB = os.path.join(HERE, "libdualmap.so")
 BUILD_DEBUG = os.path.join(ROOT, "_build", "dualmap_debug")
 LIB_DEBUG = os.path.join(HERE, "libdualmap_debug.so")
 SOURCES = ["dm_api.cu", "dm_setup.cu", "dm_hash.cu", "dm_route.cu", "dm_choice.cu", "dm_commit.cu",
-           "dm_rebalance.cu", "dm_ring.cu", "dm_noalloc.cu", "dm_potc.cu"]
+           "dm_rebalance.cu", "dm_ring.cu", "dm_noalloc.cu", "dm_potc.cu", "dm_pages.cu", "dm_append.cu",
+           "dm_attend.cu", "dm_attend_wide.cu"]
 ARCH = ["-gencode", "arch=compute_103a,code=sm_103a"]
 FLAGS = ["-O3", "-lineinfo", "-std=c++17", "-Xcompiler", "-fPIC", "-Xcompiler", "-fvisibility=hidden",
          "--expt-relaxed-constexpr", "-I", os.path.join(ROOT, "include")]
@@ -44,7 +45,8 @@ def build(force=False, verbose=False, extra=(), debug=False):
     if debug:
         extra = ("-DDM_DEBUG",) + tuple(extra)
     os.makedirs(bdir, exist_ok=True)
-    headers = [os.path.join(CSRC, h) for h in ("dm_internal.cuh", "dm_launch.h", "dm_run_end.h")]
+    headers = [os.path.join(CSRC, h) for h in ("dm_internal.cuh", "dm_launch.h", "dm_run_end.h", "dm_cache.cuh",
+                                                  "dm_attend.cuh")]
     headers.append(os.path.join(ROOT, "include", "dualmap.h"))
     objs, jobs = [], []
     for s in SOURCES:

@@ -1,0 +1,211 @@
+"""An instance's prefix cache over torch tensors: pages of keys and values,
+sequences that share the pages of a common prefix, and the attention that
+reads them (dm_cache_* of include/dualmap.h).
+
+Only marshalling: it checks shapes and types, allocates outputs and work
+buffers on the device, and enqueues the C calls on torch's current stream.
+Calls on one cache, and the attention of one plan, have to be ordered by the
+caller, as work that shares a tensor is.
+"""
+
+import ctypes as C
+
+import torch
+
+from . import dualmap as D
+
+TYPES = {torch.bfloat16: D.DM_BF16, torch.float16: D.DM_F16}
+LAYOUTS = {"heads": D.DM_PAGES_HEADS, "tokens": D.DM_PAGES_TOKENS}
+
+
+class Plan:
+    """One step's division over the GPU (PagedCache.plan), for all its layers."""
+
+    def __init__(self, struct, keep, tokens, q_heads):
+        self.struct, self.keep, self.tokens, self.q_heads = struct, keep, tokens, q_heads
+
+
+class PagedCache:
+    """k, v: [layers, pages, kv_heads, page_tokens, head_dim] (layout "heads")
+    or [layers, pages, page_tokens, kv_heads, head_dim] ("tokens"), bfloat16 or
+    float16, each page contiguous; tables int32 [max_seqs, max_blocks], lengths
+    int32 [max_seqs], refs int32 [pages] (all zero in a cache without
+    sequences).  The cache keeps these tensors and changes them."""
+
+    def __init__(self, k, v, tables, lengths, refs, layout="heads"):
+        if layout not in LAYOUTS:
+            raise ValueError(f"layout {layout!r} is not one of {sorted(LAYOUTS)}")
+        if k.dim() != 5 or k.shape != v.shape or k.stride() != v.stride() or k.dtype != v.dtype:
+            raise ValueError("k and v are 5-dimensional, of one shape, layout and type")
+        if k.dtype not in TYPES:
+            raise ValueError(f"keys of type {k.dtype}: bfloat16 or float16 wanted")
+        layers, pages, a, b, dim = k.shape
+        if k.stride()[2:] != (b * dim, dim, 1):
+            raise ValueError("a page of k or v is not contiguous")
+        for name, x, shape in (("tables", tables, (lengths.shape[0], tables.shape[-1])), ("lengths", lengths, lengths.shape[:1]),
+                               ("refs", refs, (pages,))):
+            if x.dtype != torch.int32 or tuple(x.shape) != tuple(shape) or not x.is_contiguous():
+                raise ValueError(f"{name}: contiguous int32 of shape {tuple(shape)} wanted")
+        if len({x.device for x in (k, v, tables, lengths, refs)}) != 1 or k.device.type != "cuda":
+            raise ValueError("k, v, tables, lengths and refs live on one CUDA device")
+        self.k, self.v, self.tables, self.lengths, self.refs, self.layout = k, v, tables, lengths, refs, layout
+        self.device, self.dtype, self.layers, self.head_dim = k.device, k.dtype, layers, dim
+        self.kv_heads, self.page_tokens = (a, b) if layout == "heads" else (b, a)
+        self.status = torch.zeros(1, dtype=torch.int32, device=self.device)
+        self.struct = D.dm_cache(
+            k.data_ptr(), v.data_ptr(), TYPES[k.dtype], LAYOUTS[layout], layers, pages, self.page_tokens, self.kv_heads, dim,
+            lengths.shape[0], tables.shape[1], 0, k.stride(0) if layers > 1 else 0, k.stride(1) if pages > 1 else a * b * dim,
+            tables.data_ptr(), lengths.data_ptr(), refs.data_ptr(), self.status.data_ptr(), None, 0)
+        size = D.dm_cache_work_bytes(self.struct)
+        if not size:
+            raise D.DualMapError(D.DM_ERR_INVALID_ARG, "dm_cache_work_bytes")
+        self.work = torch.empty(size, dtype=torch.uint8, device=self.device)
+        self.struct.work, self.struct.work_bytes = self.work.data_ptr(), size
+
+    @classmethod
+    def empty(cls, *, pages, kv_heads, head_dim, max_seqs, max_tokens, page_tokens=16, layers=1, dtype=torch.bfloat16,
+              layout="heads", device="cuda"):
+        """A cache without sequences, each of up to max_tokens tokens."""
+        if layout not in LAYOUTS:
+            raise ValueError(f"layout {layout!r} is not one of {sorted(LAYOUTS)}")
+        inner = (kv_heads, page_tokens) if layout == "heads" else (page_tokens, kv_heads)
+        k = torch.empty((layers, pages) + inner + (head_dim,), dtype=dtype, device=device)
+        ints = dict(dtype=torch.int32, device=device)
+        return cls(k, torch.empty_like(k), torch.zeros(max_seqs, -(-max_tokens // page_tokens), **ints),
+                   torch.zeros(max_seqs, **ints), torch.zeros(pages, **ints), layout)
+
+    def _stream(self):
+        return C.c_void_p(torch.cuda.current_stream(self.device).cuda_stream)
+
+    def _ints(self, *named):
+        for name, x, n in named:
+            if x.dtype != torch.int32 or x.dim() != 1 or not x.is_contiguous() or x.device != self.device or \
+                    (n is not None and x.shape[0] != n):
+                raise ValueError(f"{name}: contiguous int32 on {self.device}" + (f" of length {n}" if n is not None else ""))
+
+    def _rows(self, name, x, tokens, heads):
+        if x.dtype != self.dtype or x.device != self.device or tuple(x.shape) != (tokens, heads, self.head_dim) or \
+                (x.shape[2] > 1 and x.stride(2) != 1):
+            raise ValueError(f"{name}: {self.dtype} on {self.device} of shape {(tokens, heads, self.head_dim)}, "
+                             f"head_dim contiguous")
+        # the stride of a dimension of one element says nothing
+        return (x.stride(0) if tokens > 1 else 0), (x.stride(1) if heads > 1 else 0)
+
+    def _call(self, where, rc):
+        if rc:
+            raise D.DualMapError(rc, where)
+
+    def last_error(self):
+        """The status of the first call that was refused on the device, which it clears (synchronises)."""
+        with torch.cuda.device(self.device):
+            return D.dm_cache_last_error(self.struct, self._stream())
+
+    def extend(self, seqs, add):
+        """Sequence seqs[i] grows by add[i] tokens; the pages it lacks are taken."""
+        self._ints(("seqs", seqs, None), ("add", add, seqs.shape[0]))
+        with torch.cuda.device(self.device):
+            self._call("dm_cache_extend", D.dm_cache_extend(self.struct, seqs, add, seqs.shape[0], self._stream()))
+
+    def fork(self, parents, children, lengths):
+        """The empty sequence children[i] becomes the first lengths[i] tokens of parents[i]."""
+        n = parents.shape[0]
+        self._ints(("parents", parents, None), ("children", children, n), ("lengths", lengths, n))
+        with torch.cuda.device(self.device):
+            self._call("dm_cache_fork", D.dm_cache_fork(self.struct, parents, children, lengths, n, self._stream()))
+
+    def free(self, seqs):
+        """The sequences give up their pages."""
+        self._ints(("seqs", seqs, None))
+        with torch.cuda.device(self.device):
+            self._call("dm_cache_free", D.dm_cache_free(self.struct, seqs, seqs.shape[0], self._stream()))
+
+    def compact(self, tables_out=None, refs_out=None, moved=None):
+        """Moves the pages in use to the lowest ids.  tables_out, refs_out: where
+        the new bookkeeping goes (default: in place); moved: an int32 tensor of
+        one element for the number of pages moved."""
+        for name, x, like in (("tables_out", tables_out, self.tables), ("refs_out", refs_out, self.refs)):
+            if x is not None and (x.dtype != torch.int32 or x.shape != like.shape or not x.is_contiguous() or
+                                  x.device != self.device):
+                raise ValueError(f"{name}: contiguous int32 of shape {tuple(like.shape)} on {self.device}")
+        if moved is not None:
+            self._ints(("moved", moved, 1))
+        with torch.cuda.device(self.device):
+            self._call("dm_cache_compact", D.dm_cache_compact(self.struct, tables_out, refs_out, moved, self._stream()))
+
+    def append(self, seqs, offsets, q, k, v, cos=None, sin=None, *, layer=0, q_weight=None, k_weight=None, eps=1e-6,
+               interleaved=False, out=None):
+        """Norms and rotates one layer's new queries and keys and stores keys and
+        values; returns the queries.
+
+        Sequence seqs[i]'s new tokens are rows offsets[i] .. offsets[i + 1] of q
+        [tokens, q_heads, head_dim], k and v [tokens, kv_heads, head_dim], and
+        the last ones of the sequence, which has been extended by them.  cos,
+        sin: float32 [positions, rotated dims / 2]; without them nothing turns.
+        q_weight, k_weight [head_dim]: without one there is no norm.  out:
+        where the queries go; may be q."""
+        n, tokens = seqs.shape[0], k.shape[0]
+        self._ints(("seqs", seqs, None), ("offsets", offsets, n + 1))
+        a = D.dm_append_args(seqs=seqs.data_ptr(), offsets=offsets.data_ptr(), n=n, tokens=tokens, layer=layer,
+                             q_heads=q.shape[1], rope_dim=0, interleaved=int(interleaved), eps=eps)
+        if out is None:
+            out = torch.empty(q.shape, dtype=self.dtype, device=self.device)
+        for name, x, heads in (("q", q, q.shape[1]), ("k", k, self.kv_heads), ("v", v, self.kv_heads),
+                               ("q_out", out, q.shape[1])):
+            strides = self._rows(name, x, tokens, heads)
+            setattr(a, name, x.data_ptr())
+            setattr(a, name + "_token", strides[0])
+            setattr(a, name + "_head", strides[1])
+        for name, x in (("q_weight", q_weight), ("k_weight", k_weight)):
+            if x is not None:
+                if x.dtype != self.dtype or tuple(x.shape) != (self.head_dim,) or not x.is_contiguous() or x.device != self.device:
+                    raise ValueError(f"{name}: contiguous {self.dtype} of shape {(self.head_dim,)} on {self.device}")
+                setattr(a, name, x.data_ptr())
+        if (cos is None) != (sin is None):
+            raise ValueError("cos and sin come together")
+        if cos is not None:
+            for name, x in (("cos", cos), ("sin", sin)):
+                if x.dtype != torch.float32 or x.dim() != 2 or x.shape != cos.shape or not x.is_contiguous() or x.device != self.device:
+                    raise ValueError(f"{name}: contiguous float32 [positions, rotated dims / 2] on {self.device}")
+            a.cos, a.sin, a.rope_rows, a.rope_dim = cos.data_ptr(), sin.data_ptr(), cos.shape[0], 2 * cos.shape[1]
+        with torch.cuda.device(self.device):
+            self._call("dm_cache_append", D.dm_cache_append(self.struct, a, self._stream()))
+        return out
+
+    def plan(self, seqs, offsets, tokens, q_heads, group_offsets=None, group_prefix=None):
+        """Divides the attention of a step of `tokens` query rows over the GPU.
+        Group g: sequences group_offsets[g] .. group_offsets[g + 1] of the step,
+        which start with the same group_prefix[g] tokens in the same pages."""
+        n = seqs.shape[0]
+        self._ints(("seqs", seqs, None), ("offsets", offsets, n + 1))
+        if (group_offsets is None) != (group_prefix is None):
+            raise ValueError("group_offsets and group_prefix come together")
+        groups = 0
+        if group_prefix is not None:
+            groups = group_prefix.shape[0]
+            self._ints(("group_prefix", group_prefix, None), ("group_offsets", group_offsets, groups + 1))
+        size = D.dm_plan_bytes(self.struct, n, groups, tokens, q_heads)
+        if not size:
+            raise D.DualMapError(D.DM_ERR_INVALID_ARG, "dm_plan_bytes")
+        work = torch.empty(size, dtype=torch.uint8, device=self.device)
+        s = D.dm_plan(seqs.data_ptr(), offsets.data_ptr(), n, tokens, q_heads, groups,
+                      group_offsets.data_ptr() if groups else None, group_prefix.data_ptr() if groups else None,
+                      work.data_ptr(), size)
+        with torch.cuda.device(self.device):
+            self._call("dm_cache_plan", D.dm_cache_plan(self.struct, s, self._stream()))
+        return Plan(s, (seqs, offsets, group_offsets, group_prefix, work), tokens, q_heads)
+
+    def attend(self, plan, q, *, layer=0, scale=None, out=None, lse=None):
+        """One layer's attention of the planned step: q [tokens, q_heads,
+        head_dim], scale (default head_dim ** -0.5).  lse: float32 [tokens,
+        q_heads] for the logarithms of the sums."""
+        if out is None:
+            out = torch.empty(q.shape, dtype=self.dtype, device=self.device)
+        qs, os = self._rows("q", q, plan.tokens, plan.q_heads), self._rows("out", out, plan.tokens, plan.q_heads)
+        if lse is not None and (lse.dtype != torch.float32 or tuple(lse.shape) != (plan.tokens, plan.q_heads) or
+                                not lse.is_contiguous() or lse.device != self.device):
+            raise ValueError(f"lse: contiguous float32 of shape {(plan.tokens, plan.q_heads)} on {self.device}")
+        a = D.dm_attend_args(layer, self.head_dim ** -0.5 if scale is None else scale, q.data_ptr(), out.data_ptr(),
+                             None if lse is None else lse.data_ptr(), *qs, *os)
+        with torch.cuda.device(self.device):
+            self._call("dm_cache_attend", D.dm_cache_attend(self.struct, plan.struct, a, self._stream()))
+        return out

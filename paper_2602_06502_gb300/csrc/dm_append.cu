@@ -1,0 +1,226 @@
+// dm_append.cu -- new tokens enter an instance's prefix cache
+// (dm_cache_append): each head's query and key is divided by its root mean
+// square, weighted and rotated by its position; queries go to the caller's
+// buffer, keys and values to their slots in the pages.
+//
+// One pass: a head's D values lie in D / 8 lanes, 16 bytes each, so the mean
+// square is a few shuffles, and the partner of a value that turns is either in
+// the same lane (pairs side by side) or a fixed number of lanes away.  All
+// arithmetic is in 32 bits; the only rounding is the store.
+//
+// Bound: HBM bandwidth, 2 bytes read and 2 written per value; a few tokens
+// alone, the latency of one launch.
+#include <algorithm>
+
+#include "dm_cache.cuh"
+
+namespace dm {
+namespace {
+
+struct AppendArgs {
+    const int32_t *seqs, *offsets, *tables, *lengths;
+    uint32_t *status;
+    const uint4 *q, *k, *v;
+    uint4 *q_out, *kc, *vc;   // kc, vc: this layer's pages
+    uint64_t qt, qh, kt, kh, vt, vh, ot, oh, page_stride;   // 16-byte units
+    uint32_t head_step, token_step;                         // within a page, 16-byte units
+    const uint4 *qw, *kw;
+    const float *cos, *sin;
+    uint32_t n, tokens, q_heads, kv_heads, B, pages, max_seqs, max_blocks, rope_rows, rope_dim, per_warp;
+    float eps;
+};
+
+template <class T>
+struct Two;
+template <>
+struct Two<__nv_bfloat16> {
+    using type = __nv_bfloat162;
+    static __device__ float2 up(type x) { return __bfloat1622float2(x); }
+    static __device__ type down(float a, float b) { return __floats2bfloat162_rn(a, b); }
+};
+template <>
+struct Two<__half> {
+    using type = __half2;
+    static __device__ float2 up(type x) { return __half22float2(x); }
+    static __device__ type down(float a, float b) { return __floats2half2_rn(a, b); }
+};
+
+template <class T>
+__device__ __forceinline__ void unpack(uint4 x, float *f) {
+    const auto *p = reinterpret_cast<const typename Two<T>::type *>(&x);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        const float2 y = Two<T>::up(p[i]);
+        f[2 * i] = y.x;
+        f[2 * i + 1] = y.y;
+    }
+}
+
+template <class T>
+__device__ __forceinline__ uint4 pack(const float *f) {
+    uint4 x;
+    auto *p = reinterpret_cast<typename Two<T>::type *>(&x);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) p[i] = Two<T>::down(f[2 * i], f[2 * i + 1]);
+    return x;
+}
+
+// A warp: 32 / (D / 8) heads at a time of one token, per_warp heads in all
+// (the token's heads in the order queries, keys, values).
+template <class T, int D, bool kInterleaved>
+__global__ void __launch_bounds__(256) k_append(AppendArgs p) {
+    constexpr uint32_t L = D / 8, H = 32 / L;
+    const uint32_t lane = threadIdx.x & 31, l = lane % L, sub = lane / L;
+    const uint32_t heads = p.q_heads + 2 * p.kv_heads, parts = (heads + p.per_warp - 1) / p.per_warp;
+    const uint64_t warp = (uint64_t)blockIdx.x * (blockDim.x / 32) + threadIdx.x / 32;
+    const uint32_t t = (uint32_t)(warp / parts), h0 = (uint32_t)(warp % parts) * p.per_warp;
+    if (t >= p.tokens || has_err(p.status)) return;
+    // the token's sequence: the last i with offsets[i] <= t
+    const int32_t first = p.offsets[0], last = p.offsets[p.n];
+    if (first < 0 || last < first || (uint32_t)last > p.tokens) {
+        if (lane == 0) set_err(p.status, DM_ERR_INVALID_ARG);
+        return;
+    }
+    if ((int32_t)t < first || (int32_t)t >= last) return;
+    uint32_t lo = 0, hi = p.n;
+    while (hi - lo > 1) {
+        const uint32_t mid = (lo + hi) / 2;
+        if (p.offsets[mid] <= (int32_t)t) lo = mid;
+        else hi = mid;
+    }
+    const int32_t s = p.seqs[lo], end = p.offsets[lo + 1];
+    bool bad = (uint32_t)s >= p.max_seqs || end <= (int32_t)t || (uint32_t)end > p.tokens;
+    const int64_t pos = bad ? 0 : (int64_t)p.lengths[s] - (end - (int32_t)t);
+    bad = bad || pos < 0 || pos / p.B >= p.max_blocks || (p.rope_dim && pos >= p.rope_rows);
+    const uint32_t page = bad ? 0 : (uint32_t)p.tables[(uint64_t)s * p.max_blocks + (uint32_t)pos / p.B];
+    if (bad || page >= p.pages) {
+        if (lane == 0) set_err(p.status, DM_ERR_INVALID_ARG);
+        return;
+    }
+    const uint64_t slot = page * p.page_stride + (uint32_t)pos % p.B * p.token_step;
+    // this lane's cosines and sines: of its own values' frequencies
+    constexpr int F = kInterleaved ? 4 : 8;
+    float c[F], sn[F];
+    const uint32_t e0 = l * 8, half = p.rope_dim / 2;
+    const bool turns = e0 < p.rope_dim, low = e0 < half;
+    if (turns) {
+        const uint64_t at = (uint64_t)pos * half + (kInterleaved ? e0 / 2 : low ? e0 : e0 - half);
+#pragma unroll
+        for (int i = 0; i < F; i += 4) {
+            *reinterpret_cast<float4 *>(c + i) = *reinterpret_cast<const float4 *>(p.cos + at + i);
+            *reinterpret_cast<float4 *>(sn + i) = *reinterpret_cast<const float4 *>(p.sin + at + i);
+        }
+    }
+    const uint32_t partner = sub * L + (low ? l + half / 8 : l - half / 8) % L;
+    float qw[8], kw[8];
+    if (p.qw) unpack<T>(p.qw[l], qw);
+    if (p.kw) unpack<T>(p.kw[l], kw);
+    const uint32_t h1 = min(heads, h0 + p.per_warp);
+    constexpr int U = 4;   // heads of a lane whose loads are in flight together
+    for (uint32_t hb = h0; hb < h1; hb += H * U) {
+        uint4 raw[U];
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            const uint32_t h = hb + u * H + sub;
+            const uint4 *src = h < p.q_heads                ? p.q + t * p.qt + h * p.qh
+                               : h < p.q_heads + p.kv_heads ? p.k + t * p.kt + (h - p.q_heads) * p.kh
+                                                            : p.v + t * p.vt + (h - p.q_heads - p.kv_heads) * p.vh;
+            if (h < h1) raw[u] = src[l];
+        }
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            const uint32_t h = hb + u * H + sub;
+            const bool is_q = h < p.q_heads, is_v = h >= p.q_heads + p.kv_heads;
+            float x[8], y[8];
+            unpack<T>(h < h1 ? raw[u] : make_uint4(0, 0, 0, 0), x);
+            float ss = 0.f;
+#pragma unroll
+            for (int i = 0; i < 8; ++i) ss += x[i] * x[i];
+#pragma unroll
+            for (uint32_t d = 1; d < L; d *= 2) ss += __shfl_xor_sync(~0u, ss, d);
+            if (is_q ? p.qw != nullptr : p.kw != nullptr) {
+                const float r = rsqrtf(ss * (1.f / D) + p.eps);
+#pragma unroll
+                for (int i = 0; i < 8; ++i) x[i] = x[i] * r * (is_q ? qw[i] : kw[i]);
+            }
+            if (kInterleaved) {
+                if (turns)
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) {
+                        const float a = x[2 * i], b = x[2 * i + 1];
+                        x[2 * i] = a * c[i % F] - b * sn[i % F];
+                        x[2 * i + 1] = b * c[i % F] + a * sn[i % F];
+                    }
+            } else if (p.rope_dim) {
+#pragma unroll
+                for (int i = 0; i < 8; ++i) y[i] = __shfl_sync(~0u, x[i], partner);
+                if (turns)
+#pragma unroll
+                    for (int i = 0; i < 8; ++i)
+                        x[i] = low ? x[i] * c[i % F] - y[i] * sn[i % F] : x[i] * c[i % F] + y[i] * sn[i % F];
+            }
+            if (h < h1) {
+                if (is_q) p.q_out[t * p.ot + h * p.oh + l] = pack<T>(x);
+                else if (is_v) p.vc[slot + (uint64_t)(h - p.q_heads - p.kv_heads) * p.head_step + l] = raw[u];
+                else p.kc[slot + (uint64_t)(h - p.q_heads) * p.head_step + l] = pack<T>(x);
+            }
+        }
+    }
+}
+
+template <class T, int D>
+void append_launch(const AppendArgs &p, bool interleaved, uint32_t grid, cudaStream_t st) {
+    if (interleaved) k_append<T, D, true><<<grid, 256, 0, st>>>(p);
+    else k_append<T, D, false><<<grid, 256, 0, st>>>(p);
+}
+
+}  // namespace
+}  // namespace dm
+
+extern "C" dm_status dm_cache_append(const dm_cache *c, const dm_append_args *a, void *stream) {
+    using namespace dm;
+    if (!cache_ok(c) || !a || a->layer >= c->layers || a->tokens > 0x7FFFFFFFu) return DM_ERR_INVALID_ARG;
+    if (a->q_heads % c->kv_heads || a->q_heads > 65535 * 32u || !(a->eps >= 0.f)) return DM_ERR_INVALID_ARG;
+    if (a->rope_dim % 16 || a->rope_dim > c->head_dim || (a->rope_dim && (!a->cos || !a->sin || !a->rope_rows)))
+        return DM_ERR_INVALID_ARG;
+    if (a->n > c->max_seqs || a->interleaved > 1) return DM_ERR_INVALID_ARG;
+    if (a->n == 0 || a->tokens == 0) return DM_OK;
+    if (!a->seqs || !a->offsets || !a->k || !a->v || (a->q_heads && (!a->q || !a->q_out))) return DM_ERR_INVALID_ARG;
+    for (const void *x : {a->q, a->k, a->v, (const void *)a->q_out, a->q_weight, a->k_weight, (const void *)a->cos,
+                          (const void *)a->sin})
+        if (!aligned(x, 16)) return DM_ERR_INVALID_ARG;
+    if ((a->q_token | a->q_head | a->k_token | a->k_head | a->v_token | a->v_head | a->q_out_token | a->q_out_head) % 8)
+        return DM_ERR_INVALID_ARG;
+    const PageShape ps = page_shape(c);
+    AppendArgs p{};
+    p.seqs = a->seqs, p.offsets = a->offsets, p.tables = c->tables, p.lengths = c->lengths, p.status = c->status;
+    p.q = (const uint4 *)a->q, p.k = (const uint4 *)a->k, p.v = (const uint4 *)a->v, p.q_out = (uint4 *)a->q_out;
+    p.kc = (uint4 *)c->k + a->layer * (c->layer_stride / 8);
+    p.vc = (uint4 *)c->v + a->layer * (c->layer_stride / 8);
+    p.qt = a->q_token / 8, p.qh = a->q_head / 8, p.kt = a->k_token / 8, p.kh = a->k_head / 8;
+    p.vt = a->v_token / 8, p.vh = a->v_head / 8, p.ot = a->q_out_token / 8, p.oh = a->q_out_head / 8;
+    p.page_stride = c->page_stride / 8, p.head_step = ps.head_step / 8, p.token_step = ps.token_step / 8;
+    p.qw = (const uint4 *)a->q_weight, p.kw = (const uint4 *)a->k_weight, p.cos = a->cos, p.sin = a->sin;
+    p.n = a->n, p.tokens = a->tokens, p.q_heads = a->q_heads, p.kv_heads = c->kv_heads, p.B = c->page_tokens;
+    p.pages = c->pages, p.max_seqs = c->max_seqs, p.max_blocks = c->max_blocks;
+    p.rope_rows = a->rope_rows, p.rope_dim = a->rope_dim, p.eps = a->eps;
+    // heads of a token per warp: all of one round of loads, halved while the
+    // warps would not fill the SMs
+    const uint32_t heads = a->q_heads + 2 * c->kv_heads, once = 32 / (c->head_dim / 8);
+    p.per_warp = once * 4;
+    while (p.per_warp > once && (uint64_t)a->tokens * ((heads + p.per_warp - 1) / p.per_warp) < (uint64_t)sm_count() * 32)
+        p.per_warp /= 2;
+    const uint64_t warps = (uint64_t)a->tokens * ((heads + p.per_warp - 1) / p.per_warp);
+    if ((warps + 7) / 8 > 0x7FFFFFFFu) return DM_ERR_INVALID_ARG;
+    const uint32_t grid = (uint32_t)((warps + 7) / 8);
+    const auto st = static_cast<cudaStream_t>(stream);
+    const bool il = a->interleaved != 0;
+    if (c->dtype == DM_BF16) {
+        if (c->head_dim == 64) append_launch<__nv_bfloat16, 64>(p, il, grid, st);
+        else append_launch<__nv_bfloat16, 128>(p, il, grid, st);
+    } else {
+        if (c->head_dim == 64) append_launch<__half, 64>(p, il, grid, st);
+        else append_launch<__half, 128>(p, il, grid, st);
+    }
+    return cudaGetLastError() == cudaSuccess ? DM_OK : DM_ERR_CUDA;
+}

@@ -1,0 +1,306 @@
+// dm_attend.cuh -- what the attention kernels over the paged cache share: the
+// division of a step's work (dm_cache_plan), and how their parts are joined.
+//
+// Rows.  A query row is a token and one of the G = q_heads / kv_heads heads
+// that read the same keys; a sequence's rows against one key head, or a whole
+// group's against its shared prefix, go through the tensor cores together.
+//
+// Work.  A block is up to 256 rows (wide: the tcgen05 kernel) or up to 16
+// (narrow) of one sequence or group and a range of keys; with a key head it is
+// a tile, cut into units of 128 (wide) or 64 (narrow) keys.  All U units of a
+// kind stand in one line, and CTA i of S (no more than there are units, so
+// that each has some) takes those from i U / S to (i + 1) U / S: every SM gets
+// the same number of keys whatever the lengths.
+// A tile that a boundary cuts, and every tile of a shared group, leaves
+// (maximum, sum, unnormalised output) per row and CTA; k_attend_join adds them
+// up.  A CTA and tile meet in one place of a staircase through (tiles x CTAs),
+// so `first row + 256 CTA` (16 for narrow) is a place of its own for each.
+#pragma once
+
+#include <cuda.h>
+
+#include "dm_cache.cuh"
+
+namespace dm {
+
+constexpr uint32_t kWideRows = 256, kWideKeys = 128, kNarrowRows = 16, kNarrowKeys = 64;
+constexpr uint32_t kShareRows = 128;   // a sequence with as many rows fills a tile by itself
+constexpr uint32_t kNarrowPerSm = 2;
+
+struct AttendBlock {
+    int32_t row;          // of tables
+    int32_t token0;       // its sequence's or group's first query token
+    uint32_t row0, rows;  // its rows among them
+    int32_t kv0, kv1;     // keys; no row sees one from kv1 on
+    int32_t pos0;         // token0's position (a group's prefix: all rows see all keys)
+    uint32_t units;       // per key head, >= 1
+    uint32_t part0;       // shared: its first row in the parts
+    uint32_t shared;
+};
+
+struct PlanHead {
+    uint64_t units[2];    // wide, narrow
+    uint32_t blocks[2];
+    uint32_t ok, pad;
+};
+
+// The plan's work buffer.
+struct PlanWork {
+    PlanHead *head;
+    AttendBlock *block[2];    // wide, narrow
+    uint64_t *cum[2];         // units before each block
+    uint32_t *first[2];       // per entity (groups, then sequences): blocks of the kind before it
+    uint32_t *group_max, *group_n;   // most rows of a sequence; sequences with rows
+    int32_t *group_of;        // per sequence: its shared group, or -1
+    float *part[2];           // rows x D
+    float2 *ml[2];            // rows: maximum (base 2), sum
+    uint64_t shared_rows[2];  // the parts' rows before the cut tiles' (two per CTA)
+};
+
+struct PlanShape {
+    uint32_t n, groups, tokens, q_heads, G, D, sms;
+    uint32_t ctas[2], blocks[2];
+    uint64_t rows[2], shared_rows[2];
+};
+
+inline bool plan_shape(const dm_cache *c, uint32_t n, uint32_t groups, uint32_t tokens, uint32_t q_heads, PlanShape &s) {
+    if (!cache_shape_ok(c) || q_heads == 0 || q_heads % c->kv_heads || q_heads > 65535u * 32) return false;
+    if (n > c->max_seqs || groups > n || tokens > 0x7FFFFFFFu) return false;
+    s.n = n, s.groups = groups, s.tokens = tokens, s.q_heads = q_heads;
+    s.G = q_heads / c->kv_heads, s.D = c->head_dim, s.sms = (uint32_t)sm_count();
+    s.ctas[0] = s.sms, s.ctas[1] = s.sms * kNarrowPerSm;
+    const uint32_t cap[2] = {kWideRows, kNarrowRows};
+    // a sequence of a shared group has fewer than kShareRows rows, a narrow
+    // one at most kNarrowRows; each of its rows has a part of the prefix and one of its own keys
+    const uint32_t most[2] = {kShareRows - 1, kNarrowRows};
+    for (int k = 0; k < 2; ++k) {
+        const uint64_t t = std::min<uint64_t>(tokens, (uint64_t)n * (most[k] / s.G));
+        s.shared_rows[k] = (groups ? 2 * t * q_heads : 0) + (uint64_t)cap[k] * s.ctas[k];
+        s.rows[k] = s.shared_rows[k] + 2ull * cap[k] * s.ctas[k];
+        if (s.rows[k] > 0xFFFFFFFFull) return false;
+    }
+    const uint64_t wide = (uint64_t)n + groups + 2 * ((uint64_t)tokens * s.G / kWideRows);
+    if (wide > 0x7FFFFFFFull || (uint64_t)tokens * s.G > 0x7FFFFFFFull) return false;
+    s.blocks[0] = (uint32_t)wide;
+    s.blocks[1] = n + groups;
+    return true;
+}
+
+// Lays the buffer out from `base` (which may be null, for its size).
+inline uint64_t plan_work(const PlanShape &s, void *base, PlanWork &w) {
+    uint64_t at = 0;
+    auto take = [&](uint64_t bytes) {
+        char *p = static_cast<char *>(base) + at;
+        at += align_up(bytes, 256);
+        return p;
+    };
+    w.head = (PlanHead *)take(sizeof(PlanHead));
+    for (int k = 0; k < 2; ++k) {
+        w.block[k] = (AttendBlock *)take(sizeof(AttendBlock) * s.blocks[k]);
+        w.cum[k] = (uint64_t *)take(8ull * s.blocks[k]);
+        w.first[k] = (uint32_t *)take(4ull * (s.n + s.groups + 1));
+    }
+    w.group_max = (uint32_t *)take(4ull * s.groups);
+    w.group_n = (uint32_t *)take(4ull * s.groups);
+    w.group_of = (int32_t *)take(4ull * s.n);
+    for (int k = 0; k < 2; ++k) {
+        w.part[k] = (float *)take(4ull * s.D * s.rows[k]);
+        w.ml[k] = (float2 *)take(8ull * s.rows[k]);
+        w.shared_rows[k] = s.shared_rows[k];
+    }
+    return at;
+}
+
+struct AttendArgs {
+    PlanWork w;
+    const int32_t *tables;
+    uint32_t *status;
+    const char *q;
+    char *o;
+    float *lse;
+    uint64_t q_token, q_head, o_token, o_head;   // bytes
+    uint32_t max_blocks, pages, B, box, G, kv_heads, q_heads;   // box: rows of a TMA box
+    float scale2;                                // scale * log2(e)
+    uint32_t ctas[2];
+    const int32_t *offsets, *group_offsets;
+    uint32_t n, groups, tokens;
+};
+
+// The CTA of S that unit u of U falls to: the last i with i U / S <= u.
+__device__ __forceinline__ uint32_t cta_of(uint64_t u, uint64_t U, uint32_t S) {
+    return (uint32_t)(((u + 1) * S - 1) / U);
+}
+
+// Walks the tiles of a CTA's units.
+template <int kKind>
+struct Walk {
+    uint64_t u, end;
+    uint32_t b, blocks;
+    // of the present piece
+    AttendBlock k;
+    uint32_t head, j0, units;   // units j0 .. j0 + units of the tile
+    bool in, out;               // another CTA has units before, behind
+
+    __device__ Walk(const AttendArgs &p) {
+        const PlanHead &h = *p.w.head;
+        const uint64_t U = h.ok ? h.units[kKind] : 0;
+        blocks = h.ok ? h.blocks[kKind] : 0;
+        const uint64_t S = min((uint64_t)gridDim.x, U);
+        u = blockIdx.x < S ? blockIdx.x * U / S : 0;
+        end = blockIdx.x < S ? (blockIdx.x + 1) * U / S : 0;
+        uint32_t lo = 0, hi = blocks;   // the last block with cum <= u
+        while (u < end && hi - lo > 1) {
+            const uint32_t mid = (lo + hi) / 2;
+            if (p.w.cum[kKind][mid] <= u) lo = mid;
+            else hi = mid;
+        }
+        b = lo;
+    }
+    __device__ bool next(const AttendArgs &p) {
+        if (u >= end) return false;
+        k = p.w.block[kKind][b];
+        uint64_t at = u - p.w.cum[kKind][b];
+        if (at >= (uint64_t)k.units * p.kv_heads) {
+            ++b;   // every block has units
+            k = p.w.block[kKind][b];
+            at = 0;
+        }
+        head = (uint32_t)(at / k.units);
+        j0 = (uint32_t)(at % k.units);
+        units = (uint32_t)min((uint64_t)(k.units - j0), end - u);
+        in = j0 > 0;
+        out = j0 + units < k.units;
+        u += units;
+        return true;
+    }
+    // Whether the rows go straight to the output, and if not their first row
+    // in the parts.
+    __device__ bool whole() const { return !k.shared && !in && !out; }
+    __device__ uint64_t part_row(const AttendArgs &p) const {
+        constexpr uint32_t cap = kKind == 0 ? kWideRows : kNarrowRows;
+        if (k.shared) return k.part0 + (uint64_t)head * k.rows + (uint64_t)cap * blockIdx.x;
+        return p.w.shared_rows[kKind] + (uint64_t)cap * (2 * blockIdx.x + (in ? 0 : 1));
+    }
+};
+
+// One past the last key that row r of a block sees.
+__device__ __forceinline__ int32_t row_limit(const AttendBlock &k, uint32_t r, uint32_t G) {
+    return min(k.kv1, k.pos0 + (int32_t)((k.row0 + r) / G) + 1);
+}
+
+__device__ __forceinline__ uint32_t smem_addr(const void *p) { return (uint32_t)__cvta_generic_to_shared(p); }
+
+__device__ __forceinline__ float exp2_(float x) {
+    float y;
+    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+    return y;
+}
+
+// -- mbarriers and TMA ---------------------------------------------------------
+
+__device__ __forceinline__ void mbar_init(uint32_t bar, uint32_t count) {
+    asm volatile("mbarrier.init.shared::cta.b64 [%0], %1;" ::"r"(bar), "r"(count) : "memory");
+}
+__device__ __forceinline__ void mbar_arrive(uint32_t bar) {
+    asm volatile("mbarrier.arrive.shared::cta.b64 _, [%0];" ::"r"(bar) : "memory");
+}
+__device__ __forceinline__ void mbar_expect(uint32_t bar, uint32_t bytes) {
+    asm volatile("mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], %1;" ::"r"(bar), "r"(bytes) : "memory");
+}
+__device__ __forceinline__ bool mbar_try(uint32_t bar, uint32_t parity) {
+    uint32_t ok;
+    asm volatile(
+        "{\n\t.reg .pred p;\n\t"
+        "mbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2;\n\t"
+        "selp.u32 %0, 1, 0, p;\n\t}"
+        : "=r"(ok)
+        : "r"(bar), "r"(parity)
+        : "memory");
+    return ok != 0;
+}
+__device__ __forceinline__ uint64_t now_ns() {
+    uint64_t t;
+    asm volatile("mov.u64 %0, %globaltimer;" : "=l"(t));
+    return t;
+}
+constexpr uint32_t kWaits = 1u << 24;
+constexpr uint64_t kWaitNs = 2'000'000'000;
+// Waits for the phase, at most kWaitNs and kWaits tries.
+__device__ __forceinline__ bool mbar_drain(uint32_t bar, uint32_t parity, const volatile uint32_t *gave_up = nullptr) {
+    if (mbar_try(bar, parity)) return true;
+    const uint64_t t0 = now_ns();
+    for (uint32_t i = 0; i < kWaits; ++i) {
+        if (mbar_try(bar, parity)) return true;
+        if (gave_up && *gave_up) return true;
+        if ((i & 63) == 63 && now_ns() - t0 > kWaitNs) break;
+    }
+    return false;
+}
+// The same by a whole warp; a wait that gives up says so in `gave_up` (shared
+// memory), and the CTA's others then return at once.  The caller goes on
+// either way: every loop is as long as its data says, so the CTA ends.
+__device__ __forceinline__ void mbar_wait(uint32_t bar, uint32_t parity, volatile uint32_t *gave_up, uint32_t *status) {
+    if (!mbar_drain(bar, parity, gave_up)) {
+        *gave_up = 1;
+        set_err(status, DM_ERR_TIMEOUT);
+    }
+    __syncwarp();
+}
+
+__device__ __forceinline__ void tma_load4(uint32_t dst, const CUtensorMap *map, uint32_t bar, int c0, int c1, int c2, int c3) {
+    asm volatile(
+        "cp.async.bulk.tensor.4d.shared::cta.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%3, %4, %5, %6}], [%2];" ::"r"(dst),
+        "l"(map), "r"(bar), "r"(c0), "r"(c1), "r"(c2), "r"(c3)
+        : "memory");
+}
+
+// Key rows tok0 .. tok0 + keys of a sequence into shared memory, as D / 64
+// halves of 128-byte rows (128-byte swizzle); pages behind block `blocks` and
+// ids out of range give zeros.  Called by a whole warp.
+template <int D, int kKeys>
+__device__ __forceinline__ void load_keys(const AttendArgs &p, const CUtensorMap *map, uint32_t dst, uint32_t bar, const int32_t *table,
+                                          uint32_t tok0, uint32_t blocks, uint32_t head) {
+    constexpr uint32_t kHalves = D / 64;
+    const uint32_t boxes = kKeys / p.box * kHalves;
+    for (uint32_t x = threadIdx.x & 31; x < boxes; x += 32) {
+        const uint32_t half = x % kHalves, at = x / kHalves * p.box, blk = (tok0 + at) / p.B;
+        uint32_t page = blk < blocks ? (uint32_t)__ldg(table + blk) : p.pages;
+        page = min(page, p.pages);   // a page that does not exist reads as zeros
+        tma_load4(dst + half * kKeys * 128 + at * 128, map, bar, (int)half * 64, (int)((tok0 + at) % p.B), (int)head, (int)page);
+    }
+}
+
+template <class T>
+struct Pack2;
+template <>
+struct Pack2<__nv_bfloat16> {
+    static constexpr uint32_t kMmaType = 1;   // of the tcgen05 instruction descriptor
+    static __device__ __forceinline__ uint32_t pack(float lo, float hi) {
+        uint32_t r;
+        asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(r) : "f"(hi), "f"(lo));
+        return r;
+    }
+    static __device__ __forceinline__ void mma(float *c, const uint32_t *a, uint32_t b0, uint32_t b1) {
+        asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
+                     : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3])
+                     : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
+    }
+};
+template <>
+struct Pack2<__half> {
+    static constexpr uint32_t kMmaType = 0;
+    static __device__ __forceinline__ uint32_t pack(float lo, float hi) {
+        uint32_t r;
+        asm("cvt.rn.f16x2.f32 %0, %1, %2;" : "=r"(r) : "f"(hi), "f"(lo));
+        return r;
+    }
+    static __device__ __forceinline__ void mma(float *c, const uint32_t *a, uint32_t b0, uint32_t b1) {
+        asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
+                     : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3])
+                     : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
+    }
+};
+
+cudaError_t launch_attend_wide(const dm_cache *c, const AttendArgs &p, const CUtensorMap &mk, const CUtensorMap &mv, cudaStream_t st);
+
+}  // namespace dm

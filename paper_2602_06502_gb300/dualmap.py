@@ -93,6 +93,44 @@ class dm_migration(C.Structure):
     _fields_ = [("req_seq", C.c_uint64), ("from_", C.c_uint32), ("to", C.c_uint32)]
 
 
+# dm_dtype, dm_page_layout
+DM_BF16, DM_F16 = 0, 1
+DM_PAGES_HEADS, DM_PAGES_TOKENS = 0, 1
+
+
+class dm_cache(C.Structure):
+    _fields_ = [("k", C.c_void_p), ("v", C.c_void_p)] + \
+               [(name, C.c_uint32) for name in
+                ("dtype", "layout", "layers", "pages", "page_tokens", "kv_heads", "head_dim", "max_seqs", "max_blocks",
+                 "reserved0")] + \
+               [("layer_stride", C.c_uint64), ("page_stride", C.c_uint64)] + \
+               [(name, C.c_void_p) for name in ("tables", "lengths", "refs", "status", "work")] + \
+               [("work_bytes", C.c_uint64)]
+
+
+class dm_append_args(C.Structure):
+    _fields_ = [("seqs", C.c_void_p), ("offsets", C.c_void_p)] + \
+               [(name, C.c_uint32) for name in ("n", "tokens", "layer", "q_heads")] + \
+               [(name, C.c_void_p) for name in ("q", "k", "v", "q_out")] + \
+               [(name, C.c_uint64) for name in
+                ("q_token", "q_head", "k_token", "k_head", "v_token", "v_head", "q_out_token", "q_out_head")] + \
+               [(name, C.c_void_p) for name in ("q_weight", "k_weight", "cos", "sin")] + \
+               [(name, C.c_uint32) for name in ("rope_rows", "rope_dim", "interleaved")] + [("eps", C.c_float)]
+
+
+class dm_plan(C.Structure):
+    _fields_ = [("seqs", C.c_void_p), ("offsets", C.c_void_p)] + \
+               [(name, C.c_uint32) for name in ("n", "tokens", "q_heads", "groups")] + \
+               [(name, C.c_void_p) for name in ("group_offsets", "group_prefix", "work")] + \
+               [("work_bytes", C.c_uint64)]
+
+
+class dm_attend_args(C.Structure):
+    _fields_ = [("layer", C.c_uint32), ("scale", C.c_float)] + \
+               [(name, C.c_void_p) for name in ("q", "o", "lse")] + \
+               [(name, C.c_uint64) for name in ("q_token", "q_head", "o_token", "o_head")]
+
+
 class DualMapError(RuntimeError):
     def __init__(self, status, where):
         self.status = status
@@ -136,6 +174,16 @@ SIGNATURES = {
     "dm_export_prefix_tree": (C.c_int, [C.c_void_p, C.c_void_p, C.c_uint64, C.POINTER(C.c_uint64)]),
     "dm_potc_max_loads": (C.c_int, [C.c_uint32, C.c_uint64, C.c_uint32, C.c_uint32, C.c_uint64, C.c_void_p,
                                     C.c_void_p]),
+    "dm_cache_work_bytes": (C.c_uint64, [C.POINTER(dm_cache)]),
+    "dm_cache_last_error": (C.c_int, [C.POINTER(dm_cache), C.c_void_p]),
+    "dm_cache_extend": (C.c_int, [C.POINTER(dm_cache), C.c_void_p, C.c_void_p, C.c_uint32, C.c_void_p]),
+    "dm_cache_fork": (C.c_int, [C.POINTER(dm_cache), C.c_void_p, C.c_void_p, C.c_void_p, C.c_uint32, C.c_void_p]),
+    "dm_cache_free": (C.c_int, [C.POINTER(dm_cache), C.c_void_p, C.c_uint32, C.c_void_p]),
+    "dm_cache_compact": (C.c_int, [C.POINTER(dm_cache), C.c_void_p, C.c_void_p, C.c_void_p, C.c_void_p]),
+    "dm_cache_append": (C.c_int, [C.POINTER(dm_cache), C.POINTER(dm_append_args), C.c_void_p]),
+    "dm_plan_bytes": (C.c_uint64, [C.POINTER(dm_cache), C.c_uint32, C.c_uint32, C.c_uint32, C.c_uint32]),
+    "dm_cache_plan": (C.c_int, [C.POINTER(dm_cache), C.POINTER(dm_plan), C.c_void_p]),
+    "dm_cache_attend": (C.c_int, [C.POINTER(dm_cache), C.POINTER(dm_plan), C.POINTER(dm_attend_args), C.c_void_p]),
     "dm_test_fail_alloc": (None, [C.c_int64]),
     "dm_last_error": (C.c_int, [C.c_void_p]),
     "dm_set_profiling": (C.c_int, [C.c_void_p, C.c_int]),
@@ -343,6 +391,46 @@ def dm_export_prefix_tree(h):
 
 def dm_potc_max_loads(n_bins, m_balls, d, trials, seed, max_load_dev, stream=None):
     return lib().dm_potc_max_loads(n_bins, m_balls, d, trials, seed, _ptr(max_load_dev), stream)
+
+
+def dm_cache_work_bytes(c):
+    return lib().dm_cache_work_bytes(C.byref(c))
+
+
+def dm_cache_last_error(c, stream=None):
+    return lib().dm_cache_last_error(C.byref(c), stream)
+
+
+def dm_cache_extend(c, seqs, add, n, stream=None):
+    return lib().dm_cache_extend(C.byref(c), _ptr(seqs), _ptr(add), n, stream)
+
+
+def dm_cache_fork(c, parents, children, length, n, stream=None):
+    return lib().dm_cache_fork(C.byref(c), _ptr(parents), _ptr(children), _ptr(length), n, stream)
+
+
+def dm_cache_free(c, seqs, n, stream=None):
+    return lib().dm_cache_free(C.byref(c), _ptr(seqs), n, stream)
+
+
+def dm_cache_compact(c, tables_out=None, refs_out=None, moved=None, stream=None):
+    return lib().dm_cache_compact(C.byref(c), _ptr(tables_out), _ptr(refs_out), _ptr(moved), stream)
+
+
+def dm_cache_append(c, args, stream=None):
+    return lib().dm_cache_append(C.byref(c), C.byref(args), stream)
+
+
+def dm_plan_bytes(c, n, groups, tokens, q_heads):
+    return lib().dm_plan_bytes(C.byref(c), n, groups, tokens, q_heads)
+
+
+def dm_cache_plan(c, plan, stream=None):
+    return lib().dm_cache_plan(C.byref(c), C.byref(plan), stream)
+
+
+def dm_cache_attend(c, plan, args, stream=None):
+    return lib().dm_cache_attend(C.byref(c), C.byref(plan), C.byref(args), stream)
 
 
 def dm_last_error(h):
