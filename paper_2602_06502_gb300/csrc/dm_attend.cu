@@ -225,7 +225,10 @@ constexpr uint32_t kSlotKeys = 32;
 template <int D>
 struct Narrow {
     static constexpr uint32_t kHalf = kSlotKeys * D * 2;            // bytes of a slot's keys, or values
-    static constexpr uint32_t kSlots = D == 128 ? 5 : 8;
+    // Even, so that a ring place always belongs to the same pair of warps: a
+    // pair that skipped a round could take the phase before it for its own.
+    static constexpr uint32_t kSlots = D == 128 ? 4 : 8;
+    static_assert(kSlots % 2 == 0, "each ring place has one pair of readers");
     static constexpr uint32_t kRed = kSlots * 2 * kHalf;            // 2 x 16 x D floats
     static constexpr uint32_t kMl = kRed + 2 * 16 * D * 4;          // 4 x 16 float2
     static constexpr uint32_t kBars = kMl + 4 * 16 * 8;             // full, empty per slot, then the give-up word
