@@ -161,24 +161,25 @@ __global__ void __cluster_dims__(kPlanCl, 1, 1) __launch_bounds__(kPlanT) k_plan
                         else hi = mid;
                     }
                     const uint32_t e = lo, rows = rows_of(e);
-                    k.row0 = (b - __ldcg(p.w.first[kind] + e)) * cap;
-                    k.rows = min(rows - k.row0, cap);
+                    const uint32_t row0 = (b - __ldcg(p.w.first[kind] + e)) * cap;
+                    k.rows = min(rows - row0, cap);
+                    k.lead = row0 % p.G;
                     if (e < p.groups) {
                         const int32_t i = p.group_offsets[e];
                         k.row = p.seqs[i];
-                        k.token0 = p.offsets[i];
+                        k.token = p.offsets[i] + (int32_t)(row0 / p.G);
                         k.kv1 = p.group_prefix[e];
-                        k.pos0 = 1 << 30;   // behind every key of the prefix
+                        k.pos = 1 << 30;   // behind every key of the prefix
                         k.shared = 1;
                     } else {
                         const uint32_t i = e - p.groups;
                         const int32_t g = __ldcg(p.w.group_of + i), used = p.offsets[i + 1] - p.offsets[i];
                         k.row = p.seqs[i];
-                        k.token0 = p.offsets[i];
+                        k.token = p.offsets[i] + (int32_t)(row0 / p.G);
                         k.shared = g >= 0;
                         k.kv0 = g >= 0 ? p.group_prefix[g] : 0;
-                        k.pos0 = p.lengths[k.row] - used;
-                        k.kv1 = max(k.kv0, k.pos0 + (int32_t)((k.row0 + k.rows - 1) / p.G) + 1);
+                        k.pos = p.lengths[k.row] - used + (int32_t)(row0 / p.G);
+                        k.kv1 = max(k.kv0, k.pos + (int32_t)((k.lead + k.rows - 1) / p.G) + 1);
                     }
                     k.units = max(1u, ((uint32_t)(k.kv1 - k.kv0) + keys - 1) / keys);
                 }
@@ -272,23 +273,33 @@ __global__ void __launch_bounds__(160, kNarrowPerSm)
     Walk<1> w(p);
     if (wid == 4) {
         uint32_t c = 0;   // slots so far
-        bool stop = false;
-        while (!stop && w.next(p)) {
-            const int32_t *table = p.tables + (uint64_t)w.k.row * p.max_blocks;
-            const uint32_t blocks = ((uint32_t)w.k.kv1 + p.B - 1) / p.B;
-            for (uint32_t j = 0; j < 2 * w.units; ++j, ++c) {
-                const uint32_t slot = c % N::kSlots, round = c / N::kSlots, at = s_at + slot * 2 * N::kHalf;
-                if (round) mbar_wait(empty(slot), (round - 1) & 1, gave_up, p.status);
-                if (__any_sync(~0u, *gave_up)) {
-                    stop = true;
-                    break;
-                }
-                if (lane == 0) mbar_expect(full(slot), 2 * N::kHalf);
-                __syncwarp();
-                const uint32_t tok = (uint32_t)w.k.kv0 + w.j0 * kNarrowKeys + j * kSlotKeys;
-                load_keys<D, kSlotKeys>(p, &mk, at, full(slot), table, tok, blocks, w.head);
-                load_keys<D, kSlotKeys>(p, &mv, at + N::kHalf, full(slot), table, tok, blocks, w.head);
-            }
+        KeyBoxes<D, kSlotKeys> boxes;
+        bool more = w.next(p);
+        const int32_t *table = nullptr;
+        uint32_t blocks = 0, tok = 0, left = 0, head = 0;   // the next slot; slots left of the piece
+        auto piece = [&] {
+            table = p.tables + (uint64_t)w.k.row * p.max_blocks;
+            blocks = ((uint32_t)w.k.kv1 + (1u << p.B_log) - 1) >> p.B_log;
+            tok = (uint32_t)w.k.kv0 + w.j0 * kNarrowKeys;
+            left = 2 * w.units;
+            head = w.head;
+        };
+        if (more) {
+            piece();
+            boxes.find(p, table, tok, blocks);
+        }
+        while (more) {
+            const uint32_t slot = c % N::kSlots, round = c / N::kSlots, at = s_at + slot * 2 * N::kHalf;
+            if (round) mbar_wait(empty(slot), (round - 1) & 1, gave_up, p.status);
+            if (__any_sync(~0u, *gave_up)) break;
+            if (lane == 0) mbar_expect(full(slot), 2 * N::kHalf);
+            __syncwarp();
+            boxes.load(p, &mk, at, full(slot), tok, head);
+            boxes.load(p, &mv, at + N::kHalf, full(slot), tok, head);
+            ++c;
+            tok += kSlotKeys;
+            if (--left == 0 && (more = w.next(p))) piece();
+            if (more) boxes.find(p, table, tok, blocks);
         }
         // no copy may be in flight when the CTA ends
         for (uint32_t i = c > N::kSlots ? c - N::kSlots : 0; i < c; ++i)
@@ -307,9 +318,9 @@ __global__ void __launch_bounds__(160, kNarrowPerSm)
         for (int r = 0; r < 2; ++r) {
             const uint32_t row = g + 8 * r;
             const bool on = row < w.k.rows;
-            limit[r] = on ? row_limit(w.k, row, p.G) : 0;
-            const uint32_t rr = w.k.row0 + (on ? row : 0);
-            const char *src = p.q + (uint64_t)(w.k.token0 + rr / p.G) * p.q_token + (uint64_t)(w.head * p.G + rr % p.G) * p.q_head;
+            const Row at = row_at(p, w.k, on ? row : 0);
+            limit[r] = on ? row_limit(w.k, at.token) : 0;
+            const char *src = p.q + (uint64_t)(w.k.token + at.token) * p.q_token + (uint64_t)(w.head * p.G + at.head) * p.q_head;
 #pragma unroll
             for (int kk = 0; kk < D / 16; ++kk) {
                 qf[kk][r] = on ? __ldg(reinterpret_cast<const uint32_t *>(src + kk * 32 + t4 * 4)) : 0;
@@ -448,9 +459,9 @@ __global__ void __launch_bounds__(160, kNarrowPerSm)
             for (int r = 0; r < 2; ++r) {
                 const uint32_t row = g + 8 * r;
                 if (row >= w.k.rows) continue;
-                const uint32_t rr = w.k.row0 + row;
-                const uint64_t tok = (uint64_t)(w.k.token0 + rr / p.G);
-                const uint32_t h = w.head * p.G + rr % p.G;
+                const Row at = row_at(p, w.k, row);
+                const uint64_t tok = (uint64_t)(w.k.token + at.token);
+                const uint32_t h = w.head * p.G + at.head;
                 if (whole) {
                     const float inv = L[r] > 0.f ? 1.f / L[r] : 0.f;
                     char *dst = p.o + tok * p.o_token + h * p.o_head;
@@ -581,6 +592,8 @@ cudaError_t launch_rest(const AttendArgs &p, const CUtensorMap &mk, const CUtens
     return cudaGetLastError();
 }
 
+uint32_t log2_of(uint32_t x) { return 31 - (uint32_t)__builtin_clz(x); }
+
 bool plan_ok(const dm_cache *c, const dm_plan *p, PlanShape &s, PlanWork &w) {
     if (!cache_ok(c) || !p || !plan_shape(c, p->n, p->groups, p->tokens, p->q_heads, s)) return false;
     if ((p->n && (!p->seqs || !p->offsets)) || (p->groups && (!p->group_offsets || !p->group_prefix))) return false;
@@ -622,14 +635,16 @@ extern "C" dm_status dm_cache_attend(const dm_cache *c, const dm_plan *pl, const
     p.tables = c->tables, p.status = c->status;
     p.q = static_cast<const char *>(a->q), p.o = static_cast<char *>(a->o), p.lse = a->lse;
     p.q_token = a->q_token * 2, p.q_head = a->q_head * 2, p.o_token = a->o_token * 2, p.o_head = a->o_head * 2;
-    p.max_blocks = c->max_blocks, p.pages = c->pages, p.B = c->page_tokens, p.box = std::min(c->page_tokens, kSlotKeys);
+    const uint32_t box = std::min(c->page_tokens, kSlotKeys);
+    p.max_blocks = c->max_blocks, p.pages = c->pages, p.B_log = log2_of(c->page_tokens), p.box_log = log2_of(box);
+    p.G_mul = (uint32_t)((0xFFFFFFFFull + s.G) / s.G);   // 2^32 / G, rounded up
     p.G = s.G, p.kv_heads = c->kv_heads, p.q_heads = s.q_heads, p.scale2 = a->scale * 1.44269504089f;
     p.ctas[0] = s.ctas[0], p.ctas[1] = s.ctas[1];
     p.offsets = pl->offsets, p.group_offsets = pl->group_offsets;
     p.n = pl->n, p.groups = pl->groups, p.tokens = pl->tokens;
     if (((uint64_t)p.tokens * p.q_heads + 7) / 8 > 0x7FFFFFFFull) return DM_ERR_INVALID_ARG;
     CUtensorMap mk, mv;
-    if (!page_map(&mk, c, c->k, a->layer, p.box) || !page_map(&mv, c, c->v, a->layer, p.box)) return DM_ERR_CUDA;
+    if (!page_map(&mk, c, c->k, a->layer, box) || !page_map(&mv, c, c->v, a->layer, box)) return DM_ERR_CUDA;
     const auto st = static_cast<cudaStream_t>(stream);
     cudaError_t e = launch_attend_wide(c, p, mk, mv, st);
     if (e == cudaSuccess) {

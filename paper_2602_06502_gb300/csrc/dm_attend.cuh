@@ -29,10 +29,10 @@ constexpr uint32_t kNarrowPerSm = 2;
 
 struct AttendBlock {
     int32_t row;          // of tables
-    int32_t token0;       // its sequence's or group's first query token
-    uint32_t row0, rows;  // its rows among them
+    int32_t token;        // query token of its first row
+    uint32_t lead, rows;  // that row's head within G; its rows
     int32_t kv0, kv1;     // keys; no row sees one from kv1 on
-    int32_t pos0;         // token0's position (a group's prefix: all rows see all keys)
+    int32_t pos;          // the first token's position (a group's prefix: all rows see all keys)
     uint32_t units;       // per key head, >= 1
     uint32_t part0;       // shared: its first row in the parts
     uint32_t shared;
@@ -67,6 +67,7 @@ inline bool plan_shape(const dm_cache *c, uint32_t n, uint32_t groups, uint32_t 
     if (!cache_shape_ok(c) || q_heads == 0 || q_heads % c->kv_heads || q_heads > 65535u * 32) return false;
     if (n > c->max_seqs || groups > n || tokens > 0x7FFFFFFFu) return false;
     s.n = n, s.groups = groups, s.tokens = tokens, s.q_heads = q_heads;
+    if (q_heads / c->kv_heads > 32768) return false;   // row_at's division
     s.G = q_heads / c->kv_heads, s.D = c->head_dim, s.sms = (uint32_t)sm_count();
     s.ctas[0] = s.sms, s.ctas[1] = s.sms * kNarrowPerSm;
     const uint32_t cap[2] = {kWideRows, kNarrowRows};
@@ -119,7 +120,8 @@ struct AttendArgs {
     char *o;
     float *lse;
     uint64_t q_token, q_head, o_token, o_head;   // bytes
-    uint32_t max_blocks, pages, B, box, G, kv_heads, q_heads;   // box: rows of a TMA box
+    uint32_t max_blocks, pages, G, G_mul, kv_heads, q_heads;   // x / G = x * G_mul >> 32 for x <= G + 256
+    uint32_t B_log, box_log;                     // log2 of a page's tokens and of a TMA box's
     float scale2;                                // scale * log2(e)
     uint32_t ctas[2];
     const int32_t *offsets, *group_offsets;
@@ -183,9 +185,17 @@ struct Walk {
     }
 };
 
-// One past the last key that row r of a block sees.
-__device__ __forceinline__ int32_t row_limit(const AttendBlock &k, uint32_t r, uint32_t G) {
-    return min(k.kv1, k.pos0 + (int32_t)((k.row0 + r) / G) + 1);
+// Row r of a block: its token, counted from the block's first, and its head.
+struct Row {
+    uint32_t token, head;
+};
+__device__ __forceinline__ Row row_at(const AttendArgs &p, const AttendBlock &k, uint32_t r) {
+    const uint32_t x = k.lead + r, t = p.G == 1 ? x : __umulhi(x, p.G_mul);
+    return {t, x - t * p.G};
+}
+// One past the last key that a token of a block sees.
+__device__ __forceinline__ int32_t row_limit(const AttendBlock &k, uint32_t token) {
+    return min(k.kv1, k.pos + (int32_t)token + 1);
 }
 
 __device__ __forceinline__ uint32_t smem_addr(const void *p) { return (uint32_t)__cvta_generic_to_shared(p); }
@@ -254,21 +264,36 @@ __device__ __forceinline__ void tma_load4(uint32_t dst, const CUtensorMap *map, 
         : "memory");
 }
 
-// Key rows tok0 .. tok0 + keys of a sequence into shared memory, as D / 64
-// halves of 128-byte rows (128-byte swizzle); pages behind block `blocks` and
-// ids out of range give zeros.  Called by a whole warp.
+// Key rows tok .. tok + keys of a sequence into shared memory, as D / 64 halves
+// of 128-byte rows (128-byte swizzle): TMA boxes of up to a page, shared out to
+// the lanes of a warp.  A page that does not exist (a block from `blocks` on,
+// an id out of range) reads as zeros.  find() loads the ids some time before
+// load() needs them.
 template <int D, int kKeys>
-__device__ __forceinline__ void load_keys(const AttendArgs &p, const CUtensorMap *map, uint32_t dst, uint32_t bar, const int32_t *table,
-                                          uint32_t tok0, uint32_t blocks, uint32_t head) {
-    constexpr uint32_t kHalves = D / 64;
-    const uint32_t boxes = kKeys / p.box * kHalves;
-    for (uint32_t x = threadIdx.x & 31; x < boxes; x += 32) {
-        const uint32_t half = x % kHalves, at = x / kHalves * p.box, blk = (tok0 + at) / p.B;
-        uint32_t page = blk < blocks ? (uint32_t)__ldg(table + blk) : p.pages;
-        page = min(page, p.pages);   // a page that does not exist reads as zeros
-        tma_load4(dst + half * kKeys * 128 + at * 128, map, bar, (int)half * 64, (int)((tok0 + at) % p.B), (int)head, (int)page);
+struct KeyBoxes {
+    static constexpr uint32_t kHalves = D / 64, kEach = (kKeys / 4 * kHalves + 31) / 32;   // boxes a lane, with 4-token pages
+    uint32_t page[kEach];
+
+    __device__ __forceinline__ void find(const AttendArgs &p, const int32_t *table, uint32_t tok, uint32_t blocks) {
+        const uint32_t boxes = kKeys * kHalves >> p.box_log, lane = threadIdx.x & 31;
+#pragma unroll
+        for (uint32_t i = 0; i < kEach; ++i) {
+            const uint32_t x = lane + 32 * i, blk = (tok + (x / kHalves << p.box_log)) >> p.B_log;
+            page[i] = x < boxes && blk < blocks ? min((uint32_t)__ldg(table + blk), p.pages) : p.pages;
+        }
     }
-}
+    __device__ __forceinline__ void load(const AttendArgs &p, const CUtensorMap *map, uint32_t dst, uint32_t bar, uint32_t tok,
+                                         uint32_t head) const {
+        const uint32_t boxes = kKeys * kHalves >> p.box_log, lane = threadIdx.x & 31;
+#pragma unroll
+        for (uint32_t i = 0; i < kEach; ++i) {
+            const uint32_t x = lane + 32 * i, half = x % kHalves, at = x / kHalves << p.box_log;
+            if (x < boxes)
+                tma_load4(dst + half * kKeys * 128 + at * 128, map, bar, (int)half * 64, (int)((tok + at) & ((1u << p.B_log) - 1)),
+                          (int)head, (int)page[i]);
+        }
+    }
+};
 
 template <class T>
 struct Pack2;

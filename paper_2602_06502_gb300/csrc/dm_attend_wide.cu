@@ -26,7 +26,7 @@
 namespace dm {
 namespace {
 
-constexpr uint32_t kWideT = 320;
+constexpr uint32_t kWideT = 384;   // three warpgroups: softmax of A, of B, and the issuing warps
 
 template <int D>
 struct Wide {
@@ -34,8 +34,8 @@ struct Wide {
     static constexpr uint32_t kStages = D == 128 ? 5 : 10;
     static constexpr uint32_t kRing = 2 * kTile;                    // after Q of A and B
     static constexpr uint32_t kBars = kRing + kStages * kTile;
-    // full, empty per stage; then per tile: q, s, p, o; then done
-    static constexpr uint32_t kWord = kBars + 16 * kStages + 8 * 9; // give-up word, tensor memory address
+    // full, empty per stage; then per tile: q, s, p (two halves), o; then done
+    static constexpr uint32_t kWord = kBars + 16 * kStages + 8 * 11; // give-up word, tensor memory address
     static constexpr uint32_t kBytes = kWord + 16 + 1024;
     static constexpr uint32_t kS = 0, kO = 256;                     // tensor memory columns: S of A, B; O of A, B
 };
@@ -68,6 +68,32 @@ __device__ __forceinline__ void fence_before() { asm volatile("tcgen05.fence::be
 __device__ __forceinline__ void fence_after() { asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory"); }
 __device__ __forceinline__ void wait_st() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
 __device__ __forceinline__ void fence_async() { asm volatile("fence.proxy.async.shared::cta;" ::: "memory"); }
+
+// True in one thread of the warp.
+__device__ __forceinline__ bool elect() {
+    uint32_t one;
+    asm volatile("{\n\t.reg .pred p;\n\telect.sync _|p, 0xFFFFFFFF;\n\tselp.u32 %0, 1, 0, p;\n\t}" : "=r"(one));
+    return one != 0;
+}
+
+// Two 32-bit operations in one instruction.
+__device__ __forceinline__ float2 fma2(float2 a, float2 b, float2 c) {
+    float2 d;
+    asm("{\n\t.reg .b64 x, y, z;\n\t"
+        "mov.b64 x, {%2, %3};\n\tmov.b64 y, {%4, %5};\n\tmov.b64 z, {%6, %7};\n\t"
+        "fma.rn.f32x2 x, x, y, z;\n\tmov.b64 {%0, %1}, x;\n\t}"
+        : "=f"(d.x), "=f"(d.y)
+        : "f"(a.x), "f"(a.y), "f"(b.x), "f"(b.y), "f"(c.x), "f"(c.y));
+    return d;
+}
+__device__ __forceinline__ float2 add2(float2 a, float2 b) {
+    float2 d;
+    asm("{\n\t.reg .b64 x, y;\n\tmov.b64 x, {%2, %3};\n\tmov.b64 y, {%4, %5};\n\t"
+        "add.rn.f32x2 x, x, y;\n\tmov.b64 {%0, %1}, x;\n\t}"
+        : "=f"(d.x), "=f"(d.y)
+        : "f"(a.x), "f"(a.y), "f"(b.x), "f"(b.y));
+    return d;
+}
 
 // 32 columns of this warp's 32 lanes.
 __device__ __forceinline__ void tm_ld(uint32_t *r, uint32_t at) {
@@ -106,6 +132,18 @@ __device__ __forceinline__ void wait_ld(uint32_t *r, uint32_t n = 32) {
     for (uint32_t i = 0; i < n; i += 32) tm_use(r + i);
 }
 
+// 64 scores of this thread's row; minus infinity from the `seen`-th on.
+__device__ __forceinline__ void scores64(uint32_t *raw, uint32_t at, int32_t seen) {
+    tm_ld(raw, at);
+    tm_ld(raw + 32, at + 32);
+    wait_ld(raw, 64);
+    if (seen < 64)
+#pragma unroll
+        for (int32_t i = 0; i < 64; ++i)
+            if (i >= seen) raw[i] = 0xFF800000u;
+    __syncwarp();
+}
+
 template <class T, int D>
 __global__ void __launch_bounds__(kWideT, 1)
     k_attend_wide(const __grid_constant__ CUtensorMap mk, const __grid_constant__ CUtensorMap mv, AttendArgs p) {
@@ -114,14 +152,14 @@ __global__ void __launch_bounds__(kWideT, 1)
     char *s = reinterpret_cast<char *>(align_up(reinterpret_cast<uint64_t>(s_raw), 1024));
     const uint32_t s_at = smem_addr(s), bars = s_at + W::kBars, more = bars + 16 * W::kStages;
     volatile uint32_t *gave_up = reinterpret_cast<uint32_t *>(s + W::kWord);
-    const uint32_t tid = threadIdx.x, wid = tid >> 5, lane = tid & 31;
+    const uint32_t tid = threadIdx.x, wid = __shfl_sync(~0u, tid >> 5, 0), lane = tid & 31;
     auto full = [&](uint32_t i) { return bars + 16 * i; };
     auto empty = [&](uint32_t i) { return bars + 16 * i + 8; };
     auto q_full = [&](uint32_t x) { return more + 8 * x; };
     auto s_full = [&](uint32_t x) { return more + 16 + 8 * x; };
-    auto p_full = [&](uint32_t x) { return more + 32 + 8 * x; };
-    auto o_full = [&](uint32_t x) { return more + 48 + 8 * x; };
-    const uint32_t done = more + 64;
+    auto p_full = [&](uint32_t x, uint32_t half) { return more + 32 + 16 * x + 8 * half; };
+    auto o_full = [&](uint32_t x) { return more + 64 + 8 * x; };
+    const uint32_t done = more + 80;
     if (__syncthreads_or(has_err(p.status) || !p.w.head->ok || p.w.head->units[0] == 0)) return;
     if (tid == 0) {
         for (uint32_t i = 0; i < W::kStages; ++i) {
@@ -131,7 +169,8 @@ __global__ void __launch_bounds__(kWideT, 1)
         for (uint32_t x = 0; x < 2; ++x) {
             mbar_init(q_full(x), 128);
             mbar_init(s_full(x), 1);
-            mbar_init(p_full(x), 128);
+            mbar_init(p_full(x, 0), 128);
+            mbar_init(p_full(x, 1), 128);
             mbar_init(o_full(x), 1);
         }
         mbar_init(done, 1);
@@ -148,153 +187,193 @@ __global__ void __launch_bounds__(kWideT, 1)
     const uint32_t tmem = *reinterpret_cast<volatile uint32_t *>(s + W::kWord + 4);
     Walk<0> w(p);
 
-    if (wid == 8) {
-        uint32_t c = 0;   // stages so far: K of unit 0, V of unit 0, K of unit 1, ...
-        bool stop = false;
-        while (!stop && w.next(p)) {
-            const int32_t *table = p.tables + (uint64_t)w.k.row * p.max_blocks;
-            const uint32_t blocks = ((uint32_t)w.k.kv1 + p.B - 1) / p.B;
-            for (uint32_t j = 0; j < 2 * w.units; ++j, ++c) {
-                const uint32_t i = c % W::kStages, round = c / W::kStages;
-                if (round) mbar_wait(empty(i), (round - 1) & 1, gave_up, p.status);
-                if (__any_sync(~0u, *gave_up)) {
-                    stop = true;
-                    break;
-                }
-                if (lane == 0) mbar_expect(full(i), W::kTile);
-                __syncwarp();
-                load_keys<D, kWideKeys>(p, j & 1 ? &mv : &mk, s_at + W::kRing + i * W::kTile, full(i), table,
-                                        (uint32_t)w.k.kv0 + (w.j0 + j / 2) * kWideKeys, blocks, w.head);
+    // 384 x 168 registers at the start; 2 x 128 x 208 + 128 x 88 are as many
+    if (wid >= 8) {
+        asm volatile("setmaxnreg.dec.sync.aligned.u32 88;");
+        if (wid == 8) {
+            uint32_t c = 0;   // stages so far: K of unit 0, V of unit 0, K of unit 1, ...
+            KeyBoxes<D, kWideKeys> boxes;
+            bool stop = false, more = w.next(p);
+            const int32_t *table = nullptr;
+            uint32_t blocks = 0, tok = 0, left = 0, head = 0;   // the next unit; units left of the piece
+            auto piece = [&] {
+                table = p.tables + (uint64_t)w.k.row * p.max_blocks;
+                blocks = ((uint32_t)w.k.kv1 + (1u << p.B_log) - 1) >> p.B_log;
+                tok = (uint32_t)w.k.kv0 + w.j0 * kWideKeys;
+                left = w.units;
+                head = w.head;
+            };
+            if (more) {
+                piece();
+                boxes.find(p, table, tok, blocks);
             }
-        }
-        // no copy may be in flight when the CTA ends
-        for (uint32_t i = c > W::kStages ? c - W::kStages : 0; i < c; ++i)
-            mbar_drain(full(i % W::kStages), (i / W::kStages) & 1);
-    } else if (wid == 9) {
-        constexpr uint32_t kType = Pack2<T>::kMmaType;
-        // f32 accumulators, the operands' type, N, M = 128; V's rows (dims) are contiguous
-        constexpr uint32_t desc_s = 1u << 4 | kType << 7 | kType << 10 | (kWideKeys / 8) << 17 | 8u << 24;
-        constexpr uint32_t desc_o = 1u << 4 | kType << 7 | kType << 10 | 1u << 16 | (D / 8) << 17 | 8u << 24;
-        auto scores = [&](uint32_t x, uint32_t stage) {   // S_x = Q_x K^T
-            const uint32_t qa = s_at + x * W::kTile, ka = s_at + W::kRing + stage * W::kTile;
-            if (lane == 0 && !*gave_up) {
-#pragma unroll
-                for (uint32_t kk = 0; kk < D / 16; ++kk) {
-                    const uint32_t at = kk / 4 * 16384 + kk % 4 * 32;
-                    mma_ss(tmem + W::kS + x * 128, operand(qa + at, 16), operand(ka + at, 16), desc_s, kk > 0);
-                }
-                mma_commit(s_full(x));
-            }
-            __syncwarp();
-        };
-        auto product = [&](uint32_t x, uint32_t stage, bool first) {   // O_x += P_x V
-            const uint32_t va = s_at + W::kRing + stage * W::kTile;
-            if (lane == 0 && !*gave_up) {
-#pragma unroll
-                for (uint32_t kk = 0; kk < kWideKeys / 16; ++kk)
-                    mma_ts(tmem + W::kO + x * D, tmem + W::kS + x * 128 + kk * 8, operand(va + kk * 2048, 16384), desc_o, !first || kk > 0);
-            }
-            __syncwarp();
-        };
-        auto release = [&](uint32_t bar) {
-            if (lane == 0 && !*gave_up) mma_commit(bar);
-            __syncwarp();
-        };
-        uint32_t c = 0, pieces[2] = {0, 0}, ps[2] = {0, 0};   // stages; pieces and weight tiles of A and B
-        while (w.next(p)) {
-            const uint32_t X = w.k.rows > 128 ? 2 : 1;
-            for (uint32_t x = 0; x < X; ++x) mbar_wait(q_full(x), pieces[x] & 1, gave_up, p.status);
-            mbar_wait(full(c % W::kStages), (c / W::kStages) & 1, gave_up, p.status);
-            fence_after();
-            for (uint32_t x = 0; x < X; ++x) scores(x, c % W::kStages);
-            release(empty(c % W::kStages));
-            for (uint32_t j = 0; j < w.units; ++j) {
-                const uint32_t v = c + 1, vs = v % W::kStages, nk = c + 2, ns = nk % W::kStages;
-                const bool last = j + 1 == w.units;
-                mbar_wait(full(vs), (v / W::kStages) & 1, gave_up, p.status);
-                const int32_t left = w.k.kv1 - (w.k.kv0 + (int32_t)((w.j0 + j) * kWideKeys));
-                if (left > 0 && left < (int32_t)kWideKeys && left % (int32_t)p.B) {
-                    // slots of the last page behind the end hold whatever was
-                    // there; a weight of zero does not silence an infinity
-                    const uint32_t to = align_up((uint32_t)left, p.B), chunks = (to - left) * (D / 8);
-                    for (uint32_t e = lane; e < chunks; e += 32) {
-                        const uint32_t row = left + e / (D / 8), ch = e % (D / 8);
-                        *reinterpret_cast<uint4 *>(s + W::kRing + vs * W::kTile + ch / 8 * 16384 + row * 128 + ((ch % 8) ^ (row % 8)) * 16) =
-                            make_uint4(0, 0, 0, 0);
-                    }
-                    fence_async();
+            while (more && !stop) {
+                for (uint32_t v = 0; v < 2; ++v, ++c) {
+                    const uint32_t i = c % W::kStages, round = c / W::kStages;
+                    if (round) mbar_wait(empty(i), (round - 1) & 1, gave_up, p.status);
+                    if ((stop = __any_sync(~0u, *gave_up))) break;
+                    if (lane == 0) mbar_expect(full(i), W::kTile);
                     __syncwarp();
+                    boxes.load(p, v ? &mv : &mk, s_at + W::kRing + i * W::kTile, full(i), tok, head);
                 }
-                for (uint32_t x = 0; x < X; ++x) {
-                    mbar_wait(p_full(x), ps[x] & 1, gave_up, p.status);
-                    ++ps[x];
-                    fence_after();
-                    product(x, vs, j == 0);
-                    if (last) {
-                        release(o_full(x));
-                    } else {
-                        if (x == 0) mbar_wait(full(ns), (nk / W::kStages) & 1, gave_up, p.status);
-                        fence_after();
-                        scores(x, ns);
-                    }
-                }
-                release(empty(vs));
-                if (!last) release(empty(ns));
-                c += 2;
+                tok += kWideKeys;
+                if (--left == 0 && (more = w.next(p))) piece();
+                if (more) boxes.find(p, table, tok, blocks);
             }
-            for (uint32_t x = 0; x < X; ++x) ++pieces[x];
+            // no copy may be in flight when the CTA ends
+            for (uint32_t i = c > W::kStages ? c - W::kStages : 0; i < c; ++i)
+                mbar_drain(full(i % W::kStages), (i / W::kStages) & 1);
+        } else if (wid == 9) {
+            constexpr uint32_t kType = Pack2<T>::kMmaType;
+            // f32 accumulators, the operands' type, N, M = 128; V's rows (dims) are contiguous
+            constexpr uint32_t desc_s = 1u << 4 | kType << 7 | kType << 10 | (kWideKeys / 8) << 17 | 8u << 24;
+            constexpr uint32_t desc_o = 1u << 4 | kType << 7 | kType << 10 | 1u << 16 | (D / 8) << 17 | 8u << 24;
+            // The tensor cores' operands are in uniform registers: one thread
+            // elected by the whole warp issues, and what it issues is the same
+            // in every lane, so that no value has to be moved there first.
+            const bool one = elect();
+            const uint32_t tm = __shfl_sync(~0u, tmem, 0);
+            const uint64_t q_op = operand(s_at, 16), k_op = operand(s_at + W::kRing, 16), v_op = operand(s_at + W::kRing, 16384);
+            auto scores = [&](uint32_t x, uint32_t stage) {   // S_x = Q_x K^T
+                const uint64_t qa = q_op + x * (W::kTile >> 4), ka = k_op + stage * (W::kTile >> 4);
+                if (one) {
+#pragma unroll
+                    for (uint32_t kk = 0; kk < D / 16; ++kk) {
+                        const uint32_t at = (kk / 4 * 16384 + kk % 4 * 32) >> 4;
+                        mma_ss(tm + W::kS + x * 128, qa + at, ka + at, desc_s, kk > 0);
+                    }
+                    mma_commit(s_full(x));
+                }
+                __syncwarp();
+            };
+            auto product = [&](uint32_t x, uint32_t stage, uint32_t half, bool first) {   // O_x += P_x V, over half the keys
+                const uint64_t va = v_op + stage * (W::kTile >> 4) + half * 512;
+                if (one) {
+#pragma unroll
+                    for (uint32_t kk = 0; kk < 4; ++kk)
+                        mma_ts(tm + W::kO + x * D, tm + W::kS + x * 128 + half * 32 + kk * 8, va + kk * 128, desc_o, !first || half || kk > 0);
+                }
+                __syncwarp();
+            };
+            auto release = [&](uint32_t bar) {
+                if (one) mma_commit(bar);
+                __syncwarp();
+            };
+            uint32_t c = 0, pieces[2] = {0, 0}, ps[2] = {0, 0};   // stages; pieces and weight tiles of A and B
+            while (w.next(p)) {
+                const uint32_t X = w.k.rows > 128 ? 2 : 1;
+                for (uint32_t x = 0; x < X; ++x) mbar_wait(q_full(x), pieces[x] & 1, gave_up, p.status);
+                mbar_wait(full(c % W::kStages), (c / W::kStages) & 1, gave_up, p.status);
+                fence_after();
+                for (uint32_t x = 0; x < X; ++x) scores(x, c % W::kStages);
+                release(empty(c % W::kStages));
+                for (uint32_t j = 0; j < w.units; ++j) {
+                    const uint32_t v = c + 1, vs = v % W::kStages, nk = c + 2, ns = nk % W::kStages;
+                    const bool last = j + 1 == w.units;
+                    mbar_wait(full(vs), (v / W::kStages) & 1, gave_up, p.status);
+                    const int32_t left = w.k.kv1 - (w.k.kv0 + (int32_t)((w.j0 + j) * kWideKeys));
+                    if (left > 0 && left < (int32_t)kWideKeys && (left & ((1 << p.B_log) - 1))) {
+                        // slots of the last page behind the end hold whatever was
+                        // there; a weight of zero does not silence an infinity
+                        const uint32_t to = (uint32_t)align_up(left, 1u << p.B_log), chunks = (to - left) * (D / 8);
+                        for (uint32_t e = lane; e < chunks; e += 32) {
+                            const uint32_t row = left + e / (D / 8), ch = e % (D / 8);
+                            *reinterpret_cast<uint4 *>(s + W::kRing + vs * W::kTile + ch / 8 * 16384 + row * 128 + ((ch % 8) ^ (row % 8)) * 16) =
+                                make_uint4(0, 0, 0, 0);
+                        }
+                        fence_async();
+                        __syncwarp();
+                    }
+                    for (uint32_t x = 0; x < X; ++x) {
+                        for (uint32_t half = 0; half < 2; ++half) {
+                            mbar_wait(p_full(x, half), ps[x] & 1, gave_up, p.status);
+                            fence_after();
+                            product(x, vs, half, j == 0);
+                        }
+                        ++ps[x];
+                        if (last) {
+                            release(o_full(x));
+                        } else {
+                            if (x == 0) mbar_wait(full(ns), (nk / W::kStages) & 1, gave_up, p.status);
+                            fence_after();
+                            scores(x, ns);
+                        }
+                    }
+                    release(empty(vs));
+                    if (!last) release(empty(ns));
+                    c += 2;
+                }
+                for (uint32_t x = 0; x < X; ++x) ++pieces[x];
+            }
+            // nothing may be in flight when tensor memory is given back
+            release(done);
+            mbar_drain(done, 0);
         }
-        // nothing may be in flight when tensor memory is given back
-        if (lane == 0) mma_commit(done);
-        __syncwarp();
-        mbar_drain(done, 0);
     } else {
+        asm volatile("setmaxnreg.inc.sync.aligned.u32 208;");
         const uint32_t x = wid >> 2, r = tid & 127;   // tile, row (= tensor memory lane)
         const uint32_t lanes = (wid & 3) << 21;       // this warp's lanes of tensor memory
         const uint32_t t_s = tmem + W::kS + x * 128 + lanes, t_o = tmem + W::kO + x * D + lanes;
         uint32_t ss = 0, pieces = 0;
-        while (w.next(p)) {
-            if (w.k.rows <= 128 * x) continue;
-            const uint32_t rows = min(128u, w.k.rows - 128 * x);
-            // Q of this tile: 16 bytes a thread and step, zeros for the rows that are not there
-#pragma unroll
-            for (uint32_t it = 0; it < D / 8; ++it) {
-                const uint32_t e = it * 128 + r, row = e / (D / 8), ch = e % (D / 8);
-                uint4 v = make_uint4(0, 0, 0, 0);
-                if (row < rows) {
-                    const uint32_t rr = w.k.row0 + 128 * x + row;
-                    v = __ldg(reinterpret_cast<const uint4 *>(p.q + (uint64_t)(w.k.token0 + rr / p.G) * p.q_token +
-                                                              (uint64_t)(w.head * p.G + rr % p.G) * p.q_head + ch * 16));
-                }
-                *reinterpret_cast<uint4 *>(s + x * W::kTile + ch / 8 * 16384 + row * 128 + ((ch % 8) ^ (row % 8)) * 16) = v;
+        // The next piece that has rows in this tile.
+        auto next = [&](Walk<0> &k) {
+            while (k.next(p))
+                if (k.k.rows > 128 * x) return true;
+            return false;
+        };
+        // A piece's Q, 16 bytes a thread and step, zeros for the rows that are
+        // not there.  Begun when the last scores of the piece before are done,
+        // so that the next piece's first product need not wait for it.
+        auto fetch = [&](const Walk<0> &k) {
+            const uint32_t rows = min(128u, k.k.rows - 128 * x), ch = r % (D / 8);
+#pragma unroll 4
+            for (uint32_t row = r / (D / 8); row < 128; row += 1024 / D) {
+                const Row at = row_at(p, k.k, 128 * x + min(row, rows - 1));
+                const char *src = p.q + (uint64_t)(k.k.token + at.token) * p.q_token + (uint64_t)(k.head * p.G + at.head) * p.q_head + ch * 16;
+                asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(s_at + x * W::kTile + ch / 8 * 16384 + row * 128 + ((ch % 8) ^ (row % 8)) * 16),
+                             "l"(src), "r"(row < rows ? 16 : 0)
+                             : "memory");
             }
+        };
+        auto fetched = [&] {
+            asm volatile("cp.async.wait_all;" ::: "memory");
             fence_async();
-            fence_before();   // the last piece's O has been read
             mbar_arrive(q_full(x));
-            const int32_t limit = r < rows ? row_limit(w.k, 128 * x + r, p.G) : 0;
+        };
+        bool more = next(w);
+        if (more) {
+            fetch(w);
+            fetched();
+        }
+        while (more) {
+            const uint32_t rows = min(128u, w.k.rows - 128 * x);
+            const Row mine = row_at(p, w.k, 128 * x + min(r, rows - 1));
+            const int32_t limit = r < rows ? row_limit(w.k, mine.token) : 0;
+            Walk<0> ahead = w;
+            more = next(ahead);
             float m = -INFINITY, l = 0.f;   // the maximum in the scores' own unit
             for (uint32_t j = 0; j < w.units; ++j, ++ss) {
                 mbar_wait(s_full(x), ss & 1, gave_up, p.status);
                 fence_after();
-                uint32_t raw[128];
-#pragma unroll
-                for (uint32_t q = 0; q < 4; ++q) tm_ld(raw + 32 * q, t_s + 32 * q);
-                wait_ld(raw, 128);
-                float *sc = reinterpret_cast<float *>(raw);
+                if (j + 1 == w.units && more) fetch(ahead);
                 const int32_t seen = limit - (w.k.kv0 + (int32_t)((w.j0 + j) * kWideKeys));
-                if (seen < (int32_t)kWideKeys)
+                // 64 scores at a time: the maximum over the second half, then
+                // over the first, which stays in registers
+                uint32_t raw[64];
+                float top = -INFINITY;
 #pragma unroll
-                    for (int32_t i = 0; i < (int32_t)kWideKeys; ++i)
-                        if (i >= seen) sc[i] = -INFINITY;
-                float m0 = sc[0], m1 = sc[1], m2 = sc[2], m3 = sc[3];
+                for (uint32_t half = 2; half-- > 0;) {
+                    scores64(raw, t_s + 64 * half, seen - 64 * (int32_t)half);
+                    float m0 = top, m1 = -INFINITY, m2 = -INFINITY, m3 = -INFINITY;
 #pragma unroll
-                for (uint32_t i = 4; i < kWideKeys; i += 4) {
-                    m0 = fmaxf(m0, sc[i]);
-                    m1 = fmaxf(m1, sc[i + 1]);
-                    m2 = fmaxf(m2, sc[i + 2]);
-                    m3 = fmaxf(m3, sc[i + 3]);
+                    for (uint32_t i = 0; i < 64; i += 8) {
+                        m0 = fmaxf(fmaxf(m0, __uint_as_float(raw[i])), __uint_as_float(raw[i + 1]));
+                        m1 = fmaxf(fmaxf(m1, __uint_as_float(raw[i + 2])), __uint_as_float(raw[i + 3]));
+                        m2 = fmaxf(fmaxf(m2, __uint_as_float(raw[i + 4])), __uint_as_float(raw[i + 5]));
+                        m3 = fmaxf(fmaxf(m3, __uint_as_float(raw[i + 6])), __uint_as_float(raw[i + 7]));
+                    }
+                    top = fmaxf(fmaxf(m0, m1), fmaxf(m2, m3));
                 }
-                const float top = fmaxf(fmaxf(m0, m1), fmaxf(m2, m3));
                 float f = 1.f;
                 if ((top - m) * p.scale2 > 8.f) {
                     f = exp2_((m - top) * p.scale2);   // 0 for the first that the row sees
@@ -315,33 +394,38 @@ __global__ void __launch_bounds__(kWideT, 1)
                     }
                 }
                 const float base = m == -INFINITY ? 0.f : m * p.scale2;
-                float l0 = 0.f, l1 = 0.f, l2 = 0.f, l3 = 0.f;
+                const float2 scale2 = make_float2(p.scale2, p.scale2), minus = make_float2(-base, -base);
+                float2 la = make_float2(0.f, 0.f), lb = la;
+                // the weights in the cache's type, as the tensor cores take
+                // them; the product over the first half of the keys begins
+                // while the second half is computed
 #pragma unroll
-                for (uint32_t i = 0; i < kWideKeys; i += 4) {
-                    const float a = exp2_(fmaf(sc[i], p.scale2, -base)), b = exp2_(fmaf(sc[i + 1], p.scale2, -base));
-                    const float d = exp2_(fmaf(sc[i + 2], p.scale2, -base)), e = exp2_(fmaf(sc[i + 3], p.scale2, -base));
-                    l0 += a;
-                    l1 += b;
-                    l2 += d;
-                    l3 += e;
-                    // the weights in the cache's type, as the tensor cores take them
-                    raw[i / 2] = Pack2<T>::pack(a, b);
-                    raw[i / 2 + 1] = Pack2<T>::pack(d, e);
+                for (uint32_t half = 0; half < 2; ++half) {
+                    if (half) scores64(raw, t_s + 64, seen - 64);
+#pragma unroll
+                    for (uint32_t i = 0; i < 64; i += 4) {
+                        const float2 a = fma2(make_float2(__uint_as_float(raw[i]), __uint_as_float(raw[i + 1])), scale2, minus);
+                        const float2 b = fma2(make_float2(__uint_as_float(raw[i + 2]), __uint_as_float(raw[i + 3])), scale2, minus);
+                        const float2 ea = make_float2(exp2_(a.x), exp2_(a.y)), eb = make_float2(exp2_(b.x), exp2_(b.y));
+                        la = add2(la, ea);
+                        lb = add2(lb, eb);
+                        raw[i / 2] = Pack2<T>::pack(ea.x, ea.y);
+                        raw[i / 2 + 1] = Pack2<T>::pack(eb.x, eb.y);
+                    }
+                    tm_st(t_s + 32 * half, raw);
+                    wait_st();
+                    fence_before();
+                    mbar_arrive(p_full(x, half));
                 }
-                l += (l0 + l1) + (l2 + l3);
-                tm_st(t_s, raw);
-                tm_st(t_s + 32, raw + 32);
-                wait_st();
-                fence_before();
-                mbar_arrive(p_full(x));
+                l += (la.x + la.y) + (lb.x + lb.y);
             }
+            if (more) fetched();
             mbar_wait(o_full(x), pieces & 1, gave_up, p.status);
             ++pieces;
             fence_after();
             const bool whole = w.whole(), on = r < rows;
-            const uint32_t rr = w.k.row0 + 128 * x + (on ? r : 0);
-            const uint64_t tok = (uint64_t)(w.k.token0 + rr / p.G);
-            const uint32_t h = w.head * p.G + rr % p.G;
+            const uint64_t tok = (uint64_t)(w.k.token + mine.token);
+            const uint32_t h = w.head * p.G + mine.head;
             const uint64_t part = whole ? 0 : w.part_row(p) + 128 * x + r;
             const float inv = l > 0.f ? 1.f / l : 0.f;
             char *dst = p.o + tok * p.o_token + h * p.o_head;
@@ -373,6 +457,8 @@ __global__ void __launch_bounds__(kWideT, 1)
                 else if (p.lse) p.lse[tok * p.q_heads + h] = l > 0.f ? (m2 + log2f(l)) * 0.69314718056f : -INFINITY;
             }
             __syncwarp();
+            fence_before();   // O has been read; the next product may write it
+            w = ahead;
         }
     }
     fence_before();
