@@ -273,7 +273,7 @@ __global__ void __launch_bounds__(160, kNarrowPerSm)
     Walk<1> w(p);
     if (wid == 4) {
         uint32_t c = 0;   // slots so far
-        KeyBoxes<D, kSlotKeys> boxes;
+        KeyBoxes<D, kSlotKeys, 1> boxes(0);
         bool more = w.next(p);
         const int32_t *table = nullptr;
         uint32_t blocks = 0, tok = 0, left = 0, head = 0;   // the next slot; slots left of the piece

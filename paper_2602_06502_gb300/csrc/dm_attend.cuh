@@ -266,28 +266,32 @@ __device__ __forceinline__ void tma_load4(uint32_t dst, const CUtensorMap *map, 
 
 // Key rows tok .. tok + keys of a sequence into shared memory, as D / 64 halves
 // of 128-byte rows (128-byte swizzle): TMA boxes of up to a page, shared out to
-// the lanes of a warp.  A page that does not exist (a block from `blocks` on,
+// the lanes of kWarps warps (a warp issues its lanes' boxes one after another,
+// about 55 cycles each).  A page that does not exist (a block from `blocks` on,
 // an id out of range) reads as zeros.  find() loads the ids some time before
 // load() needs them.
-template <int D, int kKeys>
+template <int D, int kKeys, uint32_t kWarps>
 struct KeyBoxes {
-    static constexpr uint32_t kHalves = D / 64, kEach = (kKeys / 4 * kHalves + 31) / 32;   // boxes a lane, with 4-token pages
-    uint32_t page[kEach];
+    static constexpr uint32_t kHalves = D / 64;
+    static constexpr uint32_t kEach = (kKeys / 4 * kHalves + 32 * kWarps - 1) / (32 * kWarps);   // a lane's, with 4-token pages
+    uint32_t first, page[kEach];
+
+    __device__ __forceinline__ explicit KeyBoxes(uint32_t warp) : first((threadIdx.x & 31) * kWarps + warp) {}
 
     __device__ __forceinline__ void find(const AttendArgs &p, const int32_t *table, uint32_t tok, uint32_t blocks) {
-        const uint32_t boxes = kKeys * kHalves >> p.box_log, lane = threadIdx.x & 31;
+        const uint32_t boxes = kKeys * kHalves >> p.box_log;
 #pragma unroll
         for (uint32_t i = 0; i < kEach; ++i) {
-            const uint32_t x = lane + 32 * i, blk = (tok + (x / kHalves << p.box_log)) >> p.B_log;
+            const uint32_t x = first + 32 * kWarps * i, blk = (tok + (x / kHalves << p.box_log)) >> p.B_log;
             page[i] = x < boxes && blk < blocks ? min((uint32_t)__ldg(table + blk), p.pages) : p.pages;
         }
     }
     __device__ __forceinline__ void load(const AttendArgs &p, const CUtensorMap *map, uint32_t dst, uint32_t bar, uint32_t tok,
                                          uint32_t head) const {
-        const uint32_t boxes = kKeys * kHalves >> p.box_log, lane = threadIdx.x & 31;
+        const uint32_t boxes = kKeys * kHalves >> p.box_log;
 #pragma unroll
         for (uint32_t i = 0; i < kEach; ++i) {
-            const uint32_t x = lane + 32 * i, half = x % kHalves, at = x / kHalves << p.box_log;
+            const uint32_t x = first + 32 * kWarps * i, half = x % kHalves, at = x / kHalves << p.box_log;
             if (x < boxes)
                 tma_load4(dst + half * kKeys * 128 + at * 128, map, bar, (int)half * 64, (int)((tok + at) & ((1u << p.B_log) - 1)),
                           (int)head, (int)page[i]);

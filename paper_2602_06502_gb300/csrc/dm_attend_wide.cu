@@ -4,7 +4,7 @@
 // One CTA per SM walks its units (dm_attend.cuh).  Rows come in two tiles of
 // 128 (A and B) that read the same keys:
 //   warps 0-3, 4-7  softmax of A and of B, a row per thread
-//   warp 8          TMA: keys and values page by page into a ring of stages
+//   warps 8, 10, 11 TMA: keys and values page by page into a ring of stages
 //   warp 9          tcgen05.mma: S = Q K^T (128 x 128, both operands in shared
 //                   memory), O += P V (P in tensor memory over S, V in shared
 //                   memory, dims contiguous)
@@ -190,9 +190,10 @@ __global__ void __launch_bounds__(kWideT, 1)
     // 384 x 168 registers at the start; 2 x 128 x 208 + 128 x 88 are as many
     if (wid >= 8) {
         asm volatile("setmaxnreg.dec.sync.aligned.u32 88;");
-        if (wid == 8) {
+        if (wid != 9) {
             uint32_t c = 0;   // stages so far: K of unit 0, V of unit 0, K of unit 1, ...
-            KeyBoxes<D, kWideKeys> boxes;
+            const uint32_t pw = wid == 8 ? 0 : wid - 9;
+            KeyBoxes<D, kWideKeys, 3> boxes(pw);
             bool stop = false, more = w.next(p);
             const int32_t *table = nullptr;
             uint32_t blocks = 0, tok = 0, left = 0, head = 0;   // the next unit; units left of the piece
@@ -212,7 +213,7 @@ __global__ void __launch_bounds__(kWideT, 1)
                     const uint32_t i = c % W::kStages, round = c / W::kStages;
                     if (round) mbar_wait(empty(i), (round - 1) & 1, gave_up, p.status);
                     if ((stop = __any_sync(~0u, *gave_up))) break;
-                    if (lane == 0) mbar_expect(full(i), W::kTile);
+                    if (pw == 0 && lane == 0) mbar_expect(full(i), W::kTile);   // the phase ends with this and all the bytes
                     __syncwarp();
                     boxes.load(p, v ? &mv : &mk, s_at + W::kRing + i * W::kTile, full(i), tok, head);
                 }
@@ -223,7 +224,7 @@ __global__ void __launch_bounds__(kWideT, 1)
             // no copy may be in flight when the CTA ends
             for (uint32_t i = c > W::kStages ? c - W::kStages : 0; i < c; ++i)
                 mbar_drain(full(i % W::kStages), (i / W::kStages) & 1);
-        } else if (wid == 9) {
+        } else {
             constexpr uint32_t kType = Pack2<T>::kMmaType;
             // f32 accumulators, the operands' type, N, M = 128; V's rows (dims) are contiguous
             constexpr uint32_t desc_s = 1u << 4 | kType << 7 | kType << 10 | (kWideKeys / 8) << 17 | 8u << 24;
