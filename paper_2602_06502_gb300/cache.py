@@ -8,8 +8,6 @@ Calls on one cache, and the attention of one plan, have to be ordered by the
 caller, as work that shares a tensor is.
 """
 
-import ctypes as C
-
 import torch
 
 from . import dualmap as D
@@ -74,63 +72,70 @@ class PagedCache:
         return cls(k, torch.empty_like(k), torch.zeros(max_seqs, -(-max_tokens // page_tokens), **ints),
                    torch.zeros(max_seqs, **ints), torch.zeros(pages, **ints), layout)
 
-    def _stream(self):
-        return C.c_void_p(torch.cuda.current_stream(self.device).cuda_stream)
+    # These run once per call of a decode step, so they ask each tensor for
+    # little: a call costs a few microseconds of Python.
 
-    def _ints(self, *named):
-        for name, x, n in named:
-            if x.dtype != torch.int32 or x.dim() != 1 or not x.is_contiguous() or x.device != self.device or \
-                    (n is not None and x.shape[0] != n):
-                raise ValueError(f"{name}: contiguous int32 on {self.device}" + (f" of length {n}" if n is not None else ""))
+    def _ints(self, name, x, n=None):
+        """The address of a contiguous int32 vector (of n elements)."""
+        if x.dtype is not torch.int32 or x.dim() != 1 or x.device != self.device or not x.is_contiguous() or \
+                (n is not None and x.shape[0] != n):
+            raise ValueError(f"{name}: contiguous int32 on {self.device}" + (f" of length {n}" if n is not None else ""))
+        return x.data_ptr()
 
     def _rows(self, name, x, tokens, heads):
-        if x.dtype != self.dtype or x.device != self.device or tuple(x.shape) != (tokens, heads, self.head_dim) or \
-                (x.shape[2] > 1 and x.stride(2) != 1):
-            raise ValueError(f"{name}: {self.dtype} on {self.device} of shape {(tokens, heads, self.head_dim)}, "
-                             f"head_dim contiguous")
+        """Address and strides (token, head) of [tokens, heads, head_dim]."""
+        shape, stride = (tokens, heads, self.head_dim), x.stride()
+        if x.dtype is not self.dtype or x.device != self.device or x.shape != shape or stride[2] != 1:
+            raise ValueError(f"{name}: {self.dtype} on {self.device} of shape {shape}, head_dim contiguous")
         # the stride of a dimension of one element says nothing
-        return (x.stride(0) if tokens > 1 else 0), (x.stride(1) if heads > 1 else 0)
+        return x.data_ptr(), (stride[0] if tokens > 1 else 0), (stride[1] if heads > 1 else 0)
 
-    def _call(self, where, rc):
+    def _vector(self, name, x):
+        if x is None:
+            return None
+        if x.dtype is not self.dtype or x.shape != (self.head_dim,) or x.device != self.device or not x.is_contiguous():
+            raise ValueError(f"{name}: contiguous {self.dtype} of shape {(self.head_dim,)} on {self.device}")
+        return x.data_ptr()
+
+    def _call(self, name, *args):
+        """Enqueues a dm_cache_* call on torch's current stream of the cache's device."""
+        if torch.cuda.current_device() != self.device.index:
+            with torch.cuda.device(self.device):
+                return self._call(name, *args)
+        rc = getattr(D, name)(self.struct, *args, torch._C._cuda_getCurrentRawStream(self.device.index))
         if rc:
-            raise D.DualMapError(rc, where)
+            raise D.DualMapError(rc, name)
 
     def last_error(self):
         """The status of the first call that was refused on the device, which it clears (synchronises)."""
         with torch.cuda.device(self.device):
-            return D.dm_cache_last_error(self.struct, self._stream())
+            return D.dm_cache_last_error(self.struct, torch._C._cuda_getCurrentRawStream(self.device.index))
 
     def extend(self, seqs, add):
         """Sequence seqs[i] grows by add[i] tokens; the pages it lacks are taken."""
-        self._ints(("seqs", seqs, None), ("add", add, seqs.shape[0]))
-        with torch.cuda.device(self.device):
-            self._call("dm_cache_extend", D.dm_cache_extend(self.struct, seqs, add, seqs.shape[0], self._stream()))
+        n = seqs.shape[0]
+        self._call("dm_cache_extend", self._ints("seqs", seqs), self._ints("add", add, n), n)
 
     def fork(self, parents, children, lengths):
         """The empty sequence children[i] becomes the first lengths[i] tokens of parents[i]."""
         n = parents.shape[0]
-        self._ints(("parents", parents, None), ("children", children, n), ("lengths", lengths, n))
-        with torch.cuda.device(self.device):
-            self._call("dm_cache_fork", D.dm_cache_fork(self.struct, parents, children, lengths, n, self._stream()))
+        self._call("dm_cache_fork", self._ints("parents", parents), self._ints("children", children, n),
+                   self._ints("lengths", lengths, n), n)
 
     def free(self, seqs):
         """The sequences give up their pages."""
-        self._ints(("seqs", seqs, None))
-        with torch.cuda.device(self.device):
-            self._call("dm_cache_free", D.dm_cache_free(self.struct, seqs, seqs.shape[0], self._stream()))
+        self._call("dm_cache_free", self._ints("seqs", seqs), seqs.shape[0])
 
     def compact(self, tables_out=None, refs_out=None, moved=None):
         """Moves the pages in use to the lowest ids.  tables_out, refs_out: where
         the new bookkeeping goes (default: in place); moved: an int32 tensor of
         one element for the number of pages moved."""
         for name, x, like in (("tables_out", tables_out, self.tables), ("refs_out", refs_out, self.refs)):
-            if x is not None and (x.dtype != torch.int32 or x.shape != like.shape or not x.is_contiguous() or
+            if x is not None and (x.dtype is not torch.int32 or x.shape != like.shape or not x.is_contiguous() or
                                   x.device != self.device):
                 raise ValueError(f"{name}: contiguous int32 of shape {tuple(like.shape)} on {self.device}")
-        if moved is not None:
-            self._ints(("moved", moved, 1))
-        with torch.cuda.device(self.device):
-            self._call("dm_cache_compact", D.dm_cache_compact(self.struct, tables_out, refs_out, moved, self._stream()))
+        self._call("dm_cache_compact", None if tables_out is None else tables_out.data_ptr(),
+                   None if refs_out is None else refs_out.data_ptr(), None if moved is None else self._ints("moved", moved, 1))
 
     def append(self, seqs, offsets, q, k, v, cos=None, sin=None, *, layer=0, q_weight=None, k_weight=None, eps=1e-6,
                interleaved=False, out=None):
@@ -143,55 +148,46 @@ class PagedCache:
         sin: float32 [positions, rotated dims / 2]; without them nothing turns.
         q_weight, k_weight [head_dim]: without one there is no norm.  out:
         where the queries go; may be q."""
-        n, tokens = seqs.shape[0], k.shape[0]
-        self._ints(("seqs", seqs, None), ("offsets", offsets, n + 1))
-        a = D.dm_append_args(seqs=seqs.data_ptr(), offsets=offsets.data_ptr(), n=n, tokens=tokens, layer=layer,
-                             q_heads=q.shape[1], rope_dim=0, interleaved=int(interleaved), eps=eps)
+        n, tokens, heads = seqs.shape[0], k.shape[0], q.shape[1]
         if out is None:
             out = torch.empty(q.shape, dtype=self.dtype, device=self.device)
-        for name, x, heads in (("q", q, q.shape[1]), ("k", k, self.kv_heads), ("v", v, self.kv_heads),
-                               ("q_out", out, q.shape[1])):
-            strides = self._rows(name, x, tokens, heads)
-            setattr(a, name, x.data_ptr())
-            setattr(a, name + "_token", strides[0])
-            setattr(a, name + "_head", strides[1])
-        for name, x in (("q_weight", q_weight), ("k_weight", k_weight)):
-            if x is not None:
-                if x.dtype != self.dtype or tuple(x.shape) != (self.head_dim,) or not x.is_contiguous() or x.device != self.device:
-                    raise ValueError(f"{name}: contiguous {self.dtype} of shape {(self.head_dim,)} on {self.device}")
-                setattr(a, name, x.data_ptr())
+        qp, qt, qh = self._rows("q", q, tokens, heads)
+        kp, kt, kh = self._rows("k", k, tokens, self.kv_heads)
+        vp, vt, vh = self._rows("v", v, tokens, self.kv_heads)
+        op, ot, oh = self._rows("out", out, tokens, heads)
         if (cos is None) != (sin is None):
             raise ValueError("cos and sin come together")
+        cp = sp = None
+        rows = dims = 0
         if cos is not None:
             for name, x in (("cos", cos), ("sin", sin)):
-                if x.dtype != torch.float32 or x.dim() != 2 or x.shape != cos.shape or not x.is_contiguous() or x.device != self.device:
+                if x.dtype is not torch.float32 or x.dim() != 2 or x.shape != cos.shape or not x.is_contiguous() or \
+                        x.device != self.device:
                     raise ValueError(f"{name}: contiguous float32 [positions, rotated dims / 2] on {self.device}")
-            a.cos, a.sin, a.rope_rows, a.rope_dim = cos.data_ptr(), sin.data_ptr(), cos.shape[0], 2 * cos.shape[1]
-        with torch.cuda.device(self.device):
-            self._call("dm_cache_append", D.dm_cache_append(self.struct, a, self._stream()))
+            cp, sp, (rows, dims) = cos.data_ptr(), sin.data_ptr(), cos.shape
+        a = D.dm_append_args(self._ints("seqs", seqs), self._ints("offsets", offsets, n + 1), n, tokens, layer, heads,
+                             qp, kp, vp, op, qt, qh, kt, kh, vt, vh, ot, oh, self._vector("q_weight", q_weight),
+                             self._vector("k_weight", k_weight), cp, sp, rows, 2 * dims, bool(interleaved), eps)
+        self._call("dm_cache_append", a)
         return out
 
     def plan(self, seqs, offsets, tokens, q_heads, group_offsets=None, group_prefix=None):
         """Divides the attention of a step of `tokens` query rows over the GPU.
         Group g: sequences group_offsets[g] .. group_offsets[g + 1] of the step,
         which start with the same group_prefix[g] tokens in the same pages."""
-        n = seqs.shape[0]
-        self._ints(("seqs", seqs, None), ("offsets", offsets, n + 1))
+        n, groups, go, gp = seqs.shape[0], 0, None, None
         if (group_offsets is None) != (group_prefix is None):
             raise ValueError("group_offsets and group_prefix come together")
-        groups = 0
         if group_prefix is not None:
             groups = group_prefix.shape[0]
-            self._ints(("group_prefix", group_prefix, None), ("group_offsets", group_offsets, groups + 1))
+            gp, go = self._ints("group_prefix", group_prefix), self._ints("group_offsets", group_offsets, groups + 1)
         size = D.dm_plan_bytes(self.struct, n, groups, tokens, q_heads)
         if not size:
             raise D.DualMapError(D.DM_ERR_INVALID_ARG, "dm_plan_bytes")
         work = torch.empty(size, dtype=torch.uint8, device=self.device)
-        s = D.dm_plan(seqs.data_ptr(), offsets.data_ptr(), n, tokens, q_heads, groups,
-                      group_offsets.data_ptr() if groups else None, group_prefix.data_ptr() if groups else None,
+        s = D.dm_plan(self._ints("seqs", seqs), self._ints("offsets", offsets, n + 1), n, tokens, q_heads, groups, go, gp,
                       work.data_ptr(), size)
-        with torch.cuda.device(self.device):
-            self._call("dm_cache_plan", D.dm_cache_plan(self.struct, s, self._stream()))
+        self._call("dm_cache_plan", s)
         return Plan(s, (seqs, offsets, group_offsets, group_prefix, work), tokens, q_heads)
 
     def attend(self, plan, q, *, layer=0, scale=None, out=None, lse=None):
@@ -200,12 +196,12 @@ class PagedCache:
         q_heads] for the logarithms of the sums."""
         if out is None:
             out = torch.empty(q.shape, dtype=self.dtype, device=self.device)
-        qs, os = self._rows("q", q, plan.tokens, plan.q_heads), self._rows("out", out, plan.tokens, plan.q_heads)
-        if lse is not None and (lse.dtype != torch.float32 or tuple(lse.shape) != (plan.tokens, plan.q_heads) or
+        qp, qt, qh = self._rows("q", q, plan.tokens, plan.q_heads)
+        op, ot, oh = self._rows("out", out, plan.tokens, plan.q_heads)
+        if lse is not None and (lse.dtype is not torch.float32 or lse.shape != (plan.tokens, plan.q_heads) or
                                 not lse.is_contiguous() or lse.device != self.device):
             raise ValueError(f"lse: contiguous float32 of shape {(plan.tokens, plan.q_heads)} on {self.device}")
-        a = D.dm_attend_args(layer, self.head_dim ** -0.5 if scale is None else scale, q.data_ptr(), out.data_ptr(),
-                             None if lse is None else lse.data_ptr(), *qs, *os)
-        with torch.cuda.device(self.device):
-            self._call("dm_cache_attend", D.dm_cache_attend(self.struct, plan.struct, a, self._stream()))
+        a = D.dm_attend_args(layer, self.head_dim ** -0.5 if scale is None else scale, qp, op,
+                             None if lse is None else lse.data_ptr(), qt, qh, ot, oh)
+        self._call("dm_cache_attend", plan.struct, a)
         return out

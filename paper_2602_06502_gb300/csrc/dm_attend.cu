@@ -25,7 +25,7 @@ struct PlanArgs {
     PlanWork w;
     const int32_t *tables, *lengths, *seqs, *offsets, *group_offsets, *group_prefix;
     uint32_t *status;
-    uint32_t n, groups, tokens, G, kv_heads, B, max_seqs, max_blocks, blocks[2];
+    uint32_t n, groups, tokens, G, kv_heads, B, max_seqs, max_blocks, ctas[2];
 };
 
 __device__ __forceinline__ uint64_t scan_incl(uint64_t x) {
@@ -50,32 +50,47 @@ __device__ uint64_t block_scan(uint64_t x, uint64_t *s_warp, uint64_t &total) {
     return in - x + (wid ? s_warp[wid - 1] : 0);
 }
 
-// The group of sequence i: the last g with group_offsets[g] <= i, -1 if i is
-// outside them all or the group shares nothing.
-__device__ __forceinline__ int32_t group_at(const PlanArgs &p, uint32_t i) {
-    if (p.groups == 0 || (int32_t)i < p.group_offsets[0] || (int32_t)i >= p.group_offsets[p.groups]) return -1;
-    uint32_t lo = 0, hi = p.groups;
+constexpr uint32_t kFewGroups = 512, kFewBlocks = 2048;   // kept in shared memory
+
+// The group of sequence i: the last g with offsets[g] <= i, -1 if i is outside
+// them all or the group shares nothing.
+__device__ __forceinline__ int32_t group_at(const int32_t *offsets, const int32_t *prefix, uint32_t groups, uint32_t i) {
+    if (groups == 0 || (int32_t)i < offsets[0] || (int32_t)i >= offsets[groups]) return -1;
+    uint32_t lo = 0, hi = groups;
     while (hi - lo > 1) {
         const uint32_t mid = (lo + hi) / 2;
-        if (p.group_offsets[mid] <= (int32_t)i) lo = mid;
+        if (offsets[mid] <= (int32_t)i) lo = mid;
         else hi = mid;
     }
-    return p.group_prefix[lo] > 0 ? (int32_t)lo : -1;
+    return prefix[lo] > 0 ? (int32_t)lo : -1;
 }
 
 // CTA 0 lays the work out; the others see that a group's sequences begin with
-// the same pages.
+// the same pages.  Bound: latency, a chain of small steps (6 us for 256
+// sequences), so what is searched is kept in shared memory.
 __global__ void __cluster_dims__(kPlanCl, 1, 1) __launch_bounds__(kPlanT) k_plan(PlanArgs p) {
-    __shared__ uint64_t s_warp[32];
+    __shared__ uint64_t s_warp[32], s_cum[kFewBlocks];
+    __shared__ int32_t s_offsets[kFewGroups + 1], s_prefix[kFewGroups];
+    __shared__ uint32_t s_max[kFewGroups], s_n[kFewGroups];
     __shared__ uint32_t s_bad;
     cg::cluster_group cl = cg::this_cluster();
     const uint32_t rank = cl.block_rank(), tid = threadIdx.x;
+    const bool few = p.groups <= kFewGroups;
+    const int32_t *go = few ? s_offsets : p.group_offsets, *gp = few ? s_prefix : p.group_prefix;
+    uint32_t *gmax = few ? s_max : p.w.group_max, *gn = few ? s_n : p.w.group_n;
     if (tid == 0) s_bad = 0;
+    if (few)
+        for (uint32_t g = tid; p.groups && g <= p.groups; g += kPlanT) {
+            s_offsets[g] = p.group_offsets[g];
+            if (g < p.groups) s_prefix[g] = p.group_prefix[g];
+        }
+    if (rank == 0)
+        for (uint32_t g = tid; g < p.groups; g += kPlanT) gmax[g] = gn[g] = 0;
     __syncthreads();
     bool bad = false;
     // every CTA: groups and sequences in range (the page check below relies on it)
     for (uint32_t g = tid; g < p.groups; g += kPlanT) {
-        const int32_t a = p.group_offsets[g], b = p.group_offsets[g + 1], P = p.group_prefix[g];
+        const int32_t a = go[g], b = go[g + 1], P = gp[g];
         bad |= a < 0 || b < a || b > (int32_t)p.n || P < 0 || P % (int32_t)p.B || (uint32_t)P > p.max_blocks * p.B;
     }
     if (__syncthreads_or(bad)) s_bad = 1;
@@ -87,61 +102,58 @@ __global__ void __cluster_dims__(kPlanCl, 1, 1) __launch_bounds__(kPlanT) k_plan
                 continue;
             }
             const int64_t len = p.lengths[s], used = b - a;
-            const int32_t g = group_at(p, i);
-            bad |= len < 0 || len > (int64_t)p.max_blocks * p.B || (g >= 0 && used > 0 && p.group_prefix[g] > len - used);
+            const int32_t g = group_at(go, gp, p.groups, i);
+            bad |= len < 0 || len > (int64_t)p.max_blocks * p.B || (g >= 0 && used > 0 && gp[g] > len - used);
+            if (rank == 0 && g >= 0 && used) {
+                atomicMax(gmax + g, (uint32_t)used * p.G);
+                atomicAdd(gn + g, 1u);
+            }
         }
-        // a group's prefix is read through its first sequence's row, so that
-        // one's id has to be in range too (it is one of the n)
         if (__syncthreads_or(bad)) s_bad = 1;
     }
     __syncthreads();
-    if (rank > 0 && !s_bad && p.groups) {   // a warp per sequence
+    if (rank > 0 && !s_bad && p.groups) {   // a warp per sequence, against its group's first
         const uint32_t lane = tid & 31, warps = (kPlanCl - 1) * kPlanT / 32;
         for (uint32_t i = (rank - 1) * (kPlanT / 32) + tid / 32; i < p.n; i += warps) {
-            const int32_t g = group_at(p, i);
+            const int32_t g = group_at(go, gp, p.groups, i);
             if (g < 0 || p.offsets[i + 1] == p.offsets[i]) continue;
             const int32_t *mine = p.tables + (uint64_t)p.seqs[i] * p.max_blocks;
-            const int32_t *lead = p.tables + (uint64_t)p.seqs[p.group_offsets[g]] * p.max_blocks;
-            const uint32_t nb = (uint32_t)p.group_prefix[g] / p.B;
-#pragma unroll 4
+            const int32_t *lead = p.tables + (uint64_t)p.seqs[go[g]] * p.max_blocks;
+            const uint32_t nb = (uint32_t)gp[g] / p.B;
+#pragma unroll 8
             for (uint32_t j = lane; j < nb; j += 32) bad |= mine[j] != lead[j];
         }
         if (bad) s_bad = 1;
     }
     if (rank == 0 && !s_bad) {
-        for (uint32_t g = tid; g < p.groups; g += kPlanT) p.w.group_max[g] = p.w.group_n[g] = 0;
-        __syncthreads();
-        for (uint32_t i = tid; i < p.n; i += kPlanT) {
-            const int32_t g = group_at(p, i);
-            const uint32_t rows = (uint32_t)(p.offsets[i + 1] - p.offsets[i]) * p.G;
-            if (g >= 0 && rows) {
-                atomicMax(p.w.group_max + g, rows);
-                atomicAdd(p.w.group_n + g, 1u);
-            }
-        }
-        __syncthreads();
-        auto shares = [&](int32_t g) { return g >= 0 && __ldcg(p.w.group_max + g) < kShareRows && __ldcg(p.w.group_n + g) >= 2; };
-        auto rows_of = [&](uint32_t e) -> uint32_t {   // of an entity: groups, then sequences
-            if (e < p.groups) {
-                if (!shares(p.group_prefix[e] > 0 ? (int32_t)e : -1)) return 0;
-                return (uint32_t)(p.offsets[p.group_offsets[e + 1]] - p.offsets[p.group_offsets[e]]) * p.G;
-            }
-            return (uint32_t)(p.offsets[e - p.groups + 1] - p.offsets[e - p.groups]) * p.G;
-        };
-        for (uint32_t i = tid; i < p.n; i += kPlanT) {
-            const int32_t g = group_at(p, i);
-            p.w.group_of[i] = shares(g) ? g : -1;
-        }
         const uint32_t ents = p.groups + p.n;
         uint64_t carry = 0;   // wide blocks in the low half, narrow ones above
         for (uint32_t e0 = 0; e0 < ents; e0 += kPlanT) {
-            const uint32_t e = e0 + tid, rows = e < ents ? rows_of(e) : 0;
-            const uint64_t mine = rows == 0 ? 0 : rows <= kNarrowRows ? 1ull << 32 : (rows + kWideRows - 1) / kWideRows;
+            const uint32_t e = e0 + tid;
+            PlanEntity x{};
+            if (e < ents) {
+                const uint32_t i = e < p.groups ? (uint32_t)go[e] : e - p.groups;
+                const int32_t g = e < p.groups ? (gp[e] > 0 ? (int32_t)e : -1) : group_at(go, gp, p.groups, i);
+                const bool shares = g >= 0 && gmax[g] < kShareRows && gn[g] >= 2;
+                x.group = shares ? g : -1;
+                if (e >= p.groups || shares) {
+                    const int32_t last = e < p.groups ? p.offsets[go[e + 1]] : p.offsets[i + 1];
+                    x.row = p.seqs[i];
+                    x.token = p.offsets[i];
+                    x.rows = (uint32_t)(last - x.token) * p.G;
+                    x.shared = e < p.groups ? kPrefix : shares ? kOwn : 0;
+                    x.kv0 = e < p.groups || !shares ? 0 : gp[g];
+                    x.pos = e < p.groups ? 1 << 30 /* behind every key */ : p.lengths[x.row] - (last - x.token);
+                }
+            }
+            const uint64_t mine = x.rows == 0 ? 0 : x.rows <= kNarrowRows ? 1ull << 32 : (x.rows + kWideRows - 1) / kWideRows;
             uint64_t total;
             const uint64_t before = carry + block_scan(mine, s_warp, total);
             if (e < ents) {
-                p.w.first[0][e] = (uint32_t)before;
-                p.w.first[1][e] = (uint32_t)(before >> 32);
+                const int kind = x.rows <= kNarrowRows;
+                x.first = (uint32_t)(kind ? before >> 32 : before);
+                p.w.entity[e] = x;
+                for (uint32_t j = 0; j < (uint32_t)(kind ? mine >> 32 : mine); ++j) p.w.owner[kind][x.first + j] = e;
             }
             carry += total;
         }
@@ -149,39 +161,30 @@ __global__ void __cluster_dims__(kPlanCl, 1, 1) __launch_bounds__(kPlanT) k_plan
         __syncthreads();
         for (int kind = 0; kind < 2; ++kind) {
             const uint32_t cap = kind == 0 ? kWideRows : kNarrowRows, keys = kind == 0 ? kWideKeys : kNarrowKeys;
+            uint64_t *cum = count[kind] <= kFewBlocks ? s_cum : p.w.cum[kind];
             uint64_t units0 = 0, parts0 = 0;
             for (uint32_t b0 = 0; b0 < count[kind]; b0 += kPlanT) {
                 const uint32_t b = b0 + tid;
                 AttendBlock k{};
                 if (b < count[kind]) {
-                    uint32_t lo = 0, hi = ents;   // the last entity with first <= b; those without blocks come before it
-                    while (hi - lo > 1) {
-                        const uint32_t mid = (lo + hi) / 2;
-                        if (__ldcg(p.w.first[kind] + mid) <= b) lo = mid;
-                        else hi = mid;
-                    }
-                    const uint32_t e = lo, rows = rows_of(e);
-                    const uint32_t row0 = (b - __ldcg(p.w.first[kind] + e)) * cap;
-                    k.rows = min(rows - row0, cap);
+                    const uint32_t e = p.w.owner[kind][b];
+                    const PlanEntity x = p.w.entity[e];
+                    const uint32_t row0 = (b - x.first) * cap;
+                    k.row = x.row;
+                    k.rows = min(x.rows - row0, cap);
                     k.lead = row0 % p.G;
-                    if (e < p.groups) {
-                        const int32_t i = p.group_offsets[e];
-                        k.row = p.seqs[i];
-                        k.token = p.offsets[i] + (int32_t)(row0 / p.G);
-                        k.kv1 = p.group_prefix[e];
-                        k.pos = 1 << 30;   // behind every key of the prefix
-                        k.shared = 1;
-                    } else {
-                        const uint32_t i = e - p.groups;
-                        const int32_t g = __ldcg(p.w.group_of + i), used = p.offsets[i + 1] - p.offsets[i];
-                        k.row = p.seqs[i];
-                        k.token = p.offsets[i] + (int32_t)(row0 / p.G);
-                        k.shared = g >= 0;
-                        k.kv0 = g >= 0 ? p.group_prefix[g] : 0;
-                        k.pos = p.lengths[k.row] - used + (int32_t)(row0 / p.G);
-                        k.kv1 = max(k.kv0, k.pos + (int32_t)((k.lead + k.rows - 1) / p.G) + 1);
-                    }
+                    k.token = x.token + (int32_t)(row0 / p.G);
+                    k.kv0 = x.kv0;
+                    k.shared = x.shared;
+                    k.pos = x.pos + (int32_t)(row0 / p.G);
+                    k.kv1 = x.shared == kPrefix ? gp[e] : max(k.kv0, k.pos + (int32_t)((k.lead + k.rows - 1) / p.G) + 1);
                     k.units = max(1u, ((uint32_t)(k.kv1 - k.kv0) + keys - 1) / keys);
+                    if (x.shared == kOwn) {
+                        const PlanEntity pre = p.w.entity[x.group];
+                        k.pre = pre.first;
+                        k.pre_kind = pre.rows <= kNarrowRows;
+                        k.pre_row = (uint32_t)(x.token - pre.token) * p.G + row0;
+                    }
                 }
                 uint64_t units, parts;
                 const uint64_t at = units0 + block_scan((uint64_t)k.units * p.kv_heads, s_warp, units);
@@ -190,14 +193,29 @@ __global__ void __cluster_dims__(kPlanCl, 1, 1) __launch_bounds__(kPlanT) k_plan
                     k.part0 = (uint32_t)part;
                     p.w.block[kind][b] = k;
                     p.w.cum[kind][b] = at;
+                    cum[b] = at;
                 }
                 units0 += units;
                 parts0 += parts;
             }
+            __syncthreads();
+            const uint32_t S = (uint32_t)min((uint64_t)p.ctas[kind], units0);
+            for (uint32_t c = tid; c < S; c += kPlanT) {
+                const uint64_t u = c * units0 / S;
+                uint32_t lo = 0, hi = count[kind];   // the last block with cum <= u
+                while (hi - lo > 1) {
+                    const uint32_t mid = (lo + hi) / 2;
+                    if (cum[mid] <= u) lo = mid;
+                    else hi = mid;
+                }
+                p.w.start[kind][c] = lo;
+            }
             if (tid == 0) {
                 p.w.head->units[kind] = units0;
                 p.w.head->blocks[kind] = count[kind];
+                p.w.head->ctas[kind] = S;
             }
+            __syncthreads();
         }
     }
     cl.sync();
@@ -231,7 +249,8 @@ struct Narrow {
     static constexpr uint32_t kSlots = D == 128 ? 4 : 8;
     static_assert(kSlots % 2 == 0, "each ring place has one pair of readers");
     static constexpr uint32_t kRed = kSlots * 2 * kHalf;            // 2 x 16 x D floats
-    static constexpr uint32_t kMl = kRed + 2 * 16 * D * 4;          // 4 x 16 float2
+    static constexpr uint32_t kQ = kRed + 2 * 16 * D * 4;           // two pieces' queries, 16 rows each
+    static constexpr uint32_t kMl = kQ + 2 * 16 * D * 2;            // 4 x 16 float2
     static constexpr uint32_t kBars = kMl + 4 * 16 * 8;             // full, empty per slot, then the give-up word
     static constexpr uint32_t kBytes = kBars + 16 * kSlots + 16 + 1024;   // with room to align
 };
@@ -309,24 +328,38 @@ __global__ void __launch_bounds__(160, kNarrowPerSm)
     float *red = reinterpret_cast<float *>(s + N::kRed);
     float2 *s_ml = reinterpret_cast<float2 *>(s + N::kMl);
     const uint32_t g = lane >> 2, t4 = lane & 3, pair = wid >> 1, key0 = (wid & 1) * 16;
-    uint32_t c = 0;
-    while (w.next(p)) {
+    uint32_t c = 0, buf = 0;
+    // A piece's queries to shared memory, zeros for the rows that are not there.
+    auto fetch = [&](const Walk<1> &k, uint32_t to) {
+#pragma unroll
+        for (uint32_t e = tid; e < 16 * D / 8; e += 128) {
+            const uint32_t row = e / (D / 8), ch = e % (D / 8);
+            const Row at = row_at(p, k.k, min(row, k.k.rows - 1));
+            const char *src = p.q + (uint64_t)(k.k.token + at.token) * p.q_token + (uint64_t)(k.head * p.G + at.head) * p.q_head + ch * 16;
+            asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(s_at + N::kQ + to * 32 * D + ch / 8 * 2048 + row * 128 + ((ch % 8) ^ (row % 8)) * 16),
+                         "l"(src), "r"(row < k.k.rows ? 16 : 0)
+                         : "memory");
+        }
+    };
+    bool more = w.next(p);
+    if (more) fetch(w, 0);
+    while (more) {
         // this thread's rows are g and g + 8
         uint32_t qf[D / 16][4];
         int32_t limit[2];
 #pragma unroll
         for (int r = 0; r < 2; ++r) {
             const uint32_t row = g + 8 * r;
-            const bool on = row < w.k.rows;
-            const Row at = row_at(p, w.k, on ? row : 0);
-            limit[r] = on ? row_limit(w.k, at.token) : 0;
-            const char *src = p.q + (uint64_t)(w.k.token + at.token) * p.q_token + (uint64_t)(w.head * p.G + at.head) * p.q_head;
-#pragma unroll
-            for (int kk = 0; kk < D / 16; ++kk) {
-                qf[kk][r] = on ? __ldg(reinterpret_cast<const uint32_t *>(src + kk * 32 + t4 * 4)) : 0;
-                qf[kk][r + 2] = on ? __ldg(reinterpret_cast<const uint32_t *>(src + kk * 32 + 16 + t4 * 4)) : 0;
-            }
+            limit[r] = row < w.k.rows ? row_limit(w.k, row_at(p, w.k, row).token) : 0;
         }
+        asm volatile("cp.async.wait_all;" ::: "memory");
+        bar_consumers();
+#pragma unroll
+        for (int kk = 0; kk < D / 16; ++kk) {
+            const uint32_t row = lane & 15, chunk = kk * 2 + (lane >> 4);
+            ldsm4(qf[kk], s_at + N::kQ + buf * 32 * D + (chunk >> 3) * 2048 + row * 128 + (((chunk & 7) ^ (row & 7)) << 4));
+        }
+        Walk<1> ahead = w;
         float o[D / 8][4], m[2] = {-INFINITY, -INFINITY}, l[2] = {0.f, 0.f};
 #pragma unroll
         for (int i = 0; i < D / 8; ++i) o[i][0] = o[i][1] = o[i][2] = o[i][3] = 0.f;
@@ -406,8 +439,10 @@ __global__ void __launch_bounds__(160, kNarrowPerSm)
             }
             __syncwarp();
             if (lane == 0) mbar_arrive(empty(slot));
+            if (j == pair && (more = ahead.next(p))) fetch(ahead, buf ^ 1);   // while the ring is full
         }
         c += 2 * w.units;
+        buf ^= 1;
         // the four warps' parts: maxima and sums first, then the outputs in a fixed order
 #pragma unroll
         for (int r = 0; r < 2; ++r) {
@@ -483,71 +518,99 @@ __global__ void __launch_bounds__(160, kNarrowPerSm)
                 }
             }
         }
+        w = ahead;
     }
 }
 
 // -- joining parts --------------------------------------------------------------------
 
-// A warp per token and head: its parts from the group's prefix and from its
-// own keys, in the order of the CTAs that left them.  A token whose only part
-// went straight to the output has nothing to do.
+// CTAs walk the tiles of sequences' own keys; a warp takes a row: its parts of
+// the group's prefix, and those of its own keys in the order of the CTAs that
+// left them.  A tile that went straight to the output has nothing to do.
+// 32 parts' maxima and sums are looked at together, so that the parts
+// themselves are independent loads.  Bound: latency, then L2 (4 D + 8 bytes a
+// row and part).
+constexpr uint32_t kJoinPerSm = 4;
+
 template <class T, int D>
 __global__ void __launch_bounds__(256) k_attend_join(AttendArgs p) {
     constexpr int V = D / 32;
-    const uint64_t warp = (uint64_t)blockIdx.x * 8 + threadIdx.x / 32;
-    const uint32_t lane = threadIdx.x & 31;
-    const uint32_t tok = (uint32_t)(warp / p.q_heads), h = (uint32_t)(warp % p.q_heads);
-    if (tok >= p.tokens || has_err(p.status) || !p.w.head->ok) return;
-    if ((int32_t)tok < p.offsets[0] || (int32_t)tok >= p.offsets[p.n]) return;
-    uint32_t i = 0, hi = p.n;
-    while (hi - i > 1) {
-        const uint32_t mid = (i + hi) / 2;
-        if (p.offsets[mid] <= (int32_t)tok) i = mid;
-        else hi = mid;
-    }
-    const int32_t g = p.w.group_of[i];
-    const uint32_t kvh = h / p.G;
-    float acc[V], M = -INFINITY, L = 0.f;
+    const PlanHead h = *p.w.head;
+    const uint32_t lane = threadIdx.x & 31, wid = threadIdx.x / 32;
+    if (has_err(p.status) || !h.ok) return;
+    const uint64_t tiles = (uint64_t)(h.blocks[0] + h.blocks[1]) * p.kv_heads;
+    for (uint64_t t = blockIdx.x; t < tiles; t += gridDim.x) {
+        const uint32_t bb = (uint32_t)(t / p.kv_heads), head = (uint32_t)(t % p.kv_heads);
+        const int kind = bb >= h.blocks[0];
+        const uint32_t b = kind ? bb - h.blocks[0] : bb;
+        const AttendBlock k = (kind ? p.w.block[1] : p.w.block[0])[b];
+        if (k.shared == kPrefix) continue;
+        // the CTAs of a tile, and where row r of it is among CTA c's parts
+        struct Parts {
+            uint32_t c0, n;
+            uint64_t at, step;   // of the first; between CTAs' (a cut tile's first is one place off)
+            uint32_t odd;
+        };
+        auto parts = [&](int kd, uint32_t blk, const AttendBlock &x) {
+            const uint64_t u0 = (kd ? p.w.cum[1] : p.w.cum[0])[blk] + (uint64_t)head * x.units, U = kd ? h.units[1] : h.units[0];
+            const uint32_t cap = kd ? kNarrowRows : kWideRows, S = kd ? h.ctas[1] : h.ctas[0];
+            const uint32_t c0 = cta_of(u0, U, S), c1 = cta_of(u0 + x.units - 1, U, S);
+            if (x.shared) return Parts{c0, c1 - c0 + 1, x.part0 + (uint64_t)head * x.rows + (uint64_t)cap * c0, cap, 0};
+            return Parts{c0, c1 - c0 + 1, (kd ? p.w.shared_rows[1] : p.w.shared_rows[0]) + (uint64_t)cap * 2 * c0, 2 * cap, cap};
+        };
+        const Parts own = parts(kind, b, k);
+        if (!k.shared && own.n == 1) continue;
+        const uint32_t pre_cap = k.pre_kind ? kNarrowRows : kWideRows;
+        for (uint32_t r = wid; r < k.rows; r += 8) {
+            float acc[V], M = -INFINITY, L = 0.f;
 #pragma unroll
-    for (int v = 0; v < V; ++v) acc[v] = 0.f;
-    // parts of entity e whose first query token is t0; false: it went straight out
-    auto join = [&](uint32_t e, uint32_t t0, uint32_t rows_all) {
-        const uint32_t row = (tok - t0) * p.G + h % p.G;
-        const int kind = rows_all <= kNarrowRows;
-        const uint32_t cap = kind ? kNarrowRows : kWideRows, b = p.w.first[kind][e] + row / cap, r = row % cap;
-        const AttendBlock k = p.w.block[kind][b];
-        const uint64_t u0 = p.w.cum[kind][b] + (uint64_t)kvh * k.units, U = p.w.head->units[kind];
-        const uint32_t S = (uint32_t)min((uint64_t)p.ctas[kind], U);
-        const uint32_t c0 = cta_of(u0, U, S), c1 = cta_of(u0 + k.units - 1, U, S);
-        if (!k.shared && c0 == c1) return false;
-        for (uint32_t c = c0; c <= c1; ++c) {
-            const uint64_t at = k.shared ? k.part0 + (uint64_t)kvh * k.rows + (uint64_t)cap * c + r
-                                         : p.w.shared_rows[kind] + (uint64_t)cap * (2 * c + (c == c0 ? 1 : 0)) + r;
-            const float2 ml = p.w.ml[kind][at];
-            const float *src = p.w.part[kind] + at * D + lane * V;
-            float x[V];
-            if constexpr (V == 4) *reinterpret_cast<float4 *>(x) = *reinterpret_cast<const float4 *>(src);
-            else *reinterpret_cast<float2 *>(x) = *reinterpret_cast<const float2 *>(src);
-            const float now = fmaxf(M, ml.x), base = now == -INFINITY ? 0.f : now;
-            const float f = exp2_(M - base), fx = exp2_(ml.x - base);
+            for (int v = 0; v < V; ++v) acc[v] = 0.f;
+            auto join = [&](int kd, const Parts &x, uint32_t row) {
+                const float *part = kd ? p.w.part[1] : p.w.part[0];
+                const float2 *mls = kd ? p.w.ml[1] : p.w.ml[0];
+                for (uint32_t i0 = 0; i0 < x.n; i0 += 32) {
+                    const uint32_t n = min(32u, x.n - i0), i = i0 + lane;
+                    const uint64_t mine = x.at + i * x.step + (i == 0 ? x.odd : 0) + row;
+                    const float2 ml = lane < n ? mls[mine] : make_float2(-INFINITY, 0.f);
+                    float now = ml.x;
 #pragma unroll
-            for (int v = 0; v < V; ++v) acc[v] = acc[v] * f + x[v] * fx;
-            L = L * f + ml.y * fx;
-            M = now;
+                    for (int d = 16; d; d /= 2) now = fmaxf(now, __shfl_xor_sync(~0u, now, d));
+                    now = fmaxf(now, M);
+                    const float base = now == -INFINITY ? 0.f : now, f = exp2_(M - base), fi = exp2_(ml.x - base);
+                    float l = ml.y * fi;
+#pragma unroll
+                    for (int d = 16; d; d /= 2) l += __shfl_xor_sync(~0u, l, d);
+                    L = L * f + l;
+                    M = now;
+#pragma unroll
+                    for (int v = 0; v < V; ++v) acc[v] *= f;
+#pragma unroll 8
+                    for (uint32_t j = 0; j < n; ++j) {
+                        const float fj = __shfl_sync(~0u, fi, j);
+                        const float *src = part + (x.at + (i0 + j) * x.step + (i0 + j == 0 ? x.odd : 0) + row) * D + lane * V;
+                        float y[V];
+                        if constexpr (V == 4) *reinterpret_cast<float4 *>(y) = *reinterpret_cast<const float4 *>(src);
+                        else *reinterpret_cast<float2 *>(y) = *reinterpret_cast<const float2 *>(src);
+#pragma unroll
+                        for (int v = 0; v < V; ++v) acc[v] += y[v] * fj;
+                    }
+                }
+            };
+            if (k.shared) {
+                const uint32_t row = k.pre_row + r, blk = k.pre + row / pre_cap;
+                join((int)k.pre_kind, parts((int)k.pre_kind, blk, (k.pre_kind ? p.w.block[1] : p.w.block[0])[blk]), row % pre_cap);
+            }
+            join(kind, own, r);
+            const Row at = row_at(p, k, r);
+            const uint64_t tok = (uint64_t)(k.token + at.token);
+            const uint32_t qh = head * p.G + at.head;
+            const float inv = L > 0.f ? 1.f / L : 0.f;
+            char *dst = p.o + tok * p.o_token + qh * p.o_head + lane * V * 2;
+            if constexpr (V == 4) *reinterpret_cast<uint2 *>(dst) = make_uint2(Pack2<T>::pack(acc[0] * inv, acc[1] * inv), Pack2<T>::pack(acc[2] * inv, acc[3] * inv));
+            else *reinterpret_cast<uint32_t *>(dst) = Pack2<T>::pack(acc[0] * inv, acc[1] * inv);
+            if (p.lse && lane == 0) p.lse[tok * p.q_heads + qh] = L > 0.f ? (M + log2f(L)) * 0.69314718056f : -INFINITY;
         }
-        return true;
-    };
-    if (g >= 0) {
-        const uint32_t a = (uint32_t)p.offsets[p.group_offsets[g]], b = (uint32_t)p.offsets[p.group_offsets[g + 1]];
-        join((uint32_t)g, a, (b - a) * p.G);
     }
-    const uint32_t t0 = (uint32_t)p.offsets[i];
-    if (!join(p.groups + i, t0, ((uint32_t)p.offsets[i + 1] - t0) * p.G)) return;
-    const float inv = L > 0.f ? 1.f / L : 0.f;
-    char *dst = p.o + tok * p.o_token + h * p.o_head + lane * V * 2;
-    if constexpr (V == 4) *reinterpret_cast<uint2 *>(dst) = make_uint2(Pack2<T>::pack(acc[0] * inv, acc[1] * inv), Pack2<T>::pack(acc[2] * inv, acc[3] * inv));
-    else *reinterpret_cast<uint32_t *>(dst) = Pack2<T>::pack(acc[0] * inv, acc[1] * inv);
-    if (p.lse && lane == 0) p.lse[(uint64_t)tok * p.q_heads + h] = L > 0.f ? (M + log2f(L)) * 0.69314718056f : -INFINITY;
 }
 
 // -- launches -----------------------------------------------------------------------------
@@ -587,8 +650,7 @@ cudaError_t launch_rest(const AttendArgs &p, const CUtensorMap &mk, const CUtens
     DM_TRY(opt_in_smem(opt, Narrow<D>::kBytes, k_attend_narrow<T, D>));
     k_attend_narrow<T, D><<<p.ctas[1], 160, Narrow<D>::kBytes, st>>>(mk, mv, p);
     DM_TRY(cudaGetLastError());
-    const uint64_t warps = (uint64_t)p.tokens * p.q_heads;
-    k_attend_join<T, D><<<(uint32_t)((warps + 7) / 8), 256, 0, st>>>(p);
+    k_attend_join<T, D><<<p.ctas[0] * kJoinPerSm, 256, 0, st>>>(p);
     return cudaGetLastError();
 }
 
@@ -618,7 +680,7 @@ extern "C" dm_status dm_cache_plan(const dm_cache *c, const dm_plan *pl, void *s
     p.tables = c->tables, p.lengths = c->lengths, p.status = c->status;
     p.seqs = pl->seqs, p.offsets = pl->offsets, p.group_offsets = pl->group_offsets, p.group_prefix = pl->group_prefix;
     p.n = pl->n, p.groups = pl->groups, p.tokens = pl->tokens, p.G = s.G, p.kv_heads = c->kv_heads, p.B = c->page_tokens;
-    p.max_seqs = c->max_seqs, p.max_blocks = c->max_blocks;
+    p.max_seqs = c->max_seqs, p.max_blocks = c->max_blocks, p.ctas[0] = s.ctas[0], p.ctas[1] = s.ctas[1];
     k_plan<<<kPlanCl, kPlanT, 0, static_cast<cudaStream_t>(stream)>>>(p);
     return cudaGetLastError() == cudaSuccess ? DM_OK : DM_ERR_CUDA;
 }
@@ -640,13 +702,11 @@ extern "C" dm_status dm_cache_attend(const dm_cache *c, const dm_plan *pl, const
     p.G_mul = (uint32_t)((0xFFFFFFFFull + s.G) / s.G);   // 2^32 / G, rounded up
     p.G = s.G, p.kv_heads = c->kv_heads, p.q_heads = s.q_heads, p.scale2 = a->scale * 1.44269504089f;
     p.ctas[0] = s.ctas[0], p.ctas[1] = s.ctas[1];
-    p.offsets = pl->offsets, p.group_offsets = pl->group_offsets;
-    p.n = pl->n, p.groups = pl->groups, p.tokens = pl->tokens;
-    if (((uint64_t)p.tokens * p.q_heads + 7) / 8 > 0x7FFFFFFFull) return DM_ERR_INVALID_ARG;
     CUtensorMap mk, mv;
     if (!page_map(&mk, c, c->k, a->layer, box) || !page_map(&mv, c, c->v, a->layer, box)) return DM_ERR_CUDA;
     const auto st = static_cast<cudaStream_t>(stream);
-    cudaError_t e = launch_attend_wide(c, p, mk, mv, st);
+    // so few rows that no block of them is wide
+    cudaError_t e = (uint64_t)pl->tokens * s.G <= kNarrowRows ? cudaSuccess : launch_attend_wide(c, p, mk, mv, st);
     if (e == cudaSuccess) {
         if (c->dtype == DM_BF16)
             e = c->head_dim == 64 ? launch_rest<__nv_bfloat16, 64>(p, mk, mv, st) : launch_rest<__nv_bfloat16, 128>(p, mk, mv, st);

@@ -35,13 +35,25 @@ struct AttendBlock {
     int32_t pos;          // the first token's position (a group's prefix: all rows see all keys)
     uint32_t units;       // per key head, >= 1
     uint32_t part0;       // shared: its first row in the parts
-    uint32_t shared;
+    uint32_t shared;      // kPrefix, kOwn, or 0
+    // kOwn: where the rows' parts of the prefix are, a block of kind pre_kind
+    // and on, and the first row's place among the group's
+    uint32_t pre, pre_kind, pre_row;
 };
+constexpr uint32_t kOwn = 1, kPrefix = 2;
 
 struct PlanHead {
     uint64_t units[2];    // wide, narrow
     uint32_t blocks[2];
+    uint32_t ctas[2];     // that have units
     uint32_t ok, pad;
+};
+
+// A sequence or a group of the step.
+struct PlanEntity {
+    int32_t row, token, group, kv0, pos;
+    uint32_t rows, shared;
+    uint32_t first;       // its first block of its kind
 };
 
 // The plan's work buffer.
@@ -49,9 +61,10 @@ struct PlanWork {
     PlanHead *head;
     AttendBlock *block[2];    // wide, narrow
     uint64_t *cum[2];         // units before each block
-    uint32_t *first[2];       // per entity (groups, then sequences): blocks of the kind before it
+    uint32_t *start[2];       // per CTA: the block of its first unit
+    uint32_t *owner[2];       // per block: its entity
+    PlanEntity *entity;       // groups, then sequences
     uint32_t *group_max, *group_n;   // most rows of a sequence; sequences with rows
-    int32_t *group_of;        // per sequence: its shared group, or -1
     float *part[2];           // rows x D
     float2 *ml[2];            // rows: maximum (base 2), sum
     uint64_t shared_rows[2];  // the parts' rows before the cut tiles' (two per CTA)
@@ -99,11 +112,12 @@ inline uint64_t plan_work(const PlanShape &s, void *base, PlanWork &w) {
     for (int k = 0; k < 2; ++k) {
         w.block[k] = (AttendBlock *)take(sizeof(AttendBlock) * s.blocks[k]);
         w.cum[k] = (uint64_t *)take(8ull * s.blocks[k]);
-        w.first[k] = (uint32_t *)take(4ull * (s.n + s.groups + 1));
+        w.start[k] = (uint32_t *)take(4ull * s.ctas[k]);
+        w.owner[k] = (uint32_t *)take(4ull * s.blocks[k]);
     }
+    w.entity = (PlanEntity *)take(sizeof(PlanEntity) * (s.n + (uint64_t)s.groups));
     w.group_max = (uint32_t *)take(4ull * s.groups);
     w.group_n = (uint32_t *)take(4ull * s.groups);
-    w.group_of = (int32_t *)take(4ull * s.n);
     for (int k = 0; k < 2; ++k) {
         w.part[k] = (float *)take(4ull * s.D * s.rows[k]);
         w.ml[k] = (float2 *)take(8ull * s.rows[k]);
@@ -123,9 +137,7 @@ struct AttendArgs {
     uint32_t max_blocks, pages, G, G_mul, kv_heads, q_heads;   // x / G = x * G_mul >> 32 for x <= G + 256
     uint32_t B_log, box_log;                     // log2 of a page's tokens and of a TMA box's
     float scale2;                                // scale * log2(e)
-    uint32_t ctas[2];
-    const int32_t *offsets, *group_offsets;
-    uint32_t n, groups, tokens;
+    uint32_t ctas[2];                            // launched
 };
 
 // The CTA of S that unit u of U falls to: the last i with i U / S <= u.
@@ -137,7 +149,7 @@ __device__ __forceinline__ uint32_t cta_of(uint64_t u, uint64_t U, uint32_t S) {
 template <int kKind>
 struct Walk {
     uint64_t u, end;
-    uint32_t b, blocks;
+    uint32_t b;
     // of the present piece
     AttendBlock k;
     uint32_t head, j0, units;   // units j0 .. j0 + units of the tile
@@ -145,18 +157,14 @@ struct Walk {
 
     __device__ Walk(const AttendArgs &p) {
         const PlanHead &h = *p.w.head;
-        const uint64_t U = h.ok ? h.units[kKind] : 0;
-        blocks = h.ok ? h.blocks[kKind] : 0;
-        const uint64_t S = min((uint64_t)gridDim.x, U);
-        u = blockIdx.x < S ? blockIdx.x * U / S : 0;
-        end = blockIdx.x < S ? (blockIdx.x + 1) * U / S : 0;
-        uint32_t lo = 0, hi = blocks;   // the last block with cum <= u
-        while (u < end && hi - lo > 1) {
-            const uint32_t mid = (lo + hi) / 2;
-            if (p.w.cum[kKind][mid] <= u) lo = mid;
-            else hi = mid;
+        const uint64_t U = h.units[kKind];
+        const uint32_t S = h.ok ? h.ctas[kKind] : 0;
+        u = end = b = 0;
+        if (blockIdx.x < S) {
+            u = blockIdx.x * U / S;
+            end = (blockIdx.x + 1) * U / S;
+            b = p.w.start[kKind][blockIdx.x];
         }
-        b = lo;
     }
     __device__ bool next(const AttendArgs &p) {
         if (u >= end) return false;

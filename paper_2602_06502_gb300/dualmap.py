@@ -218,9 +218,9 @@ def _check(rc, where):
 
 
 def _ptr(t):
-    """Device (or host) address of a torch tensor / numpy array, or None."""
-    if t is None:
-        return None
+    """Device (or host) address of a torch tensor / numpy array; an address or None as it is."""
+    if t is None or isinstance(t, int):
+        return t
     if hasattr(t, "data_ptr"):
         return t.data_ptr()
     return t.ctypes.data
