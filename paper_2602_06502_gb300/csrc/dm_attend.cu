@@ -72,7 +72,7 @@ __global__ void __cluster_dims__(kPlanCl, 1, 1) __launch_bounds__(kPlanT) k_plan
     __shared__ uint64_t s_warp[32], s_cum[kFewBlocks];
     __shared__ int32_t s_offsets[kFewGroups + 1], s_prefix[kFewGroups];
     __shared__ uint32_t s_max[kFewGroups], s_n[kFewGroups];
-    __shared__ uint32_t s_bad;
+    __shared__ uint32_t s_bad, s_cuts;
     cg::cluster_group cl = cg::this_cluster();
     const uint32_t rank = cl.block_rank(), tid = threadIdx.x;
     const bool few = p.groups <= kFewGroups;
@@ -162,7 +162,8 @@ __global__ void __cluster_dims__(kPlanCl, 1, 1) __launch_bounds__(kPlanT) k_plan
         for (int kind = 0; kind < 2; ++kind) {
             const uint32_t cap = kind == 0 ? kWideRows : kNarrowRows, keys = kind == 0 ? kWideKeys : kNarrowKeys;
             uint64_t *cum = count[kind] <= kFewBlocks ? s_cum : p.w.cum[kind];
-            uint64_t units0 = 0, parts0 = 0;
+            uint64_t units0 = 0, parts0 = 0, own0 = 0;
+            if (tid == 0) s_cuts = 0;
             for (uint32_t b0 = 0; b0 < count[kind]; b0 += kPlanT) {
                 const uint32_t b = b0 + tid;
                 AttendBlock k{};
@@ -186,10 +187,12 @@ __global__ void __cluster_dims__(kPlanCl, 1, 1) __launch_bounds__(kPlanT) k_plan
                         k.pre_row = (uint32_t)(x.token - pre.token) * p.G + row0;
                     }
                 }
-                uint64_t units, parts;
+                uint64_t units, parts, owns;
                 const uint64_t at = units0 + block_scan((uint64_t)k.units * p.kv_heads, s_warp, units);
                 const uint64_t part = parts0 + block_scan(k.shared ? (uint64_t)k.rows * p.kv_heads : 0, s_warp, parts);
+                const uint64_t own = own0 + (p.groups ? block_scan(k.shared == kOwn, s_warp, owns) : owns = 0);
                 if (b < count[kind]) {
+                    if (k.shared == kOwn) p.w.own[kind][own] = b;
                     k.part0 = (uint32_t)part;
                     p.w.block[kind][b] = k;
                     p.w.cum[kind][b] = at;
@@ -197,6 +200,7 @@ __global__ void __cluster_dims__(kPlanCl, 1, 1) __launch_bounds__(kPlanT) k_plan
                 }
                 units0 += units;
                 parts0 += parts;
+                own0 += owns;
             }
             __syncthreads();
             const uint32_t S = (uint32_t)min((uint64_t)p.ctas[kind], units0);
@@ -209,8 +213,15 @@ __global__ void __cluster_dims__(kPlanCl, 1, 1) __launch_bounds__(kPlanT) k_plan
                     else hi = mid;
                 }
                 p.w.start[kind][c] = lo;
+                // the first boundary inside a tile
+                const AttendBlock k = p.w.block[kind][lo];
+                const uint64_t inside = (u - cum[lo]) % k.units;
+                if (!k.shared && inside && (c - 1) * units0 / S <= u - inside) p.w.cut[kind][atomicAdd(&s_cuts, 1u)] = c;
             }
+            __syncthreads();
             if (tid == 0) {
+                p.w.head->own[kind] = (uint32_t)own0;
+                p.w.head->cuts[kind] = s_cuts;
                 p.w.head->units[kind] = units0;
                 p.w.head->blocks[kind] = count[kind];
                 p.w.head->ctas[kind] = S;
@@ -248,8 +259,9 @@ struct Narrow {
     // pair that skipped a round could take the phase before it for its own.
     static constexpr uint32_t kSlots = D == 128 ? 4 : 8;
     static_assert(kSlots % 2 == 0, "each ring place has one pair of readers");
-    static constexpr uint32_t kRed = kSlots * 2 * kHalf;            // 2 x 16 x D floats
-    static constexpr uint32_t kQ = kRed + 2 * 16 * D * 4;           // two pieces' queries, 16 rows each
+    static constexpr uint32_t kRow = D + 8;                         // floats, no two of a half warp's stores in one bank
+    static constexpr uint32_t kRed = kSlots * 2 * kHalf;            // four warps' 8 rows
+    static constexpr uint32_t kQ = kRed + 4 * 8 * kRow * 4;         // two pieces' queries, 16 rows each
     static constexpr uint32_t kMl = kQ + 2 * 16 * D * 2;            // 4 x 16 float2
     static constexpr uint32_t kBars = kMl + 4 * 16 * 8;             // full, empty per slot, then the give-up word
     static constexpr uint32_t kBytes = kBars + 16 * kSlots + 16 + 1024;   // with room to align
@@ -443,78 +455,63 @@ __global__ void __launch_bounds__(160, kNarrowPerSm)
         }
         c += 2 * w.units;
         buf ^= 1;
-        // the four warps' parts: maxima and sums first, then the outputs in a fixed order
+        // The four warps' parts, eight rows at a time: each warp leaves its
+        // own, then adds up a quarter of the dims, in the order of the warps.
 #pragma unroll
         for (int r = 0; r < 2; ++r) {
             l[r] += __shfl_xor_sync(~0u, l[r], 1);
             l[r] += __shfl_xor_sync(~0u, l[r], 2);
             if (t4 == 0) s_ml[wid * 16 + g + 8 * r] = make_float2(m[r], l[r]);
         }
-        bar_consumers();
-        float M[2], L[2];
+        const bool whole = w.whole();
+        const uint64_t part = whole ? 0 : w.part_row(p);
 #pragma unroll
         for (int r = 0; r < 2; ++r) {
+            if (8u * r >= w.k.rows) break;
+            if (r) bar_consumers();   // the first eight have been added up
+#pragma unroll
+            for (int i = 0; i < D / 8; ++i)
+                *reinterpret_cast<float2 *>(red + (wid * 8 + g) * N::kRow + i * 8 + t4 * 2) = make_float2(o[i][2 * r], o[i][2 * r + 1]);
+            bar_consumers();
+            constexpr uint32_t kMine = D / 16;   // dims of a thread
+            const uint32_t row = 8 * r + g, col = wid * (D / 4) + t4 * kMine;
             float2 x[4];
 #pragma unroll
-            for (int i = 0; i < 4; ++i) x[i] = s_ml[i * 16 + g + 8 * r];
-            M[r] = fmaxf(fmaxf(x[0].x, x[1].x), fmaxf(x[2].x, x[3].x));
-            const float base = M[r] == -INFINITY ? 0.f : M[r];
-            L[r] = 0.f;
+            for (int i = 0; i < 4; ++i) x[i] = s_ml[i * 16 + row];
+            const float M = fmaxf(fmaxf(x[0].x, x[1].x), fmaxf(x[2].x, x[3].x)), base = M == -INFINITY ? 0.f : M;
+            float L = 0.f, acc[kMine];
 #pragma unroll
-            for (int i = 0; i < 4; ++i) L[r] += x[i].y * exp2_(x[i].x - base);
-            const float f = exp2_(m[r] - base);
+            for (uint32_t e = 0; e < kMine; ++e) acc[e] = 0.f;
 #pragma unroll
-            for (int i = 0; i < D / 8; ++i) {
-                o[i][2 * r] *= f;
-                o[i][2 * r + 1] *= f;
-            }
-        }
-        auto cell = [&](uint32_t part, int i, int r) { return reinterpret_cast<float2 *>(red + part * 16 * D + (g + 8 * r) * D + i * 8 + t4 * 2); };
-        if (wid >= 2)
+            for (int i = 0; i < 4; ++i) {
+                const float f = exp2_(x[i].x - base);
+                L += x[i].y * f;
 #pragma unroll
-            for (int i = 0; i < D / 8; ++i)
-#pragma unroll
-                for (int r = 0; r < 2; ++r) *cell(wid - 2, i, r) = make_float2(o[i][2 * r], o[i][2 * r + 1]);
-        bar_consumers();
-        if (wid < 2)
-#pragma unroll
-            for (int i = 0; i < D / 8; ++i)
-#pragma unroll
-                for (int r = 0; r < 2; ++r) {
-                    const float2 x = *cell(wid, i, r);
-                    o[i][2 * r] += x.x;
-                    o[i][2 * r + 1] += x.y;
-                    if (wid == 1) *cell(1, i, r) = make_float2(o[i][2 * r], o[i][2 * r + 1]);
+                for (uint32_t e = 0; e < kMine; e += 4) {
+                    const float4 y = *reinterpret_cast<const float4 *>(red + (i * 8 + g) * N::kRow + col + e);
+                    acc[e] += y.x * f;
+                    acc[e + 1] += y.y * f;
+                    acc[e + 2] += y.z * f;
+                    acc[e + 3] += y.w * f;
                 }
-        bar_consumers();
-        if (wid == 0) {
-            const bool whole = w.whole();
-            const uint64_t part = whole ? 0 : w.part_row(p);
-#pragma unroll
-            for (int r = 0; r < 2; ++r) {
-                const uint32_t row = g + 8 * r;
-                if (row >= w.k.rows) continue;
-                const Row at = row_at(p, w.k, row);
-                const uint64_t tok = (uint64_t)(w.k.token + at.token);
-                const uint32_t h = w.head * p.G + at.head;
+            }
+            if (row < w.k.rows) {
                 if (whole) {
-                    const float inv = L[r] > 0.f ? 1.f / L[r] : 0.f;
-                    char *dst = p.o + tok * p.o_token + h * p.o_head;
+                    const Row at = row_at(p, w.k, row);
+                    const uint64_t tok = (uint64_t)(w.k.token + at.token);
+                    const uint32_t h = w.head * p.G + at.head;
+                    const float inv = L > 0.f ? 1.f / L : 0.f;
+                    char *dst = p.o + tok * p.o_token + h * p.o_head + col * 2;
 #pragma unroll
-                    for (int i = 0; i < D / 8; ++i) {
-                        const float2 x = *cell(1, i, r);
-                        *reinterpret_cast<uint32_t *>(dst + i * 16 + t4 * 4) =
-                            Pack2<T>::pack((o[i][2 * r] + x.x) * inv, (o[i][2 * r + 1] + x.y) * inv);
-                    }
-                    if (p.lse && t4 == 0) p.lse[tok * p.q_heads + h] = L[r] > 0.f ? (M[r] + log2f(L[r])) * 0.69314718056f : -INFINITY;
+                    for (uint32_t e = 0; e < kMine; e += 4)
+                        *reinterpret_cast<uint2 *>(dst + e * 2) =
+                            make_uint2(Pack2<T>::pack(acc[e] * inv, acc[e + 1] * inv), Pack2<T>::pack(acc[e + 2] * inv, acc[e + 3] * inv));
+                    if (p.lse && wid == 0 && t4 == 0) p.lse[tok * p.q_heads + h] = L > 0.f ? (M + log2f(L)) * 0.69314718056f : -INFINITY;
                 } else {
-                    float *dst = p.w.part[1] + (part + row) * D;
 #pragma unroll
-                    for (int i = 0; i < D / 8; ++i) {
-                        const float2 x = *cell(1, i, r);
-                        *reinterpret_cast<float2 *>(dst + i * 8 + t4 * 2) = make_float2(o[i][2 * r] + x.x, o[i][2 * r + 1] + x.y);
-                    }
-                    if (t4 == 0) p.w.ml[1][part + row] = make_float2(M[r], L[r]);
+                    for (uint32_t e = 0; e < kMine; e += 4)
+                        *reinterpret_cast<float4 *>(p.w.part[1] + (part + row) * D + col + e) = make_float4(acc[e], acc[e + 1], acc[e + 2], acc[e + 3]);
+                    if (wid == 0 && t4 == 0) p.w.ml[1][part + row] = make_float2(M, L);
                 }
             }
         }
@@ -524,83 +521,114 @@ __global__ void __launch_bounds__(160, kNarrowPerSm)
 
 // -- joining parts --------------------------------------------------------------------
 
-// CTAs walk the tiles of sequences' own keys; a warp takes a row: its parts of
-// the group's prefix, and those of its own keys in the order of the CTAs that
-// left them.  A tile that went straight to the output has nothing to do.
-// 32 parts' maxima and sums are looked at together, so that the parts
-// themselves are independent loads.  Bound: latency, then L2 (4 D + 8 bytes a
-// row and part).
-constexpr uint32_t kJoinPerSm = 4;
-
+// A warp takes a row of a shared group's sequence (its parts of the prefix,
+// then those of its own keys) or of another tile that CTAs share, parts in the
+// order of the CTAs that left them.  32 parts' maxima and sums are looked at
+// together, so that the parts themselves are independent loads.  Bound:
+// latency, then L2 (4 D + 8 bytes a row and part).
 template <class T, int D>
 __global__ void __launch_bounds__(256) k_attend_join(AttendArgs p) {
     constexpr int V = D / 32;
     const PlanHead h = *p.w.head;
-    const uint32_t lane = threadIdx.x & 31, wid = threadIdx.x / 32;
+    const uint32_t lane = threadIdx.x & 31;
     if (has_err(p.status) || !h.ok) return;
-    const uint64_t tiles = (uint64_t)(h.blocks[0] + h.blocks[1]) * p.kv_heads;
-    for (uint64_t t = blockIdx.x; t < tiles; t += gridDim.x) {
-        const uint32_t bb = (uint32_t)(t / p.kv_heads), head = (uint32_t)(t % p.kv_heads);
-        const int kind = bb >= h.blocks[0];
-        const uint32_t b = kind ? bb - h.blocks[0] : bb;
+    const uint64_t own1 = (uint64_t)h.own[1] * p.kv_heads * kNarrowRows, own0 = own1 + (uint64_t)h.own[0] * p.kv_heads * kShareRows;
+    const uint64_t cut0 = own0 + (uint64_t)h.cuts[0] * kWideRows, jobs = cut0 + (uint64_t)h.cuts[1] * kNarrowRows;
+    for (uint64_t t = blockIdx.x * 8ull + threadIdx.x / 32; t < jobs; t += gridDim.x * 8ull) {
+        uint32_t b, head, r;
+        int kind;
+        if (t < own0) {
+            kind = t < own1;
+            const uint64_t x = kind ? t : t - own1;
+            const uint32_t cap = kind ? kNarrowRows : kShareRows;
+            const uint32_t tile = (uint32_t)(x / cap);
+            r = (uint32_t)(x % cap);
+            b = (kind ? p.w.own[1] : p.w.own[0])[tile / p.kv_heads];
+            head = tile % p.kv_heads;
+        } else {
+            kind = t >= cut0;
+            const uint64_t x = kind ? t - cut0 : t - own0;
+            const uint32_t cap = kind ? kNarrowRows : kWideRows;
+            r = (uint32_t)(x % cap);
+            const uint32_t c = (kind ? p.w.cut[1] : p.w.cut[0])[x / cap];
+            b = (kind ? p.w.start[1] : p.w.start[0])[c];
+            const uint64_t u = c * (kind ? h.units[1] : h.units[0]) / (kind ? h.ctas[1] : h.ctas[0]);
+            head = (uint32_t)((u - (kind ? p.w.cum[1] : p.w.cum[0])[b]) / (kind ? p.w.block[1] : p.w.block[0])[b].units);
+        }
         const AttendBlock k = (kind ? p.w.block[1] : p.w.block[0])[b];
-        if (k.shared == kPrefix) continue;
-        // the CTAs of a tile, and where row r of it is among CTA c's parts
+        if (r >= k.rows) continue;
+        // a tile's parts: how many, and where row r of the i-th is
         struct Parts {
-            uint32_t c0, n;
-            uint64_t at, step;   // of the first; between CTAs' (a cut tile's first is one place off)
-            uint32_t odd;
+            const float *part;
+            const float2 *ml;
+            uint32_t n, step, odd;   // a cut tile's first part is `odd` rows off
+            uint64_t at;
+            __device__ uint64_t row(uint32_t i) const { return at + (uint64_t)i * step + (i == 0 ? odd : 0); }
         };
-        auto parts = [&](int kd, uint32_t blk, const AttendBlock &x) {
+        auto parts = [&](int kd, uint32_t blk, const AttendBlock &x, uint32_t row) {
             const uint64_t u0 = (kd ? p.w.cum[1] : p.w.cum[0])[blk] + (uint64_t)head * x.units, U = kd ? h.units[1] : h.units[0];
             const uint32_t cap = kd ? kNarrowRows : kWideRows, S = kd ? h.ctas[1] : h.ctas[0];
             const uint32_t c0 = cta_of(u0, U, S), c1 = cta_of(u0 + x.units - 1, U, S);
-            if (x.shared) return Parts{c0, c1 - c0 + 1, x.part0 + (uint64_t)head * x.rows + (uint64_t)cap * c0, cap, 0};
-            return Parts{c0, c1 - c0 + 1, (kd ? p.w.shared_rows[1] : p.w.shared_rows[0]) + (uint64_t)cap * 2 * c0, 2 * cap, cap};
+            Parts q{kd ? p.w.part[1] : p.w.part[0], kd ? p.w.ml[1] : p.w.ml[0], c1 - c0 + 1, cap, 0, 0};
+            if (x.shared) {
+                q.at = x.part0 + (uint64_t)head * x.rows + (uint64_t)cap * c0 + row;
+            } else {
+                q.at = (kd ? p.w.shared_rows[1] : p.w.shared_rows[0]) + (uint64_t)cap * 2 * c0 + row;
+                q.step = 2 * cap;
+                q.odd = cap;
+            }
+            return q;
         };
-        const Parts own = parts(kind, b, k);
-        if (!k.shared && own.n == 1) continue;
-        const uint32_t pre_cap = k.pre_kind ? kNarrowRows : kWideRows;
-        for (uint32_t r = wid; r < k.rows; r += 8) {
+        Parts pre{};
+        if (k.shared) {
+            const uint32_t cap = k.pre_kind ? kNarrowRows : kWideRows, row = k.pre_row + r, blk = k.pre + row / cap;
+            pre = parts((int)k.pre_kind, blk, (k.pre_kind ? p.w.block[1] : p.w.block[0])[blk], row % cap);
+        }
+        const Parts own = parts(kind, b, k, r);
+        const uint32_t N = pre.n + own.n;
+        {
             float acc[V], M = -INFINITY, L = 0.f;
 #pragma unroll
             for (int v = 0; v < V; ++v) acc[v] = 0.f;
-            auto join = [&](int kd, const Parts &x, uint32_t row) {
-                const float *part = kd ? p.w.part[1] : p.w.part[0];
-                const float2 *mls = kd ? p.w.ml[1] : p.w.ml[0];
-                for (uint32_t i0 = 0; i0 < x.n; i0 += 32) {
-                    const uint32_t n = min(32u, x.n - i0), i = i0 + lane;
-                    const uint64_t mine = x.at + i * x.step + (i == 0 ? x.odd : 0) + row;
-                    const float2 ml = lane < n ? mls[mine] : make_float2(-INFINITY, 0.f);
-                    float now = ml.x;
+            constexpr uint32_t kAhead = 8;
+            float y[kAhead][V];
+            auto load = [&](uint32_t i0) {
 #pragma unroll
-                    for (int d = 16; d; d /= 2) now = fmaxf(now, __shfl_xor_sync(~0u, now, d));
-                    now = fmaxf(now, M);
-                    const float base = now == -INFINITY ? 0.f : now, f = exp2_(M - base), fi = exp2_(ml.x - base);
-                    float l = ml.y * fi;
-#pragma unroll
-                    for (int d = 16; d; d /= 2) l += __shfl_xor_sync(~0u, l, d);
-                    L = L * f + l;
-                    M = now;
-#pragma unroll
-                    for (int v = 0; v < V; ++v) acc[v] *= f;
-#pragma unroll 8
-                    for (uint32_t j = 0; j < n; ++j) {
-                        const float fj = __shfl_sync(~0u, fi, j);
-                        const float *src = part + (x.at + (i0 + j) * x.step + (i0 + j == 0 ? x.odd : 0) + row) * D + lane * V;
-                        float y[V];
-                        if constexpr (V == 4) *reinterpret_cast<float4 *>(y) = *reinterpret_cast<const float4 *>(src);
-                        else *reinterpret_cast<float2 *>(y) = *reinterpret_cast<const float2 *>(src);
-#pragma unroll
-                        for (int v = 0; v < V; ++v) acc[v] += y[v] * fj;
-                    }
+                for (uint32_t j = 0; j < kAhead; ++j) {
+                    const uint32_t i = i0 + j;
+                    if (i >= N) break;
+                    const float *src = (i < pre.n ? pre.part + pre.row(i) * D : own.part + own.row(i - pre.n) * D) + lane * V;
+                    if constexpr (V == 4) *reinterpret_cast<float4 *>(y[j]) = *reinterpret_cast<const float4 *>(src);
+                    else *reinterpret_cast<float2 *>(y[j]) = *reinterpret_cast<const float2 *>(src);
                 }
             };
-            if (k.shared) {
-                const uint32_t row = k.pre_row + r, blk = k.pre + row / pre_cap;
-                join((int)k.pre_kind, parts((int)k.pre_kind, blk, (k.pre_kind ? p.w.block[1] : p.w.block[0])[blk]), row % pre_cap);
+            for (uint32_t i0 = 0; i0 < N; i0 += 32) {
+                const uint32_t i = i0 + lane;
+                const float2 ml = i >= N ? make_float2(-INFINITY, 0.f) : i < pre.n ? pre.ml[pre.row(i)] : own.ml[own.row(i - pre.n)];
+                load(i0);
+                float now = ml.x;
+#pragma unroll
+                for (int d = 16; d; d /= 2) now = fmaxf(now, __shfl_xor_sync(~0u, now, d));
+                now = fmaxf(now, M);
+                const float base = now == -INFINITY ? 0.f : now, f = exp2_(M - base), fi = exp2_(ml.x - base);
+                float l = ml.y * fi;
+#pragma unroll
+                for (int d = 16; d; d /= 2) l += __shfl_xor_sync(~0u, l, d);
+                L = L * f + l;
+                M = now;
+#pragma unroll
+                for (int v = 0; v < V; ++v) acc[v] *= f;
+                for (uint32_t j0 = 0; j0 < 32 && i0 + j0 < N; j0 += kAhead) {
+                    if (j0) load(i0 + j0);
+#pragma unroll
+                    for (uint32_t j = 0; j < kAhead; ++j) {
+                        const float fj = __shfl_sync(~0u, fi, j0 + j);
+                        if (i0 + j0 + j >= N) break;
+#pragma unroll
+                        for (int v = 0; v < V; ++v) acc[v] += y[j][v] * fj;
+                    }
+                }
             }
-            join(kind, own, r);
             const Row at = row_at(p, k, r);
             const uint64_t tok = (uint64_t)(k.token + at.token);
             const uint32_t qh = head * p.G + at.head;
@@ -645,12 +673,14 @@ bool page_map(CUtensorMap *m, const dm_cache *c, void *pool, uint32_t layer, uin
 }
 
 template <class T, int D>
-cudaError_t launch_rest(const AttendArgs &p, const CUtensorMap &mk, const CUtensorMap &mv, cudaStream_t st) {
+cudaError_t launch_rest(const AttendArgs &p, uint64_t rows, const CUtensorMap &mk, const CUtensorMap &mv, cudaStream_t st) {
     static SmemOptIn opt;
     DM_TRY(opt_in_smem(opt, Narrow<D>::kBytes, k_attend_narrow<T, D>));
     k_attend_narrow<T, D><<<p.ctas[1], 160, Narrow<D>::kBytes, st>>>(mk, mv, p);
     DM_TRY(cudaGetLastError());
-    k_attend_join<T, D><<<p.ctas[0] * kJoinPerSm, 256, 0, st>>>(p);
+    // a warp per row, or as many as the GPU holds
+    const uint64_t warps = std::min<uint64_t>(rows, (uint64_t)p.ctas[0] * 64);
+    k_attend_join<T, D><<<(uint32_t)((warps + 7) / 8), 256, 0, st>>>(p);
     return cudaGetLastError();
 }
 
@@ -708,10 +738,12 @@ extern "C" dm_status dm_cache_attend(const dm_cache *c, const dm_plan *pl, const
     // so few rows that no block of them is wide
     cudaError_t e = (uint64_t)pl->tokens * s.G <= kNarrowRows ? cudaSuccess : launch_attend_wide(c, p, mk, mv, st);
     if (e == cudaSuccess) {
+        // narrow tiles count 16 rows in the joining
+        const uint64_t rows = (uint64_t)pl->tokens * s.q_heads + (uint64_t)pl->n * c->kv_heads * kNarrowRows;
         if (c->dtype == DM_BF16)
-            e = c->head_dim == 64 ? launch_rest<__nv_bfloat16, 64>(p, mk, mv, st) : launch_rest<__nv_bfloat16, 128>(p, mk, mv, st);
+            e = c->head_dim == 64 ? launch_rest<__nv_bfloat16, 64>(p, rows, mk, mv, st) : launch_rest<__nv_bfloat16, 128>(p, rows, mk, mv, st);
         else
-            e = c->head_dim == 64 ? launch_rest<__half, 64>(p, mk, mv, st) : launch_rest<__half, 128>(p, mk, mv, st);
+            e = c->head_dim == 64 ? launch_rest<__half, 64>(p, rows, mk, mv, st) : launch_rest<__half, 128>(p, rows, mk, mv, st);
     }
     return e == cudaSuccess ? DM_OK : DM_ERR_CUDA;
 }

@@ -46,6 +46,8 @@ struct PlanHead {
     uint64_t units[2];    // wide, narrow
     uint32_t blocks[2];
     uint32_t ctas[2];     // that have units
+    uint32_t own[2];      // blocks of shared groups' sequences
+    uint32_t cuts[2];     // other tiles that more than one CTA has part of
     uint32_t ok, pad;
 };
 
@@ -63,6 +65,8 @@ struct PlanWork {
     uint64_t *cum[2];         // units before each block
     uint32_t *start[2];       // per CTA: the block of its first unit
     uint32_t *owner[2];       // per block: its entity
+    uint32_t *own[2];         // the blocks of shared groups' sequences
+    uint32_t *cut[2];         // per other cut tile: the second CTA that has part of it
     PlanEntity *entity;       // groups, then sequences
     uint32_t *group_max, *group_n;   // most rows of a sequence; sequences with rows
     float *part[2];           // rows x D
@@ -114,6 +118,8 @@ inline uint64_t plan_work(const PlanShape &s, void *base, PlanWork &w) {
         w.cum[k] = (uint64_t *)take(8ull * s.blocks[k]);
         w.start[k] = (uint32_t *)take(4ull * s.ctas[k]);
         w.owner[k] = (uint32_t *)take(4ull * s.blocks[k]);
+        w.own[k] = (uint32_t *)take(4ull * s.blocks[k]);
+        w.cut[k] = (uint32_t *)take(4ull * s.ctas[k]);
     }
     w.entity = (PlanEntity *)take(sizeof(PlanEntity) * (s.n + (uint64_t)s.groups));
     w.group_max = (uint32_t *)take(4ull * s.groups);
