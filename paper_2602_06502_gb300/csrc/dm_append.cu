@@ -65,16 +65,30 @@ __device__ __forceinline__ uint4 pack(const float *f) {
     return x;
 }
 
-// A warp: 32 / (D / 8) heads at a time of one token, per_warp heads in all
-// (the token's heads in the order queries, keys, values).
+// A warp: per_warp heads of one token (its heads in the order queries, keys,
+// values), kAhead x 32 / (D / 8) of them at a time.  The first are loaded before
+// the token's sequence is known, the others while the ones before them are
+// computed.
+constexpr uint32_t kAhead = 4;
+
 template <class T, int D, bool kInterleaved>
-__global__ void __launch_bounds__(256) k_append(AppendArgs p) {
+__global__ void __launch_bounds__(256, 3) k_append(AppendArgs p) {
     constexpr uint32_t L = D / 8, H = 32 / L;
     const uint32_t lane = threadIdx.x & 31, l = lane % L, sub = lane / L;
     const uint32_t heads = p.q_heads + 2 * p.kv_heads, parts = (heads + p.per_warp - 1) / p.per_warp;
     const uint64_t warp = (uint64_t)blockIdx.x * (blockDim.x / 32) + threadIdx.x / 32;
     const uint32_t t = (uint32_t)(warp / parts), h0 = (uint32_t)(warp % parts) * p.per_warp;
     if (t >= p.tokens || has_err(p.status)) return;
+    const uint32_t h1 = min(heads, h0 + p.per_warp), k0 = p.q_heads, v0 = k0 + p.kv_heads;
+    uint4 raw[kAhead];
+    auto load = [&](uint32_t hb) {
+#pragma unroll
+        for (uint32_t u = 0; u < kAhead; ++u) {
+            const uint32_t h = hb + u * H + sub;
+            if (h < h1) raw[u] = __ldcs((h < k0 ? p.q + t * p.qt + h * p.qh : h < v0 ? p.k + t * p.kt + (h - k0) * p.kh : p.v + t * p.vt + (h - v0) * p.vh) + l);
+        }
+    };
+    load(h0);
     // the token's sequence: the last i with offsets[i] <= t
     const int32_t first = p.offsets[0], last = p.offsets[p.n];
     if (first < 0 || last < first || (uint32_t)last > p.tokens) {
@@ -110,39 +124,42 @@ __global__ void __launch_bounds__(256) k_append(AppendArgs p) {
             *reinterpret_cast<float4 *>(c + i) = *reinterpret_cast<const float4 *>(p.cos + at + i);
             *reinterpret_cast<float4 *>(sn + i) = *reinterpret_cast<const float4 *>(p.sin + at + i);
         }
+        if (!kInterleaved && low)   // a cos - b sin below, b cos + a sin above
+#pragma unroll
+            for (int i = 0; i < F; ++i) sn[i] = -sn[i];
     }
     const uint32_t partner = sub * L + (low ? l + half / 8 : l - half / 8) % L;
-    float qw[8], kw[8];
-    if (p.qw) unpack<T>(p.qw[l], qw);
-    if (p.kw) unpack<T>(p.kw[l], kw);
-    const uint32_t h1 = min(heads, h0 + p.per_warp);
-    constexpr int U = 4;   // heads of a lane whose loads are in flight together
-    for (uint32_t hb = h0; hb < h1; hb += H * U) {
-        uint4 raw[U];
+    const uint4 qw = p.qw ? p.qw[l] : make_uint4(0, 0, 0, 0), kw = p.kw ? p.kw[l] : make_uint4(0, 0, 0, 0);
+    for (uint32_t hb = h0; hb < h1; hb += H * kAhead) {
+        uint4 now[kAhead];
 #pragma unroll
-        for (int u = 0; u < U; ++u) {
+        for (uint32_t u = 0; u < kAhead; ++u) now[u] = raw[u];
+        if (hb + H * kAhead < h1) load(hb + H * kAhead);
+#pragma unroll
+        for (uint32_t u = 0; u < kAhead; ++u) {
             const uint32_t h = hb + u * H + sub;
-            const uint4 *src = h < p.q_heads                ? p.q + t * p.qt + h * p.qh
-                               : h < p.q_heads + p.kv_heads ? p.k + t * p.kt + (h - p.q_heads) * p.kh
-                                                            : p.v + t * p.vt + (h - p.q_heads - p.kv_heads) * p.vh;
-            if (h < h1) raw[u] = src[l];
-        }
-#pragma unroll
-        for (int u = 0; u < U; ++u) {
-            const uint32_t h = hb + u * H + sub;
-            const bool is_q = h < p.q_heads, is_v = h >= p.q_heads + p.kv_heads;
-            float x[8], y[8];
-            unpack<T>(h < h1 ? raw[u] : make_uint4(0, 0, 0, 0), x);
-            float ss = 0.f;
-#pragma unroll
-            for (int i = 0; i < 8; ++i) ss += x[i] * x[i];
-#pragma unroll
-            for (uint32_t d = 1; d < L; d *= 2) ss += __shfl_xor_sync(~0u, ss, d);
-            if (is_q ? p.qw != nullptr : p.kw != nullptr) {
-                const float r = rsqrtf(ss * (1.f / D) + p.eps);
-#pragma unroll
-                for (int i = 0; i < 8; ++i) x[i] = x[i] * r * (is_q ? qw[i] : kw[i]);
+            if (hb + u * H >= h1) break;   // the whole warp
+            const bool is_q = h < k0, is_v = h >= v0;
+            if (__all_sync(~0u, is_v)) {
+                if (h < h1) __stcs(p.vc + slot + (uint64_t)(h - v0) * p.head_step + l, now[u]);
+                continue;
             }
+            float x[8];
+            unpack<T>(now[u], x);
+            if (is_q ? p.qw != nullptr : p.kw != nullptr) {
+                // a head's lanes come here together
+                float ss = 0.f, w[8];
+#pragma unroll
+                for (int i = 0; i < 8; ++i) ss += x[i] * x[i];
+                const uint32_t mask = (L == 32 ? ~0u : ((1u << L) - 1) << (sub * L));
+#pragma unroll
+                for (uint32_t d = 1; d < L; d *= 2) ss += __shfl_xor_sync(mask, ss, d);
+                const float r = rsqrtf(ss * (1.f / D) + p.eps);
+                unpack<T>(is_q ? qw : kw, w);
+#pragma unroll
+                for (int i = 0; i < 8; ++i) x[i] = x[i] * r * w[i];
+            }
+            __syncwarp();
             if (kInterleaved) {
                 if (turns)
 #pragma unroll
@@ -152,17 +169,17 @@ __global__ void __launch_bounds__(256) k_append(AppendArgs p) {
                         x[2 * i + 1] = b * c[i % F] + a * sn[i % F];
                     }
             } else if (p.rope_dim) {
+                float y[8];
 #pragma unroll
                 for (int i = 0; i < 8; ++i) y[i] = __shfl_sync(~0u, x[i], partner);
                 if (turns)
 #pragma unroll
-                    for (int i = 0; i < 8; ++i)
-                        x[i] = low ? x[i] * c[i % F] - y[i] * sn[i % F] : x[i] * c[i % F] + y[i] * sn[i % F];
+                    for (int i = 0; i < 8; ++i) x[i] = x[i] * c[i % F] + y[i] * sn[i % F];
             }
             if (h < h1) {
-                if (is_q) p.q_out[t * p.ot + h * p.oh + l] = pack<T>(x);
-                else if (is_v) p.vc[slot + (uint64_t)(h - p.q_heads - p.kv_heads) * p.head_step + l] = raw[u];
-                else p.kc[slot + (uint64_t)(h - p.q_heads) * p.head_step + l] = pack<T>(x);
+                if (is_q) __stcs(p.q_out + t * p.ot + h * p.oh + l, pack<T>(x));
+                else if (is_v) __stcs(p.vc + slot + (uint64_t)(h - v0) * p.head_step + l, now[u]);
+                else __stcs(p.kc + slot + (uint64_t)(h - k0) * p.head_step + l, pack<T>(x));
             }
         }
     }
@@ -204,12 +221,13 @@ extern "C" dm_status dm_cache_append(const dm_cache *c, const dm_append_args *a,
     p.n = a->n, p.tokens = a->tokens, p.q_heads = a->q_heads, p.kv_heads = c->kv_heads, p.B = c->page_tokens;
     p.pages = c->pages, p.max_seqs = c->max_seqs, p.max_blocks = c->max_blocks;
     p.rope_rows = a->rope_rows, p.rope_dim = a->rope_dim, p.eps = a->eps;
-    // heads of a token per warp: all of one round of loads, halved while the
-    // warps would not fill the SMs
+    // heads of a token per warp: all of them, fewer while the warps would not
+    // fill the SMs (48 heads of 64 tokens: 8 warps a token)
     const uint32_t heads = a->q_heads + 2 * c->kv_heads, once = 32 / (c->head_dim / 8);
-    p.per_warp = once * 4;
-    while (p.per_warp > once && (uint64_t)a->tokens * ((heads + p.per_warp - 1) / p.per_warp) < (uint64_t)sm_count() * 32)
-        p.per_warp /= 2;
+    p.per_warp = (heads + once - 1) / once * once;
+    const uint64_t enough = (uint64_t)sm_count() * 24;
+    while (p.per_warp > once && (uint64_t)a->tokens * ((heads + p.per_warp - 1) / p.per_warp) < enough)
+        p.per_warp = (p.per_warp / 2 + once - 1) / once * once;
     const uint64_t warps = (uint64_t)a->tokens * ((heads + p.per_warp - 1) / p.per_warp);
     if ((warps + 7) / 8 > 0x7FFFFFFFu) return DM_ERR_INVALID_ARG;
     const uint32_t grid = (uint32_t)((warps + 7) / 8);
