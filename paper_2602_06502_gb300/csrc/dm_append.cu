@@ -11,6 +11,7 @@
 // Bound: HBM bandwidth, 2 bytes read and 2 written per value; a few tokens
 // alone, the latency of one launch.
 #include <algorithm>
+#include <type_traits>
 
 #include "dm_cache.cuh"
 
@@ -66,29 +67,35 @@ __device__ __forceinline__ uint4 pack(const float *f) {
 }
 
 // A warp: per_warp heads of one token (its heads in the order queries, keys,
-// values), kAhead x 32 / (D / 8) of them at a time.  The first are loaded before
-// the token's sequence is known, the others while the ones before them are
-// computed.
-constexpr uint32_t kAhead = 4;
+// values), 32 / (D / 8) of them at a time and kAhead such rounds in flight.  The
+// first are loaded before the token's sequence is known.  Instructions are the
+// next bound after HBM (3,600 a token of 48 heads in a form that chose between
+// queries, keys and values head by head; 228 us at 46,000 tokens against 178
+// so), hence a loop for each of the three.
+constexpr uint32_t kAhead = 4, kThreads = 128;
 
 template <class T, int D, bool kInterleaved>
-__global__ void __launch_bounds__(256, 3) k_append(AppendArgs p) {
+__global__ void __launch_bounds__(kThreads, 6) k_append(AppendArgs p) {
     constexpr uint32_t L = D / 8, H = 32 / L;
     const uint32_t lane = threadIdx.x & 31, l = lane % L, sub = lane / L;
     const uint32_t heads = p.q_heads + 2 * p.kv_heads, parts = (heads + p.per_warp - 1) / p.per_warp;
-    const uint64_t warp = (uint64_t)blockIdx.x * (blockDim.x / 32) + threadIdx.x / 32;
+    const uint64_t warp = (uint64_t)blockIdx.x * (kThreads / 32) + threadIdx.x / 32;
     const uint32_t t = (uint32_t)(warp / parts), h0 = (uint32_t)(warp % parts) * p.per_warp;
     if (t >= p.tokens || has_err(p.status)) return;
     const uint32_t h1 = min(heads, h0 + p.per_warp), k0 = p.q_heads, v0 = k0 + p.kv_heads;
     uint4 raw[kAhead];
-    auto load = [&](uint32_t hb) {
+    // heads h .. end of a segment from here on, this lane's first being h + sub
+    auto load = [&](const uint4 *src, uint64_t step, uint32_t h, uint32_t end) {
 #pragma unroll
-        for (uint32_t u = 0; u < kAhead; ++u) {
-            const uint32_t h = hb + u * H + sub;
-            if (h < h1) raw[u] = __ldcs((h < k0 ? p.q + t * p.qt + h * p.qh : h < v0 ? p.k + t * p.kt + (h - k0) * p.kh : p.v + t * p.vt + (h - v0) * p.vh) + l);
-        }
+        for (uint32_t u = 0; u < kAhead; ++u)
+            if (h + u * H + sub < end) raw[u] = __ldcs(src + u * H * step);
     };
-    load(h0);
+    const uint4 *src_q = p.q + t * p.qt + (h0 + sub) * p.qh + l;
+    const uint32_t hk = max(h0, k0), hv = max(h0, v0);
+    const uint4 *src_k = p.k + t * p.kt + (hk - k0 + sub) * p.kh + l, *src_v = p.v + t * p.vt + (hv - v0 + sub) * p.vh + l;
+    if (h0 < k0) load(src_q, p.qh, h0, min(h1, k0));
+    else if (h0 < v0) load(src_k, p.kh, h0, min(h1, v0));
+    else load(src_v, p.vh, h0, h1);
     // the token's sequence: the last i with offsets[i] <= t
     const int32_t first = p.offsets[0], last = p.offsets[p.n];
     if (first < 0 || last < first || (uint32_t)last > p.tokens) {
@@ -129,66 +136,69 @@ __global__ void __launch_bounds__(256, 3) k_append(AppendArgs p) {
             for (int i = 0; i < F; ++i) sn[i] = -sn[i];
     }
     const uint32_t partner = sub * L + (low ? l + half / 8 : l - half / 8) % L;
-    const uint4 qw = p.qw ? p.qw[l] : make_uint4(0, 0, 0, 0), kw = p.kw ? p.kw[l] : make_uint4(0, 0, 0, 0);
-    for (uint32_t hb = h0; hb < h1; hb += H * kAhead) {
-        uint4 now[kAhead];
+    // heads h .. end: normed and rotated (kTurn) or as they are, loads ahead
+    auto run = [&](auto turn, const uint4 *src, uint64_t step, uint4 *dst, uint64_t dst_step, uint32_t h, uint32_t end, const uint4 *weight,
+                   bool loaded) {
+        constexpr bool kTurn = decltype(turn)::value;
+        if (h >= end) return;
+        if (!loaded) load(src, step, h, end);
+        float w[8];
+        if (kTurn && weight) unpack<T>(weight[l], w);
+        for (; h < end; h += H * kAhead) {
+            uint4 now[kAhead];
 #pragma unroll
-        for (uint32_t u = 0; u < kAhead; ++u) now[u] = raw[u];
-        if (hb + H * kAhead < h1) load(hb + H * kAhead);
+            for (uint32_t u = 0; u < kAhead; ++u) now[u] = raw[u];
+            src += kAhead * H * step;
+            load(src, step, h + H * kAhead, end);
 #pragma unroll
-        for (uint32_t u = 0; u < kAhead; ++u) {
-            const uint32_t h = hb + u * H + sub;
-            if (hb + u * H >= h1) break;   // the whole warp
-            const bool is_q = h < k0, is_v = h >= v0;
-            if (__all_sync(~0u, is_v)) {
-                if (h < h1) __stcs(p.vc + slot + (uint64_t)(h - v0) * p.head_step + l, now[u]);
-                continue;
-            }
-            float x[8];
-            unpack<T>(now[u], x);
-            if (is_q ? p.qw != nullptr : p.kw != nullptr) {
-                // a head's lanes come here together
-                float ss = 0.f, w[8];
+            for (uint32_t u = 0; u < kAhead; ++u) {
+                if (h + u * H >= end) break;   // the whole warp
+                uint4 y = now[u];
+                if constexpr (kTurn) {
+                    float x[8];
+                    unpack<T>(y, x);
+                    if (weight) {
+                        float ss = 0.f;
 #pragma unroll
-                for (int i = 0; i < 8; ++i) ss += x[i] * x[i];
-                const uint32_t mask = (L == 32 ? ~0u : ((1u << L) - 1) << (sub * L));
+                        for (int i = 0; i < 8; ++i) ss += x[i] * x[i];
 #pragma unroll
-                for (uint32_t d = 1; d < L; d *= 2) ss += __shfl_xor_sync(mask, ss, d);
-                const float r = rsqrtf(ss * (1.f / D) + p.eps);
-                unpack<T>(is_q ? qw : kw, w);
+                        for (uint32_t d = 1; d < L; d *= 2) ss += __shfl_xor_sync(~0u, ss, d);
+                        const float r = rsqrtf(ss * (1.f / D) + p.eps);
 #pragma unroll
-                for (int i = 0; i < 8; ++i) x[i] = x[i] * r * w[i];
-            }
-            __syncwarp();
-            if (kInterleaved) {
-                if (turns)
-#pragma unroll
-                    for (int i = 0; i < 4; ++i) {
-                        const float a = x[2 * i], b = x[2 * i + 1];
-                        x[2 * i] = a * c[i % F] - b * sn[i % F];
-                        x[2 * i + 1] = b * c[i % F] + a * sn[i % F];
+                        for (int i = 0; i < 8; ++i) x[i] = x[i] * r * w[i];
                     }
-            } else if (p.rope_dim) {
-                float y[8];
+                    if (kInterleaved) {
+                        if (turns)
 #pragma unroll
-                for (int i = 0; i < 8; ++i) y[i] = __shfl_sync(~0u, x[i], partner);
-                if (turns)
+                            for (int i = 0; i < 4; ++i) {
+                                const float a = x[2 * i], b = x[2 * i + 1];
+                                x[2 * i] = a * c[i % F] - b * sn[i % F];
+                                x[2 * i + 1] = b * c[i % F] + a * sn[i % F];
+                            }
+                    } else if (p.rope_dim) {
+                        float z[8];
 #pragma unroll
-                    for (int i = 0; i < 8; ++i) x[i] = x[i] * c[i % F] + y[i] * sn[i % F];
+                        for (int i = 0; i < 8; ++i) z[i] = __shfl_sync(~0u, x[i], partner);
+                        if (turns)
+#pragma unroll
+                            for (int i = 0; i < 8; ++i) x[i] = x[i] * c[i % F] + z[i] * sn[i % F];
+                    }
+                    y = pack<T>(x);
+                }
+                if (h + u * H + sub < end) __stcs(dst + u * H * dst_step, y);
             }
-            if (h < h1) {
-                if (is_q) __stcs(p.q_out + t * p.ot + h * p.oh + l, pack<T>(x));
-                else if (is_v) __stcs(p.vc + slot + (uint64_t)(h - v0) * p.head_step + l, now[u]);
-                else __stcs(p.kc + slot + (uint64_t)(h - k0) * p.head_step + l, pack<T>(x));
-            }
+            dst += kAhead * H * dst_step;
         }
-    }
+    };
+    run(std::true_type{}, src_q, p.qh, p.q_out + t * p.ot + (h0 + sub) * p.oh + l, p.oh, h0, min(h1, k0), p.qw, true);
+    run(std::true_type{}, src_k, p.kh, p.kc + slot + (uint64_t)(hk - k0 + sub) * p.head_step + l, p.head_step, hk, min(h1, v0), p.kw, h0 >= k0);
+    run(std::false_type{}, src_v, p.vh, p.vc + slot + (uint64_t)(hv - v0 + sub) * p.head_step + l, p.head_step, hv, h1, nullptr, h0 >= v0);
 }
 
 template <class T, int D>
 void append_launch(const AppendArgs &p, bool interleaved, uint32_t grid, cudaStream_t st) {
-    if (interleaved) k_append<T, D, true><<<grid, 256, 0, st>>>(p);
-    else k_append<T, D, false><<<grid, 256, 0, st>>>(p);
+    if (interleaved) k_append<T, D, true><<<grid, kThreads, 0, st>>>(p);
+    else k_append<T, D, false><<<grid, kThreads, 0, st>>>(p);
 }
 
 }  // namespace
@@ -229,8 +239,9 @@ extern "C" dm_status dm_cache_append(const dm_cache *c, const dm_append_args *a,
     while (p.per_warp > once && (uint64_t)a->tokens * ((heads + p.per_warp - 1) / p.per_warp) < enough)
         p.per_warp = (p.per_warp / 2 + once - 1) / once * once;
     const uint64_t warps = (uint64_t)a->tokens * ((heads + p.per_warp - 1) / p.per_warp);
-    if ((warps + 7) / 8 > 0x7FFFFFFFu) return DM_ERR_INVALID_ARG;
-    const uint32_t grid = (uint32_t)((warps + 7) / 8);
+    constexpr uint32_t kWarps = kThreads / 32;
+    if ((warps + kWarps - 1) / kWarps > 0x7FFFFFFFu) return DM_ERR_INVALID_ARG;
+    const uint32_t grid = (uint32_t)((warps + kWarps - 1) / kWarps);
     const auto st = static_cast<cudaStream_t>(stream);
     const bool il = a->interleaved != 0;
     if (c->dtype == DM_BF16) {
