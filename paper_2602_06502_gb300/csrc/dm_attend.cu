@@ -72,7 +72,7 @@ __global__ void __cluster_dims__(kPlanCl, 1, 1) __launch_bounds__(kPlanT) k_plan
     __shared__ uint64_t s_warp[32], s_cum[kFewBlocks];
     __shared__ int32_t s_offsets[kFewGroups + 1], s_prefix[kFewGroups];
     __shared__ uint32_t s_max[kFewGroups], s_n[kFewGroups];
-    __shared__ uint32_t s_bad, s_cuts;
+    __shared__ uint32_t s_bad, s_cuts, s_rows;
     cg::cluster_group cl = cg::this_cluster();
     const uint32_t rank = cl.block_rank(), tid = threadIdx.x;
     const bool few = p.groups <= kFewGroups;
@@ -163,7 +163,7 @@ __global__ void __cluster_dims__(kPlanCl, 1, 1) __launch_bounds__(kPlanT) k_plan
             const uint32_t cap = kind == 0 ? kWideRows : kNarrowRows, keys = kind == 0 ? kWideKeys : kNarrowKeys;
             uint64_t *cum = count[kind] <= kFewBlocks ? s_cum : p.w.cum[kind];
             uint64_t units0 = 0, parts0 = 0, own0 = 0;
-            if (tid == 0) s_cuts = 0;
+            if (tid == 0) s_cuts = s_rows = 0;
             for (uint32_t b0 = 0; b0 < count[kind]; b0 += kPlanT) {
                 const uint32_t b = b0 + tid;
                 AttendBlock k{};
@@ -192,7 +192,10 @@ __global__ void __cluster_dims__(kPlanCl, 1, 1) __launch_bounds__(kPlanT) k_plan
                 const uint64_t part = parts0 + block_scan(k.shared ? (uint64_t)k.rows * p.kv_heads : 0, s_warp, parts);
                 const uint64_t own = own0 + (p.groups ? block_scan(k.shared == kOwn, s_warp, owns) : owns = 0);
                 if (b < count[kind]) {
-                    if (k.shared == kOwn) p.w.own[kind][own] = b;
+                    if (k.shared == kOwn) {
+                        p.w.own[kind][own] = b;
+                        atomicMax(&s_rows, k.rows);
+                    }
                     k.part0 = (uint32_t)part;
                     p.w.block[kind][b] = k;
                     p.w.cum[kind][b] = at;
@@ -221,6 +224,8 @@ __global__ void __cluster_dims__(kPlanCl, 1, 1) __launch_bounds__(kPlanT) k_plan
             __syncthreads();
             if (tid == 0) {
                 p.w.head->own[kind] = (uint32_t)own0;
+                p.w.head->own_rows[kind] = s_rows;
+                p.w.head->inv[kind] = units0 ? ~0ull / units0 : 0;
                 p.w.head->cuts[kind] = s_cuts;
                 p.w.head->units[kind] = units0;
                 p.w.head->blocks[kind] = count[kind];
@@ -526,13 +531,15 @@ __global__ void __launch_bounds__(160, kNarrowPerSm)
 // order of the CTAs that left them.  32 parts' maxima and sums are looked at
 // together, so that the parts themselves are independent loads.  Bound:
 // latency, then L2 (4 D + 8 bytes a row and part).
+constexpr uint32_t kJoinCtas = 4, kAhead = 4;
+
 template <class T, int D>
-__global__ void __launch_bounds__(256) k_attend_join(AttendArgs p) {
+__global__ void __launch_bounds__(256, kJoinCtas) k_attend_join(AttendArgs p) {
     constexpr int V = D / 32;
     const PlanHead h = *p.w.head;
     const uint32_t lane = threadIdx.x & 31;
     if (has_err(p.status) || !h.ok) return;
-    const uint64_t own1 = (uint64_t)h.own[1] * p.kv_heads * kNarrowRows, own0 = own1 + (uint64_t)h.own[0] * p.kv_heads * kShareRows;
+    const uint64_t own1 = (uint64_t)h.own[1] * p.kv_heads * h.own_rows[1], own0 = own1 + (uint64_t)h.own[0] * p.kv_heads * h.own_rows[0];
     const uint64_t cut0 = own0 + (uint64_t)h.cuts[0] * kWideRows, jobs = cut0 + (uint64_t)h.cuts[1] * kNarrowRows;
     for (uint64_t t = blockIdx.x * 8ull + threadIdx.x / 32; t < jobs; t += gridDim.x * 8ull) {
         uint32_t b, head, r;
@@ -540,7 +547,7 @@ __global__ void __launch_bounds__(256) k_attend_join(AttendArgs p) {
         if (t < own0) {
             kind = t < own1;
             const uint64_t x = kind ? t : t - own1;
-            const uint32_t cap = kind ? kNarrowRows : kShareRows;
+            const uint32_t cap = kind ? h.own_rows[1] : h.own_rows[0];
             const uint32_t tile = (uint32_t)(x / cap);
             r = (uint32_t)(x % cap);
             b = (kind ? p.w.own[1] : p.w.own[0])[tile / p.kv_heads];
@@ -568,7 +575,8 @@ __global__ void __launch_bounds__(256) k_attend_join(AttendArgs p) {
         auto parts = [&](int kd, uint32_t blk, const AttendBlock &x, uint32_t row) {
             const uint64_t u0 = (kd ? p.w.cum[1] : p.w.cum[0])[blk] + (uint64_t)head * x.units, U = kd ? h.units[1] : h.units[0];
             const uint32_t cap = kd ? kNarrowRows : kWideRows, S = kd ? h.ctas[1] : h.ctas[0];
-            const uint32_t c0 = cta_of(u0, U, S), c1 = cta_of(u0 + x.units - 1, U, S);
+            const uint64_t inv = kd ? h.inv[1] : h.inv[0];
+            const uint32_t c0 = cta_of(u0, U, inv, S), c1 = cta_of(u0 + x.units - 1, U, inv, S);
             Parts q{kd ? p.w.part[1] : p.w.part[0], kd ? p.w.ml[1] : p.w.ml[0], c1 - c0 + 1, cap, 0, 0};
             if (x.shared) {
                 q.at = x.part0 + (uint64_t)head * x.rows + (uint64_t)cap * c0 + row;
@@ -590,7 +598,6 @@ __global__ void __launch_bounds__(256) k_attend_join(AttendArgs p) {
             float acc[V], M = -INFINITY, L = 0.f;
 #pragma unroll
             for (int v = 0; v < V; ++v) acc[v] = 0.f;
-            constexpr uint32_t kAhead = 8;
             float y[kAhead][V];
             auto load = [&](uint32_t i0) {
 #pragma unroll

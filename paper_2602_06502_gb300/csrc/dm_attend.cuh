@@ -44,9 +44,11 @@ constexpr uint32_t kOwn = 1, kPrefix = 2;
 
 struct PlanHead {
     uint64_t units[2];    // wide, narrow
+    uint64_t inv[2];      // 2^64 / units
     uint32_t blocks[2];
     uint32_t ctas[2];     // that have units
     uint32_t own[2];      // blocks of shared groups' sequences
+    uint32_t own_rows[2]; // the most rows of one
     uint32_t cuts[2];     // other tiles that more than one CTA has part of
     uint32_t ok, pad;
 };
@@ -146,9 +148,12 @@ struct AttendArgs {
     uint32_t ctas[2];                            // launched
 };
 
-// The CTA of S that unit u of U falls to: the last i with i U / S <= u.
-__device__ __forceinline__ uint32_t cta_of(uint64_t u, uint64_t U, uint32_t S) {
-    return (uint32_t)(((u + 1) * S - 1) / U);
+// The CTA of S that unit u of U falls to, the last i with i U / S <= u:
+// ((u + 1) S - 1) / U.  inv = 2^64 / U rounded down gives that or one less
+// ((u + 1) S < 2^64 / U would have to fail for more).
+__device__ __forceinline__ uint32_t cta_of(uint64_t u, uint64_t U, uint64_t inv, uint32_t S) {
+    const uint64_t x = (u + 1) * S - 1, i = __umul64hi(x, inv);
+    return (uint32_t)(x - i * U >= U ? i + 1 : i);
 }
 
 // Walks the tiles of a CTA's units.
