@@ -81,6 +81,7 @@ __global__ void __launch_bounds__(kThreads, 6) k_append(AppendArgs p) {
     const uint32_t heads = p.q_heads + 2 * p.kv_heads, parts = (heads + p.per_warp - 1) / p.per_warp;
     const uint64_t warp = (uint64_t)blockIdx.x * (kThreads / 32) + threadIdx.x / 32;
     const uint32_t t = (uint32_t)(warp / parts), h0 = (uint32_t)(warp % parts) * p.per_warp;
+    pdl_enter();
     if (t >= p.tokens || has_err(p.status)) return;
     const uint32_t h1 = min(heads, h0 + p.per_warp), k0 = p.q_heads, v0 = k0 + p.kv_heads;
     uint4 raw[kAhead];
@@ -196,9 +197,8 @@ __global__ void __launch_bounds__(kThreads, 6) k_append(AppendArgs p) {
 }
 
 template <class T, int D>
-void append_launch(const AppendArgs &p, bool interleaved, uint32_t grid, cudaStream_t st) {
-    if (interleaved) k_append<T, D, true><<<grid, kThreads, 0, st>>>(p);
-    else k_append<T, D, false><<<grid, kThreads, 0, st>>>(p);
+cudaError_t append_launch(const AppendArgs &p, bool interleaved, uint32_t grid, cudaStream_t st) {
+    return launch_pdl(interleaved ? k_append<T, D, true> : k_append<T, D, false>, grid, kThreads, 0, st, p);
 }
 
 }  // namespace
@@ -244,12 +244,8 @@ extern "C" dm_status dm_cache_append(const dm_cache *c, const dm_append_args *a,
     const uint32_t grid = (uint32_t)((warps + kWarps - 1) / kWarps);
     const auto st = static_cast<cudaStream_t>(stream);
     const bool il = a->interleaved != 0;
-    if (c->dtype == DM_BF16) {
-        if (c->head_dim == 64) append_launch<__nv_bfloat16, 64>(p, il, grid, st);
-        else append_launch<__nv_bfloat16, 128>(p, il, grid, st);
-    } else {
-        if (c->head_dim == 64) append_launch<__half, 64>(p, il, grid, st);
-        else append_launch<__half, 128>(p, il, grid, st);
-    }
-    return cudaGetLastError() == cudaSuccess ? DM_OK : DM_ERR_CUDA;
+    if (c->dtype == DM_BF16)
+        return status_of(c->head_dim == 64 ? append_launch<__nv_bfloat16, 64>(p, il, grid, st)
+                                           : append_launch<__nv_bfloat16, 128>(p, il, grid, st));
+    return status_of(c->head_dim == 64 ? append_launch<__half, 64>(p, il, grid, st) : append_launch<__half, 128>(p, il, grid, st));
 }

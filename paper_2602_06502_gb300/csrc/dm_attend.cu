@@ -73,6 +73,7 @@ __global__ void __cluster_dims__(kPlanCl, 1, 1) __launch_bounds__(kPlanT) k_plan
     __shared__ int32_t s_offsets[kFewGroups + 1], s_prefix[kFewGroups];
     __shared__ uint32_t s_max[kFewGroups], s_n[kFewGroups];
     __shared__ uint32_t s_bad, s_cuts, s_rows;
+    pdl_enter();
     cg::cluster_group cl = cg::this_cluster();
     const uint32_t rank = cl.block_rank(), tid = threadIdx.x;
     const bool few = p.groups <= kFewGroups;
@@ -305,6 +306,7 @@ __global__ void __launch_bounds__(160, kNarrowPerSm)
         *gave_up = 0;
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     }
+    pdl_enter();
     if (__syncthreads_or(has_err(p.status))) return;
     Walk<1> w(p);
     if (wid == 4) {
@@ -536,6 +538,7 @@ constexpr uint32_t kJoinCtas = 4, kAhead = 4;
 template <class T, int D>
 __global__ void __launch_bounds__(256, kJoinCtas) k_attend_join(AttendArgs p) {
     constexpr int V = D / 32;
+    pdl_enter();
     const PlanHead h = *p.w.head;
     const uint32_t lane = threadIdx.x & 31;
     if (has_err(p.status) || !h.ok) return;
@@ -683,12 +686,10 @@ template <class T, int D>
 cudaError_t launch_rest(const AttendArgs &p, uint64_t rows, const CUtensorMap &mk, const CUtensorMap &mv, cudaStream_t st) {
     static SmemOptIn opt;
     DM_TRY(opt_in_smem(opt, Narrow<D>::kBytes, k_attend_narrow<T, D>));
-    k_attend_narrow<T, D><<<p.ctas[1], 160, Narrow<D>::kBytes, st>>>(mk, mv, p);
-    DM_TRY(cudaGetLastError());
+    DM_TRY(launch_pdl(k_attend_narrow<T, D>, p.ctas[1], 160, Narrow<D>::kBytes, st, mk, mv, p));
     // a warp per row, or as many as the GPU holds
     const uint64_t warps = std::min<uint64_t>(rows, (uint64_t)p.ctas[0] * 64);
-    k_attend_join<T, D><<<(uint32_t)((warps + 7) / 8), 256, 0, st>>>(p);
-    return cudaGetLastError();
+    return launch_pdl(k_attend_join<T, D>, (uint32_t)((warps + 7) / 8), 256, 0, st, p);
 }
 
 uint32_t log2_of(uint32_t x) { return 31 - (uint32_t)__builtin_clz(x); }
@@ -718,8 +719,7 @@ extern "C" dm_status dm_cache_plan(const dm_cache *c, const dm_plan *pl, void *s
     p.seqs = pl->seqs, p.offsets = pl->offsets, p.group_offsets = pl->group_offsets, p.group_prefix = pl->group_prefix;
     p.n = pl->n, p.groups = pl->groups, p.tokens = pl->tokens, p.G = s.G, p.kv_heads = c->kv_heads, p.B = c->page_tokens;
     p.max_seqs = c->max_seqs, p.max_blocks = c->max_blocks, p.ctas[0] = s.ctas[0], p.ctas[1] = s.ctas[1];
-    k_plan<<<kPlanCl, kPlanT, 0, static_cast<cudaStream_t>(stream)>>>(p);
-    return cudaGetLastError() == cudaSuccess ? DM_OK : DM_ERR_CUDA;
+    return status_of(launch_pdl(k_plan, kPlanCl, kPlanT, 0, static_cast<cudaStream_t>(stream), p));
 }
 
 extern "C" dm_status dm_cache_attend(const dm_cache *c, const dm_plan *pl, const dm_attend_args *a, void *stream) {
@@ -752,5 +752,5 @@ extern "C" dm_status dm_cache_attend(const dm_cache *c, const dm_plan *pl, const
         else
             e = c->head_dim == 64 ? launch_rest<__half, 64>(p, rows, mk, mv, st) : launch_rest<__half, 128>(p, rows, mk, mv, st);
     }
-    return e == cudaSuccess ? DM_OK : DM_ERR_CUDA;
+    return status_of(e);
 }

@@ -160,7 +160,6 @@ __global__ void __launch_bounds__(kWideT, 1)
     auto p_full = [&](uint32_t x, uint32_t half) { return more + 32 + 16 * x + 8 * half; };
     auto o_full = [&](uint32_t x) { return more + 64 + 8 * x; };
     const uint32_t done = more + 80;
-    if (__syncthreads_or(has_err(p.status) || !p.w.head->ok || p.w.head->units[0] == 0)) return;
     if (tid == 0) {
         for (uint32_t i = 0; i < W::kStages; ++i) {
             mbar_init(full(i), 1);
@@ -177,6 +176,8 @@ __global__ void __launch_bounds__(kWideT, 1)
         *gave_up = 0;
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     }
+    pdl_enter();
+    if (__syncthreads_or(has_err(p.status) || !p.w.head->ok || p.w.head->units[0] == 0)) return;
     if (wid == 9) {
         asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], 512;" ::"r"(s_at + W::kWord + 4) : "memory");
         asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;");
@@ -472,8 +473,7 @@ template <class T, int D>
 cudaError_t launch(const AttendArgs &p, const CUtensorMap &mk, const CUtensorMap &mv, cudaStream_t st) {
     static SmemOptIn opt;
     DM_TRY(opt_in_smem(opt, Wide<D>::kBytes, k_attend_wide<T, D>));
-    k_attend_wide<T, D><<<p.ctas[0], kWideT, Wide<D>::kBytes, st>>>(mk, mv, p);
-    return cudaGetLastError();
+    return launch_pdl(k_attend_wide<T, D>, p.ctas[0], kWideT, Wide<D>::kBytes, st, mk, mv, p);
 }
 
 }  // namespace

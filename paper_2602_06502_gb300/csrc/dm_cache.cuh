@@ -57,6 +57,8 @@ inline bool cache_ok(const dm_cache *c) {
     return c->work_bytes >= cache_work_ints(c) * 4;
 }
 
+inline dm_status status_of(cudaError_t e) { return e == cudaSuccess ? DM_OK : DM_ERR_CUDA; }
+
 // Elements of a page, and where (head, token) of it begins.
 struct PageShape {
     uint32_t heads, tokens, dim, head_step, token_step;
@@ -72,7 +74,7 @@ __device__ __forceinline__ uint32_t owner_of(const int32_t *off, uint32_t n, int
     uint32_t lo = 0, hi = n;
     while (hi - lo > 1) {
         const uint32_t mid = (lo + hi) / 2;
-        if (__ldcg(off + mid) <= x) lo = mid;
+        if (off[mid] <= x) lo = mid;
         else hi = mid;
     }
     return lo;

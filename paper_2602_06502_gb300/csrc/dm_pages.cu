@@ -24,6 +24,7 @@ namespace {
 constexpr uint32_t kCl = 8;             // CTAs of the cluster
 constexpr uint32_t kPt = 1024;          // threads of each
 constexpr uint32_t kPw = kPt / 32;
+constexpr uint32_t kFewRequests = 2048; // whose places are searched in shared memory
 constexpr int kCopyT = 256;             // threads of a copying CTA
 
 struct PagesArgs {
@@ -83,6 +84,8 @@ template <bool kFork>
 __global__ void __cluster_dims__(kCl, 1, 1) __launch_bounds__(kPt) k_grow(PagesArgs p, const int32_t *a, const int32_t *b,
                                                                         const int32_t *c, uint32_t n) {
     __shared__ uint32_t s_warp[32], s_free, s_need, s_err;
+    __shared__ int32_t s_off[kFewRequests + 1];
+    pdl_enter();
     cg::cluster_group cl = cg::this_cluster();
     const uint32_t rank = cl.block_rank(), tid = threadIdx.x, wid = tid >> 5, lane = tid & 31;
     if (tid == 0) s_err = 0;
@@ -150,6 +153,12 @@ __global__ void __cluster_dims__(kCl, 1, 1) __launch_bounds__(kPt) k_grow(PagesA
         if (!ok && err != ~0u) set_err(p.status, err == 2u ? DM_ERR_INVALID_ARG : DM_ERR_CAPACITY);
         p.w.head[0] = ok;
     }
+    const bool few = n <= kFewRequests;
+    if (ok && need && few) {
+        for (uint32_t i = tid; i <= n; i += kPt) s_off[i] = __ldcg(p.w.off + i);
+        __syncthreads();
+    }
+    const int32_t *off = few ? s_off : p.w.off;
     if (ok) {
         uint32_t next = before + s_warp[wid];
         for (uint32_t i0 = begin; i0 < end && next < need; i0 += 128) {
@@ -158,12 +167,12 @@ __global__ void __cluster_dims__(kCl, 1, 1) __launch_bounds__(kPt) k_grow(PagesA
             const uint32_t cnt = __popc(m), in = scan_incl(cnt);
             uint32_t at = next + in - cnt;
             for (; m && at < need; m &= m - 1, ++at) {
-                const uint32_t page = i + __ffs(m) - 1, r = owner_of(p.w.off, n, (int32_t)at);
+                const uint32_t page = i + __ffs(m) - 1, r = owner_of(off, n, (int32_t)at);
                 if (kFork) {
                     p.w.aux[r] = (int32_t)page;
                 } else {
                     const uint64_t row = (uint64_t)(uint32_t)a[r] * p.max_blocks;
-                    p.tables[row + __ldcg(p.w.aux + r) + (at - __ldcg(p.w.off + r))] = (int32_t)page;
+                    p.tables[row + __ldcg(p.w.aux + r) + (at - off[r])] = (int32_t)page;
                 }
                 p.refs[page] = 1;
             }
@@ -175,19 +184,20 @@ __global__ void __cluster_dims__(kCl, 1, 1) __launch_bounds__(kPt) k_grow(PagesA
     cl.sync();   // no CTA leaves while another reads its counts
 }
 
-// bytes (a multiple of 16) from src to dst by a CTA.
-__device__ __forceinline__ void copy_run(char *dst, const char *src, uint32_t bytes) {
-    constexpr int U = 8;
-    const uint32_t step = kCopyT * 16;
-    uint32_t i = threadIdx.x * 16;
-    for (; i + (U - 1) * step < bytes; i += U * step) {
+// bytes (a multiple of 16) from src to dst by N threads, eight loads of each in
+// flight.
+template <uint32_t N>
+__device__ __forceinline__ void copy_run(char *dst, const char *src, uint32_t bytes, uint32_t thread) {
+    constexpr uint32_t U = 8, step = N * 16;
+    for (uint32_t i = thread * 16; i < bytes; i += U * step) {
         uint4 x[U];
 #pragma unroll
-        for (int u = 0; u < U; ++u) x[u] = __ldcs(reinterpret_cast<const uint4 *>(src + i + u * step));
+        for (uint32_t u = 0; u < U; ++u)
+            if (i + u * step < bytes) x[u] = __ldcs(reinterpret_cast<const uint4 *>(src + i + u * step));
 #pragma unroll
-        for (int u = 0; u < U; ++u) __stcs(reinterpret_cast<uint4 *>(dst + i + u * step), x[u]);
+        for (uint32_t u = 0; u < U; ++u)
+            if (i + u * step < bytes) __stcs(reinterpret_cast<uint4 *>(dst + i + u * step), x[u]);
     }
-    for (; i < bytes; i += step) *reinterpret_cast<uint4 *>(dst + i) = *reinterpret_cast<const uint4 *>(src + i);
 }
 
 struct CopyArgs {
@@ -201,6 +211,7 @@ struct CopyArgs {
 // then each pool's copied tokens.
 __global__ void __launch_bounds__(kCopyT) k_fork_copy(PagesArgs p, CopyArgs c, const int32_t *parents,
                                                       const int32_t *children, const int32_t *keep, uint32_t n) {
+    pdl_enter();
     if (p.w.head[0] == 0) return;
     const uint32_t per = 1 + 2 * c.layers;
     for (uint64_t job = blockIdx.x; job < (uint64_t)n * per; job += gridDim.x) {
@@ -229,13 +240,12 @@ __global__ void __launch_bounds__(kCopyT) k_fork_copy(PagesArgs p, CopyArgs c, c
             const char *src = pool + old * c.page_bytes;
             char *dst = pool + (uint64_t)(uint32_t)p.w.aux[i] * c.page_bytes;
             if (c.tokens_first) {
-                copy_run(dst, src, tail * c.heads * c.row_bytes);
+                copy_run<kCopyT>(dst, src, tail * c.heads * c.row_bytes, threadIdx.x);
             } else {
-                const uint32_t run = tail * c.row_bytes, head = p.B * c.row_bytes, per_head = run / 16;
-                for (uint32_t x = threadIdx.x; x < c.heads * per_head; x += kCopyT) {
-                    const uint64_t at = (uint64_t)(x / per_head) * head + x % per_head * 16;
-                    *reinterpret_cast<uint4 *>(dst + at) = *reinterpret_cast<const uint4 *>(src + at);
-                }
+                // a warp per head, a run of up to 16 KB each
+                const uint32_t run = tail * c.row_bytes, head = p.B * c.row_bytes;
+                for (uint32_t h = threadIdx.x / 32; h < c.heads; h += kCopyT / 32)
+                    copy_run<32>(dst + (uint64_t)h * head, src + (uint64_t)h * head, run, threadIdx.x & 31);
             }
         }
     }
@@ -243,6 +253,7 @@ __global__ void __launch_bounds__(kCopyT) k_fork_copy(PagesArgs p, CopyArgs c, c
 
 __global__ void __launch_bounds__(256) k_free(PagesArgs p, const int32_t *seqs, uint32_t n) {
     __shared__ int32_t s_len;
+    pdl_enter();
     if (has_err(p.status)) return;
     uint32_t bad = 0;   // every CTA looks at every id: one out of range stops them all
     for (uint32_t i = threadIdx.x; i < n; i += 256) bad |= (uint32_t)seqs[i] >= p.max_seqs;
@@ -269,6 +280,7 @@ __global__ void __launch_bounds__(256) k_free(PagesArgs p, const int32_t *seqs, 
 // the pages in use from `live` on, to[] the new id of each of the latter.
 __global__ void __cluster_dims__(kCl, 1, 1) __launch_bounds__(kPt) k_compact_plan(PagesArgs p, uint32_t *moved) {
     __shared__ uint32_t s_warp[32], s_free, s_cnt;
+    pdl_enter();
     cg::cluster_group cl = cg::this_cluster();
     const uint32_t rank = cl.block_rank(), tid = threadIdx.x, wid = tid >> 5, lane = tid & 31;
     uint32_t begin, end;
@@ -337,6 +349,7 @@ __global__ void __cluster_dims__(kCl, 1, 1) __launch_bounds__(kPt) k_compact_pla
 constexpr uint32_t kRefChunk = 4096;
 __global__ void __launch_bounds__(kCopyT) k_compact_copy(PagesArgs p, CopyArgs c, int32_t *tables_out,
                                                          int32_t *refs_out) {
+    pdl_enter();
     if (p.w.head[0] == 0) return;
     const uint32_t moves = (uint32_t)p.w.head[1], live = (uint32_t)p.w.head[2];
     const uint64_t copies = (uint64_t)moves * 2 * c.layers, rows = p.max_seqs;
@@ -345,8 +358,9 @@ __global__ void __launch_bounds__(kCopyT) k_compact_copy(PagesArgs p, CopyArgs c
         if (job < copies) {
             const uint32_t pool = (uint32_t)(job / moves), k = (uint32_t)(job % moves);
             char *base = (pool & 1 ? c.v : c.k) + (pool >> 1) * c.layer_bytes;
-            copy_run(base + (uint64_t)(uint32_t)p.w.list[k] * c.page_bytes,
-                     base + (uint64_t)(uint32_t)p.w.list[p.pages + k] * c.page_bytes, c.heads * p.B * c.row_bytes);
+            copy_run<kCopyT>(base + (uint64_t)(uint32_t)p.w.list[k] * c.page_bytes,
+                             base + (uint64_t)(uint32_t)p.w.list[p.pages + k] * c.page_bytes, c.heads * p.B * c.row_bytes,
+                             threadIdx.x);
         } else if (job < copies + rows) {
             const uint64_t s = job - copies;
             const uint32_t nb = min(((uint32_t)p.lengths[s] + p.B - 1) / p.B, p.max_blocks);
@@ -384,8 +398,6 @@ CopyArgs copy_args(const dm_cache *c) {
 
 uint32_t copy_grid(uint64_t jobs) { return (uint32_t)std::min<uint64_t>(jobs, (uint64_t)sm_count() * 8); }
 
-dm_status launched() { return cudaGetLastError() == cudaSuccess ? DM_OK : DM_ERR_CUDA; }
-
 }  // namespace
 }  // namespace dm
 
@@ -408,9 +420,8 @@ extern "C" dm_status dm_cache_extend(const dm_cache *c, const int32_t *seqs, con
                                      void *stream) {
     if (!dm::cache_ok(c) || n > c->max_seqs || (n && (!seqs || !add))) return DM_ERR_INVALID_ARG;
     if (n == 0) return DM_OK;
-    dm::k_grow<false><<<dm::kCl, dm::kPt, 0, static_cast<cudaStream_t>(stream)>>>(dm::pages_args(c), seqs, add,
-                                                                                  nullptr, n);
-    return dm::launched();
+    return dm::status_of(dm::launch_pdl(dm::k_grow<false>, dm::kCl, dm::kPt, 0, static_cast<cudaStream_t>(stream),
+                                        dm::pages_args(c), seqs, add, nullptr, n));
 }
 
 extern "C" dm_status dm_cache_fork(const dm_cache *c, const int32_t *parents, const int32_t *children,
@@ -419,17 +430,18 @@ extern "C" dm_status dm_cache_fork(const dm_cache *c, const int32_t *parents, co
     if (n == 0) return DM_OK;
     const auto st = static_cast<cudaStream_t>(stream);
     const dm::PagesArgs p = dm::pages_args(c);
-    dm::k_grow<true><<<dm::kCl, dm::kPt, 0, st>>>(p, parents, len, children, n);
-    dm::k_fork_copy<<<dm::copy_grid((uint64_t)n * (1 + 2 * c->layers)), dm::kCopyT, 0, st>>>(
-        p, dm::copy_args(c), parents, children, len, n);
-    return dm::launched();
+    cudaError_t e = dm::launch_pdl(dm::k_grow<true>, dm::kCl, dm::kPt, 0, st, p, parents, len, children, n);
+    if (e == cudaSuccess)
+        e = dm::launch_pdl(dm::k_fork_copy, dm::copy_grid((uint64_t)n * (1 + 2 * c->layers)), dm::kCopyT, 0, st, p,
+                           dm::copy_args(c), parents, children, len, n);
+    return dm::status_of(e);
 }
 
 extern "C" dm_status dm_cache_free(const dm_cache *c, const int32_t *seqs, uint32_t n, void *stream) {
     if (!dm::cache_ok(c) || n > c->max_seqs || (n && !seqs)) return DM_ERR_INVALID_ARG;
     if (n == 0) return DM_OK;
-    dm::k_free<<<dm::copy_grid(n), 256, 0, static_cast<cudaStream_t>(stream)>>>(dm::pages_args(c), seqs, n);
-    return dm::launched();
+    return dm::status_of(
+        dm::launch_pdl(dm::k_free, dm::copy_grid(n), 256, 0, static_cast<cudaStream_t>(stream), dm::pages_args(c), seqs, n));
 }
 
 extern "C" dm_status dm_cache_compact(const dm_cache *c, int32_t *tables_out, int32_t *refs_out, uint32_t *moved,
@@ -437,10 +449,10 @@ extern "C" dm_status dm_cache_compact(const dm_cache *c, int32_t *tables_out, in
     if (!dm::cache_ok(c) || !dm::aligned(refs_out, 16)) return DM_ERR_INVALID_ARG;
     const auto st = static_cast<cudaStream_t>(stream);
     const dm::PagesArgs p = dm::pages_args(c);
-    dm::k_compact_plan<<<dm::kCl, dm::kPt, 0, st>>>(p, moved);
+    cudaError_t e = dm::launch_pdl(dm::k_compact_plan, dm::kCl, dm::kPt, 0, st, p, moved);
     const uint64_t jobs = (uint64_t)c->pages * c->layers + c->max_seqs + (c->pages + dm::kRefChunk - 1) / dm::kRefChunk;
-    dm::k_compact_copy<<<dm::copy_grid(jobs), dm::kCopyT, 0, st>>>(p, dm::copy_args(c),
-                                                                   tables_out ? tables_out : c->tables,
-                                                                   refs_out ? refs_out : c->refs);
-    return dm::launched();
+    if (e == cudaSuccess)
+        e = dm::launch_pdl(dm::k_compact_copy, dm::copy_grid(jobs), dm::kCopyT, 0, st, p, dm::copy_args(c),
+                           tables_out ? tables_out : c->tables, refs_out ? refs_out : c->refs);
+    return dm::status_of(e);
 }
