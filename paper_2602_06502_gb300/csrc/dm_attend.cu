@@ -26,6 +26,7 @@ struct PlanArgs {
     const int32_t *tables, *lengths, *seqs, *offsets, *group_offsets, *group_prefix;
     uint32_t *status;
     uint32_t n, groups, tokens, G, kv_heads, B, max_seqs, max_blocks, ctas[2];
+    PlanCosts costs;
 };
 
 __device__ __forceinline__ uint64_t scan_incl(uint64_t x) {
@@ -50,6 +51,8 @@ __device__ uint64_t block_scan(uint64_t x, uint64_t *s_warp, uint64_t &total) {
     return in - x + (wid ? s_warp[wid - 1] : 0);
 }
 
+// Measured on attend_templates' and attend_drafts' shapes.
+constexpr PlanCosts kCosts128 = {23, 20, 75, 24, 8}, kCosts64 = {20, 17, 38, 15, 6};
 constexpr uint32_t kFewGroups = 512, kFewBlocks = 2048;   // kept in shared memory
 
 // The group of sequence i: the last g with offsets[g] <= i, -1 if i is outside
@@ -160,38 +163,84 @@ __global__ void __cluster_dims__(kPlanCl, 1, 1) __launch_bounds__(kPlanT) k_plan
         }
         const uint32_t count[2] = {(uint32_t)carry, (uint32_t)(carry >> 32)};
         __syncthreads();
-        for (int kind = 0; kind < 2; ++kind) {
+        // block b of a kind, but for its place in the line and in the parts
+        auto block_at = [&](int kind, uint32_t b) {
             const uint32_t cap = kind == 0 ? kWideRows : kNarrowRows, keys = kind == 0 ? kWideKeys : kNarrowKeys;
+            AttendBlock k{};
+            const uint32_t e = p.w.owner[kind][b];
+            const PlanEntity x = p.w.entity[e];
+            const uint32_t row0 = (b - x.first) * cap;
+            k.row = x.row;
+            k.rows = min(x.rows - row0, cap);
+            k.lead = row0 % p.G;
+            k.token = x.token + (int32_t)(row0 / p.G);
+            k.kv0 = x.kv0;
+            k.shared = x.shared;
+            k.pos = x.pos + (int32_t)(row0 / p.G);
+            k.kv1 = x.shared == kPrefix ? gp[e] : max(k.kv0, k.pos + (int32_t)((k.lead + k.rows - 1) / p.G) + 1);
+            k.units = max(1u, ((uint32_t)(k.kv1 - k.kv0) + keys - 1) / keys);
+            k.cost = kind ? p.costs.narrow : k.rows > 128 ? p.costs.two : p.costs.one;
+            k.over = kind ? p.costs.narrow_over : p.costs.wide_over;
+            if (x.shared == kOwn) {
+                const PlanEntity pre = p.w.entity[x.group];
+                k.pre = pre.first;
+                k.pre_kind = pre.rows <= kNarrowRows;
+                k.pre_row = (uint32_t)(x.token - pre.token) * p.G + row0;
+            }
+            return k;
+        };
+        // What each kind costs, and its units.
+        uint64_t cost[2], units[2];
+        for (int kind = 0; kind < 2; ++kind) {
+            uint64_t c = 0, u = 0;
+            for (uint32_t b = tid; b < count[kind]; b += kPlanT) {
+                const AttendBlock k = block_at(kind, b);
+                c += (uint64_t)(k.units * (uint64_t)k.cost + k.over) * p.kv_heads;
+                u += (uint64_t)k.units * p.kv_heads;
+            }
+            block_scan(c, s_warp, cost[kind]);
+            block_scan(u, s_warp, units[kind]);
+        }
+        // The SMs are shared out so that both kernels, which run side by side,
+        // take about as long; kNarrowPerSm narrow CTAs share an SM.
+        uint32_t sms = 0;
+        if (units[0]) {
+            const uint64_t wide = cost[0] * kNarrowPerSm, all = wide + cost[1];
+            sms = (uint32_t)((wide * p.ctas[0] + all / 2) / all);
+            sms = max(1u, min(sms, units[1] ? p.ctas[0] - 1 : p.ctas[0]));
+        }
+        for (int kind = 0; kind < 2; ++kind) {
+            if (units[kind] == 0) {
+                if (tid == 0) p.w.head->cost[kind] = p.w.head->inv[kind] = p.w.head->ctas[kind] = p.w.head->own[kind] = p.w.head->cuts[kind] = 0;
+                continue;
+            }
+            // Each CTA has a unit where its share is not less than the widest
+            // gap between two units' beginnings.  So little work that this
+            // would leave CTAs idle goes a unit at a time.
+            const uint32_t most = kind == 0 ? sms : (p.ctas[0] - sms) * kNarrowPerSm;
+            const uint32_t gap = kind == 0 ? max(p.costs.two, p.costs.one) + p.costs.wide_over : p.costs.narrow + p.costs.narrow_over;
+            const bool even = cost[kind] / gap < most;
+            const uint64_t C = even ? units[kind] : cost[kind];
+            const uint32_t S = (uint32_t)min((uint64_t)most, C);
             uint64_t *cum = count[kind] <= kFewBlocks ? s_cum : p.w.cum[kind];
-            uint64_t units0 = 0, parts0 = 0, own0 = 0;
+            uint64_t at0 = 0, parts0 = 0, own0 = 0;
             if (tid == 0) s_cuts = s_rows = 0;
             for (uint32_t b0 = 0; b0 < count[kind]; b0 += kPlanT) {
                 const uint32_t b = b0 + tid;
                 AttendBlock k{};
                 if (b < count[kind]) {
-                    const uint32_t e = p.w.owner[kind][b];
-                    const PlanEntity x = p.w.entity[e];
-                    const uint32_t row0 = (b - x.first) * cap;
-                    k.row = x.row;
-                    k.rows = min(x.rows - row0, cap);
-                    k.lead = row0 % p.G;
-                    k.token = x.token + (int32_t)(row0 / p.G);
-                    k.kv0 = x.kv0;
-                    k.shared = x.shared;
-                    k.pos = x.pos + (int32_t)(row0 / p.G);
-                    k.kv1 = x.shared == kPrefix ? gp[e] : max(k.kv0, k.pos + (int32_t)((k.lead + k.rows - 1) / p.G) + 1);
-                    k.units = max(1u, ((uint32_t)(k.kv1 - k.kv0) + keys - 1) / keys);
-                    if (x.shared == kOwn) {
-                        const PlanEntity pre = p.w.entity[x.group];
-                        k.pre = pre.first;
-                        k.pre_kind = pre.rows <= kNarrowRows;
-                        k.pre_row = (uint32_t)(x.token - pre.token) * p.G + row0;
-                    }
+                    k = block_at(kind, b);
+                    if (even) k.cost = 1, k.over = 0;
                 }
-                uint64_t units, parts, owns;
-                const uint64_t at = units0 + block_scan((uint64_t)k.units * p.kv_heads, s_warp, units);
-                const uint64_t part = parts0 + block_scan(k.shared ? (uint64_t)k.rows * p.kv_heads : 0, s_warp, parts);
-                const uint64_t own = own0 + (p.groups ? block_scan(k.shared == kOwn, s_warp, owns) : owns = 0);
+                uint64_t length, parts, owns = 0;
+                const uint64_t at = at0 + block_scan((uint64_t)(k.units * (uint64_t)k.cost + k.over) * p.kv_heads, s_warp, length);
+                uint64_t part = 0, own = 0;
+                if (p.groups) {
+                    part = parts0 + block_scan(k.shared ? (uint64_t)k.rows * p.kv_heads : 0, s_warp, parts);
+                    own = own0 + block_scan(k.shared == kOwn, s_warp, owns);
+                    parts0 += parts;
+                    own0 += owns;
+                }
                 if (b < count[kind]) {
                     if (k.shared == kOwn) {
                         p.w.own[kind][own] = b;
@@ -202,35 +251,40 @@ __global__ void __cluster_dims__(kPlanCl, 1, 1) __launch_bounds__(kPlanT) k_plan
                     p.w.cum[kind][b] = at;
                     cum[b] = at;
                 }
-                units0 += units;
-                parts0 += parts;
-                own0 += owns;
+                at0 += length;
             }
             __syncthreads();
-            const uint32_t S = (uint32_t)min((uint64_t)p.ctas[kind], units0);
             for (uint32_t c = tid; c < S; c += kPlanT) {
-                const uint64_t u = c * units0 / S;
-                uint32_t lo = 0, hi = count[kind];   // the last block with cum <= u
+                const uint64_t from = c * C / S;
+                uint32_t lo = 0, hi = count[kind];   // the last block that begins by then
                 while (hi - lo > 1) {
                     const uint32_t mid = (lo + hi) / 2;
-                    if (cum[mid] <= u) lo = mid;
+                    if (cum[mid] <= from) lo = mid;
                     else hi = mid;
                 }
-                p.w.start[kind][c] = lo;
-                // the first boundary inside a tile
                 const AttendBlock k = p.w.block[kind][lo];
-                const uint64_t inside = (u - cum[lo]) % k.units;
-                if (!k.shared && inside && (c - 1) * units0 / S <= u - inside) p.w.cut[kind][atomicAdd(&s_cuts, 1u)] = c;
+                const uint64_t tile = (uint64_t)k.units * k.cost + k.over, inside = from - cum[lo];
+                PlanStart x{0, lo, (uint32_t)(inside / tile), 0, 0};
+                const uint64_t begin = cum[lo] + x.head * tile, rest = from - begin;   // of the tile; into it
+                if (rest) x.unit = rest <= k.over + k.cost ? 1 : (uint32_t)((rest - k.over + k.cost - 1) / k.cost);
+                x.at = begin + (x.unit ? k.over + (uint64_t)x.unit * k.cost : 0);
+                if (x.unit == k.units) {   // the next tile
+                    x.unit = 0;
+                    if (++x.head == p.kv_heads) x.head = 0, ++x.block;
+                }
+                p.w.start[kind][c] = x;
+                // the first boundary inside a tile
+                if (!k.shared && x.unit && (c - 1) * C / S <= begin) p.w.cut[kind][atomicAdd(&s_cuts, 1u)] = c;
             }
             __syncthreads();
             if (tid == 0) {
-                p.w.head->own[kind] = (uint32_t)own0;
-                p.w.head->own_rows[kind] = s_rows;
-                p.w.head->inv[kind] = units0 ? ~0ull / units0 : 0;
-                p.w.head->cuts[kind] = s_cuts;
-                p.w.head->units[kind] = units0;
-                p.w.head->blocks[kind] = count[kind];
-                p.w.head->ctas[kind] = S;
+                PlanHead *h = p.w.head;
+                h->cost[kind] = C;
+                h->inv[kind] = ~0ull / C;
+                h->ctas[kind] = S;
+                h->own[kind] = (uint32_t)own0;
+                h->own_rows[kind] = s_rows;
+                h->cuts[kind] = s_cuts;
             }
             __syncthreads();
         }
@@ -251,12 +305,12 @@ __global__ void __cluster_dims__(kPlanCl, 1, 1) __launch_bounds__(kPlanT) k_plan
 //
 // Memory's kernel: every key and value is used by at most 16 rows, so the
 // tensor work is small and mma.sync's rate is enough; what counts is bytes in
-// flight.  A producer warp keeps a ring of 32-key slots (keys and values, 8 KB
-// or 16 KB) full through TMA, two CTAs per SM; each of four warps takes the 16
+// flight.  Two warps keep a ring of 32-key slots (keys and values, 8 KB or 16 KB)
+// full through TMA, two CTAs per SM; each of four warps takes the 16
 // keys of its half of every other slot, with its own running maximum and sum,
 // and the four join once per tile.
 
-constexpr uint32_t kSlotKeys = 32;
+constexpr uint32_t kSlotKeys = 32, kNarrowT = 192;
 
 template <int D>
 struct Narrow {
@@ -288,7 +342,7 @@ __device__ __forceinline__ void ldsm4t(uint32_t *r, uint32_t at) {
 __device__ __forceinline__ void bar_consumers() { asm volatile("bar.sync 1, 128;" ::: "memory"); }
 
 template <class T, int D>
-__global__ void __launch_bounds__(160, kNarrowPerSm)
+__global__ void __launch_bounds__(kNarrowT, kNarrowPerSm)
     k_attend_narrow(const __grid_constant__ CUtensorMap mk, const __grid_constant__ CUtensorMap mv, AttendArgs p) {
     using N = Narrow<D>;
     extern __shared__ char s_raw[];
@@ -306,42 +360,33 @@ __global__ void __launch_bounds__(160, kNarrowPerSm)
         *gave_up = 0;
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     }
-    pdl_enter();
-    if (__syncthreads_or(has_err(p.status))) return;
+    // After a wide kernel this one runs beside it: that one's CTAs have seen the
+    // plan and everything before it complete before they let this one begin,
+    // and this one ends after it, for what follows.  What the plan wrote is
+    // therefore read through L2.
+    if (p.beside) asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+    else pdl_enter();
+    if (__syncthreads_or(has_err(p.status))) {
+        if (p.beside) asm volatile("griddepcontrol.wait;" ::: "memory");
+        return;
+    }
     Walk<1> w(p);
-    if (wid == 4) {
+    if (wid >= 4) {
+        // one warp the keys, one the values
+        const bool keys = wid == 4;
         uint32_t c = 0;   // slots so far
-        KeyBoxes<D, kSlotKeys, 1> boxes(0);
-        bool more = w.next(p);
-        const int32_t *table = nullptr;
-        uint32_t blocks = 0, tok = 0, left = 0, head = 0;   // the next slot; slots left of the piece
-        auto piece = [&] {
-            table = p.tables + (uint64_t)w.k.row * p.max_blocks;
-            blocks = ((uint32_t)w.k.kv1 + (1u << p.B_log) - 1) >> p.B_log;
-            tok = (uint32_t)w.k.kv0 + w.j0 * kNarrowKeys;
-            left = 2 * w.units;
-            head = w.head;
-        };
-        if (more) {
-            piece();
-            boxes.find(p, table, tok, blocks);
-        }
-        while (more) {
+        for (Slots<1, D, kSlotKeys, 1> next(p, w, 0); next.more; next.step(p), ++c) {
             const uint32_t slot = c % N::kSlots, round = c / N::kSlots, at = s_at + slot * 2 * N::kHalf;
             if (round) mbar_wait(empty(slot), (round - 1) & 1, gave_up, p.status);
             if (__any_sync(~0u, *gave_up)) break;
-            if (lane == 0) mbar_expect(full(slot), 2 * N::kHalf);
+            if (keys && lane == 0) mbar_expect(full(slot), 2 * N::kHalf);   // the phase ends with this and all the bytes
             __syncwarp();
-            boxes.load(p, &mk, at, full(slot), tok, head);
-            boxes.load(p, &mv, at + N::kHalf, full(slot), tok, head);
-            ++c;
-            tok += kSlotKeys;
-            if (--left == 0 && (more = w.next(p))) piece();
-            if (more) boxes.find(p, table, tok, blocks);
+            next.boxes.load(p, keys ? &mk : &mv, keys ? at : at + N::kHalf, full(slot), next.tok, next.head);
         }
         // no copy may be in flight when the CTA ends
         for (uint32_t i = c > N::kSlots ? c - N::kSlots : 0; i < c; ++i)
             mbar_drain(full(i % N::kSlots), (i / N::kSlots) & 1);
+        if (p.beside) asm volatile("griddepcontrol.wait;" ::: "memory");
         return;
     }
     float *red = reinterpret_cast<float *>(s + N::kRed);
@@ -524,6 +569,7 @@ __global__ void __launch_bounds__(160, kNarrowPerSm)
         }
         w = ahead;
     }
+    if (p.beside) asm volatile("griddepcontrol.wait;" ::: "memory");
 }
 
 // -- joining parts --------------------------------------------------------------------
@@ -560,10 +606,9 @@ __global__ void __launch_bounds__(256, kJoinCtas) k_attend_join(AttendArgs p) {
             const uint64_t x = kind ? t - cut0 : t - own0;
             const uint32_t cap = kind ? kNarrowRows : kWideRows;
             r = (uint32_t)(x % cap);
-            const uint32_t c = (kind ? p.w.cut[1] : p.w.cut[0])[x / cap];
-            b = (kind ? p.w.start[1] : p.w.start[0])[c];
-            const uint64_t u = c * (kind ? h.units[1] : h.units[0]) / (kind ? h.ctas[1] : h.ctas[0]);
-            head = (uint32_t)((u - (kind ? p.w.cum[1] : p.w.cum[0])[b]) / (kind ? p.w.block[1] : p.w.block[0])[b].units);
+            const PlanStart &from = (kind ? p.w.start[1] : p.w.start[0])[(kind ? p.w.cut[1] : p.w.cut[0])[x / cap]];
+            b = from.block;
+            head = from.head;
         }
         const AttendBlock k = (kind ? p.w.block[1] : p.w.block[0])[b];
         if (r >= k.rows) continue;
@@ -576,10 +621,11 @@ __global__ void __launch_bounds__(256, kJoinCtas) k_attend_join(AttendArgs p) {
             __device__ uint64_t row(uint32_t i) const { return at + (uint64_t)i * step + (i == 0 ? odd : 0); }
         };
         auto parts = [&](int kd, uint32_t blk, const AttendBlock &x, uint32_t row) {
-            const uint64_t u0 = (kd ? p.w.cum[1] : p.w.cum[0])[blk] + (uint64_t)head * x.units, U = kd ? h.units[1] : h.units[0];
+            const uint64_t C = kd ? h.cost[1] : h.cost[0], begin = (kd ? p.w.cum[1] : p.w.cum[0])[blk] + head * ((uint64_t)x.units * x.cost + x.over);
+            const uint64_t last = begin + (x.units > 1 ? x.over + (x.units - 1ull) * x.cost : 0);   // its last unit
             const uint32_t cap = kd ? kNarrowRows : kWideRows, S = kd ? h.ctas[1] : h.ctas[0];
             const uint64_t inv = kd ? h.inv[1] : h.inv[0];
-            const uint32_t c0 = cta_of(u0, U, inv, S), c1 = cta_of(u0 + x.units - 1, U, inv, S);
+            const uint32_t c0 = cta_of(begin, C, inv, S), c1 = cta_of(last, C, inv, S);
             Parts q{kd ? p.w.part[1] : p.w.part[0], kd ? p.w.ml[1] : p.w.ml[0], c1 - c0 + 1, cap, 0, 0};
             if (x.shared) {
                 q.at = x.part0 + (uint64_t)head * x.rows + (uint64_t)cap * c0 + row;
@@ -686,7 +732,7 @@ template <class T, int D>
 cudaError_t launch_rest(const AttendArgs &p, uint64_t rows, const CUtensorMap &mk, const CUtensorMap &mv, cudaStream_t st) {
     static SmemOptIn opt;
     DM_TRY(opt_in_smem(opt, Narrow<D>::kBytes, k_attend_narrow<T, D>));
-    DM_TRY(launch_pdl(k_attend_narrow<T, D>, p.ctas[1], 160, Narrow<D>::kBytes, st, mk, mv, p));
+    DM_TRY(launch_pdl(k_attend_narrow<T, D>, p.ctas[1], kNarrowT, Narrow<D>::kBytes, st, mk, mv, p));
     // a warp per row, or as many as the GPU holds
     const uint64_t warps = std::min<uint64_t>(rows, (uint64_t)p.ctas[0] * 64);
     return launch_pdl(k_attend_join<T, D>, (uint32_t)((warps + 7) / 8), 256, 0, st, p);
@@ -719,6 +765,7 @@ extern "C" dm_status dm_cache_plan(const dm_cache *c, const dm_plan *pl, void *s
     p.seqs = pl->seqs, p.offsets = pl->offsets, p.group_offsets = pl->group_offsets, p.group_prefix = pl->group_prefix;
     p.n = pl->n, p.groups = pl->groups, p.tokens = pl->tokens, p.G = s.G, p.kv_heads = c->kv_heads, p.B = c->page_tokens;
     p.max_seqs = c->max_seqs, p.max_blocks = c->max_blocks, p.ctas[0] = s.ctas[0], p.ctas[1] = s.ctas[1];
+    p.costs = c->head_dim == 128 ? kCosts128 : kCosts64;
     return status_of(launch_pdl(k_plan, kPlanCl, kPlanT, 0, static_cast<cudaStream_t>(stream), p));
 }
 
@@ -739,11 +786,12 @@ extern "C" dm_status dm_cache_attend(const dm_cache *c, const dm_plan *pl, const
     p.G_mul = (uint32_t)((0xFFFFFFFFull + s.G) / s.G);   // 2^32 / G, rounded up
     p.G = s.G, p.kv_heads = c->kv_heads, p.q_heads = s.q_heads, p.scale2 = a->scale * 1.44269504089f;
     p.ctas[0] = s.ctas[0], p.ctas[1] = s.ctas[1];
+    p.o_wide = aligned(a->o, 32) && (a->o_token | a->o_head) % 16 == 0;
     CUtensorMap mk, mv;
     if (!page_map(&mk, c, c->k, a->layer, box) || !page_map(&mv, c, c->v, a->layer, box)) return DM_ERR_CUDA;
     const auto st = static_cast<cudaStream_t>(stream);
-    // so few rows that no block of them is wide
-    cudaError_t e = (uint64_t)pl->tokens * s.G <= kNarrowRows ? cudaSuccess : launch_attend_wide(c, p, mk, mv, st);
+    p.beside = (uint64_t)pl->tokens * s.G > kNarrowRows;   // else so few rows that no block of them is wide
+    cudaError_t e = p.beside ? launch_attend_wide(c, p, mk, mv, st) : cudaSuccess;
     if (e == cudaSuccess) {
         // narrow tiles count 16 rows in the joining
         const uint64_t rows = (uint64_t)pl->tokens * s.q_heads + (uint64_t)pl->n * c->kv_heads * kNarrowRows;

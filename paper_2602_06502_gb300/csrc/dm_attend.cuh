@@ -7,10 +7,11 @@
 //
 // Work.  A block is up to 256 rows (wide: the tcgen05 kernel) or up to 16
 // (narrow) of one sequence or group and a range of keys; with a key head it is
-// a tile, cut into units of 128 (wide) or 64 (narrow) keys.  All U units of a
-// kind stand in one line, and CTA i of S (no more than there are units, so
-// that each has some) takes those from i U / S to (i + 1) U / S: every SM gets
-// the same number of keys whatever the lengths.
+// a tile, cut into units of 128 (wide) or 64 (narrow) keys.  All tiles of a
+// kind stand in one line, each as long as it costs (`cost` a unit and `over`
+// besides, which the first unit has), and CTA i of S takes the units that begin
+// from i C / S to (i + 1) C / S of the line's length C.  S is small enough that
+// each has some: every CTA is busy for about as long whatever the lengths.
 // A tile that a boundary cuts, and every tile of a shared group, leaves
 // (maximum, sum, unnormalised output) per row and CTA; k_attend_join adds them
 // up.  A CTA and tile meet in one place of a staircase through (tiles x CTAs),
@@ -34,6 +35,7 @@ struct AttendBlock {
     int32_t kv0, kv1;     // keys; no row sees one from kv1 on
     int32_t pos;          // the first token's position (a group's prefix: all rows see all keys)
     uint32_t units;       // per key head, >= 1
+    uint32_t cost, over;
     uint32_t part0;       // shared: its first row in the parts
     uint32_t shared;      // kPrefix, kOwn, or 0
     // kOwn: where the rows' parts of the prefix are, a block of kind pre_kind
@@ -43,14 +45,25 @@ struct AttendBlock {
 constexpr uint32_t kOwn = 1, kPrefix = 2;
 
 struct PlanHead {
-    uint64_t units[2];    // wide, narrow
-    uint64_t inv[2];      // 2^64 / units
-    uint32_t blocks[2];
+    uint64_t cost[2];     // wide, narrow
+    uint64_t inv[2];      // 2^64 / cost
     uint32_t ctas[2];     // that have units
     uint32_t own[2];      // blocks of shared groups' sequences
     uint32_t own_rows[2]; // the most rows of one
     uint32_t cuts[2];     // other tiles that more than one CTA has part of
     uint32_t ok, pad;
+};
+
+// A CTA's first unit.
+struct PlanStart {
+    uint64_t at;          // along the line
+    uint32_t block, head, unit, pad;
+};
+
+// What the parts of a block cost, in 100 cycles of a CTA.
+struct PlanCosts {
+    uint32_t two, one, wide_over;     // a wide unit with two tiles of rows, with one; a wide tile besides
+    uint32_t narrow, narrow_over;
 };
 
 // A sequence or a group of the step.
@@ -64,8 +77,8 @@ struct PlanEntity {
 struct PlanWork {
     PlanHead *head;
     AttendBlock *block[2];    // wide, narrow
-    uint64_t *cum[2];         // units before each block
-    uint32_t *start[2];       // per CTA: the block of its first unit
+    uint64_t *cum[2];         // where each block begins along the line
+    PlanStart *start[2];      // per CTA
     uint32_t *owner[2];       // per block: its entity
     uint32_t *own[2];         // the blocks of shared groups' sequences
     uint32_t *cut[2];         // per other cut tile: the second CTA that has part of it
@@ -118,7 +131,7 @@ inline uint64_t plan_work(const PlanShape &s, void *base, PlanWork &w) {
     for (int k = 0; k < 2; ++k) {
         w.block[k] = (AttendBlock *)take(sizeof(AttendBlock) * s.blocks[k]);
         w.cum[k] = (uint64_t *)take(8ull * s.blocks[k]);
-        w.start[k] = (uint32_t *)take(4ull * s.ctas[k]);
+        w.start[k] = (PlanStart *)take(sizeof(PlanStart) * s.ctas[k]);
         w.owner[k] = (uint32_t *)take(4ull * s.blocks[k]);
         w.own[k] = (uint32_t *)take(4ull * s.blocks[k]);
         w.cut[k] = (uint32_t *)take(4ull * s.ctas[k]);
@@ -146,52 +159,68 @@ struct AttendArgs {
     uint32_t B_log, box_log;                     // log2 of a page's tokens and of a TMA box's
     float scale2;                                // scale * log2(e)
     uint32_t ctas[2];                            // launched
+    uint32_t o_wide;                             // rows of o begin on 32 bytes
+    uint32_t beside;                             // the narrow kernel runs beside a wide one
 };
 
-// The CTA of S that unit u of U falls to, the last i with i U / S <= u:
-// ((u + 1) S - 1) / U.  inv = 2^64 / U rounded down gives that or one less
-// ((u + 1) S < 2^64 / U would have to fail for more).
-__device__ __forceinline__ uint32_t cta_of(uint64_t u, uint64_t U, uint64_t inv, uint32_t S) {
-    const uint64_t x = (u + 1) * S - 1, i = __umul64hi(x, inv);
-    return (uint32_t)(x - i * U >= U ? i + 1 : i);
+// The CTA of S whose units begin at `at` of a line of length C, the last i with
+// i C / S <= at: ((at + 1) S - 1) / C.  inv = 2^64 / C rounded down gives that
+// or one less ((at + 1) S <= C S < 2^64).
+__device__ __forceinline__ uint32_t cta_of(uint64_t at, uint64_t C, uint64_t inv, uint32_t S) {
+    const uint64_t x = (at + 1) * S - 1, i = __umul64hi(x, inv);
+    return (uint32_t)(x - i * C >= C ? i + 1 : i);
 }
 
 // Walks the tiles of a CTA's units.
 template <int kKind>
 struct Walk {
-    uint64_t u, end;
-    uint32_t b;
+    uint64_t at, end;           // of the next unit along the line; of this CTA's share
+    uint32_t b, next_head, next_unit;
     // of the present piece
     AttendBlock k;
     uint32_t head, j0, units;   // units j0 .. j0 + units of the tile
     bool in, out;               // another CTA has units before, behind
 
     __device__ Walk(const AttendArgs &p) {
-        const PlanHead &h = *p.w.head;
-        const uint64_t U = h.units[kKind];
-        const uint32_t S = h.ok ? h.ctas[kKind] : 0;
-        u = end = b = 0;
+        const PlanHead *h = p.w.head;
+        const uint64_t C = __ldcg(&h->cost[kKind]);
+        const uint32_t S = __ldcg(&h->ok) ? __ldcg(&h->ctas[kKind]) : 0;
+        at = end = 0;
+        b = next_head = next_unit = 0;
         if (blockIdx.x < S) {
-            u = blockIdx.x * U / S;
-            end = (blockIdx.x + 1) * U / S;
-            b = p.w.start[kKind][blockIdx.x];
+            const PlanStart *s = p.w.start[kKind] + blockIdx.x;
+            at = __ldcg(&s->at);
+            b = __ldcg(&s->block);
+            next_head = __ldcg(&s->head);
+            next_unit = __ldcg(&s->unit);
+            end = (blockIdx.x + 1) * C / S;
         }
     }
     __device__ bool next(const AttendArgs &p) {
-        if (u >= end) return false;
-        k = p.w.block[kKind][b];
-        uint64_t at = u - p.w.cum[kKind][b];
-        if (at >= (uint64_t)k.units * p.kv_heads) {
-            ++b;   // every block has units
-            k = p.w.block[kKind][b];
-            at = 0;
-        }
-        head = (uint32_t)(at / k.units);
-        j0 = (uint32_t)(at % k.units);
-        units = (uint32_t)min((uint64_t)(k.units - j0), end - u);
+        if (at >= end) return false;
+        static_assert(sizeof(AttendBlock) % 4 == 0);
+        const uint32_t *src = reinterpret_cast<const uint32_t *>(p.w.block[kKind] + b);
+        uint32_t *dst = reinterpret_cast<uint32_t *>(&k);
+#pragma unroll
+        for (uint32_t i = 0; i < sizeof(AttendBlock) / 4; ++i) dst[i] = __ldcg(src + i);
+        head = next_head;
+        j0 = next_unit;
         in = j0 > 0;
+        // units of the tile that begin before `end`; the second begins `over` later
+        const uint32_t over = in ? 0 : k.over, room = (uint32_t)min(end - at, (uint64_t)0x7FFFFFFF);
+        units = room <= over + k.cost ? 1 : (room - over + k.cost - 1) / k.cost;
+        units = min(units, k.units - j0);
         out = j0 + units < k.units;
-        u += units;
+        if (out) {
+            at = end;
+        } else {
+            at += over + (uint64_t)units * k.cost;
+            next_unit = 0;
+            if (++next_head == p.kv_heads) {
+                next_head = 0;
+                ++b;
+            }
+        }
         return true;
     }
     // Whether the rows go straight to the output, and if not their first row
@@ -302,7 +331,7 @@ struct KeyBoxes {
 #pragma unroll
         for (uint32_t i = 0; i < kEach; ++i) {
             const uint32_t x = first + 32 * kWarps * i, blk = (tok + (x / kHalves << p.box_log)) >> p.B_log;
-            page[i] = x < boxes && blk < blocks ? min((uint32_t)__ldg(table + blk), p.pages) : p.pages;
+            page[i] = x < boxes && blk < blocks ? min((uint32_t)__ldcg(table + blk), p.pages) : p.pages;
         }
     }
     __device__ __forceinline__ void load(const AttendArgs &p, const CUtensorMap *map, uint32_t dst, uint32_t bar, uint32_t tok,
@@ -315,6 +344,38 @@ struct KeyBoxes {
                 tma_load4(dst + half * kKeys * 128 + at * 128, map, bar, (int)half * 64, (int)((tok + at) & ((1u << p.B_log) - 1)),
                           (int)head, (int)page[i]);
         }
+    }
+};
+
+// A CTA's key slots of kKeys, one after another over its pieces, and the pages
+// of the next.
+template <int kKind, int D, int kKeys, uint32_t kWarps>
+struct Slots {
+    static constexpr uint32_t kUnit = kKind == 0 ? kWideKeys : kNarrowKeys;
+    Walk<kKind> w;
+    KeyBoxes<D, kKeys, kWarps> boxes;
+    const int32_t *table;
+    uint32_t blocks, tok, left, head;   // left: of the piece
+    bool more;
+
+    __device__ __forceinline__ Slots(const AttendArgs &p, const Walk<kKind> &from, uint32_t warp) : w(from), boxes(warp) {
+        left = 1;
+        tok = 0;
+        more = true;
+        step(p);
+    }
+    __device__ __forceinline__ void step(const AttendArgs &p) {
+        tok += kKeys;
+        if (--left == 0) {
+            more = w.next(p);
+            if (!more) return;
+            table = p.tables + (uint64_t)w.k.row * p.max_blocks;
+            blocks = ((uint32_t)w.k.kv1 + (1u << p.B_log) - 1) >> p.B_log;
+            tok = (uint32_t)w.k.kv0 + w.j0 * kUnit;
+            left = w.units * (kUnit / kKeys);
+            head = w.head;
+        }
+        boxes.find(p, table, tok, blocks);
     }
 };
 

@@ -69,6 +69,13 @@ __device__ __forceinline__ void fence_after() { asm volatile("tcgen05.fence::aft
 __device__ __forceinline__ void wait_st() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
 __device__ __forceinline__ void fence_async() { asm volatile("fence.proxy.async.shared::cta;" ::: "memory"); }
 
+// 32 bytes, 32-byte aligned.
+__device__ __forceinline__ void store32(void *to, const uint32_t *r) {
+    asm volatile("st.global.v8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};" ::"l"(to), "r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]),
+                 "r"(r[5]), "r"(r[6]), "r"(r[7])
+                 : "memory");
+}
+
 // True in one thread of the warp.
 __device__ __forceinline__ bool elect() {
     uint32_t one;
@@ -176,8 +183,11 @@ __global__ void __launch_bounds__(kWideT, 1)
         *gave_up = 0;
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     }
-    pdl_enter();
-    if (__syncthreads_or(has_err(p.status) || !p.w.head->ok || p.w.head->units[0] == 0)) return;
+    // first the wait, then the leave for the next kernel: the narrow one relies
+    // on all before this kernel being complete
+    asm volatile("griddepcontrol.wait;" ::: "memory");
+    asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+    if (__syncthreads_or(has_err(p.status) || !p.w.head->ok || blockIdx.x >= p.w.head->ctas[0])) return;
     if (wid == 9) {
         asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], 512;" ::"r"(s_at + W::kWord + 4) : "memory");
         asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;");
@@ -192,35 +202,18 @@ __global__ void __launch_bounds__(kWideT, 1)
     if (wid >= 8) {
         asm volatile("setmaxnreg.dec.sync.aligned.u32 88;");
         if (wid != 9) {
-            uint32_t c = 0;   // stages so far: K of unit 0, V of unit 0, K of unit 1, ...
             const uint32_t pw = wid == 8 ? 0 : wid - 9;
-            KeyBoxes<D, kWideKeys, 3> boxes(pw);
-            bool stop = false, more = w.next(p);
-            const int32_t *table = nullptr;
-            uint32_t blocks = 0, tok = 0, left = 0, head = 0;   // the next unit; units left of the piece
-            auto piece = [&] {
-                table = p.tables + (uint64_t)w.k.row * p.max_blocks;
-                blocks = ((uint32_t)w.k.kv1 + (1u << p.B_log) - 1) >> p.B_log;
-                tok = (uint32_t)w.k.kv0 + w.j0 * kWideKeys;
-                left = w.units;
-                head = w.head;
-            };
-            if (more) {
-                piece();
-                boxes.find(p, table, tok, blocks);
-            }
-            while (more && !stop) {
+            uint32_t c = 0;   // stages so far: K of unit 0, V of unit 0, K of unit 1, ...
+            bool stop = false;
+            for (Slots<0, D, kWideKeys, 3> next(p, w, pw); next.more && !stop; next.step(p)) {
                 for (uint32_t v = 0; v < 2; ++v, ++c) {
                     const uint32_t i = c % W::kStages, round = c / W::kStages;
                     if (round) mbar_wait(empty(i), (round - 1) & 1, gave_up, p.status);
                     if ((stop = __any_sync(~0u, *gave_up))) break;
                     if (pw == 0 && lane == 0) mbar_expect(full(i), W::kTile);   // the phase ends with this and all the bytes
                     __syncwarp();
-                    boxes.load(p, v ? &mv : &mk, s_at + W::kRing + i * W::kTile, full(i), tok, head);
+                    next.boxes.load(p, v ? &mv : &mk, s_at + W::kRing + i * W::kTile, full(i), next.tok, next.head);
                 }
-                tok += kWideKeys;
-                if (--left == 0 && (more = w.next(p))) piece();
-                if (more) boxes.find(p, table, tok, blocks);
             }
             // no copy may be in flight when the CTA ends
             for (uint32_t i = c > W::kStages ? c - W::kStages : 0; i < c; ++i)
@@ -350,7 +343,9 @@ __global__ void __launch_bounds__(kWideT, 1)
         while (more) {
             const uint32_t rows = min(128u, w.k.rows - 128 * x);
             const Row mine = row_at(p, w.k, 128 * x + min(r, rows - 1));
-            const int32_t limit = r < rows ? row_limit(w.k, mine.token) : 0;
+            // rows that are not there (their Q is zero) see everything: a row that
+            // is masked costs its warp the masking of every tile
+            const int32_t limit = r < rows ? row_limit(w.k, mine.token) : 1 << 30;
             Walk<0> ahead = w;
             more = next(ahead);
             float m = -INFINITY, l = 0.f;   // the maximum in the scores' own unit
@@ -436,20 +431,25 @@ __global__ void __launch_bounds__(kWideT, 1)
                 uint32_t o[32];
                 tm_ld(o, t_o + 32 * q);
                 wait_ld(o);
+                // A row per thread is 32 lines per store, so the widest store
+                // there is; 16 bytes where the caller's rows allow no more.
                 if (on && whole) {
+                    uint32_t y[16];
 #pragma unroll
-                    for (uint32_t i = 0; i < 32; i += 8) {
-                        uint4 v;
-                        v.x = Pack2<T>::pack(__uint_as_float(o[i]) * inv, __uint_as_float(o[i + 1]) * inv);
-                        v.y = Pack2<T>::pack(__uint_as_float(o[i + 2]) * inv, __uint_as_float(o[i + 3]) * inv);
-                        v.z = Pack2<T>::pack(__uint_as_float(o[i + 4]) * inv, __uint_as_float(o[i + 5]) * inv);
-                        v.w = Pack2<T>::pack(__uint_as_float(o[i + 6]) * inv, __uint_as_float(o[i + 7]) * inv);
-                        *reinterpret_cast<uint4 *>(dst + q * 64 + i * 2) = v;
+                    for (uint32_t i = 0; i < 16; ++i) y[i] = Pack2<T>::pack(__uint_as_float(o[2 * i]) * inv, __uint_as_float(o[2 * i + 1]) * inv);
+#pragma unroll
+                    for (uint32_t i = 0; i < 16; i += 8) {
+                        if (p.o_wide) {
+                            store32(dst + q * 64 + i * 4, y + i);
+                        } else {
+                            *reinterpret_cast<uint4 *>(dst + q * 64 + i * 4) = make_uint4(y[i], y[i + 1], y[i + 2], y[i + 3]);
+                            *reinterpret_cast<uint4 *>(dst + q * 64 + i * 4 + 16) = make_uint4(y[i + 4], y[i + 5], y[i + 6], y[i + 7]);
+                        }
                     }
                 } else if (on) {
-                    uint4 *to = reinterpret_cast<uint4 *>(p.w.part[0] + part * D + q * 32);
+                    float *to = p.w.part[0] + part * D + q * 32;
 #pragma unroll
-                    for (uint32_t i = 0; i < 8; ++i) to[i] = make_uint4(o[4 * i], o[4 * i + 1], o[4 * i + 2], o[4 * i + 3]);
+                    for (uint32_t i = 0; i < 32; i += 8) store32(to + i, o + i);
                 }
                 __syncwarp();
             }
