@@ -68,9 +68,10 @@ __device__ __forceinline__ int32_t group_at(const int32_t *offsets, const int32_
     return prefix[lo] > 0 ? (int32_t)lo : -1;
 }
 
-// CTA 0 lays the work out; the others see that a group's sequences begin with
-// the same pages.  Bound: latency, a chain of small steps (6 us for 256
-// sequences), so what is searched is kept in shared memory.
+// CTA 0 lays the wide blocks out and CTA 1 the narrow ones (both work out the
+// entities, writing the same); the others see that a group's sequences begin
+// with the same pages.  Bound: latency, a chain of small steps, so what is
+// searched is kept in shared memory.
 __global__ void __cluster_dims__(kPlanCl, 1, 1) __launch_bounds__(kPlanT) k_plan(PlanArgs p) {
     __shared__ uint64_t s_warp[32], s_cum[kFewBlocks];
     __shared__ int32_t s_offsets[kFewGroups + 1], s_prefix[kFewGroups];
@@ -81,16 +82,19 @@ __global__ void __cluster_dims__(kPlanCl, 1, 1) __launch_bounds__(kPlanT) k_plan
     const uint32_t rank = cl.block_rank(), tid = threadIdx.x;
     const bool few = p.groups <= kFewGroups;
     const int32_t *go = few ? s_offsets : p.group_offsets, *gp = few ? s_prefix : p.group_prefix;
-    uint32_t *gmax = few ? s_max : p.w.group_max, *gn = few ? s_n : p.w.group_n;
-    if (tid == 0) s_bad = 0;
+    uint32_t *gmax = few ? s_max : p.w.group_max + (rank & 1) * p.groups, *gn = few ? s_n : p.w.group_n + (rank & 1) * p.groups;
+    __shared__ uint64_t s_sum[4];   // cost and units of each kind
+    __shared__ uint32_t s_any;      // rank 0: some CTA found the step wrong
+    if (tid < 4) s_sum[tid] = 0;
+    if (tid == 0) s_bad = s_any = has_err(p.status);
     if (few)
         for (uint32_t g = tid; p.groups && g <= p.groups; g += kPlanT) {
             s_offsets[g] = p.group_offsets[g];
             if (g < p.groups) s_prefix[g] = p.group_prefix[g];
         }
-    if (rank == 0)
+    if (rank < 2)
         for (uint32_t g = tid; g < p.groups; g += kPlanT) gmax[g] = gn[g] = 0;
-    __syncthreads();
+    cl.sync();   // rank 0's s_any is set before another writes it
     bool bad = false;
     // every CTA: groups and sequences in range (the page check below relies on it)
     for (uint32_t g = tid; g < p.groups; g += kPlanT) {
@@ -108,7 +112,7 @@ __global__ void __cluster_dims__(kPlanCl, 1, 1) __launch_bounds__(kPlanT) k_plan
             const int64_t len = p.lengths[s], used = b - a;
             const int32_t g = group_at(go, gp, p.groups, i);
             bad |= len < 0 || len > (int64_t)p.max_blocks * p.B || (g >= 0 && used > 0 && gp[g] > len - used);
-            if (rank == 0 && g >= 0 && used) {
+            if (rank < 2 && g >= 0 && used) {
                 atomicMax(gmax + g, (uint32_t)used * p.G);
                 atomicAdd(gn + g, 1u);
             }
@@ -116,9 +120,9 @@ __global__ void __cluster_dims__(kPlanCl, 1, 1) __launch_bounds__(kPlanT) k_plan
         if (__syncthreads_or(bad)) s_bad = 1;
     }
     __syncthreads();
-    if (rank > 0 && !s_bad && p.groups) {   // a warp per sequence, against its group's first
-        const uint32_t lane = tid & 31, warps = (kPlanCl - 1) * kPlanT / 32;
-        for (uint32_t i = (rank - 1) * (kPlanT / 32) + tid / 32; i < p.n; i += warps) {
+    if (rank > 1 && !s_bad && p.groups) {   // a warp per sequence, against its group's first
+        const uint32_t lane = tid & 31, warps = (kPlanCl - 2) * kPlanT / 32;
+        for (uint32_t i = (rank - 2) * (kPlanT / 32) + tid / 32; i < p.n; i += warps) {
             const int32_t g = group_at(go, gp, p.groups, i);
             if (g < 0 || p.offsets[i + 1] == p.offsets[i]) continue;
             const int32_t *mine = p.tables + (uint64_t)p.seqs[i] * p.max_blocks;
@@ -129,7 +133,7 @@ __global__ void __cluster_dims__(kPlanCl, 1, 1) __launch_bounds__(kPlanT) k_plan
         }
         if (bad) s_bad = 1;
     }
-    if (rank == 0 && !s_bad) {
+    if (rank < 2 && !s_bad) {
         const uint32_t ents = p.groups + p.n;
         uint64_t carry = 0;   // wide blocks in the low half, narrow ones above
         for (uint32_t e0 = 0; e0 < ents; e0 += kPlanT) {
@@ -189,18 +193,29 @@ __global__ void __cluster_dims__(kPlanCl, 1, 1) __launch_bounds__(kPlanT) k_plan
             }
             return k;
         };
-        // What each kind costs, and its units.
-        uint64_t cost[2], units[2];
-        for (int kind = 0; kind < 2; ++kind) {
+        // What each kind costs, and its units.  A thread keeps the first block
+        // that it lays out.
+        const int kind = (int)rank;
+        AttendBlock mine{};
+        for (int kd = 0; kd < 2; ++kd) {
             uint64_t c = 0, u = 0;
-            for (uint32_t b = tid; b < count[kind]; b += kPlanT) {
-                const AttendBlock k = block_at(kind, b);
+            for (uint32_t b = tid; b < count[kd]; b += kPlanT) {
+                const AttendBlock k = block_at(kd, b);
+                if (kd == kind && b == tid) mine = k;
                 c += (uint64_t)(k.units * (uint64_t)k.cost + k.over) * p.kv_heads;
                 u += (uint64_t)k.units * p.kv_heads;
             }
-            block_scan(c, s_warp, cost[kind]);
-            block_scan(u, s_warp, units[kind]);
+            if (count[kd] > tid / 32 * 32) {   // the warp has some
+                c = scan_incl(c);
+                u = scan_incl(u);
+                if ((tid & 31) == 31) {
+                    atomicAdd(reinterpret_cast<unsigned long long *>(s_sum + 2 * kd), (unsigned long long)c);
+                    atomicAdd(reinterpret_cast<unsigned long long *>(s_sum + 2 * kd + 1), (unsigned long long)u);
+                }
+            }
         }
+        __syncthreads();
+        const uint64_t cost[2] = {s_sum[0], s_sum[2]}, units[2] = {s_sum[1], s_sum[3]};
         // The SMs are shared out so that both kernels, which run side by side,
         // take about as long; kNarrowPerSm narrow CTAs share an SM.
         uint32_t sms = 0;
@@ -209,60 +224,62 @@ __global__ void __cluster_dims__(kPlanCl, 1, 1) __launch_bounds__(kPlanT) k_plan
             sms = (uint32_t)((wide * p.ctas[0] + all / 2) / all);
             sms = max(1u, min(sms, units[1] ? p.ctas[0] - 1 : p.ctas[0]));
         }
-        for (int kind = 0; kind < 2; ++kind) {
-            if (units[kind] == 0) {
-                if (tid == 0) p.w.head->cost[kind] = p.w.head->inv[kind] = p.w.head->ctas[kind] = p.w.head->own[kind] = p.w.head->cuts[kind] = 0;
-                continue;
-            }
+        PlanHead *h = p.w.head;
+        const uint32_t mine_n = kind ? count[1] : count[0];
+        const uint64_t mine_cost = kind ? cost[1] : cost[0], mine_units = kind ? units[1] : units[0];
+        AttendBlock *block = kind ? p.w.block[1] : p.w.block[0];
+        PlanStart *start = kind ? p.w.start[1] : p.w.start[0];
+        uint64_t *all_cum = kind ? p.w.cum[1] : p.w.cum[0];
+        if (mine_units == 0) {
+            if (tid == 0) h->cost[kind] = h->inv[kind] = h->ctas[kind] = h->own[kind] = h->own_rows[kind] = h->cuts[kind] = 0;
+        } else {
             // Each CTA has a unit where its share is not less than the widest
             // gap between two units' beginnings.  So little work that this
             // would leave CTAs idle goes a unit at a time.
             const uint32_t most = kind == 0 ? sms : (p.ctas[0] - sms) * kNarrowPerSm;
             const uint32_t gap = kind == 0 ? max(p.costs.two, p.costs.one) + p.costs.wide_over : p.costs.narrow + p.costs.narrow_over;
-            const bool even = cost[kind] / gap < most;
-            const uint64_t C = even ? units[kind] : cost[kind];
+            const bool even = mine_cost / gap < most;
+            const uint64_t C = even ? mine_units : mine_cost;
             const uint32_t S = (uint32_t)min((uint64_t)most, C);
-            uint64_t *cum = count[kind] <= kFewBlocks ? s_cum : p.w.cum[kind];
-            uint64_t at0 = 0, parts0 = 0, own0 = 0;
+            uint64_t *cum = mine_n <= kFewBlocks ? s_cum : all_cum;
+            uint64_t at0 = 0, parts0 = 0;   // parts: rows below, blocks of their own from bit 40 on
             if (tid == 0) s_cuts = s_rows = 0;
-            for (uint32_t b0 = 0; b0 < count[kind]; b0 += kPlanT) {
+            for (uint32_t b0 = 0; b0 < mine_n; b0 += kPlanT) {
                 const uint32_t b = b0 + tid;
                 AttendBlock k{};
-                if (b < count[kind]) {
-                    k = block_at(kind, b);
+                if (b < mine_n) {
+                    k = b0 ? block_at(kind, b) : mine;
                     if (even) k.cost = 1, k.over = 0;
                 }
-                uint64_t length, parts, owns = 0;
+                uint64_t length, parts;
                 const uint64_t at = at0 + block_scan((uint64_t)(k.units * (uint64_t)k.cost + k.over) * p.kv_heads, s_warp, length);
-                uint64_t part = 0, own = 0;
+                at0 += length;
+                uint64_t part = 0;
                 if (p.groups) {
-                    part = parts0 + block_scan(k.shared ? (uint64_t)k.rows * p.kv_heads : 0, s_warp, parts);
-                    own = own0 + block_scan(k.shared == kOwn, s_warp, owns);
+                    part = parts0 + block_scan((k.shared ? (uint64_t)k.rows * p.kv_heads : 0) | (uint64_t)(k.shared == kOwn) << 40, s_warp, parts);
                     parts0 += parts;
-                    own0 += owns;
                 }
-                if (b < count[kind]) {
+                if (b < mine_n) {
                     if (k.shared == kOwn) {
-                        p.w.own[kind][own] = b;
+                        (kind ? p.w.own[1] : p.w.own[0])[part >> 40] = b;
                         atomicMax(&s_rows, k.rows);
                     }
                     k.part0 = (uint32_t)part;
-                    p.w.block[kind][b] = k;
-                    p.w.cum[kind][b] = at;
+                    block[b] = k;
+                    all_cum[b] = at;
                     cum[b] = at;
                 }
-                at0 += length;
             }
             __syncthreads();
             for (uint32_t c = tid; c < S; c += kPlanT) {
                 const uint64_t from = c * C / S;
-                uint32_t lo = 0, hi = count[kind];   // the last block that begins by then
+                uint32_t lo = 0, hi = mine_n;   // the last block that begins by then
                 while (hi - lo > 1) {
                     const uint32_t mid = (lo + hi) / 2;
                     if (cum[mid] <= from) lo = mid;
                     else hi = mid;
                 }
-                const AttendBlock k = p.w.block[kind][lo];
+                const AttendBlock k = block[lo];
                 const uint64_t tile = (uint64_t)k.units * k.cost + k.over, inside = from - cum[lo];
                 PlanStart x{0, lo, (uint32_t)(inside / tile), 0, 0};
                 const uint64_t begin = cum[lo] + x.head * tile, rest = from - begin;   // of the tile; into it
@@ -272,33 +289,50 @@ __global__ void __cluster_dims__(kPlanCl, 1, 1) __launch_bounds__(kPlanT) k_plan
                     x.unit = 0;
                     if (++x.head == p.kv_heads) x.head = 0, ++x.block;
                 }
-                p.w.start[kind][c] = x;
+                start[c] = x;
                 // the first boundary inside a tile
-                if (!k.shared && x.unit && (c - 1) * C / S <= begin) p.w.cut[kind][atomicAdd(&s_cuts, 1u)] = c;
+                if (!k.shared && x.unit && (c - 1) * C / S <= begin) (kind ? p.w.cut[1] : p.w.cut[0])[atomicAdd(&s_cuts, 1u)] = c;
             }
             __syncthreads();
             if (tid == 0) {
-                PlanHead *h = p.w.head;
                 h->cost[kind] = C;
                 h->inv[kind] = ~0ull / C;
                 h->ctas[kind] = S;
-                h->own[kind] = (uint32_t)own0;
+                h->own[kind] = (uint32_t)(parts0 >> 40);
                 h->own_rows[kind] = s_rows;
                 h->cuts[kind] = s_cuts;
             }
-            __syncthreads();
         }
     }
+    __syncthreads();
+    if (tid == 0 && s_bad) *cl.map_shared_rank(&s_any, 0) = 1;
     cl.sync();
-    if (rank == 0 && tid < 32) {
-        const bool any = tid < kPlanCl && *cl.map_shared_rank(&s_bad, tid);
-        const bool failed = __any_sync(~0u, any) || has_err(p.status);
-        if (tid == 0) {
-            p.w.head->ok = !failed;
-            if (failed) set_err(p.status, DM_ERR_INVALID_ARG);
-        }
+    const bool failed = rank == 0 ? s_any != 0 : s_bad != 0;
+    if (rank == 0 && tid == 0) {
+        p.w.head->ok = !failed;
+        if (failed) set_err(p.status, DM_ERR_INVALID_ARG);
     }
-    cl.sync();
+    if (s_bad || !p.groups) return;
+    // what joining needs of the shared groups' own blocks, all CTAs
+    const uint32_t own0 = __ldcg(p.w.head->own), owns = own0 + __ldcg(p.w.head->own + 1);
+    for (uint32_t i = rank * kPlanT + tid; i < owns; i += kPlanCl * kPlanT) {
+        const int kd = i >= own0;
+        const uint32_t j = kd ? i - own0 : i, b = __ldcg((kd ? p.w.own[1] : p.w.own[0]) + j);
+        JoinOwn x;
+        auto side = [&](int from, uint32_t blk, uint32_t row) {
+            const AttendBlock k = load_block(from ? p.w.block[1] : p.w.block[0], blk);
+            return JoinSide{__ldcg((from ? p.w.cum[1] : p.w.cum[0]) + blk), k.units, k.cost, k.over, k.rows, k.part0, row};
+        };
+        const AttendBlock k = load_block(kd ? p.w.block[1] : p.w.block[0], b);
+        const uint32_t cap = k.pre_kind ? kNarrowRows : kWideRows;
+        x.own = side(kd, b, 0);
+        x.pre_kind = k.pre_kind;
+        x.pre_block = k.pre + k.pre_row / cap;
+        x.pre = side((int)k.pre_kind, x.pre_block, k.pre_row % cap);
+        x.token = k.token;
+        x.lead = k.lead;
+        (kd ? p.w.join[1] : p.w.join[0])[j] = x;
+    }
 }
 
 // -- few rows: up to 16 per key head ------------------------------------------------
@@ -591,28 +625,7 @@ __global__ void __launch_bounds__(256, kJoinCtas) k_attend_join(AttendArgs p) {
     const uint64_t own1 = (uint64_t)h.own[1] * p.kv_heads * h.own_rows[1], own0 = own1 + (uint64_t)h.own[0] * p.kv_heads * h.own_rows[0];
     const uint64_t cut0 = own0 + (uint64_t)h.cuts[0] * kWideRows, jobs = cut0 + (uint64_t)h.cuts[1] * kNarrowRows;
     for (uint64_t t = blockIdx.x * 8ull + threadIdx.x / 32; t < jobs; t += gridDim.x * 8ull) {
-        uint32_t b, head, r;
-        int kind;
-        if (t < own0) {
-            kind = t < own1;
-            const uint64_t x = kind ? t : t - own1;
-            const uint32_t cap = kind ? h.own_rows[1] : h.own_rows[0];
-            const uint32_t tile = (uint32_t)(x / cap);
-            r = (uint32_t)(x % cap);
-            b = (kind ? p.w.own[1] : p.w.own[0])[tile / p.kv_heads];
-            head = tile % p.kv_heads;
-        } else {
-            kind = t >= cut0;
-            const uint64_t x = kind ? t - cut0 : t - own0;
-            const uint32_t cap = kind ? kNarrowRows : kWideRows;
-            r = (uint32_t)(x % cap);
-            const PlanStart &from = (kind ? p.w.start[1] : p.w.start[0])[(kind ? p.w.cut[1] : p.w.cut[0])[x / cap]];
-            b = from.block;
-            head = from.head;
-        }
-        const AttendBlock k = (kind ? p.w.block[1] : p.w.block[0])[b];
-        if (r >= k.rows) continue;
-        // a tile's parts: how many, and where row r of the i-th is
+        // a tile's parts: how many, and where a row of it is in the i-th
         struct Parts {
             const float *part;
             const float2 *ml;
@@ -620,14 +633,14 @@ __global__ void __launch_bounds__(256, kJoinCtas) k_attend_join(AttendArgs p) {
             uint64_t at;
             __device__ uint64_t row(uint32_t i) const { return at + (uint64_t)i * step + (i == 0 ? odd : 0); }
         };
-        auto parts = [&](int kd, uint32_t blk, const AttendBlock &x, uint32_t row) {
-            const uint64_t C = kd ? h.cost[1] : h.cost[0], begin = (kd ? p.w.cum[1] : p.w.cum[0])[blk] + head * ((uint64_t)x.units * x.cost + x.over);
+        auto parts = [&](int kd, const JoinSide &x, uint32_t head, uint32_t row, bool shared) {
+            const uint64_t C = kd ? h.cost[1] : h.cost[0], begin = x.cum + head * ((uint64_t)x.units * x.cost + x.over);
             const uint64_t last = begin + (x.units > 1 ? x.over + (x.units - 1ull) * x.cost : 0);   // its last unit
             const uint32_t cap = kd ? kNarrowRows : kWideRows, S = kd ? h.ctas[1] : h.ctas[0];
             const uint64_t inv = kd ? h.inv[1] : h.inv[0];
             const uint32_t c0 = cta_of(begin, C, inv, S), c1 = cta_of(last, C, inv, S);
             Parts q{kd ? p.w.part[1] : p.w.part[0], kd ? p.w.ml[1] : p.w.ml[0], c1 - c0 + 1, cap, 0, 0};
-            if (x.shared) {
+            if (shared) {
                 q.at = x.part0 + (uint64_t)head * x.rows + (uint64_t)cap * c0 + row;
             } else {
                 q.at = (kd ? p.w.shared_rows[1] : p.w.shared_rows[0]) + (uint64_t)cap * 2 * c0 + row;
@@ -636,12 +649,42 @@ __global__ void __launch_bounds__(256, kJoinCtas) k_attend_join(AttendArgs p) {
             }
             return q;
         };
-        Parts pre{};
-        if (k.shared) {
-            const uint32_t cap = k.pre_kind ? kNarrowRows : kWideRows, row = k.pre_row + r, blk = k.pre + row / cap;
-            pre = parts((int)k.pre_kind, blk, (k.pre_kind ? p.w.block[1] : p.w.block[0])[blk], row % cap);
+        uint32_t head, r, lead;
+        int32_t token;
+        Parts pre{}, own;
+        if (t < own0) {
+            const int kind = t < own1;
+            const uint64_t x = kind ? t : t - own1;
+            const uint32_t cap = kind ? h.own_rows[1] : h.own_rows[0], tile = (uint32_t)(x / cap);
+            r = (uint32_t)(x % cap);
+            head = tile % p.kv_heads;
+            const JoinOwn &k = (kind ? p.w.join[1] : p.w.join[0])[tile / p.kv_heads];
+            if (r >= k.own.rows) continue;
+            token = k.token;
+            lead = k.lead;
+            own = parts(kind, k.own, head, r, true);
+            JoinSide side = k.pre;
+            const uint32_t pre_cap = k.pre_kind ? kNarrowRows : kWideRows;
+            uint32_t row = side.row + r;
+            if (row >= pre_cap) {   // in the prefix's next block
+                row -= pre_cap;
+                const AttendBlock y = (k.pre_kind ? p.w.block[1] : p.w.block[0])[k.pre_block + 1];
+                side = {(k.pre_kind ? p.w.cum[1] : p.w.cum[0])[k.pre_block + 1], y.units, y.cost, y.over, y.rows, y.part0, 0};
+            }
+            pre = parts((int)k.pre_kind, side, head, row, true);
+        } else {
+            const int kind = t >= cut0;
+            const uint64_t x = kind ? t - cut0 : t - own0;
+            const uint32_t cap = kind ? kNarrowRows : kWideRows;
+            r = (uint32_t)(x % cap);
+            const PlanStart &from = (kind ? p.w.start[1] : p.w.start[0])[(kind ? p.w.cut[1] : p.w.cut[0])[x / cap]];
+            const AttendBlock y = (kind ? p.w.block[1] : p.w.block[0])[from.block];
+            if (r >= y.rows) continue;
+            head = from.head;
+            token = y.token;
+            lead = y.lead;
+            own = parts(kind, {(kind ? p.w.cum[1] : p.w.cum[0])[from.block], y.units, y.cost, y.over, y.rows, y.part0, 0}, head, r, false);
         }
-        const Parts own = parts(kind, b, k, r);
         const uint32_t N = pre.n + own.n;
         {
             float acc[V], M = -INFINITY, L = 0.f;
@@ -685,8 +728,8 @@ __global__ void __launch_bounds__(256, kJoinCtas) k_attend_join(AttendArgs p) {
                     }
                 }
             }
-            const Row at = row_at(p, k, r);
-            const uint64_t tok = (uint64_t)(k.token + at.token);
+            const Row at = row_at(p, lead, r);
+            const uint64_t tok = (uint64_t)(token + at.token);
             const uint32_t qh = head * p.G + at.head;
             const float inv = L > 0.f ? 1.f / L : 0.f;
             char *dst = p.o + tok * p.o_token + qh * p.o_head + lane * V * 2;

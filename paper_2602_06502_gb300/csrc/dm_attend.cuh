@@ -66,6 +66,19 @@ struct PlanCosts {
     uint32_t narrow, narrow_over;
 };
 
+// Where a block's parts are, and all that k_attend_join needs of a block of a
+// shared group's sequence.
+struct JoinSide {
+    uint64_t cum;
+    uint32_t units, cost, over, rows, part0, row;   // row: of the block's first row among that block's
+};
+struct alignas(16) JoinOwn {
+    JoinSide own, pre;
+    uint32_t pre_kind, pre_block;
+    int32_t token;
+    uint32_t lead;
+};
+
 // A sequence or a group of the step.
 struct PlanEntity {
     int32_t row, token, group, kv0, pos;
@@ -81,9 +94,10 @@ struct PlanWork {
     PlanStart *start[2];      // per CTA
     uint32_t *owner[2];       // per block: its entity
     uint32_t *own[2];         // the blocks of shared groups' sequences
+    JoinOwn *join[2];         // and what joining them needs
     uint32_t *cut[2];         // per other cut tile: the second CTA that has part of it
     PlanEntity *entity;       // groups, then sequences
-    uint32_t *group_max, *group_n;   // most rows of a sequence; sequences with rows
+    uint32_t *group_max, *group_n;   // most rows of a sequence; sequences with rows (two copies)
     float *part[2];           // rows x D
     float2 *ml[2];            // rows: maximum (base 2), sum
     uint64_t shared_rows[2];  // the parts' rows before the cut tiles' (two per CTA)
@@ -134,11 +148,12 @@ inline uint64_t plan_work(const PlanShape &s, void *base, PlanWork &w) {
         w.start[k] = (PlanStart *)take(sizeof(PlanStart) * s.ctas[k]);
         w.owner[k] = (uint32_t *)take(4ull * s.blocks[k]);
         w.own[k] = (uint32_t *)take(4ull * s.blocks[k]);
+        w.join[k] = (JoinOwn *)take(s.groups ? sizeof(JoinOwn) * s.blocks[k] : 0);
         w.cut[k] = (uint32_t *)take(4ull * s.ctas[k]);
     }
     w.entity = (PlanEntity *)take(sizeof(PlanEntity) * (s.n + (uint64_t)s.groups));
-    w.group_max = (uint32_t *)take(4ull * s.groups);
-    w.group_n = (uint32_t *)take(4ull * s.groups);
+    w.group_max = (uint32_t *)take(8ull * s.groups);
+    w.group_n = (uint32_t *)take(8ull * s.groups);
     for (int k = 0; k < 2; ++k) {
         w.part[k] = (float *)take(4ull * s.D * s.rows[k]);
         w.ml[k] = (float2 *)take(8ull * s.rows[k]);
@@ -171,6 +186,18 @@ __device__ __forceinline__ uint32_t cta_of(uint64_t at, uint64_t C, uint64_t inv
     return (uint32_t)(x - i * C >= C ? i + 1 : i);
 }
 
+// A block through L2: it may have been written by another CTA of this kernel, or
+// before a kernel that this one runs beside.
+__device__ __forceinline__ AttendBlock load_block(const AttendBlock *blocks, uint32_t b) {
+    static_assert(sizeof(AttendBlock) % 4 == 0);
+    AttendBlock k;
+    const uint32_t *src = reinterpret_cast<const uint32_t *>(blocks + b);
+    uint32_t *dst = reinterpret_cast<uint32_t *>(&k);
+#pragma unroll
+    for (uint32_t i = 0; i < sizeof(AttendBlock) / 4; ++i) dst[i] = __ldcg(src + i);
+    return k;
+}
+
 // Walks the tiles of a CTA's units.
 template <int kKind>
 struct Walk {
@@ -198,11 +225,7 @@ struct Walk {
     }
     __device__ bool next(const AttendArgs &p) {
         if (at >= end) return false;
-        static_assert(sizeof(AttendBlock) % 4 == 0);
-        const uint32_t *src = reinterpret_cast<const uint32_t *>(p.w.block[kKind] + b);
-        uint32_t *dst = reinterpret_cast<uint32_t *>(&k);
-#pragma unroll
-        for (uint32_t i = 0; i < sizeof(AttendBlock) / 4; ++i) dst[i] = __ldcg(src + i);
+        k = load_block(p.w.block[kKind], b);
         head = next_head;
         j0 = next_unit;
         in = j0 > 0;
@@ -237,10 +260,11 @@ struct Walk {
 struct Row {
     uint32_t token, head;
 };
-__device__ __forceinline__ Row row_at(const AttendArgs &p, const AttendBlock &k, uint32_t r) {
-    const uint32_t x = k.lead + r, t = p.G == 1 ? x : __umulhi(x, p.G_mul);
+__device__ __forceinline__ Row row_at(const AttendArgs &p, uint32_t lead, uint32_t r) {
+    const uint32_t x = lead + r, t = p.G == 1 ? x : __umulhi(x, p.G_mul);
     return {t, x - t * p.G};
 }
+__device__ __forceinline__ Row row_at(const AttendArgs &p, const AttendBlock &k, uint32_t r) { return row_at(p, k.lead, r); }
 // One past the last key that a token of a block sees.
 __device__ __forceinline__ int32_t row_limit(const AttendBlock &k, uint32_t token) {
     return min(k.kv1, k.pos + (int32_t)token + 1);
