@@ -198,9 +198,9 @@ __global__ void __launch_bounds__(kWideT, 1)
     const uint32_t tmem = *reinterpret_cast<volatile uint32_t *>(s + W::kWord + 4);
     Walk<0> w(p);
 
-    // 384 x 168 registers at the start; 2 x 128 x 208 + 128 x 88 are as many
+    // 384 x 168 registers at the start; 2 x 128 x 200 + 128 x 104 are as many
     if (wid >= 8) {
-        asm volatile("setmaxnreg.dec.sync.aligned.u32 88;");
+        asm volatile("setmaxnreg.dec.sync.aligned.u32 104;");
         if (wid != 9) {
             const uint32_t pw = wid == 8 ? 0 : wid - 9;
             uint32_t c = 0;   // stages so far: K of unit 0, V of unit 0, K of unit 1, ...
@@ -305,7 +305,7 @@ __global__ void __launch_bounds__(kWideT, 1)
             mbar_drain(done, 0);
         }
     } else {
-        asm volatile("setmaxnreg.inc.sync.aligned.u32 208;");
+        asm volatile("setmaxnreg.inc.sync.aligned.u32 200;");
         const uint32_t x = wid >> 2, r = tid & 127;   // tile, row (= tensor memory lane)
         const uint32_t lanes = (wid & 3) << 21;       // this warp's lanes of tensor memory
         const uint32_t t_s = tmem + W::kS + x * 128 + lanes, t_o = tmem + W::kO + x * D + lanes;
