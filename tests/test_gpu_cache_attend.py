@@ -208,3 +208,58 @@ def test_refusals(torch):
     c.attend(c.plan(b["seqs"], R.ints([0, 0, 0, 0]), 0, 4), none)
     c.attend(c.plan(R.ints([]), R.ints([0]), 0, 4), none)
     assert c.last_error() == 0
+
+
+@pytest.mark.parametrize("groups", [0, 700])
+def test_many_sequences(torch, groups):
+    """More sequences, groups and blocks than the plan keeps in shared memory."""
+    import random
+    rng = random.Random(groups)
+    n = 2600
+    sizes = None
+    if groups:
+        sizes = [rng.randint(2, 4) for _ in range(groups)]
+        while sum(sizes) > n:
+            sizes.pop()
+    own = [rng.randint(0, 70) for _ in range(n)]
+    new = [rng.choice([0, 1, 1, 1, 2, 9, 40]) for _ in range(n)]
+    run(torch, 50 + groups, hq=2, page=4, layout="heads", dtype=torch.bfloat16, dim=64, kv_heads=1, groups=sizes,
+        prefix=[4 * rng.randint(1, 12) for _ in sizes or []], own=own, new=new)
+
+
+def test_long_prompt_of_many_blocks(torch):
+    """A prompt of more row blocks than threads lay out at once."""
+    run(torch, 60, hq=64, page=64, layout="tokens", dtype=torch.float16, dim=64, kv_heads=1, own=[0, 3], new=[4500, 1])
+
+
+def test_one_sm_each(torch):
+    """A little wide work beside much narrow work, and the other way round."""
+    run(torch, 61, hq=8, page=16, layout="heads", dtype=torch.bfloat16, dim=128, kv_heads=1, own=[9000] * 20 + [3], new=[1] * 20 + [5])
+    run(torch, 62, hq=8, page=16, layout="heads", dtype=torch.bfloat16, dim=128, kv_heads=1, own=[7, 2000, 30], new=[1, 600, 1])
+
+
+def test_layers_of_one_plan_and_graphs(torch):
+    """One plan for several layers, captured into a graph and replayed."""
+    import cache_reference as R
+    b = R.make_batch(70, page=16, kv_heads=2, dim=128, dtype=torch.bfloat16, layers=3, groups=[6], prefix=(320,),
+                     own=[5, 40, 0, 17, 33, 100, 600], new=[1, 1, 2, 1, 1, 1, 130])
+    c, T = b["cache"], b["tokens"]
+    q = torch.randn(T, 8, 128, generator=b["gen"], device="cuda").bfloat16()
+    plan = c.plan(b["seqs"], b["offsets"], T, 8, b["group_offsets"], b["group_prefix"])
+    outs = [torch.empty_like(q) for _ in range(3)]
+    want = [c.attend(plan, q, layer=i) for i in range(3)]
+    s = torch.cuda.Stream()
+    s.wait_stream(torch.cuda.current_stream())
+    g = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(g, stream=s):
+        for i in range(3):
+            c.attend(plan, q, layer=i, out=outs[i])
+    for _ in range(3):
+        for o in outs:
+            o.zero_()
+        g.replay()
+    assert c.last_error() == 0
+    for i in range(3):
+        ref, _, mass = R.attend_reference(b, q, 128 ** -0.5, i)
+        assert torch.equal(outs[i], want[i])
+        assert bool(((outs[i].double() - ref).abs() <= R.attend_bound(ref, mass, torch.bfloat16, 700, 6.0)).all())

@@ -206,3 +206,35 @@ def test_argument_checks(torch):
         c.free(ints([0]).long())
     with pytest.raises(D.DualMapError):   # more than the sequences there are
         c.free(ints([0] * 41))
+
+
+def test_many_requests(torch):
+    """More requests in a call than are searched in shared memory."""
+    from cache_reference import ints
+    n = 5000
+    c, m = make(torch, pages=30_000, page_tokens=4, max_seqs=2 * n, max_blocks=6, layers=1, kv_heads=1)
+    rng = random.Random(8)
+    k = c.k.clone()
+    seqs, add = rng.sample(range(2 * n), n), [rng.randint(0, 20) for _ in range(n)]
+    m.extend(seqs, add)
+    c.extend(ints(seqs), ints(add))
+    assert c.last_error() == 0
+    same_books(c, m)
+    live = [s for s in seqs if m.lengths[s]]
+    kids = [s for s in range(2 * n) if not m.lengths[s]][:n]
+    par = [rng.choice(live) for _ in kids]
+    keep = [rng.randint(0, m.lengths[p]) for p in par]
+    for old, new, tail in m.fork(par, kids, keep):
+        copy_tail(k, "heads", old, new, tail)
+    c.fork(ints(par), ints(kids), ints(keep))
+    assert c.last_error() == 0
+    same_books(c, m)
+    assert torch.equal(c.k.view(torch.int16), k.view(torch.int16))
+    m.free(live)
+    c.free(ints(live))
+    m.compact()
+    c.compact()
+    same_books(c, m)
+    m.free(kids)
+    c.free(ints(kids))
+    assert c.refs.sum().item() == 0
