@@ -8,6 +8,8 @@ Calls on one cache, and the attention of one plan, have to be ordered by the
 caller, as work that shares a tensor is.
 """
 
+import ctypes as C
+
 import torch
 
 from . import dualmap as D
@@ -20,7 +22,7 @@ class Plan:
     """One step's division over the GPU (PagedCache.plan), for all its layers."""
 
     def __init__(self, struct, keep, tokens, q_heads):
-        self.struct, self.keep, self.tokens, self.q_heads = struct, keep, tokens, q_heads
+        self.struct, self.ref, self.keep, self.tokens, self.q_heads = struct, C.byref(struct), keep, tokens, q_heads
 
 
 class PagedCache:
@@ -59,6 +61,7 @@ class PagedCache:
             raise D.DualMapError(D.DM_ERR_INVALID_ARG, "dm_cache_work_bytes")
         self.work = torch.empty(size, dtype=torch.uint8, device=self.device)
         self.struct.work, self.struct.work_bytes = self.work.data_ptr(), size
+        self._lib, self._ref, self._plan_bytes = D.lib(), C.byref(self.struct), {}
 
     @classmethod
     def empty(cls, *, pages, kv_heads, head_dim, max_seqs, max_tokens, page_tokens=16, layers=1, dtype=torch.bfloat16,
@@ -102,7 +105,7 @@ class PagedCache:
         if torch.cuda.current_device() != self.device.index:
             with torch.cuda.device(self.device):
                 return self._call(name, *args)
-        rc = getattr(D, name)(self.struct, *args, torch._C._cuda_getCurrentRawStream(self.device.index))
+        rc = getattr(self._lib, name)(self._ref, *args, torch._C._cuda_getCurrentRawStream(self.device.index))
         if rc:
             raise D.DualMapError(rc, name)
 
@@ -168,7 +171,7 @@ class PagedCache:
         a = D.dm_append_args(self._ints("seqs", seqs), self._ints("offsets", offsets, n + 1), n, tokens, layer, heads,
                              qp, kp, vp, op, qt, qh, kt, kh, vt, vh, ot, oh, self._vector("q_weight", q_weight),
                              self._vector("k_weight", k_weight), cp, sp, rows, 2 * dims, bool(interleaved), eps)
-        self._call("dm_cache_append", a)
+        self._call("dm_cache_append", C.byref(a))
         return out
 
     def plan(self, seqs, offsets, tokens, q_heads, group_offsets=None, group_prefix=None):
@@ -181,13 +184,19 @@ class PagedCache:
         if group_prefix is not None:
             groups = group_prefix.shape[0]
             gp, go = self._ints("group_prefix", group_prefix), self._ints("group_offsets", group_offsets, groups + 1)
-        size = D.dm_plan_bytes(self.struct, n, groups, tokens, q_heads)
-        if not size:
-            raise D.DualMapError(D.DM_ERR_INVALID_ARG, "dm_plan_bytes")
+        shape = (n, groups, tokens, q_heads)
+        size = self._plan_bytes.get(shape)
+        if size is None:
+            size = D.dm_plan_bytes(self.struct, *shape)
+            if not size:
+                raise D.DualMapError(D.DM_ERR_INVALID_ARG, "dm_plan_bytes")
+            if len(self._plan_bytes) > 4096:
+                self._plan_bytes.clear()
+            self._plan_bytes[shape] = size
         work = torch.empty(size, dtype=torch.uint8, device=self.device)
         s = D.dm_plan(self._ints("seqs", seqs), self._ints("offsets", offsets, n + 1), n, tokens, q_heads, groups, go, gp,
                       work.data_ptr(), size)
-        self._call("dm_cache_plan", s)
+        self._call("dm_cache_plan", C.byref(s))
         return Plan(s, (seqs, offsets, group_offsets, group_prefix, work), tokens, q_heads)
 
     def attend(self, plan, q, *, layer=0, scale=None, out=None, lse=None):
@@ -203,5 +212,5 @@ class PagedCache:
             raise ValueError(f"lse: contiguous float32 of shape {(plan.tokens, plan.q_heads)} on {self.device}")
         a = D.dm_attend_args(layer, self.head_dim ** -0.5 if scale is None else scale, qp, op,
                              None if lse is None else lse.data_ptr(), qt, qh, ot, oh)
-        self._call("dm_cache_attend", plan.struct, a)
+        self._call("dm_cache_attend", plan.ref, C.byref(a))
         return out
