@@ -19,7 +19,9 @@ namespace {
 
 // -- the plan ----------------------------------------------------------------------
 
-constexpr uint32_t kPlanCl = 8, kPlanT = 1024;
+// 256 threads a CTA for a few sequences (9.9 -> 8.3 us for four; with 256
+// sequences the page check needs them all).
+constexpr uint32_t kPlanCl = 8, kPlanT = 1024, kPlanFew = 32;
 
 struct PlanArgs {
     PlanWork w;
@@ -47,7 +49,7 @@ __device__ uint64_t block_scan(uint64_t x, uint64_t *s_warp, uint64_t &total) {
     __syncthreads();
     if (wid == 0) s_warp[lane] = scan_incl(s_warp[lane]);
     __syncthreads();
-    total = s_warp[kPlanT / 32 - 1];
+    total = s_warp[blockDim.x / 32 - 1];
     return in - x + (wid ? s_warp[wid - 1] : 0);
 }
 
@@ -79,7 +81,7 @@ __global__ void __cluster_dims__(kPlanCl, 1, 1) __launch_bounds__(kPlanT) k_plan
     __shared__ uint32_t s_bad, s_cuts, s_rows;
     pdl_enter();
     cg::cluster_group cl = cg::this_cluster();
-    const uint32_t rank = cl.block_rank(), tid = threadIdx.x;
+    const uint32_t rank = cl.block_rank(), tid = threadIdx.x, T = blockDim.x;
     const bool few = p.groups <= kFewGroups;
     const int32_t *go = few ? s_offsets : p.group_offsets, *gp = few ? s_prefix : p.group_prefix;
     uint32_t *gmax = few ? s_max : p.w.group_max + (rank & 1) * p.groups, *gn = few ? s_n : p.w.group_n + (rank & 1) * p.groups;
@@ -88,22 +90,22 @@ __global__ void __cluster_dims__(kPlanCl, 1, 1) __launch_bounds__(kPlanT) k_plan
     if (tid < 4) s_sum[tid] = 0;
     if (tid == 0) s_bad = s_any = has_err(p.status);
     if (few)
-        for (uint32_t g = tid; p.groups && g <= p.groups; g += kPlanT) {
+        for (uint32_t g = tid; p.groups && g <= p.groups; g += T) {
             s_offsets[g] = p.group_offsets[g];
             if (g < p.groups) s_prefix[g] = p.group_prefix[g];
         }
     if (rank < 2)
-        for (uint32_t g = tid; g < p.groups; g += kPlanT) gmax[g] = gn[g] = 0;
+        for (uint32_t g = tid; g < p.groups; g += T) gmax[g] = gn[g] = 0;
     cl.sync();   // rank 0's s_any is set before another writes it
     bool bad = false;
     // every CTA: groups and sequences in range (the page check below relies on it)
-    for (uint32_t g = tid; g < p.groups; g += kPlanT) {
+    for (uint32_t g = tid; g < p.groups; g += T) {
         const int32_t a = go[g], b = go[g + 1], P = gp[g];
         bad |= a < 0 || b < a || b > (int32_t)p.n || P < 0 || P % (int32_t)p.B || (uint32_t)P > p.max_blocks * p.B;
     }
     if (__syncthreads_or(bad)) s_bad = 1;
     if (!s_bad) {
-        for (uint32_t i = tid; i < p.n; i += kPlanT) {
+        for (uint32_t i = tid; i < p.n; i += T) {
             const int32_t s = p.seqs[i], a = p.offsets[i], b = p.offsets[i + 1];
             if ((uint32_t)s >= p.max_seqs || a < 0 || b < a || b > (int32_t)p.tokens) {
                 bad = true;
@@ -121,8 +123,8 @@ __global__ void __cluster_dims__(kPlanCl, 1, 1) __launch_bounds__(kPlanT) k_plan
     }
     __syncthreads();
     if (rank > 1 && !s_bad && p.groups) {   // a warp per sequence, against its group's first
-        const uint32_t lane = tid & 31, warps = (kPlanCl - 2) * kPlanT / 32;
-        for (uint32_t i = (rank - 2) * (kPlanT / 32) + tid / 32; i < p.n; i += warps) {
+        const uint32_t lane = tid & 31, warps = (kPlanCl - 2) * T / 32;
+        for (uint32_t i = (rank - 2) * (T / 32) + tid / 32; i < p.n; i += warps) {
             const int32_t g = group_at(go, gp, p.groups, i);
             if (g < 0 || p.offsets[i + 1] == p.offsets[i]) continue;
             const int32_t *mine = p.tables + (uint64_t)p.seqs[i] * p.max_blocks;
@@ -136,7 +138,7 @@ __global__ void __cluster_dims__(kPlanCl, 1, 1) __launch_bounds__(kPlanT) k_plan
     if (rank < 2 && !s_bad) {
         const uint32_t ents = p.groups + p.n;
         uint64_t carry = 0;   // wide blocks in the low half, narrow ones above
-        for (uint32_t e0 = 0; e0 < ents; e0 += kPlanT) {
+        for (uint32_t e0 = 0; e0 < ents; e0 += T) {
             const uint32_t e = e0 + tid;
             PlanEntity x{};
             if (e < ents) {
@@ -199,7 +201,7 @@ __global__ void __cluster_dims__(kPlanCl, 1, 1) __launch_bounds__(kPlanT) k_plan
         AttendBlock mine{};
         for (int kd = 0; kd < 2; ++kd) {
             uint64_t c = 0, u = 0;
-            for (uint32_t b = tid; b < count[kd]; b += kPlanT) {
+            for (uint32_t b = tid; b < count[kd]; b += T) {
                 const AttendBlock k = block_at(kd, b);
                 if (kd == kind && b == tid) mine = k;
                 c += (uint64_t)(k.units * (uint64_t)k.cost + k.over) * p.kv_heads;
@@ -244,7 +246,7 @@ __global__ void __cluster_dims__(kPlanCl, 1, 1) __launch_bounds__(kPlanT) k_plan
             uint64_t *cum = mine_n <= kFewBlocks ? s_cum : all_cum;
             uint64_t at0 = 0, parts0 = 0;   // parts: rows below, blocks of their own from bit 40 on
             if (tid == 0) s_cuts = s_rows = 0;
-            for (uint32_t b0 = 0; b0 < mine_n; b0 += kPlanT) {
+            for (uint32_t b0 = 0; b0 < mine_n; b0 += T) {
                 const uint32_t b = b0 + tid;
                 AttendBlock k{};
                 if (b < mine_n) {
@@ -271,7 +273,7 @@ __global__ void __cluster_dims__(kPlanCl, 1, 1) __launch_bounds__(kPlanT) k_plan
                 }
             }
             __syncthreads();
-            for (uint32_t c = tid; c < S; c += kPlanT) {
+            for (uint32_t c = tid; c < S; c += T) {
                 const uint64_t from = c * C / S;
                 uint32_t lo = 0, hi = mine_n;   // the last block that begins by then
                 while (hi - lo > 1) {
@@ -315,7 +317,7 @@ __global__ void __cluster_dims__(kPlanCl, 1, 1) __launch_bounds__(kPlanT) k_plan
     if (s_bad || !p.groups) return;
     // what joining needs of the shared groups' own blocks, all CTAs
     const uint32_t own0 = __ldcg(p.w.head->own), owns = own0 + __ldcg(p.w.head->own + 1);
-    for (uint32_t i = rank * kPlanT + tid; i < owns; i += kPlanCl * kPlanT) {
+    for (uint32_t i = rank * T + tid; i < owns; i += kPlanCl * T) {
         const int kd = i >= own0;
         const uint32_t j = kd ? i - own0 : i, b = __ldcg((kd ? p.w.own[1] : p.w.own[0]) + j);
         JoinOwn x;
@@ -809,7 +811,7 @@ extern "C" dm_status dm_cache_plan(const dm_cache *c, const dm_plan *pl, void *s
     p.n = pl->n, p.groups = pl->groups, p.tokens = pl->tokens, p.G = s.G, p.kv_heads = c->kv_heads, p.B = c->page_tokens;
     p.max_seqs = c->max_seqs, p.max_blocks = c->max_blocks, p.ctas[0] = s.ctas[0], p.ctas[1] = s.ctas[1];
     p.costs = c->head_dim == 128 ? kCosts128 : kCosts64;
-    return status_of(launch_pdl(k_plan, kPlanCl, kPlanT, 0, static_cast<cudaStream_t>(stream), p));
+    return status_of(launch_pdl(k_plan, kPlanCl, pl->n <= kPlanFew ? 256 : kPlanT, 0, static_cast<cudaStream_t>(stream), p));
 }
 
 extern "C" dm_status dm_cache_attend(const dm_cache *c, const dm_plan *pl, const dm_attend_args *a, void *stream) {
