@@ -615,10 +615,11 @@ __global__ void __launch_bounds__(kNarrowT, kNarrowPerSm)
 // order of the CTAs that left them.  32 parts' maxima and sums are looked at
 // together, so that the parts themselves are independent loads.  Bound:
 // latency, then L2 (4 D + 8 bytes a row and part).
-constexpr uint32_t kJoinCtas = 4, kAhead = 4;
-
-template <class T, int D>
-__global__ void __launch_bounds__(256, kJoinCtas) k_attend_join(AttendArgs p) {
+// kAhead parts are loaded at once: four with four CTAs an SM where there are
+// many rows, 16 with one where the GPU has a warp for each row anyway
+// (attend_few's 27 parts a row: 5.5 us with four).
+template <class T, int D, uint32_t kAhead, uint32_t kCtas>
+__global__ void __launch_bounds__(256, kCtas) k_attend_join(AttendArgs p) {
     constexpr int V = D / 32;
     pdl_enter();
     const PlanHead h = *p.w.head;
@@ -780,7 +781,8 @@ cudaError_t launch_rest(const AttendArgs &p, uint64_t rows, const CUtensorMap &m
     DM_TRY(launch_pdl(k_attend_narrow<T, D>, p.ctas[1], kNarrowT, Narrow<D>::kBytes, st, mk, mv, p));
     // a warp per row, or as many as the GPU holds
     const uint64_t warps = std::min<uint64_t>(rows, (uint64_t)p.ctas[0] * 64);
-    return launch_pdl(k_attend_join<T, D>, (uint32_t)((warps + 7) / 8), 256, 0, st, p);
+    const auto join = rows <= p.ctas[0] * 8ull ? k_attend_join<T, D, 16, 1> : k_attend_join<T, D, 4, 4>;
+    return launch_pdl(join, (uint32_t)((warps + 7) / 8), 256, 0, st, p);
 }
 
 uint32_t log2_of(uint32_t x) { return 31 - (uint32_t)__builtin_clz(x); }
