@@ -737,7 +737,10 @@ typedef struct {
  * they hold.  Scores, maxima, sums and the output are held in 32 bits; the
  * weights are rounded to the cache's type for the product with v.  Rows
  * outside offsets[0] .. offsets[n] are not touched.  Uses the plan's work
- * buffer, so layers of one plan run one after another.  Recorded:
+ * buffer, so layers of one plan run one after another.  A key or value in a
+ * sequence's own slots that is not finite can reach the step's other rows of
+ * that sequence, those before it too (a weight of zero does not silence it).
+ * Recorded: DM_ERR_INVALID_ARG (the buffer holds no plan of this shape),
  * DM_ERR_TIMEOUT (a wait in the kernel gave up).  Asynchronous. */
 DM_API dm_status dm_cache_attend(const dm_cache *c, const dm_plan *p, const dm_attend_args *a, void *stream);
 

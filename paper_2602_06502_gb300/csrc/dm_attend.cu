@@ -27,7 +27,7 @@ struct PlanArgs {
     PlanWork w;
     const int32_t *tables, *lengths, *seqs, *offsets, *group_offsets, *group_prefix;
     uint32_t *status;
-    uint32_t n, groups, tokens, G, kv_heads, B, max_seqs, max_blocks, ctas[2];
+    uint32_t n, groups, tokens, G, kv_heads, B, max_seqs, max_blocks, key, ctas[2];
     PlanCosts costs;
 };
 
@@ -153,7 +153,7 @@ __global__ void __cluster_dims__(kPlanCl, 1, 1) __launch_bounds__(kPlanT) k_plan
                     x.rows = (uint32_t)(last - x.token) * p.G;
                     x.shared = e < p.groups ? kPrefix : shares ? kOwn : 0;
                     x.kv0 = e < p.groups || !shares ? 0 : gp[g];
-                    x.pos = e < p.groups ? 1 << 30 /* behind every key */ : p.lengths[x.row] - (last - x.token);
+                    x.pos = e < p.groups ? gp[e] - 1 : p.lengths[x.row] - (last - x.token);
                 }
             }
             const uint64_t mine = x.rows == 0 ? 0 : x.rows <= kNarrowRows ? 1ull << 32 : (x.rows + kWideRows - 1) / kWideRows;
@@ -182,7 +182,7 @@ __global__ void __cluster_dims__(kPlanCl, 1, 1) __launch_bounds__(kPlanT) k_plan
             k.token = x.token + (int32_t)(row0 / p.G);
             k.kv0 = x.kv0;
             k.shared = x.shared;
-            k.pos = x.pos + (int32_t)(row0 / p.G);
+            k.pos = x.pos + (x.shared == kPrefix ? 0 : (int32_t)(row0 / p.G));
             k.kv1 = x.shared == kPrefix ? gp[e] : max(k.kv0, k.pos + (int32_t)((k.lead + k.rows - 1) / p.G) + 1);
             k.units = max(1u, ((uint32_t)(k.kv1 - k.kv0) + keys - 1) / keys);
             k.cost = kind ? p.costs.narrow : k.rows > 128 ? p.costs.two : p.costs.one;
@@ -311,7 +311,7 @@ __global__ void __cluster_dims__(kPlanCl, 1, 1) __launch_bounds__(kPlanT) k_plan
     cl.sync();
     const bool failed = rank == 0 ? s_any != 0 : s_bad != 0;
     if (rank == 0 && tid == 0) {
-        p.w.head->ok = !failed;
+        p.w.head->key = failed ? kRefused : p.key;
         if (failed) set_err(p.status, DM_ERR_INVALID_ARG);
     }
     if (s_bad || !p.groups) return;
@@ -588,13 +588,13 @@ __global__ void __launch_bounds__(kNarrowT, kNarrowPerSm)
                     const Row at = row_at(p, w.k, row);
                     const uint64_t tok = (uint64_t)(w.k.token + at.token);
                     const uint32_t h = w.head * p.G + at.head;
-                    const float inv = L > 0.f ? 1.f / L : 0.f;
+                    const float inv = L == 0.f ? 0.f : 1.f / L;
                     char *dst = p.o + tok * p.o_token + h * p.o_head + col * 2;
 #pragma unroll
                     for (uint32_t e = 0; e < kMine; e += 4)
                         *reinterpret_cast<uint2 *>(dst + e * 2) =
                             make_uint2(Pack2<T>::pack(acc[e] * inv, acc[e + 1] * inv), Pack2<T>::pack(acc[e + 2] * inv, acc[e + 3] * inv));
-                    if (p.lse && wid == 0 && t4 == 0) p.lse[tok * p.q_heads + h] = L > 0.f ? (M + log2f(L)) * 0.69314718056f : -INFINITY;
+                    if (p.lse && wid == 0 && t4 == 0) p.lse[tok * p.q_heads + h] = L == 0.f ? -INFINITY : (M + log2f(L)) * 0.69314718056f;
                 } else {
 #pragma unroll
                     for (uint32_t e = 0; e < kMine; e += 4)
@@ -624,7 +624,11 @@ __global__ void __launch_bounds__(256, kCtas) k_attend_join(AttendArgs p) {
     pdl_enter();
     const PlanHead h = *p.w.head;
     const uint32_t lane = threadIdx.x & 31;
-    if (has_err(p.status) || !h.ok) return;
+    if (has_err(p.status)) return;
+    if (h.key != p.key) {   // no plan, or one of another step's shape: the kernels before this one did nothing either
+        if (h.key != kRefused && blockIdx.x == 0 && threadIdx.x == 0) set_err(p.status, DM_ERR_INVALID_ARG);
+        return;
+    }
     const uint64_t own1 = (uint64_t)h.own[1] * p.kv_heads * h.own_rows[1], own0 = own1 + (uint64_t)h.own[0] * p.kv_heads * h.own_rows[0];
     const uint64_t cut0 = own0 + (uint64_t)h.cuts[0] * kWideRows, jobs = cut0 + (uint64_t)h.cuts[1] * kNarrowRows;
     for (uint64_t t = blockIdx.x * 8ull + threadIdx.x / 32; t < jobs; t += gridDim.x * 8ull) {
@@ -734,11 +738,11 @@ __global__ void __launch_bounds__(256, kCtas) k_attend_join(AttendArgs p) {
             const Row at = row_at(p, lead, r);
             const uint64_t tok = (uint64_t)(token + at.token);
             const uint32_t qh = head * p.G + at.head;
-            const float inv = L > 0.f ? 1.f / L : 0.f;
+            const float inv = L == 0.f ? 0.f : 1.f / L;
             char *dst = p.o + tok * p.o_token + qh * p.o_head + lane * V * 2;
             if constexpr (V == 4) *reinterpret_cast<uint2 *>(dst) = make_uint2(Pack2<T>::pack(acc[0] * inv, acc[1] * inv), Pack2<T>::pack(acc[2] * inv, acc[3] * inv));
             else *reinterpret_cast<uint32_t *>(dst) = Pack2<T>::pack(acc[0] * inv, acc[1] * inv);
-            if (p.lse && lane == 0) p.lse[tok * p.q_heads + qh] = L > 0.f ? (M + log2f(L)) * 0.69314718056f : -INFINITY;
+            if (p.lse && lane == 0) p.lse[tok * p.q_heads + qh] = L == 0.f ? -INFINITY : (M + log2f(L)) * 0.69314718056f;
         }
     }
 }
@@ -811,7 +815,7 @@ extern "C" dm_status dm_cache_plan(const dm_cache *c, const dm_plan *pl, void *s
     p.tables = c->tables, p.lengths = c->lengths, p.status = c->status;
     p.seqs = pl->seqs, p.offsets = pl->offsets, p.group_offsets = pl->group_offsets, p.group_prefix = pl->group_prefix;
     p.n = pl->n, p.groups = pl->groups, p.tokens = pl->tokens, p.G = s.G, p.kv_heads = c->kv_heads, p.B = c->page_tokens;
-    p.max_seqs = c->max_seqs, p.max_blocks = c->max_blocks, p.ctas[0] = s.ctas[0], p.ctas[1] = s.ctas[1];
+    p.max_seqs = c->max_seqs, p.max_blocks = c->max_blocks, p.ctas[0] = s.ctas[0], p.ctas[1] = s.ctas[1], p.key = s.key;
     p.costs = c->head_dim == 128 ? kCosts128 : kCosts64;
     return status_of(launch_pdl(k_plan, kPlanCl, pl->n <= kPlanFew ? 256 : kPlanT, 0, static_cast<cudaStream_t>(stream), p));
 }
@@ -832,7 +836,7 @@ extern "C" dm_status dm_cache_attend(const dm_cache *c, const dm_plan *pl, const
     p.max_blocks = c->max_blocks, p.pages = c->pages, p.B_log = log2_of(c->page_tokens), p.box_log = log2_of(box);
     p.G_mul = (uint32_t)((0xFFFFFFFFull + s.G) / s.G);   // 2^32 / G, rounded up
     p.G = s.G, p.kv_heads = c->kv_heads, p.q_heads = s.q_heads, p.scale2 = a->scale * 1.44269504089f;
-    p.ctas[0] = s.ctas[0], p.ctas[1] = s.ctas[1];
+    p.ctas[0] = s.ctas[0], p.ctas[1] = s.ctas[1], p.key = s.key;
     p.o_wide = aligned(a->o, 32) && (a->o_token | a->o_head) % 16 == 0;
     CUtensorMap mk, mv;
     if (!page_map(&mk, c, c->k, a->layer, box) || !page_map(&mv, c, c->v, a->layer, box)) return DM_ERR_CUDA;

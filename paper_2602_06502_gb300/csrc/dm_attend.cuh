@@ -33,7 +33,7 @@ struct AttendBlock {
     int32_t token;        // query token of its first row
     uint32_t lead, rows;  // that row's head within G; its rows
     int32_t kv0, kv1;     // keys; no row sees one from kv1 on
-    int32_t pos;          // the first token's position (a group's prefix: all rows see all keys)
+    int32_t pos;          // the first token's position; a group's prefix, all of which all rows see: its last key
     uint32_t units;       // per key head, >= 1
     uint32_t cost, over;
     uint32_t part0;       // shared: its first row in the parts
@@ -51,8 +51,10 @@ struct PlanHead {
     uint32_t own[2];      // blocks of shared groups' sequences
     uint32_t own_rows[2]; // the most rows of one
     uint32_t cuts[2];     // other tiles that more than one CTA has part of
-    uint32_t ok, pad;
+    uint32_t key, pad;    // the step's shape (PlanShape.key), or kRefused
 };
+
+constexpr uint32_t kRefused = 2;   // PlanHead.key of a step that was found wrong
 
 // A CTA's first unit.
 struct PlanStart {
@@ -107,6 +109,7 @@ struct PlanShape {
     uint32_t n, groups, tokens, q_heads, G, D, sms;
     uint32_t ctas[2], blocks[2];
     uint64_t rows[2], shared_rows[2];
+    uint32_t key;         // of the sizes that a plan holds for, odd
 };
 
 inline bool plan_shape(const dm_cache *c, uint32_t n, uint32_t groups, uint32_t tokens, uint32_t q_heads, PlanShape &s) {
@@ -130,6 +133,10 @@ inline bool plan_shape(const dm_cache *c, uint32_t n, uint32_t groups, uint32_t 
     if (wide > 0x7FFFFFFFull || (uint64_t)tokens * s.G > 0x7FFFFFFFull) return false;
     s.blocks[0] = (uint32_t)wide;
     s.blocks[1] = n + groups;
+    s.key = 0;
+    for (uint32_t x : {n, groups, tokens, q_heads, c->kv_heads, c->head_dim, c->page_tokens, c->max_seqs, c->max_blocks})
+        s.key = (s.key ^ x) * 0x9E3779B1u, s.key ^= s.key >> 15;
+    s.key |= 1;
     return true;
 }
 
@@ -175,6 +182,7 @@ struct AttendArgs {
     float scale2;                                // scale * log2(e)
     uint32_t ctas[2];                            // launched
     uint32_t o_wide;                             // rows of o begin on 32 bytes
+    uint32_t key;                                // the plan's
     uint32_t beside;                             // the narrow kernel runs beside a wide one
 };
 
@@ -211,7 +219,7 @@ struct Walk {
     __device__ Walk(const AttendArgs &p) {
         const PlanHead *h = p.w.head;
         const uint64_t C = __ldcg(&h->cost[kKind]);
-        const uint32_t S = __ldcg(&h->ok) ? __ldcg(&h->ctas[kKind]) : 0;
+        const uint32_t S = __ldcg(&h->key) == p.key ? __ldcg(&h->ctas[kKind]) : 0;
         at = end = 0;
         b = next_head = next_unit = 0;
         if (blockIdx.x < S) {

@@ -187,7 +187,7 @@ __global__ void __launch_bounds__(kWideT, 1)
     // on all before this kernel being complete
     asm volatile("griddepcontrol.wait;" ::: "memory");
     asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
-    if (__syncthreads_or(has_err(p.status) || !p.w.head->ok || blockIdx.x >= p.w.head->ctas[0])) return;
+    if (__syncthreads_or(has_err(p.status) || p.w.head->key != p.key || blockIdx.x >= p.w.head->ctas[0])) return;
     if (wid == 9) {
         asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], 512;" ::"r"(s_at + W::kWord + 4) : "memory");
         asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;");
@@ -345,7 +345,7 @@ __global__ void __launch_bounds__(kWideT, 1)
             const Row mine = row_at(p, w.k, 128 * x + min(r, rows - 1));
             // rows that are not there (their Q is zero) see everything: a row that
             // is masked costs its warp the masking of every tile
-            const int32_t limit = r < rows ? row_limit(w.k, mine.token) : 1 << 30;
+            const int32_t limit = r < rows ? row_limit(w.k, mine.token) : INT32_MAX;
             Walk<0> ahead = w;
             more = next(ahead);
             float m = -INFINITY, l = 0.f;   // the maximum in the scores' own unit
@@ -424,7 +424,7 @@ __global__ void __launch_bounds__(kWideT, 1)
             const uint64_t tok = (uint64_t)(w.k.token + mine.token);
             const uint32_t h = w.head * p.G + mine.head;
             const uint64_t part = whole ? 0 : w.part_row(p) + 128 * x + r;
-            const float inv = l > 0.f ? 1.f / l : 0.f;
+            const float inv = l == 0.f ? 0.f : 1.f / l;
             char *dst = p.o + tok * p.o_token + h * p.o_head;
 #pragma unroll
             for (uint32_t q = 0; q < D / 32; ++q) {
@@ -456,7 +456,7 @@ __global__ void __launch_bounds__(kWideT, 1)
             if (on) {
                 const float m2 = m * p.scale2;   // minus infinity where the row saw nothing
                 if (!whole) p.w.ml[0][part] = make_float2(m2, l);
-                else if (p.lse) p.lse[tok * p.q_heads + h] = l > 0.f ? (m2 + log2f(l)) * 0.69314718056f : -INFINITY;
+                else if (p.lse) p.lse[tok * p.q_heads + h] = l == 0.f ? -INFINITY : (m2 + log2f(l)) * 0.69314718056f;
             }
             __syncwarp();
             fence_before();   // O has been read; the next product may write it

@@ -254,7 +254,7 @@ __global__ void __launch_bounds__(kCopyT, 4) k_fork_copy(PagesArgs p, CopyArgs c
 __global__ void __launch_bounds__(256) k_free(PagesArgs p, const int32_t *seqs, uint32_t n) {
     __shared__ int32_t s_len;
     pdl_enter();
-    if (has_err(p.status)) return;
+    if (__syncthreads_or(has_err(p.status))) return;   // another CTA may be setting it
     uint32_t bad = 0;   // every CTA looks at every id: one out of range stops them all
     for (uint32_t i = threadIdx.x; i < n; i += 256) bad |= (uint32_t)seqs[i] >= p.max_seqs;
     if (__syncthreads_or(bad)) {

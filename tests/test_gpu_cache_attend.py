@@ -263,3 +263,48 @@ def test_layers_of_one_plan_and_graphs(torch):
         ref, _, mass = R.attend_reference(b, q, 128 ** -0.5, i)
         assert torch.equal(outs[i], want[i])
         assert bool(((outs[i].double() - ref).abs() <= R.attend_bound(ref, mass, torch.bfloat16, 700, 6.0)).all())
+
+
+def test_buffer_without_the_plan(torch):
+    """attend on a work buffer that holds no plan, or another step's, writes nothing and says so."""
+    import cache_reference as R
+    from paper_2602_06502_gb300 import dualmap as D
+    b = R.make_batch(6, page=16, kv_heads=2, dim=64, dtype=torch.bfloat16, own=[30, 200], new=[1, 40])
+    c, T = b["cache"], b["tokens"]
+    q = torch.randn(T, 4, 64, generator=b["gen"], device="cuda").bfloat16()
+    out = torch.full_like(q, 5.0)
+    other = c.plan(b["seqs"], b["offsets"], T + 1, 4)
+    for fill in (0, 255):
+        plan = c.plan(b["seqs"], b["offsets"], T, 4)
+        assert c.last_error() == 0
+        plan.keep[-1].fill_(fill)
+        c.attend(plan, q, out=out)
+        assert c.last_error() == D.DM_ERR_INVALID_ARG and bool((out == 5).all())
+    plan = c.plan(b["seqs"], b["offsets"], T, 4)
+    held = plan.struct.work
+    plan.struct.work = other.struct.work
+    assert plan.struct.work_bytes <= other.struct.work_bytes
+    c.attend(plan, q, out=out)
+    assert c.last_error() == D.DM_ERR_INVALID_ARG and bool((out == 5).all())
+    plan.struct.work = held
+    c.attend(plan, q, out=out)
+    assert c.last_error() == 0 and not bool((out == 5).all())
+
+
+@pytest.mark.parametrize("new", [[1, 2], [1, 60]])   # few rows, many rows
+def test_a_query_that_is_not_finite(torch, new):
+    """NaN in one query stays in its own row, and its logarithm says so too."""
+    import cache_reference as R
+    b = R.make_batch(8, page=16, kv_heads=2, dim=64, dtype=torch.bfloat16, own=[30, 700], new=new)
+    c, T = b["cache"], b["tokens"]
+    q = torch.randn(T, 4, 64, generator=b["gen"], device="cuda").bfloat16()
+    plan = c.plan(b["seqs"], b["offsets"], T, 4)
+    lse, clean = torch.empty(T, 4, device="cuda"), torch.empty(T, 4, device="cuda")
+    ref = c.attend(plan, q, lse=clean)
+    q[T - 1, 3] = float("nan")
+    o = c.attend(plan, q, lse=lse)
+    bad = torch.zeros(T, 4, dtype=torch.bool, device="cuda")
+    bad[T - 1, 3] = True
+    assert torch.equal(torch.isnan(lse), bad) and torch.equal(torch.isnan(o).all(-1), bad)
+    assert torch.equal(lse[~bad], clean[~bad]) and torch.equal(o[~bad], ref[~bad])
+    assert c.last_error() == 0
