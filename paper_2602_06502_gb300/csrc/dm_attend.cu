@@ -317,7 +317,7 @@ __global__ void __cluster_dims__(kPlanCl, 1, 1) __launch_bounds__(kPlanT) k_plan
     if (s_bad || !p.groups) return;
     // what joining needs of the shared groups' own blocks, all CTAs
     const uint32_t own0 = __ldcg(p.w.head->own), owns = own0 + __ldcg(p.w.head->own + 1);
-    for (uint32_t i = rank * T + tid; i < owns; i += kPlanCl * T) {
+    for (uint32_t i = tid * kPlanCl + rank; i < owns; i += kPlanCl * T) {
         const int kd = i >= own0;
         const uint32_t j = kd ? i - own0 : i, b = __ldcg((kd ? p.w.own[1] : p.w.own[0]) + j);
         JoinOwn x;

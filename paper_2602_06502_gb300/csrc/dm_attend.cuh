@@ -28,7 +28,9 @@ constexpr uint32_t kWideRows = 256, kWideKeys = 128, kNarrowRows = 16, kNarrowKe
 constexpr uint32_t kShareRows = 128;   // a sequence with as many rows fills a tile by itself
 constexpr uint32_t kNarrowPerSm = 2;
 
-struct AttendBlock {
+// The plan's records are read and written 16 bytes at a time (a thread each: a
+// word at a time is a line per lane and word).
+struct alignas(16) AttendBlock {
     int32_t row;          // of tables
     int32_t token;        // query token of its first row
     uint32_t lead, rows;  // that row's head within G; its rows
@@ -57,7 +59,7 @@ struct PlanHead {
 constexpr uint32_t kRefused = 2;   // PlanHead.key of a step that was found wrong
 
 // A CTA's first unit.
-struct PlanStart {
+struct alignas(16) PlanStart {
     uint64_t at;          // along the line
     uint32_t block, head, unit, pad;
 };
@@ -82,7 +84,7 @@ struct alignas(16) JoinOwn {
 };
 
 // A sequence or a group of the step.
-struct PlanEntity {
+struct alignas(16) PlanEntity {
     int32_t row, token, group, kv0, pos;
     uint32_t rows, shared;
     uint32_t first;       // its first block of its kind
@@ -197,12 +199,11 @@ __device__ __forceinline__ uint32_t cta_of(uint64_t at, uint64_t C, uint64_t inv
 // A block through L2: it may have been written by another CTA of this kernel, or
 // before a kernel that this one runs beside.
 __device__ __forceinline__ AttendBlock load_block(const AttendBlock *blocks, uint32_t b) {
-    static_assert(sizeof(AttendBlock) % 4 == 0);
     AttendBlock k;
-    const uint32_t *src = reinterpret_cast<const uint32_t *>(blocks + b);
-    uint32_t *dst = reinterpret_cast<uint32_t *>(&k);
+    const uint4 *src = reinterpret_cast<const uint4 *>(blocks + b);
+    uint4 *dst = reinterpret_cast<uint4 *>(&k);
 #pragma unroll
-    for (uint32_t i = 0; i < sizeof(AttendBlock) / 4; ++i) dst[i] = __ldcg(src + i);
+    for (uint32_t i = 0; i < sizeof(AttendBlock) / 16; ++i) dst[i] = __ldcg(src + i);
     return k;
 }
 
