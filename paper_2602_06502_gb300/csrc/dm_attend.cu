@@ -610,17 +610,19 @@ __global__ void __launch_bounds__(kNarrowT, kNarrowPerSm)
 
 // -- joining parts --------------------------------------------------------------------
 
-// A warp takes a row of a shared group's sequence (its parts of the prefix,
-// then those of its own keys) or of another tile that CTAs share, parts in the
-// order of the CTAs that left them.  32 parts' maxima and sums are looked at
-// together, so that the parts themselves are independent loads.  Bound:
-// latency, then L2 (4 D + 8 bytes a row and part).
-// kAhead parts are loaded at once: four with four CTAs an SM where there are
-// many rows, 16 with one where the GPU has a warp for each row anyway
-// (attend_few's 27 parts a row: 5.5 us with four).
-template <class T, int D, uint32_t kAhead, uint32_t kCtas>
+// A warp takes kRows rows of a tile: of a shared group's sequence (their parts of
+// the prefix, then those of its own keys) or of another tile that CTAs share,
+// parts in the order of the CTAs that left them.  32 parts' maxima and sums are
+// looked at together, so that the parts themselves are independent loads,
+// kAhead of each row at once.  Bound: latency, then L2 (4 D + 8 bytes a row and
+// part).  Finding a tile's parts takes a warp longer than adding a few up, so
+// four rows go together once the GPU's warps all have four; with fewer rows
+// more warps are worth more.  Where the GPU has a warp for each row anyway, one
+// CTA an SM has 16 parts in flight (27 parts a row: 5.5 us with four).
+template <class T, int D, uint32_t kRows, uint32_t kAhead, uint32_t kCtas>
 __global__ void __launch_bounds__(256, kCtas) k_attend_join(AttendArgs p) {
     constexpr int V = D / 32;
+    static_assert(kNarrowRows % kRows == 0 && kWideRows % kRows == 0);
     pdl_enter();
     const PlanHead h = *p.w.head;
     const uint32_t lane = threadIdx.x & 31;
@@ -629,10 +631,15 @@ __global__ void __launch_bounds__(256, kCtas) k_attend_join(AttendArgs p) {
         if (h.key != kRefused && blockIdx.x == 0 && threadIdx.x == 0) set_err(p.status, DM_ERR_INVALID_ARG);
         return;
     }
-    const uint64_t own1 = (uint64_t)h.own[1] * p.kv_heads * h.own_rows[1], own0 = own1 + (uint64_t)h.own[0] * p.kv_heads * h.own_rows[0];
-    const uint64_t cut0 = own0 + (uint64_t)h.cuts[0] * kWideRows, jobs = cut0 + (uint64_t)h.cuts[1] * kNarrowRows;
+    // A sequence's rows are taken in fours of its group's, none of which is in
+    // two blocks of the prefix; where its first is not the first of a four, it
+    // may need one more.
+    const uint32_t more = p.G % kRows ? kRows - 1 : 0;
+    const uint32_t fours[2] = {(h.own_rows[0] + more + kRows - 1) / kRows, (h.own_rows[1] + more + kRows - 1) / kRows};
+    const uint64_t own1 = (uint64_t)h.own[1] * p.kv_heads * fours[1], own0 = own1 + (uint64_t)h.own[0] * p.kv_heads * fours[0];
+    const uint64_t cut0 = own0 + (uint64_t)h.cuts[0] * (kWideRows / kRows), jobs = cut0 + (uint64_t)h.cuts[1] * (kNarrowRows / kRows);
     for (uint64_t t = blockIdx.x * 8ull + threadIdx.x / 32; t < jobs; t += gridDim.x * 8ull) {
-        // a tile's parts: how many, and where a row of it is in the i-th
+        // a tile's parts: how many, and where its row 0 is in the i-th
         struct Parts {
             const float *part;
             const float2 *ml;
@@ -640,7 +647,7 @@ __global__ void __launch_bounds__(256, kCtas) k_attend_join(AttendArgs p) {
             uint64_t at;
             __device__ uint64_t row(uint32_t i) const { return at + (uint64_t)i * step + (i == 0 ? odd : 0); }
         };
-        auto parts = [&](int kd, const JoinSide &x, uint32_t head, uint32_t row, bool shared) {
+        auto parts = [&](int kd, const JoinSide &x, uint32_t head, bool shared) {
             const uint64_t C = kd ? h.cost[1] : h.cost[0], begin = x.cum + head * ((uint64_t)x.units * x.cost + x.over);
             const uint64_t last = begin + (x.units > 1 ? x.over + (x.units - 1ull) * x.cost : 0);   // its last unit
             const uint32_t cap = kd ? kNarrowRows : kWideRows, S = kd ? h.ctas[1] : h.ctas[0];
@@ -648,101 +655,138 @@ __global__ void __launch_bounds__(256, kCtas) k_attend_join(AttendArgs p) {
             const uint32_t c0 = cta_of(begin, C, inv, S), c1 = cta_of(last, C, inv, S);
             Parts q{kd ? p.w.part[1] : p.w.part[0], kd ? p.w.ml[1] : p.w.ml[0], c1 - c0 + 1, cap, 0, 0};
             if (shared) {
-                q.at = x.part0 + (uint64_t)head * x.rows + (uint64_t)cap * c0 + row;
+                q.at = x.part0 + (uint64_t)head * x.rows + (uint64_t)cap * c0;
             } else {
-                q.at = (kd ? p.w.shared_rows[1] : p.w.shared_rows[0]) + (uint64_t)cap * 2 * c0 + row;
+                q.at = (kd ? p.w.shared_rows[1] : p.w.shared_rows[0]) + (uint64_t)cap * 2 * c0;
                 q.step = 2 * cap;
                 q.odd = cap;
             }
             return q;
         };
-        uint32_t head, r, lead;
-        int32_t token;
+        uint32_t head, lead;
+        int32_t token, r0, rows;   // the first row, of `rows`
         Parts pre{}, own;
         if (t < own0) {
             const int kind = t < own1;
             const uint64_t x = kind ? t : t - own1;
-            const uint32_t cap = kind ? h.own_rows[1] : h.own_rows[0], tile = (uint32_t)(x / cap);
-            r = (uint32_t)(x % cap);
+            const uint32_t per = kind ? fours[1] : fours[0], tile = (uint32_t)(x / per);
             head = tile % p.kv_heads;
             const JoinOwn &k = (kind ? p.w.join[1] : p.w.join[0])[tile / p.kv_heads];
-            if (r >= k.own.rows) continue;
+            rows = (int32_t)k.own.rows;
+            r0 = (int32_t)((uint32_t)(x % per) * kRows) - (int32_t)(k.pre.row % kRows);
+            if (r0 >= rows) continue;
             token = k.token;
             lead = k.lead;
-            own = parts(kind, k.own, head, r, true);
+            own = parts(kind, k.own, head, true);
             JoinSide side = k.pre;
-            const uint32_t pre_cap = k.pre_kind ? kNarrowRows : kWideRows;
-            uint32_t row = side.row + r;
-            if (row >= pre_cap) {   // in the prefix's next block
-                row -= pre_cap;
+            int32_t at = (int32_t)side.row;   // of row 0 among the rows of the prefix's block
+            const int32_t pre_cap = k.pre_kind ? kNarrowRows : kWideRows;
+            if (at + max(r0, 0) >= pre_cap) {   // in the prefix's next block
+                at -= pre_cap;
                 const AttendBlock y = (k.pre_kind ? p.w.block[1] : p.w.block[0])[k.pre_block + 1];
                 side = {(k.pre_kind ? p.w.cum[1] : p.w.cum[0])[k.pre_block + 1], y.units, y.cost, y.over, y.rows, y.part0, 0};
             }
-            pre = parts((int)k.pre_kind, side, head, row, true);
+            pre = parts((int)k.pre_kind, side, head, true);
+            pre.at += at;   // row 0 may lie before the block; the rows taken do not
         } else {
             const int kind = t >= cut0;
             const uint64_t x = kind ? t - cut0 : t - own0;
-            const uint32_t cap = kind ? kNarrowRows : kWideRows;
-            r = (uint32_t)(x % cap);
-            const PlanStart &from = (kind ? p.w.start[1] : p.w.start[0])[(kind ? p.w.cut[1] : p.w.cut[0])[x / cap]];
+            const uint32_t per = kind ? kNarrowRows / kRows : kWideRows / kRows;
+            const PlanStart &from = (kind ? p.w.start[1] : p.w.start[0])[(kind ? p.w.cut[1] : p.w.cut[0])[x / per]];
             const AttendBlock y = (kind ? p.w.block[1] : p.w.block[0])[from.block];
-            if (r >= y.rows) continue;
+            rows = (int32_t)y.rows;
+            r0 = (int32_t)((uint32_t)(x % per) * kRows);
+            if (r0 >= rows) continue;
             head = from.head;
             token = y.token;
             lead = y.lead;
-            own = parts(kind, {(kind ? p.w.cum[1] : p.w.cum[0])[from.block], y.units, y.cost, y.over, y.rows, y.part0, 0}, head, r, false);
+            own = parts(kind, {(kind ? p.w.cum[1] : p.w.cum[0])[from.block], y.units, y.cost, y.over, y.rows, y.part0, 0}, head, false);
         }
         const uint32_t N = pre.n + own.n;
-        {
-            float acc[V], M = -INFINITY, L = 0.f;
+        const int32_t lo = max(r0, 0), hi = min(r0 + (int32_t)kRows, rows);
+        float acc[kRows][V], M[kRows], L[kRows];
+        uint32_t r[kRows];   // rows outside lo .. hi are read as the nearest inside
 #pragma unroll
-            for (int v = 0; v < V; ++v) acc[v] = 0.f;
-            float y[kAhead][V];
-            auto load = [&](uint32_t i0) {
+        for (uint32_t q = 0; q < kRows; ++q) {
+            r[q] = (uint32_t)min(max(r0 + (int32_t)q, lo), hi - 1);
+            M[q] = -INFINITY;
+            L[q] = 0.f;
+#pragma unroll
+            for (int v = 0; v < V; ++v) acc[q][v] = 0.f;
+        }
+        for (uint32_t i0 = 0; i0 < N; i0 += 32) {
+            const uint32_t i = i0 + lane, n = min(N - i0, 32u);
+            const float *mine = nullptr;   // row 0 of part i
+            float2 ml[kRows];
+#pragma unroll
+            for (uint32_t q = 0; q < kRows; ++q) ml[q] = make_float2(-INFINITY, 0.f);
+            if (i < N) {
+                const bool first = i < pre.n;
+                const uint64_t row = first ? pre.row(i) : own.row(i - pre.n);
+                const float2 *src = (first ? pre.ml : own.ml) + row;
+                mine = (first ? pre.part : own.part) + row * D;
+#pragma unroll
+                for (uint32_t q = 0; q < kRows; ++q) ml[q] = src[r[q]];
+            }
+            __syncwarp();
+            float y[kAhead][kRows][V];
+            auto load = [&](uint32_t j0) {
 #pragma unroll
                 for (uint32_t j = 0; j < kAhead; ++j) {
-                    const uint32_t i = i0 + j;
-                    if (i >= N) break;
-                    const float *src = (i < pre.n ? pre.part + pre.row(i) * D : own.part + own.row(i - pre.n) * D) + lane * V;
-                    if constexpr (V == 4) *reinterpret_cast<float4 *>(y[j]) = *reinterpret_cast<const float4 *>(src);
-                    else *reinterpret_cast<float2 *>(y[j]) = *reinterpret_cast<const float2 *>(src);
+                    if (j0 + j >= n) break;
+                    const float *src = reinterpret_cast<const float *>(__shfl_sync(~0u, reinterpret_cast<uint64_t>(mine), j0 + j)) + lane * V;
+#pragma unroll
+                    for (uint32_t q = 0; q < kRows; ++q) {
+                        if constexpr (V == 4) *reinterpret_cast<float4 *>(y[j][q]) = *reinterpret_cast<const float4 *>(src + r[q] * D);
+                        else *reinterpret_cast<float2 *>(y[j][q]) = *reinterpret_cast<const float2 *>(src + r[q] * D);
+                    }
                 }
             };
-            for (uint32_t i0 = 0; i0 < N; i0 += 32) {
-                const uint32_t i = i0 + lane;
-                const float2 ml = i >= N ? make_float2(-INFINITY, 0.f) : i < pre.n ? pre.ml[pre.row(i)] : own.ml[own.row(i - pre.n)];
-                load(i0);
-                float now = ml.x;
+            load(0);
+            float fi[kRows];
+#pragma unroll
+            for (uint32_t q = 0; q < kRows; ++q) {
+                float now = ml[q].x;
 #pragma unroll
                 for (int d = 16; d; d /= 2) now = fmaxf(now, __shfl_xor_sync(~0u, now, d));
-                now = fmaxf(now, M);
-                const float base = now == -INFINITY ? 0.f : now, f = exp2_(M - base), fi = exp2_(ml.x - base);
-                float l = ml.y * fi;
+                now = fmaxf(now, M[q]);
+                const float base = now == -INFINITY ? 0.f : now, f = exp2_(M[q] - base);
+                fi[q] = exp2_(ml[q].x - base);
+                float l = ml[q].y * fi[q];
 #pragma unroll
                 for (int d = 16; d; d /= 2) l += __shfl_xor_sync(~0u, l, d);
-                L = L * f + l;
-                M = now;
+                L[q] = L[q] * f + l;
+                M[q] = now;
 #pragma unroll
-                for (int v = 0; v < V; ++v) acc[v] *= f;
-                for (uint32_t j0 = 0; j0 < 32 && i0 + j0 < N; j0 += kAhead) {
-                    if (j0) load(i0 + j0);
+                for (int v = 0; v < V; ++v) acc[q][v] *= f;
+            }
+            for (uint32_t j0 = 0; j0 < n; j0 += kAhead) {
+                if (j0) load(j0);
 #pragma unroll
-                    for (uint32_t j = 0; j < kAhead; ++j) {
-                        const float fj = __shfl_sync(~0u, fi, j0 + j);
-                        if (i0 + j0 + j >= N) break;
+                for (uint32_t j = 0; j < kAhead; ++j) {
+                    if (j0 + j >= n) break;
 #pragma unroll
-                        for (int v = 0; v < V; ++v) acc[v] += y[j][v] * fj;
+                    for (uint32_t q = 0; q < kRows; ++q) {
+                        const float fj = __shfl_sync(~0u, fi[q], j0 + j);
+#pragma unroll
+                        for (int v = 0; v < V; ++v) acc[q][v] += y[j][q][v] * fj;
                     }
                 }
             }
-            const Row at = row_at(p, lead, r);
+        }
+#pragma unroll
+        for (uint32_t q = 0; q < kRows; ++q) {
+            if (r0 + (int32_t)q < lo || r0 + (int32_t)q >= hi) continue;
+            const Row at = row_at(p, lead, r[q]);
             const uint64_t tok = (uint64_t)(token + at.token);
             const uint32_t qh = head * p.G + at.head;
-            const float inv = L == 0.f ? 0.f : 1.f / L;
+            const float inv = L[q] == 0.f ? 0.f : 1.f / L[q];
             char *dst = p.o + tok * p.o_token + qh * p.o_head + lane * V * 2;
-            if constexpr (V == 4) *reinterpret_cast<uint2 *>(dst) = make_uint2(Pack2<T>::pack(acc[0] * inv, acc[1] * inv), Pack2<T>::pack(acc[2] * inv, acc[3] * inv));
-            else *reinterpret_cast<uint32_t *>(dst) = Pack2<T>::pack(acc[0] * inv, acc[1] * inv);
-            if (p.lse && lane == 0) p.lse[tok * p.q_heads + qh] = L == 0.f ? -INFINITY : (M + log2f(L)) * 0.69314718056f;
+            if constexpr (V == 4)
+                *reinterpret_cast<uint2 *>(dst) =
+                    make_uint2(Pack2<T>::pack(acc[q][0] * inv, acc[q][1] * inv), Pack2<T>::pack(acc[q][2] * inv, acc[q][3] * inv));
+            else *reinterpret_cast<uint32_t *>(dst) = Pack2<T>::pack(acc[q][0] * inv, acc[q][1] * inv);
+            if (p.lse && lane == 0) p.lse[tok * p.q_heads + qh] = L[q] == 0.f ? -INFINITY : (M[q] + log2f(L[q])) * 0.69314718056f;
         }
     }
 }
@@ -779,13 +823,18 @@ bool page_map(CUtensorMap *m, const dm_cache *c, void *pool, uint32_t layer, uin
 }
 
 template <class T, int D>
-cudaError_t launch_rest(const AttendArgs &p, uint64_t rows, const CUtensorMap &mk, const CUtensorMap &mv, cudaStream_t st) {
+cudaError_t launch_rest(const AttendArgs &p, uint64_t q_rows, uint64_t rows, const CUtensorMap &mk, const CUtensorMap &mv, cudaStream_t st) {
     static SmemOptIn opt;
     DM_TRY(opt_in_smem(opt, Narrow<D>::kBytes, k_attend_narrow<T, D>));
     DM_TRY(launch_pdl(k_attend_narrow<T, D>, p.ctas[1], kNarrowT, Narrow<D>::kBytes, st, mk, mv, p));
-    // a warp per row, or as many as the GPU holds
-    const uint64_t warps = std::min<uint64_t>(rows, (uint64_t)p.ctas[0] * 64);
-    const auto join = rows <= p.ctas[0] * 8ull ? k_attend_join<T, D, 16, 1> : k_attend_join<T, D, 4, 4>;
+    // Four rows a warp from 64 rows an SM on, about four for each warp that the
+    // GPU then holds.  Attention of 256 tokens with 64 heads: 182 us one row at a
+    // time, 178 by fours; 8,000 tokens of prompts with 32 heads: 584 and 573; two
+    // layers of 128 tokens with 32 heads (27 rows an SM): 200 and 206.
+    const bool four = q_rows >= p.ctas[0] * 64ull;
+    const auto join = four ? k_attend_join<T, D, 4, 2, 2> : rows <= p.ctas[0] * 8ull ? k_attend_join<T, D, 1, 16, 1> : k_attend_join<T, D, 1, 4, 4>;
+    // a warp per row or four, or twice as many as the GPU holds
+    const uint64_t warps = std::min<uint64_t>(rows, p.ctas[0] * (four ? 32ull : 64ull));
     return launch_pdl(join, (uint32_t)((warps + 7) / 8), 256, 0, st, p);
 }
 
@@ -845,11 +894,11 @@ extern "C" dm_status dm_cache_attend(const dm_cache *c, const dm_plan *pl, const
     cudaError_t e = p.beside ? launch_attend_wide(c, p, mk, mv, st) : cudaSuccess;
     if (e == cudaSuccess) {
         // narrow tiles count 16 rows in the joining
-        const uint64_t rows = (uint64_t)pl->tokens * s.q_heads + (uint64_t)pl->n * c->kv_heads * kNarrowRows;
+        const uint64_t q_rows = (uint64_t)pl->tokens * s.q_heads, rows = q_rows + (uint64_t)pl->n * c->kv_heads * kNarrowRows;
         if (c->dtype == DM_BF16)
-            e = c->head_dim == 64 ? launch_rest<__nv_bfloat16, 64>(p, rows, mk, mv, st) : launch_rest<__nv_bfloat16, 128>(p, rows, mk, mv, st);
+            e = c->head_dim == 64 ? launch_rest<__nv_bfloat16, 64>(p, q_rows, rows, mk, mv, st) : launch_rest<__nv_bfloat16, 128>(p, q_rows, rows, mk, mv, st);
         else
-            e = c->head_dim == 64 ? launch_rest<__half, 64>(p, rows, mk, mv, st) : launch_rest<__half, 128>(p, rows, mk, mv, st);
+            e = c->head_dim == 64 ? launch_rest<__half, 64>(p, q_rows, rows, mk, mv, st) : launch_rest<__half, 128>(p, q_rows, rows, mk, mv, st);
     }
     return status_of(e);
 }

@@ -227,6 +227,16 @@ def test_many_sequences(torch, groups):
         prefix=[4 * rng.randint(1, 12) for _ in sizes or []], own=own, new=new)
 
 
+@pytest.mark.parametrize("kv_heads, hq, dim", [(12, 36, 64), (8, 40, 128), (36, 36, 64), (9, 36, 128)])
+def test_many_rows_joined(torch, kv_heads, hq, dim):
+    """So many rows of shared groups, and of prompts that CTAs share, that several are joined at a time; groups'
+    rows that begin anywhere among them, and behind the first 256."""
+    new = [1 + i % 3 for i in range(300)] + [0, 250, 61]
+    run(torch, 64 + dim + hq, hq=hq, page=16, layout="heads", dtype=torch.bfloat16 if dim == 64 else torch.float16, dim=dim,
+        kv_heads=kv_heads, groups=[150, 3, 40, 2], prefix=(320, 96, 1024, 160), own=[i % 41 for i in range(300)] + [5, 700, 3000],
+        new=new)
+
+
 def test_long_prompt_of_many_blocks(torch):
     """A prompt of more row blocks than threads lay out at once."""
     run(torch, 60, hq=64, page=64, layout="tokens", dtype=torch.float16, dim=64, kv_heads=1, own=[0, 3], new=[4500, 1])
