@@ -4,5 +4,6 @@ probes, SLO-aware choice, LRU commit, hotspot rebalancing, ring add/remove.
 
 The compute lives in libdualmap.so (hand-written CUDA behind the C ABI in
 include/dualmap.h); `dualmap` is its ctypes binding and `scheduler` a thin
-wrapper holding torch device buffers.
+wrapper holding torch device buffers.  `cache` is an instance's prefix cache
+(pages, appended keys, attention), `instance` a small decoder on it.
 """

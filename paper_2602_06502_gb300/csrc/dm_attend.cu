@@ -53,7 +53,9 @@ __device__ uint64_t block_scan(uint64_t x, uint64_t *s_warp, uint64_t &total) {
     return in - x + (wid ? s_warp[wid - 1] : 0);
 }
 
-// Measured on attend_templates' and attend_drafts' shapes.
+// Measured with 256 single tokens of 64 heads behind 12 prefixes (D = 128), and
+// with drafts of up to 8 tokens and 12 heads for 96 sequences (D = 64): the
+// times of CTAs with units of one sort, in cycles / 100.
 constexpr PlanCosts kCosts128 = {23, 20, 75, 24, 8}, kCosts64 = {20, 17, 38, 15, 6};
 constexpr uint32_t kFewGroups = 512, kFewBlocks = 2048;   // kept in shared memory
 
@@ -73,7 +75,8 @@ __device__ __forceinline__ int32_t group_at(const int32_t *offsets, const int32_
 // CTA 0 lays the wide blocks out and CTA 1 the narrow ones (both work out the
 // entities, writing the same); the others see that a group's sequences begin
 // with the same pages.  Bound: latency, a chain of small steps, so what is
-// searched is kept in shared memory.
+// searched is kept in shared memory.  8 us for four sequences, 13 to 16 for 96
+// to 256 in five to twelve groups.
 __global__ void __cluster_dims__(kPlanCl, 1, 1) __launch_bounds__(kPlanT) k_plan(PlanArgs p) {
     __shared__ uint64_t s_warp[32], s_cum[kFewBlocks];
     __shared__ int32_t s_offsets[kFewGroups + 1], s_prefix[kFewGroups];
@@ -344,7 +347,9 @@ __global__ void __cluster_dims__(kPlanCl, 1, 1) __launch_bounds__(kPlanT) k_plan
 // flight.  Two warps keep a ring of 32-key slots (keys and values, 8 KB or 16 KB)
 // full through TMA, two CTAs per SM; each of four warps takes the 16
 // keys of its half of every other slot, with its own running maximum and sum,
-// and the four join once per tile.
+// and the four join once per tile.  16 sequences of up to 100,000 keys of their
+// own, two key heads, D = 128: 169 us at 6.1 TB/s from HBM, beside 154 us of the
+// wide kernel's SMs.
 
 constexpr uint32_t kSlotKeys = 32, kNarrowT = 192;
 

@@ -9,8 +9,10 @@
 // page its rank.  A call that cannot be met is found between the two walks,
 // before anything is written.
 //
-// Bound: latency of one launch where few pages change hands; the copies'
-// bandwidth where pages move (k_fork_copy, k_compact_copy).
+// Bound: latency of one launch where few pages change hands (k_grow 7 to 11 us,
+// k_compact_plan 8, k_free 3 to 5); the copies' bandwidth where pages move
+// (k_compact_copy below; k_fork_copy 45 us for 512 sequences' last pages in
+// eight layers, runs of 0.25 to 4 KB a head).
 #include <algorithm>
 #include <cooperative_groups.h>
 
@@ -396,8 +398,9 @@ CopyArgs copy_args(const dm_cache *c) {
             c->kv_heads, c->head_dim * 2, c->layout == DM_PAGES_TOKENS};
 }
 
-// Many more CTAs than fit at once: late ones even the ends out (compact_many
-// 333 us with 8 an SM, 313 with 32).
+// Many more CTAs than fit at once: late ones even the ends out (4,915 of
+// 8,192 pages in use, eight layers of 64 KB a page compacted: 333 us with 8 an
+// SM, 313 with 32, 6.6 TB/s).
 uint32_t copy_grid(uint64_t jobs) { return (uint32_t)std::min<uint64_t>(jobs, (uint64_t)sm_count() * 32); }
 
 }  // namespace
