@@ -715,7 +715,9 @@ DM_API uint64_t dm_plan_bytes(const dm_cache *c, uint32_t n, uint32_t groups, ui
  * The plan holds until lengths or tables change.  Recorded:
  * DM_ERR_INVALID_ARG (an id, offset or group out of range, a prefix that is
  * no multiple of B, that reaches into the new tokens of a sequence, or whose
- * pages differ), and the plan is then empty.  Asynchronous. */
+ * pages differ), and the plan is then empty: attention on it writes nothing
+ * and, this error having been read, records nothing more.  A call made while
+ * an earlier error stands leaves no plan.  Asynchronous. */
 DM_API dm_status dm_cache_plan(const dm_cache *c, const dm_plan *p, void *stream);
 
 /* One layer's attention of a planned step (dm_cache_attend).  Strides and
@@ -740,8 +742,8 @@ typedef struct {
  * buffer, so layers of one plan run one after another.  A key or value in a
  * sequence's own slots that is not finite can reach the step's other rows of
  * that sequence, those before it too (a weight of zero does not silence it).
- * Recorded: DM_ERR_INVALID_ARG (the buffer holds no plan of this shape),
- * DM_ERR_TIMEOUT (a wait in the kernel gave up).  Asynchronous. */
+ * Recorded: DM_ERR_INVALID_ARG (the buffer holds no plan of this shape, as
+ * after a dm_cache_plan that did nothing), DM_ERR_TIMEOUT (a wait in the kernel gave up).  Asynchronous. */
 DM_API dm_status dm_cache_attend(const dm_cache *c, const dm_plan *p, const dm_attend_args *a, void *stream);
 
 /* Testing only (no paper counterpart): after this call the library's

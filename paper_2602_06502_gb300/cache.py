@@ -21,8 +21,9 @@ LAYOUTS = {"heads": D.DM_PAGES_HEADS, "tokens": D.DM_PAGES_TOKENS}
 class Plan:
     """One step's division over the GPU (PagedCache.plan), for all its layers."""
 
-    def __init__(self, struct, keep, tokens, q_heads):
+    def __init__(self, struct, keep, tokens, q_heads, errors):
         self.struct, self.ref, self.keep, self.tokens, self.q_heads = struct, C.byref(struct), keep, tokens, q_heads
+        self.errors = errors   # that the cache had reported by then
 
 
 class PagedCache:
@@ -61,7 +62,7 @@ class PagedCache:
             raise D.DualMapError(D.DM_ERR_INVALID_ARG, "dm_cache_work_bytes")
         self.work = torch.empty(size, dtype=torch.uint8, device=self.device)
         self.struct.work, self.struct.work_bytes = self.work.data_ptr(), size
-        self._lib, self._ref, self._plan_bytes = D.lib(), C.byref(self.struct), {}
+        self._lib, self._ref, self._plan_bytes, self._errors = D.lib(), C.byref(self.struct), {}, 0
 
     @classmethod
     def empty(cls, *, pages, kv_heads, head_dim, max_seqs, max_tokens, page_tokens=16, layers=1, dtype=torch.bfloat16,
@@ -112,7 +113,9 @@ class PagedCache:
     def last_error(self):
         """The status of the first call that was refused on the device, which it clears (synchronises)."""
         with torch.cuda.device(self.device):
-            return D.dm_cache_last_error(self.struct, torch._C._cuda_getCurrentRawStream(self.device.index))
+            e = D.dm_cache_last_error(self.struct, torch._C._cuda_getCurrentRawStream(self.device.index))
+        self._errors += e != 0
+        return e
 
     def extend(self, seqs, add):
         """Sequence seqs[i] grows by add[i] tokens; the pages it lacks are taken."""
@@ -197,14 +200,17 @@ class PagedCache:
         s = D.dm_plan(self._ints("seqs", seqs), self._ints("offsets", offsets, n + 1), n, tokens, q_heads, groups, go, gp,
                       work.data_ptr(), size)
         self._call("dm_cache_plan", C.byref(s))
-        return Plan(s, (seqs, offsets, group_offsets, group_prefix, work), tokens, q_heads)
+        return Plan(s, (seqs, offsets, group_offsets, group_prefix, work), tokens, q_heads, self._errors)
 
     def attend(self, plan, q, *, layer=0, scale=None, out=None, lse=None):
         """One layer's attention of the planned step: q [tokens, q_heads,
         head_dim], scale (default head_dim ** -0.5).  lse: float32 [tokens,
-        q_heads] for the logarithms of the sums."""
+        q_heads] for the logarithms of the sums.  A plan that was refused writes
+        nothing: a new output then is NaN once that error has been read."""
         if out is None:
             out = torch.empty(q.shape, dtype=self.dtype, device=self.device)
+            if plan.errors != self._errors:   # the error may have been the plan's
+                out.fill_(float("nan"))
         qp, qt, qh = self._rows("q", q, plan.tokens, plan.q_heads)
         op, ot, oh = self._rows("out", out, plan.tokens, plan.q_heads)
         if lse is not None and (lse.dtype is not torch.float32 or lse.shape != (plan.tokens, plan.q_heads) or

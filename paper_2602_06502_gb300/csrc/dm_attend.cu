@@ -91,7 +91,8 @@ __global__ void __cluster_dims__(kPlanCl, 1, 1) __launch_bounds__(kPlanT) k_plan
     __shared__ uint64_t s_sum[4];   // cost and units of each kind
     __shared__ uint32_t s_any;      // rank 0: some CTA found the step wrong
     if (tid < 4) s_sum[tid] = 0;
-    if (tid == 0) s_bad = s_any = has_err(p.status);
+    const bool stood = tid == 0 && has_err(p.status);   // an earlier call's error
+    if (tid == 0) s_bad = s_any = stood;
     if (few)
         for (uint32_t g = tid; p.groups && g <= p.groups; g += T) {
             s_offsets[g] = p.group_offsets[g];
@@ -314,7 +315,9 @@ __global__ void __cluster_dims__(kPlanCl, 1, 1) __launch_bounds__(kPlanT) k_plan
     cl.sync();
     const bool failed = rank == 0 ? s_any != 0 : s_bad != 0;
     if (rank == 0 && tid == 0) {
-        p.w.head->key = failed ? kRefused : p.key;
+        // a step that was not looked at leaves no plan: once that error has been
+        // read, attention on the buffer says so
+        p.w.head->key = !failed ? p.key : stood ? 0 : kRefused;
         if (failed) set_err(p.status, DM_ERR_INVALID_ARG);
     }
     if (s_bad || !p.groups) return;

@@ -53,7 +53,7 @@ struct PlanHead {
     uint32_t own[2];      // blocks of shared groups' sequences
     uint32_t own_rows[2]; // the most rows of one
     uint32_t cuts[2];     // other tiles that more than one CTA has part of
-    uint32_t key, pad;    // the step's shape (PlanShape.key), or kRefused
+    uint32_t key, pad;    // the step's shape (PlanShape.key), kRefused, or 0: no plan
 };
 
 constexpr uint32_t kRefused = 2;   // PlanHead.key of a step that was found wrong
