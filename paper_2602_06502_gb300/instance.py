@@ -48,6 +48,7 @@ class Instance:
         self.tokens = {}        # sequence -> its tokens, oldest first
         self.origin = {}        # sequence -> (sequence it forked from, tokens it kept)
         self.blocks = {}        # (block before, the block's tokens) -> sequence that holds it
+        self.max_tokens, self.max_seqs = max_tokens, max_seqs
         self.free_seqs = list(range(max_seqs - 1, -1, -1))
         self.reused = self.computed = 0
 
@@ -70,20 +71,33 @@ class Instance:
             seq, n = self.blocks[key], n + B
         return seq, n
 
-    def _make_room(self, pages):
-        """Drops the oldest sequences until `pages` pages are free, and packs the rest."""
-        while self.tokens and int((self.cache.refs == 0).sum()) < pages:
+    def _short(self, pages, seqs):
+        return len(self.free_seqs) < seqs or int((self.cache.refs == 0).sum()) < pages
+
+    def _make_room(self, pages, seqs):
+        """Drops the oldest sequences until `pages` pages and `seqs` sequence ids are free, and packs the rest."""
+        dropped = False
+        while self.tokens and self._short(pages, seqs):
             self.drop([next(iter(self.tokens))])
-            if not self.tokens or int((self.cache.refs == 0).sum()) >= pages:
-                self.cache.compact()
+            dropped = True
+        if dropped:
+            self.cache.compact()
+        if self._short(pages, seqs):
+            raise ValueError(f"no room for {seqs} sequences in {pages} pages")
 
     def admit(self, prompts, hits=None, room=0):
         """Starts a sequence per prompt (uint32 arrays) and runs the tokens that
         no held prefix covers; hits: the router's cached-prefix tokens, which
         bound what is reused; room: tokens that each will be decoded.  Returns (sequences, logits of their last tokens),
-        in the order in which the sequences run: those of one prefix together."""
+        in the order in which the sequences run: those of one prefix together.
+        A batch that the cache could not hold even by itself is refused, and nothing changes."""
         B = self.cache.page_tokens
-        self._make_room(sum(-(-(len(t) + room) // B) for t in prompts))
+        if not prompts or not all(1 <= len(t) <= self.max_tokens - room for t in prompts):
+            raise ValueError(f"prompts have 1 to {self.max_tokens - room} tokens")
+        pages = sum(-(-(len(t) + room) // B) for t in prompts)
+        if len(prompts) > self.max_seqs or pages > self.cache.refs.shape[0]:
+            raise ValueError(f"a batch of {len(prompts)} sequences in {pages} pages: more than the cache has")
+        self._make_room(pages, len(prompts))
         found = [self._held(t, min(len(t) - 1, len(t) if hits is None else int(h)))
                  for t, h in zip(prompts, hits if hits is not None else [0] * len(prompts))]
         order = sorted(range(len(prompts)), key=lambda i: found[i])
