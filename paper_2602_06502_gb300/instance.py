@@ -46,11 +46,12 @@ class Instance:
             10_000.0 ** (-torch.arange(0, head_dim, 2, device=device, dtype=torch.float64) / head_dim)
         self.cos, self.sin = angle.cos().float(), angle.sin().float()
         self.tokens = {}        # sequence -> its tokens, oldest first
-        self.origin = {}        # sequence -> (sequence it forked from, tokens it kept)
+        self.serial = {}        # sequence -> its number among all that were ever admitted (ids are given out again)
+        self.origin = {}        # sequence -> (serial of the sequence it forked from or -1, tokens it kept)
         self.blocks = {}        # (block before, the block's tokens) -> sequence that holds it
         self.max_tokens, self.max_seqs = max_tokens, max_seqs
         self.free_seqs = list(range(max_seqs - 1, -1, -1))
-        self.reused = self.computed = 0
+        self.reused = self.computed = self.admitted = 0
 
     def _ints(self, values):
         return torch.tensor(values, dtype=torch.int32, device=self.device)
@@ -109,7 +110,9 @@ class Instance:
         news = []
         for i, s in zip(order, seqs):
             self.tokens[s] = np.ascontiguousarray(prompts[i], dtype=np.uint32)
-            self.origin[s] = found[i]
+            self.origin[s] = self.serial.get(found[i][0], -1), found[i][1]
+            self.serial[s] = self.admitted
+            self.admitted += 1
             news.append(self.tokens[s][found[i][1]:])
             self.reused += found[i][1]
         logits = self._forward(seqs, news)
@@ -137,7 +140,7 @@ class Instance:
             for key in self._chain(self.tokens[s]):
                 if self.blocks.get(key) == s:
                     del self.blocks[key]
-            del self.tokens[s], self.origin[s]
+            del self.tokens[s], self.origin[s], self.serial[s]
             self.free_seqs.append(s)
 
     def groups(self, seqs):

@@ -66,3 +66,39 @@ def test_a_batch_that_cannot_run_changes_nothing(make, batch, room):
     assert books(node) == before
     node.admit([prompt(rng, 40)], room=1)
     check_books(node)
+
+
+def decode_alone(make, tokens, steps, followed):
+    """Logits of a sequence run by itself, fed the tokens that were decoded."""
+    node = make()
+    seqs, logits = node.admit([tokens], room=steps)
+    out = [logits[0]]
+    for t in followed:
+        out.append(node._forward(seqs, [np.asarray([t], dtype=np.uint32)])[0])
+    return out
+
+
+def test_a_reused_id_is_another_origin(make):
+    """Children of a sequence, and children of the one that its id went to, decode side by side."""
+    import torch
+    rng, node = np.random.default_rng(3), make(pages=200, max_seqs=12)
+    first, other = prompt(rng, 32), prompt(rng, 32)
+    parent, _ = node.admit([prompt(rng, first, 3)])
+    old, old_logits = node.admit([prompt(rng, first, 2), prompt(rng, first, 5)], room=3)
+    node.drop(parent)
+    again, _ = node.admit([prompt(rng, other, 4)])
+    assert again == parent   # the id is given out again
+    new, new_logits = node.admit([prompt(rng, other, 1), prompt(rng, other, 7)], room=3)
+    assert node.reused == 4 * 32
+    seqs, logits = old + new, torch.cat([old_logits, new_logits])
+    start = [node.tokens[s] for s in seqs]
+    decoded = node.decode(seqs, logits, 3)
+    assert node.cache.last_error() == 0
+    for i, tokens in enumerate(start):
+        alone = decode_alone(make, tokens, 3, decoded[:, i].tolist())
+        # the same sums in 32 bits in another order: far less than 2^-12 of logits of order 1
+        assert [int(x.argmax()) for x in alone[:3]] == decoded[:, i].tolist()
+        assert float((logits[i] - alone[0]).abs().max()) < 2.0 ** -12
+    offsets, prefixes = node.groups(seqs)
+    assert offsets.tolist() == [0, 2, 4] and prefixes.tolist() == [32, 32]
+    check_books(node)
