@@ -48,7 +48,7 @@ class Instance:
         self.tokens = {}        # sequence -> its tokens, oldest first
         self.serial = {}        # sequence -> its number among all that were ever admitted (ids are given out again)
         self.origin = {}        # sequence -> (serial of the sequence it forked from or -1, tokens it kept)
-        self.blocks = {}        # (block before, the block's tokens) -> sequence that holds it
+        self.blocks = {}        # (block before, the block's tokens) -> sequences that hold it, oldest first
         self.max_tokens, self.max_seqs = max_tokens, max_seqs
         self.free_seqs = list(range(max_seqs - 1, -1, -1))
         self.reused = self.computed = self.admitted = 0
@@ -69,7 +69,7 @@ class Instance:
         for key in self._chain(tokens):
             if key not in self.blocks or n + B > most:
                 break
-            seq, n = self.blocks[key], n + B
+            seq, n = next(reversed(self.blocks[key])), n + B
         return seq, n
 
     def _short(self, pages, seqs):
@@ -118,7 +118,7 @@ class Instance:
         logits = self._forward(seqs, news)
         for s in seqs:
             for key in self._chain(self.tokens[s]):
-                self.blocks[key] = s
+                self.blocks.setdefault(key, {})[s] = None
         return seqs, logits
 
     def decode(self, seqs, logits, steps):
@@ -138,8 +138,10 @@ class Instance:
         self.cache.free(self._ints(seqs))
         for s in seqs:
             for key in self._chain(self.tokens[s]):
-                if self.blocks.get(key) == s:
-                    del self.blocks[key]
+                holders = self.blocks.get(key, {})
+                holders.pop(s, None)
+                if not holders:
+                    self.blocks.pop(key, None)
             del self.tokens[s], self.origin[s], self.serial[s]
             self.free_seqs.append(s)
 

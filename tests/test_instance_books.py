@@ -25,7 +25,7 @@ def prompt(rng, *parts):
 
 
 def books(node):
-    return (list(node.free_seqs), dict(node.origin), dict(node.blocks), {s: t.tolist() for s, t in node.tokens.items()},
+    return (list(node.free_seqs), dict(node.origin), {k: list(h) for k, h in node.blocks.items()}, {s: t.tolist() for s, t in node.tokens.items()},
             node.cache.books.refs[:], node.cache.books.lengths[:])
 
 
@@ -36,7 +36,7 @@ def check_books(node):
         assert m.lengths[s] == len(t) and node.origin[s][1] % m.B == 0
     for s in node.free_seqs:
         assert m.lengths[s] == 0
-    assert set(node.origin) == set(node.tokens) and set(node.blocks.values()) <= set(node.tokens)
+    assert set(node.origin) == set(node.tokens) and all(h and set(h) <= set(node.tokens) for h in node.blocks.values())
 
 
 def test_oldest_sequences_make_room_for_ids(make):
@@ -102,3 +102,21 @@ def test_a_reused_id_is_another_origin(make):
     offsets, prefixes = node.groups(seqs)
     assert offsets.tolist() == [0, 2, 4] and prefixes.tolist() == [32, 32]
     check_books(node)
+
+
+@pytest.mark.parametrize("gone", [0, 1, 2])
+def test_a_prefix_stays_held_while_someone_holds_it(make, gone):
+    """Of three sequences with one prefix any may be dropped: the others' pages are found."""
+    rng, node = np.random.default_rng(5), make(pages=200, max_seqs=12)
+    head = prompt(rng, 48)
+    held = [node.admit([prompt(rng, head, n)])[0][0] for n in (3, 20, 9)]
+    assert node.reused == 2 * 48
+    node.drop([held[gone]])
+    before = node.reused
+    seqs, _ = node.admit([prompt(rng, head, 4)])
+    assert node.reused - before == 48
+    check_books(node)
+    node.drop([s for s in held if s in node.tokens and s not in seqs] + seqs)
+    assert node.blocks == {} and not any(node.cache.books.refs)
+    _, reused = node.admit([prompt(rng, head, 4)]), node.reused
+    assert reused == before + 48   # nobody holds it any more
