@@ -20,6 +20,7 @@ import time
 import numpy as np
 import torch
 
+from . import dualmap as D
 from .cache import PagedCache
 
 
@@ -114,8 +115,12 @@ class Instance:
             self.serial[s] = self.admitted
             self.admitted += 1
             news.append(self.tokens[s][found[i][1]:])
-            self.reused += found[i][1]
-        logits = self._forward(seqs, news)
+        try:
+            logits = self._forward(seqs, news)
+        except D.DualMapError:
+            self.drop(seqs)
+            raise
+        self.reused += sum(found[i][1] for i in order)
         for s in seqs:
             for key in self._chain(self.tokens[s]):
                 self.blocks.setdefault(key, {})[s] = None
@@ -128,9 +133,9 @@ class Instance:
             token = logits.argmax(-1)
             out.append(token)
             host = token.cpu().numpy().astype(np.uint32)
+            logits = self._forward(seqs, [t[None] for t in host])
             for s, t in zip(seqs, host):
                 self.tokens[s] = np.append(self.tokens[s], t)
-            logits = self._forward(seqs, [t[None] for t in host])
         return torch.stack(out) if out else torch.empty(0, len(seqs), dtype=torch.int64, device=self.device)
 
     def drop(self, seqs):
@@ -157,7 +162,8 @@ class Instance:
         return self._ints(offsets + [len(seqs)]), self._ints(prefix)
 
     def _forward(self, seqs, news):
-        """Appends the new tokens of each sequence and returns the logits of its last one."""
+        """Appends the new tokens of each sequence and returns the logits of its last one.
+        A step that the cache refused raises DualMapError (synchronises)."""
         counts = [len(t) for t in news]
         offsets = np.concatenate([[0], np.cumsum(counts)])
         T, hq, hk, d = int(offsets[-1]), self.q_heads, self.kv_heads, self.dim
@@ -172,6 +178,9 @@ class Instance:
             q = self.cache.append(ids, at, qkv[:, :hq], qkv[:, hq:hq + hk], qkv[:, hq + hk:], self.cos, self.sin, layer=layer,
                                   q_weight=qw, k_weight=kw)
             x = x + self.cache.attend(plan, q, layer=layer).view(T, hq * d) @ self.out[layer]
+        err = self.cache.last_error()
+        if err:
+            raise D.DualMapError(err, "instance")
         self.computed += T
         return x[at[1:].long() - 1] @ self.embedding.T
 
@@ -181,7 +190,6 @@ def run(workload_name, instance=0, batches=4, decode=16, overrides=None, pages=8
     sys.path.insert(0, os.path.dirname(os.path.dirname(os.path.abspath(__file__))))
     from tracegen import Trace, workload
 
-    from . import dualmap as D
     from .scheduler import Scheduler
 
     w = workload(workload_name, **(overrides or {}))

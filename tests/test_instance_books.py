@@ -120,3 +120,33 @@ def test_a_prefix_stays_held_while_someone_holds_it(make, gone):
     assert node.blocks == {} and not any(node.cache.books.refs)
     _, reused = node.admit([prompt(rng, head, 4)]), node.reused
     assert reused == before + 48   # nobody holds it any more
+
+
+def test_decoding_past_the_pages_is_an_error(make):
+    """A step that the pages do not suffice for raises; what is held stays as it was."""
+    from paper_2602_06502_gb300 import dualmap as D
+    rng, node = np.random.default_rng(6), make(pages=4)
+    seqs, logits = node.admit([prompt(rng, 30), prompt(rng, 31)])
+    with pytest.raises(D.DualMapError):
+        node.decode(seqs, logits, 5)
+    assert sorted(len(node.tokens[s]) for s in seqs) == [31, 32]   # one step fitted
+    check_books(node)
+    assert node.cache.last_error() == 0
+
+
+def test_a_prompt_that_fails_leaves_nothing(make, monkeypatch):
+    from paper_2602_06502_gb300 import dualmap as D
+    rng, node = np.random.default_rng(7), make()
+    head = prompt(rng, 32)
+    node.admit([prompt(rng, head, 3)])
+    before = books(node)
+
+    def refused(*a, **k):
+        node.cache.error = D.DM_ERR_INVALID_ARG
+
+    with monkeypatch.context() as m:
+        m.setattr(node.cache, "plan", refused)
+        with pytest.raises(D.DualMapError):
+            node.admit([prompt(rng, head, 5), prompt(rng, 12)])
+    after = books(node)
+    assert sorted(after[0]) == sorted(before[0]) and after[1:] == before[1:] and node.reused == 0
