@@ -56,17 +56,22 @@ __device__ __forceinline__ void warp_run(uint32_t pages, uint32_t gw, uint32_t &
     end = min(pages, begin + per);
 }
 
+// Sums stop at kTooMany, more than the pages of any cache: 1,024 sequences may
+// each ask for 2^22 blocks and more, which 32 bits do not hold.
+constexpr uint32_t kTooMany = (1u << 30) + 1;
+
 __device__ __forceinline__ uint32_t scan_incl(uint32_t x) {
     const uint32_t lane = threadIdx.x & 31;
 #pragma unroll
     for (int d = 1; d < 32; d *= 2) {
         const uint32_t y = __shfl_up_sync(~0u, x, d);
-        if (lane >= d) x += y;
+        if (lane >= d) x = min(x + y, kTooMany);
     }
     return x;
 }
 
-// Exclusive scan over the CTA's threads; total receives the sum.
+// Exclusive scan over the CTA's threads; total receives the sum.  Where that is
+// kTooMany the scan is not one: the caller refuses the call.
 __device__ uint32_t block_scan(uint32_t x, uint32_t *s_warp, uint32_t &total) {
     const uint32_t wid = threadIdx.x >> 5, lane = threadIdx.x & 31;
     const uint32_t in = scan_incl(x);

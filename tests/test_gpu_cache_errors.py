@@ -50,3 +50,21 @@ def test_output_of_a_refused_plan(torch):
     assert bool(torch.isnan(c.attend(plan, q)).all())
     assert torch.equal(c.attend(good, q), want)   # a plan from before the error still holds
     assert c.last_error() == 0
+
+
+@pytest.mark.parametrize("more", [0, 4])
+def test_blocks_past_32_bits(torch, more):
+    """1,024 sequences that together ask for 2^32 blocks (and one more) of a small pool."""
+    import cache_reference as R
+    from paper_2602_06502_gb300 import dualmap as D
+    from paper_2602_06502_gb300.cache import PagedCache
+    n, blocks = 1024, (1 << 22) + 1
+    z = dict(dtype=torch.int32, device="cuda")
+    k = torch.zeros(1, 8, 1, 4, 64, dtype=torch.bfloat16, device="cuda")
+    c = PagedCache(k, k.clone(), torch.empty(n, blocks, **z), torch.zeros(n, **z), torch.zeros(8, **z))
+    c.extend(R.ints(range(n)), R.ints([1 << 24] * (n - 1) + [(1 << 24) + more]))
+    assert c.last_error() == D.DM_ERR_CAPACITY
+    assert not bool(c.lengths.any()) and not bool(c.refs.any())
+    c.extend(R.ints([5, 3]), R.ints([9, 20]))
+    assert c.last_error() == 0
+    assert c.tables[5, :3].tolist() == [0, 1, 2] and c.tables[3, :5].tolist() == [3, 4, 5, 6, 7]
