@@ -682,8 +682,9 @@ typedef struct {
  * rotate turns the pair (a, b) of frequency j at position p to (a cos - b
  * sin, b cos + a sin) with cos[p][j] and sin[p][j].  Computed in 32 bits and
  * rounded once.  Rows outside offsets[0] .. offsets[n] are not touched.
- * Recorded: DM_ERR_INVALID_ARG (an id, offset or page out of range, more new
- * tokens than the sequence has, a position beyond rope_rows); which of the
+ * Recorded: DM_ERR_INVALID_ARG (an id, offset or page out of range, a sequence
+ * with new tokens twice, more new tokens than the sequence has, a position
+ * beyond rope_rows); which of the
  * call's other rows are then stored is not specified.  Asynchronous. */
 DM_API dm_status dm_cache_append(const dm_cache *c, const dm_append_args *a, void *stream);
 

@@ -22,6 +22,7 @@ namespace {
 struct AppendArgs {
     const int32_t *seqs, *offsets, *tables, *lengths;
     uint32_t *status;
+    int32_t *mark;            // per sequence: which of the call's named it last
     const uint4 *q, *k, *v;
     uint4 *q_out, *kc, *vc;   // kc, vc: this layer's pages
     uint64_t qt, qh, kt, kh, vt, vh, ot, oh, page_stride;   // 16-byte units
@@ -120,6 +121,12 @@ __global__ void __launch_bounds__(kThreads, 6) k_append(AppendArgs p) {
         if (lane == 0) set_err(p.status, DM_ERR_INVALID_ARG);
         return;
     }
+    // A sequence named twice would have two writers in its slots.  Of the two
+    // that have tokens the later one here finds the other; a mark that an
+    // earlier call left is checked against this call's sequences, so it says
+    // nothing wrong.
+    uint32_t named = lo;
+    if (h0 == 0 && lane == 0 && (int32_t)t == p.offsets[lo]) named = (uint32_t)atomicExch(p.mark + s, (int32_t)lo);
     const uint64_t slot = page * p.page_stride + (uint32_t)pos % p.B * p.token_step;
     // this lane's cosines and sines: of its own values' frequencies
     constexpr int F = kInterleaved ? 4 : 8;
@@ -137,6 +144,7 @@ __global__ void __launch_bounds__(kThreads, 6) k_append(AppendArgs p) {
 #pragma unroll
             for (int i = 0; i < F; ++i) sn[i] = -sn[i];
     }
+    if (named != lo && named < p.n && p.seqs[named] == s && p.offsets[named + 1] > p.offsets[named]) set_err(p.status, DM_ERR_INVALID_ARG);
     const uint32_t partner = sub * L + (low ? l + half / 8 : l - half / 8) % L;
     // heads h .. end: normed and rotated (kTurn) or as they are, loads ahead
     auto run = [&](auto turn, const uint4 *src, uint64_t step, uint4 *dst, uint64_t dst_step, uint32_t h, uint32_t end, const uint4 *weight,
@@ -222,6 +230,7 @@ extern "C" dm_status dm_cache_append(const dm_cache *c, const dm_append_args *a,
     const PageShape ps = page_shape(c);
     AppendArgs p{};
     p.seqs = a->seqs, p.offsets = a->offsets, p.tables = c->tables, p.lengths = c->lengths, p.status = c->status;
+    p.mark = cache_work(c).mark;
     p.q = (const uint4 *)a->q, p.k = (const uint4 *)a->k, p.v = (const uint4 *)a->v, p.q_out = (uint4 *)a->q_out;
     p.kc = (uint4 *)c->k + a->layer * (c->layer_stride / 8);
     p.vc = (uint4 *)c->v + a->layer * (c->layer_stride / 8);

@@ -155,3 +155,34 @@ def test_refusals(torch):
     c.lengths[b["place"][1]] = 0                                   # more new tokens than the sequence has
     c.append(b["seqs"], b["offsets"], q, k, k, cos, sin)
     assert c.last_error() == inv
+
+
+def test_a_sequence_named_twice(torch):
+    """Two of a call's entries with tokens for one sequence are refused, wherever they stand; other orders of the
+    same sequences, one after another, are not."""
+    import cache_reference as R
+    from paper_2602_06502_gb300 import dualmap as D
+    n = 300
+    b = R.make_batch(9, page=16, kv_heads=1, dim=64, dtype=torch.float16, own=[20 + i % 7 for i in range(n)], new=[1] * n)
+    c, place = b["cache"], b["place"]
+    x = torch.randn(n, 1, 64, generator=b["gen"], device="cuda").half()
+    once = R.ints(range(n + 1))
+    for order in (place, place[::-1], place[7:] + place[:7], place):
+        c.append(R.ints(order), once, x, x, x)
+        assert c.last_error() == 0
+    for i, j in ((0, 1), (3, 299), (120, 121), (0, 299)):
+        order = list(place)
+        order[j] = order[i]
+        for _ in range(3):
+            c.append(R.ints(order), once, x, x, x)
+            assert c.last_error() == D.DM_ERR_INVALID_ARG
+        # without tokens the second is no writer
+        gaps = [0]
+        for k in range(n):
+            gaps.append(gaps[-1] + (k != j))
+        c.append(R.ints(order), R.ints(gaps), x[:n - 1], x[:n - 1], x[:n - 1])
+        assert c.last_error() == 0
+        c.append(b["seqs"], once, x, x, x)
+        assert c.last_error() == 0
+    for i in (0, 150, 299):
+        assert torch.equal(R.read_seq(b, c.k, i)[-1], x[i]) and torch.equal(R.read_seq(b, c.v, i)[-1], x[i])
