@@ -21,9 +21,10 @@ LAYOUTS = {"heads": D.DM_PAGES_HEADS, "tokens": D.DM_PAGES_TOKENS}
 class Plan:
     """One step's division over the GPU (PagedCache.plan), for all its layers."""
 
-    def __init__(self, struct, keep, tokens, q_heads, errors):
+    def __init__(self, struct, keep, tokens, q_heads, errors, stream):
         self.struct, self.ref, self.keep, self.tokens, self.q_heads = struct, C.byref(struct), keep, tokens, q_heads
         self.errors = errors   # that the cache had reported by then
+        self.streams = {stream}   # whose work may still use the plan's buffer, first the one it was allocated on
 
 
 class PagedCache:
@@ -63,6 +64,7 @@ class PagedCache:
         self.work = torch.empty(size, dtype=torch.uint8, device=self.device)
         self.struct.work, self.struct.work_bytes = self.work.data_ptr(), size
         self._lib, self._ref, self._plan_bytes, self._errors = D.lib(), C.byref(self.struct), {}, 0
+        self._streams = set()   # whose work may still use the cache
 
     @classmethod
     def empty(cls, *, pages, kv_heads, head_dim, max_seqs, max_tokens, page_tokens=16, layers=1, dtype=torch.bfloat16,
@@ -106,9 +108,19 @@ class PagedCache:
         if torch.cuda.current_device() != self.device.index:
             with torch.cuda.device(self.device):
                 return self._call(name, *args)
-        rc = getattr(self._lib, name)(self._ref, *args, torch._C._cuda_getCurrentRawStream(self.device.index))
+        stream = torch._C._cuda_getCurrentRawStream(self.device.index)
+        if stream not in self._streams:
+            self._hold(stream, self._streams, self.k, self.v, self.tables, self.lengths, self.refs, self.status, self.work)
+        rc = getattr(self._lib, name)(self._ref, *args, stream)
         if rc:
             raise D.DualMapError(rc, name)
+
+    def _hold(self, stream, seen, *tensors):
+        """Keeps the memory of `tensors`, once they are dropped, from being given
+        out before the current stream is done with them (once per stream)."""
+        for x in tensors:
+            x.record_stream(torch.cuda.current_stream(self.device))
+        seen.add(stream)
 
     def last_error(self):
         """The status of the first call that was refused on the device, which it clears (synchronises)."""
@@ -200,7 +212,8 @@ class PagedCache:
         s = D.dm_plan(self._ints("seqs", seqs), self._ints("offsets", offsets, n + 1), n, tokens, q_heads, groups, go, gp,
                       work.data_ptr(), size)
         self._call("dm_cache_plan", C.byref(s))
-        return Plan(s, (seqs, offsets, group_offsets, group_prefix, work), tokens, q_heads, self._errors)
+        return Plan(s, (seqs, offsets, group_offsets, group_prefix, work), tokens, q_heads, self._errors,
+                    torch._C._cuda_getCurrentRawStream(self.device.index))
 
     def attend(self, plan, q, *, layer=0, scale=None, out=None, lse=None):
         """One layer's attention of the planned step: q [tokens, q_heads,
@@ -216,6 +229,9 @@ class PagedCache:
         if lse is not None and (lse.dtype is not torch.float32 or lse.shape != (plan.tokens, plan.q_heads) or
                                 not lse.is_contiguous() or lse.device != self.device):
             raise ValueError(f"lse: contiguous float32 of shape {(plan.tokens, plan.q_heads)} on {self.device}")
+        stream = torch._C._cuda_getCurrentRawStream(self.device.index)
+        if stream not in plan.streams:
+            self._hold(stream, plan.streams, plan.keep[-1])
         a = D.dm_attend_args(layer, self.head_dim ** -0.5 if scale is None else scale, qp, op,
                              None if lse is None else lse.data_ptr(), qt, qh, ot, oh)
         self._call("dm_cache_attend", plan.ref, C.byref(a))
