@@ -202,7 +202,8 @@ class PagedCache:
         shape = (n, groups, tokens, q_heads)
         size = self._plan_bytes.get(shape)
         if size is None:
-            size = D.dm_plan_bytes(self.struct, *shape)
+            with torch.cuda.device(self.device):   # it depends on the device's SMs
+                size = D.dm_plan_bytes(self.struct, *shape)
             if not size:
                 raise D.DualMapError(D.DM_ERR_INVALID_ARG, "dm_plan_bytes")
             if len(self._plan_bytes) > 4096:
