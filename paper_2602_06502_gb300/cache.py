@@ -5,7 +5,8 @@ reads them (dm_cache_* of include/dualmap.h).
 Only marshalling: it checks shapes and types, allocates outputs and work
 buffers on the device, and enqueues the C calls on torch's current stream.
 Calls on one cache, and the attention of one plan, have to be ordered by the
-caller, as work that shares a tensor is.
+caller, as work that shares a tensor is.  The calls serve: they give no
+gradients, so with grad mode on they refuse tensors that want one.
 """
 
 import ctypes as C
@@ -88,11 +89,17 @@ class PagedCache:
             raise ValueError(f"{name}: contiguous int32 on {self.device}" + (f" of length {n}" if n is not None else ""))
         return x.data_ptr()
 
+    @staticmethod
+    def _no_grad(name, x):
+        if x.requires_grad and torch.is_grad_enabled():
+            raise ValueError(f"{name} requires grad, and this call gives no gradients: use torch.no_grad() or detach it")
+
     def _rows(self, name, x, tokens, heads):
         """Address and strides (token, head) of [tokens, heads, head_dim]."""
         shape, stride = (tokens, heads, self.head_dim), x.stride()
         if x.dtype is not self.dtype or x.device != self.device or x.shape != shape or stride[2] != 1:
             raise ValueError(f"{name}: {self.dtype} on {self.device} of shape {shape}, head_dim contiguous")
+        self._no_grad(name, x)
         # the stride of a dimension of one element says nothing
         return x.data_ptr(), (stride[0] if tokens > 1 else 0), (stride[1] if heads > 1 else 0)
 
@@ -101,6 +108,7 @@ class PagedCache:
             return None
         if x.dtype is not self.dtype or x.shape != (self.head_dim,) or x.device != self.device or not x.is_contiguous():
             raise ValueError(f"{name}: contiguous {self.dtype} of shape {(self.head_dim,)} on {self.device}")
+        self._no_grad(name, x)
         return x.data_ptr()
 
     def _call(self, name, *args):
@@ -182,6 +190,7 @@ class PagedCache:
                 if x.dtype is not torch.float32 or x.dim() != 2 or x.shape != cos.shape or not x.is_contiguous() or \
                         x.device != self.device:
                     raise ValueError(f"{name}: contiguous float32 [positions, rotated dims / 2] on {self.device}")
+                self._no_grad(name, x)
             cp, sp, (rows, dims) = cos.data_ptr(), sin.data_ptr(), cos.shape
         a = D.dm_append_args(self._ints("seqs", seqs), self._ints("offsets", offsets, n + 1), n, tokens, layer, heads,
                              qp, kp, vp, op, qt, qh, kt, kh, vt, vh, ot, oh, self._vector("q_weight", q_weight),
