@@ -574,7 +574,7 @@ DM_API dm_status dm_potc_max_loads(uint32_t n_bins, uint64_t m_balls, uint32_t d
  * and its work buffer, so the caller orders them (one stream, or events).
  * Arguments that the host can check return an error and change nothing.
  * What only the device can check (ids, lengths, free pages) is recorded in
- * *status: the call that found it changes nothing, and the calls after it do
+ * *status: the call that found it changes nothing (unless it says otherwise), and the calls after it do
  * nothing, until dm_cache_last_error has read and cleared the status. */
 
 typedef enum { DM_BF16 = 0, DM_F16 = 1 } dm_dtype;
@@ -586,7 +586,11 @@ typedef enum { DM_PAGES_HEADS = 0, DM_PAGES_TOKENS = 1 } dm_page_layout;
  * is slot p % page_tokens of page tables[s * max_blocks + p / page_tokens].
  * refs[p] counts the sequences that hold page p; 0 = free.  A page that is
  * held more than once is full, and nothing writes it.  A cache without
- * sequences has lengths and refs of zero. */
+ * sequences has lengths and refs of zero.  The table entries of the blocks
+ * that a sequence holds are ids of pages.  Where one is not, no call leaves
+ * the arrays, but the cache is no longer one: append, fork and free record
+ * DM_ERR_INVALID_ARG and may have changed a part of what they should, and
+ * attention reads zeros. */
 typedef struct {
     void *k, *v;              /* layer 0's page 0; 16-byte aligned */
     uint32_t dtype;           /* dm_dtype */
@@ -738,8 +742,9 @@ typedef struct {
  * the keys and values of head h / (q_heads / kv_heads); *lse receives the
  * natural logarithm of the softmax's sum.  A token at a negative position
  * (a sequence shorter than its new tokens) sees nothing: zeros, and an lse
- * of minus infinity.  Slots behind a sequence's end are not read, whatever
- * they hold.  Scores, maxima, sums and the output are held in 32 bits; the
+ * of minus infinity.  What the slots behind a sequence's end hold does not
+ * matter, but they are read with their page, so nothing may write them
+ * meanwhile.  Scores, maxima, sums and the output are held in 32 bits; the
  * weights are rounded to the cache's type for the product with v.  Rows
  * outside offsets[0] .. offsets[n] are not touched.  Uses the plan's work
  * buffer, so layers of one plan run one after another.  A key or value in a

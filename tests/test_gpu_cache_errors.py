@@ -68,3 +68,37 @@ def test_blocks_past_32_bits(torch, more):
     c.extend(R.ints([5, 3]), R.ints([9, 20]))
     assert c.last_error() == 0
     assert c.tables[5, :3].tolist() == [0, 1, 2] and c.tables[3, :5].tolist() == [3, 4, 5, 6, 7]
+
+
+def test_table_entries_that_are_no_pages(torch):
+    """fork, free and append record them and write nothing outside the cache; attention reads zeros there."""
+    import cache_reference as R
+    from paper_2602_06502_gb300 import dualmap as D
+    from paper_2602_06502_gb300.cache import PagedCache
+    b, c, q = step(torch, junk=False)
+    guard = torch.zeros(c.refs.shape[0] + 8, dtype=torch.int32, device="cuda")
+    guard[4:-4] = c.refs
+    at, child, inv = b["place"][1], min(set(range(4)) - set(b["place"])), D.DM_ERR_INVALID_ARG
+    spare = int((c.refs == 0).nonzero()[0])
+    c.k[:, spare], c.v[:, spare] = 0, 0
+    c = PagedCache(c.k, c.v, c.tables, c.lengths, guard[4:-4])
+    k, v = c.k.clone(), c.v.clone()
+    c.tables[at, 2] = spare
+    zeros = c.attend(c.plan(b["seqs"], b["offsets"], b["tokens"], 4), q)
+    rows = torch.ones(220, 8, 64, dtype=torch.bfloat16, device="cuda")
+    for bad in (c.refs.shape[0], -1, 1 << 30):
+        c.tables[at, 2] = bad
+        got = c.attend(c.plan(b["seqs"], b["offsets"], b["tokens"], 4), q)
+        assert c.last_error() == 0 and torch.equal(got, zeros)
+        c.append(R.ints([at]), R.ints([0, 220]), rows[:, :4], rows[:, 4:6], rows[:, 6:])
+        assert c.last_error() == inv
+        assert torch.equal(c.k[:, spare], k[:, spare])
+        c.k.copy_(k)
+        c.v.copy_(v)
+        c.fork(R.ints([at]), R.ints([child]), R.ints([64]))
+        assert c.last_error() == inv
+        c.free(R.ints([child]))
+        c.last_error()
+        c.lengths[child] = 0
+        assert torch.equal(c.k, k) and torch.equal(c.v, v)
+    assert not bool(guard[:4].any()) and not bool(guard[-4:].any())
