@@ -186,3 +186,29 @@ def test_a_sequence_named_twice(torch):
         assert c.last_error() == 0
     for i in (0, 150, 299):
         assert torch.equal(R.read_seq(b, c.k, i)[-1], x[i]) and torch.equal(R.read_seq(b, c.v, i)[-1], x[i])
+
+
+@pytest.mark.parametrize("page,layout,dtype,dim,hk,hq,new,own,rot,inter,norms", CASES)
+def test_every_row_is_stored(torch, page, layout, dtype, dim, hk, hq, new, own, rot, inter, norms):
+    """All keys and values of a call, gathered from their slots at once, and all slots that are not theirs."""
+    import cache_reference as R
+    dt = getattr(torch, dtype)
+    b = R.make_batch(15, page=page, kv_heads=hk, dim=dim, dtype=dt, layout=layout, own=own, new=new, layers=2, junk=False)
+    c, T = b["cache"], b["tokens"]
+    x = (torch.randn(T, hq + 2 * hk, dim, generator=b["gen"], device="cuda") * 3).to(dt)
+    q, k, v = x[:, :hq], x[:, hq:hq + hk], x[:, hq + hk:]
+    qw, kw = ((1 + 0.3 * torch.randn(dim, generator=b["gen"], device="cuda")).to(dt) if norms else None for _ in range(2))
+    cos, sin = tables(torch, max(b["length"]), rot) if rot else (None, None)
+    held = c.k.clone(), c.v.clone()
+    got = c.append(b["seqs"], b["offsets"], q, k, v, cos, sin, layer=1, q_weight=qw, k_weight=kw, eps=1e-5, interleaved=inter)
+    assert c.last_error() == 0
+    pos = torch.cat([torch.arange(n - w, n, device="cuda") for n, w in zip(b["length"], new)])
+    at = torch.tensor([b["rows"][i][p // page] for i, (n, w) in enumerate(zip(b["length"], new)) for p in range(n - w, n)],
+                      dtype=torch.long, device="cuda")
+    where = (1, at, slice(None), pos % page) if layout == "heads" else (1, at, pos % page)
+    check(torch, got, *reference(torch, q, qw, 1e-5, cos, sin, pos, rot, inter), dt)
+    check(torch, c.k[where], *reference(torch, k, kw, 1e-5, cos, sin, pos, rot, inter), dt)
+    assert torch.equal(c.v[where], v)
+    for pool, before in zip((c.k, c.v), held):
+        pool[where] = before[where]
+        assert torch.equal(pool, before)

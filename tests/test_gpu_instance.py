@@ -79,3 +79,32 @@ def test_behind_the_router():
     assert len(rows) == 2 and rows[1]["requests"] > 0
     assert 0 < rows[1]["reused_tokens"] <= rows[1]["router_hit_tokens"]
     assert rows[1]["reused_tokens"] + rows[1]["computed_tokens"] == rows[1]["prompt_tokens"] + 3 * rows[1]["requests"]
+
+
+def test_decoded_steps_give_the_same_logits():
+    """Step by step: sequences that decode together behind shared prefixes, and each alone, fed the same tokens."""
+    lib_ready()
+    rng = np.random.default_rng(4)
+    node, alone = make(), make()
+    first = prompts(rng, [("a", 200, 5), ("b", 64, 40)], 500)
+    node.admit(first)
+    batch = [np.concatenate([first[0][:192], rng.integers(0, 500, size=n).astype(np.uint32)]) for n in (7, 1, 40, 16)]
+    batch += [np.concatenate([first[1][:64], rng.integers(0, 500, size=n).astype(np.uint32)]) for n in (3, 15)]
+    batch += prompts(rng, [("c", 0, 33)], 500)
+    steps = 20   # over the ends of pages
+    seqs, logits = node.admit(batch, room=steps)
+    assert node.reused == 4 * 192 + 2 * 64
+    offsets, prefixes = node.groups(seqs)
+    assert sorted(prefixes.tolist()) == [0, 64, 192]
+    start = [node.tokens[s] for s in seqs]
+    feed = rng.integers(0, 500, size=(steps, len(seqs))).astype(np.uint32)
+    together = [logits] + [node._forward(seqs, [t[None] for t in row]) for row in feed]
+    for k, tokens in enumerate(start):
+        own, ref = alone.admit([tokens], room=steps)
+        refs = [ref] + [alone._forward(own, [row[k][None]]) for row in feed]
+        for i, (x, y) in enumerate(zip(together, refs)):
+            # as for the prompts: a unit in an activation's last place (2^-8) here and there, over two layers
+            far = (x[k].float() - y[0].float()).norm() / y[0].float().norm()
+            assert float(far) < 2.0 ** -5, (k, i, float(far))
+        alone.drop(own)
+    assert node.cache.last_error() == 0
