@@ -763,6 +763,12 @@ DM_API dm_status dm_cache_attend(const dm_cache *c, const dm_plan *p, const dm_a
  * allocating calls. */
 DM_API void dm_test_fail_alloc(int64_t n);
 
+/* Testing only, in the debug build: while ns > 0, the first keys of every
+ * dm_cache_attend never arrive and its waits end after ns nanoseconds, so a
+ * test can check that the call records DM_ERR_TIMEOUT, ends, and leaves the
+ * GPU as it was.  A release build returns DM_ERR_INVALID_ARG for ns > 0. */
+DM_API dm_status dm_test_attend_wait(uint64_t ns);
+
 /* Synchronise the stream and return the sticky error (DM_OK if none). */
 DM_API dm_status dm_last_error(dm_handle *h);
 

@@ -8,6 +8,7 @@
 // shared prefix and a sequence's own keys are two such parts, so the prefix is
 // read for all the rows of the group together.
 #include <algorithm>
+#include <atomic>
 #include <cooperative_groups.h>
 
 #include "dm_attend.cuh"
@@ -421,8 +422,9 @@ __global__ void __launch_bounds__(kNarrowT, kNarrowPerSm)
         uint32_t c = 0;   // slots so far
         for (Slots<1, D, kSlotKeys, 1> next(p, w, 0); next.more; next.step(p), ++c) {
             const uint32_t slot = c % N::kSlots, round = c / N::kSlots, at = s_at + slot * 2 * N::kHalf;
-            if (round) mbar_wait(empty(slot), (round - 1) & 1, gave_up, p.status);
+            if (round) mbar_wait(empty(slot), (round - 1) & 1, gave_up, p);
             if (__any_sync(~0u, *gave_up)) break;
+            if (withheld(p, c)) continue;
             if (keys && lane == 0) mbar_expect(full(slot), 2 * N::kHalf);   // the phase ends with this and all the bytes
             __syncwarp();
             next.boxes.load(p, keys ? &mk : &mv, keys ? at : at + N::kHalf, full(slot), next.tok, next.head);
@@ -473,7 +475,7 @@ __global__ void __launch_bounds__(kNarrowT, kNarrowPerSm)
         for (int i = 0; i < D / 8; ++i) o[i][0] = o[i][1] = o[i][2] = o[i][3] = 0.f;
         for (uint32_t j = pair; j < 2 * w.units; j += 2) {
             const uint32_t slot = (c + j) % N::kSlots, round = (c + j) / N::kSlots, at = s_at + slot * 2 * N::kHalf;
-            mbar_wait(full(slot), round & 1, gave_up, p.status);
+            mbar_wait(full(slot), round & 1, gave_up, p);
             const int32_t first = w.k.kv0 + (int32_t)(w.j0 * kNarrowKeys + j * kSlotKeys + key0);
             if (first < w.k.kv1) {
                 // scores: 16 rows x 16 keys
@@ -877,6 +879,19 @@ extern "C" dm_status dm_cache_plan(const dm_cache *c, const dm_plan *pl, void *s
     return status_of(launch_pdl(k_plan, kPlanCl, pl->n <= kPlanFew ? 256 : kPlanT, 0, static_cast<cudaStream_t>(stream), p));
 }
 
+#ifdef DM_DEBUG
+static std::atomic<uint64_t> g_test_wait_ns{0};
+#endif
+
+extern "C" dm_status dm_test_attend_wait(uint64_t ns) {
+#ifdef DM_DEBUG
+    g_test_wait_ns = ns;
+    return DM_OK;
+#else
+    return ns ? DM_ERR_INVALID_ARG : DM_OK;
+#endif
+}
+
 extern "C" dm_status dm_cache_attend(const dm_cache *c, const dm_plan *pl, const dm_attend_args *a, void *stream) {
     using namespace dm;
     PlanShape s;
@@ -897,6 +912,9 @@ extern "C" dm_status dm_cache_attend(const dm_cache *c, const dm_plan *pl, const
     p.o_wide = aligned(a->o, 32) && (a->o_token | a->o_head) % 16 == 0;
     CUtensorMap mk, mv;
     if (!page_map(&mk, c, c->k, a->layer, box) || !page_map(&mv, c, c->v, a->layer, box)) return DM_ERR_CUDA;
+#ifdef DM_DEBUG
+    p.test_wait_ns = g_test_wait_ns;
+#endif
     const auto st = static_cast<cudaStream_t>(stream);
     p.beside = (uint64_t)pl->tokens * s.G > kNarrowRows;   // else so few rows that no block of them is wide
     cudaError_t e = p.beside ? launch_attend_wide(c, p, mk, mv, st) : cudaSuccess;

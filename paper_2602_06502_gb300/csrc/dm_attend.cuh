@@ -186,7 +186,19 @@ struct AttendArgs {
     uint32_t o_wide;                             // rows of o begin on 32 bytes
     uint32_t key;                                // the plan's
     uint32_t beside;                             // the narrow kernel runs beside a wide one
+#ifdef DM_DEBUG
+    uint64_t test_wait_ns;                       // dm_test_attend_wait: 0, or how long waits last
+#endif
 };
+
+// Whether a test has slot c of this CTA's keys never arrive.
+__device__ __forceinline__ bool withheld(const AttendArgs &p, uint32_t c) {
+#ifdef DM_DEBUG
+    return p.test_wait_ns && blockIdx.x == 0 && c == 0;
+#else
+    return false;
+#endif
+}
 
 // The CTA of S whose units begin at `at` of a line of length C, the last i with
 // i C / S <= at: ((at + 1) S - 1) / C.  inv = 2^64 / C rounded down gives that
@@ -316,24 +328,28 @@ __device__ __forceinline__ uint64_t now_ns() {
 }
 constexpr uint32_t kWaits = 1u << 24;
 constexpr uint64_t kWaitNs = 2'000'000'000;
-// Waits for the phase, at most kWaitNs and kWaits tries.
-__device__ __forceinline__ bool mbar_drain(uint32_t bar, uint32_t parity, const volatile uint32_t *gave_up = nullptr) {
+// Waits for the phase, at most `ns` and kWaits tries.
+__device__ __forceinline__ bool mbar_drain(uint32_t bar, uint32_t parity, const volatile uint32_t *gave_up = nullptr, uint64_t ns = kWaitNs) {
     if (mbar_try(bar, parity)) return true;
     const uint64_t t0 = now_ns();
     for (uint32_t i = 0; i < kWaits; ++i) {
         if (mbar_try(bar, parity)) return true;
         if (gave_up && *gave_up) return true;
-        if ((i & 63) == 63 && now_ns() - t0 > kWaitNs) break;
+        if ((i & 63) == 63 && now_ns() - t0 > ns) break;
     }
     return false;
 }
 // The same by a whole warp; a wait that gives up says so in `gave_up` (shared
 // memory), and the CTA's others then return at once.  The caller goes on
 // either way: every loop is as long as its data says, so the CTA ends.
-__device__ __forceinline__ void mbar_wait(uint32_t bar, uint32_t parity, volatile uint32_t *gave_up, uint32_t *status) {
-    if (!mbar_drain(bar, parity, gave_up)) {
+__device__ __forceinline__ void mbar_wait(uint32_t bar, uint32_t parity, volatile uint32_t *gave_up, const AttendArgs &p) {
+    uint64_t ns = kWaitNs;
+#ifdef DM_DEBUG
+    if (p.test_wait_ns) ns = p.test_wait_ns;
+#endif
+    if (!mbar_drain(bar, parity, gave_up, ns)) {
         *gave_up = 1;
-        set_err(status, DM_ERR_TIMEOUT);
+        set_err(p.status, DM_ERR_TIMEOUT);
     }
     __syncwarp();
 }

@@ -210,8 +210,9 @@ __global__ void __launch_bounds__(kWideT, 1)
             for (Slots<0, D, kWideKeys, 3> next(p, w, pw); next.more && !stop; next.step(p)) {
                 for (uint32_t v = 0; v < 2; ++v, ++c) {
                     const uint32_t i = c % W::kStages, round = c / W::kStages;
-                    if (round) mbar_wait(empty(i), (round - 1) & 1, gave_up, p.status);
+                    if (round) mbar_wait(empty(i), (round - 1) & 1, gave_up, p);
                     if ((stop = __any_sync(~0u, *gave_up))) break;
+                    if (withheld(p, c)) continue;
                     if (pw == 0 && lane == 0) mbar_expect(full(i), W::kTile);   // the phase ends with this and all the bytes
                     __syncwarp();
                     next.boxes.load(p, v ? &mv : &mk, s_at + W::kRing + i * W::kTile, full(i), next.tok, next.head);
@@ -259,15 +260,15 @@ __global__ void __launch_bounds__(kWideT, 1)
             uint32_t c = 0, pieces[2] = {0, 0}, ps[2] = {0, 0};   // stages; pieces and weight tiles of A and B
             while (w.next(p)) {
                 const uint32_t X = w.k.rows > 128 ? 2 : 1;
-                for (uint32_t x = 0; x < X; ++x) mbar_wait(q_full(x), pieces[x] & 1, gave_up, p.status);
-                mbar_wait(full(c % W::kStages), (c / W::kStages) & 1, gave_up, p.status);
+                for (uint32_t x = 0; x < X; ++x) mbar_wait(q_full(x), pieces[x] & 1, gave_up, p);
+                mbar_wait(full(c % W::kStages), (c / W::kStages) & 1, gave_up, p);
                 fence_after();
                 for (uint32_t x = 0; x < X; ++x) scores(x, c % W::kStages);
                 release(empty(c % W::kStages));
                 for (uint32_t j = 0; j < w.units; ++j) {
                     const uint32_t v = c + 1, vs = v % W::kStages, nk = c + 2, ns = nk % W::kStages;
                     const bool last = j + 1 == w.units;
-                    mbar_wait(full(vs), (v / W::kStages) & 1, gave_up, p.status);
+                    mbar_wait(full(vs), (v / W::kStages) & 1, gave_up, p);
                     const int32_t left = w.k.kv1 - (w.k.kv0 + (int32_t)((w.j0 + j) * kWideKeys));
                     if (left > 0 && left < (int32_t)kWideKeys && (left & ((1 << p.B_log) - 1))) {
                         // slots of the last page behind the end hold whatever was
@@ -283,7 +284,7 @@ __global__ void __launch_bounds__(kWideT, 1)
                     }
                     for (uint32_t x = 0; x < X; ++x) {
                         for (uint32_t half = 0; half < 2; ++half) {
-                            mbar_wait(p_full(x, half), ps[x] & 1, gave_up, p.status);
+                            mbar_wait(p_full(x, half), ps[x] & 1, gave_up, p);
                             fence_after();
                             product(x, vs, half, j == 0);
                         }
@@ -291,7 +292,7 @@ __global__ void __launch_bounds__(kWideT, 1)
                         if (last) {
                             release(o_full(x));
                         } else {
-                            if (x == 0) mbar_wait(full(ns), (nk / W::kStages) & 1, gave_up, p.status);
+                            if (x == 0) mbar_wait(full(ns), (nk / W::kStages) & 1, gave_up, p);
                             fence_after();
                             scores(x, ns);
                         }
@@ -352,7 +353,7 @@ __global__ void __launch_bounds__(kWideT, 1)
             more = next(ahead);
             float m = -INFINITY, l = 0.f;   // the maximum in the scores' own unit
             for (uint32_t j = 0; j < w.units; ++j, ++ss) {
-                mbar_wait(s_full(x), ss & 1, gave_up, p.status);
+                mbar_wait(s_full(x), ss & 1, gave_up, p);
                 fence_after();
                 if (j + 1 == w.units && more) fetch(ahead);
                 const int32_t seen = limit - (w.k.kv0 + (int32_t)((w.j0 + j) * kWideKeys));
@@ -419,7 +420,7 @@ __global__ void __launch_bounds__(kWideT, 1)
                 l += (la.x + la.y) + (lb.x + lb.y);
             }
             if (more) fetched();
-            mbar_wait(o_full(x), pieces & 1, gave_up, p.status);
+            mbar_wait(o_full(x), pieces & 1, gave_up, p);
             ++pieces;
             fence_after();
             const bool whole = w.whole(), on = r < rows;

@@ -185,6 +185,7 @@ SIGNATURES = {
     "dm_cache_plan": (C.c_int, [C.POINTER(dm_cache), C.POINTER(dm_plan), C.c_void_p]),
     "dm_cache_attend": (C.c_int, [C.POINTER(dm_cache), C.POINTER(dm_plan), C.POINTER(dm_attend_args), C.c_void_p]),
     "dm_test_fail_alloc": (None, [C.c_int64]),
+    "dm_test_attend_wait": (C.c_int, [C.c_uint64]),
     "dm_last_error": (C.c_int, [C.c_void_p]),
     "dm_set_profiling": (C.c_int, [C.c_void_p, C.c_int]),
     "dm_get_stage_times": (C.c_int, [C.c_void_p, C.c_void_p, C.c_void_p, C.c_int]),
