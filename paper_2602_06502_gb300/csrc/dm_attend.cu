@@ -91,9 +91,9 @@ __global__ void __cluster_dims__(kPlanCl, 1, 1) __launch_bounds__(kPlanT) k_plan
     uint32_t *gmax = few ? s_max : p.w.group_max + (rank & 1) * p.groups, *gn = few ? s_n : p.w.group_n + (rank & 1) * p.groups;
     __shared__ uint64_t s_sum[4];   // cost and units of each kind
     __shared__ uint32_t s_any;      // rank 0: some CTA found the step wrong
+    __shared__ uint32_t s_stood;    // an earlier call's error
     if (tid < 4) s_sum[tid] = 0;
-    const bool stood = tid == 0 && has_err(p.status);   // an earlier call's error
-    if (tid == 0) s_bad = s_any = stood;
+    if (tid == 0) s_bad = s_any = s_stood = has_err(p.status);
     if (few)
         for (uint32_t g = tid; p.groups && g <= p.groups; g += T) {
             s_offsets[g] = p.group_offsets[g];
@@ -318,7 +318,7 @@ __global__ void __cluster_dims__(kPlanCl, 1, 1) __launch_bounds__(kPlanT) k_plan
     if (rank == 0 && tid == 0) {
         // a step that was not looked at leaves no plan: once that error has been
         // read, attention on the buffer says so
-        p.w.head->key = !failed ? p.key : stood ? 0 : kRefused;
+        p.w.head->key = !failed ? p.key : s_stood ? 0 : kRefused;
         if (failed) set_err(p.status, DM_ERR_INVALID_ARG);
     }
     if (s_bad || !p.groups) return;
