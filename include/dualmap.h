@@ -718,7 +718,8 @@ DM_API uint64_t dm_plan_bytes(const dm_cache *c, uint32_t n, uint32_t groups, ui
 /* Divide a step's attention over the GPU, from lengths as they are: once per
  * step, for all its layers.  A group's prefix is read once for all its
  * sequences where each of them has fewer than 128 query rows (new tokens x
- * query heads per key head); otherwise each sequence reads it by itself.
+ * query heads per key head); otherwise each sequence reads it by itself.  So
+ * a sequence with more is better named in a group of its own.
  * The plan holds until lengths or tables change.  Recorded:
  * DM_ERR_INVALID_ARG (an id, offset or group out of range, a prefix that is
  * no multiple of B, that reaches into the new tokens of a sequence, or whose

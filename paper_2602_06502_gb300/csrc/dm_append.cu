@@ -9,7 +9,7 @@
 // arithmetic is in 32 bits; the only rounding is the store.
 //
 // Bound: HBM bandwidth, 2 bytes read and 2 written per value (46,000 tokens of
-// 48 heads, D = 128: 176 us, 6.4 TB/s); a few tokens alone, the latency of one
+// 48 heads, D = 128: 177 us, 6.4 TB/s); a few tokens alone, the latency of one
 // launch (61 tokens: 5.6 us).
 #include <algorithm>
 #include <type_traits>

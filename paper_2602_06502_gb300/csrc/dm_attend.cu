@@ -20,7 +20,7 @@ namespace {
 
 // -- the plan ----------------------------------------------------------------------
 
-// 256 threads a CTA for a few sequences (9.9 -> 8.3 us for four; with 256
+// 256 threads a CTA for a few sequences (10.7 -> 9.2 us for four; with 256
 // sequences the page check needs them all).
 constexpr uint32_t kPlanCl = 8, kPlanT = 1024, kPlanFew = 32;
 
@@ -56,7 +56,9 @@ __device__ uint64_t block_scan(uint64_t x, uint64_t *s_warp, uint64_t &total) {
 
 // Measured with 256 single tokens of 64 heads behind 12 prefixes (D = 128), and
 // with drafts of up to 8 tokens and 12 heads for 96 sequences (D = 64): the
-// times of CTAs with units of one sort, in cycles / 100.
+// times of CTAs with units of one sort, in cycles / 100.  They share the SMs out
+// between the kernels and even the CTAs' ends out; for prompts, whose units
+// arithmetic bounds, they are the same.
 constexpr PlanCosts kCosts128 = {23, 20, 75, 24, 8}, kCosts64 = {20, 17, 38, 15, 6};
 constexpr uint32_t kFewGroups = 512, kFewBlocks = 2048;   // kept in shared memory
 
@@ -76,7 +78,7 @@ __device__ __forceinline__ int32_t group_at(const int32_t *offsets, const int32_
 // CTA 0 lays the wide blocks out and CTA 1 the narrow ones (both work out the
 // entities, writing the same); the others see that a group's sequences begin
 // with the same pages.  Bound: latency, a chain of small steps, so what is
-// searched is kept in shared memory.  8 us for four sequences, 13 to 16 for 96
+// searched is kept in shared memory.  9 us for four sequences, 13 to 16 for 96
 // to 256 in five to twelve groups.
 __global__ void __cluster_dims__(kPlanCl, 1, 1) __launch_bounds__(kPlanT) k_plan(PlanArgs p) {
     __shared__ uint64_t s_warp[32], s_cum[kFewBlocks];
@@ -352,7 +354,7 @@ __global__ void __cluster_dims__(kPlanCl, 1, 1) __launch_bounds__(kPlanT) k_plan
 // full through TMA, two CTAs per SM; each of four warps takes the 16
 // keys of its half of every other slot, with its own running maximum and sum,
 // and the four join once per tile.  16 sequences of up to 100,000 keys of their
-// own, two key heads, D = 128: 169 us at 6.1 TB/s from HBM, beside 154 us of the
+// own, two key heads, D = 128: 171 us at 6.1 TB/s from HBM, beside 153 us of the
 // wide kernel's SMs.
 
 constexpr uint32_t kSlotKeys = 32, kNarrowT = 192;

@@ -19,7 +19,7 @@
 //
 // Bound: the exponentials and the tensor cores in about equal parts where
 // there are 256 rows; memory where there are few.  16 prompts' 100-1,000 new
-// tokens behind 2,048-8,192 cached ones, 32 heads over 8, D = 128: 545 us, 1.6
+// tokens behind 2,048-8,192 cached ones, 32 heads over 8, D = 128: 550 us, 1.6
 // PFLOP/s (the tensor pipe busy for 72% of the cycles).
 #include <algorithm>
 
