@@ -170,8 +170,9 @@ class PagedCache:
 
         Sequence seqs[i]'s new tokens are rows offsets[i] .. offsets[i + 1] of q
         [tokens, q_heads, head_dim], k and v [tokens, kv_heads, head_dim], and
-        the last ones of the sequence, which has been extended by them.  cos,
-        sin: float32 [positions, rotated dims / 2]; without them nothing turns.
+        the last ones of the sequence, which has been extended by them; each is
+        named once.  cos, sin: float32 [positions, rotated dims / 2]; without
+        them nothing turns.
         q_weight, k_weight [head_dim]: without one there is no norm.  out:
         where the queries go; may be q."""
         n, tokens, heads = seqs.shape[0], k.shape[0], q.shape[1]
