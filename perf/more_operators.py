@@ -286,7 +286,7 @@ def run(s):
     if c["kind"] == "route":
         if not own:
             return _plain_route(s["logits"], c["top_k"], c["renormalize"])
-        r = X.route(s["logits"], c["top_k"], renormalize=c["renormalize"])
+        r = X.choose(s["logits"], c["top_k"], renormalize=c["renormalize"])
         return dict(ids=r.ids, weights=r.weights, offsets=r.offsets, slots=r.slots, sources=r.sources)
     if c["kind"] == "grouped":
         if own:
