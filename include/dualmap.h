@@ -577,7 +577,12 @@ DM_API dm_status dm_potc_max_loads(uint32_t n_bins, uint64_t m_balls, uint32_t d
  * *status: the call that found it changes nothing (unless it says otherwise), and the calls after it do
  * nothing, until dm_cache_last_error has read and cleared the status. */
 
-typedef enum { DM_BF16 = 0, DM_F16 = 1 } dm_dtype;
+typedef enum {
+    DM_BF16 = 0,
+    DM_F16 = 1,
+    DM_I8 = 2,    /* weights and rows of dm_product; not in a cache */
+    DM_F32 = 3    /* scores of dm_choose_experts, outputs of dm_product */
+} dm_dtype;
 
 /* Order of a page's values: [head][token][dim] or [token][head][dim]. */
 typedef enum { DM_PAGES_HEADS = 0, DM_PAGES_TOKENS = 1 } dm_page_layout;
@@ -593,7 +598,7 @@ typedef enum { DM_PAGES_HEADS = 0, DM_PAGES_TOKENS = 1 } dm_page_layout;
  * attention reads zeros. */
 typedef struct {
     void *k, *v;              /* layer 0's page 0; 16-byte aligned */
-    uint32_t dtype;           /* dm_dtype */
+    uint32_t dtype;           /* DM_BF16 or DM_F16 */
     uint32_t layout;          /* dm_page_layout */
     uint32_t layers;          /* >= 1 */
     uint32_t pages;           /* 1 .. 2^30 */
@@ -754,6 +759,147 @@ typedef struct {
  * Recorded: DM_ERR_INVALID_ARG (the buffer holds no plan of this shape, as
  * after a dm_cache_plan that did nothing), DM_ERR_TIMEOUT (a wait in the kernel gave up).  Asynchronous. */
 DM_API dm_status dm_cache_attend(const dm_cache *c, const dm_plan *p, const dm_attend_args *a, void *stream);
+
+/* ---------------------------------------------------------------------------
+ * An instance's projections and expert layers (the paper leaves them to the
+ * serving engine): products with 16-bit weights or with 8-bit ones that have a
+ * scale per output channel, for one set of weights or for many experts whose
+ * rows are ragged, the quantising of rows, the choice of experts, and the layer
+ * made of them.
+ *
+ * As the prefix cache's, these calls take no handle: the caller owns the memory
+ * and every call enqueues its work on `stream` and returns.  Arguments that the
+ * host can check return an error and change nothing.  What only the device can
+ * check is recorded in *status (one word, 0 at the start): the product that
+ * found it may have written a part of its rows, and the products after it do
+ * nothing, until dm_products_last_error has read and cleared the word.
+ *
+ * A matrix's rows are `row` elements apart, a multiple of 16 bytes, and begin
+ * on 16 bytes; what lies between a row's end and the next is neither used nor
+ * written, whatever it holds (it is read where it shares 16 bytes with the row). */
+
+/* Weights of `experts` products, [expert][n][k]: y = x w^T. */
+typedef struct {
+    const void *w;            /* 16-byte aligned */
+    const float *scale;       /* DM_I8: [expert][n] */
+    uint32_t dtype;           /* DM_BF16, DM_F16 or DM_I8 */
+    uint32_t experts;         /* 1 .. 1024 */
+    uint32_t n, k;            /* 1 .. 2^24 */
+    uint64_t row;             /* elements; a multiple of 16 bytes, >= k */
+    uint64_t expert;          /* elements from an expert to the next; a multiple of 16 bytes */
+} dm_weights;
+
+/* Synchronise `stream`, return the status that was recorded first (DM_OK if
+ * none) and clear it. */
+DM_API dm_status dm_products_last_error(uint32_t *status, void *stream);
+
+/* Rows in 8 bits (dm_quantize). */
+typedef struct {
+    const void *x;            /* rows x k, DM_BF16 or DM_F16 */
+    int8_t *q;                /* rows x k */
+    float *scale;             /* rows */
+    const int32_t *count;     /* device: only the first *count rows; NULL: all */
+    uint64_t x_row, q_row;    /* elements; multiples of 16 bytes */
+    uint32_t dtype, rows, k;
+    float eps;                /* of a norm, >= 0; negative: no norm */
+} dm_quantize_args;
+
+/* scale = max |x| / 127 over a row and q = 127 x / max |x|, to the nearest
+ * whole number, ties to even; a row of zeros has zeros and a scale of 0, and a
+ * row with a value that is not finite has zeros and a scale that is NaN.  With
+ * eps >= 0 the row is divided by the root of (mean x^2 + eps) first, which
+ * changes its scale alone.  Asynchronous. */
+DM_API dm_status dm_quantize(const dm_quantize_args *a, void *stream);
+
+/* The choice of experts for a batch's tokens (dm_choose_experts). */
+typedef struct {
+    const void *logits;       /* tokens x experts, DM_BF16, DM_F16 or DM_F32; rows of any distance */
+    uint64_t logits_row;      /* elements, >= experts */
+    uint32_t dtype;
+    uint32_t tokens;          /* tokens * top_k < 2^31 */
+    uint32_t experts;         /* 1 .. 1024 */
+    uint32_t top_k;           /* 1 .. min(experts, 32) */
+    uint32_t renormalize;     /* 1: softmax over the chosen, 0: over all experts */
+    uint32_t reserved0;       /* must be 0 */
+    int32_t *ids;             /* tokens x top_k, the largest score first */
+    float *weights;           /* tokens x top_k */
+    int32_t *offsets;         /* experts + 1 */
+    int32_t *slots;           /* tokens x top_k */
+    int32_t *sources;         /* tokens * top_k */
+    void *work;               /* dm_choose_bytes bytes, 16-byte aligned */
+    uint64_t work_bytes;
+} dm_choose_args;
+
+/* Size of dm_choose_args.work; 0 for an invalid shape. */
+DM_API uint64_t dm_choose_bytes(uint32_t tokens, uint32_t experts, uint32_t top_k);
+
+/* Each token's top_k experts by score (ties to the lowest id) and their
+ * weights; and the chosen pairs sorted by expert, then by token and place:
+ * expert e's are slots offsets[e] .. offsets[e+1]), slots[p] is the slot of
+ * pair p = token * top_k + place, and sources[s] the pair of slot s.  An expert
+ * with a score of minus infinity is never chosen: its id and slot are -1 and
+ * its weight 0, so a row of nothing else takes no slot.  sources is -1 behind
+ * the last slot.  A score that is NaN counts as the lowest finite number and
+ * makes the token's weights NaN.  Asynchronous. */
+DM_API dm_status dm_choose_experts(const dm_choose_args *a, void *stream);
+
+/* A product's rows (dm_product). */
+typedef struct {
+    const void *x;            /* x_rows x k: of the weights' type */
+    const float *x_scale;     /* DM_I8: x_rows */
+    void *y;                  /* rows x n (n / 2 where gated); any alignment of its type */
+    const int32_t *offsets;   /* experts + 1, not decreasing, within 0 .. rows: expert e has rows
+                                 offsets[e] .. offsets[e+1]); NULL with one expert: all rows */
+    const int32_t *sources;   /* rows: row r reads row sources[r] / per_source of x; NULL: row r */
+    uint32_t *status;
+    void *work;               /* dm_product_bytes bytes, 256-byte aligned */
+    uint64_t work_bytes;
+    uint64_t x_row, y_row;    /* elements; x_row a multiple of 16 bytes */
+    uint32_t rows, x_rows;    /* below 2^31 */
+    uint32_t per_source;      /* >= 1 with sources */
+    uint32_t y_dtype;         /* DM_BF16, DM_F16 or DM_F32 */
+    uint32_t gated;           /* 1: the first half of the channels is a gate */
+    uint32_t reserved0;       /* must be 0 */
+} dm_product_args;
+
+/* Size of dm_product_args.work on the current device (it depends on its SMs);
+ * 0 for an invalid shape. */
+DM_API uint64_t dm_product_bytes(const dm_weights *w, uint32_t rows, uint32_t gated);
+
+/* y[r, c] = sum over j of x[r, j] w[e, c, j], times x_scale[r] scale[e, c] for
+ * 8-bit weights; gated: y[r, c] = silu(z[r, c]) z[r, n/2 + c] of that z, with
+ * silu(g) = g / (1 + exp(-g)).  Sums are held in 32 bits, and y is rounded
+ * once.  Sums of 8-bit products are exact below 2^24 (any k up to 1,040).  Rows
+ * outside offsets[0] .. offsets[experts] are not touched.
+ * Recorded: DM_ERR_INVALID_ARG (offsets or sources out of range),
+ * DM_ERR_TIMEOUT (a wait in the kernel gave up).  Asynchronous. */
+DM_API dm_status dm_product(const dm_weights *w, const dm_product_args *a, void *stream);
+
+/* A layer of experts (dm_experts). */
+typedef struct {
+    const void *x;            /* tokens x k, DM_BF16 or DM_F16 */
+    const void *logits;       /* as dm_choose_args */
+    const void *residual;     /* tokens x k of x's type, or NULL */
+    void *y;                  /* tokens x k of x's type; may be residual, and overlap nothing else */
+    uint32_t *status;
+    void *work;               /* dm_experts_bytes bytes, 256-byte aligned */
+    uint64_t work_bytes;
+    uint64_t x_row, logits_row, residual_row, y_row;   /* elements; but for the logits' multiples of 16 bytes */
+    uint32_t dtype, logits_dtype;
+    uint32_t tokens, top_k, renormalize;
+    uint32_t reserved0;       /* must be 0 */
+} dm_experts_args;
+
+/* Size of dm_experts_args.work on the current device; 0 for an invalid shape. */
+DM_API uint64_t dm_experts_bytes(const dm_weights *up, const dm_weights *down, uint32_t tokens, uint32_t top_k);
+
+/* y[t] = residual[t] + sum over the chosen experts e of weight(t, e)
+ * down_e(h), h = silu(g) u with (g, u) the halves of up_e(x[t]): up has 2 m
+ * channels over x's k, down has k channels over m.  h is rounded to x's type;
+ * with 8-bit weights (both) x and then h are quantised row by row.  The
+ * experts' parts and their sum are held in 32 bits.  A token without experts
+ * gets its residual, or zeros.  Recorded: as dm_product.  Asynchronous. */
+DM_API dm_status dm_experts(const dm_weights *up, const dm_weights *down, const dm_experts_args *a, void *stream);
 
 /* Testing only (no paper counterpart): after this call the library's
  * (n + 1)-th device allocation, counted over every handle of the process,

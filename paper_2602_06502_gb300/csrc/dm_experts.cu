@@ -1,0 +1,605 @@
+// dm_experts.cu -- what surrounds the products of an expert layer: rows in 8
+// bits (dm_quantize), the choice of experts (dm_choose_experts), the sum of
+// their parts, and the layer made of all (dm_experts).
+#include <algorithm>
+
+#include "dm_product.cuh"
+
+namespace dm {
+namespace {
+
+template <class T>
+struct Two;
+template <>
+struct Two<__nv_bfloat16> {
+    using type = __nv_bfloat162;
+    static __device__ __forceinline__ float2 up(type x) { return __bfloat1622float2(x); }
+    static __device__ __forceinline__ type down(float a, float b) { return __floats2bfloat162_rn(a, b); }
+};
+template <>
+struct Two<__half> {
+    using type = __half2;
+    static __device__ __forceinline__ float2 up(type x) { return __half22float2(x); }
+    static __device__ __forceinline__ type down(float a, float b) { return __floats2half2_rn(a, b); }
+};
+
+template <class T>
+__device__ __forceinline__ void unpack(const uint4 &x, float *f) {
+    const auto *p = reinterpret_cast<const typename Two<T>::type *>(&x);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        const float2 y = Two<T>::up(p[i]);
+        f[2 * i] = y.x;
+        f[2 * i + 1] = y.y;
+    }
+}
+
+// 8 values of a row from element `at` on, zeros from `end` on.
+template <class T>
+__device__ __forceinline__ void load8(const T *row, uint32_t at, uint32_t end, float *f) {
+    uint4 x = make_uint4(0, 0, 0, 0);
+    if (at < end) x = *reinterpret_cast<const uint4 *>(row + at);
+    unpack<T>(x, f);
+    if (at < end && end - at < 8) {
+#pragma unroll
+        for (uint32_t i = 0; i < 8; ++i)
+            if (i >= end - at) f[i] = 0.f;
+    }
+}
+
+// -- rows in 8 bits -------------------------------------------------------------------
+//
+// Bound: memory, 2 bytes read and 1 written per value.  A row stays in the
+// registers of a warp (up to 2,048 values) or of a CTA (up to 16,384); a longer
+// one is read twice.
+//
+// 127 x is exact in 32 bits, and 127 x / top lies on a border between two steps
+// only where that is a whole number of halves, or at least 1 / 4096 away from
+// one (x and top have up to 11 bits).  So the product with 127 / top, which is
+// off by less than 2^-15, decides all but what is near a border, and there the
+// exact division decides: q is what the formula says to the last case.
+
+struct QuantizeArgs {
+    const char *x;
+    int8_t *q;
+    float *scale;
+    const int32_t *count;
+    uint64_t x_row, q_row;   // elements
+    uint32_t rows, k;
+    float eps;
+};
+
+__device__ __forceinline__ uint32_t step_of(float x, float by, float f, float top) {
+    const float y = x * by, r = rintf(y);
+    if (fabsf(fabsf(y - r) - 0.5f) < 1e-3f) return (uint32_t)(__float2int_rn(__fdiv_rn(x * f, top))) & 0xFF;
+    return (uint32_t)__float2int_rn(y) & 0xFF;
+}
+
+template <class T, uint32_t kLanes>
+__global__ void __launch_bounds__(256) k_quantize(QuantizeArgs p) {
+    constexpr uint32_t kHeld = 8, kPer = 256 / kLanes;   // vectors of a lane; rows of a CTA
+    __shared__ float s_part[8][2];
+    pdl_enter();
+    const uint32_t lane = threadIdx.x % kLanes, rows = p.count ? (uint32_t)min(max(__ldcg(p.count), 0), (int32_t)p.rows) : p.rows;
+    for (uint32_t r = blockIdx.x * kPer + threadIdx.x / kLanes; r < rows; r += gridDim.x * kPer) {
+        const T *x = reinterpret_cast<const T *>(p.x) + r * p.x_row;
+        float top = 0.f, sum = 0.f;
+        bool odd = false;   // a value that is not finite
+        uint4 held[kHeld];
+        auto look = [&](const float *f) {
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+                odd |= !(fabsf(f[i]) <= 3.4028235e38f);
+                top = fmaxf(top, fabsf(f[i]));
+                sum += f[i] * f[i];
+            }
+        };
+#pragma unroll
+        for (uint32_t i = 0; i < kHeld; ++i) {
+            const uint32_t at = (i * kLanes + lane) * 8;
+            held[i] = make_uint4(0, 0, 0, 0);
+            if (at < p.k) held[i] = *reinterpret_cast<const uint4 *>(x + at);
+        }
+#pragma unroll
+        for (uint32_t i = 0; i < kHeld; ++i) {
+            const uint32_t at = (i * kLanes + lane) * 8;
+            float f[8];
+            unpack<T>(held[i], f);
+            if (at + 8 > p.k) {
+#pragma unroll
+                for (uint32_t j = 0; j < 8; ++j)
+                    if (at + j >= p.k) f[j] = 0.f;
+            }
+            look(f);
+        }
+        for (uint32_t at = (kHeld * kLanes + lane) * 8; at < p.k; at += kLanes * 8) {
+            float f[8];
+            load8(x, at, p.k, f);
+            look(f);
+        }
+        if (odd) top = INFINITY;
+#pragma unroll
+        for (int d = 16; d; d /= 2) {
+            top = fmaxf(top, __shfl_xor_sync(~0u, top, d));
+            sum += __shfl_xor_sync(~0u, sum, d);
+        }
+        if constexpr (kLanes > 32) {
+            __syncthreads();   // the row before has been read
+            if (lane % 32 == 0) s_part[lane / 32][0] = top, s_part[lane / 32][1] = sum;
+            __syncthreads();
+            top = sum = 0.f;
+#pragma unroll
+            for (uint32_t i = 0; i < kLanes / 32; ++i) top = fmaxf(top, s_part[i][0]), sum += s_part[i][1];
+        }
+        float scale = __fdiv_rn(top, 127.f);
+        if (p.eps >= 0.f) scale *= rsqrtf(sum / (float)p.k + p.eps);
+        if (top == INFINITY) scale = __int_as_float(0x7FC00000);
+        if (lane == 0) p.scale[r] = scale;
+        // powers of two keep 127 / top and 127 x in range
+        const float shift = top > 1e30f ? 0x1p-64f : top < 1e-30f ? 0x1p64f : 1.f;
+        const float big = top * shift, by = top == 0.f || top == INFINITY ? 0.f : __fdiv_rn(127.f, big);
+        int8_t *q = p.q + r * p.q_row;
+        auto put = [&](uint32_t at, const float *f) {
+            uint32_t b[8];
+#pragma unroll
+            for (int i = 0; i < 8; ++i) b[i] = by == 0.f ? 0u : step_of(f[i] * shift, by, 127.f, big);
+            if (at + 8 <= p.k) {
+                *reinterpret_cast<uint2 *>(q + at) =
+                    make_uint2(b[0] | b[1] << 8 | b[2] << 16 | b[3] << 24, b[4] | b[5] << 8 | b[6] << 16 | b[7] << 24);
+            } else {
+#pragma unroll
+                for (uint32_t i = 0; i < 8; ++i)
+                    if (at + i < p.k) q[at + i] = (int8_t)b[i];
+            }
+        };
+#pragma unroll
+        for (uint32_t i = 0; i < kHeld; ++i) {
+            const uint32_t at = (i * kLanes + lane) * 8;
+            if (at >= p.k) break;
+            float f[8];
+            unpack<T>(held[i], f);
+            put(at, f);
+        }
+        for (uint32_t at = (kHeld * kLanes + lane) * 8; at < p.k; at += kLanes * 8) {
+            float f[8];
+            load8(x, at, p.k, f);
+            put(at, f);
+        }
+    }
+}
+
+template <class T>
+cudaError_t launch_quantize(const QuantizeArgs &p, cudaStream_t st) {
+    const uint32_t most = (uint32_t)sm_count() * 8;
+    if (p.k <= 2048) return launch_pdl(k_quantize<T, 32>, std::min((p.rows + 7) / 8, most), 256, 0, st, p);
+    return launch_pdl(k_quantize<T, 256>, std::min(p.rows, most), 256, 0, st, p);
+}
+
+// -- the choice of experts ---------------------------------------------------------------
+//
+// A warp per token: scores in the lanes' registers as whole numbers of the same
+// order; the best that is left is a maximum over the warp, top_k times.  A CTA
+// takes a tile of tokens and counts each expert's.  The second kernel (the
+// first itself, where one tile holds all) places the pairs: an expert's first
+// slot is the sum of the counts of the experts before it and of its own in the
+// tiles before; within a tile a pair's place is the number of equal ones before
+// it, found for 32 pairs at a time.
+//
+// Bound: latency.
+
+constexpr uint32_t kChooseT = 1024, kTilePairs = 1024, kTileTokens = 128, kTurn = 256;
+
+struct ChooseArgs {
+    const char *logits;
+    uint64_t row;   // elements
+    uint32_t tokens, experts, top_k, renormalize, tile, tiles, pitch;   // tokens of a tile; its count; counts between experts
+    int32_t *ids, *offsets, *slots, *sources;
+    float *weights;
+    int32_t *counts;   // [expert][tile]
+};
+
+uint32_t tile_tokens(uint32_t top_k) { return std::min(kTileTokens, kTilePairs / top_k); }
+
+__device__ __forceinline__ float score_at(const __nv_bfloat16 *p) { return __bfloat162float(*p); }
+__device__ __forceinline__ float score_at(const __half *p) { return __half2float(*p); }
+__device__ __forceinline__ float score_at(const float *p) { return *p; }
+
+// Whole numbers in the order of the scores; 0: nothing to choose.
+__device__ __forceinline__ uint32_t order_of(float x) {
+    if (x == -INFINITY) return 0;
+    if (x != x) x = -3.4028235e38f;
+    if (x == 0.f) x = 0.f;   // -0 is 0
+    const uint32_t b = __float_as_uint(x);
+    return b >> 31 ? ~b : b | 0x80000000u;
+}
+__device__ __forceinline__ float score_of(uint32_t o) { return o == 0 ? -INFINITY : __uint_as_float(o >> 31 ? o & 0x7FFFFFFFu : ~o); }
+
+// The slots of a tile's pairs.  s_off: where each expert's pairs of this tile
+// begin; s_seen: room for kTurn / 32 counts of each.
+__device__ void place_pairs(const ChooseArgs &p, uint32_t tile, int32_t *s_off, uint32_t *s_seen) {
+    const uint32_t tid = threadIdx.x, wid = tid >> 5, lane = tid & 31, E = p.experts;
+    const uint32_t first = tile * p.tile, pairs = min(p.tile, p.tokens - first) * p.top_k;
+    for (uint32_t i0 = 0; i0 < pairs; i0 += kTurn) {
+        for (uint32_t i = tid; i < kTurn / 32 * E; i += kChooseT) s_seen[i] = 0;
+        __syncthreads();
+        const uint32_t i = i0 + tid, pair = first * p.top_k + i;
+        int32_t e = -1;
+        uint32_t same = 0;
+        if (tid < kTurn) {
+            if (i < pairs) e = __ldcg(p.ids + pair);
+            same = __match_any_sync(~0u, e);
+            if (e >= 0 && lane == (uint32_t)__ffs(same) - 1) s_seen[wid * E + e] = __popc(same);
+        }
+        __syncthreads();
+        for (uint32_t x = tid; x < E; x += kChooseT) {
+            uint32_t sum = (uint32_t)s_off[x];
+#pragma unroll
+            for (uint32_t q = 0; q < kTurn / 32; ++q) {
+                const uint32_t n = s_seen[q * E + x];
+                s_seen[q * E + x] = sum;
+                sum += n;
+            }
+            s_off[x] = (int32_t)sum;
+        }
+        __syncthreads();
+        if (tid < kTurn && i < pairs) {
+            int32_t slot = -1;
+            if (e >= 0) {
+                slot = (int32_t)(s_seen[wid * E + e] + __popc(same & ((1u << lane) - 1)));
+                p.sources[slot] = (int32_t)pair;
+            }
+            p.slots[pair] = slot;
+        }
+        __syncthreads();
+    }
+}
+
+// Exclusive sums over the experts of s_off, one a thread; also their sum.
+__device__ int32_t scan_experts(int32_t x, int32_t *s_warp, int32_t &total) {
+    const uint32_t wid = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    int32_t in = x;
+#pragma unroll
+    for (int d = 1; d < 32; d *= 2) {
+        const int32_t y = __shfl_up_sync(~0u, in, d);
+        if ((int)lane >= d) in += y;
+    }
+    if (lane == 31) s_warp[wid] = in;
+    __syncthreads();
+    if (wid == 0) {
+        int32_t z = s_warp[lane];
+#pragma unroll
+        for (int d = 1; d < 32; d *= 2) {
+            const int32_t y = __shfl_up_sync(~0u, z, d);
+            if ((int)lane >= d) z += y;
+        }
+        s_warp[lane] = z;
+    }
+    __syncthreads();
+    total = s_warp[31];
+    return in - x + (wid ? s_warp[wid - 1] : 0);
+}
+
+template <class T, uint32_t kV>
+__global__ void __launch_bounds__(kChooseT) k_choose(ChooseArgs p) {
+    extern __shared__ uint32_t s_seen[];
+    __shared__ int32_t s_off[kChooseT], s_warp[32];
+    pdl_enter();
+    const uint32_t tid = threadIdx.x, wid = tid >> 5, lane = tid & 31, tile = blockIdx.x;
+    s_off[tid] = 0;
+    __syncthreads();
+    const uint32_t first = tile * p.tile, last = min(first + p.tile, p.tokens);
+    for (uint32_t token = first + wid; token < last; token += kChooseT / 32) {
+        const T *row = reinterpret_cast<const T *>(p.logits) + token * p.row;
+        uint32_t o[kV];
+        bool nan = false;
+#pragma unroll
+        for (uint32_t v = 0; v < kV; ++v) {
+            const uint32_t e = v * 32 + lane;
+            const float x = e < p.experts ? score_at(row + e) : -INFINITY;
+            nan |= x != x;
+            o[v] = order_of(x);
+        }
+        nan = __any_sync(~0u, nan);
+        uint32_t most = 0;
+#pragma unroll
+        for (uint32_t v = 0; v < kV; ++v) most = max(most, o[v]);
+        const float top = score_of(__reduce_max_sync(~0u, most));
+        float all = 0.f;
+        if (!p.renormalize) {
+#pragma unroll
+            for (uint32_t v = 0; v < kV; ++v) all += o[v] ? expf(score_of(o[v]) - top) : 0.f;
+#pragma unroll
+            for (int d = 16; d; d /= 2) all += __shfl_xor_sync(~0u, all, d);
+        }
+        int32_t mine = -1;   // lane j keeps the j-th choice
+        float score = -INFINITY;
+        for (uint32_t j = 0; j < p.top_k; ++j) {
+            uint32_t best = 0, at = ~0u;
+#pragma unroll
+            for (uint32_t v = 0; v < kV; ++v)
+                if (o[v] > best) best = o[v], at = v * 32 + lane;
+            const uint32_t got = __reduce_max_sync(~0u, best);
+            if (got == 0) break;
+            const uint32_t e = __reduce_min_sync(~0u, best == got ? at : ~0u);
+#pragma unroll
+            for (uint32_t v = 0; v < kV; ++v)
+                if (v * 32 + lane == e) o[v] = 0;
+            if (lane == j) {
+                mine = (int32_t)e;
+                score = score_of(got);
+            }
+        }
+        float w = mine >= 0 ? expf(score - top) : 0.f, sum = w;
+        if (p.renormalize) {
+#pragma unroll
+            for (int d = 16; d; d /= 2) sum += __shfl_xor_sync(~0u, sum, d);
+        } else {
+            sum = all;
+        }
+        if (mine >= 0) w = nan ? __int_as_float(0x7FC00000) : w / sum;
+        if (lane < p.top_k) {
+            p.ids[token * p.top_k + lane] = mine;
+            p.weights[token * p.top_k + lane] = w;
+            if (mine >= 0) atomicAdd(s_off + mine, 1);   // whole numbers: in any order
+        }
+    }
+    __syncthreads();
+    if (p.tiles > 1) {
+        if (tid < p.experts) p.counts[tid * p.pitch + tile] = s_off[tid];
+        return;
+    }
+    int32_t total;
+    const int32_t before = scan_experts(s_off[tid], s_warp, total);
+    s_off[tid] = before;
+    if (tid < p.experts) p.offsets[tid] = before;
+    if (tid == 0) p.offsets[p.experts] = total;
+    for (uint32_t i = (uint32_t)total + tid; i < p.tokens * p.top_k; i += kChooseT) p.sources[i] = -1;
+    __syncthreads();   // the ids too
+    place_pairs(p, 0, s_off, s_seen);
+}
+
+__global__ void __launch_bounds__(kChooseT) k_choose_place(ChooseArgs p) {
+    extern __shared__ uint32_t s_seen[];
+    __shared__ int32_t s_off[kChooseT], s_warp[32];
+    pdl_enter();
+    const uint32_t tid = threadIdx.x, tile = blockIdx.x;
+    int32_t mine = 0, earlier = 0;
+    if (tid < p.experts) {
+        const int4 *c = reinterpret_cast<const int4 *>(p.counts + tid * p.pitch);
+        for (uint32_t i = 0; i < p.tiles; i += 4) {
+            const int4 x = __ldcg(c + i / 4);
+            const int32_t y[4] = {x.x, x.y, x.z, x.w};
+#pragma unroll
+            for (uint32_t j = 0; j < 4; ++j) {
+                if (i + j < p.tiles) mine += y[j];
+                if (i + j < tile) earlier += y[j];
+            }
+        }
+    }
+    int32_t total;
+    const int32_t before = scan_experts(mine, s_warp, total);
+    s_off[tid] = before + earlier;
+    if (tile == 0) {
+        if (tid < p.experts) p.offsets[tid] = before;
+        if (tid == 0) p.offsets[p.experts] = total;
+    }
+    for (uint32_t i = (uint32_t)total + tile * kChooseT + tid; i < p.tokens * p.top_k; i += gridDim.x * kChooseT) p.sources[i] = -1;
+    __syncthreads();
+    place_pairs(p, tile, s_off, s_seen);
+}
+
+template <class T>
+cudaError_t launch_choose(const ChooseArgs &p, cudaStream_t st) {
+    const uint32_t per = (p.experts + 31) / 32, seen = kTurn / 32 * 4 * p.experts;
+    const auto k = per <= 1 ? k_choose<T, 1> : per <= 2 ? k_choose<T, 2> : per <= 4 ? k_choose<T, 4> : per <= 8 ? k_choose<T, 8>
+                 : per <= 16 ? k_choose<T, 16> : k_choose<T, 32>;
+    DM_TRY(launch_pdl(k, p.tiles, kChooseT, seen, st, p));
+    return p.tiles > 1 ? launch_pdl(k_choose_place, p.tiles, kChooseT, seen, st, p) : cudaSuccess;
+}
+
+uint64_t choose_bytes(uint32_t tokens, uint32_t experts, uint32_t top_k) {
+    if (experts < 1 || experts > 1024 || top_k < 1 || top_k > std::min(experts, 32u) || (uint64_t)tokens * top_k > 0x7FFFFFFFull) return 0;
+    const uint64_t tiles = (tokens + tile_tokens(top_k) - 1) / tile_tokens(top_k);
+    return 256 + align_up(tiles, 4) * experts * 4;
+}
+
+cudaError_t choose(const ChooseArgs &from, uint32_t dtype, cudaStream_t st) {
+    ChooseArgs p = from;
+    p.tile = tile_tokens(p.top_k);
+    p.tiles = (p.tokens + p.tile - 1) / p.tile;
+    p.pitch = (uint32_t)align_up(p.tiles, 4);
+    if (p.tokens == 0) p.tiles = 1;   // the offsets
+    return dtype == DM_BF16 ? launch_choose<__nv_bfloat16>(p, st) : dtype == DM_F16 ? launch_choose<__half>(p, st) : launch_choose<float>(p, st);
+}
+
+// -- the sum of the experts' parts ---------------------------------------------------------
+
+struct JoinArgs {
+    const float *parts;   // slot x pitch
+    const int32_t *slots;
+    const float *weights;
+    const char *residual;
+    char *y;
+    uint32_t *status;
+    uint64_t pitch, residual_row, y_row;   // elements
+    uint32_t tokens, top_k, k;
+};
+
+// 4 channels a thread, the parts in the order of the choice.  Bound: memory, 4
+// bytes read for each of a token's parts.
+template <class T>
+__global__ void __launch_bounds__(256) k_join_experts(JoinArgs p) {
+    pdl_enter();
+    if (has_err(p.status)) return;
+    const uint32_t each = (p.k + 3) / 4;
+    for (uint64_t i = blockIdx.x * 256ull + threadIdx.x; i < (uint64_t)p.tokens * each; i += gridDim.x * 256ull) {
+        const uint32_t token = (uint32_t)(i / each), at = (uint32_t)(i % each) * 4, n = min(p.k - at, 4u);
+        float y[4] = {};
+        const T *from = reinterpret_cast<const T *>(p.residual) + token * p.residual_row + at;
+        if (p.residual)
+            for (uint32_t j = 0; j < n; ++j) y[j] = score_at(from + j);
+        for (uint32_t j = 0; j < p.top_k; ++j) {
+            const int32_t slot = __ldcg(p.slots + token * p.top_k + j);
+            if (slot < 0) continue;
+            const float w = __ldcg(p.weights + token * p.top_k + j);
+            const float4 x = __ldcg(reinterpret_cast<const float4 *>(p.parts + (uint64_t)slot * p.pitch + at));
+            y[0] += w * x.x;
+            y[1] += w * x.y;
+            y[2] += w * x.z;
+            y[3] += w * x.w;
+        }
+        T *to = reinterpret_cast<T *>(p.y) + token * p.y_row + at;
+        if (n == 4) {
+            const auto a = Two<T>::down(y[0], y[1]), b = Two<T>::down(y[2], y[3]);
+            *reinterpret_cast<uint2 *>(to) = make_uint2(*reinterpret_cast<const uint32_t *>(&a), *reinterpret_cast<const uint32_t *>(&b));
+        } else {
+            for (uint32_t j = 0; j < n; ++j) to[j] = Two<T>::down(y[j], 0.f).x;
+        }
+    }
+}
+
+// -- the layer ---------------------------------------------------------------------------------
+
+// The layer's work buffer.
+struct LayerWork {
+    int32_t *ids, *offsets, *slots, *sources, *counts;
+    float *weights, *x_scale, *h_scale, *parts;
+    char *xq, *h, *hq, *product;
+    uint64_t h_row, parts_row, xq_row, hq_row;   // elements
+};
+
+uint64_t layer_work(const dm_weights *up, const dm_weights *down, uint32_t tokens, uint32_t top_k, void *base, LayerWork &w) {
+    uint64_t at = 0;
+    auto take = [&](uint64_t bytes) {
+        char *p = static_cast<char *>(base) + at;
+        at += align_up(bytes, 256);
+        return p;
+    };
+    const uint64_t slots = (uint64_t)tokens * top_k;
+    const bool eight = up->dtype == DM_I8;
+    w.h_row = align_up(down->k, 16), w.parts_row = align_up(down->n, 4), w.xq_row = align_up(up->k, 16), w.hq_row = w.h_row;
+    w.offsets = (int32_t *)take(4ull * (up->experts + 1));
+    w.ids = (int32_t *)take(4 * slots);
+    w.weights = (float *)take(4 * slots);
+    w.slots = (int32_t *)take(4 * slots);
+    w.sources = (int32_t *)take(4 * slots);
+    w.counts = (int32_t *)take(choose_bytes(tokens, up->experts, top_k));
+    w.h = take(2 * slots * w.h_row);
+    w.parts = (float *)take(4 * slots * w.parts_row);
+    w.xq = take(eight ? tokens * w.xq_row : 0);
+    w.x_scale = (float *)take(eight ? 4ull * tokens : 0);
+    w.hq = take(eight ? slots * w.hq_row : 0);
+    w.h_scale = (float *)take(eight ? 4 * slots : 0);
+    w.product = take(std::max(dm_product_bytes(up, (uint32_t)slots, 1), dm_product_bytes(down, (uint32_t)slots, 0)));
+    return at;
+}
+
+bool layer_ok(const dm_weights *up, const dm_weights *down, uint32_t tokens, uint32_t top_k) {
+    if (!weights_ok(up) || !weights_ok(down) || up->dtype != down->dtype || up->experts != down->experts) return false;
+    return up->n % 2 == 0 && down->k == up->n / 2 && down->n == up->k && choose_bytes(tokens, up->experts, top_k) != 0;
+}
+
+cudaError_t quantize(uint32_t dtype, const QuantizeArgs &p, cudaStream_t st) {
+    return dtype == DM_BF16 ? launch_quantize<__nv_bfloat16>(p, st) : launch_quantize<__half>(p, st);
+}
+
+}  // namespace
+}  // namespace dm
+
+extern "C" dm_status dm_products_last_error(uint32_t *status, void *stream) {
+    if (!status) return DM_ERR_INVALID_ARG;
+    const auto st = static_cast<cudaStream_t>(stream);
+    uint32_t e = 0;
+    if (cudaMemcpyAsync(&e, status, 4, cudaMemcpyDeviceToHost, st) != cudaSuccess || cudaStreamSynchronize(st) != cudaSuccess)
+        return DM_ERR_CUDA;
+    if (e && cudaMemsetAsync(status, 0, 4, st) != cudaSuccess) return DM_ERR_CUDA;
+    return static_cast<dm_status>(e);
+}
+
+extern "C" dm_status dm_quantize(const dm_quantize_args *a, void *stream) {
+    using namespace dm;
+    if (!a || a->dtype > DM_F16 || a->k < 1 || a->k > (1u << 24) || a->rows > 0x7FFFFFFFu || !(a->eps <= 3.4e38f)) return DM_ERR_INVALID_ARG;
+    if (a->rows == 0) return DM_OK;
+    if (!a->x || !a->q || !a->scale || !aligned(a->x, 16) || !aligned(a->q, 16) || !aligned(a->scale, 4) || !aligned(a->count, 4))
+        return DM_ERR_INVALID_ARG;
+    if (a->x_row % 8 || a->q_row % 16 || a->x_row > (1ull << 32) || a->q_row > (1ull << 32)) return DM_ERR_INVALID_ARG;
+    if (a->rows > 1 && (a->x_row < a->k || a->q_row < a->k)) return DM_ERR_INVALID_ARG;
+    return status_of(quantize(a->dtype, {static_cast<const char *>(a->x), a->q, a->scale, a->count, a->x_row, a->q_row, a->rows, a->k, a->eps},
+                              static_cast<cudaStream_t>(stream)));
+}
+
+extern "C" uint64_t dm_choose_bytes(uint32_t tokens, uint32_t experts, uint32_t top_k) { return dm::choose_bytes(tokens, experts, top_k); }
+
+extern "C" dm_status dm_choose_experts(const dm_choose_args *a, void *stream) {
+    using namespace dm;
+    if (!a || a->reserved0 || a->dtype > DM_F32 || a->dtype == DM_I8 || a->renormalize > 1) return DM_ERR_INVALID_ARG;
+    const uint64_t need = choose_bytes(a->tokens, a->experts, a->top_k);
+    if (!need || a->work_bytes < need || !a->work || !aligned(a->work, 16) || !a->offsets || !aligned(a->offsets, 4)) return DM_ERR_INVALID_ARG;
+    if (a->logits_row > (1ull << 32) || (a->tokens > 1 && a->logits_row < a->experts)) return DM_ERR_INVALID_ARG;
+    if (a->tokens && (!a->logits || !a->ids || !a->weights || !a->slots || !a->sources || !aligned(a->logits, dtype_size(a->dtype)) ||
+                      !aligned(a->ids, 4) || !aligned(a->weights, 4) || !aligned(a->slots, 4) || !aligned(a->sources, 4)))
+        return DM_ERR_INVALID_ARG;
+    ChooseArgs p{};
+    p.logits = static_cast<const char *>(a->logits), p.row = a->logits_row;
+    p.tokens = a->tokens, p.experts = a->experts, p.top_k = a->top_k, p.renormalize = a->renormalize;
+    p.ids = a->ids, p.weights = a->weights, p.offsets = a->offsets, p.slots = a->slots, p.sources = a->sources;
+    p.counts = static_cast<int32_t *>(a->work);
+    return status_of(choose(p, a->dtype, static_cast<cudaStream_t>(stream)));
+}
+
+extern "C" uint64_t dm_experts_bytes(const dm_weights *up, const dm_weights *down, uint32_t tokens, uint32_t top_k) {
+    using namespace dm;
+    LayerWork w;
+    return layer_ok(up, down, tokens, top_k) ? layer_work(up, down, tokens, top_k, nullptr, w) : 0;
+}
+
+extern "C" dm_status dm_experts(const dm_weights *up, const dm_weights *down, const dm_experts_args *a, void *stream) {
+    using namespace dm;
+    if (!a || a->reserved0 || a->renormalize > 1 || a->dtype > DM_F16 || a->logits_dtype > DM_F32 || a->logits_dtype == DM_I8)
+        return DM_ERR_INVALID_ARG;
+    if (!layer_ok(up, down, a->tokens, a->top_k) || !a->status) return DM_ERR_INVALID_ARG;
+    const bool eight = up->dtype == DM_I8;
+    if (!eight && up->dtype != a->dtype) return DM_ERR_INVALID_ARG;
+    LayerWork w;
+    if (!a->work || !aligned(a->work, 256) || a->work_bytes < layer_work(up, down, a->tokens, a->top_k, a->work, w)) return DM_ERR_INVALID_ARG;
+    if (a->tokens == 0) return DM_OK;
+    if (!a->x || !a->logits || !a->y || !aligned(a->x, 16) || !aligned(a->y, 16) || !aligned(a->residual, 16) ||
+        !aligned(a->logits, dtype_size(a->logits_dtype)))
+        return DM_ERR_INVALID_ARG;
+    if (a->x_row % 8 || a->y_row % 8 || a->residual_row % 8 || a->logits_row > (1ull << 32) || a->x_row > (1ull << 32) ||
+        a->y_row > (1ull << 32) || a->residual_row > (1ull << 32))
+        return DM_ERR_INVALID_ARG;
+    if (a->tokens > 1 && (a->x_row < up->k || a->y_row < up->k || a->logits_row < up->experts || (a->residual && a->residual_row < up->k)))
+        return DM_ERR_INVALID_ARG;
+    const auto st = static_cast<cudaStream_t>(stream);
+    const uint32_t slots = a->tokens * a->top_k;
+    ChooseArgs c{};
+    c.logits = static_cast<const char *>(a->logits), c.row = a->logits_row;
+    c.tokens = a->tokens, c.experts = up->experts, c.top_k = a->top_k, c.renormalize = a->renormalize;
+    c.ids = w.ids, c.weights = w.weights, c.offsets = w.offsets, c.slots = w.slots, c.sources = w.sources, c.counts = w.counts;
+    const auto layer = [&]() -> cudaError_t {
+        DM_TRY(choose(c, a->logits_dtype, st));
+        dm_product_args u{};
+        u.x = a->x, u.x_row = a->x_row, u.x_rows = a->tokens, u.sources = w.sources, u.per_source = a->top_k, u.offsets = w.offsets;
+        u.y = w.h, u.y_row = w.h_row, u.y_dtype = a->dtype, u.rows = slots, u.gated = 1, u.status = a->status;
+        if (eight) {
+            DM_TRY(quantize(a->dtype, {static_cast<const char *>(a->x), (int8_t *)w.xq, w.x_scale, nullptr, a->x_row, w.xq_row, a->tokens, up->k, -1.f}, st));
+            u.x = w.xq, u.x_row = w.xq_row, u.x_scale = w.x_scale;
+        }
+        DM_TRY(launch_product(up, product_args(up, &u), w.product, st));
+        dm_product_args d{};
+        d.x = w.h, d.x_row = w.h_row, d.x_rows = slots, d.offsets = w.offsets;
+        d.y = w.parts, d.y_row = w.parts_row, d.y_dtype = DM_F32, d.rows = slots, d.status = a->status;
+        if (eight) {
+            DM_TRY(quantize(a->dtype, {w.h, (int8_t *)w.hq, w.h_scale, w.offsets + up->experts, w.h_row, w.hq_row, slots, down->k, -1.f}, st));
+            d.x = w.hq, d.x_row = w.hq_row, d.x_scale = w.h_scale;
+        }
+        DM_TRY(launch_product(down, product_args(down, &d), w.product, st));
+        JoinArgs j{w.parts, w.slots, w.weights, static_cast<const char *>(a->residual), static_cast<char *>(a->y), a->status,
+                   w.parts_row, a->residual_row, a->y_row, a->tokens, a->top_k, up->k};
+        const uint64_t each = (uint64_t)a->tokens * ((up->k + 3) / 4);
+        const uint32_t grid = (uint32_t)std::min<uint64_t>((each + 255) / 256, (uint64_t)sm_count() * 8);
+        return a->dtype == DM_BF16 ? launch_pdl(k_join_experts<__nv_bfloat16>, grid, 256, 0, st, j) : launch_pdl(k_join_experts<__half>, grid, 256, 0, st, j);
+    };
+    return status_of(layer());
+}

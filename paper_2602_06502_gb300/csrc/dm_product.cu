@@ -1,0 +1,204 @@
+// dm_product.cu -- products of rows with 16-bit or 8-bit weights, of one
+// expert or of many (dm_product), and the kernel for few rows.
+#include <algorithm>
+
+#include "dm_product.cuh"
+
+namespace dm {
+namespace {
+
+// -- few rows ---------------------------------------------------------------------
+//
+// The weights' bytes are all there is to it: each is read once from memory and
+// used for at most 32 rows, so mma.sync's rate is enough and no weight goes
+// through shared memory.  The product's sum may be taken in any order, as long
+// as both operands agree on it: lane (g, t) of a warp loads 16 consecutive bytes
+// of channel g (and g + 8), and of row g, and what the tensor cores take for
+// their columns 2 t .. are the values that the lane has.  A warp's load is so 64
+// consecutive bytes of eight rows.
+//
+// A CTA has 16 channels (gated: and their 16 partners); its eight warps share
+// out k, 64 bytes at a time, and add their sums up in the order of the warps.
+
+constexpr uint32_t kFewT = 256, kFewWarps = 8;
+
+template <class T>
+struct Few;   // T: of the weights and rows
+template <>
+struct Few<__nv_bfloat16> {
+    static constexpr int kMmas = 2;
+    static __device__ __forceinline__ void operand(const uint4 &x, int i, uint32_t &lo, uint32_t &hi) { lo = i ? x.z : x.x, hi = i ? x.w : x.y; }
+    static __device__ __forceinline__ void mma(float *c, const uint32_t *a, uint32_t b0, uint32_t b1) {
+        asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
+                     : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3])
+                     : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
+    }
+};
+template <>
+struct Few<__half> {
+    static constexpr int kMmas = 2;
+    static __device__ __forceinline__ void operand(const uint4 &x, int i, uint32_t &lo, uint32_t &hi) { lo = i ? x.z : x.x, hi = i ? x.w : x.y; }
+    static __device__ __forceinline__ void mma(float *c, const uint32_t *a, uint32_t b0, uint32_t b1) {
+        asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
+                     : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3])
+                     : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
+    }
+};
+template <>
+struct Few<int8_t> {
+    static constexpr int kMmas = 4;
+    static __device__ __forceinline__ void operand(const uint4 &x, int i, uint32_t &lo, uint32_t &hi) {
+        bytes_to_halves(i == 0 ? x.x : i == 1 ? x.y : i == 2 ? x.z : x.w, lo, hi);
+    }
+    static __device__ __forceinline__ void mma(float *c, const uint32_t *a, uint32_t b0, uint32_t b1) { Few<__half>::mma(c, a, b0, b1); }
+};
+
+// 16 bytes of a row from byte `at` on; zeros from byte `end` on.
+__device__ __forceinline__ uint4 load16(const char *row, uint32_t at, uint32_t end) {
+    if (at >= end) return make_uint4(0, 0, 0, 0);
+    uint4 x = *reinterpret_cast<const uint4 *>(row + at);
+    if (end - at < 16) {
+        uint32_t *w = reinterpret_cast<uint32_t *>(&x);
+#pragma unroll
+        for (uint32_t i = 0; i < 4; ++i) {
+            const uint32_t left = end - at > 4 * i ? min(end - at - 4 * i, 4u) : 0;
+            w[i] = left == 4 ? w[i] : w[i] & ((1u << 8 * left) - 1);
+        }
+    }
+    return x;
+}
+
+// kTiles: 8-row tiles at a time; kM: 16-channel tiles (2: gated).
+template <class T, int kTiles, int kM>
+__global__ void __launch_bounds__(kFewT, 2) k_product_few(ProductArgs p) {
+    constexpr uint32_t kCols = 16 * kM + 4, kU = 4;
+    __shared__ float s_red[kFewWarps][8 * kTiles][kCols];
+    pdl_enter();
+    if (__syncthreads_or(has_err(p.status))) return;
+    const uint32_t tid = threadIdx.x, wid = tid >> 5, lane = tid & 31, g = lane >> 2, t = lane & 3;
+    const uint32_t e = blockIdx.y, c0 = blockIdx.x * 16;
+    const Rows rows = expert_rows(p, e);
+    const uint32_t end = p.k * (uint32_t)sizeof(T), chunks = (end + 63) / 64;
+    const char *w[kM][2];
+#pragma unroll
+    for (int m = 0; m < kM; ++m)
+#pragma unroll
+        for (int h = 0; h < 2; ++h) w[m][h] = p.w + e * p.w_expert + (m * (uint64_t)p.n + min(c0 + g + 8 * h, p.n - 1)) * p.w_row;
+    for (int32_t r0 = rows.a; r0 < rows.b; r0 += 8 * kTiles) {
+        const char *x[kTiles];
+#pragma unroll
+        for (int j = 0; j < kTiles; ++j) x[j] = p.x + source_row(p, (uint32_t)min(r0 + 8 * j + (int32_t)g, rows.b - 1)) * p.x_row;
+        float acc[kM][kTiles][4] = {};
+        for (uint32_t c = wid; c < chunks; c += kFewWarps * kU) {
+            uint4 wv[kU][kM][2], xv[kU][kTiles];
+#pragma unroll
+            for (uint32_t u = 0; u < kU; ++u) {
+                const uint32_t at = (c + kFewWarps * u) * 64 + t * 16;
+#pragma unroll
+                for (int m = 0; m < kM; ++m)
+#pragma unroll
+                    for (int h = 0; h < 2; ++h) wv[u][m][h] = load16(w[m][h], at, end);
+#pragma unroll
+                for (int j = 0; j < kTiles; ++j) xv[u][j] = load16(x[j], at, end);
+            }
+#pragma unroll
+            for (uint32_t u = 0; u < kU; ++u)
+#pragma unroll
+                for (int i = 0; i < Few<T>::kMmas; ++i) {
+                    uint32_t a[kM][4];
+#pragma unroll
+                    for (int m = 0; m < kM; ++m)
+#pragma unroll
+                        for (int h = 0; h < 2; ++h) Few<T>::operand(wv[u][m][h], i, a[m][h], a[m][2 + h]);
+#pragma unroll
+                    for (int j = 0; j < kTiles; ++j) {
+                        uint32_t b0, b1;
+                        Few<T>::operand(xv[u][j], i, b0, b1);
+#pragma unroll
+                        for (int m = 0; m < kM; ++m) Few<T>::mma(acc[m][j], a[m], b0, b1);
+                    }
+                }
+        }
+        __syncthreads();   // the sums before have been read
+#pragma unroll
+        for (int m = 0; m < kM; ++m)
+#pragma unroll
+            for (int j = 0; j < kTiles; ++j)
+#pragma unroll
+                for (int i = 0; i < 4; ++i) s_red[wid][8 * j + 2 * t + (i & 1)][16 * m + g + 8 * (i >> 1)] = acc[m][j][i];
+        __syncthreads();
+        for (uint32_t i = tid; i < 8 * kTiles * 16; i += kFewT) {
+            const uint32_t row = i / 16, ch = i % 16;
+            const int32_t r = r0 + (int32_t)row;
+            if (r >= rows.b || c0 + ch >= p.n) continue;
+            float z[kM] = {};
+#pragma unroll
+            for (uint32_t q = 0; q < kFewWarps; ++q)
+#pragma unroll
+                for (int m = 0; m < kM; ++m) z[m] += s_red[q][row][16 * m + ch];
+            if constexpr (sizeof(T) == 1) {
+                const float sx = p.x_scale[source_row(p, (uint32_t)r)];
+#pragma unroll
+                for (int m = 0; m < kM; ++m) z[m] *= sx * p.w_scale[(uint64_t)e * kM * p.n + m * p.n + c0 + ch];
+            }
+            store_y(p, (uint64_t)r * p.y_row + c0 + ch, kM == 2 ? gate(z[0], z[kM - 1]) : z[0]);
+        }
+    }
+}
+
+template <class T, int kTiles>
+cudaError_t launch_few_tiles(const ProductArgs &p, cudaStream_t st) {
+    const dim3 grid((p.n + 15) / 16, p.experts);
+    return p.gated ? launch_pdl(k_product_few<T, kTiles, 2>, grid, kFewT, 0, st, p) : launch_pdl(k_product_few<T, kTiles, 1>, grid, kFewT, 0, st, p);
+}
+
+template <class T>
+cudaError_t launch_few(const ProductArgs &p, cudaStream_t st) {
+    const uint32_t each = (p.rows + p.experts - 1) / p.experts;
+    return each <= 8 ? launch_few_tiles<T, 1>(p, st) : launch_few_tiles<T, 2>(p, st);
+}
+
+}  // namespace
+
+ProductArgs product_args(const dm_weights *w, const dm_product_args *a) {
+    ProductArgs p{};
+    const uint32_t size = dtype_size(w->dtype);
+    p.w = static_cast<const char *>(w->w), p.w_scale = w->scale, p.w_row = w->row * size, p.w_expert = w->expert * size;
+    p.experts = w->experts, p.k = w->k, p.n = a->gated ? w->n / 2 : w->n, p.gated = a->gated;
+    p.x = static_cast<const char *>(a->x), p.x_scale = a->x_scale, p.x_row = a->x_row * size;
+    p.y = a->y, p.y_row = a->y_row, p.y_dtype = a->y_dtype;
+    p.offsets = a->offsets, p.sources = a->sources, p.per = a->per_source, p.status = a->status;
+    p.rows = a->rows, p.x_rows = a->x_rows;
+    return p;
+}
+
+cudaError_t launch_product(const dm_weights *w, const ProductArgs &p, void *work, cudaStream_t st) {
+    if (w->dtype == DM_BF16) return launch_few<__nv_bfloat16>(p, st);
+    return w->dtype == DM_F16 ? launch_few<__half>(p, st) : launch_few<int8_t>(p, st);
+}
+
+}  // namespace dm
+
+extern "C" uint64_t dm_product_bytes(const dm_weights *w, uint32_t rows, uint32_t gated) {
+    using namespace dm;
+    if (!weights_ok(w) || rows > 0x7FFFFFFFu || gated > 1 || (gated && w->n % 2)) return 0;
+    return 256;
+}
+
+extern "C" dm_status dm_product(const dm_weights *w, const dm_product_args *a, void *stream) {
+    using namespace dm;
+    if (!a) return DM_ERR_INVALID_ARG;
+    const uint64_t need = dm_product_bytes(w, a->rows, a->gated);
+    if (!need || a->reserved0 || !a->status || a->work_bytes < need || !a->work || !aligned(a->work, 256)) return DM_ERR_INVALID_ARG;
+    const uint32_t size = dtype_size(w->dtype), n = a->gated ? w->n / 2 : w->n;
+    if (a->y_dtype > DM_F32 || a->y_dtype == DM_I8 || a->x_rows > 0x7FFFFFFFu) return DM_ERR_INVALID_ARG;
+    if (!a->offsets && w->experts != 1) return DM_ERR_INVALID_ARG;
+    if (a->sources ? a->per_source < 1 : a->x_rows < a->rows) return DM_ERR_INVALID_ARG;
+    if (a->rows == 0) return DM_OK;
+    if (a->x_rows == 0 || !a->x || !a->y || !aligned(a->x, 16) || !aligned(a->y, dtype_size(a->y_dtype))) return DM_ERR_INVALID_ARG;
+    if (a->x_row * size % 16 || a->x_row > (1ull << 32) || (a->x_rows > 1 && a->x_row < w->k)) return DM_ERR_INVALID_ARG;
+    if (a->y_row > (1ull << 32) || (a->rows > 1 && a->y_row < n)) return DM_ERR_INVALID_ARG;
+    if (w->dtype == DM_I8 && (!a->x_scale || !aligned(a->x_scale, 4))) return DM_ERR_INVALID_ARG;
+    if (!aligned(a->offsets, 4) || !aligned(a->sources, 4)) return DM_ERR_INVALID_ARG;
+    return status_of(launch_product(w, product_args(w, a), a->work, static_cast<cudaStream_t>(stream)));
+}

@@ -94,7 +94,7 @@ class dm_migration(C.Structure):
 
 
 # dm_dtype, dm_page_layout
-DM_BF16, DM_F16 = 0, 1
+DM_BF16, DM_F16, DM_I8, DM_F32 = 0, 1, 2, 3
 DM_PAGES_HEADS, DM_PAGES_TOKENS = 0, 1
 
 
@@ -129,6 +129,37 @@ class dm_attend_args(C.Structure):
     _fields_ = [("layer", C.c_uint32), ("scale", C.c_float)] + \
                [(name, C.c_void_p) for name in ("q", "o", "lse")] + \
                [(name, C.c_uint64) for name in ("q_token", "q_head", "o_token", "o_head")]
+
+
+class dm_weights(C.Structure):
+    _fields_ = [("w", C.c_void_p), ("scale", C.c_void_p)] + \
+               [(name, C.c_uint32) for name in ("dtype", "experts", "n", "k")] + \
+               [("row", C.c_uint64), ("expert", C.c_uint64)]
+
+
+class dm_quantize_args(C.Structure):
+    _fields_ = [(name, C.c_void_p) for name in ("x", "q", "scale", "count")] + \
+               [("x_row", C.c_uint64), ("q_row", C.c_uint64)] + \
+               [(name, C.c_uint32) for name in ("dtype", "rows", "k")] + [("eps", C.c_float)]
+
+
+class dm_choose_args(C.Structure):
+    _fields_ = [("logits", C.c_void_p), ("logits_row", C.c_uint64)] + \
+               [(name, C.c_uint32) for name in ("dtype", "tokens", "experts", "top_k", "renormalize", "reserved0")] + \
+               [(name, C.c_void_p) for name in ("ids", "weights", "offsets", "slots", "sources", "work")] + \
+               [("work_bytes", C.c_uint64)]
+
+
+class dm_product_args(C.Structure):
+    _fields_ = [(name, C.c_void_p) for name in ("x", "x_scale", "y", "offsets", "sources", "status", "work")] + \
+               [(name, C.c_uint64) for name in ("work_bytes", "x_row", "y_row")] + \
+               [(name, C.c_uint32) for name in ("rows", "x_rows", "per_source", "y_dtype", "gated", "reserved0")]
+
+
+class dm_experts_args(C.Structure):
+    _fields_ = [(name, C.c_void_p) for name in ("x", "logits", "residual", "y", "status", "work")] + \
+               [(name, C.c_uint64) for name in ("work_bytes", "x_row", "logits_row", "residual_row", "y_row")] + \
+               [(name, C.c_uint32) for name in ("dtype", "logits_dtype", "tokens", "top_k", "renormalize", "reserved0")]
 
 
 class DualMapError(RuntimeError):
@@ -184,6 +215,14 @@ SIGNATURES = {
     "dm_plan_bytes": (C.c_uint64, [C.POINTER(dm_cache), C.c_uint32, C.c_uint32, C.c_uint32, C.c_uint32]),
     "dm_cache_plan": (C.c_int, [C.POINTER(dm_cache), C.POINTER(dm_plan), C.c_void_p]),
     "dm_cache_attend": (C.c_int, [C.POINTER(dm_cache), C.POINTER(dm_plan), C.POINTER(dm_attend_args), C.c_void_p]),
+    "dm_products_last_error": (C.c_int, [C.c_void_p, C.c_void_p]),
+    "dm_quantize": (C.c_int, [C.POINTER(dm_quantize_args), C.c_void_p]),
+    "dm_choose_bytes": (C.c_uint64, [C.c_uint32, C.c_uint32, C.c_uint32]),
+    "dm_choose_experts": (C.c_int, [C.POINTER(dm_choose_args), C.c_void_p]),
+    "dm_product_bytes": (C.c_uint64, [C.POINTER(dm_weights), C.c_uint32, C.c_uint32]),
+    "dm_product": (C.c_int, [C.POINTER(dm_weights), C.POINTER(dm_product_args), C.c_void_p]),
+    "dm_experts_bytes": (C.c_uint64, [C.POINTER(dm_weights), C.POINTER(dm_weights), C.c_uint32, C.c_uint32]),
+    "dm_experts": (C.c_int, [C.POINTER(dm_weights), C.POINTER(dm_weights), C.POINTER(dm_experts_args), C.c_void_p]),
     "dm_test_fail_alloc": (None, [C.c_int64]),
     "dm_test_attend_wait": (C.c_int, [C.c_uint64]),
     "dm_last_error": (C.c_int, [C.c_void_p]),
@@ -432,6 +471,38 @@ def dm_cache_plan(c, plan, stream=None):
 
 def dm_cache_attend(c, plan, args, stream=None):
     return lib().dm_cache_attend(C.byref(c), C.byref(plan), C.byref(args), stream)
+
+
+def dm_products_last_error(status, stream=None):
+    return lib().dm_products_last_error(_ptr(status), stream)
+
+
+def dm_quantize(args, stream=None):
+    return lib().dm_quantize(C.byref(args), stream)
+
+
+def dm_choose_bytes(tokens, experts, top_k):
+    return lib().dm_choose_bytes(tokens, experts, top_k)
+
+
+def dm_choose_experts(args, stream=None):
+    return lib().dm_choose_experts(C.byref(args), stream)
+
+
+def dm_product_bytes(w, rows, gated=0):
+    return lib().dm_product_bytes(C.byref(w), rows, gated)
+
+
+def dm_product(w, args, stream=None):
+    return lib().dm_product(C.byref(w), C.byref(args), stream)
+
+
+def dm_experts_bytes(up, down, tokens, top_k):
+    return lib().dm_experts_bytes(C.byref(up), C.byref(down), tokens, top_k)
+
+
+def dm_experts(up, down, args, stream=None):
+    return lib().dm_experts(C.byref(up), C.byref(down), C.byref(args), stream)
 
 
 def dm_last_error(h):

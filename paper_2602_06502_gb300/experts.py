@@ -1,0 +1,286 @@
+"""An instance's projections and expert layers over torch tensors: products with
+16-bit weights or with 8-bit ones, of one set of weights or grouped by expert,
+the quantising of rows, the choice of experts, and the layer made of them
+(dm_quantize, dm_choose_experts, dm_product and dm_experts of include/dualmap.h).
+
+Only marshalling: it checks shapes and types, allocates outputs and work
+buffers on the device, and enqueues the C calls on torch's current stream of
+the inputs' device.  A call's work buffer is its own, so calls on one set of
+weights may overlap.  The calls serve: they give no gradients, so with grad mode
+on they refuse tensors that want one.
+
+A matrix's last dimension is contiguous and its rows begin on 16 bytes: a width
+that is no multiple of 16 bytes lies in wider rows (x = buffer[:, :k]).
+"""
+
+import ctypes as C
+
+import torch
+
+from . import dualmap as D
+
+TYPES = {torch.bfloat16: D.DM_BF16, torch.float16: D.DM_F16}
+SCORES = {torch.bfloat16: D.DM_BF16, torch.float16: D.DM_F16, torch.float32: D.DM_F32}
+_sizes = {}   # of work buffers, by device and shape
+
+
+def _size(name, device, key, *args):
+    """What the C call `name` answers for a work buffer on `device`; key: what it depends on."""
+    at = (name, device, key)
+    size = _sizes.get(at)
+    if size is None:
+        with torch.cuda.device(device):   # it depends on the device's SMs
+            size = getattr(D.lib(), name)(*args)
+        if not size:
+            raise D.DualMapError(D.DM_ERR_INVALID_ARG, name)
+        if len(_sizes) > 4096:
+            _sizes.clear()
+        _sizes[at] = size
+    return size
+
+
+def _call(name, device, *args):
+    """Enqueues a C call on torch's current stream of the device."""
+    if torch.cuda.current_device() != device.index:
+        with torch.cuda.device(device):
+            return _call(name, device, *args)
+    rc = getattr(D.lib(), name)(*args, torch._C._cuda_getCurrentRawStream(device.index))
+    if rc:
+        raise D.DualMapError(rc, name)
+
+
+def _cuda(name, x):
+    if x.device.type != "cuda":
+        raise ValueError(f"{name}: a CUDA tensor wanted")
+    return x.device
+
+
+def _matrix(name, x, dtypes, device, shape=(None, None)):
+    """(address, distance of rows) of a matrix."""
+    if x.dim() != 2 or x.dtype not in dtypes or x.device != device or any(w is not None and n != w for n, w in zip(x.shape, shape)):
+        raise ValueError(f"{name}: a matrix of shape {shape} on {device}, of one of the types {list(dtypes)}")
+    row, one = x.stride()
+    if x.shape[1] > 1 and one != 1:
+        raise ValueError(f"{name}: its last dimension is contiguous")
+    if x.requires_grad and torch.is_grad_enabled():
+        raise ValueError(f"{name} requires grad, and this call gives no gradients: use torch.no_grad() or detach it")
+    if x.shape[0] <= 1:   # the stride of a dimension of one element says nothing
+        row = 0
+    elif row < x.shape[1]:
+        raise ValueError(f"{name}: its rows lie one after another")
+    return x.data_ptr(), row
+
+
+def _vector(name, x, dtype, device, n):
+    if x.dtype is not dtype or x.shape != (n,) or x.device != device or not x.is_contiguous():
+        raise ValueError(f"{name}: contiguous {dtype} of length {n} on {device}")
+    if x.requires_grad and torch.is_grad_enabled():
+        raise ValueError(f"{name} requires grad, and this call gives no gradients: use torch.no_grad() or detach it")
+    return x.data_ptr()
+
+
+def quantize(x, *, eps=None, count=None):
+    """(q, scale): the rows of x [rows, k], bfloat16 or float16, in 8 bits: q
+    int8 [rows, k] = 127 x / max |x| rounded, scale float32 [rows].  eps: rows
+    are first divided by the root of their mean square plus eps.  count: an
+    int32 tensor of one element, the number of rows that there are."""
+    device = _cuda("x", x)
+    xp, row = _matrix("x", x, TYPES, device)
+    rows, k = x.shape
+    q = torch.empty(rows, -(-k // 16) * 16, dtype=torch.int8, device=device)[:, :k]
+    scale = torch.empty(rows, dtype=torch.float32, device=device)
+    if eps is not None and not eps >= 0:
+        raise ValueError("eps is not negative")
+    a = D.dm_quantize_args(xp, q.data_ptr(), scale.data_ptr(), None if count is None else _vector("count", count, torch.int32, device, 1),
+                           row, q.stride(0), TYPES[x.dtype], rows, k, -1.0 if eps is None else eps)
+    _call("dm_quantize", device, C.byref(a))
+    return q, scale
+
+
+class Weights:
+    """Weights of a product, w [n, k], or of many experts', [experts, n, k]:
+    bfloat16 or float16, or int8 with scale float32 [(experts,) n].  Keeps the
+    tensors; calls that fail on the device say so in last_error()."""
+
+    def __init__(self, w, scale=None):
+        if w.dim() not in (2, 3) or w.numel() == 0 or w.shape[-1] > 1 and w.stride(-1) != 1:
+            raise ValueError("weights are [n, k] or [experts, n, k], not empty, the last dimension contiguous")
+        if (w.dtype is torch.int8) != (scale is not None) or (scale is None and w.dtype not in TYPES):
+            raise ValueError("weights are bfloat16 or float16, or int8 with a scale")
+        self.device = _cuda("w", w)
+        for name, x in (("w", w), ("scale", scale)):
+            if x is not None and x.requires_grad:
+                raise ValueError(f"{name} requires grad, and products give no gradients: detach it")
+        if scale is not None and (scale.dtype is not torch.float32 or scale.shape != w.shape[:-1] or not scale.is_contiguous() or
+                                  scale.device != w.device):
+            raise ValueError(f"scale: contiguous float32 of shape {tuple(w.shape[:-1])} on {w.device}")
+        self.w, self.scale, self.dtype, self.grouped = w, scale, w.dtype, w.dim() == 3
+        self.experts = w.shape[0] if self.grouped else 1
+        self.n, self.k = w.shape[-2:]
+        step = 16 // w.element_size()
+        row = w.stride(-2) if self.n > 1 else -(-self.k // step) * step
+        self.struct = D.dm_weights(w.data_ptr(), None if scale is None else scale.data_ptr(),
+                                   D.DM_I8 if scale is not None else TYPES[w.dtype], self.experts, self.n, self.k, row,
+                                   w.stride(0) if self.experts > 1 else 0)
+        self.ref, self.key = C.byref(self.struct), (w.dtype, self.experts, self.n, self.k)
+        self.status = torch.zeros(1, dtype=torch.int32, device=self.device)
+        self._streams = set()   # whose work may still use the weights
+        _size("dm_product_bytes", self.device, (self.key, 0, 0), self.ref, 0, 0)   # refuses what is no set of weights
+
+    @classmethod
+    def quantized(cls, w):
+        """8-bit weights, a scale a channel, of bfloat16 or float16 ones."""
+        q, scale = quantize(w.detach().flatten(0, -2))
+        if w.dim() == 3:
+            q, scale = q.unflatten(0, w.shape[:2]), scale.unflatten(0, w.shape[:2])
+        return cls(q, scale)
+
+    def last_error(self):
+        """The status of the first product that failed on the device, which it clears (synchronises)."""
+        with torch.cuda.device(self.device):
+            return D.dm_products_last_error(self.status, torch._C._cuda_getCurrentRawStream(self.device.index))
+
+    def hold(self):
+        """Keeps the memory, once it is dropped, from being given out before the
+        current stream is done with it (once per stream)."""
+        raw = torch._C._cuda_getCurrentRawStream(self.device.index)
+        if raw not in self._streams:
+            stream = torch.cuda.current_stream(self.device)
+            for x in (self.w, self.scale, self.status):
+                if x is not None:
+                    x.record_stream(stream)
+            self._streams.add(raw)
+
+
+def product(x, weights, offsets=None, *, x_scale=None, sources=None, per_source=1, gated=False, rows=None, out=None, dtype=None):
+    """Rows times their expert's weights: y [rows, n], or [rows, n / 2] where
+    gated: silu of the first half of the channels times the second.
+
+    x [x_rows, k] of the weights' type; int8 with x_scale float32 [x_rows].
+    offsets: int32 [experts + 1], expert e has rows offsets[e] .. offsets[e +
+    1]; without it one expert has them all.  sources: int32 [rows], row r reads
+    row sources[r] // per_source of x.  out: where y goes, [rows, n] of bfloat16,
+    float16 or float32; rows outside the offsets stay as they were (in a new
+    output: whatever memory held).  dtype: of a new output (default: x's, for int8
+    bfloat16)."""
+    w, device = weights, weights.device
+    xp, x_row = _matrix("x", x, (w.dtype,), device, (None, w.k))
+    if (x_scale is None) != (w.scale is None):
+        raise ValueError("x_scale comes with int8 weights")
+    sp = None if x_scale is None else _vector("x_scale", x_scale, torch.float32, device, x.shape[0])
+    if offsets is None and w.experts > 1:
+        raise ValueError("products of many experts want offsets")
+    op = None if offsets is None else _vector("offsets", offsets, torch.int32, device, w.experts + 1)
+    n = x.shape[0] if sources is None else sources.shape[0]
+    if gated and w.n % 2:
+        raise ValueError("a gated product has an even number of channels")
+    if per_source < 1:
+        raise ValueError("per_source is at least 1")
+    width = w.n // 2 if gated else w.n
+    if out is None:
+        out = torch.empty(n, width, dtype=dtype or (torch.bfloat16 if w.scale is not None else w.dtype), device=device)
+    yp, y_row = _matrix("out", out, SCORES, device, (n, width))
+    size = _size("dm_product_bytes", device, (w.key, n, gated), w.ref, n, int(gated))
+    w.hold()
+    work = torch.empty(size, dtype=torch.uint8, device=device)
+    a = D.dm_product_args(xp, sp, yp, op, None if sources is None else _vector("sources", sources, torch.int32, device, n),
+                          w.status.data_ptr(), work.data_ptr(), size, x_row, y_row, n, x.shape[0], per_source, SCORES[out.dtype], gated, 0)
+    _call("dm_product", device, w.ref, C.byref(a))
+    return out
+
+
+class Choice:
+    """The experts of a batch's tokens (choose)."""
+
+    def __init__(self, ids, weights, offsets, slots, sources):
+        self.ids, self.weights, self.offsets, self.slots, self.sources = ids, weights, offsets, slots, sources
+
+
+def choose(logits, top_k, *, renormalize=True):
+    """The top_k experts of each row of logits [tokens, experts], bfloat16,
+    float16 or float32, ties to the lowest id; a Choice of ids int32 [tokens,
+    top_k], weights float32 [tokens, top_k] (softmax over the chosen, or over
+    all where not renormalize), and the pairs sorted by expert: offsets int32
+    [experts + 1], slots int32 [tokens, top_k] (pair -> slot) and sources int32
+    [tokens * top_k] (slot -> pair, token * top_k + place).  An expert with a
+    score of minus infinity is not chosen: id and slot -1, weight 0."""
+    device = _cuda("logits", logits)
+    xp, row = _matrix("logits", logits, SCORES, device)
+    tokens, experts = logits.shape
+    size = _size("dm_choose_bytes", device, (tokens, experts, top_k), tokens, experts, top_k)
+    ints = dict(dtype=torch.int32, device=device)
+    ids, slots = torch.empty(2, tokens, top_k, **ints)
+    weights = torch.empty(tokens, top_k, dtype=torch.float32, device=device)
+    offsets, sources = torch.empty(experts + 1, **ints), torch.empty(tokens * top_k, **ints)
+    work = torch.empty(size, dtype=torch.uint8, device=device)
+    a = D.dm_choose_args(xp, row, SCORES[logits.dtype], tokens, experts, top_k, bool(renormalize), 0, ids.data_ptr(),
+                         weights.data_ptr(), offsets.data_ptr(), slots.data_ptr(), sources.data_ptr(), work.data_ptr(), size)
+    _call("dm_choose_experts", device, C.byref(a))
+    return Choice(ids, weights, offsets, slots, sources)
+
+
+class Linear:
+    """y = x w^T for one set of weights; with 8-bit weights the rows are
+    quantised first."""
+
+    def __init__(self, weights):
+        if weights.grouped:
+            raise ValueError("a projection has one set of weights [n, k]")
+        self.weights = weights
+
+    def __call__(self, x, *, eps=None, out=None):
+        """x [rows, k], bfloat16 or float16; y of x's type, or out.  eps (8-bit
+        weights): rows are first divided by the root of their mean square plus
+        eps, which costs nothing here."""
+        w = self.weights
+        if w.scale is None:
+            if eps is not None:
+                raise ValueError("a norm comes with int8 weights")
+            return product(x, w, out=out)
+        q, scale = quantize(x, eps=eps)
+        return product(q, w, x_scale=scale, out=out, dtype=x.dtype)
+
+    def last_error(self):
+        return self.weights.last_error()
+
+
+class Experts:
+    """A layer of experts, each down(silu(g) u) with (g, u) = up(x): up [experts,
+    2 m, k] and down [experts, k, m], both 16-bit or both int8."""
+
+    def __init__(self, up, down, top_k, *, renormalize=True):
+        if not up.grouped or not down.grouped or up.device != down.device or up.dtype is not down.dtype:
+            raise ValueError("up and down are experts' weights of one type on one device")
+        if up.experts != down.experts or up.n != 2 * down.k or down.n != up.k:
+            raise ValueError("up is [experts, 2 m, k] and down [experts, k, m]")
+        if not 1 <= top_k <= min(up.experts, 32):
+            raise ValueError("top_k is 1 to the number of experts, and at most 32")
+        self.up, self.down, self.top_k, self.renormalize = up, down, top_k, bool(renormalize)
+        self.key = up.key, down.key, top_k
+
+    def __call__(self, x, logits, *, residual=None, out=None):
+        """y [tokens, k] = residual + the sum over each token's top_k experts by
+        logits [tokens, experts] of weight times expert(x [tokens, k]).  out may
+        be residual, and overlaps nothing else."""
+        up, device, tokens = self.up, self.up.device, x.shape[0]
+        types = TYPES if up.scale is not None else (up.dtype,)
+        xp, x_row = _matrix("x", x, types, device, (None, up.k))
+        lp, l_row = _matrix("logits", logits, SCORES, device, (tokens, up.experts))
+        if out is None:
+            out = torch.empty(tokens, -(-up.k // 8) * 8, dtype=x.dtype, device=device)
+            if out.shape[1] != up.k:
+                out = out[:, :up.k]
+        yp, y_row = _matrix("out", out, (x.dtype,), device, (tokens, up.k))
+        rp, r_row = (None, 0) if residual is None else _matrix("residual", residual, (x.dtype,), device, (tokens, up.k))
+        size = _size("dm_experts_bytes", device, (self.key, tokens), up.ref, self.down.ref, tokens, self.top_k)
+        up.hold()
+        self.down.hold()
+        work = torch.empty(size, dtype=torch.uint8, device=device)
+        a = D.dm_experts_args(xp, lp, rp, yp, up.status.data_ptr(), work.data_ptr(), size, x_row, l_row, r_row, y_row,
+                              TYPES[x.dtype], SCORES[logits.dtype], tokens, self.top_k, self.renormalize, 0)
+        _call("dm_experts", device, up.ref, self.down.ref, C.byref(a))
+        return out
+
+    def last_error(self):
+        """The status of the first call that failed on the device, which it clears (synchronises)."""
+        return self.up.last_error()
