@@ -805,22 +805,6 @@ __global__ void __launch_bounds__(256, kCtas) k_attend_join(AttendArgs p) {
 
 // -- launches -----------------------------------------------------------------------------
 
-using EncodeTiled = CUresult (*)(CUtensorMap *, CUtensorMapDataType, cuuint32_t, void *, const cuuint64_t *, const cuuint64_t *,
-                                 const cuuint32_t *, const cuuint32_t *, CUtensorMapInterleave, CUtensorMapSwizzle,
-                                 CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
-
-EncodeTiled encode_tiled() {
-    static const EncodeTiled f = [] {
-        void *fn = nullptr;
-        cudaDriverEntryPointQueryResult q;
-        if (cudaGetDriverEntryPointByVersion("cuTensorMapEncodeTiled", &fn, 12000, cudaEnableDefault, &q) != cudaSuccess ||
-            q != cudaDriverEntryPointSuccess)
-            return EncodeTiled(nullptr);
-        return reinterpret_cast<EncodeTiled>(fn);
-    }();
-    return f;
-}
-
 // A pool's pages of one layer as (dim, token, head, page); a box is 64 dims of
 // `box` tokens.
 bool page_map(CUtensorMap *m, const dm_cache *c, void *pool, uint32_t layer, uint32_t box) {

@@ -18,9 +18,8 @@
 // so `first row + 256 CTA` (16 for narrow) is a place of its own for each.
 #pragma once
 
-#include <cuda.h>
-
 #include "dm_cache.cuh"
+#include "dm_tensor.cuh"
 
 namespace dm {
 
@@ -291,55 +290,13 @@ __device__ __forceinline__ int32_t row_limit(const AttendBlock &k, uint32_t toke
     return min(k.kv1, k.pos + (int32_t)token + 1);
 }
 
-__device__ __forceinline__ uint32_t smem_addr(const void *p) { return (uint32_t)__cvta_generic_to_shared(p); }
-
 __device__ __forceinline__ float exp2_(float x) {
     float y;
     asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
     return y;
 }
 
-// -- mbarriers and TMA ---------------------------------------------------------
-
-__device__ __forceinline__ void mbar_init(uint32_t bar, uint32_t count) {
-    asm volatile("mbarrier.init.shared::cta.b64 [%0], %1;" ::"r"(bar), "r"(count) : "memory");
-}
-__device__ __forceinline__ void mbar_arrive(uint32_t bar) {
-    asm volatile("mbarrier.arrive.shared::cta.b64 _, [%0];" ::"r"(bar) : "memory");
-}
-__device__ __forceinline__ void mbar_expect(uint32_t bar, uint32_t bytes) {
-    asm volatile("mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], %1;" ::"r"(bar), "r"(bytes) : "memory");
-}
-__device__ __forceinline__ bool mbar_try(uint32_t bar, uint32_t parity) {
-    uint32_t ok;
-    asm volatile(
-        "{\n\t.reg .pred p;\n\t"
-        "mbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2;\n\t"
-        "selp.u32 %0, 1, 0, p;\n\t}"
-        : "=r"(ok)
-        : "r"(bar), "r"(parity)
-        : "memory");
-    return ok != 0;
-}
-__device__ __forceinline__ uint64_t now_ns() {
-    uint64_t t;
-    asm volatile("mov.u64 %0, %globaltimer;" : "=l"(t));
-    return t;
-}
-constexpr uint32_t kWaits = 1u << 24;
-constexpr uint64_t kWaitNs = 2'000'000'000;
-// Waits for the phase, at most `ns` and kWaits tries.
-__device__ __forceinline__ bool mbar_drain(uint32_t bar, uint32_t parity, const volatile uint32_t *gave_up = nullptr, uint64_t ns = kWaitNs) {
-    if (mbar_try(bar, parity)) return true;
-    const uint64_t t0 = now_ns();
-    for (uint32_t i = 0; i < kWaits; ++i) {
-        if (mbar_try(bar, parity)) return true;
-        if (gave_up && *gave_up) return true;
-        if ((i & 63) == 63 && now_ns() - t0 > ns) break;
-    }
-    return false;
-}
-// The same by a whole warp; a wait that gives up says so in `gave_up` (shared
+// mbar_drain by a whole warp; a wait that gives up says so in `gave_up` (shared
 // memory), and the CTA's others then return at once.  The caller goes on
 // either way: every loop is as long as its data says, so the CTA ends.
 __device__ __forceinline__ void mbar_wait(uint32_t bar, uint32_t parity, volatile uint32_t *gave_up, const AttendArgs &p) {
@@ -352,13 +309,6 @@ __device__ __forceinline__ void mbar_wait(uint32_t bar, uint32_t parity, volatil
         set_err(p.status, DM_ERR_TIMEOUT);
     }
     __syncwarp();
-}
-
-__device__ __forceinline__ void tma_load4(uint32_t dst, const CUtensorMap *map, uint32_t bar, int c0, int c1, int c2, int c3) {
-    asm volatile(
-        "cp.async.bulk.tensor.4d.shared::cta.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%3, %4, %5, %6}], [%2];" ::"r"(dst),
-        "l"(map), "r"(bar), "r"(c0), "r"(c1), "r"(c2), "r"(c3)
-        : "memory");
 }
 
 // Key rows tok .. tok + keys of a sequence into shared memory, as D / 64 halves
