@@ -863,8 +863,8 @@ typedef struct {
 } dm_product_args;
 
 /* Size of dm_product_args.work on the current device (it depends on its SMs);
- * 0 for an invalid shape. */
-DM_API uint64_t dm_product_bytes(const dm_weights *w, uint32_t rows, uint32_t gated);
+ * gathered: 1 where the rows have sources.  0 for an invalid shape. */
+DM_API uint64_t dm_product_bytes(const dm_weights *w, uint32_t rows, uint32_t gated, uint32_t gathered);
 
 /* y[r, c] = sum over j of x[r, j] w[e, c, j], times x_scale[r] scale[e, c] for
  * 8-bit weights; gated: y[r, c] = silu(z[r, c]) z[r, n/2 + c] of that z, with
@@ -879,12 +879,12 @@ DM_API dm_status dm_product(const dm_weights *w, const dm_product_args *a, void 
 typedef struct {
     const void *x;            /* tokens x k, DM_BF16 or DM_F16 */
     const void *logits;       /* as dm_choose_args */
-    const void *residual;     /* tokens x k of x's type, or NULL */
-    void *y;                  /* tokens x k of x's type; may be residual, and overlap nothing else */
+    const void *residual;     /* tokens x k of x's type, any alignment of it; or NULL */
+    void *y;                  /* the same; may be residual, and overlap nothing else */
     uint32_t *status;
     void *work;               /* dm_experts_bytes bytes, 256-byte aligned */
     uint64_t work_bytes;
-    uint64_t x_row, logits_row, residual_row, y_row;   /* elements; but for the logits' multiples of 16 bytes */
+    uint64_t x_row, logits_row, residual_row, y_row;   /* elements; x_row a multiple of 16 bytes */
     uint32_t dtype, logits_dtype;
     uint32_t tokens, top_k, renormalize;
     uint32_t reserved0;       /* must be 0 */

@@ -22,7 +22,8 @@ BUILD_DEBUG = os.path.join(ROOT, "_build", "dualmap_debug")
 LIB_DEBUG = os.path.join(HERE, "libdualmap_debug.so")
 SOURCES = ["dm_api.cu", "dm_setup.cu", "dm_hash.cu", "dm_route.cu", "dm_choice.cu", "dm_commit.cu",
            "dm_rebalance.cu", "dm_ring.cu", "dm_noalloc.cu", "dm_potc.cu", "dm_pages.cu", "dm_append.cu",
-           "dm_attend.cu", "dm_attend_wide.cu", "dm_product.cu", "dm_experts.cu"]
+           "dm_attend.cu", "dm_attend_wide.cu", "dm_product.cu", "dm_product_wide.cu",
+           "dm_experts.cu"]
 ARCH = ["-gencode", "arch=compute_103a,code=sm_103a"]
 FLAGS = ["-O3", "-lineinfo", "-std=c++17", "-Xcompiler", "-fPIC", "-Xcompiler", "-fvisibility=hidden",
          "--expt-relaxed-constexpr", "-I", os.path.join(ROOT, "include")]

@@ -423,6 +423,7 @@ struct JoinArgs {
     uint32_t *status;
     uint64_t pitch, residual_row, y_row;   // elements
     uint32_t tokens, top_k, k;
+    uint32_t words;   // rows of residual and y begin on 8 bytes
 };
 
 // 4 channels a thread, the parts in the order of the choice.  Bound: memory, 4
@@ -436,8 +437,13 @@ __global__ void __launch_bounds__(256) k_join_experts(JoinArgs p) {
         const uint32_t token = (uint32_t)(i / each), at = (uint32_t)(i % each) * 4, n = min(p.k - at, 4u);
         float y[4] = {};
         const T *from = reinterpret_cast<const T *>(p.residual) + token * p.residual_row + at;
-        if (p.residual)
+        if (p.residual && n == 4 && p.words) {
+            const uint2 x = *reinterpret_cast<const uint2 *>(from);
+            const float2 lo = Two<T>::up(*reinterpret_cast<const typename Two<T>::type *>(&x.x)), hi = Two<T>::up(*reinterpret_cast<const typename Two<T>::type *>(&x.y));
+            y[0] = lo.x, y[1] = lo.y, y[2] = hi.x, y[3] = hi.y;
+        } else if (p.residual) {
             for (uint32_t j = 0; j < n; ++j) y[j] = score_at(from + j);
+        }
         for (uint32_t j = 0; j < p.top_k; ++j) {
             const int32_t slot = __ldcg(p.slots + token * p.top_k + j);
             if (slot < 0) continue;
@@ -449,7 +455,7 @@ __global__ void __launch_bounds__(256) k_join_experts(JoinArgs p) {
             y[3] += w * x.w;
         }
         T *to = reinterpret_cast<T *>(p.y) + token * p.y_row + at;
-        if (n == 4) {
+        if (n == 4 && p.words) {
             const auto a = Two<T>::down(y[0], y[1]), b = Two<T>::down(y[2], y[3]);
             *reinterpret_cast<uint2 *>(to) = make_uint2(*reinterpret_cast<const uint32_t *>(&a), *reinterpret_cast<const uint32_t *>(&b));
         } else {
@@ -490,7 +496,7 @@ uint64_t layer_work(const dm_weights *up, const dm_weights *down, uint32_t token
     w.x_scale = (float *)take(eight ? 4ull * tokens : 0);
     w.hq = take(eight ? slots * w.hq_row : 0);
     w.h_scale = (float *)take(eight ? 4 * slots : 0);
-    w.product = take(std::max(dm_product_bytes(up, (uint32_t)slots, 1), dm_product_bytes(down, (uint32_t)slots, 0)));
+    w.product = take(std::max(dm_product_bytes(up, (uint32_t)slots, 1, 1), dm_product_bytes(down, (uint32_t)slots, 0, 0)));
     return at;
 }
 
@@ -563,10 +569,10 @@ extern "C" dm_status dm_experts(const dm_weights *up, const dm_weights *down, co
     LayerWork w;
     if (!a->work || !aligned(a->work, 256) || a->work_bytes < layer_work(up, down, a->tokens, a->top_k, a->work, w)) return DM_ERR_INVALID_ARG;
     if (a->tokens == 0) return DM_OK;
-    if (!a->x || !a->logits || !a->y || !aligned(a->x, 16) || !aligned(a->y, 16) || !aligned(a->residual, 16) ||
+    if (!a->x || !a->logits || !a->y || !aligned(a->x, 16) || !aligned(a->y, 2) || !aligned(a->residual, 2) ||
         !aligned(a->logits, dtype_size(a->logits_dtype)))
         return DM_ERR_INVALID_ARG;
-    if (a->x_row % 8 || a->y_row % 8 || a->residual_row % 8 || a->logits_row > (1ull << 32) || a->x_row > (1ull << 32) ||
+    if (a->x_row % 8 || a->logits_row > (1ull << 32) || a->x_row > (1ull << 32) ||
         a->y_row > (1ull << 32) || a->residual_row > (1ull << 32))
         return DM_ERR_INVALID_ARG;
     if (a->tokens > 1 && (a->x_row < up->k || a->y_row < up->k || a->logits_row < up->experts || (a->residual && a->residual_row < up->k)))
@@ -596,7 +602,8 @@ extern "C" dm_status dm_experts(const dm_weights *up, const dm_weights *down, co
         }
         DM_TRY(launch_product(down, product_args(down, &d), w.product, st));
         JoinArgs j{w.parts, w.slots, w.weights, static_cast<const char *>(a->residual), static_cast<char *>(a->y), a->status,
-                   w.parts_row, a->residual_row, a->y_row, a->tokens, a->top_k, up->k};
+                   w.parts_row, a->residual_row, a->y_row, a->tokens, a->top_k, up->k,
+                   aligned(a->residual, 8) && aligned(a->y, 8) && (a->residual_row | a->y_row) % 4 == 0};
         const uint64_t each = (uint64_t)a->tokens * ((up->k + 3) / 4);
         const uint32_t grid = (uint32_t)std::min<uint64_t>((each + 255) / 256, (uint64_t)sm_count() * 8);
         return a->dtype == DM_BF16 ? launch_pdl(k_join_experts<__nv_bfloat16>, grid, 256, 0, st, j) : launch_pdl(k_join_experts<__half>, grid, 256, 0, st, j);

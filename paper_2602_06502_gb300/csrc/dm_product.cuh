@@ -81,6 +81,16 @@ inline bool weights_ok(const dm_weights *w) {
     return w->experts == 1 || w->expert >= (w->n - 1) * w->row + w->k;
 }
 
+// How the kernel for many rows takes a product: tiles across the channels,
+// parts of k and the stages they share out, and its work buffer: rows laid out
+// for it, then the parts' sums.
+struct WideShape {
+    uint32_t blocks, splits, steps;
+    uint64_t x_row, x_bytes, part_bytes;
+};
+WideShape wide_shape(const dm_weights *w, uint32_t rows, uint32_t gated, bool gathered);
+cudaError_t launch_product_wide(const dm_weights *w, const ProductArgs &p, const WideShape &s, void *work, cudaStream_t st);
+
 // A product of the layer's own, whose arguments are known to be right.
 cudaError_t launch_product(const dm_weights *w, const ProductArgs &p, void *work, cudaStream_t st);
 ProductArgs product_args(const dm_weights *w, const dm_product_args *a);

@@ -219,7 +219,7 @@ SIGNATURES = {
     "dm_quantize": (C.c_int, [C.POINTER(dm_quantize_args), C.c_void_p]),
     "dm_choose_bytes": (C.c_uint64, [C.c_uint32, C.c_uint32, C.c_uint32]),
     "dm_choose_experts": (C.c_int, [C.POINTER(dm_choose_args), C.c_void_p]),
-    "dm_product_bytes": (C.c_uint64, [C.POINTER(dm_weights), C.c_uint32, C.c_uint32]),
+    "dm_product_bytes": (C.c_uint64, [C.POINTER(dm_weights), C.c_uint32, C.c_uint32, C.c_uint32]),
     "dm_product": (C.c_int, [C.POINTER(dm_weights), C.POINTER(dm_product_args), C.c_void_p]),
     "dm_experts_bytes": (C.c_uint64, [C.POINTER(dm_weights), C.POINTER(dm_weights), C.c_uint32, C.c_uint32]),
     "dm_experts": (C.c_int, [C.POINTER(dm_weights), C.POINTER(dm_weights), C.POINTER(dm_experts_args), C.c_void_p]),
@@ -489,8 +489,8 @@ def dm_choose_experts(args, stream=None):
     return lib().dm_choose_experts(C.byref(args), stream)
 
 
-def dm_product_bytes(w, rows, gated=0):
-    return lib().dm_product_bytes(C.byref(w), rows, gated)
+def dm_product_bytes(w, rows, gated=0, gathered=0):
+    return lib().dm_product_bytes(C.byref(w), rows, gated, gathered)
 
 
 def dm_product(w, args, stream=None):

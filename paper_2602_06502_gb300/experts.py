@@ -125,7 +125,7 @@ class Weights:
         self.ref, self.key = C.byref(self.struct), (w.dtype, self.experts, self.n, self.k)
         self.status = torch.zeros(1, dtype=torch.int32, device=self.device)
         self._streams = set()   # whose work may still use the weights
-        _size("dm_product_bytes", self.device, (self.key, 0, 0), self.ref, 0, 0)   # refuses what is no set of weights
+        _size("dm_product_bytes", self.device, (self.key, 0, 0, 0), self.ref, 0, 0, 0)   # refuses what is no set of weights
 
     @classmethod
     def quantized(cls, w):
@@ -180,7 +180,8 @@ def product(x, weights, offsets=None, *, x_scale=None, sources=None, per_source=
     if out is None:
         out = torch.empty(n, width, dtype=dtype or (torch.bfloat16 if w.scale is not None else w.dtype), device=device)
     yp, y_row = _matrix("out", out, SCORES, device, (n, width))
-    size = _size("dm_product_bytes", device, (w.key, n, gated), w.ref, n, int(gated))
+    gathered = sources is not None
+    size = _size("dm_product_bytes", device, (w.key, n, gated, gathered), w.ref, n, int(gated), int(gathered))
     w.hold()
     work = torch.empty(size, dtype=torch.uint8, device=device)
     a = D.dm_product_args(xp, sp, yp, op, None if sources is None else _vector("sources", sources, torch.int32, device, n),
@@ -267,9 +268,7 @@ class Experts:
         xp, x_row = _matrix("x", x, types, device, (None, up.k))
         lp, l_row = _matrix("logits", logits, SCORES, device, (tokens, up.experts))
         if out is None:
-            out = torch.empty(tokens, -(-up.k // 8) * 8, dtype=x.dtype, device=device)
-            if out.shape[1] != up.k:
-                out = out[:, :up.k]
+            out = torch.empty(tokens, up.k, dtype=x.dtype, device=device)
         yp, y_row = _matrix("out", out, (x.dtype,), device, (tokens, up.k))
         rp, r_row = (None, 0) if residual is None else _matrix("residual", residual, (x.dtype,), device, (tokens, up.k))
         size = _size("dm_experts_bytes", device, (self.key, tokens), up.ref, self.down.ref, tokens, self.top_k)
