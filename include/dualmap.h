@@ -830,7 +830,8 @@ typedef struct {
     uint64_t work_bytes;
 } dm_choose_args;
 
-/* Size of dm_choose_args.work; 0 for an invalid shape. */
+/* Size of dm_choose_args.work; 1: none is needed, and work may be NULL; 0 for an
+ * invalid shape. */
 DM_API uint64_t dm_choose_bytes(uint32_t tokens, uint32_t experts, uint32_t top_k);
 
 /* Each token's top_k experts by score (ties to the lowest id) and their
@@ -863,7 +864,8 @@ typedef struct {
 } dm_product_args;
 
 /* Size of dm_product_args.work on the current device (it depends on its SMs);
- * gathered: 1 where the rows have sources.  0 for an invalid shape. */
+ * gathered: 1 where the rows have sources.  1: none is needed, and work may be
+ * NULL; 0 for an invalid shape. */
 DM_API uint64_t dm_product_bytes(const dm_weights *w, uint32_t rows, uint32_t gated, uint32_t gathered);
 
 /* y[r, c] = sum over j of x[r, j] w[e, c, j], times x_scale[r] scale[e, c] for
@@ -874,6 +876,26 @@ DM_API uint64_t dm_product_bytes(const dm_weights *w, uint32_t rows, uint32_t ga
  * Recorded: DM_ERR_INVALID_ARG (offsets or sources out of range),
  * DM_ERR_TIMEOUT (a wait in the kernel gave up).  Asynchronous. */
 DM_API dm_status dm_product(const dm_weights *w, const dm_product_args *a, void *stream);
+
+/* A projection with 8-bit weights (dm_linear). */
+typedef struct {
+    const void *x;            /* rows x k, DM_BF16 or DM_F16 */
+    void *y;                  /* rows x n; any alignment of its type */
+    uint32_t *status;
+    void *work;               /* dm_linear_bytes bytes, 256-byte aligned */
+    uint64_t work_bytes;
+    uint64_t x_row, y_row;    /* elements; x_row a multiple of 16 bytes */
+    uint32_t dtype, y_dtype;  /* of x; of y: DM_BF16, DM_F16 or DM_F32 */
+    uint32_t rows;
+    float eps;                /* of a norm, >= 0; negative: no norm */
+} dm_linear_args;
+
+/* Size of dm_linear_args.work on the current device; 0 for an invalid shape. */
+DM_API uint64_t dm_linear_bytes(const dm_weights *w, uint32_t rows);
+
+/* dm_quantize and then dm_product with one expert's 8-bit weights.  Recorded: as
+ * dm_product.  Asynchronous. */
+DM_API dm_status dm_linear(const dm_weights *w, const dm_linear_args *a, void *stream);
 
 /* A layer of experts (dm_experts). */
 typedef struct {

@@ -34,18 +34,9 @@ __device__ __forceinline__ void unpack(const uint4 &x, float *f) {
     }
 }
 
-// 8 values of a row from element `at` on, zeros from `end` on.
-template <class T>
-__device__ __forceinline__ void load8(const T *row, uint32_t at, uint32_t end, float *f) {
-    uint4 x = make_uint4(0, 0, 0, 0);
-    if (at < end) x = *reinterpret_cast<const uint4 *>(row + at);
-    unpack<T>(x, f);
-    if (at < end && end - at < 8) {
-#pragma unroll
-        for (uint32_t i = 0; i < 8; ++i)
-            if (i >= end - at) f[i] = 0.f;
-    }
-}
+__device__ __forceinline__ float score_at(const __nv_bfloat16 *p) { return __bfloat162float(*p); }
+__device__ __forceinline__ float score_at(const __half *p) { return __half2float(*p); }
+__device__ __forceinline__ float score_at(const float *p) { return *p; }
 
 // -- rows in 8 bits -------------------------------------------------------------------
 //
@@ -53,15 +44,15 @@ __device__ __forceinline__ void load8(const T *row, uint32_t at, uint32_t end, f
 // registers of a warp (up to 2,048 values) or of a CTA (up to 16,384); a longer
 // one is read twice.
 //
-// 127 x is exact in 32 bits, and 127 x / top lies on a border between two steps
-// only where that is a whole number of halves, or at least 1 / 4096 away from
-// one (x and top have up to 11 bits).  So the product with 127 / top, which is
-// off by less than 2^-15, decides all but what is near a border, and there the
-// exact division decides: q is what the formula says to the last case.
+// 127 x is exact in 32 bits, and 127 x / top lies on a border between two steps,
+// or at least 1 / 4096 away from one (x and top have up to 11 bits).  The product
+// with 127 / top is off by less than 2^-16, so it decides all but what is near a
+// border, and there the exact division does: q is what the formula says to the
+// last case.
 
 struct QuantizeArgs {
     const char *x;
-    int8_t *q;
+    void *q;   // int8, or halves that hold the same whole numbers
     float *scale;
     const int32_t *count;
     uint64_t x_row, q_row;   // elements
@@ -69,110 +60,148 @@ struct QuantizeArgs {
     float eps;
 };
 
-__device__ __forceinline__ uint32_t step_of(float x, float by, float f, float top) {
-    const float y = x * by, r = rintf(y);
-    if (fabsf(fabsf(y - r) - 0.5f) < 1e-3f) return (uint32_t)(__float2int_rn(__fdiv_rn(x * f, top))) & 0xFF;
-    return (uint32_t)__float2int_rn(y) & 0xFF;
-}
+// The largest of the sizes in a and b, two 16-bit values each: without their
+// signs the bits of floating-point numbers are in their order, and what is not
+// finite is above the rest.
+__device__ __forceinline__ uint32_t larger2(uint32_t a, uint32_t b) { return __vmaxu2(a, b & 0x7FFF7FFFu); }
 
-template <class T, uint32_t kLanes>
-__global__ void __launch_bounds__(256) k_quantize(QuantizeArgs p) {
-    constexpr uint32_t kHeld = 8, kPer = 256 / kLanes;   // vectors of a lane; rows of a CTA
-    __shared__ float s_part[8][2];
+// Added to a number below 2^22 it leaves that number, rounded to even, in the low bits.
+constexpr float kRound = 12582912.f;
+
+template <class T, bool kHalves, bool kNorm, uint32_t kLanes, uint32_t kHeld>
+__global__ void __launch_bounds__(256, kHeld <= 2 ? 5 : kHeld <= 4 ? 4 : 3) k_quantize(QuantizeArgs p) {
+    constexpr uint32_t kPer = 256 / kLanes;   // rows of a CTA; kHeld: vectors of 8 values a lane keeps
+    constexpr uint32_t kFinite = std::is_same_v<T, __half> ? 0x7C00 : 0x7F80;
+    __shared__ uint32_t s_top[8];
+    __shared__ float s_sum[8];
     pdl_enter();
     const uint32_t lane = threadIdx.x % kLanes, rows = p.count ? (uint32_t)min(max(__ldcg(p.count), 0), (int32_t)p.rows) : p.rows;
     for (uint32_t r = blockIdx.x * kPer + threadIdx.x / kLanes; r < rows; r += gridDim.x * kPer) {
         const T *x = reinterpret_cast<const T *>(p.x) + r * p.x_row;
-        float top = 0.f, sum = 0.f;
-        bool odd = false;   // a value that is not finite
-        uint4 held[kHeld];
-        auto look = [&](const float *f) {
+        uint32_t tops = 0;
+        float sum = 0.f;
+        // values from the row's end on are zeros
+        auto load = [&](uint32_t at) {
+            uint4 v = make_uint4(0, 0, 0, 0);
+            if (at < p.k) v = *reinterpret_cast<const uint4 *>(x + at);
+            return v;
+        };
+        auto cut = [&](uint4 &v, uint32_t at) {
+            if (at < p.k && p.k - at < 8) {
+                uint32_t *w = reinterpret_cast<uint32_t *>(&v);
 #pragma unroll
-            for (int i = 0; i < 8; ++i) {
-                odd |= !(fabsf(f[i]) <= 3.4028235e38f);
-                top = fmaxf(top, fabsf(f[i]));
-                sum += f[i] * f[i];
+                for (uint32_t i = 0; i < 4; ++i) w[i] &= (at + 2 * i < p.k ? 0xFFFFu : 0u) | (at + 2 * i + 1 < p.k ? 0xFFFF0000u : 0u);
             }
         };
+        auto look = [&](const uint4 &v) {
+            tops = larger2(larger2(larger2(larger2(tops, v.x), v.y), v.z), v.w);
+            if constexpr (kNorm) {
+                float f[8];
+                unpack<T>(v, f);
 #pragma unroll
-        for (uint32_t i = 0; i < kHeld; ++i) {
-            const uint32_t at = (i * kLanes + lane) * 8;
-            held[i] = make_uint4(0, 0, 0, 0);
-            if (at < p.k) held[i] = *reinterpret_cast<const uint4 *>(x + at);
-        }
-#pragma unroll
-        for (uint32_t i = 0; i < kHeld; ++i) {
-            const uint32_t at = (i * kLanes + lane) * 8;
-            float f[8];
-            unpack<T>(held[i], f);
-            if (at + 8 > p.k) {
-#pragma unroll
-                for (uint32_t j = 0; j < 8; ++j)
-                    if (at + j >= p.k) f[j] = 0.f;
+                for (int i = 0; i < 8; ++i) sum += f[i] * f[i];
             }
-            look(f);
+        };
+        uint4 held[kHeld];
+#pragma unroll
+        for (uint32_t i = 0; i < kHeld; ++i) held[i] = load((i * kLanes + lane) * 8);
+#pragma unroll
+        for (uint32_t i = 0; i < kHeld; ++i) {
+            cut(held[i], (i * kLanes + lane) * 8);
+            look(held[i]);
         }
         for (uint32_t at = (kHeld * kLanes + lane) * 8; at < p.k; at += kLanes * 8) {
-            float f[8];
-            load8(x, at, p.k, f);
-            look(f);
+            uint4 v = load(at);
+            cut(v, at);
+            look(v);
         }
-        if (odd) top = INFINITY;
+        uint32_t bits = __reduce_max_sync(~0u, max(tops & 0xFFFFu, tops >> 16));
+        if constexpr (kNorm)
 #pragma unroll
-        for (int d = 16; d; d /= 2) {
-            top = fmaxf(top, __shfl_xor_sync(~0u, top, d));
-            sum += __shfl_xor_sync(~0u, sum, d);
-        }
+            for (int d = 16; d; d /= 2) sum += __shfl_xor_sync(~0u, sum, d);
         if constexpr (kLanes > 32) {
             __syncthreads();   // the row before has been read
-            if (lane % 32 == 0) s_part[lane / 32][0] = top, s_part[lane / 32][1] = sum;
+            if (lane % 32 == 0) s_top[lane / 32] = bits, s_sum[lane / 32] = sum;
             __syncthreads();
-            top = sum = 0.f;
+            bits = 0;
+            sum = 0.f;
 #pragma unroll
-            for (uint32_t i = 0; i < kLanes / 32; ++i) top = fmaxf(top, s_part[i][0]), sum += s_part[i][1];
+            for (uint32_t i = 0; i < kLanes / 32; ++i) bits = max(bits, s_top[i]), sum += s_sum[i];
         }
+        const uint16_t low = (uint16_t)bits;
+        const bool finite = bits < kFinite;
+        const float top = score_at(reinterpret_cast<const T *>(&low));
         float scale = __fdiv_rn(top, 127.f);
-        if (p.eps >= 0.f) scale *= rsqrtf(sum / (float)p.k + p.eps);
-        if (top == INFINITY) scale = __int_as_float(0x7FC00000);
-        if (lane == 0) p.scale[r] = scale;
+        if constexpr (kNorm) scale *= rsqrtf(sum / (float)p.k + p.eps);
+        if (lane == 0) p.scale[r] = finite ? scale : __int_as_float(0x7FC00000);
         // powers of two keep 127 / top and 127 x in range
         const float shift = top > 1e30f ? 0x1p-64f : top < 1e-30f ? 0x1p64f : 1.f;
-        const float big = top * shift, by = top == 0.f || top == INFINITY ? 0.f : __fdiv_rn(127.f, big);
-        int8_t *q = p.q + r * p.q_row;
-        auto put = [&](uint32_t at, const float *f) {
-            uint32_t b[8];
+        const float big = top * shift, by = bits == 0 || !finite ? 0.f : __fdiv_rn(127.f, big);
+        auto put = [&](const uint4 &v, uint32_t at) {
+            float f[8], far = 0.f;
+            uint32_t n[8];   // kRound + the step
+            unpack<T>(v, f);
 #pragma unroll
-            for (int i = 0; i < 8; ++i) b[i] = by == 0.f ? 0u : step_of(f[i] * shift, by, 127.f, big);
-            if (at + 8 <= p.k) {
-                *reinterpret_cast<uint2 *>(q + at) =
-                    make_uint2(b[0] | b[1] << 8 | b[2] << 16 | b[3] << 24, b[4] | b[5] << 8 | b[6] << 16 | b[7] << 24);
+            for (int i = 0; i < 8; ++i) {
+                f[i] = by == 0.f ? 0.f : f[i] * shift;
+                const float y = __fmaf_rn(f[i], by, kRound);
+                n[i] = __float_as_uint(y);
+                far = fmaxf(far, fabsf(__fmaf_rn(f[i], by, kRound - y)));
+            }
+            if (far > 0.5f - 0x1p-15f) {
+#pragma unroll
+                for (int i = 0; i < 8; ++i) n[i] = __float_as_uint(rintf(__fdiv_rn(f[i] * 127.f, big)) + kRound);
+            }
+            if constexpr (kHalves) {
+                // 1536 + the step is a half with the step in its low bits
+                const __half2 minus = __half2half2(__ushort_as_half(0x6600));
+                uint4 y;
+                uint32_t *w = reinterpret_cast<uint32_t *>(&y);
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    const uint32_t two = (n[2 * i] + 0x6600u & 0xFFFFu) | (n[2 * i + 1] + 0x6600u) << 16;
+                    const __half2 z = __hsub2(*reinterpret_cast<const __half2 *>(&two), minus);
+                    w[i] = *reinterpret_cast<const uint32_t *>(&z);
+                }
+                *reinterpret_cast<uint4 *>(static_cast<__half *>(p.q) + r * p.q_row + at) = y;   // rows of whole vectors
             } else {
+                int8_t *q = static_cast<int8_t *>(p.q) + r * p.q_row + at;
+                const uint2 y = make_uint2(__byte_perm(__byte_perm(n[0], n[1], 0x0040), __byte_perm(n[2], n[3], 0x0040), 0x5410),
+                                           __byte_perm(__byte_perm(n[4], n[5], 0x0040), __byte_perm(n[6], n[7], 0x0040), 0x5410));
+                if (at + 8 <= p.k) {
+                    *reinterpret_cast<uint2 *>(q) = y;
+                } else {
 #pragma unroll
-                for (uint32_t i = 0; i < 8; ++i)
-                    if (at + i < p.k) q[at + i] = (int8_t)b[i];
+                    for (uint32_t i = 0; i < 8; ++i)
+                        if (at + i < p.k) q[i] = (int8_t)n[i];
+                }
             }
         };
 #pragma unroll
         for (uint32_t i = 0; i < kHeld; ++i) {
             const uint32_t at = (i * kLanes + lane) * 8;
-            if (at >= p.k) break;
-            float f[8];
-            unpack<T>(held[i], f);
-            put(at, f);
+            if (at < p.k) put(held[i], at);
         }
         for (uint32_t at = (kHeld * kLanes + lane) * 8; at < p.k; at += kLanes * 8) {
-            float f[8];
-            load8(x, at, p.k, f);
-            put(at, f);
+            uint4 v = load(at);
+            cut(v, at);
+            put(v, at);
         }
     }
 }
 
-template <class T>
+template <class T, bool kHalves, bool kNorm>
 cudaError_t launch_quantize(const QuantizeArgs &p, cudaStream_t st) {
-    const uint32_t most = (uint32_t)sm_count() * 8;
-    if (p.k <= 2048) return launch_pdl(k_quantize<T, 32>, std::min((p.rows + 7) / 8, most), 256, 0, st, p);
-    return launch_pdl(k_quantize<T, 256>, std::min(p.rows, most), 256, 0, st, p);
+    const auto by_warps = p.k <= 512 ? k_quantize<T, kHalves, kNorm, 32, 2> : p.k <= 1024 ? k_quantize<T, kHalves, kNorm, 32, 4> : k_quantize<T, kHalves, kNorm, 32, 8>;
+    const auto by_ctas = p.k <= 4096 ? k_quantize<T, kHalves, kNorm, 256, 2> : p.k <= 8192 ? k_quantize<T, kHalves, kNorm, 256, 4> : k_quantize<T, kHalves, kNorm, 256, 8>;
+    const uint32_t sms = (uint32_t)sm_count(), ctas = p.k <= 2048 ? (p.rows + 7) / 8 : p.rows;
+    return launch_pdl(p.k <= 2048 ? by_warps : by_ctas, std::min(ctas, sms * 8), 256, 0, st, p);
+}
+
+template <class T>
+cudaError_t launch_quantize(const QuantizeArgs &p, bool halves, cudaStream_t st) {
+    if (p.eps >= 0.f) return halves ? launch_quantize<T, true, true>(p, st) : launch_quantize<T, false, true>(p, st);
+    return halves ? launch_quantize<T, true, false>(p, st) : launch_quantize<T, false, false>(p, st);
 }
 
 // -- the choice of experts ---------------------------------------------------------------
@@ -199,10 +228,6 @@ struct ChooseArgs {
 };
 
 uint32_t tile_tokens(uint32_t top_k) { return std::min(kTileTokens, kTilePairs / top_k); }
-
-__device__ __forceinline__ float score_at(const __nv_bfloat16 *p) { return __bfloat162float(*p); }
-__device__ __forceinline__ float score_at(const __half *p) { return __half2float(*p); }
-__device__ __forceinline__ float score_at(const float *p) { return *p; }
 
 // Whole numbers in the order of the scores; 0: nothing to choose.
 __device__ __forceinline__ uint32_t order_of(float x) {
@@ -400,7 +425,7 @@ cudaError_t launch_choose(const ChooseArgs &p, cudaStream_t st) {
 uint64_t choose_bytes(uint32_t tokens, uint32_t experts, uint32_t top_k) {
     if (experts < 1 || experts > 1024 || top_k < 1 || top_k > std::min(experts, 32u) || (uint64_t)tokens * top_k > 0x7FFFFFFFull) return 0;
     const uint64_t tiles = (tokens + tile_tokens(top_k) - 1) / tile_tokens(top_k);
-    return 256 + align_up(tiles, 4) * experts * 4;
+    return tiles <= 1 ? 1 : align_up(tiles, 4) * experts * 4;
 }
 
 cudaError_t choose(const ChooseArgs &from, uint32_t dtype, cudaStream_t st) {
@@ -494,9 +519,9 @@ uint64_t layer_work(const dm_weights *up, const dm_weights *down, uint32_t token
     w.parts = (float *)take(4 * slots * w.parts_row);
     w.xq = take(eight ? tokens * w.xq_row : 0);
     w.x_scale = (float *)take(eight ? 4ull * tokens : 0);
-    w.hq = take(eight ? slots * w.hq_row : 0);
+    w.hq = take(eight ? slots * w.hq_row * (takes_halves(down, (uint32_t)slots) ? 2 : 1) : 0);
     w.h_scale = (float *)take(eight ? 4 * slots : 0);
-    w.product = take(std::max(dm_product_bytes(up, (uint32_t)slots, 1, 1), dm_product_bytes(down, (uint32_t)slots, 0, 0)));
+    w.product = take(std::max(product_bytes(up, (uint32_t)slots, 1, kGathered), product_bytes(down, (uint32_t)slots, 0, kHalves)));
     return at;
 }
 
@@ -505,9 +530,32 @@ bool layer_ok(const dm_weights *up, const dm_weights *down, uint32_t tokens, uin
     return up->n % 2 == 0 && down->k == up->n / 2 && down->n == up->k && choose_bytes(tokens, up->experts, top_k) != 0;
 }
 
-cudaError_t quantize(uint32_t dtype, const QuantizeArgs &p, cudaStream_t st) {
-    return dtype == DM_BF16 ? launch_quantize<__nv_bfloat16>(p, st) : launch_quantize<__half>(p, st);
+cudaError_t quantize(uint32_t dtype, const QuantizeArgs &p, bool halves, cudaStream_t st) {
+    return dtype == DM_BF16 ? launch_quantize<__nv_bfloat16>(p, halves, st) : launch_quantize<__half>(p, halves, st);
 }
+
+// A projection's work buffer.
+struct LinearWork {
+    char *q, *product;
+    float *scale;
+    uint64_t q_row;   // elements
+};
+
+uint64_t linear_work(const dm_weights *w, uint32_t rows, void *base, LinearWork &x) {
+    uint64_t at = 0;
+    auto take = [&](uint64_t bytes) {
+        char *p = static_cast<char *>(base) + at;
+        at += align_up(bytes, 256);
+        return p;
+    };
+    x.q_row = align_up(w->k, 16);
+    x.q = take(rows * x.q_row * (takes_halves(w, rows) ? 2 : 1));
+    x.scale = (float *)take(4ull * rows);
+    x.product = take(product_bytes(w, rows, 0, kHalves));
+    return at;
+}
+
+bool linear_ok(const dm_weights *w, uint32_t rows) { return weights_ok(w) && w->dtype == DM_I8 && w->experts == 1 && rows <= 0x7FFFFFFFu; }
 
 }  // namespace
 }  // namespace dm
@@ -531,7 +579,37 @@ extern "C" dm_status dm_quantize(const dm_quantize_args *a, void *stream) {
     if (a->x_row % 8 || a->q_row % 16 || a->x_row > (1ull << 32) || a->q_row > (1ull << 32)) return DM_ERR_INVALID_ARG;
     if (a->rows > 1 && (a->x_row < a->k || a->q_row < a->k)) return DM_ERR_INVALID_ARG;
     return status_of(quantize(a->dtype, {static_cast<const char *>(a->x), a->q, a->scale, a->count, a->x_row, a->q_row, a->rows, a->k, a->eps},
-                              static_cast<cudaStream_t>(stream)));
+                              false, static_cast<cudaStream_t>(stream)));
+}
+
+extern "C" uint64_t dm_linear_bytes(const dm_weights *w, uint32_t rows) {
+    using namespace dm;
+    LinearWork x;
+    return linear_ok(w, rows) ? linear_work(w, rows, nullptr, x) : 0;
+}
+
+extern "C" dm_status dm_linear(const dm_weights *w, const dm_linear_args *a, void *stream) {
+    using namespace dm;
+    if (!a || !linear_ok(w, a->rows) || !a->status || a->dtype > DM_F16 || a->y_dtype > DM_F32 || a->y_dtype == DM_I8 || !(a->eps <= 3.4e38f))
+        return DM_ERR_INVALID_ARG;
+    LinearWork x;
+    if (!a->work || !aligned(a->work, 256) || a->work_bytes < linear_work(w, a->rows, a->work, x)) return DM_ERR_INVALID_ARG;
+    if (a->rows == 0) return DM_OK;
+    if (!a->x || !a->y || !aligned(a->x, 16) || !aligned(a->y, dtype_size(a->y_dtype))) return DM_ERR_INVALID_ARG;
+    if (a->x_row % 8 || a->x_row > (1ull << 32) || a->y_row > (1ull << 32)) return DM_ERR_INVALID_ARG;
+    if (a->rows > 1 && (a->x_row < w->k || a->y_row < w->n)) return DM_ERR_INVALID_ARG;
+    const auto st = static_cast<cudaStream_t>(stream);
+    const auto linear = [&]() -> cudaError_t {
+        dm_product_args d{};
+        d.x = x.q, d.x_scale = x.scale, d.x_row = x.q_row, d.x_rows = d.rows = a->rows;
+        d.y = a->y, d.y_row = a->y_row, d.y_dtype = a->y_dtype, d.status = a->status;
+        ProductArgs p = product_args(w, &d);
+        p.x_halves = takes_halves(w, a->rows);
+        p.x_row = x.q_row * (p.x_halves ? 2 : 1);
+        DM_TRY(quantize(a->dtype, {static_cast<const char *>(a->x), x.q, x.scale, nullptr, a->x_row, x.q_row, a->rows, w->k, a->eps}, p.x_halves, st));
+        return launch_product(w, p, x.product, st);
+    };
+    return status_of(linear());
 }
 
 extern "C" uint64_t dm_choose_bytes(uint32_t tokens, uint32_t experts, uint32_t top_k) { return dm::choose_bytes(tokens, experts, top_k); }
@@ -540,7 +618,7 @@ extern "C" dm_status dm_choose_experts(const dm_choose_args *a, void *stream) {
     using namespace dm;
     if (!a || a->reserved0 || a->dtype > DM_F32 || a->dtype == DM_I8 || a->renormalize > 1) return DM_ERR_INVALID_ARG;
     const uint64_t need = choose_bytes(a->tokens, a->experts, a->top_k);
-    if (!need || a->work_bytes < need || !a->work || !aligned(a->work, 16) || !a->offsets || !aligned(a->offsets, 4)) return DM_ERR_INVALID_ARG;
+    if (!need || (need > 1 && (a->work_bytes < need || !a->work || !aligned(a->work, 16))) || !a->offsets || !aligned(a->offsets, 4)) return DM_ERR_INVALID_ARG;
     if (a->logits_row > (1ull << 32) || (a->tokens > 1 && a->logits_row < a->experts)) return DM_ERR_INVALID_ARG;
     if (a->tokens && (!a->logits || !a->ids || !a->weights || !a->slots || !a->sources || !aligned(a->logits, dtype_size(a->dtype)) ||
                       !aligned(a->ids, 4) || !aligned(a->weights, 4) || !aligned(a->slots, 4) || !aligned(a->sources, 4)))
@@ -589,18 +667,21 @@ extern "C" dm_status dm_experts(const dm_weights *up, const dm_weights *down, co
         u.x = a->x, u.x_row = a->x_row, u.x_rows = a->tokens, u.sources = w.sources, u.per_source = a->top_k, u.offsets = w.offsets;
         u.y = w.h, u.y_row = w.h_row, u.y_dtype = a->dtype, u.rows = slots, u.gated = 1, u.status = a->status;
         if (eight) {
-            DM_TRY(quantize(a->dtype, {static_cast<const char *>(a->x), (int8_t *)w.xq, w.x_scale, nullptr, a->x_row, w.xq_row, a->tokens, up->k, -1.f}, st));
+            DM_TRY(quantize(a->dtype, {static_cast<const char *>(a->x), w.xq, w.x_scale, nullptr, a->x_row, w.xq_row, a->tokens, up->k, -1.f}, false, st));
             u.x = w.xq, u.x_row = w.xq_row, u.x_scale = w.x_scale;
         }
         DM_TRY(launch_product(up, product_args(up, &u), w.product, st));
         dm_product_args d{};
         d.x = w.h, d.x_row = w.h_row, d.x_rows = slots, d.offsets = w.offsets;
         d.y = w.parts, d.y_row = w.parts_row, d.y_dtype = DM_F32, d.rows = slots, d.status = a->status;
+        ProductArgs dp = product_args(down, &d);
         if (eight) {
-            DM_TRY(quantize(a->dtype, {w.h, (int8_t *)w.hq, w.h_scale, w.offsets + up->experts, w.h_row, w.hq_row, slots, down->k, -1.f}, st));
-            d.x = w.hq, d.x_row = w.hq_row, d.x_scale = w.h_scale;
+            // straight to the halves that the tensor cores take, where they do
+            dp.x = w.hq, dp.x_scale = w.h_scale, dp.x_halves = takes_halves(down, slots);
+            dp.x_row = w.hq_row * (dp.x_halves ? 2 : 1);
+            DM_TRY(quantize(a->dtype, {w.h, w.hq, w.h_scale, w.offsets + up->experts, w.h_row, w.hq_row, slots, down->k, -1.f}, dp.x_halves, st));
         }
-        DM_TRY(launch_product(down, product_args(down, &d), w.product, st));
+        DM_TRY(launch_product(down, dp, w.product, st));
         JoinArgs j{w.parts, w.slots, w.weights, static_cast<const char *>(a->residual), static_cast<char *>(a->y), a->status,
                    w.parts_row, a->residual_row, a->y_row, a->tokens, a->top_k, up->k,
                    aligned(a->residual, 8) && aligned(a->y, 8) && (a->residual_row | a->y_row) % 4 == 0};

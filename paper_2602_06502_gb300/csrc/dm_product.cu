@@ -21,6 +21,7 @@ namespace {
 // out k, 64 bytes at a time, and add their sums up in the order of the warps.
 
 constexpr uint32_t kFewT = 256, kFewWarps = 8;
+constexpr uint32_t kFewRows = 8;   // an expert's, on average, up to which this kernel has them
 
 template <class T>
 struct Few;   // T: of the weights and rows
@@ -172,10 +173,18 @@ ProductArgs product_args(const dm_weights *w, const dm_product_args *a) {
     return p;
 }
 
-static bool many_rows(const dm_weights *w, uint32_t rows) { return rows > 16ull * w->experts; }
+static bool many_rows(const dm_weights *w, uint32_t rows) { return rows > kFewRows * (uint64_t)w->experts; }
+
+bool takes_halves(const dm_weights *w, uint32_t rows) { return w->dtype == DM_I8 && many_rows(w, rows); }
+
+uint64_t product_bytes(const dm_weights *w, uint32_t rows, uint32_t gated, RowsAre are) {
+    if (!many_rows(w, rows)) return 1;
+    const WideShape s = wide_shape(w, rows, gated, are);
+    return std::max<uint64_t>(s.x_bytes + s.part_bytes, 1);
+}
 
 cudaError_t launch_product(const dm_weights *w, const ProductArgs &p, void *work, cudaStream_t st) {
-    if (many_rows(w, p.rows)) return launch_product_wide(w, p, wide_shape(w, p.rows, p.gated, p.sources != nullptr), work, st);
+    if (many_rows(w, p.rows)) return launch_product_wide(w, p, wide_shape(w, p.rows, p.gated, p.x_halves ? kHalves : p.sources ? kGathered : kPlain), work, st);
     if (w->dtype == DM_BF16) return launch_few<__nv_bfloat16>(p, st);
     return w->dtype == DM_F16 ? launch_few<__half>(p, st) : launch_few<int8_t>(p, st);
 }
@@ -185,16 +194,15 @@ cudaError_t launch_product(const dm_weights *w, const ProductArgs &p, void *work
 extern "C" uint64_t dm_product_bytes(const dm_weights *w, uint32_t rows, uint32_t gated, uint32_t gathered) {
     using namespace dm;
     if (!weights_ok(w) || rows > 0x7FFFFFFFu || gated > 1 || gathered > 1 || (gated && w->n % 2)) return 0;
-    if (!many_rows(w, rows)) return 256;
-    const WideShape s = wide_shape(w, rows, gated, gathered);
-    return 256 + s.x_bytes + s.part_bytes;
+    return product_bytes(w, rows, gated, gathered ? kGathered : kPlain);
 }
 
 extern "C" dm_status dm_product(const dm_weights *w, const dm_product_args *a, void *stream) {
     using namespace dm;
     if (!a) return DM_ERR_INVALID_ARG;
     const uint64_t need = dm_product_bytes(w, a->rows, a->gated, a->sources != nullptr);
-    if (!need || a->reserved0 || !a->status || a->work_bytes < need || !a->work || !aligned(a->work, 256)) return DM_ERR_INVALID_ARG;
+    if (!need || a->reserved0 || !a->status) return DM_ERR_INVALID_ARG;
+    if (need > 1 && (a->work_bytes < need || !a->work || !aligned(a->work, 256))) return DM_ERR_INVALID_ARG;
     const uint32_t size = dtype_size(w->dtype), n = a->gated ? w->n / 2 : w->n;
     if (a->y_dtype > DM_F32 || a->y_dtype == DM_I8 || a->x_rows > 0x7FFFFFFFu) return DM_ERR_INVALID_ARG;
     if (!a->offsets && w->experts != 1) return DM_ERR_INVALID_ARG;

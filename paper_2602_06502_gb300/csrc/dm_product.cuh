@@ -25,6 +25,7 @@ struct ProductArgs {
     uint32_t rows, x_rows, per, experts;
     uint32_t n, k;                     // channels of y; elements of a row of x
     uint32_t y_dtype, gated;
+    uint32_t x_halves;                 // 8-bit: x holds halves (for the kernel for many rows)
 };
 
 // Expert e's rows [a, b); none, and an error, where the offsets are wrong.
@@ -88,7 +89,11 @@ struct WideShape {
     uint32_t blocks, splits, steps;
     uint64_t x_row, x_bytes, part_bytes;
 };
-WideShape wide_shape(const dm_weights *w, uint32_t rows, uint32_t gated, bool gathered);
+// Where a product's rows are: as they came, named by sources, or halves of 8-bit values.
+enum RowsAre { kPlain, kGathered, kHalves };
+WideShape wide_shape(const dm_weights *w, uint32_t rows, uint32_t gated, RowsAre are);
+uint64_t product_bytes(const dm_weights *w, uint32_t rows, uint32_t gated, RowsAre are);
+bool takes_halves(const dm_weights *w, uint32_t rows);   // 8-bit values as halves are worth having
 cudaError_t launch_product_wide(const dm_weights *w, const ProductArgs &p, const WideShape &s, void *work, cudaStream_t st);
 
 // A product of the layer's own, whose arguments are known to be right.

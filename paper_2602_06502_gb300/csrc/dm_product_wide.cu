@@ -536,7 +536,7 @@ cudaError_t launch(const dm_weights *w, const WideArgs &a, const CUtensorMap &mw
 
 }  // namespace
 
-WideShape wide_shape(const dm_weights *w, uint32_t rows, uint32_t gated, bool gathered) {
+WideShape wide_shape(const dm_weights *w, uint32_t rows, uint32_t gated, RowsAre are) {
     WideShape s{};
     const bool eight = w->dtype == DM_I8;
     const uint32_t most = eight ? Wide<true>::kRows : Wide<false>::kRows, step = eight ? Wide<true>::kStep : Wide<false>::kStep;
@@ -549,7 +549,7 @@ WideShape wide_shape(const dm_weights *w, uint32_t rows, uint32_t gated, bool ga
         if (tiles * 2 <= pairs) s.splits = (uint32_t)std::min<uint64_t>({pairs / tiles, s.steps, 8});
     }
     s.x_row = align_up(w->k, 8) * 2;
-    s.x_bytes = eight || gathered ? align_up(rows * s.x_row, 256) : 0;
+    s.x_bytes = are == dm::kGathered || (eight && are == kPlain) ? align_up(rows * s.x_row, 256) : 0;
     s.part_bytes = s.splits > 1 ? align_up((uint64_t)s.splits * rows * w->n * 4, 256) : 0;
     return s;
 }

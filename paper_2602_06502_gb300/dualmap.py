@@ -156,6 +156,12 @@ class dm_product_args(C.Structure):
                [(name, C.c_uint32) for name in ("rows", "x_rows", "per_source", "y_dtype", "gated", "reserved0")]
 
 
+class dm_linear_args(C.Structure):
+    _fields_ = [(name, C.c_void_p) for name in ("x", "y", "status", "work")] + \
+               [(name, C.c_uint64) for name in ("work_bytes", "x_row", "y_row")] + \
+               [(name, C.c_uint32) for name in ("dtype", "y_dtype", "rows")] + [("eps", C.c_float)]
+
+
 class dm_experts_args(C.Structure):
     _fields_ = [(name, C.c_void_p) for name in ("x", "logits", "residual", "y", "status", "work")] + \
                [(name, C.c_uint64) for name in ("work_bytes", "x_row", "logits_row", "residual_row", "y_row")] + \
@@ -221,6 +227,8 @@ SIGNATURES = {
     "dm_choose_experts": (C.c_int, [C.POINTER(dm_choose_args), C.c_void_p]),
     "dm_product_bytes": (C.c_uint64, [C.POINTER(dm_weights), C.c_uint32, C.c_uint32, C.c_uint32]),
     "dm_product": (C.c_int, [C.POINTER(dm_weights), C.POINTER(dm_product_args), C.c_void_p]),
+    "dm_linear_bytes": (C.c_uint64, [C.POINTER(dm_weights), C.c_uint32]),
+    "dm_linear": (C.c_int, [C.POINTER(dm_weights), C.POINTER(dm_linear_args), C.c_void_p]),
     "dm_experts_bytes": (C.c_uint64, [C.POINTER(dm_weights), C.POINTER(dm_weights), C.c_uint32, C.c_uint32]),
     "dm_experts": (C.c_int, [C.POINTER(dm_weights), C.POINTER(dm_weights), C.POINTER(dm_experts_args), C.c_void_p]),
     "dm_test_fail_alloc": (None, [C.c_int64]),
@@ -495,6 +503,14 @@ def dm_product_bytes(w, rows, gated=0, gathered=0):
 
 def dm_product(w, args, stream=None):
     return lib().dm_product(C.byref(w), C.byref(args), stream)
+
+
+def dm_linear_bytes(w, rows):
+    return lib().dm_linear_bytes(C.byref(w), rows)
+
+
+def dm_linear(w, args, stream=None):
+    return lib().dm_linear(C.byref(w), C.byref(args), stream)
 
 
 def dm_experts_bytes(up, down, tokens, top_k):

@@ -49,34 +49,54 @@ def _call(name, device, *args):
         raise D.DualMapError(rc, name)
 
 
-def _cuda(name, x):
-    if x.device.type != "cuda":
-        raise ValueError(f"{name}: a CUDA tensor wanted")
-    return x.device
+# These run once per call of a decode step, so they ask each tensor for little.
 
-
-def _matrix(name, x, dtypes, device, shape=(None, None)):
-    """(address, distance of rows) of a matrix."""
-    if x.dim() != 2 or x.dtype not in dtypes or x.device != device or any(w is not None and n != w for n, w in zip(x.shape, shape)):
-        raise ValueError(f"{name}: a matrix of shape {shape} on {device}, of one of the types {list(dtypes)}")
-    row, one = x.stride()
-    if x.shape[1] > 1 and one != 1:
-        raise ValueError(f"{name}: its last dimension is contiguous")
+def _refuse_grad(name, x):
     if x.requires_grad and torch.is_grad_enabled():
         raise ValueError(f"{name} requires grad, and this call gives no gradients: use torch.no_grad() or detach it")
-    if x.shape[0] <= 1:   # the stride of a dimension of one element says nothing
+
+
+def _matrix(name, x, dtypes, device, n=None, k=None):
+    """(address, distance of rows) of a matrix [n, k] (None: of any number)."""
+    if x.dim() != 2 or x.dtype not in dtypes or x.device != device or device.type != "cuda":
+        raise ValueError(f"{name}: a matrix on a CUDA device, with the other tensors, of one of the types {list(dtypes)}")
+    rows, width = x.shape
+    if (n is not None and rows != n) or (k is not None and width != k):
+        raise ValueError(f"{name}: shape {(rows, width)}, wanted {(n, k)}")
+    row, one = x.stride()
+    if one != 1 and width > 1:
+        raise ValueError(f"{name}: its last dimension is contiguous")
+    if x.requires_grad:
+        _refuse_grad(name, x)
+    if rows <= 1:   # the stride of a dimension of one element says nothing
         row = 0
-    elif row < x.shape[1]:
+    elif row < width:
         raise ValueError(f"{name}: its rows lie one after another")
     return x.data_ptr(), row
 
 
 def _vector(name, x, dtype, device, n):
-    if x.dtype is not dtype or x.shape != (n,) or x.device != device or not x.is_contiguous():
+    if x.dtype is not dtype or x.dim() != 1 or x.shape[0] != n or x.device != device or not x.is_contiguous():
         raise ValueError(f"{name}: contiguous {dtype} of length {n} on {device}")
-    if x.requires_grad and torch.is_grad_enabled():
-        raise ValueError(f"{name} requires grad, and this call gives no gradients: use torch.no_grad() or detach it")
+    if x.requires_grad:
+        _refuse_grad(name, x)
     return x.data_ptr()
+
+
+def _work(size, device):
+    """(tensor, address) of a work buffer; a size of 1 says that none is needed."""
+    if size == 1:
+        return None, None
+    work = torch.empty(size, dtype=torch.uint8, device=device)
+    return work, work.data_ptr()
+
+
+def _eps(eps):
+    if eps is None:
+        return -1.0
+    if not eps >= 0:
+        raise ValueError("eps is not negative")
+    return eps
 
 
 def quantize(x, *, eps=None, count=None):
@@ -84,17 +104,16 @@ def quantize(x, *, eps=None, count=None):
     int8 [rows, k] = 127 x / max |x| rounded, scale float32 [rows].  eps: rows
     are first divided by the root of their mean square plus eps.  count: an
     int32 tensor of one element, the number of rows that there are."""
-    device = _cuda("x", x)
+    device = x.device
     xp, row = _matrix("x", x, TYPES, device)
     rows, k = x.shape
-    q = torch.empty(rows, -(-k // 16) * 16, dtype=torch.int8, device=device)[:, :k]
+    q_row = -(-k // 16) * 16
+    q = torch.empty(rows, q_row, dtype=torch.int8, device=device)
     scale = torch.empty(rows, dtype=torch.float32, device=device)
-    if eps is not None and not eps >= 0:
-        raise ValueError("eps is not negative")
     a = D.dm_quantize_args(xp, q.data_ptr(), scale.data_ptr(), None if count is None else _vector("count", count, torch.int32, device, 1),
-                           row, q.stride(0), TYPES[x.dtype], rows, k, -1.0 if eps is None else eps)
+                           row, q_row, TYPES[x.dtype], rows, k, _eps(eps))
     _call("dm_quantize", device, C.byref(a))
-    return q, scale
+    return q if q_row == k else q[:, :k], scale
 
 
 class Weights:
@@ -107,7 +126,9 @@ class Weights:
             raise ValueError("weights are [n, k] or [experts, n, k], not empty, the last dimension contiguous")
         if (w.dtype is torch.int8) != (scale is not None) or (scale is None and w.dtype not in TYPES):
             raise ValueError("weights are bfloat16 or float16, or int8 with a scale")
-        self.device = _cuda("w", w)
+        if w.device.type != "cuda":
+            raise ValueError("weights live on a CUDA device")
+        self.device = w.device
         for name, x in (("w", w), ("scale", scale)):
             if x is not None and x.requires_grad:
                 raise ValueError(f"{name} requires grad, and products give no gradients: detach it")
@@ -124,6 +145,7 @@ class Weights:
                                    w.stride(0) if self.experts > 1 else 0)
         self.ref, self.key = C.byref(self.struct), (w.dtype, self.experts, self.n, self.k)
         self.status = torch.zeros(1, dtype=torch.int32, device=self.device)
+        self.status_at = self.status.data_ptr()
         self._streams = set()   # whose work may still use the weights
         _size("dm_product_bytes", self.device, (self.key, 0, 0, 0), self.ref, 0, 0, 0)   # refuses what is no set of weights
 
@@ -164,7 +186,7 @@ def product(x, weights, offsets=None, *, x_scale=None, sources=None, per_source=
     output: whatever memory held).  dtype: of a new output (default: x's, for int8
     bfloat16)."""
     w, device = weights, weights.device
-    xp, x_row = _matrix("x", x, (w.dtype,), device, (None, w.k))
+    xp, x_row = _matrix("x", x, (w.dtype,), device, None, w.k)
     if (x_scale is None) != (w.scale is None):
         raise ValueError("x_scale comes with int8 weights")
     sp = None if x_scale is None else _vector("x_scale", x_scale, torch.float32, device, x.shape[0])
@@ -179,13 +201,13 @@ def product(x, weights, offsets=None, *, x_scale=None, sources=None, per_source=
     width = w.n // 2 if gated else w.n
     if out is None:
         out = torch.empty(n, width, dtype=dtype or (torch.bfloat16 if w.scale is not None else w.dtype), device=device)
-    yp, y_row = _matrix("out", out, SCORES, device, (n, width))
+    yp, y_row = _matrix("out", out, SCORES, device, n, width)
     gathered = sources is not None
     size = _size("dm_product_bytes", device, (w.key, n, gated, gathered), w.ref, n, int(gated), int(gathered))
     w.hold()
-    work = torch.empty(size, dtype=torch.uint8, device=device)
+    work, at = _work(size, device)
     a = D.dm_product_args(xp, sp, yp, op, None if sources is None else _vector("sources", sources, torch.int32, device, n),
-                          w.status.data_ptr(), work.data_ptr(), size, x_row, y_row, n, x.shape[0], per_source, SCORES[out.dtype], gated, 0)
+                          w.status_at, at, size, x_row, y_row, n, x.shape[0], per_source, SCORES[out.dtype], gated, 0)
     _call("dm_product", device, w.ref, C.byref(a))
     return out
 
@@ -205,17 +227,18 @@ def choose(logits, top_k, *, renormalize=True):
     [experts + 1], slots int32 [tokens, top_k] (pair -> slot) and sources int32
     [tokens * top_k] (slot -> pair, token * top_k + place).  An expert with a
     score of minus infinity is not chosen: id and slot -1, weight 0."""
-    device = _cuda("logits", logits)
+    device = logits.device
     xp, row = _matrix("logits", logits, SCORES, device)
     tokens, experts = logits.shape
     size = _size("dm_choose_bytes", device, (tokens, experts, top_k), tokens, experts, top_k)
-    ints = dict(dtype=torch.int32, device=device)
-    ids, slots = torch.empty(2, tokens, top_k, **ints)
+    ids = torch.empty(tokens, top_k, dtype=torch.int32, device=device)
     weights = torch.empty(tokens, top_k, dtype=torch.float32, device=device)
-    offsets, sources = torch.empty(experts + 1, **ints), torch.empty(tokens * top_k, **ints)
-    work = torch.empty(size, dtype=torch.uint8, device=device)
+    slots = torch.empty(tokens, top_k, dtype=torch.int32, device=device)
+    offsets = torch.empty(experts + 1, dtype=torch.int32, device=device)
+    sources = torch.empty(tokens * top_k, dtype=torch.int32, device=device)
+    work, at = _work(size, device)
     a = D.dm_choose_args(xp, row, SCORES[logits.dtype], tokens, experts, top_k, bool(renormalize), 0, ids.data_ptr(),
-                         weights.data_ptr(), offsets.data_ptr(), slots.data_ptr(), sources.data_ptr(), work.data_ptr(), size)
+                         weights.data_ptr(), offsets.data_ptr(), slots.data_ptr(), sources.data_ptr(), at, size)
     _call("dm_choose_experts", device, C.byref(a))
     return Choice(ids, weights, offsets, slots, sources)
 
@@ -238,8 +261,17 @@ class Linear:
             if eps is not None:
                 raise ValueError("a norm comes with int8 weights")
             return product(x, w, out=out)
-        q, scale = quantize(x, eps=eps)
-        return product(q, w, x_scale=scale, out=out, dtype=x.dtype)
+        device, rows = w.device, x.shape[0]
+        xp, x_row = _matrix("x", x, TYPES, device, None, w.k)
+        if out is None:
+            out = torch.empty(rows, w.n, dtype=x.dtype, device=device)
+        yp, y_row = _matrix("out", out, SCORES, device, rows, w.n)
+        size = _size("dm_linear_bytes", device, (w.key, rows), w.ref, rows)
+        w.hold()
+        work = torch.empty(size, dtype=torch.uint8, device=device)
+        a = D.dm_linear_args(xp, yp, w.status_at, work.data_ptr(), size, x_row, y_row, TYPES[x.dtype], SCORES[out.dtype], rows, _eps(eps))
+        _call("dm_linear", device, w.ref, C.byref(a))
+        return out
 
     def last_error(self):
         return self.weights.last_error()
@@ -265,17 +297,17 @@ class Experts:
         be residual, and overlaps nothing else."""
         up, device, tokens = self.up, self.up.device, x.shape[0]
         types = TYPES if up.scale is not None else (up.dtype,)
-        xp, x_row = _matrix("x", x, types, device, (None, up.k))
-        lp, l_row = _matrix("logits", logits, SCORES, device, (tokens, up.experts))
+        xp, x_row = _matrix("x", x, types, device, None, up.k)
+        lp, l_row = _matrix("logits", logits, SCORES, device, tokens, up.experts)
         if out is None:
             out = torch.empty(tokens, up.k, dtype=x.dtype, device=device)
-        yp, y_row = _matrix("out", out, (x.dtype,), device, (tokens, up.k))
-        rp, r_row = (None, 0) if residual is None else _matrix("residual", residual, (x.dtype,), device, (tokens, up.k))
+        yp, y_row = _matrix("out", out, (x.dtype,), device, tokens, up.k)
+        rp, r_row = (None, 0) if residual is None else _matrix("residual", residual, (x.dtype,), device, tokens, up.k)
         size = _size("dm_experts_bytes", device, (self.key, tokens), up.ref, self.down.ref, tokens, self.top_k)
         up.hold()
         self.down.hold()
         work = torch.empty(size, dtype=torch.uint8, device=device)
-        a = D.dm_experts_args(xp, lp, rp, yp, up.status.data_ptr(), work.data_ptr(), size, x_row, l_row, r_row, y_row,
+        a = D.dm_experts_args(xp, lp, rp, yp, up.status_at, work.data_ptr(), size, x_row, l_row, r_row, y_row,
                               TYPES[x.dtype], SCORES[logits.dtype], tokens, self.top_k, self.renormalize, 0)
         _call("dm_experts", device, up.ref, self.down.ref, C.byref(a))
         return out
