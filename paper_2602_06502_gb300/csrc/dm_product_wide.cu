@@ -30,14 +30,14 @@ struct Wide {
     static constexpr uint32_t kW = 128 * 128;                         // bytes of a stage's weights
     static constexpr uint32_t kHalf = kRows / 2 * 128;                // bytes of 64 elements of this CTA's rows
     static constexpr uint32_t kX = kW, kStage = kW + kHalf * (kStep / 64);
-    static constexpr uint32_t kA = 2 * kRows, kAs = 2;                // 8-bit: columns of the weights in tensor memory, their places
+    static constexpr uint32_t kA = 2 * kRows, kAs = 4;                // 8-bit: columns of the weights in tensor memory, in places of 64 elements of k
     static constexpr uint32_t kSwap = kStages * kStage;               // gated: 32 rows of 64 channels, floats
     static constexpr uint32_t kFirst = kSwap + 32 * 64 * 4;           // tiles before each expert
     static constexpr uint32_t kBars = kFirst + 1032 * 4;
     // per stage: full (the pair's), empty, weights full, weights empty; per
     // buffer of sums: full, empty (the pair's); per place of weights: full (the
     // pair's), empty
-    static constexpr uint32_t kWord = kBars + 32 * kStages + 32 + 32 + 16;   // after the last, `done`
+    static constexpr uint32_t kWord = kBars + 32 * kStages + 32 + 16 * kAs + 16;   // after the last, `done`
     static constexpr uint32_t kBytes = kWord + 16 + 1024;
 };
 
@@ -59,19 +59,11 @@ __device__ __forceinline__ uint32_t of_first(uint32_t addr) {   // the same plac
     asm("mapa.shared::cluster.u32 %0, %1, 0;" : "=r"(r) : "r"(addr));
     return r;
 }
+// What is handed over is tensor memory, which tcgen05's own fences order, so
+// neither this nor the waits order other memory between the CTAs (at cluster
+// scope each costs some hundred cycles).
 __device__ __forceinline__ void arrive_pair(uint32_t bar) {   // bar: of_first()
-    asm volatile("mbarrier.arrive.release.cluster.shared::cluster.b64 _, [%0];" ::"r"(bar) : "memory");
-}
-__device__ __forceinline__ bool try_pair(uint32_t bar, uint32_t parity) {
-    uint32_t ok;
-    asm volatile(
-        "{\n\t.reg .pred p;\n\t"
-        "mbarrier.try_wait.parity.acquire.cluster.shared::cta.b64 p, [%1], %2;\n\t"
-        "selp.u32 %0, 1, 0, p;\n\t}"
-        : "=r"(ok)
-        : "r"(bar), "r"(parity)
-        : "memory");
-    return ok != 0;
+    asm volatile("mbarrier.arrive.relaxed.cluster.shared::cluster.b64 _, [%0];" ::"r"(bar) : "memory");
 }
 __device__ __forceinline__ uint32_t peer_word(uint32_t addr, uint32_t rank) {
     uint32_t x;
@@ -124,10 +116,10 @@ __device__ __forceinline__ void commit2(uint32_t bar) {
 // `gave_up`, and the CTA's others then return at once: every loop is as long as
 // its data says, so the CTA ends.
 __device__ __forceinline__ void wait(uint32_t bar, uint32_t parity, volatile uint32_t *gave_up, uint32_t *status) {
-    if (!try_pair(bar, parity)) {
+    if (!mbar_try(bar, parity)) {
         const uint64_t t0 = now_ns();
         for (uint32_t i = 0;; ++i) {
-            if (try_pair(bar, parity) || *gave_up) break;
+            if (mbar_try(bar, parity) || *gave_up) break;
             if ((i & 63) == 63 && (now_ns() - t0 > kWaitNs || i > kWaits)) {
                 *gave_up = 1;
                 set_err(status, DM_ERR_TIMEOUT);
@@ -213,17 +205,19 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(Wide<kEight>::kThrea
     auto sum_empty = [&](uint32_t i) { return more + 16 * i + 8; };
     auto a_full = [&](uint32_t i) { return more + 32 + 16 * i; };
     auto a_empty = [&](uint32_t i) { return more + 32 + 16 * i + 8; };
-    const uint32_t done = more + 64;
+    const uint32_t done = more + 32 + 16 * W::kAs;
     if (tid == 0) {
         for (uint32_t i = 0; i < W::kStages; ++i) {
             mbar_init(full(i), 1);
             mbar_init(empty(i), 1);
             mbar_init(w_full(i), 1);
-            mbar_init(w_empty(i), 4);
+            mbar_init(w_empty(i), 8);
         }
         for (uint32_t i = 0; i < 2; ++i) {
             mbar_init(sum_full(i), 1);
             mbar_init(sum_empty(i), 8);   // four warps of two CTAs
+        }
+        for (uint32_t i = 0; i < W::kAs; ++i) {
             mbar_init(a_full(i), 8);
             mbar_init(a_empty(i), 1);
         }
@@ -328,20 +322,27 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(Wide<kEight>::kThrea
                 if (n >= 2) wait(sum_empty(buf), (n / 2 - 1) & 1, gave_up, p.status);
                 fence_after();
                 for (uint32_t j = 0; j < steps; ++j, ++c) {
-                    const uint32_t st = c % W::kStages, round = c / W::kStages, as = c % W::kAs;
-                    wait(full(st), round & 1, gave_up, p.status);
-                    if constexpr (kEight) wait(a_full(as), (c / W::kAs) & 1, gave_up, p.status);
-                    fence_after();
+                    const uint32_t st = c % W::kStages;
+                    wait(full(st), (c / W::kStages) & 1, gave_up, p.status);
                     const uint64_t wa = w_op + st * (W::kStage >> 4), xa = x_op + st * (W::kStage >> 4);
-                    if (one) {
 #pragma unroll
-                        for (uint32_t kk = 0; kk < W::kStep / 16; ++kk) {
-                            const uint32_t x_at = (kk / 4 * W::kHalf + kk % 4 * 32) >> 4;
-                            if constexpr (kEight) mma2_ts(tm + buf * W::kRows, tm + W::kA + as * 64 + kk * 8, xa + x_at, desc, j > 0 || kk > 0);
-                            else mma2_ss(tm + buf * W::kRows, wa + (kk * 32 >> 4), xa + x_at, desc, j > 0 || kk > 0);
+                    for (uint32_t sub = 0; sub < W::kStep / 64; ++sub) {
+                        const uint32_t use = c * (W::kStep / 64) + sub, as = use % W::kAs;
+                        if constexpr (kEight) wait(a_full(as), (use / W::kAs) & 1, gave_up, p.status);
+                        fence_after();
+                        if (one) {
+#pragma unroll
+                            for (uint32_t kk = 0; kk < 4; ++kk) {
+                                const uint64_t x = xa + ((sub * W::kHalf + kk * 32) >> 4);
+                                if constexpr (kEight) mma2_ts(tm + buf * W::kRows, tm + W::kA + as * 32 + kk * 8, x, desc, j > 0 || sub > 0 || kk > 0);
+                                else mma2_ss(tm + buf * W::kRows, wa + (kk * 32 >> 4), x, desc, j > 0 || kk > 0);
+                            }
+                            if constexpr (kEight) commit2(a_empty(as));
                         }
+                        __syncwarp();
+                    }
+                    if (one) {
                         commit2(empty(st));
-                        if constexpr (kEight) commit2(a_empty(as));
                         if (j + 1 == steps) commit2(sum_full(buf));
                     }
                     __syncwarp();
@@ -412,8 +413,8 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(Wide<kEight>::kThrea
             }
         }
     } else if (kEight && wid >= 8) {
-        // 128 channels of 128 bytes to 64 columns of halves; two groups of four
-        // warps take every other stage
+        // 128 channels of 128 bytes to columns of halves: two groups of four warps
+        // have 64 bytes each
         const uint32_t group = (wid - 8) / 4, r = (wid & 3) * 32 + lane;
         uint32_t c = 0;
         for (uint32_t i = pair; i < tiles && !__any_sync(~0u, *gave_up); i += pairs) {
@@ -421,36 +422,32 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(Wide<kEight>::kThrea
             uint32_t from;
             const uint32_t steps = steps_of(t, from);
             for (uint32_t j = 0; j < steps; ++j, ++c) {
-                if ((c & 1) != group) continue;
-                const uint32_t st = c % W::kStages, as = c % W::kAs, use = c / W::kAs;
+                const uint32_t st = c % W::kStages, use = 2 * c + group, as = use % W::kAs, round = use / W::kAs;
                 wait(w_full(st), (c / W::kStages) & 1, gave_up, p.status);
-                uint4 v[8];
+                uint4 v[4];
 #pragma unroll
-                for (uint32_t x = 0; x < 8; ++x) v[x] = *reinterpret_cast<const uint4 *>(s + st * W::kStage + r * 128 + ((x ^ (r & 7)) << 4));
+                for (uint32_t x = 0; x < 4; ++x) v[x] = *reinterpret_cast<const uint4 *>(s + st * W::kStage + r * 128 + (((4 * group + x) ^ (r & 7)) << 4));
                 __syncwarp();
                 if (lane == 0) mbar_arrive(w_empty(st));
-                if (use) wait(a_empty(as), (use - 1) & 1, gave_up, p.status);
-                fence_after();
+                uint32_t y[32];
 #pragma unroll
-                for (uint32_t h = 0; h < 2; ++h) {
-                    uint32_t y[32];
-#pragma unroll
-                    for (uint32_t x = 0; x < 4; ++x) {
-                        bytes_to_halves(v[4 * h + x].x, y[8 * x], y[8 * x + 1]);
-                        bytes_to_halves(v[4 * h + x].y, y[8 * x + 2], y[8 * x + 3]);
-                        bytes_to_halves(v[4 * h + x].z, y[8 * x + 4], y[8 * x + 5]);
-                        bytes_to_halves(v[4 * h + x].w, y[8 * x + 6], y[8 * x + 7]);
-                    }
-                    tm_st(tmem + W::kA + as * 64 + h * 32 + ((wid & 3) << 21), y);
+                for (uint32_t x = 0; x < 4; ++x) {
+                    bytes_to_halves(v[x].x, y[8 * x], y[8 * x + 1]);
+                    bytes_to_halves(v[x].y, y[8 * x + 2], y[8 * x + 3]);
+                    bytes_to_halves(v[x].z, y[8 * x + 4], y[8 * x + 5]);
+                    bytes_to_halves(v[x].w, y[8 * x + 6], y[8 * x + 7]);
                 }
+                if (round) wait(a_empty(as), (round - 1) & 1, gave_up, p.status);
+                fence_after();
+                tm_st(tmem + W::kA + as * 32 + ((wid & 3) << 21), y);
                 wait_st();
                 fence_before();
                 __syncwarp();
                 if (lane == 0) arrive_pair(of_first(a_full(as)));
             }
         }
-        const uint32_t uses = (c + 1 - group) / 2;   // the last has been taken before the CTA ends
-        if (uses) wait(a_empty(group), (uses - 1) & 1, gave_up, p.status);
+        // the last uses of this group's places have ended before the CTA does
+        for (uint32_t x = c > W::kAs / 2 ? c - W::kAs / 2 : 0; x < c; ++x) wait(a_empty((2 * x + group) % W::kAs), ((2 * x + group) / W::kAs) & 1, gave_up, p.status);
     }
     fence_before();
     __syncthreads();
