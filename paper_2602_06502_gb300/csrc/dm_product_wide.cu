@@ -9,9 +9,9 @@
 // all experts in one line; offsets are read on the device.
 //
 //   warps 0-3   sums to y, a channel per lane
-//   warp 4      copies by tensor map into a ring of stages
+//   warps 4, 6  copies of weights and of rows by tensor map, into a ring of stages
 //   warp 5      tcgen05.mma, in the first CTA of the pair
-//   warps 8-15  8-bit weights alone: to halves, in tensor memory, from where
+//   warps 8-23  8-bit weights alone: to halves, in tensor memory, from where
 //               the tensor cores take them: no second pass through shared memory
 #include <algorithm>
 
@@ -23,17 +23,18 @@ namespace {
 
 template <bool kEight>
 struct Wide {
-    static constexpr uint32_t kThreads = kEight ? 512 : 192;
+    static constexpr uint32_t kThreads = kEight ? 768 : 224;
     static constexpr uint32_t kRows = kEight ? 192 : 256;             // of a tile
     static constexpr uint32_t kStep = kEight ? 128 : 64;              // elements of k in a stage
     static constexpr uint32_t kStages = kEight ? 5 : 6;
     static constexpr uint32_t kW = 128 * 128;                         // bytes of a stage's weights
     static constexpr uint32_t kHalf = kRows / 2 * 128;                // bytes of 64 elements of this CTA's rows
     static constexpr uint32_t kX = kW, kStage = kW + kHalf * (kStep / 64);
-    static constexpr uint32_t kA = 2 * kRows, kAs = 4;                // 8-bit: columns of the weights in tensor memory, in places of 64 elements of k
+    static constexpr uint32_t kA = 2 * kRows, kAs = 4;                // 8-bit: columns of the weights in tensor memory, in places of 64 elements of k: one for each group of converting warps
     static constexpr uint32_t kSwap = kStages * kStage;               // gated: 32 rows of 64 channels, floats
-    static constexpr uint32_t kFirst = kSwap + 32 * 64 * 4;           // tiles before each expert
-    static constexpr uint32_t kBars = kFirst + 1032 * 4;
+    static constexpr uint32_t kFirst = kSwap + 32 * 64 * 4;           // tiles before each expert, widest tiles first
+    static constexpr uint32_t kOrder = kFirst + 1032 * 4;             // those experts (16 bits)
+    static constexpr uint32_t kBars = kOrder + 1024 * 2;
     // per stage: full (the pair's), empty, weights full, weights empty; per
     // buffer of sums: full, empty (the pair's); per place of weights: full (the
     // pair's), empty
@@ -140,20 +141,33 @@ struct Tile {
 template <uint32_t kRows>
 __device__ __forceinline__ uint32_t row_blocks(uint32_t rows) { return (rows + kRows - 1) / kRows; }
 
+// An expert's rows in blocks of about the same size, multiples of 16.
+template <uint32_t kRows>
+__device__ __forceinline__ uint32_t block_rows(uint32_t rows) {
+    const uint32_t n = row_blocks<kRows>(rows);
+    return ((rows + n - 1) / n + 15) / 16 * 16;
+}
+
+struct Line {   // of tiles
+    const uint32_t *first;
+    const uint16_t *order;
+    uint32_t tiles, pair, pairs;
+};
+
 // Tile i: an expert's tiles go through its rows first (they share the weights), then through the channels.
 template <uint32_t kRows>
-__device__ __forceinline__ Tile tile_at(const WideArgs &a, const uint32_t *first, uint32_t i) {
+__device__ __forceinline__ Tile tile_at(const WideArgs &a, const Line &l, uint32_t i) {
     uint32_t lo = 0, hi = a.p.experts;   // the last expert that begins by then
     while (hi - lo > 1) {
         const uint32_t mid = (lo + hi) / 2;
-        if (first[mid] <= i) lo = mid;
+        if (l.first[mid] <= i) lo = mid;
         else hi = mid;
     }
-    const int32_t from = a.p.offsets ? __ldcg(a.p.offsets + lo) : 0, to = a.p.offsets ? __ldcg(a.p.offsets + lo + 1) : (int32_t)a.p.rows;
-    const uint32_t rows = (uint32_t)(to - from), n = row_blocks<kRows>(rows), each = ((rows + n - 1) / n + 15) / 16 * 16;
-    uint32_t x = i - first[lo];
     Tile t;
-    t.e = lo;
+    t.e = l.order[lo];
+    const int32_t from = a.p.offsets ? __ldcg(a.p.offsets + t.e) : 0, to = a.p.offsets ? __ldcg(a.p.offsets + t.e + 1) : (int32_t)a.p.rows;
+    const uint32_t rows = (uint32_t)(to - from), n = row_blocks<kRows>(rows), each = block_rows<kRows>(rows);
+    uint32_t x = i - l.first[lo];
     t.split = x % a.splits;
     x /= a.splits;
     const uint32_t block = x % n;
@@ -163,6 +177,28 @@ __device__ __forceinline__ Tile tile_at(const WideArgs &a, const uint32_t *first
     t.c0 = x / n * (a.p.gated ? 128 : 256);
     return t;
 }
+
+// A pair's tiles, and their steps of k.  The line begins with the widest tiles
+// and pairs take turns in alternating order, so each has about as much to do:
+// with the experts' own order pairs differed by 9 to 12% (32 experts of 27 to
+// 1,862 rows).
+template <uint32_t kRows>
+struct Walk {
+    uint32_t turn, k0, steps;   // turns so far; of the present tile
+    Tile t;
+
+    __device__ __forceinline__ Walk() : turn(0) {}
+    __device__ __forceinline__ bool next(const WideArgs &a, const Line &l) {
+        const uint32_t i = turn * l.pairs + (turn & 1 ? l.pairs - 1 - l.pair : l.pair);
+        if (turn * l.pairs >= l.tiles) return false;
+        ++turn;
+        if (i >= l.tiles) return false;   // the last turn
+        t = tile_at<kRows>(a, l, i);
+        k0 = (uint32_t)((uint64_t)t.split * a.steps / a.splits);
+        steps = (uint32_t)((uint64_t)(t.split + 1) * a.steps / a.splits) - k0;
+        return true;
+    }
+};
 
 template <class Y>
 __device__ __forceinline__ Y to_y(float x) {
@@ -195,6 +231,8 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(Wide<kEight>::kThrea
     const ProductArgs &p = a.p;
     const uint32_t s_at = smem_addr(s), bars = s_at + W::kBars, more = bars + 32 * W::kStages;
     uint32_t *first = reinterpret_cast<uint32_t *>(s + W::kFirst);
+    uint16_t *order = reinterpret_cast<uint16_t *>(s + W::kOrder);
+    uint32_t *held = reinterpret_cast<uint32_t *>(s + W::kSwap);   // an expert's rows, until the tiles are counted
     volatile uint32_t *gave_up = reinterpret_cast<uint32_t *>(s + W::kWord);
     const uint32_t tid = threadIdx.x, wid = __shfl_sync(~0u, tid >> 5, 0), lane = tid & 31, rank = blockIdx.x & 1;
     auto full = [&](uint32_t i) { return bars + 32 * i; };
@@ -230,17 +268,54 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(Wide<kEight>::kThrea
         asm volatile("tcgen05.alloc.cta_group::2.sync.aligned.shared::cta.b32 [%0], 512;" ::"r"(s_at + W::kWord + 4) : "memory");
         asm volatile("tcgen05.relinquish_alloc_permit.cta_group::2.sync.aligned;");
     }
-    // tiles before each expert; with an earlier error there are none
+    // the experts by the width of their tiles, and the tiles before each; with
+    // an earlier error there are none
     const bool stop = has_err(p.status);
     for (uint32_t e = tid; e < p.experts; e += W::kThreads) {
         const Rows r = stop ? Rows{0, 0} : expert_rows(p, e);
-        first[e + 1] = row_blocks<W::kRows>((uint32_t)(r.b - r.a)) * a.blocks * a.splits;
+        const uint32_t rows = (uint32_t)(r.b - r.a);
+        held[e] = rows;
     }
     __syncthreads();
     if (wid == 0) {
+        // lane x keeps how many experts have blocks of 16 (32 - x) rows, and
+        // then where the next of them goes
+        uint32_t at = 0;
+        auto lane_of = [&](uint32_t e) { return 32 - (held[e] ? block_rows<W::kRows>(held[e]) / 16 : 1); };
+        auto each32 = [&](auto f) {
+            for (uint32_t e0 = 0; e0 < p.experts; e0 += 32) {
+                const uint32_t e = e0 + lane, of = e < p.experts ? lane_of(e) : 0;   // blocks have at most 16 times 16 rows: nobody's
+                const uint32_t same = __match_any_sync(~0u, of);
+                f(e, of, same);
+            }
+        };
+        each32([&](uint32_t e, uint32_t of, uint32_t same) {
+#pragma unroll
+            for (uint32_t x = 16; x < 32; ++x) {
+                const uint32_t who = __ballot_sync(~0u, of == x);
+                if (lane == x) at += __popc(who);
+            }
+        });
+        uint32_t in = at;
+#pragma unroll
+        for (int d = 1; d < 32; d *= 2) {
+            const uint32_t y = __shfl_up_sync(~0u, in, d);
+            if ((int)lane >= d) in += y;
+        }
+        at = in - at;
+        each32([&](uint32_t e, uint32_t of, uint32_t same) {
+            const uint32_t place = __shfl_sync(~0u, at, of) + __popc(same & ((1u << lane) - 1));
+            if (e < p.experts) order[place] = (uint16_t)e;
+#pragma unroll
+            for (uint32_t x = 16; x < 32; ++x) {
+                const uint32_t who = __ballot_sync(~0u, of == x);
+                if (lane == x) at += __popc(who);
+            }
+        });
+        __syncwarp();
         uint32_t carry = 0;
         for (uint32_t e0 = 0; e0 < p.experts; e0 += 32) {
-            uint32_t x = e0 + lane < p.experts ? first[e0 + lane + 1] : 0;
+            uint32_t x = e0 + lane < p.experts ? row_blocks<W::kRows>(held[order[e0 + lane]]) * a.blocks * a.splits : 0;
 #pragma unroll
             for (int d = 1; d < 32; d *= 2) {
                 const uint32_t y = __shfl_up_sync(~0u, x, d);
@@ -260,43 +335,47 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(Wide<kEight>::kThrea
     uint32_t tiles = first[p.experts];
     if (peer_word(smem_addr(first + p.experts), rank ^ 1) != tiles) tiles = 0;
     const uint32_t tmem = *reinterpret_cast<volatile uint32_t *>(s + W::kWord + 4);
-    const uint32_t pair = blockIdx.x / 2, pairs = gridDim.x / 2;
-    auto steps_of = [&](const Tile &t, uint32_t &from) {
-        from = (uint32_t)((uint64_t)t.split * a.steps / a.splits);
-        return (uint32_t)((uint64_t)(t.split + 1) * a.steps / a.splits) - from;
-    };
-    if (wid == 4) {
+    const Line line{first, order, tiles, blockIdx.x / 2, gridDim.x / 2};
+    Walk<W::kRows> walk;
+    const Tile &t = walk.t;
+    if (wid == 4 || wid == 6) {
+        // One warp copies weights, one rows: a copy takes its warp about 100
+        // cycles to issue.  An elected thread issues what is the same in every
+        // lane, as it goes through uniform registers.
+        const bool weights = wid == 4, one = elect();
         uint32_t c = 0;   // stages so far
-        for (uint32_t i = pair; i < tiles && !__any_sync(~0u, *gave_up); i += pairs) {
-            const Tile t = tile_at<W::kRows>(a, first, i);
-            uint32_t from;
-            const uint32_t steps = steps_of(t, from), half = t.width / 2, boxes = half > W::kRows / 4 ? 0 : (half + kSmallBox - 1) / kSmallBox;
-            const uint32_t x_bytes = (boxes ? boxes * kSmallBox * 128 : W::kHalf) * (W::kStep / 64);
-            const int row = (int)(t.row + rank * half);
+        while (!__any_sync(~0u, *gave_up) && walk.next(a, line)) {
+            const uint32_t half = t.width / 2, boxes = half > W::kRows / 4 ? 0 : (half + kSmallBox - 1) / kSmallBox;
+            const int row = (int)(t.row + rank * half), e = (int)t.e;
             const int w0 = (int)(p.gated ? t.c0 + rank * 64 : t.c0 + rank * 128), w1 = (int)(p.gated ? p.n + t.c0 + rank * 64 : t.c0 + rank * 128 + 64);
+            const uint32_t x_bytes = (boxes ? boxes * kSmallBox * 128 : W::kHalf) * (W::kStep / 64);
+            const uint32_t steps = walk.steps;
             for (uint32_t j = 0; j < steps; ++j, ++c) {
-                const uint32_t st = c % W::kStages, round = c / W::kStages, at = s_at + st * W::kStage;
-                const int k0 = (int)((from + j) * W::kStep);
+                const uint32_t st = c % W::kStages, round = c / W::kStages, at = s_at + st * W::kStage, bar = of_first(full(st));
+                const int k0 = (int)((walk.k0 + j) * W::kStep);
                 if (round) {
-                    wait(empty(st), (round - 1) & 1, gave_up, p.status);
-                    if constexpr (kEight) wait(w_empty(st), (round - 1) & 1, gave_up, p.status);
+                    if (!kEight || !weights) wait(empty(st), (round - 1) & 1, gave_up, p.status);
+                    else wait(w_empty(st), (round - 1) & 1, gave_up, p.status);
                 }
-                if (lane == 0) {
-                    const uint32_t pair_bar = of_first(full(st));
-                    if (rank == 0) mbar_expect(full(st), 2 * (x_bytes + (kEight ? 0 : W::kW)));
-                    const uint32_t w_bar = kEight ? w_full(st) : pair_bar;
-                    if constexpr (kEight) mbar_expect(w_bar, W::kW);
-                    load3(at, &mw, w_bar, k0, w0, (int)t.e);
-                    load3(at + W::kW / 2, &mw, w_bar, k0, w1, (int)t.e);
-#pragma unroll
-                    for (uint32_t sub = 0; sub < W::kStep / 64; ++sub) {
-                        if (boxes == 0) {
-                            load2(at + W::kX + sub * W::kHalf, &mx, pair_bar, k0 + 64 * sub, row);
-                        } else {
-                            for (uint32_t b = 0; b < boxes; ++b)
-                                load2(at + W::kX + sub * W::kHalf + b * kSmallBox * 128, &ms, pair_bar, k0 + 64 * sub, row + b * kSmallBox);
-                        }
+                if (weights) {
+                    const uint32_t w_bar = kEight ? w_full(st) : bar;
+                    if (one) {
+                        if (kEight || rank == 0) mbar_expect(kEight ? w_full(st) : full(st), kEight ? W::kW : 2 * (x_bytes + W::kW));
+                        load3(at, &mw, w_bar, k0, w0, e);
+                        load3(at + W::kW / 2, &mw, w_bar, k0, w1, e);
                     }
+                } else if (boxes == 0) {
+                    if (one) {
+                        if (kEight && rank == 0) mbar_expect(full(st), 2 * x_bytes);
+#pragma unroll
+                        for (uint32_t sub = 0; sub < W::kStep / 64; ++sub) load2(at + W::kX + sub * W::kHalf, &mx, bar, k0 + 64 * sub, row);
+                    }
+                } else if (one) {
+                    if (kEight && rank == 0) mbar_expect(full(st), 2 * x_bytes);
+#pragma unroll
+                    for (uint32_t sub = 0; sub < W::kStep / 64; ++sub)
+                        for (uint32_t b = 0; b < boxes; ++b)
+                            load2(at + W::kX + sub * W::kHalf + b * kSmallBox * 128, &ms, bar, k0 + 64 * sub, row + b * kSmallBox);
                 }
                 __syncwarp();
             }
@@ -304,7 +383,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(Wide<kEight>::kThrea
         // no copy may be in flight when the CTA ends: its stages have been taken
         for (uint32_t i = c > W::kStages ? c - W::kStages : 0; i < c; ++i) {
             wait(empty(i % W::kStages), (i / W::kStages) & 1, gave_up, p.status);
-            if constexpr (kEight) mbar_drain(w_full(i % W::kStages), (i / W::kStages) & 1);
+            if (kEight && weights) wait(w_empty(i % W::kStages), (i / W::kStages) & 1, gave_up, p.status);
         }
     } else if (wid == 5) {
         if (rank == 0) {
@@ -313,10 +392,8 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(Wide<kEight>::kThrea
             const uint32_t tm = __shfl_sync(~0u, tmem, 0);
             const uint64_t w_op = operand(s_at, 16), x_op = operand(s_at + W::kX, 16);
             uint32_t c = 0, n = 0;
-            for (uint32_t i = pair; i < tiles && !__any_sync(~0u, *gave_up); i += pairs, ++n) {
-                const Tile t = tile_at<W::kRows>(a, first, i);
-                uint32_t from;
-                const uint32_t steps = steps_of(t, from), buf = n & 1;
+            for (; !__any_sync(~0u, *gave_up) && walk.next(a, line); ++n) {
+                const uint32_t steps = walk.steps, buf = n & 1;
                 // f32 sums, the operands' type, N, M = 256
                 const uint32_t desc = 1u << 4 | kType << 7 | kType << 10 | (t.width / 8) << 17 | 16u << 24;
                 if (n >= 2) wait(sum_empty(buf), (n / 2 - 1) & 1, gave_up, p.status);
@@ -356,8 +433,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(Wide<kEight>::kThrea
     } else if (wid < 4) {
         float *swap = reinterpret_cast<float *>(s + W::kSwap);
         uint32_t n = 0;
-        for (uint32_t i = pair; i < tiles; i += pairs, ++n) {   // the four warps meet, so none leaves early
-            const Tile t = tile_at<W::kRows>(a, first, i);
+        for (; walk.next(a, line); ++n) {   // the four warps meet, so none leaves early
             const uint32_t buf = n & 1, at = tmem + buf * W::kRows + ((wid & 3) << 21);
             // this lane's channel of the weights, and of y
             const uint32_t c = p.gated ? t.c0 + rank * 64 + (tid & 63) : t.c0 + rank * 128 + tid;
@@ -413,20 +489,20 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(Wide<kEight>::kThrea
             }
         }
     } else if (kEight && wid >= 8) {
-        // 128 channels of 128 bytes to columns of halves: two groups of four warps
-        // have 64 bytes each
-        const uint32_t group = (wid - 8) / 4, r = (wid & 3) * 32 + lane;
-        uint32_t c = 0;
-        for (uint32_t i = pair; i < tiles && !__any_sync(~0u, *gave_up); i += pairs) {
-            const Tile t = tile_at<W::kRows>(a, first, i);
-            uint32_t from;
-            const uint32_t steps = steps_of(t, from);
-            for (uint32_t j = 0; j < steps; ++j, ++c) {
-                const uint32_t st = c % W::kStages, use = 2 * c + group, as = use % W::kAs, round = use / W::kAs;
+        // 128 channels of 128 bytes to columns of halves: four groups of four warps
+        // have a place each, 64 bytes of every other stage
+        const uint32_t group = (wid - 8) / 4, half = group & 1, r = (wid & 3) * 32 + lane;
+        const uint32_t place = tmem + W::kA + group * 32 + ((wid & 3) << 21), bar = of_first(a_full(group));
+        uint32_t c = 0, uses = 0;
+        while (!__any_sync(~0u, *gave_up) && walk.next(a, line)) {
+            const uint32_t end = c + walk.steps;
+            for (; c < end; ++c) {
+                if ((c & 1) != group >> 1) continue;
+                const uint32_t st = c % W::kStages;
                 wait(w_full(st), (c / W::kStages) & 1, gave_up, p.status);
                 uint4 v[4];
 #pragma unroll
-                for (uint32_t x = 0; x < 4; ++x) v[x] = *reinterpret_cast<const uint4 *>(s + st * W::kStage + r * 128 + (((4 * group + x) ^ (r & 7)) << 4));
+                for (uint32_t x = 0; x < 4; ++x) v[x] = *reinterpret_cast<const uint4 *>(s + st * W::kStage + r * 128 + (((4 * half + x) ^ (r & 7)) << 4));
                 __syncwarp();
                 if (lane == 0) mbar_arrive(w_empty(st));
                 uint32_t y[32];
@@ -437,17 +513,17 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(Wide<kEight>::kThrea
                     bytes_to_halves(v[x].z, y[8 * x + 4], y[8 * x + 5]);
                     bytes_to_halves(v[x].w, y[8 * x + 6], y[8 * x + 7]);
                 }
-                if (round) wait(a_empty(as), (round - 1) & 1, gave_up, p.status);
+                if (uses) wait(a_empty(group), (uses - 1) & 1, gave_up, p.status);
+                ++uses;
                 fence_after();
-                tm_st(tmem + W::kA + as * 32 + ((wid & 3) << 21), y);
+                tm_st(place, y);
                 wait_st();
                 fence_before();
                 __syncwarp();
-                if (lane == 0) arrive_pair(of_first(a_full(as)));
+                if (lane == 0) arrive_pair(bar);
             }
         }
-        // the last uses of this group's places have ended before the CTA does
-        for (uint32_t x = c > W::kAs / 2 ? c - W::kAs / 2 : 0; x < c; ++x) wait(a_empty((2 * x + group) % W::kAs), ((2 * x + group) / W::kAs) & 1, gave_up, p.status);
+        if (uses) wait(a_empty(group), (uses - 1) & 1, gave_up, p.status);   // the last has been taken before the CTA ends
     }
     fence_before();
     __syncthreads();
