@@ -30,7 +30,7 @@ struct Wide {
     static constexpr uint32_t kW = 128 * 128;                         // bytes of a stage's weights
     static constexpr uint32_t kHalf = kRows / 2 * 128;                // bytes of 64 elements of this CTA's rows
     static constexpr uint32_t kX = kW, kStage = kW + kHalf * (kStep / 64);
-    static constexpr uint32_t kA = 2 * kRows, kAs = 4;                // 8-bit: columns of the weights in tensor memory, in places of 64 elements of k: one for each group of converting warps
+    static constexpr uint32_t kA = 2 * kRows, kAs = (512 - kA) / 32;  // 8-bit: columns of the weights in tensor memory, in places of 64 elements of k
     static constexpr uint32_t kSwap = kStages * kStage;               // gated: 32 rows of 64 channels, floats
     static constexpr uint32_t kFirst = kSwap + 32 * 64 * 4;           // tiles before each expert, widest tiles first
     static constexpr uint32_t kOrder = kFirst + 1032 * 4;             // those experts (16 bits)
@@ -111,6 +111,19 @@ __device__ __forceinline__ void commit2(uint32_t bar) {
     asm volatile("tcgen05.commit.cta_group::2.mbarrier::arrive::one.shared::cluster.multicast::cluster.b64 [%0], %1;" ::"r"(bar),
                  "h"((uint16_t)3)
                  : "memory");
+}
+
+// Whether the phase is over; does not wait.
+__device__ __forceinline__ bool over(uint32_t bar, uint32_t parity) {
+    uint32_t ok;
+    asm volatile(
+        "{\n\t.reg .pred p;\n\t"
+        "mbarrier.test_wait.parity.shared::cta.b64 p, [%1], %2;\n\t"
+        "selp.u32 %0, 1, 0, p;\n\t}"
+        : "=r"(ok)
+        : "r"(bar), "r"(parity)
+        : "memory");
+    return ok != 0;
 }
 
 // Waits for the phase, by a whole warp.  A wait that gives up says so in
@@ -391,38 +404,43 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(Wide<kEight>::kThrea
             const bool one = elect();
             const uint32_t tm = __shfl_sync(~0u, tmem, 0);
             const uint64_t w_op = operand(s_at, 16), x_op = operand(s_at + W::kX, 16);
-            uint32_t c = 0, n = 0;
+            // The next stage is asked for while the present one's products are
+            // issued: asking takes about as long as they do.
+            uint32_t n = 0, st = 0, parity = 0, as = 0, a_parity = 0;
+            bool ready = false, a_ready = false;
             for (; !__any_sync(~0u, *gave_up) && walk.next(a, line); ++n) {
-                const uint32_t steps = walk.steps, buf = n & 1;
+                const uint32_t steps = walk.steps, buf = n & 1, d = tm + buf * W::kRows;
                 // f32 sums, the operands' type, N, M = 256
                 const uint32_t desc = 1u << 4 | kType << 7 | kType << 10 | (t.width / 8) << 17 | 16u << 24;
                 if (n >= 2) wait(sum_empty(buf), (n / 2 - 1) & 1, gave_up, p.status);
-                fence_after();
-                for (uint32_t j = 0; j < steps; ++j, ++c) {
-                    const uint32_t st = c % W::kStages;
-                    wait(full(st), (c / W::kStages) & 1, gave_up, p.status);
+                for (uint32_t j = 0; j < steps; ++j) {
+                    if (!ready) wait(full(st), parity, gave_up, p.status);
                     const uint64_t wa = w_op + st * (W::kStage >> 4), xa = x_op + st * (W::kStage >> 4);
+                    const uint32_t now = st;
+                    if (++st == W::kStages) st = 0, parity ^= 1;
 #pragma unroll
                     for (uint32_t sub = 0; sub < W::kStep / 64; ++sub) {
-                        const uint32_t use = c * (W::kStep / 64) + sub, as = use % W::kAs;
-                        if constexpr (kEight) wait(a_full(as), (use / W::kAs) & 1, gave_up, p.status);
+                        if (kEight && !a_ready) wait(a_full(as), a_parity, gave_up, p.status);
                         fence_after();
                         if (one) {
 #pragma unroll
                             for (uint32_t kk = 0; kk < 4; ++kk) {
                                 const uint64_t x = xa + ((sub * W::kHalf + kk * 32) >> 4);
-                                if constexpr (kEight) mma2_ts(tm + buf * W::kRows, tm + W::kA + as * 32 + kk * 8, x, desc, j > 0 || sub > 0 || kk > 0);
-                                else mma2_ss(tm + buf * W::kRows, wa + (kk * 32 >> 4), x, desc, j > 0 || kk > 0);
+                                if constexpr (kEight) mma2_ts(d, tm + W::kA + as * 32 + kk * 8, x, desc, j > 0 || sub > 0 || kk > 0);
+                                else mma2_ss(d, wa + (kk * 32 >> 4), x, desc, j > 0 || kk > 0);
                             }
                             if constexpr (kEight) commit2(a_empty(as));
                         }
-                        __syncwarp();
+                        if constexpr (kEight) {
+                            if (++as == W::kAs) as = 0, a_parity ^= 1;
+                            a_ready = __all_sync(~0u, over(a_full(as), a_parity));
+                        }
                     }
                     if (one) {
-                        commit2(empty(st));
+                        commit2(empty(now));
                         if (j + 1 == steps) commit2(sum_full(buf));
                     }
-                    __syncwarp();
+                    ready = __all_sync(~0u, over(full(st), parity));
                 }
             }
             // nothing may be in flight when tensor memory is given back
@@ -490,10 +508,10 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(Wide<kEight>::kThrea
         }
     } else if (kEight && wid >= 8) {
         // 128 channels of 128 bytes to columns of halves: four groups of four warps
-        // have a place each, 64 bytes of every other stage
+        // have 64 bytes of every other stage each
         const uint32_t group = (wid - 8) / 4, half = group & 1, r = (wid & 3) * 32 + lane;
-        const uint32_t place = tmem + W::kA + group * 32 + ((wid & 3) << 21), bar = of_first(a_full(group));
-        uint32_t c = 0, uses = 0;
+        const uint32_t places = tmem + W::kA + ((wid & 3) << 21), bars_first = of_first(a_full(0));
+        uint32_t c = 0, as = group, round = 0;
         while (!__any_sync(~0u, *gave_up) && walk.next(a, line)) {
             const uint32_t end = c + walk.steps;
             for (; c < end; ++c) {
@@ -513,17 +531,20 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(Wide<kEight>::kThrea
                     bytes_to_halves(v[x].z, y[8 * x + 4], y[8 * x + 5]);
                     bytes_to_halves(v[x].w, y[8 * x + 6], y[8 * x + 7]);
                 }
-                if (uses) wait(a_empty(group), (uses - 1) & 1, gave_up, p.status);
-                ++uses;
+                if (round) wait(a_empty(as), (round - 1) & 1, gave_up, p.status);
                 fence_after();
-                tm_st(place, y);
+                tm_st(places + as * 32, y);
                 wait_st();
                 fence_before();
                 __syncwarp();
-                if (lane == 0) arrive_pair(bar);
+                if (lane == 0) arrive_pair(bars_first + 16 * as);
+                as += 4;   // the group's next use is the fourth from here
+                if (as >= W::kAs) as -= W::kAs, ++round;
             }
         }
-        if (uses) wait(a_empty(group), (uses - 1) & 1, gave_up, p.status);   // the last has been taken before the CTA ends
+        // the last uses of all places have ended before the CTA does
+        const uint32_t uses = 2 * c;
+        for (uint32_t u = uses > W::kAs ? uses - W::kAs : 0; u < uses; ++u) wait(a_empty(u % W::kAs), (u / W::kAs) & 1, gave_up, p.status);
     }
     fence_before();
     __syncthreads();
