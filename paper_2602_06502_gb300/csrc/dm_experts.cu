@@ -2,8 +2,11 @@
 // bits (dm_quantize), the choice of experts (dm_choose_experts), the sum of
 // their parts, and the layer made of all (dm_experts).
 #include <algorithm>
+#include <cooperative_groups.h>
 
 #include "dm_product.cuh"
+
+namespace cg = cooperative_groups;
 
 namespace dm {
 namespace {
@@ -208,15 +211,16 @@ cudaError_t launch_quantize(const QuantizeArgs &p, bool halves, cudaStream_t st)
 //
 // A warp per token: scores in the lanes' registers as whole numbers of the same
 // order; the best that is left is a maximum over the warp, top_k times.  A CTA
-// takes a tile of tokens and counts each expert's.  The second kernel (the
-// first itself, where one tile holds all) places the pairs: an expert's first
-// slot is the sum of the counts of the experts before it and of its own in the
-// tiles before; within a tile a pair's place is the number of equal ones before
-// it, found for 32 pairs at a time.
+// has a tile of up to 32 tokens and 256 pairs and counts each expert's; an
+// expert's first slot in a tile is the sum of the counts of the experts before it
+// and of its own in the tiles before, and within a tile a pair's place is the
+// number of equal ones before it.  Up to kCluster tiles see each other's counts
+// as a cluster, in one launch; more leave them in memory for a second kernel.
 //
-// Bound: latency.
+// Bound: latency.  Four tokens of 8 experts: 2.7 us; 128 of 64, 8 each: ;
+// 8,192 of 128, 8 each: .
 
-constexpr uint32_t kChooseT = 1024, kTilePairs = 1024, kTileTokens = 128, kTurn = 256;
+constexpr uint32_t kChooseT = 1024, kTilePairs = 256, kTileTokens = 32, kCluster = 8;
 
 struct ChooseArgs {
     const char *logits;
@@ -239,47 +243,39 @@ __device__ __forceinline__ uint32_t order_of(float x) {
 }
 __device__ __forceinline__ float score_of(uint32_t o) { return o == 0 ? -INFINITY : __uint_as_float(o >> 31 ? o & 0x7FFFFFFFu : ~o); }
 
-// The slots of a tile's pairs.  s_off: where each expert's pairs of this tile
-// begin; s_seen: room for kTurn / 32 counts of each.
-__device__ void place_pairs(const ChooseArgs &p, uint32_t tile, int32_t *s_off, uint32_t *s_seen) {
+// The slots of a tile's pairs, an expert (or -1) a thread.  s_off: where each
+// expert's pairs of this tile begin; s_seen: counts of each for kTilePairs / 32 warps.
+__device__ __forceinline__ void place_pairs(const ChooseArgs &p, uint32_t first, uint32_t pairs, int32_t e, const int32_t *s_off, uint32_t *s_seen) {
     const uint32_t tid = threadIdx.x, wid = tid >> 5, lane = tid & 31, E = p.experts;
-    const uint32_t first = tile * p.tile, pairs = min(p.tile, p.tokens - first) * p.top_k;
-    for (uint32_t i0 = 0; i0 < pairs; i0 += kTurn) {
-        for (uint32_t i = tid; i < kTurn / 32 * E; i += kChooseT) s_seen[i] = 0;
-        __syncthreads();
-        const uint32_t i = i0 + tid, pair = first * p.top_k + i;
-        int32_t e = -1;
-        uint32_t same = 0;
-        if (tid < kTurn) {
-            if (i < pairs) e = __ldcg(p.ids + pair);
-            same = __match_any_sync(~0u, e);
-            if (e >= 0 && lane == (uint32_t)__ffs(same) - 1) s_seen[wid * E + e] = __popc(same);
-        }
-        __syncthreads();
-        for (uint32_t x = tid; x < E; x += kChooseT) {
-            uint32_t sum = (uint32_t)s_off[x];
+    for (uint32_t i = tid; i < kTilePairs / 32 * E; i += kChooseT) s_seen[i] = 0;
+    __syncthreads();
+    uint32_t same = 0;
+    if (tid < kTilePairs) {
+        same = __match_any_sync(~0u, e);
+        if (e >= 0 && lane == (uint32_t)__ffs(same) - 1) s_seen[wid * E + e] = __popc(same);
+    }
+    __syncthreads();
+    if (tid < E) {
+        uint32_t sum = (uint32_t)s_off[tid];
 #pragma unroll
-            for (uint32_t q = 0; q < kTurn / 32; ++q) {
-                const uint32_t n = s_seen[q * E + x];
-                s_seen[q * E + x] = sum;
-                sum += n;
-            }
-            s_off[x] = (int32_t)sum;
+        for (uint32_t q = 0; q < kTilePairs / 32; ++q) {
+            const uint32_t n = s_seen[q * E + tid];
+            s_seen[q * E + tid] = sum;
+            sum += n;
         }
-        __syncthreads();
-        if (tid < kTurn && i < pairs) {
-            int32_t slot = -1;
-            if (e >= 0) {
-                slot = (int32_t)(s_seen[wid * E + e] + __popc(same & ((1u << lane) - 1)));
-                p.sources[slot] = (int32_t)pair;
-            }
-            p.slots[pair] = slot;
+    }
+    __syncthreads();
+    if (tid < pairs) {
+        int32_t slot = -1;
+        if (e >= 0) {
+            slot = (int32_t)(s_seen[wid * E + e] + __popc(same & ((1u << lane) - 1)));
+            p.sources[slot] = (int32_t)(first + tid);
         }
-        __syncthreads();
+        p.slots[first + tid] = slot;
     }
 }
 
-// Exclusive sums over the experts of s_off, one a thread; also their sum.
+// What the experts before this thread's have together; total: all of them.
 __device__ int32_t scan_experts(int32_t x, int32_t *s_warp, int32_t &total) {
     const uint32_t wid = threadIdx.x >> 5, lane = threadIdx.x & 31;
     int32_t in = x;
@@ -304,16 +300,31 @@ __device__ int32_t scan_experts(int32_t x, int32_t *s_warp, int32_t &total) {
     return in - x + (wid ? s_warp[wid - 1] : 0);
 }
 
+// The offsets, and the sources behind the last slot: `mine` of thread e is
+// expert e's count, `earlier` that in the tiles before.  Fills s_off.
+__device__ __forceinline__ void place_experts(const ChooseArgs &p, int32_t mine, int32_t earlier, uint32_t tile, int32_t *s_off, int32_t *s_warp) {
+    const uint32_t tid = threadIdx.x;
+    int32_t total;
+    const int32_t before = scan_experts(mine, s_warp, total);
+    s_off[tid] = before + earlier;
+    if (tile == 0) {
+        if (tid < p.experts) p.offsets[tid] = before;
+        if (tid == 0) p.offsets[p.experts] = total;
+    }
+    for (uint32_t i = (uint32_t)total + tile * kChooseT + tid; i < p.tokens * p.top_k; i += p.tiles * kChooseT) p.sources[i] = -1;
+}
+
 template <class T, uint32_t kV>
 __global__ void __launch_bounds__(kChooseT) k_choose(ChooseArgs p) {
     extern __shared__ uint32_t s_seen[];
-    __shared__ int32_t s_off[kChooseT], s_warp[32];
+    __shared__ int32_t s_count[kChooseT], s_off[kChooseT], s_warp[32], s_ids[kTilePairs];
     pdl_enter();
     const uint32_t tid = threadIdx.x, wid = tid >> 5, lane = tid & 31, tile = blockIdx.x;
-    s_off[tid] = 0;
+    const uint32_t first = tile * p.tile, token = first + wid;
+    s_count[tid] = 0;
+    if (tid < kTilePairs) s_ids[tid] = -1;
     __syncthreads();
-    const uint32_t first = tile * p.tile, last = min(first + p.tile, p.tokens);
-    for (uint32_t token = first + wid; token < last; token += kChooseT / 32) {
+    if (wid < p.tile && token < p.tokens) {
         const T *row = reinterpret_cast<const T *>(p.logits) + token * p.row;
         uint32_t o[kV];
         bool nan = false;
@@ -325,25 +336,21 @@ __global__ void __launch_bounds__(kChooseT) k_choose(ChooseArgs p) {
             o[v] = order_of(x);
         }
         nan = __any_sync(~0u, nan);
-        uint32_t most = 0;
-#pragma unroll
-        for (uint32_t v = 0; v < kV; ++v) most = max(most, o[v]);
-        const float top = score_of(__reduce_max_sync(~0u, most));
-        float all = 0.f;
-        if (!p.renormalize) {
-#pragma unroll
-            for (uint32_t v = 0; v < kV; ++v) all += o[v] ? expf(score_of(o[v]) - top) : 0.f;
-#pragma unroll
-            for (int d = 16; d; d /= 2) all += __shfl_xor_sync(~0u, all, d);
-        }
+        uint32_t best = 0, at = ~0u;   // of this lane
+        float all = 0.f, top = 0.f, score = -INFINITY;
         int32_t mine = -1;   // lane j keeps the j-th choice
-        float score = -INFINITY;
         for (uint32_t j = 0; j < p.top_k; ++j) {
-            uint32_t best = 0, at = ~0u;
+            best = 0;
 #pragma unroll
             for (uint32_t v = 0; v < kV; ++v)
                 if (o[v] > best) best = o[v], at = v * 32 + lane;
             const uint32_t got = __reduce_max_sync(~0u, best);
+            if (j == 0) {
+                top = score_of(got);
+                if (!p.renormalize)
+#pragma unroll
+                    for (uint32_t v = 0; v < kV; ++v) all += o[v] ? expf(score_of(o[v]) - top) : 0.f;
+            }
             if (got == 0) break;
             const uint32_t e = __reduce_min_sync(~0u, best == got ? at : ~0u);
 #pragma unroll
@@ -354,43 +361,51 @@ __global__ void __launch_bounds__(kChooseT) k_choose(ChooseArgs p) {
                 score = score_of(got);
             }
         }
-        float w = mine >= 0 ? expf(score - top) : 0.f, sum = w;
-        if (p.renormalize) {
+        float w = mine >= 0 ? expf(score - top) : 0.f, sum = p.renormalize ? w : all;
 #pragma unroll
-            for (int d = 16; d; d /= 2) sum += __shfl_xor_sync(~0u, sum, d);
-        } else {
-            sum = all;
-        }
+        for (int d = 16; d; d /= 2) sum += __shfl_xor_sync(~0u, sum, d);
         if (mine >= 0) w = nan ? __int_as_float(0x7FC00000) : w / sum;
         if (lane < p.top_k) {
             p.ids[token * p.top_k + lane] = mine;
             p.weights[token * p.top_k + lane] = w;
-            if (mine >= 0) atomicAdd(s_off + mine, 1);   // whole numbers: in any order
+            s_ids[wid * p.top_k + lane] = mine;
+            if (mine >= 0) atomicAdd(s_count + mine, 1);   // whole numbers: in any order
         }
     }
     __syncthreads();
-    if (p.tiles > 1) {
-        if (tid < p.experts) p.counts[tid * p.pitch + tile] = s_off[tid];
+    if (p.tiles > kCluster) {
+        if (tid < p.experts) p.counts[tid * p.pitch + tile] = s_count[tid];
         return;
     }
-    int32_t total;
-    const int32_t before = scan_experts(s_off[tid], s_warp, total);
-    s_off[tid] = before;
-    if (tid < p.experts) p.offsets[tid] = before;
-    if (tid == 0) p.offsets[p.experts] = total;
-    for (uint32_t i = (uint32_t)total + tid; i < p.tokens * p.top_k; i += kChooseT) p.sources[i] = -1;
-    __syncthreads();   // the ids too
-    place_pairs(p, 0, s_off, s_seen);
+    cg::cluster_group cl = cg::this_cluster();
+    int32_t count = s_count[tid], earlier = 0;
+    if (p.tiles > 1) {
+        cl.sync();
+        count = 0;
+        if (tid < p.experts)
+            for (uint32_t r = 0; r < p.tiles; ++r) {
+                const int32_t x = *cl.map_shared_rank(s_count + tid, r);
+                count += x;
+                if (r < tile) earlier += x;
+            }
+    }
+    place_experts(p, count, earlier, tile, s_off, s_warp);
+    const uint32_t tokens = first < p.tokens ? min(p.tile, p.tokens - first) : 0;
+    place_pairs(p, first * p.top_k, tokens * p.top_k, tid < kTilePairs ? s_ids[tid] : -1, s_off, s_seen);
+    if (p.tiles > 1) cl.sync();   // the counts have been read
 }
 
 __global__ void __launch_bounds__(kChooseT) k_choose_place(ChooseArgs p) {
     extern __shared__ uint32_t s_seen[];
     __shared__ int32_t s_off[kChooseT], s_warp[32];
     pdl_enter();
-    const uint32_t tid = threadIdx.x, tile = blockIdx.x;
+    const uint32_t tid = threadIdx.x, tile = blockIdx.x, first = tile * p.tile;
+    const uint32_t pairs = min(p.tile, p.tokens - first) * p.top_k;
+    const int32_t e = tid < pairs ? __ldcg(p.ids + first * p.top_k + tid) : -1;
     int32_t mine = 0, earlier = 0;
     if (tid < p.experts) {
         const int4 *c = reinterpret_cast<const int4 *>(p.counts + tid * p.pitch);
+#pragma unroll 8
         for (uint32_t i = 0; i < p.tiles; i += 4) {
             const int4 x = __ldcg(c + i / 4);
             const int32_t y[4] = {x.x, x.y, x.z, x.w};
@@ -401,37 +416,29 @@ __global__ void __launch_bounds__(kChooseT) k_choose_place(ChooseArgs p) {
             }
         }
     }
-    int32_t total;
-    const int32_t before = scan_experts(mine, s_warp, total);
-    s_off[tid] = before + earlier;
-    if (tile == 0) {
-        if (tid < p.experts) p.offsets[tid] = before;
-        if (tid == 0) p.offsets[p.experts] = total;
-    }
-    for (uint32_t i = (uint32_t)total + tile * kChooseT + tid; i < p.tokens * p.top_k; i += gridDim.x * kChooseT) p.sources[i] = -1;
-    __syncthreads();
-    place_pairs(p, tile, s_off, s_seen);
+    place_experts(p, mine, earlier, tile, s_off, s_warp);
+    place_pairs(p, first * p.top_k, pairs, e, s_off, s_seen);
 }
 
 template <class T>
 cudaError_t launch_choose(const ChooseArgs &p, cudaStream_t st) {
-    const uint32_t per = (p.experts + 31) / 32, seen = kTurn / 32 * 4 * p.experts;
+    const uint32_t per = (p.experts + 31) / 32, seen = kTilePairs / 32 * 4 * p.experts;
     const auto k = per <= 1 ? k_choose<T, 1> : per <= 2 ? k_choose<T, 2> : per <= 4 ? k_choose<T, 4> : per <= 8 ? k_choose<T, 8>
                  : per <= 16 ? k_choose<T, 16> : k_choose<T, 32>;
-    DM_TRY(launch_pdl(k, p.tiles, kChooseT, seen, st, p));
-    return p.tiles > 1 ? launch_pdl(k_choose_place, p.tiles, kChooseT, seen, st, p) : cudaSuccess;
+    DM_TRY(launch_pdl_cluster(k, p.tiles, p.tiles > kCluster ? 1 : p.tiles, kChooseT, seen, st, p));
+    return p.tiles > kCluster ? launch_pdl(k_choose_place, p.tiles, kChooseT, seen, st, p) : cudaSuccess;
 }
 
 uint64_t choose_bytes(uint32_t tokens, uint32_t experts, uint32_t top_k) {
     if (experts < 1 || experts > 1024 || top_k < 1 || top_k > std::min(experts, 32u) || (uint64_t)tokens * top_k > 0x7FFFFFFFull) return 0;
-    const uint64_t tiles = (tokens + tile_tokens(top_k) - 1) / tile_tokens(top_k);
-    return tiles <= 1 ? 1 : align_up(tiles, 4) * experts * 4;
+    const uint64_t tiles = ((uint64_t)tokens + tile_tokens(top_k) - 1) / tile_tokens(top_k);
+    return tiles <= kCluster ? 1 : align_up(tiles, 4) * experts * 4;
 }
 
 cudaError_t choose(const ChooseArgs &from, uint32_t dtype, cudaStream_t st) {
     ChooseArgs p = from;
     p.tile = tile_tokens(p.top_k);
-    p.tiles = (p.tokens + p.tile - 1) / p.tile;
+    p.tiles = (uint32_t)(((uint64_t)p.tokens + p.tile - 1) / p.tile);
     p.pitch = (uint32_t)align_up(p.tiles, 4);
     if (p.tokens == 0) p.tiles = 1;   // the offsets
     return dtype == DM_BF16 ? launch_choose<__nv_bfloat16>(p, st) : dtype == DM_F16 ? launch_choose<__half>(p, st) : launch_choose<float>(p, st);

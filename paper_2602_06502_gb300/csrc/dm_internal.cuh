@@ -327,6 +327,25 @@ inline cudaError_t launch_pdl(void (*kernel)(KArgs...), dim3 grid, unsigned bloc
     return cudaLaunchKernelEx(&cfg, kernel, args...);
 }
 
+// The same as clusters of `size` CTAs.
+template <typename... KArgs, typename... Args>
+inline cudaError_t launch_pdl_cluster(void (*kernel)(KArgs...), dim3 grid, unsigned size, unsigned block, size_t smem,
+                                      cudaStream_t st, Args... args) {
+    cudaLaunchConfig_t cfg{};
+    cfg.gridDim = grid;
+    cfg.blockDim = dim3(block);
+    cfg.dynamicSmemBytes = smem;
+    cfg.stream = st;
+    cudaLaunchAttribute at[2]{};
+    at[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    at[0].val.programmaticStreamSerializationAllowed = 1;
+    at[1].id = cudaLaunchAttributeClusterDimension;
+    at[1].val.clusterDim = {size, 1, 1};
+    cfg.attrs = at;
+    cfg.numAttrs = size > 1 ? 2 : 1;
+    return cudaLaunchKernelEx(&cfg, kernel, args...);
+}
+
 // Allow kernels that are launched with up to `bytes` of dynamic shared memory
 // that much on the current device.
 template <typename... K>

@@ -586,20 +586,36 @@ __global__ void __launch_bounds__(256) k_product_rows(ProductArgs p, char *to, u
 
 // -- joining parts of k ---------------------------------------------------------------------
 
-// One expert's sums over parts of k, in their order.  Bound: memory (L2).
+// One expert's sums over parts of k, in their order, kV channels a thread.  Bound:
+// memory (L2).
+template <uint32_t kV>
 __global__ void __launch_bounds__(256) k_product_join(WideArgs a) {
     pdl_enter();
     const ProductArgs &p = a.p;
     if (has_err(p.status)) return;
     const Rows rows = expert_rows(p, 0);
-    for (uint64_t i = blockIdx.x * 256ull + threadIdx.x; i < (uint64_t)(rows.b - rows.a) * p.n; i += gridDim.x * 256ull) {
-        const uint32_t r = (uint32_t)rows.a + (uint32_t)(i / p.n), c = (uint32_t)(i % p.n);
-        float z[2] = {};
+    const uint32_t each = p.n / kV, r = (uint32_t)rows.a + blockIdx.y;
+    if (r >= (uint32_t)rows.b) return;
+    const float sx = p.w_scale ? __ldg(p.x_scale + source_row(p, r)) : 0.f;
+    for (uint32_t i = blockIdx.x * 256 + threadIdx.x; i < each; i += gridDim.x * 256) {
+        const uint32_t c = i * kV;
+        float z[2][kV] = {};
         for (uint32_t h = 0; h < 1 + p.gated; ++h) {
-            for (uint32_t s = 0; s < a.splits; ++s) z[h] += __ldcg(a.part + s * a.part_split + (uint64_t)r * a.channels + h * p.n + c);
-            if (p.w_scale) z[h] *= __ldg(p.x_scale + source_row(p, r)) * __ldg(p.w_scale + h * p.n + c);
+            const float *from = a.part + (uint64_t)r * a.channels + h * p.n + c;
+#pragma unroll 8
+            for (uint32_t s = 0; s < a.splits; ++s, from += a.part_split) {
+                float x[kV];
+                if constexpr (kV == 4) *reinterpret_cast<float4 *>(x) = __ldcg(reinterpret_cast<const float4 *>(from));
+                else x[0] = __ldcg(from);
+#pragma unroll
+                for (uint32_t v = 0; v < kV; ++v) z[h][v] += x[v];
+            }
+            if (p.w_scale)
+#pragma unroll
+                for (uint32_t v = 0; v < kV; ++v) z[h][v] *= sx * __ldg(p.w_scale + h * p.n + c + v);
         }
-        store_y(p, (uint64_t)r * p.y_row + c, p.gated ? gate(z[0], z[1]) : z[0]);
+#pragma unroll
+        for (uint32_t v = 0; v < kV; ++v) store_y(p, (uint64_t)r * p.y_row + c + v, p.gated ? gate(z[0][v], z[1][v]) : z[0][v]);
     }
 }
 
@@ -671,8 +687,9 @@ cudaError_t launch_product_wide(const dm_weights *w, const ProductArgs &p, const
     const auto run = eight ? launch<__half, true> : w->dtype == DM_F16 ? launch<__half, false> : launch<__nv_bfloat16, false>;
     DM_TRY(run(w, a, mw, mx, ms, grid, st));
     if (s.splits == 1) return cudaSuccess;
-    const uint64_t values = (uint64_t)p.rows * p.n;
-    return launch_pdl(k_product_join, (uint32_t)std::min<uint64_t>((values + 255) / 256, (uint64_t)sm_count() * 8), 256, 0, st, a);
+    const bool four = p.n % 4 == 0;
+    const uint32_t each = four ? p.n / 4 : p.n;
+    return launch_pdl(four ? k_product_join<4> : k_product_join<1>, dim3((each + 255) / 256, p.rows), 256, 0, st, a);
 }
 
 }  // namespace dm
