@@ -225,10 +225,10 @@ constexpr uint32_t kChooseT = 1024, kTilePairs = 256, kTileTokens = 32, kCluster
 struct ChooseArgs {
     const char *logits;
     uint64_t row;   // elements
-    uint32_t tokens, experts, top_k, renormalize, tile, tiles, pitch;   // tokens of a tile; its count; counts between experts
+    uint32_t tokens, experts, top_k, renormalize, tile, tiles;   // tokens of a tile; how many tiles
     int32_t *ids, *offsets, *slots, *sources;
     float *weights;
-    int32_t *counts;   // [expert][tile]
+    int32_t *counts;   // [tile][expert]
 };
 
 uint32_t tile_tokens(uint32_t top_k) { return std::min(kTileTokens, kTilePairs / top_k); }
@@ -374,7 +374,7 @@ __global__ void __launch_bounds__(kChooseT) k_choose(ChooseArgs p) {
     }
     __syncthreads();
     if (p.tiles > kCluster) {
-        if (tid < p.experts) p.counts[tid * p.pitch + tile] = s_count[tid];
+        if (tid < p.experts) p.counts[tile * p.experts + tid] = s_count[tid];
         return;
     }
     cg::cluster_group cl = cg::this_cluster();
@@ -402,20 +402,24 @@ __global__ void __launch_bounds__(kChooseT) k_choose_place(ChooseArgs p) {
     const uint32_t tid = threadIdx.x, tile = blockIdx.x, first = tile * p.tile;
     const uint32_t pairs = min(p.tile, p.tokens - first) * p.top_k;
     const int32_t e = tid < pairs ? __ldcg(p.ids + first * p.top_k + tid) : -1;
-    int32_t mine = 0, earlier = 0;
-    if (tid < p.experts) {
-        const int4 *c = reinterpret_cast<const int4 *>(p.counts + tid * p.pitch);
+    // tiles are shared out to groups of threads, one of them an expert's
+    __shared__ int32_t s_mine[kChooseT], s_earlier[kChooseT];
+    s_mine[tid] = s_earlier[tid] = 0;
+    __syncthreads();
+    const uint32_t groups = kChooseT / p.experts, x = tid % p.experts;
+    if (tid / p.experts < groups) {
+        int32_t mine = 0, earlier = 0;
 #pragma unroll 8
-        for (uint32_t i = 0; i < p.tiles; i += 4) {
-            const int4 x = __ldcg(c + i / 4);
-            const int32_t y[4] = {x.x, x.y, x.z, x.w};
-#pragma unroll
-            for (uint32_t j = 0; j < 4; ++j) {
-                if (i + j < p.tiles) mine += y[j];
-                if (i + j < tile) earlier += y[j];
-            }
+        for (uint32_t i = tid / p.experts; i < p.tiles; i += groups) {
+            const int32_t n = __ldcg(p.counts + i * p.experts + x);
+            mine += n;
+            if (i < tile) earlier += n;
         }
+        atomicAdd(s_mine + x, mine);   // whole numbers: in any order
+        atomicAdd(s_earlier + x, earlier);
     }
+    __syncthreads();
+    const int32_t mine = s_mine[tid], earlier = s_earlier[tid];
     place_experts(p, mine, earlier, tile, s_off, s_warp);
     place_pairs(p, first * p.top_k, pairs, e, s_off, s_seen);
 }
@@ -432,14 +436,13 @@ cudaError_t launch_choose(const ChooseArgs &p, cudaStream_t st) {
 uint64_t choose_bytes(uint32_t tokens, uint32_t experts, uint32_t top_k) {
     if (experts < 1 || experts > 1024 || top_k < 1 || top_k > std::min(experts, 32u) || (uint64_t)tokens * top_k > 0x7FFFFFFFull) return 0;
     const uint64_t tiles = ((uint64_t)tokens + tile_tokens(top_k) - 1) / tile_tokens(top_k);
-    return tiles <= kCluster ? 1 : align_up(tiles, 4) * experts * 4;
+    return tiles <= kCluster ? 1 : tiles * experts * 4;
 }
 
 cudaError_t choose(const ChooseArgs &from, uint32_t dtype, cudaStream_t st) {
     ChooseArgs p = from;
     p.tile = tile_tokens(p.top_k);
     p.tiles = (uint32_t)(((uint64_t)p.tokens + p.tile - 1) / p.tile);
-    p.pitch = (uint32_t)align_up(p.tiles, 4);
     if (p.tokens == 0) p.tiles = 1;   // the offsets
     return dtype == DM_BF16 ? launch_choose<__nv_bfloat16>(p, st) : dtype == DM_F16 ? launch_choose<__half>(p, st) : launch_choose<float>(p, st);
 }
