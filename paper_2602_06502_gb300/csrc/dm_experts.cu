@@ -47,11 +47,10 @@ __device__ __forceinline__ float score_at(const float *p) { return *p; }
 // registers of a warp (up to 2,048 values) or of a CTA (up to 16,384); a longer
 // one is read twice.
 //
-// 127 x is exact in 32 bits, and 127 x / top lies on a border between two steps,
-// or at least 1 / 4096 away from one (x and top have up to 11 bits).  The product
-// with 127 / top is off by less than 2^-16, so it decides all but what is near a
-// border, and there the exact division does: q is what the formula says to the
-// last case.
+// The product with 127 / top is off by less than 2^-16 and gives a step r.  What
+// is left, 127 x - r top, is exact in 32 bits (x and top have up to 11 bits), and
+// where it is about half of top or more it corrects r: q is what the formula
+// says to the last case.
 
 struct QuantizeArgs {
     const char *x;
@@ -72,7 +71,7 @@ __device__ __forceinline__ uint32_t larger2(uint32_t a, uint32_t b) { return __v
 constexpr float kRound = 12582912.f;
 
 template <class T, bool kHalves, bool kNorm, uint32_t kLanes, uint32_t kHeld>
-__global__ void __launch_bounds__(256, kHeld <= 2 ? 5 : kHeld <= 4 ? 4 : 3) k_quantize(QuantizeArgs p) {
+__global__ void __launch_bounds__(256, kHeld <= 2 ? 6 : kHeld <= 4 ? 4 : 3) k_quantize(QuantizeArgs p) {
     constexpr uint32_t kPer = 256 / kLanes;   // rows of a CTA; kHeld: vectors of 8 values a lane keeps
     constexpr uint32_t kFinite = std::is_same_v<T, __half> ? 0x7C00 : 0x7F80;
     __shared__ uint32_t s_top[8];
@@ -137,23 +136,33 @@ __global__ void __launch_bounds__(256, kHeld <= 2 ? 5 : kHeld <= 4 ? 4 : 3) k_qu
         float scale = __fdiv_rn(top, 127.f);
         if constexpr (kNorm) scale *= rsqrtf(sum / (float)p.k + p.eps);
         if (lane == 0) p.scale[r] = finite ? scale : __int_as_float(0x7FC00000);
-        // powers of two keep 127 / top and 127 x in range
+        // a power of two keeps 127 / top and 127 x in range
         const float shift = top > 1e30f ? 0x1p-64f : top < 1e-30f ? 0x1p64f : 1.f;
         const float big = top * shift, by = bits == 0 || !finite ? 0.f : __fdiv_rn(127.f, big);
-        auto put = [&](const uint4 &v, uint32_t at) {
+        const uint32_t keep = finite ? ~0u : 0u;
+        auto put = [&](uint4 v, uint32_t at) {
             float f[8], far = 0.f;
             uint32_t n[8];   // kRound + the step
+            v.x &= keep, v.y &= keep, v.z &= keep, v.w &= keep;
             unpack<T>(v, f);
+            if (shift != 1.f)
+#pragma unroll
+                for (int i = 0; i < 8; ++i) f[i] *= shift;
 #pragma unroll
             for (int i = 0; i < 8; ++i) {
-                f[i] = by == 0.f ? 0.f : f[i] * shift;
                 const float y = __fmaf_rn(f[i], by, kRound);
                 n[i] = __float_as_uint(y);
                 far = fmaxf(far, fabsf(__fmaf_rn(f[i], by, kRound - y)));
             }
             if (far > 0.5f - 0x1p-15f) {
+                const float half = 0.5f * big;
 #pragma unroll
-                for (int i = 0; i < 8; ++i) n[i] = __float_as_uint(rintf(__fdiv_rn(f[i] * 127.f, big)) + kRound);
+                for (int i = 0; i < 8; ++i) {
+                    const float e = __fmaf_rn(kRound - __uint_as_float(n[i]), big, 127.f * f[i]);
+                    const uint32_t odd = n[i] & 1;   // ties to even
+                    if (e > half || (e == half && odd)) ++n[i];
+                    else if (e < -half || (e == -half && odd)) --n[i];
+                }
             }
             if constexpr (kHalves) {
                 // 1536 + the step is a half with the step in its low bits
@@ -195,10 +204,12 @@ __global__ void __launch_bounds__(256, kHeld <= 2 ? 5 : kHeld <= 4 ? 4 : 3) k_qu
 
 template <class T, bool kHalves, bool kNorm>
 cudaError_t launch_quantize(const QuantizeArgs &p, cudaStream_t st) {
-    const auto by_warps = p.k <= 512 ? k_quantize<T, kHalves, kNorm, 32, 2> : p.k <= 1024 ? k_quantize<T, kHalves, kNorm, 32, 4> : k_quantize<T, kHalves, kNorm, 32, 8>;
-    const auto by_ctas = p.k <= 4096 ? k_quantize<T, kHalves, kNorm, 256, 2> : p.k <= 8192 ? k_quantize<T, kHalves, kNorm, 256, 4> : k_quantize<T, kHalves, kNorm, 256, 8>;
-    const uint32_t sms = (uint32_t)sm_count(), ctas = p.k <= 2048 ? (p.rows + 7) / 8 : p.rows;
-    return launch_pdl(p.k <= 2048 ? by_warps : by_ctas, std::min(ctas, sms * 8), 256, 0, st, p);
+    if (p.k <= 2048) {
+        const auto k = p.k <= 512 ? k_quantize<T, kHalves, kNorm, 32, 2> : p.k <= 1024 ? k_quantize<T, kHalves, kNorm, 32, 4> : k_quantize<T, kHalves, kNorm, 32, 8>;
+        return launch_pdl(k, (p.rows + 7) / 8, 256, 0, st, p);
+    }
+    const auto k = p.k <= 4096 ? k_quantize<T, kHalves, kNorm, 256, 2> : p.k <= 8192 ? k_quantize<T, kHalves, kNorm, 256, 4> : k_quantize<T, kHalves, kNorm, 256, 8>;
+    return launch_pdl(k, p.rows, 256, 0, st, p);
 }
 
 template <class T>

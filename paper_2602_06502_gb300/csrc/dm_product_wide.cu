@@ -560,27 +560,30 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(Wide<kEight>::kThrea
 
 // -- rows laid out for the tensor maps ----------------------------------------------------
 
-// Row r of `to` is the row of x that row r reads, 8-bit values as halves, 16
-// bytes of the result a thread.
+// Row r of `to` is the row of x that row r reads, 8-bit values as halves: a warp
+// a row.  Bound: memory, 2 bytes written for each value that is read.
 template <bool kEight>
 __global__ void __launch_bounds__(256) k_product_rows(ProductArgs p, char *to, uint64_t to_row) {
     pdl_enter();
     if (has_err(p.status)) return;
     const int32_t lo = p.offsets ? max(__ldcg(p.offsets), 0) : 0;
     const int32_t hi = p.offsets ? min(__ldcg(p.offsets + p.experts), (int32_t)p.rows) : (int32_t)p.rows;
-    const uint32_t each = (p.k + 7) / 8;
-    for (uint64_t i = blockIdx.x * 256ull + threadIdx.x; hi > lo && i < (uint64_t)(hi - lo) * each; i += gridDim.x * 256ull) {
-        const uint32_t r = (uint32_t)lo + (uint32_t)(i / each), at = (uint32_t)(i % each);
-        const char *x = p.x + source_row(p, r) * p.x_row;
-        uint4 y;
-        if constexpr (kEight) {
-            const uint2 v = *reinterpret_cast<const uint2 *>(x + at * 8);
-            bytes_to_halves(v.x, y.x, y.y);
-            bytes_to_halves(v.y, y.z, y.w);
-        } else {
-            y = *reinterpret_cast<const uint4 *>(x + at * 16);
+    const uint32_t each = (p.k + 7) / 8, lane = threadIdx.x & 31;
+    for (int64_t r = lo + blockIdx.x * 8ll + threadIdx.x / 32; r < hi; r += gridDim.x * 8ll) {
+        const char *x = p.x + source_row(p, (uint32_t)r) * p.x_row;
+        uint4 *y = reinterpret_cast<uint4 *>(to + (uint64_t)r * to_row);
+#pragma unroll 8
+        for (uint32_t at = lane; at < each; at += 32) {
+            uint4 v;
+            if constexpr (kEight) {
+                const uint2 b = __ldg(reinterpret_cast<const uint2 *>(x) + at);
+                bytes_to_halves(b.x, v.x, v.y);
+                bytes_to_halves(b.y, v.z, v.w);
+            } else {
+                v = __ldg(reinterpret_cast<const uint4 *>(x) + at);
+            }
+            y[at] = v;
         }
-        *reinterpret_cast<uint4 *>(to + r * to_row + at * 16) = y;
     }
 }
 
@@ -671,8 +674,7 @@ cudaError_t launch_product_wide(const dm_weights *w, const ProductArgs &p, const
     const char *x = p.x;
     uint64_t x_row = p.x_rows > 1 ? p.x_row : s.x_row, x_rows = p.x_rows;
     if (s.x_bytes) {
-        const uint64_t vectors = (uint64_t)p.rows * ((p.k + 7) / 8);
-        const uint32_t grid = (uint32_t)std::min<uint64_t>((vectors + 255) / 256, (uint64_t)sm_count() * 8);
+        const uint32_t grid = std::min((p.rows + 7) / 8, (uint32_t)sm_count() * 64);
         char *to = static_cast<char *>(work);
         const auto lay = eight ? k_product_rows<true> : k_product_rows<false>;
         DM_TRY(launch_pdl(lay, grid, 256, 0, st, p, to, s.x_row));

@@ -41,7 +41,7 @@ def _size(name, device, key, *args):
 
 def _call(name, device, *args):
     """Enqueues a C call on torch's current stream of the device."""
-    if torch.cuda.current_device() != device.index:
+    if torch._C._cuda_getDevice() != device.index:
         with torch.cuda.device(device):
             return _call(name, device, *args)
     rc = getattr(D.lib(), name)(*args, torch._C._cuda_getCurrentRawStream(device.index))
