@@ -21,7 +21,6 @@ namespace {
 // out k, 64 bytes at a time, and add their sums up in the order of the warps.
 
 constexpr uint32_t kFewT = 256, kFewWarps = 8;
-constexpr uint32_t kFewRows = 8;   // an expert's, on average, up to which this kernel has them
 
 template <class T>
 struct Few;   // T: of the weights and rows
@@ -54,32 +53,40 @@ struct Few<int8_t> {
     static __device__ __forceinline__ void mma(float *c, const uint32_t *a, uint32_t b0, uint32_t b1) { Few<__half>::mma(c, a, b0, b1); }
 };
 
-// 16 bytes of a row from byte `at` on; zeros from byte `end` on.
-__device__ __forceinline__ uint4 load16(const char *row, uint32_t at, uint32_t end) {
-    if (at >= end) return make_uint4(0, 0, 0, 0);
-    uint4 x = *reinterpret_cast<const uint4 *>(row + at);
-    if (end - at < 16) {
-        uint32_t *w = reinterpret_cast<uint32_t *>(&x);
-#pragma unroll
-        for (uint32_t i = 0; i < 4; ++i) {
-            const uint32_t left = end - at > 4 * i ? min(end - at - 4 * i, 4u) : 0;
-            w[i] = left == 4 ? w[i] : w[i] & ((1u << 8 * left) - 1);
-        }
-    }
+// 16 bytes.  In the order of the program: the compiler would else move a load
+// down to its use, and the next would wait for it.
+__device__ __forceinline__ uint4 load16(const char *p) {
+    uint4 x;
+    asm volatile("ld.global.nc.L1::no_allocate.v4.u32 {%0, %1, %2, %3}, [%4];" : "=r"(x.x), "=r"(x.y), "=r"(x.z), "=r"(x.w) : "l"(p));
     return x;
 }
+__device__ __forceinline__ uint4 load16_kept(const char *p) {   // that other warps of the SM want too
+    uint4 x;
+    asm volatile("ld.global.nc.v4.u32 {%0, %1, %2, %3}, [%4];" : "=r"(x.x), "=r"(x.y), "=r"(x.z), "=r"(x.w) : "l"(p));
+    return x;
+}
+// Zeros in the place of what lies `left` bytes and more from the first.
+__device__ __forceinline__ void cut16(uint4 &x, int32_t left) {
+    uint32_t *w = reinterpret_cast<uint32_t *>(&x);
+#pragma unroll
+    for (int32_t i = 0; i < 4; ++i) {
+        const int32_t n = min(max(left - 4 * i, 0), 4);
+        w[i] = n == 4 ? w[i] : w[i] & ((1u << 8 * n) - 1);
+    }
+}
 
-// kTiles: 8-row tiles at a time; kM: 16-channel tiles (2: gated).
-template <class T, int kTiles, int kM>
-__global__ void __launch_bounds__(kFewT, 2) k_product_few(ProductArgs p) {
-    constexpr uint32_t kCols = 16 * kM + 4, kU = 4;
+// kTiles: 8-row tiles at a time; kM: 16-channel tiles (2: gated); kU: of a warp's
+// steps of k, those whose loads are on their way together.
+template <class T, int kTiles, int kM, uint32_t kU>
+__global__ void __launch_bounds__(kFewT, kM * kTiles <= 2 ? 3 : 2) k_product_few(ProductArgs p) {
+    constexpr uint32_t kCols = 16 * kM + 4;
     __shared__ float s_red[kFewWarps][8 * kTiles][kCols];
     pdl_enter();
     if (__syncthreads_or(has_err(p.status))) return;
     const uint32_t tid = threadIdx.x, wid = tid >> 5, lane = tid & 31, g = lane >> 2, t = lane & 3;
     const uint32_t e = blockIdx.y, c0 = blockIdx.x * 16;
     const Rows rows = expert_rows(p, e);
-    const uint32_t end = p.k * (uint32_t)sizeof(T), chunks = (end + 63) / 64;
+    const uint32_t end = p.k * (uint32_t)sizeof(T), chunks = (end + 63) / 64, last = (end - 1) / 16 * 16;
     const char *w[kM][2];
 #pragma unroll
     for (int m = 0; m < kM; ++m)
@@ -94,13 +101,25 @@ __global__ void __launch_bounds__(kFewT, 2) k_product_few(ProductArgs p) {
             uint4 wv[kU][kM][2], xv[kU][kTiles];
 #pragma unroll
             for (uint32_t u = 0; u < kU; ++u) {
-                const uint32_t at = (c + kFewWarps * u) * 64 + t * 16;
+                const uint32_t at = min((c + kFewWarps * u) * 64 + t * 16, last);   // what is beyond the end becomes zero below
 #pragma unroll
                 for (int m = 0; m < kM; ++m)
 #pragma unroll
-                    for (int h = 0; h < 2; ++h) wv[u][m][h] = load16(w[m][h], at, end);
+                    for (int h = 0; h < 2; ++h) wv[u][m][h] = load16(w[m][h] + at);
 #pragma unroll
-                for (int j = 0; j < kTiles; ++j) xv[u][j] = load16(x[j], at, end);
+                for (int j = 0; j < kTiles; ++j) xv[u][j] = load16_kept(x[j] + at);
+            }
+            if ((c + kFewWarps * (kU - 1) + 1) * 64 > end) {
+#pragma unroll
+                for (uint32_t u = 0; u < kU; ++u) {
+                    const int32_t left = (int32_t)end - (int32_t)((c + kFewWarps * u) * 64 + t * 16);
+#pragma unroll
+                    for (int m = 0; m < kM; ++m)
+#pragma unroll
+                        for (int h = 0; h < 2; ++h) cut16(wv[u][m][h], left);
+#pragma unroll
+                    for (int j = 0; j < kTiles; ++j) cut16(xv[u][j], left);
+                }
             }
 #pragma unroll
             for (uint32_t u = 0; u < kU; ++u)
@@ -147,16 +166,22 @@ __global__ void __launch_bounds__(kFewT, 2) k_product_few(ProductArgs p) {
     }
 }
 
-template <class T, int kTiles>
+template <class T, int kTiles, uint32_t kU>
 cudaError_t launch_few_tiles(const ProductArgs &p, cudaStream_t st) {
     const dim3 grid((p.n + 15) / 16, p.experts);
-    return p.gated ? launch_pdl(k_product_few<T, kTiles, 2>, grid, kFewT, 0, st, p) : launch_pdl(k_product_few<T, kTiles, 1>, grid, kFewT, 0, st, p);
+    return launch_pdl(p.gated ? k_product_few<T, kTiles, 2, kU> : k_product_few<T, kTiles, 1, kU>, grid, kFewT, 0, st, p);
 }
 
 template <class T>
 cudaError_t launch_few(const ProductArgs &p, cudaStream_t st) {
     const uint32_t each = (p.rows + p.experts - 1) / p.experts;
-    return each <= 8 ? launch_few_tiles<T, 1>(p, st) : launch_few_tiles<T, 2>(p, st);
+    if (each > 16) return launch_few_tiles<T, 4, 2>(p, st);
+    if (each > 8) return launch_few_tiles<T, 2, 2>(p, st);
+    // Two steps are all that a warp has of short rows (1,536 x 1,024 in 8 bits:
+    // 3.4 us; with four, half of which are thrown away, 5.3), and as many as
+    // registers hold of gated ones (eight experts' 4,096 x 1,024: 8.7 us, 9.9
+    // with four); else four (6,144 x 4,096 in 8 bits: 7.7 us, 8.1 with two).
+    return p.gated || p.k * sizeof(T) <= 64 * kFewWarps * 2 ? launch_few_tiles<T, 1, 2>(p, st) : launch_few_tiles<T, 1, 4>(p, st);
 }
 
 }  // namespace
@@ -173,7 +198,17 @@ ProductArgs product_args(const dm_weights *w, const dm_product_args *a) {
     return p;
 }
 
-static bool many_rows(const dm_weights *w, uint32_t rows) { return rows > kFewRows * (uint64_t)w->experts; }
+// Which kernel has a product.  An expert's weights are read again for every 32
+// rows by the one for few rows, and through more hands by the other.  With 64
+// experts of 2,048 x 2,048 and 16 rows each 106 and 91 us (bf16), 77 and 77 (8
+// bits), with 8 rows 89 and 89, 64 and 76; where some experts have many more
+// rows than others, an average of 16 is 140 and 88 us (8 bits).  One of 6,144 x 4,096 with 16 rows 10
+// and 12, 9 and 20, with 32 rows 18 and 13, 16 and 20 us; one of 1,536 x 1,024
+// with 64 rows 6.6 and 9.9, 6.9 and 15.
+static bool many_rows(const dm_weights *w, uint32_t rows) {
+    const uint64_t bytes = (uint64_t)w->experts * w->n * w->k * dtype_size(w->dtype);
+    return rows > w->experts * (bytes <= (4u << 20) ? 64ull : bytes <= (32u << 20) ? 32ull : w->experts == 1 ? 16ull : 8ull);
+}
 
 bool takes_halves(const dm_weights *w, uint32_t rows) { return w->dtype == DM_I8 && many_rows(w, rows); }
 
