@@ -181,7 +181,8 @@ cudaError_t launch_few(const ProductArgs &p, cudaStream_t st) {
     // 3.4 us; with four, half of which are thrown away, 5.3), and as many as
     // registers hold of gated ones (eight experts' 4,096 x 1,024: 8.7 us, 9.9
     // with four); else four (6,144 x 4,096 in 8 bits: 7.7 us, 8.1 with two).
-    return p.gated || p.k * sizeof(T) <= 64 * kFewWarps * 2 ? launch_few_tiles<T, 1, 2>(p, st) : launch_few_tiles<T, 1, 4>(p, st);
+    if (p.gated || p.k * sizeof(T) <= 64 * kFewWarps * 2) return launch_few_tiles<T, 1, 2>(p, st);
+    return launch_pdl(k_product_few<T, 1, 1, 4>, dim3((p.n + 15) / 16, p.experts), kFewT, 0, st, p);
 }
 
 }  // namespace

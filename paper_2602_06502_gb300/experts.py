@@ -99,6 +99,13 @@ def _eps(eps):
     return eps
 
 
+def last_error(status):
+    """The status of the first product that failed on the device among those of
+    weights that share `status`, which it clears (synchronises)."""
+    with torch.cuda.device(status.device):
+        return D.dm_products_last_error(status, torch._C._cuda_getCurrentRawStream(status.device.index))
+
+
 def quantize(x, *, eps=None, count=None):
     """(q, scale): the rows of x [rows, k], bfloat16 or float16, in 8 bits: q
     int8 [rows, k] = 127 x / max |x| rounded, scale float32 [rows].  eps: rows
@@ -119,9 +126,10 @@ def quantize(x, *, eps=None, count=None):
 class Weights:
     """Weights of a product, w [n, k], or of many experts', [experts, n, k]:
     bfloat16 or float16, or int8 with scale float32 [(experts,) n].  Keeps the
-    tensors; calls that fail on the device say so in last_error()."""
+    tensors; calls that fail on the device say so in last_error().  status: an
+    int32 tensor of one element, 0, that several share, to be asked once."""
 
-    def __init__(self, w, scale=None):
+    def __init__(self, w, scale=None, *, status=None):
         if w.dim() not in (2, 3) or w.numel() == 0 or w.shape[-1] > 1 and w.stride(-1) != 1:
             raise ValueError("weights are [n, k] or [experts, n, k], not empty, the last dimension contiguous")
         if (w.dtype is torch.int8) != (scale is not None) or (scale is None and w.dtype not in TYPES):
@@ -144,23 +152,25 @@ class Weights:
                                    D.DM_I8 if scale is not None else TYPES[w.dtype], self.experts, self.n, self.k, row,
                                    w.stride(0) if self.experts > 1 else 0)
         self.ref, self.key = C.byref(self.struct), (w.dtype, self.experts, self.n, self.k)
-        self.status = torch.zeros(1, dtype=torch.int32, device=self.device)
-        self.status_at = self.status.data_ptr()
+        if status is None:
+            status = torch.zeros(1, dtype=torch.int32, device=self.device)
+        self.status = status
+        self.status_at = _vector("status", status, torch.int32, self.device, 1)
         self._streams = set()   # whose work may still use the weights
-        _size("dm_product_bytes", self.device, (self.key, 0, 0, 0), self.ref, 0, 0, 0)   # refuses what is no set of weights
+        if not D.dm_product_bytes(self.struct, 0):   # no set of weights: rows or experts that begin off 16 bytes, too many
+            raise D.DualMapError(D.DM_ERR_INVALID_ARG, "dm_product_bytes")
 
     @classmethod
-    def quantized(cls, w):
+    def quantized(cls, w, *, status=None):
         """8-bit weights, a scale a channel, of bfloat16 or float16 ones."""
         q, scale = quantize(w.detach().flatten(0, -2))
         if w.dim() == 3:
             q, scale = q.unflatten(0, w.shape[:2]), scale.unflatten(0, w.shape[:2])
-        return cls(q, scale)
+        return cls(q, scale, status=status)
 
     def last_error(self):
         """The status of the first product that failed on the device, which it clears (synchronises)."""
-        with torch.cuda.device(self.device):
-            return D.dm_products_last_error(self.status, torch._C._cuda_getCurrentRawStream(self.device.index))
+        return last_error(self.status)
 
     def hold(self):
         """Keeps the memory, once it is dropped, from being given out before the
@@ -174,7 +184,7 @@ class Weights:
             self._streams.add(raw)
 
 
-def product(x, weights, offsets=None, *, x_scale=None, sources=None, per_source=1, gated=False, rows=None, out=None, dtype=None):
+def product(x, weights, offsets=None, *, x_scale=None, sources=None, per_source=1, gated=False, out=None, dtype=None):
     """Rows times their expert's weights: y [rows, n], or [rows, n / 2] where
     gated: silu of the first half of the channels times the second.
 

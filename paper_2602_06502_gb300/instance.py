@@ -8,6 +8,11 @@ what it holds of their prefixes, their other tokens run through the layers
 (append, then attention that reads a shared prefix once), some tokens are
 decoded greedily, and the sequences stay as prefixes for later requests until
 their pages are needed.  One JSON line per batch.
+
+    ... --experts 8 --top-k 2 --eight-bits
+
+adds a layer of experts after each attention, and keeps the projections' and the
+experts' weights in 8 bits.
 """
 
 import argparse
@@ -22,14 +27,17 @@ import torch
 
 from . import dualmap as D
 from .cache import PagedCache
+from .experts import Experts, Linear, Weights, last_error
 
 
 class Instance:
     """A decoder of `layers` attention layers with random weights over a
-    PagedCache: admit() prompts, decode() greedily, keep or drop()."""
+    PagedCache: admit() prompts, decode() greedily, keep or drop().  experts: a
+    layer of so many of width `expert_width` (default: the model's) after each
+    attention, top_k a token; eight_bits: projections and experts in 8 bits."""
 
     def __init__(self, *, pages, max_tokens, max_seqs=512, page_tokens=16, layers=2, q_heads=16, kv_heads=4, head_dim=64,
-                 vocab=32000, dtype=torch.bfloat16, seed=0, device="cuda"):
+                 vocab=32000, dtype=torch.bfloat16, seed=0, device="cuda", experts=0, top_k=2, expert_width=None, eight_bits=False):
         self.cache = PagedCache.empty(pages=pages, kv_heads=kv_heads, head_dim=head_dim, max_seqs=max_seqs, max_tokens=max_tokens,
                                       page_tokens=page_tokens, layers=layers, dtype=dtype, device=device)
         self.device, self.layers, self.q_heads, self.kv_heads, self.dim = device, layers, q_heads, kv_heads, head_dim
@@ -46,6 +54,21 @@ class Instance:
         angle = torch.arange(max_tokens, device=device, dtype=torch.float64)[:, None] * \
             10_000.0 ** (-torch.arange(0, head_dim, 2, device=device, dtype=torch.float64) / head_dim)
         self.cos, self.sin = angle.cos().float(), angle.sin().float()
+        self.status, self.gates, self.experts, self.linears = None, [], [], []
+        if experts or eight_bits:
+            self.status = torch.zeros(1, dtype=torch.int32, device=device)   # of all products, asked once a step
+        if eight_bits:   # (queries, keys and values; output) of each layer
+            self.linears = [[Linear(Weights.quantized(w.T.contiguous(), status=self.status)) for w in pair]
+                            for pair in zip(self.qkv, self.out)]
+            self.qkv, self.out = [], []
+        for _ in range(layers if experts else 0):
+            m = expert_width or width
+            self.gates.append(weight(width, experts))
+            pair = []
+            for n, k in ((2 * m, width), (width, m)):
+                w = (torch.randn(experts, n, k, generator=gen, device=device) * k ** -0.5).to(dtype)
+                pair.append(Weights.quantized(w, status=self.status) if eight_bits else Weights(w, status=self.status))
+            self.experts.append(Experts(*pair, top_k))
         self.tokens = {}        # sequence -> its tokens, oldest first
         self.serial = {}        # sequence -> its number among all that were ever admitted (ids are given out again)
         self.origin = {}        # sequence -> (serial of the sequence it forked from or -1, tokens it kept)
@@ -161,6 +184,10 @@ class Instance:
                 last = self.origin[s]
         return self._ints(offsets + [len(seqs)]), self._ints(prefix)
 
+    @staticmethod
+    def _normed(x):
+        return (x.float() * torch.rsqrt(x.float().square().mean(-1, keepdim=True) + 1e-6)).to(x.dtype)
+
     def _forward(self, seqs, news):
         """Appends the new tokens of each sequence and returns the logits of its last one.
         A step that the cache refused raises DualMapError (synchronises)."""
@@ -172,21 +199,29 @@ class Instance:
         plan = self.cache.plan(ids, at, T, hq, *self.groups(seqs))   # once for all layers
         x = self.embedding[torch.from_numpy(np.concatenate(news).astype(np.int64)).to(self.device)]
         for layer in range(self.layers):
-            h = (x.float() * torch.rsqrt(x.float().square().mean(-1, keepdim=True) + 1e-6)).to(x.dtype)
-            qkv = (h @ self.qkv[layer]).view(T, hq + 2 * hk, d)
+            if self.linears:   # their rows are divided by their root mean square when they are quantised
+                qkv = self.linears[layer][0](x, eps=1e-6).view(T, hq + 2 * hk, d)
+            else:
+                qkv = (self._normed(x) @ self.qkv[layer]).view(T, hq + 2 * hk, d)
             qw, kw = self.norms[layer]
             q = self.cache.append(ids, at, qkv[:, :hq], qkv[:, hq:hq + hk], qkv[:, hq + hk:], self.cos, self.sin, layer=layer,
                                   q_weight=qw, k_weight=kw)
-            x = x + self.cache.attend(plan, q, layer=layer).view(T, hq * d) @ self.out[layer]
+            o = self.cache.attend(plan, q, layer=layer).view(T, hq * d)
+            x = x + (self.linears[layer][1](o) if self.linears else o @ self.out[layer])
+            if self.experts:
+                h = self._normed(x)
+                x = self.experts[layer](h, h @ self.gates[layer], residual=x)
         err = self.cache.last_error()
+        if self.status is not None:
+            err = last_error(self.status) or err
         if err:
             raise D.DualMapError(err, "instance")
         self.computed += T
         return x[at[1:].long() - 1] @ self.embedding.T
 
 
-def run(workload_name, instance=0, batches=4, decode=16, overrides=None, pages=8192, device="cuda:0"):
-    """Yields one dict per batch of the trace."""
+def run(workload_name, instance=0, batches=4, decode=16, overrides=None, pages=8192, device="cuda:0", **model):
+    """Yields one dict per batch of the trace.  model: of Instance."""
     sys.path.insert(0, os.path.dirname(os.path.dirname(os.path.abspath(__file__))))
     from tracegen import Trace, workload
 
@@ -196,7 +231,7 @@ def run(workload_name, instance=0, batches=4, decode=16, overrides=None, pages=8
     tr = Trace(w)
     longest = int(max(tr.L)) + decode
     node = Instance(pages=pages, max_tokens=longest, max_seqs=w["batch"] + 256, page_tokens=w["block_tokens"], vocab=w["vocab"],
-                    device=device)
+                    device=device, **model)
     g = Scheduler(block_tokens=w["block_tokens"], route_prefix_blocks=w["route_prefix_blocks"], vnodes=w["vnodes"],
                   max_instances=tr.max_instance_id() + 1, capacity=w["capacity"], slo_us=w["slo_us"], cost_us=w["cost_us"],
                   max_batch=w["batch"], max_batch_tokens=max(int(tr.batch_layout(b)[4]) for b in range(len(tr.batches))) + (1 << 16),
@@ -246,13 +281,17 @@ def main():
     ap.add_argument("--batches", type=int, default=4)
     ap.add_argument("--decode", type=int, default=16, help="tokens decoded per request")
     ap.add_argument("--pages", type=int, default=8192)
+    ap.add_argument("--experts", type=int, default=0, help="experts of a layer after each attention")
+    ap.add_argument("--top-k", type=int, default=2, help="experts that a token goes to")
+    ap.add_argument("--eight-bits", action="store_true", help="projections and experts in 8 bits")
     ap.add_argument("--set", action="append", default=[], metavar="KEY=VALUE", help="override a workload field")
     args = ap.parse_args()
     over = {}
     for kv in args.set:
         k, v = kv.split("=", 1)
         over[k] = float(v) if "." in v else int(v)
-    for row in run(args.workload, args.instance, args.batches, args.decode, over, args.pages):
+    for row in run(args.workload, args.instance, args.batches, args.decode, over, args.pages, experts=args.experts,
+                   top_k=args.top_k, eight_bits=args.eight_bits):
         print(json.dumps(row), flush=True)
 
 
