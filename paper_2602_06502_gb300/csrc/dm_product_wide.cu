@@ -32,9 +32,8 @@ struct Wide {
     static constexpr uint32_t kX = kW, kStage = kW + kHalf * (kStep / 64);
     static constexpr uint32_t kA = 2 * kRows, kAs = (512 - kA) / 32;  // 8-bit: columns of the weights in tensor memory, in places of 64 elements of k
     static constexpr uint32_t kSwap = kStages * kStage;               // gated: 32 rows of 64 channels, floats
-    static constexpr uint32_t kFirst = kSwap + 32 * 64 * 4;           // tiles before each expert, widest tiles first
-    static constexpr uint32_t kOrder = kFirst + 1032 * 4;             // those experts (16 bits)
-    static constexpr uint32_t kBars = kOrder + 1024 * 2;
+    static constexpr uint32_t kFirst = kSwap + 32 * 64 * 4;           // tiles before each expert
+    static constexpr uint32_t kBars = kFirst + 1032 * 4;
     // per stage: full (the pair's), empty, weights full, weights empty; per
     // buffer of sums: full, empty (the pair's); per place of weights: full (the
     // pair's), empty
@@ -163,7 +162,6 @@ __device__ __forceinline__ uint32_t block_rows(uint32_t rows) {
 
 struct Line {   // of tiles
     const uint32_t *first;
-    const uint16_t *order;
     uint32_t tiles, pair, pairs;
 };
 
@@ -177,7 +175,7 @@ __device__ __forceinline__ Tile tile_at(const WideArgs &a, const Line &l, uint32
         else hi = mid;
     }
     Tile t;
-    t.e = l.order[lo];
+    t.e = lo;
     const int32_t from = a.p.offsets ? __ldcg(a.p.offsets + t.e) : 0, to = a.p.offsets ? __ldcg(a.p.offsets + t.e + 1) : (int32_t)a.p.rows;
     const uint32_t rows = (uint32_t)(to - from), n = row_blocks<kRows>(rows), each = block_rows<kRows>(rows);
     uint32_t x = i - l.first[lo];
@@ -191,10 +189,7 @@ __device__ __forceinline__ Tile tile_at(const WideArgs &a, const Line &l, uint32
     return t;
 }
 
-// A pair's tiles, and their steps of k.  The line begins with the widest tiles
-// and pairs take turns in alternating order, so each has about as much to do:
-// with the experts' own order pairs differed by 9 to 12% (32 experts of 27 to
-// 1,862 rows).
+// A pair's tiles, in turn with the other pairs, and their steps of k.
 template <uint32_t kRows>
 struct Walk {
     uint32_t turn, k0, steps;   // turns so far; of the present tile
@@ -202,10 +197,8 @@ struct Walk {
 
     __device__ __forceinline__ Walk() : turn(0) {}
     __device__ __forceinline__ bool next(const WideArgs &a, const Line &l) {
-        const uint32_t i = turn * l.pairs + (turn & 1 ? l.pairs - 1 - l.pair : l.pair);
-        if (turn * l.pairs >= l.tiles) return false;
-        ++turn;
-        if (i >= l.tiles) return false;   // the last turn
+        const uint32_t i = turn++ * l.pairs + l.pair;
+        if (i >= l.tiles) return false;
         t = tile_at<kRows>(a, l, i);
         k0 = (uint32_t)((uint64_t)t.split * a.steps / a.splits);
         steps = (uint32_t)((uint64_t)(t.split + 1) * a.steps / a.splits) - k0;
@@ -244,8 +237,6 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(Wide<kEight>::kThrea
     const ProductArgs &p = a.p;
     const uint32_t s_at = smem_addr(s), bars = s_at + W::kBars, more = bars + 32 * W::kStages;
     uint32_t *first = reinterpret_cast<uint32_t *>(s + W::kFirst);
-    uint16_t *order = reinterpret_cast<uint16_t *>(s + W::kOrder);
-    uint32_t *held = reinterpret_cast<uint32_t *>(s + W::kSwap);   // an expert's rows, until the tiles are counted
     volatile uint32_t *gave_up = reinterpret_cast<uint32_t *>(s + W::kWord);
     const uint32_t tid = threadIdx.x, wid = __shfl_sync(~0u, tid >> 5, 0), lane = tid & 31, rank = blockIdx.x & 1;
     auto full = [&](uint32_t i) { return bars + 32 * i; };
@@ -275,69 +266,36 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(Wide<kEight>::kThrea
         mbar_init(done, 1);
         *gave_up = 0;
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+    } else if (tid == 32) {
+        for (const CUtensorMap *m : {&mw, &mx, &ms}) asm volatile("prefetch.tensormap [%0];" ::"l"(m) : "memory");
     }
     pdl_enter();
     if (wid == 5) {
         asm volatile("tcgen05.alloc.cta_group::2.sync.aligned.shared::cta.b32 [%0], 512;" ::"r"(s_at + W::kWord + 4) : "memory");
         asm volatile("tcgen05.relinquish_alloc_permit.cta_group::2.sync.aligned;");
     }
-    // the experts by the width of their tiles, and the tiles before each; with
-    // an earlier error there are none
+    // the tiles before each expert; with an earlier error there are none
     const bool stop = has_err(p.status);
     for (uint32_t e = tid; e < p.experts; e += W::kThreads) {
         const Rows r = stop ? Rows{0, 0} : expert_rows(p, e);
-        const uint32_t rows = (uint32_t)(r.b - r.a);
-        held[e] = rows;
+        first[e + 1] = row_blocks<W::kRows>((uint32_t)(r.b - r.a)) * a.blocks * a.splits;
     }
-    __syncthreads();
-    if (wid == 0) {
-        // lane x keeps how many experts have blocks of 16 (32 - x) rows, and
-        // then where the next of them goes
-        uint32_t at = 0;
-        auto lane_of = [&](uint32_t e) { return 32 - (held[e] ? block_rows<W::kRows>(held[e]) / 16 : 1); };
-        auto each32 = [&](auto f) {
+    if (tid == 0) first[0] = 0;
+    if (p.experts > 1) {
+        __syncthreads();
+        if (wid == 0) {
+            uint32_t carry = 0;
             for (uint32_t e0 = 0; e0 < p.experts; e0 += 32) {
-                const uint32_t e = e0 + lane, of = e < p.experts ? lane_of(e) : 0;   // blocks have at most 16 times 16 rows: nobody's
-                const uint32_t same = __match_any_sync(~0u, of);
-                f(e, of, same);
-            }
-        };
-        each32([&](uint32_t e, uint32_t of, uint32_t same) {
+                uint32_t x = e0 + lane < p.experts ? first[e0 + lane + 1] : 0;
 #pragma unroll
-            for (uint32_t x = 16; x < 32; ++x) {
-                const uint32_t who = __ballot_sync(~0u, of == x);
-                if (lane == x) at += __popc(who);
+                for (int d = 1; d < 32; d *= 2) {
+                    const uint32_t y = __shfl_up_sync(~0u, x, d);
+                    if ((int)lane >= d) x += y;
+                }
+                if (e0 + lane < p.experts) first[e0 + lane + 1] = carry + x;
+                carry += __shfl_sync(~0u, x, 31);
             }
-        });
-        uint32_t in = at;
-#pragma unroll
-        for (int d = 1; d < 32; d *= 2) {
-            const uint32_t y = __shfl_up_sync(~0u, in, d);
-            if ((int)lane >= d) in += y;
         }
-        at = in - at;
-        each32([&](uint32_t e, uint32_t of, uint32_t same) {
-            const uint32_t place = __shfl_sync(~0u, at, of) + __popc(same & ((1u << lane) - 1));
-            if (e < p.experts) order[place] = (uint16_t)e;
-#pragma unroll
-            for (uint32_t x = 16; x < 32; ++x) {
-                const uint32_t who = __ballot_sync(~0u, of == x);
-                if (lane == x) at += __popc(who);
-            }
-        });
-        __syncwarp();
-        uint32_t carry = 0;
-        for (uint32_t e0 = 0; e0 < p.experts; e0 += 32) {
-            uint32_t x = e0 + lane < p.experts ? row_blocks<W::kRows>(held[order[e0 + lane]]) * a.blocks * a.splits : 0;
-#pragma unroll
-            for (int d = 1; d < 32; d *= 2) {
-                const uint32_t y = __shfl_up_sync(~0u, x, d);
-                if ((int)lane >= d) x += y;
-            }
-            if (e0 + lane < p.experts) first[e0 + lane + 1] = carry + x;
-            carry += __shfl_sync(~0u, x, 31);
-        }
-        if (lane == 0) first[0] = 0;
     }
     fence_before();
     __syncthreads();
@@ -348,7 +306,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(Wide<kEight>::kThrea
     uint32_t tiles = first[p.experts];
     if (peer_word(smem_addr(first + p.experts), rank ^ 1) != tiles) tiles = 0;
     const uint32_t tmem = *reinterpret_cast<volatile uint32_t *>(s + W::kWord + 4);
-    const Line line{first, order, tiles, blockIdx.x / 2, gridDim.x / 2};
+    const Line line{first, tiles, blockIdx.x / 2, gridDim.x / 2};
     Walk<W::kRows> walk;
     const Tile &t = walk.t;
     if (wid == 4 || wid == 6) {
