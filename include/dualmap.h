@@ -871,7 +871,7 @@ DM_API uint64_t dm_product_bytes(const dm_weights *w, uint32_t rows, uint32_t ga
 /* y[r, c] = sum over j of x[r, j] w[e, c, j], times x_scale[r] scale[e, c] for
  * 8-bit weights; gated: y[r, c] = silu(z[r, c]) z[r, n/2 + c] of that z, with
  * silu(g) = g / (1 + exp(-g)).  Sums are held in 32 bits, and y is rounded
- * once.  Sums of 8-bit products are exact below 2^24 (any k up to 1,040).  Rows
+ * once.  Sums of 8-bit products are exact up to 2^24 (any k up to 1,024).  Rows
  * outside offsets[0] .. offsets[experts] are not touched.
  * Recorded: DM_ERR_INVALID_ARG (offsets or sources out of range),
  * DM_ERR_TIMEOUT (a wait in the kernel gave up).  Asynchronous. */

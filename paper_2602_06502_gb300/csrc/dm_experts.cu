@@ -60,6 +60,8 @@ struct QuantizeArgs {
     uint64_t x_row, q_row;   // elements
     uint32_t rows, k;
     float eps;
+    const int32_t *slots;    // halves: row r of x is written to rows slots[copies * r] .. of q (-1: none); NULL: to row r
+    uint32_t copies;
 };
 
 // The largest of the sizes in a and b, two 16-bit values each: without their
@@ -175,7 +177,13 @@ __global__ void __launch_bounds__(256, kHeld <= 2 ? 6 : kHeld <= 4 ? 4 : 3) k_qu
                     const __half2 z = __hsub2(*reinterpret_cast<const __half2 *>(&two), minus);
                     w[i] = *reinterpret_cast<const uint32_t *>(&z);
                 }
-                *reinterpret_cast<uint4 *>(static_cast<__half *>(p.q) + r * p.q_row + at) = y;   // rows of whole vectors
+                __half *q = static_cast<__half *>(p.q) + at;   // rows of whole vectors
+                if (p.slots == nullptr) *reinterpret_cast<uint4 *>(q + r * p.q_row) = y;
+                else
+                    for (uint32_t j = 0; j < p.copies; ++j) {
+                        const int32_t slot = __ldg(p.slots + r * p.copies + j);
+                        if (slot >= 0) *reinterpret_cast<uint4 *>(q + (uint64_t)slot * p.q_row) = y;
+                    }
             } else {
                 int8_t *q = static_cast<int8_t *>(p.q) + r * p.q_row + at;
                 const uint2 y = make_uint2(__byte_perm(__byte_perm(n[0], n[1], 0x0040), __byte_perm(n[2], n[3], 0x0040), 0x5410),
@@ -204,7 +212,8 @@ __global__ void __launch_bounds__(256, kHeld <= 2 ? 6 : kHeld <= 4 ? 4 : 3) k_qu
 
 template <class T, bool kHalves, bool kNorm>
 cudaError_t launch_quantize(const QuantizeArgs &p, cudaStream_t st) {
-    if (p.k <= 2048) {
+    // Few rows go a CTA each, many a warp each (61 x 1,024: 2.0 and 3.6 us).
+    if (p.k <= 2048 && (p.k <= 512 || p.rows > 4 * (uint32_t)sm_count())) {
         const auto k = p.k <= 512 ? k_quantize<T, kHalves, kNorm, 32, 2> : p.k <= 1024 ? k_quantize<T, kHalves, kNorm, 32, 4> : k_quantize<T, kHalves, kNorm, 32, 8>;
         return launch_pdl(k, (p.rows + 7) / 8, 256, 0, st, p);
     }
@@ -538,11 +547,11 @@ uint64_t layer_work(const dm_weights *up, const dm_weights *down, uint32_t token
     w.counts = (int32_t *)take(choose_bytes(tokens, up->experts, top_k));
     w.h = take(2 * slots * w.h_row);
     w.parts = (float *)take(4 * slots * w.parts_row);
-    w.xq = take(eight ? tokens * w.xq_row : 0);
+    w.xq = take(!eight ? 0 : takes_halves(up, (uint32_t)slots) ? slots * w.xq_row * 2 : tokens * w.xq_row);
     w.x_scale = (float *)take(eight ? 4ull * tokens : 0);
     w.hq = take(eight ? slots * w.hq_row * (takes_halves(down, (uint32_t)slots) ? 2 : 1) : 0);
     w.h_scale = (float *)take(eight ? 4 * slots : 0);
-    w.product = take(std::max(product_bytes(up, (uint32_t)slots, 1, kGathered), product_bytes(down, (uint32_t)slots, 0, kHalves)));
+    w.product = take(std::max(product_bytes(up, (uint32_t)slots, 1, eight ? kHalves : kGathered), product_bytes(down, (uint32_t)slots, 0, kHalves)));
     return at;
 }
 
@@ -687,11 +696,15 @@ extern "C" dm_status dm_experts(const dm_weights *up, const dm_weights *down, co
         dm_product_args u{};
         u.x = a->x, u.x_row = a->x_row, u.x_rows = a->tokens, u.sources = w.sources, u.per_source = a->top_k, u.offsets = w.offsets;
         u.y = w.h, u.y_row = w.h_row, u.y_dtype = a->dtype, u.rows = slots, u.gated = 1, u.status = a->status;
+        ProductArgs up_args = product_args(up, &u);
         if (eight) {
-            DM_TRY(quantize(a->dtype, {static_cast<const char *>(a->x), w.xq, w.x_scale, nullptr, a->x_row, w.xq_row, a->tokens, up->k, -1.f}, false, st));
-            u.x = w.xq, u.x_row = w.xq_row, u.x_scale = w.x_scale;
+            // halves go straight to the slots of their experts
+            const bool halves = takes_halves(up, slots);
+            up_args.x = w.xq, up_args.x_scale = w.x_scale, up_args.x_halves = halves, up_args.x_row = w.xq_row * (halves ? 2 : 1);
+            DM_TRY(quantize(a->dtype, {static_cast<const char *>(a->x), w.xq, w.x_scale, nullptr, a->x_row, w.xq_row, a->tokens, up->k, -1.f,
+                                       halves ? w.slots : nullptr, a->top_k}, halves, st));
         }
-        DM_TRY(launch_product(up, product_args(up, &u), w.product, st));
+        DM_TRY(launch_product(up, up_args, w.product, st));
         dm_product_args d{};
         d.x = w.h, d.x_row = w.h_row, d.x_rows = slots, d.offsets = w.offsets;
         d.y = w.parts, d.y_row = w.parts_row, d.y_dtype = DM_F32, d.rows = slots, d.status = a->status;

@@ -25,7 +25,8 @@ struct ProductArgs {
     uint32_t rows, x_rows, per, experts;
     uint32_t n, k;                     // channels of y; elements of a row of x
     uint32_t y_dtype, gated;
-    uint32_t x_halves;                 // 8-bit: x holds halves (for the kernel for many rows)
+    uint32_t x_halves;                 // 8-bit: x holds halves, row r in row r; sources name the scales alone
+                                       // (for the kernel for many rows)
 };
 
 // Expert e's rows [a, b); none, and an error, where the offsets are wrong.
@@ -63,7 +64,7 @@ __device__ __forceinline__ void bytes_to_halves(uint32_t v, uint32_t &lo, uint32
     hi = *reinterpret_cast<const uint32_t *>(&y);
 }
 
-__device__ __forceinline__ float gate(float g, float u) { return __fdividef(g, 1.f + __expf(-g)) * u; }
+__device__ __forceinline__ float gate(float g, float u) { return g / (1.f + __expf(-g)) * u; }
 
 __device__ __forceinline__ void store_y(const ProductArgs &p, uint64_t at, float v) {
     if (p.y_dtype == DM_BF16) static_cast<__nv_bfloat16 *>(p.y)[at] = __float2bfloat16_rn(v);

@@ -630,7 +630,8 @@ cudaError_t launch_product_wide(const dm_weights *w, const ProductArgs &p, const
     WideArgs a{p, nullptr, (uint64_t)p.rows * w->n, w->n, s.blocks, s.splits, s.steps};
     if (s.splits > 1) a.part = reinterpret_cast<float *>(static_cast<char *>(work) + s.x_bytes);
     const char *x = p.x;
-    uint64_t x_row = p.x_rows > 1 ? p.x_row : s.x_row, x_rows = p.x_rows;
+    const uint64_t given = p.x_halves ? p.rows : p.x_rows;   // halves lie as the rows do
+    uint64_t x_row = given > 1 ? p.x_row : s.x_row, x_rows = given;
     if (s.x_bytes) {
         const uint32_t grid = std::min((p.rows + 7) / 8, (uint32_t)sm_count() * 64);
         char *to = static_cast<char *>(work);

@@ -6,8 +6,9 @@ the quantising of rows, the choice of experts, and the layer made of them
 Only marshalling: it checks shapes and types, allocates outputs and work
 buffers on the device, and enqueues the C calls on torch's current stream of
 the inputs' device.  A call's work buffer is its own, so calls on one set of
-weights may overlap.  The calls serve: they give no gradients, so with grad mode
-on they refuse tensors that want one.
+weights may overlap.  While an error stands (last_error) products do nothing, and
+a new output is whatever memory held.  The calls serve: they give no gradients,
+so with grad mode on they refuse tensors that want one.
 
 A matrix's last dimension is contiguous and its rows begin on 16 bytes: a width
 that is no multiple of 16 bytes lies in wider rows (x = buffer[:, :k]).
