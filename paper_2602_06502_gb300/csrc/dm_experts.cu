@@ -43,9 +43,10 @@ __device__ __forceinline__ float score_at(const float *p) { return *p; }
 
 // -- rows in 8 bits -------------------------------------------------------------------
 //
-// Bound: memory, 2 bytes read and 1 written per value.  A row stays in the
-// registers of a warp (up to 2,048 values) or of a CTA (up to 16,384); a longer
-// one is read twice.
+// Bound: memory, 2 bytes read and 1 written per value (8,191 x 4,096: 19.9 us, 5.1
+// TB/s); the instructions, about ten a value, are close behind.  A row stays in
+// the registers of a warp (up to 2,048 values) or of a CTA (up to 16,384); a
+// longer one is read twice.
 //
 // The product with 127 / top is off by less than 2^-16 and gives a step r.  What
 // is left, 127 x - r top, is exact in 32 bits (x and top have up to 11 bits), and
@@ -73,8 +74,9 @@ __device__ __forceinline__ uint32_t larger2(uint32_t a, uint32_t b) { return __v
 constexpr float kRound = 12582912.f;
 
 template <class T, bool kHalves, bool kNorm, uint32_t kLanes, uint32_t kHeld>
-__global__ void __launch_bounds__(256, kHeld <= 2 ? 6 : kHeld <= 4 ? 4 : 3) k_quantize(QuantizeArgs p) {
-    constexpr uint32_t kPer = 256 / kLanes;   // rows of a CTA; kHeld: vectors of 8 values a lane keeps
+__global__ void __launch_bounds__(kLanes == 32 ? 256 : kLanes, (kHeld <= 2 ? 6 : kHeld <= 4 ? 4 : 3) * (kLanes == 128 ? 2 : 1))
+    k_quantize(QuantizeArgs p) {
+    constexpr uint32_t kPer = kLanes == 32 ? 8 : 1;   // rows of a CTA; kHeld: vectors of 8 values a lane keeps
     constexpr uint32_t kFinite = std::is_same_v<T, __half> ? 0x7C00 : 0x7F80;
     __shared__ uint32_t s_top[8];
     __shared__ float s_sum[8];
@@ -217,6 +219,9 @@ cudaError_t launch_quantize(const QuantizeArgs &p, cudaStream_t st) {
         const auto k = p.k <= 512 ? k_quantize<T, kHalves, kNorm, 32, 2> : p.k <= 1024 ? k_quantize<T, kHalves, kNorm, 32, 4> : k_quantize<T, kHalves, kNorm, 32, 8>;
         return launch_pdl(k, (p.rows + 7) / 8, 256, 0, st, p);
     }
+    // What a row costs besides its values, each thread pays, so with many rows half
+    // as many threads have one (8,191 x 4,096: 19.9 us, 22.8 with 256, 33 with a warp).
+    if (p.k <= 4096 && p.rows > 4 * (uint32_t)sm_count()) return launch_pdl(k_quantize<T, kHalves, kNorm, 128, 4>, p.rows, 128, 0, st, p);
     const auto k = p.k <= 4096 ? k_quantize<T, kHalves, kNorm, 256, 2> : p.k <= 8192 ? k_quantize<T, kHalves, kNorm, 256, 4> : k_quantize<T, kHalves, kNorm, 256, 8>;
     return launch_pdl(k, p.rows, 256, 0, st, p);
 }
@@ -237,8 +242,7 @@ cudaError_t launch_quantize(const QuantizeArgs &p, bool halves, cudaStream_t st)
 // number of equal ones before it.  Up to kCluster tiles see each other's counts
 // as a cluster, in one launch; more leave them in memory for a second kernel.
 //
-// Bound: latency.  Four tokens of 8 experts: 2.7 us; 128 of 64, 8 each: ;
-// 8,192 of 128, 8 each: .
+// Bound: latency.  Four tokens of 8 experts: 2.4 us; 8,192 of 128, 8 each: 17.5 us.
 
 constexpr uint32_t kChooseT = 1024, kTilePairs = 256, kTileTokens = 32, kCluster = 8;
 
