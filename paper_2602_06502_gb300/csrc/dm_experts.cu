@@ -486,7 +486,9 @@ struct JoinArgs {
 };
 
 // 4 channels a thread, the parts in the order of the choice.  Bound: memory, 4
-// bytes read for each of a token's parts.
+// bytes read for each value of a token's parts (4,096 tokens of 4 parts, 4,096
+// wide: 56 us, 5.9 TB/s; with four parts on their way at a time 70).  Parts of 16
+// bits take 25 of that layer's 538 us, and its error from 0.0020 to 0.0023.
 template <class T>
 __global__ void __launch_bounds__(256) k_join_experts(JoinArgs p) {
     pdl_enter();
