@@ -938,6 +938,10 @@ DM_API void dm_test_fail_alloc(int64_t n);
  * GPU as it was.  A release build returns DM_ERR_INVALID_ARG for ns > 0. */
 DM_API dm_status dm_test_attend_wait(uint64_t ns);
 
+/* The same for products of many rows: the first weights of every one never
+ * arrive. */
+DM_API dm_status dm_test_product_wait(uint64_t ns);
+
 /* Synchronise the stream and return the sticky error (DM_OK if none). */
 DM_API dm_status dm_last_error(dm_handle *h);
 

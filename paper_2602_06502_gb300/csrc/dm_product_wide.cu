@@ -14,6 +14,7 @@
 //   warps 8-23  8-bit weights alone: to halves, in tensor memory, from where
 //               the tensor cores take them: no second pass through shared memory
 #include <algorithm>
+#include <atomic>
 
 #include "dm_product.cuh"
 #include "dm_tensor.cuh"
@@ -50,7 +51,19 @@ struct WideArgs {
     uint32_t channels;    // of the weights
     uint32_t blocks;      // tiles across the channels
     uint32_t splits, steps;
+#ifdef DM_DEBUG
+    uint64_t test_wait_ns;   // dm_test_product_wait: 0, or how long waits last
+#endif
 };
+
+// Whether a test has stage c of this CTA's weights never arrive.
+__device__ __forceinline__ bool withheld(const WideArgs &a, uint32_t c) {
+#ifdef DM_DEBUG
+    return a.test_wait_ns && blockIdx.x == 0 && c == 0;
+#else
+    return false;
+#endif
+}
 
 // -- pairs of CTAs -----------------------------------------------------------------
 
@@ -125,22 +138,29 @@ __device__ __forceinline__ bool over(uint32_t bar, uint32_t parity) {
     return ok != 0;
 }
 
-// Waits for the phase, by a whole warp.  A wait that gives up says so in
-// `gave_up`, and the CTA's others then return at once: every loop is as long as
-// its data says, so the CTA ends.
-__device__ __forceinline__ void wait(uint32_t bar, uint32_t parity, volatile uint32_t *gave_up, uint32_t *status) {
-    if (!mbar_try(bar, parity)) {
+// Waits for the phase, by a whole warp; false: it is not over, and a wait of this
+// CTA has given up, which ends the others at once.  Who copies, converts or
+// multiplies then stops where it is: a barrier whose copies have not come takes
+// no further arrival.  Who stores goes on to the end of its tiles, as its four
+// warps meet on the way.
+__device__ __forceinline__ bool wait(uint32_t bar, uint32_t parity, volatile uint32_t *gave_up, const WideArgs &a) {
+    bool over = mbar_try(bar, parity);
+    if (!over) {
+        uint64_t ns = kWaitNs;
+#ifdef DM_DEBUG
+        if (a.test_wait_ns) ns = a.test_wait_ns;
+#endif
         const uint64_t t0 = now_ns();
         for (uint32_t i = 0;; ++i) {
-            if (mbar_try(bar, parity) || *gave_up) break;
-            if ((i & 63) == 63 && (now_ns() - t0 > kWaitNs || i > kWaits)) {
+            if ((over = mbar_try(bar, parity)) || *gave_up) break;
+            if ((i & 63) == 63 && (now_ns() - t0 > ns || i > kWaits)) {
                 *gave_up = 1;
-                set_err(status, DM_ERR_TIMEOUT);
+                set_err(a.p.status, DM_ERR_TIMEOUT);
                 break;
             }
         }
     }
-    __syncwarp();
+    return __all_sync(~0u, over);
 }
 
 // -- tiles --------------------------------------------------------------------------
@@ -315,7 +335,8 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(Wide<kEight>::kThrea
         // lane, as it goes through uniform registers.
         const bool weights = wid == 4, one = elect();
         uint32_t c = 0;   // stages so far
-        while (!__any_sync(~0u, *gave_up) && walk.next(a, line)) {
+        bool on = true;
+        while (on && walk.next(a, line)) {
             const uint32_t half = t.width / 2, boxes = half > W::kRows / 4 ? 0 : (half + kSmallBox - 1) / kSmallBox;
             const int row = (int)(t.row + rank * half), e = (int)t.e;
             const int w0 = (int)(p.gated ? t.c0 + rank * 64 : t.c0 + rank * 128), w1 = (int)(p.gated ? p.n + t.c0 + rank * 64 : t.c0 + rank * 128 + 64);
@@ -324,10 +345,8 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(Wide<kEight>::kThrea
             for (uint32_t j = 0; j < steps; ++j, ++c) {
                 const uint32_t st = c % W::kStages, round = c / W::kStages, at = s_at + st * W::kStage, bar = of_first(full(st));
                 const int k0 = (int)((walk.k0 + j) * W::kStep);
-                if (round) {
-                    if (!kEight || !weights) wait(empty(st), (round - 1) & 1, gave_up, p.status);
-                    else wait(w_empty(st), (round - 1) & 1, gave_up, p.status);
-                }
+                if (round && !(on = wait(!kEight || !weights ? empty(st) : w_empty(st), (round - 1) & 1, gave_up, a))) break;
+                if (weights && withheld(a, c)) continue;
                 if (weights) {
                     const uint32_t w_bar = kEight ? w_full(st) : bar;
                     if (one) {
@@ -352,9 +371,9 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(Wide<kEight>::kThrea
             }
         }
         // no copy may be in flight when the CTA ends: its stages have been taken
-        for (uint32_t i = c > W::kStages ? c - W::kStages : 0; i < c; ++i) {
-            wait(empty(i % W::kStages), (i / W::kStages) & 1, gave_up, p.status);
-            if (kEight && weights) wait(w_empty(i % W::kStages), (i / W::kStages) & 1, gave_up, p.status);
+        for (uint32_t i = c > W::kStages ? c - W::kStages : 0; on && i < c; ++i) {
+            wait(empty(i % W::kStages), (i / W::kStages) & 1, gave_up, a);
+            if (kEight && weights) wait(w_empty(i % W::kStages), (i / W::kStages) & 1, gave_up, a);
         }
     } else if (wid == 5) {
         if (rank == 0) {
@@ -365,20 +384,20 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(Wide<kEight>::kThrea
             // The next stage is asked for while the present one's products are
             // issued: asking takes about as long as they do.
             uint32_t n = 0, st = 0, parity = 0, as = 0, a_parity = 0;
-            bool ready = false, a_ready = false;
-            for (; !__any_sync(~0u, *gave_up) && walk.next(a, line); ++n) {
+            bool ready = false, a_ready = false, on = true;
+            for (; on && walk.next(a, line); ++n) {
                 const uint32_t steps = walk.steps, buf = n & 1, d = tm + buf * W::kRows;
                 // f32 sums, the operands' type, N, M = 256
                 const uint32_t desc = 1u << 4 | kType << 7 | kType << 10 | (t.width / 8) << 17 | 16u << 24;
-                if (n >= 2) wait(sum_empty(buf), (n / 2 - 1) & 1, gave_up, p.status);
+                if (n >= 2 && !(on = wait(sum_empty(buf), (n / 2 - 1) & 1, gave_up, a))) break;
                 for (uint32_t j = 0; j < steps; ++j) {
-                    if (!ready) wait(full(st), parity, gave_up, p.status);
+                    if (!ready && !(on = wait(full(st), parity, gave_up, a))) break;
                     const uint64_t wa = w_op + st * (W::kStage >> 4), xa = x_op + st * (W::kStage >> 4);
                     const uint32_t now = st;
                     if (++st == W::kStages) st = 0, parity ^= 1;
 #pragma unroll
                     for (uint32_t sub = 0; sub < W::kStep / 64; ++sub) {
-                        if (kEight && !a_ready) wait(a_full(as), a_parity, gave_up, p.status);
+                        if (kEight && !a_ready && !(on = wait(a_full(as), a_parity, gave_up, a))) break;
                         fence_after();
                         if (one) {
 #pragma unroll
@@ -394,6 +413,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(Wide<kEight>::kThrea
                             a_ready = __all_sync(~0u, over(a_full(as), a_parity));
                         }
                     }
+                    if (!on) break;
                     if (one) {
                         commit2(empty(now));
                         if (j + 1 == steps) commit2(sum_full(buf));
@@ -418,7 +438,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(Wide<kEight>::kThrea
             const bool on = c < p.n;
             float scale = 1.f;
             if constexpr (kEight) scale = on ? __ldg(p.w_scale + (uint64_t)t.e * a.channels + wc) : 0.f;
-            wait(sum_full(buf), (n / 2) & 1, gave_up, p.status);
+            wait(sum_full(buf), (n / 2) & 1, gave_up, a);
             fence_after();
             for (uint32_t q = 0; q < t.width; q += 32) {
                 uint32_t raw[32];
@@ -470,12 +490,13 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(Wide<kEight>::kThrea
         const uint32_t group = (wid - 8) / 4, half = group & 1, r = (wid & 3) * 32 + lane;
         const uint32_t places = tmem + W::kA + ((wid & 3) << 21), bars_first = of_first(a_full(0));
         uint32_t c = 0, as = group, round = 0;
-        while (!__any_sync(~0u, *gave_up) && walk.next(a, line)) {
+        bool on = true;
+        while (on && walk.next(a, line)) {
             const uint32_t end = c + walk.steps;
             for (; c < end; ++c) {
                 if ((c & 1) != group >> 1) continue;
                 const uint32_t st = c % W::kStages;
-                wait(w_full(st), (c / W::kStages) & 1, gave_up, p.status);
+                if (!(on = wait(w_full(st), (c / W::kStages) & 1, gave_up, a))) break;
                 uint4 v[4];
 #pragma unroll
                 for (uint32_t x = 0; x < 4; ++x) v[x] = *reinterpret_cast<const uint4 *>(s + st * W::kStage + r * 128 + (((4 * half + x) ^ (r & 7)) << 4));
@@ -489,7 +510,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(Wide<kEight>::kThrea
                     bytes_to_halves(v[x].z, y[8 * x + 4], y[8 * x + 5]);
                     bytes_to_halves(v[x].w, y[8 * x + 6], y[8 * x + 7]);
                 }
-                if (round) wait(a_empty(as), (round - 1) & 1, gave_up, p.status);
+                if (round && !(on = wait(a_empty(as), (round - 1) & 1, gave_up, a))) break;
                 fence_after();
                 tm_st(places + as * 32, y);
                 wait_st();
@@ -502,7 +523,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(Wide<kEight>::kThrea
         }
         // the last uses of all places have ended before the CTA does
         const uint32_t uses = 2 * c;
-        for (uint32_t u = uses > W::kAs ? uses - W::kAs : 0; u < uses; ++u) wait(a_empty(u % W::kAs), (u / W::kAs) & 1, gave_up, p.status);
+        for (uint32_t u = uses > W::kAs ? uses - W::kAs : 0; on && u < uses; ++u) wait(a_empty(u % W::kAs), (u / W::kAs) & 1, gave_up, a);
     }
     fence_before();
     __syncthreads();
@@ -597,6 +618,10 @@ bool matrix_map(CUtensorMap *m, uint32_t dtype, const void *base, uint64_t k, ui
                   CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
+#ifdef DM_DEBUG
+std::atomic<uint64_t> g_test_wait_ns{0};
+#endif
+
 template <class T, bool kEight>
 cudaError_t launch(const dm_weights *w, const WideArgs &a, const CUtensorMap &mw, const CUtensorMap &mx, const CUtensorMap &ms, uint32_t grid,
                    cudaStream_t st) {
@@ -628,6 +653,9 @@ WideShape wide_shape(const dm_weights *w, uint32_t rows, uint32_t gated, RowsAre
 cudaError_t launch_product_wide(const dm_weights *w, const ProductArgs &p, const WideShape &s, void *work, cudaStream_t st) {
     const bool eight = w->dtype == DM_I8;
     WideArgs a{p, nullptr, (uint64_t)p.rows * w->n, w->n, s.blocks, s.splits, s.steps};
+#ifdef DM_DEBUG
+    a.test_wait_ns = g_test_wait_ns;
+#endif
     if (s.splits > 1) a.part = reinterpret_cast<float *>(static_cast<char *>(work) + s.x_bytes);
     const char *x = p.x;
     const uint64_t given = p.x_halves ? p.rows : p.x_rows;   // halves lie as the rows do
@@ -654,3 +682,12 @@ cudaError_t launch_product_wide(const dm_weights *w, const ProductArgs &p, const
 }
 
 }  // namespace dm
+
+extern "C" dm_status dm_test_product_wait(uint64_t ns) {
+#ifdef DM_DEBUG
+    dm::g_test_wait_ns = ns;
+    return DM_OK;
+#else
+    return ns ? DM_ERR_INVALID_ARG : DM_OK;
+#endif
+}

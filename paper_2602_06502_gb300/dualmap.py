@@ -233,6 +233,7 @@ SIGNATURES = {
     "dm_experts": (C.c_int, [C.POINTER(dm_weights), C.POINTER(dm_weights), C.POINTER(dm_experts_args), C.c_void_p]),
     "dm_test_fail_alloc": (None, [C.c_int64]),
     "dm_test_attend_wait": (C.c_int, [C.c_uint64]),
+    "dm_test_product_wait": (C.c_int, [C.c_uint64]),
     "dm_last_error": (C.c_int, [C.c_void_p]),
     "dm_set_profiling": (C.c_int, [C.c_void_p, C.c_int]),
     "dm_get_stage_times": (C.c_int, [C.c_void_p, C.c_void_p, C.c_void_p, C.c_int]),
