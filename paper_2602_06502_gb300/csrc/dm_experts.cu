@@ -183,7 +183,7 @@ __global__ void __launch_bounds__(kLanes == 32 ? 256 : kLanes, (kHeld <= 2 ? 6 :
                 if (p.slots == nullptr) *reinterpret_cast<uint4 *>(q + r * p.q_row) = y;
                 else
                     for (uint32_t j = 0; j < p.copies; ++j) {
-                        const int32_t slot = __ldg(p.slots + r * p.copies + j);
+                        const int32_t slot = __ldcg(p.slots + r * p.copies + j);
                         if (slot >= 0) *reinterpret_cast<uint4 *>(q + (uint64_t)slot * p.q_row) = y;
                     }
             } else {

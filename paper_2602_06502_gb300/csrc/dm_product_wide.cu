@@ -13,6 +13,17 @@
 //   warp 5      tcgen05.mma, in the first CTA of the pair
 //   warps 8-23  8-bit weights alone: to halves, in tensor memory, from where
 //               the tensor cores take them: no second pass through shared memory
+//
+// A pair because each CTA then reads half of the rows from shared memory for
+// the same products; 256 x 256 because what a stage brings (64 KB for 512 cycles
+// of products) is what L2 gives.
+//
+// Bound: the tensor cores and the power they may draw where there are many rows
+// (16,384 rows of 32 experts, 2 x 1,536 x 4,096, gated, bf16: 250 us, 1.65 PFLOP/s; 8,191
+// x 6,144 x 4,096 in 8 bits: 240 us, 1.7 PFLOP/s); memory where there are few
+// (64 experts of 2,048 x 2,048 with 16 rows each: 91 us, 5.9 TB/s). In 8 bits a
+// product whose first operand is in tensor memory takes about 125 cycles, however
+// few its rows, so there memory gives 3.5 TB/s (77 us).
 #include <algorithm>
 #include <atomic>
 
@@ -233,7 +244,7 @@ __device__ __forceinline__ Y to_y(float x) {
     else return __float2bfloat16_rn(x);
 }
 
-// A warp's channel per lane of `n` rows from row r on: 2 x 32 consecutive bytes a store.
+// A warp's channel per lane of `n` rows from row r on: 64 consecutive bytes a store, or 128.
 template <class Y>
 __device__ __forceinline__ void store_rows(const ProductArgs &p, const uint32_t *raw, uint32_t r, uint32_t n, uint32_t c, bool on) {
     Y *to = static_cast<Y *>(p.y) + (uint64_t)r * p.y_row + c;
@@ -295,7 +306,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(Wide<kEight>::kThrea
         asm volatile("tcgen05.relinquish_alloc_permit.cta_group::2.sync.aligned;");
     }
     // the tiles before each expert; with an earlier error there are none
-    const bool stop = has_err(p.status);
+    const bool stop = __syncthreads_or(has_err(p.status));
     for (uint32_t e = tid; e < p.experts; e += W::kThreads) {
         const Rows r = stop ? Rows{0, 0} : expert_rows(p, e);
         first[e + 1] = row_blocks<W::kRows>((uint32_t)(r.b - r.a)) * a.blocks * a.splits;
@@ -437,7 +448,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(Wide<kEight>::kThrea
             const uint32_t wc = partner ? p.n + c : c;
             const bool on = c < p.n;
             float scale = 1.f;
-            if constexpr (kEight) scale = on ? __ldg(p.w_scale + (uint64_t)t.e * a.channels + wc) : 0.f;
+            if constexpr (kEight) scale = on ? __ldcg(p.w_scale + (uint64_t)t.e * a.channels + wc) : 0.f;
             wait(sum_full(buf), (n / 2) & 1, gave_up, a);
             fence_after();
             for (uint32_t q = 0; q < t.width; q += 32) {
@@ -460,7 +471,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(Wide<kEight>::kThrea
                 }
                 if constexpr (kEight) {
                     float sx = 0.f;
-                    if (lane < rows) sx = __ldg(p.x_scale + source_row(p, t.row + q + lane));
+                    if (lane < rows) sx = __ldcg(p.x_scale + source_row(p, t.row + q + lane));
 #pragma unroll
                     for (uint32_t r = 0; r < 32; ++r) raw[r] = __float_as_uint(__uint_as_float(raw[r]) * (__shfl_sync(~0u, sx, r) * scale));
                 }
@@ -555,11 +566,11 @@ __global__ void __launch_bounds__(256) k_product_rows(ProductArgs p, char *to, u
         for (uint32_t at = lane; at < each; at += 32) {
             uint4 v;
             if constexpr (kEight) {
-                const uint2 b = __ldg(reinterpret_cast<const uint2 *>(x) + at);
+                const uint2 b = __ldcg(reinterpret_cast<const uint2 *>(x) + at);
                 bytes_to_halves(b.x, v.x, v.y);
                 bytes_to_halves(b.y, v.z, v.w);
             } else {
-                v = __ldg(reinterpret_cast<const uint4 *>(x) + at);
+                v = __ldcg(reinterpret_cast<const uint4 *>(x) + at);
             }
             y[at] = v;
         }
@@ -578,7 +589,7 @@ __global__ void __launch_bounds__(256) k_product_join(WideArgs a) {
     const Rows rows = expert_rows(p, 0);
     const uint32_t each = p.n / kV, r = (uint32_t)rows.a + blockIdx.y;
     if (r >= (uint32_t)rows.b) return;
-    const float sx = p.w_scale ? __ldg(p.x_scale + source_row(p, r)) : 0.f;
+    const float sx = p.w_scale ? __ldcg(p.x_scale + source_row(p, r)) : 0.f;
     for (uint32_t i = blockIdx.x * 256 + threadIdx.x; i < each; i += gridDim.x * 256) {
         const uint32_t c = i * kV;
         float z[2][kV] = {};
@@ -594,7 +605,7 @@ __global__ void __launch_bounds__(256) k_product_join(WideArgs a) {
             }
             if (p.w_scale)
 #pragma unroll
-                for (uint32_t v = 0; v < kV; ++v) z[h][v] *= sx * __ldg(p.w_scale + h * p.n + c + v);
+                for (uint32_t v = 0; v < kV; ++v) z[h][v] *= sx * __ldcg(p.w_scale + h * p.n + c + v);
         }
 #pragma unroll
         for (uint32_t v = 0; v < kV; ++v) store_y(p, (uint64_t)r * p.y_row + c + v, p.gated ? gate(z[0][v], z[1][v]) : z[0][v]);
@@ -672,7 +683,7 @@ cudaError_t launch_product_wide(const dm_weights *w, const ProductArgs &p, const
     if (!matrix_map(&mw, w->dtype, w->w, w->k, w->n, w->experts, p.w_row, w->experts > 1 ? p.w_expert : align_up(w->n * p.w_row, 16), 64) ||
         !matrix_map(&mx, x_type, x, p.k, x_rows, 0, x_row, 0, big) || !matrix_map(&ms, x_type, x, p.k, x_rows, 0, x_row, 0, kSmallBox))
         return cudaErrorInvalidValue;
-    const uint32_t grid = (uint32_t)sm_count() / 2 * 2;
+    const uint32_t grid = std::max(2u, (uint32_t)sm_count() / 2 * 2);
     const auto run = eight ? launch<__half, true> : w->dtype == DM_F16 ? launch<__half, false> : launch<__nv_bfloat16, false>;
     DM_TRY(run(w, a, mw, mx, ms, grid, st));
     if (s.splits == 1) return cudaSuccess;
