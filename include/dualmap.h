@@ -848,7 +848,7 @@ DM_API dm_status dm_choose_experts(const dm_choose_args *a, void *stream);
 typedef struct {
     const void *x;            /* x_rows x k: of the weights' type */
     const float *x_scale;     /* DM_I8: x_rows */
-    void *y;                  /* rows x n (n / 2 where gated); any alignment of its type */
+    void *y;                  /* rows x n (n / 2 where gated); any alignment of its type; overlaps nothing else */
     const int32_t *offsets;   /* experts + 1, not decreasing, within 0 .. rows: expert e has rows
                                  offsets[e] .. offsets[e+1]); NULL with one expert: all rows */
     const int32_t *sources;   /* rows: row r reads row sources[r] / per_source of x; NULL: row r */
@@ -880,7 +880,7 @@ DM_API dm_status dm_product(const dm_weights *w, const dm_product_args *a, void 
 /* A projection with 8-bit weights (dm_linear). */
 typedef struct {
     const void *x;            /* rows x k, DM_BF16 or DM_F16 */
-    void *y;                  /* rows x n; any alignment of its type */
+    void *y;                  /* rows x n; any alignment of its type; overlaps nothing else */
     uint32_t *status;
     void *work;               /* dm_linear_bytes bytes, 256-byte aligned */
     uint64_t work_bytes;

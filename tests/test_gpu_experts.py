@@ -316,3 +316,58 @@ def test_layer_in_8_bits_is_its_parts(torch, tokens, experts, top_k, k, m, dtype
     # a residual, top_k products and sums in 32 bits; the pieces are the layer's own kernels
     R.close(y, want, R.round_off(want, size * (top_k + 1) * 2.0 ** -23, t))
     assert up.last_error() == 0 and down.last_error() == 0
+
+
+@pytest.mark.parametrize("dtype", ["bfloat16", "int8"])
+@pytest.mark.parametrize("most", [4, 40])
+def test_product_of_many_experts(torch, dtype, most):
+    """1,024 experts, some without rows, by both kernels: whole numbers, so nothing but the rounding."""
+    import random
+
+    from paper_2602_06502_gb300 import experts as X
+    rng = random.Random(most)
+    rows = [rng.randint(0, most) for _ in range(1024)]
+    x, xs, w, offsets, t = case(torch, most, rows, 64, 24, dtype)
+    if xs is not None:
+        xs.fill_(0.5)
+        w.scale.fill_(2.0)
+    y = X.product(x, w, ints(torch, offsets), x_scale=xs, dtype=torch.float32)
+    of = torch.repeat_interleave(torch.arange(1024, device="cuda"), torch.tensor(rows, device="cuda"))
+    assert torch.equal(y.double(), torch.einsum("rk,rnk->rn", x.double(), w.w[of].double())) and w.last_error() == 0
+
+
+@pytest.mark.parametrize("eight", [False, True])
+@pytest.mark.parametrize("tokens", [0, 1, 20, 300])
+def test_layer_of_one_expert(torch, tokens, eight):
+    """Every token goes to the one expert, with a weight of 1: what its parts give."""
+    import experts_reference as R
+    from paper_2602_06502_gb300 import experts as X
+    x, up, down, _, residual, t = make_layer(torch, tokens + 1, tokens, 1, 512, 96, "bfloat16", eight)
+    logits = torch.randn(tokens, 1, generator=gen(torch, 3), device="cuda")
+    y = X.Experts(up, down, 1)(x, logits, residual=residual)
+    assert y.shape == (tokens, 512)
+    off = ints(torch, [0, tokens])
+    q, scale = X.quantize(x) if eight else (x, None)
+    h = X.product(q, up, off, x_scale=scale, gated=True, dtype=t)
+    hq, h_scale = X.quantize(h) if eight else (h, None)
+    want = X.product(hq, down, off, x_scale=h_scale, dtype=torch.float32).double() + residual.double()
+    R.close(y, want, R.round_off(want, (want.abs() + 2 * residual.double().abs()) * 2.0 ** -22, t))   # one sum and its rounding
+    assert up.last_error() == 0 and down.last_error() == 0
+
+
+@pytest.mark.parametrize("eight", [False, True])
+@pytest.mark.parametrize("tokens", [7, 200])
+def test_layer_keeps_bad_tokens_apart(torch, tokens, eight):
+    """A token whose row or scores are not numbers is NaN, and the others are what they were."""
+    from paper_2602_06502_gb300 import experts as X
+    x, up, down, logits, residual, t = make_layer(torch, tokens, tokens, 6, 256, 64, "float16", eight)
+    logits = torch.randn(tokens, 6, generator=gen(torch, 4), device="cuda")
+    e = X.Experts(up, down, 2)
+    want = e(x, logits, residual=residual)
+    x, logits = x.clone(), logits.clone()
+    x[1, 3], x[4, 200], logits[5, 2] = float("nan"), float("inf"), float("nan")
+    y = e(x, logits, residual=residual)
+    bad = torch.zeros(tokens, dtype=torch.bool, device="cuda")
+    bad[[1, 4, 5]] = True
+    assert torch.isnan(y[[1, 5]]).all() and not torch.isfinite(y[4]).any()
+    assert torch.equal(y[~bad], want[~bad]) and up.last_error() == 0
