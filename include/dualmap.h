@@ -890,7 +890,8 @@ typedef struct {
     float eps;                /* of a norm, >= 0; negative: no norm */
 } dm_linear_args;
 
-/* Size of dm_linear_args.work on the current device; 0 for an invalid shape. */
+/* Size of dm_linear_args.work on the current device; 1: none is needed, and work
+ * may be NULL; 0 for an invalid shape. */
 DM_API uint64_t dm_linear_bytes(const dm_weights *w, uint32_t rows);
 
 /* dm_quantize and then dm_product with one expert's 8-bit weights.  Recorded: as

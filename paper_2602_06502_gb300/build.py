@@ -47,7 +47,7 @@ def build(force=False, verbose=False, extra=(), debug=False):
         extra = ("-DDM_DEBUG",) + tuple(extra)
     os.makedirs(bdir, exist_ok=True)
     headers = [os.path.join(CSRC, h) for h in ("dm_internal.cuh", "dm_launch.h", "dm_run_end.h", "dm_cache.cuh",
-                                                  "dm_attend.cuh", "dm_tensor.cuh", "dm_product.cuh")]
+                                                  "dm_attend.cuh", "dm_tensor.cuh", "dm_product.cuh", "dm_quantize.cuh")]
     headers.append(os.path.join(ROOT, "include", "dualmap.h"))
     objs, jobs = [], []
     for s in SOURCES:

@@ -5,41 +5,12 @@
 #include <cooperative_groups.h>
 
 #include "dm_product.cuh"
+#include "dm_quantize.cuh"
 
 namespace cg = cooperative_groups;
 
 namespace dm {
 namespace {
-
-template <class T>
-struct Two;
-template <>
-struct Two<__nv_bfloat16> {
-    using type = __nv_bfloat162;
-    static __device__ __forceinline__ float2 up(type x) { return __bfloat1622float2(x); }
-    static __device__ __forceinline__ type down(float a, float b) { return __floats2bfloat162_rn(a, b); }
-};
-template <>
-struct Two<__half> {
-    using type = __half2;
-    static __device__ __forceinline__ float2 up(type x) { return __half22float2(x); }
-    static __device__ __forceinline__ type down(float a, float b) { return __floats2half2_rn(a, b); }
-};
-
-template <class T>
-__device__ __forceinline__ void unpack(const uint4 &x, float *f) {
-    const auto *p = reinterpret_cast<const typename Two<T>::type *>(&x);
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-        const float2 y = Two<T>::up(p[i]);
-        f[2 * i] = y.x;
-        f[2 * i + 1] = y.y;
-    }
-}
-
-__device__ __forceinline__ float score_at(const __nv_bfloat16 *p) { return __bfloat162float(*p); }
-__device__ __forceinline__ float score_at(const __half *p) { return __half2float(*p); }
-__device__ __forceinline__ float score_at(const float *p) { return *p; }
 
 // -- rows in 8 bits -------------------------------------------------------------------
 //
@@ -47,11 +18,6 @@ __device__ __forceinline__ float score_at(const float *p) { return *p; }
 // TB/s); the instructions, about ten a value, are close behind.  A row stays in
 // the registers of a warp (up to 2,048 values) or of a CTA (up to 16,384); a
 // longer one is read twice.
-//
-// The product with 127 / top is off by less than 2^-16 and gives a step r.  What
-// is left, 127 x - r top, is exact in 32 bits (x and top have up to 11 bits), and
-// where it is about half of top or more it corrects r: q is what the formula
-// says to the last case.
 
 struct QuantizeArgs {
     const char *x;
@@ -65,19 +31,10 @@ struct QuantizeArgs {
     uint32_t copies;
 };
 
-// The largest of the sizes in a and b, two 16-bit values each: without their
-// signs the bits of floating-point numbers are in their order, and what is not
-// finite is above the rest.
-__device__ __forceinline__ uint32_t larger2(uint32_t a, uint32_t b) { return __vmaxu2(a, b & 0x7FFF7FFFu); }
-
-// Added to a number below 2^22 it leaves that number, rounded to even, in the low bits.
-constexpr float kRound = 12582912.f;
-
 template <class T, bool kHalves, bool kNorm, uint32_t kLanes, uint32_t kHeld>
 __global__ void __launch_bounds__(kLanes == 32 ? 256 : kLanes, (kHeld <= 2 ? 6 : kHeld <= 4 ? 4 : 3) * (kLanes == 128 ? 2 : 1))
     k_quantize(QuantizeArgs p) {
     constexpr uint32_t kPer = kLanes == 32 ? 8 : 1;   // rows of a CTA; kHeld: vectors of 8 values a lane keeps
-    constexpr uint32_t kFinite = std::is_same_v<T, __half> ? 0x7C00 : 0x7F80;
     __shared__ uint32_t s_top[8];
     __shared__ float s_sum[8];
     pdl_enter();
@@ -134,51 +91,15 @@ __global__ void __launch_bounds__(kLanes == 32 ? 256 : kLanes, (kHeld <= 2 ? 6 :
 #pragma unroll
             for (uint32_t i = 0; i < kLanes / 32; ++i) bits = max(bits, s_top[i]), sum += s_sum[i];
         }
-        const uint16_t low = (uint16_t)bits;
-        const bool finite = bits < kFinite;
-        const float top = score_at(reinterpret_cast<const T *>(&low));
-        float scale = __fdiv_rn(top, 127.f);
+        float scale;
+        const RowStep step = row_step<T>(bits, scale);
         if constexpr (kNorm) scale *= rsqrtf(sum / (float)p.k + p.eps);
-        if (lane == 0) p.scale[r] = finite ? scale : __int_as_float(0x7FC00000);
-        // a power of two keeps 127 / top and 127 x in range
-        const float shift = top > 1e30f ? 0x1p-64f : top < 1e-30f ? 0x1p64f : 1.f;
-        const float big = top * shift, by = bits == 0 || !finite ? 0.f : __fdiv_rn(127.f, big);
-        const uint32_t keep = finite ? ~0u : 0u;
-        auto put = [&](uint4 v, uint32_t at) {
-            float f[8], far = 0.f;
-            uint32_t n[8];   // kRound + the step
-            v.x &= keep, v.y &= keep, v.z &= keep, v.w &= keep;
-            unpack<T>(v, f);
-            if (shift != 1.f)
-#pragma unroll
-                for (int i = 0; i < 8; ++i) f[i] *= shift;
-#pragma unroll
-            for (int i = 0; i < 8; ++i) {
-                const float y = __fmaf_rn(f[i], by, kRound);
-                n[i] = __float_as_uint(y);
-                far = fmaxf(far, fabsf(__fmaf_rn(f[i], by, kRound - y)));
-            }
-            if (far > 0.5f - 0x1p-15f) {
-                const float half = 0.5f * big;
-#pragma unroll
-                for (int i = 0; i < 8; ++i) {
-                    const float e = __fmaf_rn(kRound - __uint_as_float(n[i]), big, 127.f * f[i]);
-                    const uint32_t odd = n[i] & 1;   // ties to even
-                    if (e > half || (e == half && odd)) ++n[i];
-                    else if (e < -half || (e == -half && odd)) --n[i];
-                }
-            }
+        if (lane == 0) p.scale[r] = scale;
+        auto put = [&](const uint4 &v, uint32_t at) {
+            uint32_t n[8];
+            steps8<T>(v, step, n);
             if constexpr (kHalves) {
-                // 1536 + the step is a half with the step in its low bits
-                const __half2 minus = __half2half2(__ushort_as_half(0x6600));
-                uint4 y;
-                uint32_t *w = reinterpret_cast<uint32_t *>(&y);
-#pragma unroll
-                for (int i = 0; i < 4; ++i) {
-                    const uint32_t two = (n[2 * i] + 0x6600u & 0xFFFFu) | (n[2 * i + 1] + 0x6600u) << 16;
-                    const __half2 z = __hsub2(*reinterpret_cast<const __half2 *>(&two), minus);
-                    w[i] = *reinterpret_cast<const uint32_t *>(&z);
-                }
+                const uint4 y = halves8(n);
                 __half *q = static_cast<__half *>(p.q) + at;   // rows of whole vectors
                 if (p.slots == nullptr) *reinterpret_cast<uint4 *>(q + r * p.q_row) = y;
                 else
@@ -578,6 +499,7 @@ struct LinearWork {
 };
 
 uint64_t linear_work(const dm_weights *w, uint32_t rows, void *base, LinearWork &x) {
+    if (takes_raw(w, rows)) return 1;
     uint64_t at = 0;
     auto take = [&](uint64_t bytes) {
         char *p = static_cast<char *>(base) + at;
@@ -629,7 +551,8 @@ extern "C" dm_status dm_linear(const dm_weights *w, const dm_linear_args *a, voi
     if (!a || !linear_ok(w, a->rows) || !a->status || a->dtype > DM_F16 || a->y_dtype > DM_F32 || a->y_dtype == DM_I8 || !(a->eps <= 3.4e38f))
         return DM_ERR_INVALID_ARG;
     LinearWork x;
-    if (!a->work || !aligned(a->work, 256) || a->work_bytes < linear_work(w, a->rows, a->work, x)) return DM_ERR_INVALID_ARG;
+    const uint64_t need = linear_work(w, a->rows, a->work, x);
+    if (need > 1 && (!a->work || !aligned(a->work, 256) || a->work_bytes < need)) return DM_ERR_INVALID_ARG;
     if (a->rows == 0) return DM_OK;
     if (!a->x || !a->y || !aligned(a->x, 16) || !aligned(a->y, dtype_size(a->y_dtype))) return DM_ERR_INVALID_ARG;
     if (a->x_row % 8 || a->x_row > (1ull << 32) || a->y_row > (1ull << 32)) return DM_ERR_INVALID_ARG;
@@ -637,9 +560,14 @@ extern "C" dm_status dm_linear(const dm_weights *w, const dm_linear_args *a, voi
     const auto st = static_cast<cudaStream_t>(stream);
     const auto linear = [&]() -> cudaError_t {
         dm_product_args d{};
-        d.x = x.q, d.x_scale = x.scale, d.x_row = x.q_row, d.x_rows = d.rows = a->rows;
+        d.x_rows = d.rows = a->rows;
         d.y = a->y, d.y_row = a->y_row, d.y_dtype = a->y_dtype, d.status = a->status;
         ProductArgs p = product_args(w, &d);
+        if (need == 1) {
+            p.x = static_cast<const char *>(a->x), p.x_row = a->x_row * 2, p.eps = a->eps;
+            return launch_product_raw(p, a->dtype, st);
+        }
+        p.x = x.q, p.x_scale = x.scale;
         p.x_halves = takes_halves(w, a->rows);
         p.x_row = x.q_row * (p.x_halves ? 2 : 1);
         DM_TRY(quantize(a->dtype, {static_cast<const char *>(a->x), x.q, x.scale, nullptr, a->x_row, x.q_row, a->rows, w->k, a->eps}, p.x_halves, st));

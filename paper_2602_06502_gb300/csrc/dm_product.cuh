@@ -27,6 +27,7 @@ struct ProductArgs {
     uint32_t y_dtype, gated;
     uint32_t x_halves;                 // 8-bit: x holds halves, row r in row r; sources name the scales alone
                                        // (for the kernel for many rows)
+    float eps;                         // of rows that the product quantises itself
 };
 
 // Expert e's rows [a, b); none, and an error, where the offsets are wrong.
@@ -94,6 +95,8 @@ struct WideShape {
 enum RowsAre { kPlain, kGathered, kHalves };
 WideShape wide_shape(const dm_weights *w, uint32_t rows, uint32_t gated, RowsAre are);
 uint64_t product_bytes(const dm_weights *w, uint32_t rows, uint32_t gated, RowsAre are);
+bool takes_raw(const dm_weights *w, uint32_t rows);   // a projection quantises its rows within the product
+cudaError_t launch_product_raw(const ProductArgs &p, uint32_t dtype, cudaStream_t st);
 bool takes_halves(const dm_weights *w, uint32_t rows);   // 8-bit values as halves are worth having
 cudaError_t launch_product_wide(const dm_weights *w, const ProductArgs &p, const WideShape &s, void *work, cudaStream_t st);
 

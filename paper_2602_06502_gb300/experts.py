@@ -279,8 +279,8 @@ class Linear:
         yp, y_row = _matrix("out", out, SCORES, device, rows, w.n)
         size = _size("dm_linear_bytes", device, (w.key, rows), w.ref, rows)
         w.hold()
-        work = torch.empty(size, dtype=torch.uint8, device=device)
-        a = D.dm_linear_args(xp, yp, w.status_at, work.data_ptr(), size, x_row, y_row, TYPES[x.dtype], SCORES[out.dtype], rows, _eps(eps))
+        work, at = _work(size, device)
+        a = D.dm_linear_args(xp, yp, w.status_at, at, size, x_row, y_row, TYPES[x.dtype], SCORES[out.dtype], rows, _eps(eps))
         _call("dm_linear", device, w.ref, C.byref(a))
         return out
 

@@ -132,7 +132,7 @@ def test_choose_bytes(D):
 
 def linear(D, **kw):
     base = dict(x=1 << 22, y=1 << 23, status=1 << 25, work=1 << 26, work_bytes=1 << 30, x_row=96, y_row=64, dtype=D.DM_F16, y_dtype=D.DM_F16,
-                rows=4, eps=-1.0)
+                rows=40, eps=-1.0)
     base.update(kw)
     return D.dm_linear_args(**base)
 
@@ -148,7 +148,9 @@ def test_linear_more(D):
     inv = D.DM_ERR_INVALID_ARG
     assert D.dm_linear(weights(D, experts=1), linear(D)) == inv     # 16-bit weights
     assert D.dm_linear(eight(D), linear(D)) == inv                  # many experts
-    assert D.dm_linear_bytes(weights(D, experts=1), 4) == 0 and D.dm_linear_bytes(eight(D, experts=1), 4) > 0
+    assert D.dm_linear_bytes(weights(D, experts=1), 4) == 0 and D.dm_linear_bytes(eight(D, experts=1), 40) > 1
+    assert D.dm_linear_bytes(eight(D, experts=1), 4) == 1           # so few that no work buffer is wanted
+    assert D.dm_linear(eight(D, experts=1), linear(D, rows=4, work=None, work_bytes=0, x=None)) == inv
     assert D.dm_linear(eight(D, experts=1), linear(D, rows=0)) == D.DM_OK
 
 

@@ -196,6 +196,41 @@ def test_linear(torch, rows, dtype):
     R.close(y, z, R.round_off(z, off, t))
 
 
+@pytest.mark.parametrize("dtype", ["bfloat16", "float16"])
+@pytest.mark.parametrize("k,n", [(16, 1), (31, 40), (72, 24), (1024, 40), (1031, 17), (4100, 200)])
+@pytest.mark.parametrize("rows", [1, 3, 8, 9])
+def test_linear_steps_are_the_quantised_rows(torch, rows, k, n, dtype):
+    """Few rows are quantised within the product: their steps are dm_quantize's, borders and all, so whole numbers as
+    scales give the bits of the two calls."""
+    import experts_reference as R
+    from paper_2602_06502_gb300 import experts as X
+    t, g = getattr(torch, dtype), gen(torch, rows + k)
+    x = R.padded(g, rows, k, R.pad_of(k, t) + 8, t)
+    if rows > 2:
+        x[1] = (torch.arange(k, device="cuda") % 255 - 127).to(t)   # halves of a top of 254
+        x[1, 0] = 254
+        x[2] = 0
+    if rows > 3:
+        x[3] *= 2.0 ** -14 if t is torch.float16 else 1e-33
+        x[4, k // 2] = float("nan")
+    pad = R.pad_of(k, torch.int8)
+    w = X.Weights(R.padded(g, n, k, pad, torch.int8, R.whole(g, (n, k), 127)), torch.rand(n, generator=g, device="cuda") + 0.5)
+    q, scale = X.quantize(x)
+    want = X.product(q, w, x_scale=scale, dtype=torch.float32)
+    y = X.Linear(w)(x, out=torch.empty(rows, n, device="cuda"))
+    if k <= 1024:   # exact sums
+        assert torch.equal(y.nan_to_num(nan=7e30), want.nan_to_num(nan=7e30))
+    z, off = R.sums(q, w.w, scale, w.scale)
+    ok = torch.isfinite(scale)
+    R.close(y[ok], z[ok], R.round_off(z[ok], off[ok], torch.float32))
+    assert torch.isnan(y[~ok]).all()
+    y = X.Linear(w)(x, eps=1e-6, out=torch.empty(rows, n, device="cuda"))
+    q, scale = X.quantize(x, eps=1e-6)
+    z, off = R.sums(q, w.w, scale, w.scale)
+    # and the two sums of squares, each of k terms
+    R.close(y[ok], z[ok], R.round_off(z[ok], off[ok] + z[ok].abs() * (k / 16 + 64) * 2.0 ** -24, torch.float32))
+
+
 # -- the choice of experts -------------------------------------------------------------
 
 @pytest.mark.parametrize("dtype", ["float32", "bfloat16", "float16"])
