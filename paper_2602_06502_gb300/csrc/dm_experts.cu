@@ -161,11 +161,15 @@ cudaError_t launch_quantize(const QuantizeArgs &p, bool halves, cudaStream_t st)
 // expert's first slot in a tile is the sum of the counts of the experts before it
 // and of its own in the tiles before, and within a tile a pair's place is the
 // number of equal ones before it.  Up to kCluster tiles see each other's counts
-// as a cluster, in one launch; more leave them in memory for a second kernel.
+// as a cluster, in one launch; more leave them in memory for a second kernel, each
+// of whose CTAs adds up those before its own; beyond kFewTiles a kernel between
+// the two does that once for all (128 experts, 8 each, with and without it: 2,048
+// tokens 10.4 and 10.0 us, 4,096 11.4 and 12.0, 65,536 63 and 252).
 //
-// Bound: latency.  Four tokens of 8 experts: 2.4 us; 8,192 of 128, 8 each: 17.5 us.
+// Bound: latency, then instructions.  Four tokens of 8 experts: 2.4 us; 8,192 of
+// 128, 8 each: 12 us.
 
-constexpr uint32_t kChooseT = 1024, kTilePairs = 256, kTileTokens = 32, kCluster = 8;
+constexpr uint32_t kChooseT = 1024, kTilePairs = 256, kTileTokens = 32, kCluster = 8, kFewTiles = 96;
 
 struct ChooseArgs {
     const char *logits;
@@ -173,7 +177,7 @@ struct ChooseArgs {
     uint32_t tokens, experts, top_k, renormalize, tile, tiles;   // tokens of a tile; how many tiles
     int32_t *ids, *offsets, *slots, *sources;
     float *weights;
-    int32_t *counts;   // [tile][expert]
+    int32_t *counts;   // [tile][expert]; many tiles: those before, and behind the last tile all
 };
 
 uint32_t tile_tokens(uint32_t top_k) { return std::min(kTileTokens, kTilePairs / top_k); }
@@ -256,7 +260,7 @@ __device__ __forceinline__ void place_experts(const ChooseArgs &p, int32_t mine,
         if (tid < p.experts) p.offsets[tid] = before;
         if (tid == 0) p.offsets[p.experts] = total;
     }
-    for (uint32_t i = (uint32_t)total + tile * kChooseT + tid; i < p.tokens * p.top_k; i += p.tiles * kChooseT) p.sources[i] = -1;
+    for (uint64_t i = (uint64_t)total + (uint64_t)tile * kChooseT + tid; i < p.tokens * p.top_k; i += (uint64_t)p.tiles * kChooseT) p.sources[i] = -1;
 }
 
 template <class T, uint32_t kV>
@@ -319,7 +323,7 @@ __global__ void __launch_bounds__(kChooseT) k_choose(ChooseArgs p) {
     }
     __syncthreads();
     if (p.tiles > kCluster) {
-        if (tid < p.experts) p.counts[tile * p.experts + tid] = s_count[tid];
+        if (tid < p.experts) p.counts[(uint64_t)tile * p.experts + tid] = s_count[tid];
         return;
     }
     cg::cluster_group cl = cg::this_cluster();
@@ -340,31 +344,54 @@ __global__ void __launch_bounds__(kChooseT) k_choose(ChooseArgs p) {
     if (p.tiles > 1) cl.sync();   // the counts have been read
 }
 
+// Counts become the sums of those in the tiles before, an expert a CTA.
+__global__ void __launch_bounds__(kChooseT) k_choose_sums(ChooseArgs p) {
+    __shared__ int32_t s_warp[32];
+    pdl_enter();
+    int32_t before = 0;
+    for (uint64_t i0 = 0; i0 < p.tiles; i0 += kChooseT) {
+        const uint64_t i = i0 + threadIdx.x;
+        int32_t *c = p.counts + i * p.experts + blockIdx.x;
+        int32_t total;
+        const int32_t mine = scan_experts(i < p.tiles ? __ldcg(c) : 0, s_warp, total);
+        if (i < p.tiles) *c = before + mine;
+        before += total;
+        __syncthreads();   // s_warp has been read
+    }
+    if (threadIdx.x == 0) p.counts[(uint64_t)p.tiles * p.experts + blockIdx.x] = before;
+}
+
 __global__ void __launch_bounds__(kChooseT) k_choose_place(ChooseArgs p) {
     extern __shared__ uint32_t s_seen[];
-    __shared__ int32_t s_off[kChooseT], s_warp[32];
+    __shared__ int32_t s_off[kChooseT], s_warp[32], s_mine[kChooseT], s_earlier[kChooseT];
     pdl_enter();
     const uint32_t tid = threadIdx.x, tile = blockIdx.x, first = tile * p.tile;
     const uint32_t pairs = min(p.tile, p.tokens - first) * p.top_k;
     const int32_t e = tid < pairs ? __ldcg(p.ids + first * p.top_k + tid) : -1;
-    // tiles are shared out to groups of threads, one of them an expert's
-    __shared__ int32_t s_mine[kChooseT], s_earlier[kChooseT];
-    s_mine[tid] = s_earlier[tid] = 0;
-    __syncthreads();
-    const uint32_t groups = kChooseT / p.experts, x = tid % p.experts;
-    if (tid / p.experts < groups) {
-        int32_t mine = 0, earlier = 0;
-#pragma unroll 8
-        for (uint32_t i = tid / p.experts; i < p.tiles; i += groups) {
-            const int32_t n = __ldcg(p.counts + i * p.experts + x);
-            mine += n;
-            if (i < tile) earlier += n;
+    int32_t mine = 0, earlier = 0;
+    if (p.tiles > kFewTiles) {
+        if (tid < p.experts) {
+            earlier = __ldcg(p.counts + (uint64_t)tile * p.experts + tid);
+            mine = __ldcg(p.counts + (uint64_t)p.tiles * p.experts + tid);
         }
-        atomicAdd(s_mine + x, mine);   // whole numbers: in any order
-        atomicAdd(s_earlier + x, earlier);
+    } else {
+        // tiles are shared out to groups of threads, one of them an expert's
+        s_mine[tid] = s_earlier[tid] = 0;
+        __syncthreads();
+        const uint32_t groups = kChooseT / p.experts, x = tid % p.experts;
+        if (tid / p.experts < groups) {
+#pragma unroll 8
+            for (uint32_t i = tid / p.experts; i < p.tiles; i += groups) {
+                const int32_t n = __ldcg(p.counts + i * p.experts + x);
+                mine += n;
+                if (i < tile) earlier += n;
+            }
+            atomicAdd(s_mine + x, mine);   // whole numbers: in any order
+            atomicAdd(s_earlier + x, earlier);
+        }
+        __syncthreads();
+        mine = s_mine[tid], earlier = s_earlier[tid];
     }
-    __syncthreads();
-    const int32_t mine = s_mine[tid], earlier = s_earlier[tid];
     place_experts(p, mine, earlier, tile, s_off, s_warp);
     place_pairs(p, first * p.top_k, pairs, e, s_off, s_seen);
 }
@@ -375,13 +402,14 @@ cudaError_t launch_choose(const ChooseArgs &p, cudaStream_t st) {
     const auto k = per <= 1 ? k_choose<T, 1> : per <= 2 ? k_choose<T, 2> : per <= 4 ? k_choose<T, 4> : per <= 8 ? k_choose<T, 8>
                  : per <= 16 ? k_choose<T, 16> : k_choose<T, 32>;
     DM_TRY(launch_pdl_cluster(k, p.tiles, p.tiles > kCluster ? 1 : p.tiles, kChooseT, seen, st, p));
+    if (p.tiles > kFewTiles) DM_TRY(launch_pdl(k_choose_sums, p.experts, kChooseT, 0, st, p));
     return p.tiles > kCluster ? launch_pdl(k_choose_place, p.tiles, kChooseT, seen, st, p) : cudaSuccess;
 }
 
 uint64_t choose_bytes(uint32_t tokens, uint32_t experts, uint32_t top_k) {
     if (experts < 1 || experts > 1024 || top_k < 1 || top_k > std::min(experts, 32u) || (uint64_t)tokens * top_k > 0x7FFFFFFFull) return 0;
     const uint64_t tiles = ((uint64_t)tokens + tile_tokens(top_k) - 1) / tile_tokens(top_k);
-    return tiles <= kCluster ? 1 : tiles * experts * 4;
+    return tiles <= kCluster ? 1 : (tiles + 1) * experts * 4;
 }
 
 cudaError_t choose(const ChooseArgs &from, uint32_t dtype, cudaStream_t st) {

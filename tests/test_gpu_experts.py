@@ -406,3 +406,26 @@ def test_layer_keeps_bad_tokens_apart(torch, tokens, eight):
     bad[[1, 4, 5]] = True
     assert torch.isnan(y[[1, 5]]).all() and not torch.isfinite(y[4]).any()
     assert torch.equal(y[~bad], want[~bad]) and up.last_error() == 0
+
+
+def test_choose_for_many_tokens(torch):
+    """More tokens than 32 bits of threads: 2^27 + 77 in rows of eight scores; the first, the last and the sums."""
+    from paper_2602_06502_gb300 import experts as X
+    tokens = (1 << 27) + 77
+    logits = torch.zeros(tokens, 8, dtype=torch.bfloat16, device="cuda")
+    logits[::2, 3] = 1                       # ties go to the lowest id
+    logits[1::4, 6] = 2
+    logits[-2:] = -float("inf")
+    c = X.choose(logits, 1)
+    del logits
+    want = torch.zeros(tokens, dtype=torch.int32, device="cuda")
+    want[::2], want[1::4], want[-2:] = 3, 6, -1
+    assert torch.equal(c.ids[:, 0], want)
+    counts = torch.stack([(want == e).sum() for e in range(8)])
+    assert torch.equal(c.offsets[1:].long(), counts.cumsum(0)) and int(c.offsets[0]) == 0
+    total = int(counts.sum())
+    for e in (0, 3, 6):
+        a, b = int(c.offsets[e]), int(c.offsets[e + 1])
+        assert torch.equal(c.sources[a:b].long(), torch.nonzero(want == e)[:, 0])
+    assert (c.sources[total:] == -1).all() and (c.slots[-2:] == -1).all()
+    assert torch.equal(c.slots[c.sources[:total].long(), 0], torch.arange(total, dtype=torch.int32, device="cuda"))
