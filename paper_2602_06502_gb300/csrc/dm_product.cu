@@ -26,6 +26,7 @@ namespace {
 // and 64 us: a CTA's beginning and end weigh twice as much.
 
 constexpr uint32_t kFewT = 256, kFewWarps = 8;
+constexpr int kFewShared = 35;   // percent of an SM's memory as shared memory
 
 template <class T>
 struct Few;   // T: of the weights and rows
@@ -98,6 +99,7 @@ __global__ void __launch_bounds__(kFewT, kM * kTiles <= 2 ? 3 : 2) k_product_few
     const uint32_t tid = threadIdx.x, wid = tid >> 5, lane = tid & 31, g = lane >> 2, t = lane & 3;
     const uint32_t e = blockIdx.y, c0 = blockIdx.x * 16;
     const Rows rows = expert_rows(p, e);
+    if (p.most && (uint32_t)(rows.b - rows.a) > p.most) return;
     const uint32_t end = p.k * (uint32_t)sizeof(T), chunks = (end + 63) / 64, last = (end - 1) / 16 * 16;
     const uint32_t x_last = (end - 1) % 16 >= 8 ? 16 : 0;   // kRaw: from where a row's bytes for those of a channel begin, its last 16
     const char *w[kM][2];
@@ -219,10 +221,23 @@ __global__ void __launch_bounds__(kFewT, kM * kTiles <= 2 ? 3 : 2) k_product_few
     }
 }
 
+// What is on its way lies in L1, which a kernel with much shared memory before
+// this one would leave small: this one asks for its own division of the SM (64
+// experts of 2,048 x 2,048, 8 rows each, behind k_product_wide: 158 us without).
+template <class T, int kTiles, int kM, uint32_t kU, class X = T>
+cudaError_t launch_few_one(const ProductArgs &p, cudaStream_t st) {
+    static SmemOptIn asked;
+    int dev = 0;
+    DM_TRY(cudaGetDevice(&dev));
+    if (dev < 0 || dev >= kDevices) return cudaErrorInvalidDevice;
+    const auto k = k_product_few<T, kTiles, kM, kU, X>;
+    DM_TRY(static_cast<cudaError_t>(asked.raise(dev, 1, [&] { return (int)cudaFuncSetAttribute(k, cudaFuncAttributePreferredSharedMemoryCarveout, kFewShared); })));
+    return launch_pdl(k, dim3((p.n + 15) / 16, p.experts), kFewT, 0, st, p);
+}
+
 template <class T, int kTiles, uint32_t kU>
 cudaError_t launch_few_tiles(const ProductArgs &p, cudaStream_t st) {
-    const dim3 grid((p.n + 15) / 16, p.experts);
-    return launch_pdl(p.gated ? k_product_few<T, kTiles, 2, kU> : k_product_few<T, kTiles, 1, kU>, grid, kFewT, 0, st, p);
+    return p.gated ? launch_few_one<T, kTiles, 2, kU>(p, st) : launch_few_one<T, kTiles, 1, kU>(p, st);
 }
 
 template <class T>
@@ -235,7 +250,7 @@ cudaError_t launch_few(const ProductArgs &p, cudaStream_t st) {
     // registers hold of gated ones (eight experts' 4,096 x 1,024: 8.7 us, 9.9
     // with four); else four (6,144 x 4,096 in 8 bits: 7.7 us, 8.1 with two).
     if (p.gated || p.k * sizeof(T) <= 64 * kFewWarps * 2) return launch_few_tiles<T, 1, 2>(p, st);
-    return launch_pdl(k_product_few<T, 1, 1, 4>, dim3((p.n + 15) / 16, p.experts), kFewT, 0, st, p);
+    return launch_few_one<T, 1, 1, 4>(p, st);
 }
 
 }  // namespace
@@ -259,9 +274,18 @@ ProductArgs product_args(const dm_weights *w, const dm_product_args *a) {
 // rows than others, an average of 16 is 140 and 88 us (8 bits).  One of 6,144 x 4,096 with 16 rows 10
 // and 12, 9 and 20, with 32 rows 18 and 13, 16 and 20 us; one of 1,536 x 1,024
 // with 64 rows 6.6 and 9.9, 6.9 and 15.
-static bool many_rows(const dm_weights *w, uint32_t rows) {
+// Where many experts have few rows on average, one may yet have hundreds, which
+// the kernel for few rows takes eight at a time (64 experts of 2,048 x 2,048, bf16,
+// 512 rows: 84 us where they are even, 156 where one expert has them all).  From
+// kBothRows on the other kernel runs behind it, for experts with more than
+// kMostFew: 64 us for those 156, and 3 to 8 us where there is no such expert.
+constexpr uint32_t kMostFew = 64, kBothRows = 1024;
+enum Kernels { kFew, kBoth, kWide };
+static Kernels kernels_of(const dm_weights *w, uint32_t rows) {
     const uint64_t bytes = (uint64_t)w->experts * w->n * w->k * dtype_size(w->dtype);
-    return rows > w->experts * (bytes <= (4u << 20) ? 64ull : bytes <= (32u << 20) ? 32ull : w->experts == 1 ? 16ull : 8ull);
+    const uint64_t most = bytes <= (4u << 20) ? 64 : bytes <= (32u << 20) ? 32 : w->experts == 1 ? 16 : 8;
+    if (rows > w->experts * most) return kWide;
+    return w->experts > 1 && rows > kBothRows ? kBoth : kFew;
 }
 
 // One launch and no work buffer: 4 rows of 1,536 x 1,024 take 13.3 us of the host
@@ -272,22 +296,25 @@ bool takes_raw(const dm_weights *w, uint32_t rows) {
 }
 
 cudaError_t launch_product_raw(const ProductArgs &p, uint32_t dtype, cudaStream_t st) {
-    return launch_pdl(dtype == DM_BF16 ? k_product_few<int8_t, 1, 1, 2, __nv_bfloat16> : k_product_few<int8_t, 1, 1, 2, __half>,
-                      dim3((p.n + 15) / 16), kFewT, 0, st, p);
+    return dtype == DM_BF16 ? launch_few_one<int8_t, 1, 1, 2, __nv_bfloat16>(p, st) : launch_few_one<int8_t, 1, 1, 2, __half>(p, st);
 }
 
-bool takes_halves(const dm_weights *w, uint32_t rows) { return w->dtype == DM_I8 && many_rows(w, rows); }
+bool takes_halves(const dm_weights *w, uint32_t rows) { return w->dtype == DM_I8 && kernels_of(w, rows) == kWide; }
 
 uint64_t product_bytes(const dm_weights *w, uint32_t rows, uint32_t gated, RowsAre are) {
-    if (!many_rows(w, rows)) return 1;
+    if (kernels_of(w, rows) == kFew) return 1;
     const WideShape s = wide_shape(w, rows, gated, are);
     return std::max<uint64_t>(s.x_bytes + s.part_bytes, 1);
 }
 
-cudaError_t launch_product(const dm_weights *w, const ProductArgs &p, void *work, cudaStream_t st) {
-    if (many_rows(w, p.rows)) return launch_product_wide(w, p, wide_shape(w, p.rows, p.gated, p.x_halves ? kHalves : p.sources ? kGathered : kPlain), work, st);
-    if (w->dtype == DM_BF16) return launch_few<__nv_bfloat16>(p, st);
-    return w->dtype == DM_F16 ? launch_few<__half>(p, st) : launch_few<int8_t>(p, st);
+cudaError_t launch_product(const dm_weights *w, const ProductArgs &from, void *work, cudaStream_t st) {
+    ProductArgs p = from;
+    const Kernels k = kernels_of(w, p.rows);
+    p.most = k == kBoth ? kMostFew : 0;
+    const auto few = w->dtype == DM_BF16 ? launch_few<__nv_bfloat16> : w->dtype == DM_F16 ? launch_few<__half> : launch_few<int8_t>;
+    if (k != kWide) DM_TRY(few(p, st));
+    if (k == kFew) return cudaSuccess;
+    return launch_product_wide(w, p, wide_shape(w, p.rows, p.gated, p.x_halves ? kHalves : p.sources ? kGathered : kPlain), work, st);
 }
 
 }  // namespace dm

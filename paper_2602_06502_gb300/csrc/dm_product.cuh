@@ -28,6 +28,7 @@ struct ProductArgs {
     uint32_t x_halves;                 // 8-bit: x holds halves, row r in row r; sources name the scales alone
                                        // (for the kernel for many rows)
     float eps;                         // of rows that the product quantises itself
+    uint32_t most;                     // rows of an expert that the kernel for few rows has, the other has the rest; 0: one has all
 };
 
 // Expert e's rows [a, b); none, and an error, where the offsets are wrong.

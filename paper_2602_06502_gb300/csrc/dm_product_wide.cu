@@ -309,7 +309,8 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(Wide<kEight>::kThrea
     const bool stop = __syncthreads_or(has_err(p.status));
     for (uint32_t e = tid; e < p.experts; e += W::kThreads) {
         const Rows r = stop ? Rows{0, 0} : expert_rows(p, e);
-        first[e + 1] = row_blocks<W::kRows>((uint32_t)(r.b - r.a)) * a.blocks * a.splits;
+        const uint32_t rows = (uint32_t)(r.b - r.a);
+        first[e + 1] = p.most && rows <= p.most ? 0 : row_blocks<W::kRows>(rows) * a.blocks * a.splits;
     }
     if (tid == 0) first[0] = 0;
     if (p.experts > 1) {

@@ -88,7 +88,7 @@ def test_quantize_what_is_not_finite(torch):
 # -- products -----------------------------------------------------------------------
 
 ROWS = {"few": [1, 0, 3, 8], "tiles": [9, 0, 17, 1, 0], "wide": [130, 1, 0, 64], "one": [5], "many": [700], "none": [0, 0, 0],
-        "long": [257, 31, 513], "all": [0, 40]}
+        "long": [257, 31, 513], "all": [0, 40], "one of many": [900] + [3, 0, 1, 5] * 40 + [64, 65]}
 
 
 def case(torch, seed, rows, k, n, dtype, gated=False, exact=True, spare=0):
@@ -112,7 +112,8 @@ def case(torch, seed, rows, k, n, dtype, gated=False, exact=True, spare=0):
 
 
 SHAPES = [("few", 64, 16), ("few", 1024, 256), ("tiles", 200, 48), ("tiles", 1000, 129), ("wide", 512, 384), ("wide", 72, 33), ("one", 31, 1),
-          ("one", 4096, 100), ("many", 320, 520), ("none", 64, 64), ("long", 1408, 264), ("all", 96, 8)]
+          ("one", 4096, 100), ("many", 320, 520), ("none", 64, 64), ("long", 1408, 264), ("all", 96, 8),
+          ("one of many", 520, 160)]
 
 
 @pytest.mark.parametrize("gated", [False, True])
@@ -152,7 +153,8 @@ def test_product_of_whole_numbers_is_exact(torch, rows, k, n, dtype):
 
 
 @pytest.mark.parametrize("dtype", ["bfloat16", "int8"])
-@pytest.mark.parametrize("rows,k,n,gated", [("few", 264, 40, True), ("wide", 264, 40, False), ("long", 96, 300, True)])
+@pytest.mark.parametrize("rows,k,n,gated", [("few", 264, 40, True), ("wide", 264, 40, False), ("long", 96, 300, True),
+                                            ("one of many", 520, 160, False)])
 def test_product_of_chosen_rows(torch, rows, k, n, dtype, gated):
     """Rows that name the rows of x they read, several the same one; y in rows of odd width."""
     import experts_reference as R
