@@ -19,8 +19,9 @@
 // of products) is what L2 gives.
 //
 // Bound: the tensor cores and the power they may draw where there are many rows
-// (16,384 rows of 32 experts, 2 x 1,536 x 4,096, gated, bf16: 250 us, 1.65 PFLOP/s; 8,191
-// x 6,144 x 4,096 in 8 bits: 240 us, 1.7 PFLOP/s); memory where there are few
+// (one expert, 8,191 x 6,144 x 4,096, bf16: 224 us, 1.84 PFLOP/s, 0.97 of the library's
+// rate, in 8 bits 241; 16,384 rows of 32 experts, 2 x 1,536 x 4,096, gated, bf16: 250
+// us, 1.65 PFLOP/s); memory where there are few
 // (64 experts of 2,048 x 2,048 with 16 rows each: 91 us, 5.9 TB/s). In 8 bits a
 // product whose first operand is in tensor memory takes about 125 cycles, however
 // few its rows, so there memory gives 3.5 TB/s (77 us).
@@ -62,6 +63,7 @@ struct WideArgs {
     uint32_t channels;    // of the weights
     uint32_t blocks;      // tiles across the channels
     uint32_t splits, steps;
+    uint32_t even_rows;   // that are as many bytes as an expert's weights
 #ifdef DM_DEBUG
     uint64_t test_wait_ns;   // dm_test_product_wait: 0, or how long waits last
 #endif
@@ -196,7 +198,11 @@ struct Line {   // of tiles
     uint32_t tiles, pair, pairs;
 };
 
-// Tile i: an expert's tiles go through its rows first (they share the weights), then through the channels.
+// Tile i.  An expert's tiles go through its rows first, which share weights, or
+// where its rows are more bytes than its weights through the channels first: what
+// is shared is read from memory once, and the other finds room in L2 (16,384 rows,
+// 4,096 x 4,096, bf16: 279 us, 338 through the rows; 271 and 300 us for the library's
+// product in the same runs).
 template <uint32_t kRows>
 __device__ __forceinline__ Tile tile_at(const WideArgs &a, const Line &l, uint32_t i) {
     uint32_t lo = 0, hi = a.p.experts;   // the last expert that begins by then
@@ -212,11 +218,12 @@ __device__ __forceinline__ Tile tile_at(const WideArgs &a, const Line &l, uint32
     uint32_t x = i - l.first[lo];
     t.split = x % a.splits;
     x /= a.splits;
-    const uint32_t block = x % n;
+    const bool rows_first = rows <= a.even_rows;
+    const uint32_t block = rows_first ? x % n : x / a.blocks, across = rows_first ? x / n : x % a.blocks;
     t.row = (uint32_t)from + block * each;
     t.rows = min(each, rows - block * each);
     t.width = (t.rows + 15) / 16 * 16;
-    t.c0 = x / n * (a.p.gated ? 128 : 256);
+    t.c0 = across * (a.p.gated ? 128 : 256);
     return t;
 }
 
@@ -664,7 +671,7 @@ WideShape wide_shape(const dm_weights *w, uint32_t rows, uint32_t gated, RowsAre
 
 cudaError_t launch_product_wide(const dm_weights *w, const ProductArgs &p, const WideShape &s, void *work, cudaStream_t st) {
     const bool eight = w->dtype == DM_I8;
-    WideArgs a{p, nullptr, (uint64_t)p.rows * w->n, w->n, s.blocks, s.splits, s.steps};
+    WideArgs a{p, nullptr, (uint64_t)p.rows * w->n, w->n, s.blocks, s.splits, s.steps, eight ? w->n / 2 : w->n};
 #ifdef DM_DEBUG
     a.test_wait_ns = g_test_wait_ns;
 #endif

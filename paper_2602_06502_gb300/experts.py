@@ -173,7 +173,7 @@ class Weights:
         """The status of the first product that failed on the device, which it clears (synchronises)."""
         return last_error(self.status)
 
-    def hold(self):
+    def _hold(self):
         """Keeps the memory, once it is dropped, from being given out before the
         current stream is done with it (once per stream)."""
         raw = torch._C._cuda_getCurrentRawStream(self.device.index)
@@ -215,7 +215,7 @@ def product(x, weights, offsets=None, *, x_scale=None, sources=None, per_source=
     yp, y_row = _matrix("out", out, SCORES, device, n, width)
     gathered = sources is not None
     size = _size("dm_product_bytes", device, (w.key, n, gated, gathered), w.ref, n, int(gated), int(gathered))
-    w.hold()
+    w._hold()
     work, at = _work(size, device)
     a = D.dm_product_args(xp, sp, yp, op, None if sources is None else _vector("sources", sources, torch.int32, device, n),
                           w.status_at, at, size, x_row, y_row, n, x.shape[0], per_source, SCORES[out.dtype], gated, 0)
@@ -278,7 +278,7 @@ class Linear:
             out = torch.empty(rows, w.n, dtype=x.dtype, device=device)
         yp, y_row = _matrix("out", out, SCORES, device, rows, w.n)
         size = _size("dm_linear_bytes", device, (w.key, rows), w.ref, rows)
-        w.hold()
+        w._hold()
         work, at = _work(size, device)
         a = D.dm_linear_args(xp, yp, w.status_at, at, size, x_row, y_row, TYPES[x.dtype], SCORES[out.dtype], rows, _eps(eps))
         _call("dm_linear", device, w.ref, C.byref(a))
@@ -315,8 +315,8 @@ class Experts:
         yp, y_row = _matrix("out", out, (x.dtype,), device, tokens, up.k)
         rp, r_row = (None, 0) if residual is None else _matrix("residual", residual, (x.dtype,), device, tokens, up.k)
         size = _size("dm_experts_bytes", device, (self.key, tokens), up.ref, self.down.ref, tokens, self.top_k)
-        up.hold()
-        self.down.hold()
+        up._hold()
+        self.down._hold()
         work = torch.empty(size, dtype=torch.uint8, device=device)
         a = D.dm_experts_args(xp, lp, rp, yp, up.status_at, work.data_ptr(), size, x_row, l_row, r_row, y_row,
                               TYPES[x.dtype], SCORES[logits.dtype], tokens, self.top_k, self.renormalize, 0)
