@@ -482,6 +482,8 @@ struct LayerWork {
     float *weights, *x_scale, *h_scale, *parts;
     char *xq, *h, *hq, *product;
     uint64_t h_row, parts_row, xq_row, hq_row;   // elements
+    uint64_t product_bytes;
+    RowsAre x_are, h_are;
 };
 
 uint64_t layer_work(const dm_weights *up, const dm_weights *down, uint32_t tokens, uint32_t top_k, void *base, LayerWork &w) {
@@ -493,6 +495,7 @@ uint64_t layer_work(const dm_weights *up, const dm_weights *down, uint32_t token
     };
     const uint64_t slots = (uint64_t)tokens * top_k;
     const bool eight = up->dtype == DM_I8;
+    w.x_are = rows_are(up, (uint32_t)slots, true), w.h_are = rows_are(down, (uint32_t)slots, false);
     w.h_row = align_up(down->k, 16), w.parts_row = align_up(down->n, 4), w.xq_row = align_up(up->k, 16), w.hq_row = w.h_row;
     w.offsets = (int32_t *)take(4ull * (up->experts + 1));
     w.ids = (int32_t *)take(4 * slots);
@@ -502,11 +505,12 @@ uint64_t layer_work(const dm_weights *up, const dm_weights *down, uint32_t token
     w.counts = (int32_t *)take(choose_bytes(tokens, up->experts, top_k));
     w.h = take(2 * slots * w.h_row);
     w.parts = (float *)take(4 * slots * w.parts_row);
-    w.xq = take(!eight ? 0 : takes_halves(up, (uint32_t)slots) ? slots * w.xq_row * 2 : tokens * w.xq_row);
+    w.xq = take(!eight ? 0 : w.x_are == kHalves ? slots * w.xq_row * 2 : tokens * w.xq_row);
     w.x_scale = (float *)take(eight ? 4ull * tokens : 0);
-    w.hq = take(eight ? slots * w.hq_row * (takes_halves(down, (uint32_t)slots) ? 2 : 1) : 0);
+    w.hq = take(eight ? slots * w.hq_row * (w.h_are == kHalves ? 2 : 1) : 0);
     w.h_scale = (float *)take(eight ? 4 * slots : 0);
-    w.product = take(std::max(product_bytes(up, (uint32_t)slots, 1, eight ? kHalves : kGathered), product_bytes(down, (uint32_t)slots, 0, kHalves)));
+    w.product_bytes = std::max(product_bytes(up, (uint32_t)slots, 1, w.x_are), product_bytes(down, (uint32_t)slots, 0, w.h_are));
+    w.product = take(w.product_bytes);
     return at;
 }
 
@@ -524,6 +528,8 @@ struct LinearWork {
     char *q, *product;
     float *scale;
     uint64_t q_row;   // elements
+    uint64_t product_bytes;
+    RowsAre are;
 };
 
 uint64_t linear_work(const dm_weights *w, uint32_t rows, void *base, LinearWork &x) {
@@ -535,9 +541,11 @@ uint64_t linear_work(const dm_weights *w, uint32_t rows, void *base, LinearWork 
         return p;
     };
     x.q_row = align_up(w->k, 16);
-    x.q = take(rows * x.q_row * (takes_halves(w, rows) ? 2 : 1));
+    x.are = rows_are(w, rows, false);
+    x.q = take(rows * x.q_row * (x.are == kHalves ? 2 : 1));
     x.scale = (float *)take(4ull * rows);
-    x.product = take(product_bytes(w, rows, 0, kHalves));
+    x.product_bytes = product_bytes(w, rows, 0, x.are);
+    x.product = take(x.product_bytes);
     return at;
 }
 
@@ -596,10 +604,10 @@ extern "C" dm_status dm_linear(const dm_weights *w, const dm_linear_args *a, voi
             return launch_product_raw(p, a->dtype, st);
         }
         p.x = x.q, p.x_scale = x.scale;
-        p.x_halves = takes_halves(w, a->rows);
+        p.x_halves = x.are == kHalves;
         p.x_row = x.q_row * (p.x_halves ? 2 : 1);
         DM_TRY(quantize(a->dtype, {static_cast<const char *>(a->x), x.q, x.scale, nullptr, a->x_row, x.q_row, a->rows, w->k, a->eps}, p.x_halves, st));
-        return launch_product(w, p, x.product, st);
+        return launch_product(w, p, x.product, x.product_bytes, st);
     };
     return status_of(linear());
 }
@@ -661,23 +669,23 @@ extern "C" dm_status dm_experts(const dm_weights *up, const dm_weights *down, co
         ProductArgs up_args = product_args(up, &u);
         if (eight) {
             // halves go straight to the slots of their experts
-            const bool halves = takes_halves(up, slots);
+            const bool halves = w.x_are == kHalves;
             up_args.x = w.xq, up_args.x_scale = w.x_scale, up_args.x_halves = halves, up_args.x_row = w.xq_row * (halves ? 2 : 1);
             DM_TRY(quantize(a->dtype, {static_cast<const char *>(a->x), w.xq, w.x_scale, nullptr, a->x_row, w.xq_row, a->tokens, up->k, -1.f,
                                        halves ? w.slots : nullptr, a->top_k}, halves, st));
         }
-        DM_TRY(launch_product(up, up_args, w.product, st));
+        DM_TRY(launch_product(up, up_args, w.product, w.product_bytes, st));
         dm_product_args d{};
         d.x = w.h, d.x_row = w.h_row, d.x_rows = slots, d.offsets = w.offsets;
         d.y = w.parts, d.y_row = w.parts_row, d.y_dtype = DM_F32, d.rows = slots, d.status = a->status;
         ProductArgs dp = product_args(down, &d);
         if (eight) {
             // straight to the halves that the tensor cores take, where they do
-            dp.x = w.hq, dp.x_scale = w.h_scale, dp.x_halves = takes_halves(down, slots);
+            dp.x = w.hq, dp.x_scale = w.h_scale, dp.x_halves = w.h_are == kHalves;
             dp.x_row = w.hq_row * (dp.x_halves ? 2 : 1);
             DM_TRY(quantize(a->dtype, {w.h, w.hq, w.h_scale, w.offsets + up->experts, w.h_row, w.hq_row, slots, down->k, -1.f}, dp.x_halves, st));
         }
-        DM_TRY(launch_product(down, dp, w.product, st));
+        DM_TRY(launch_product(down, dp, w.product, w.product_bytes, st));
         JoinArgs j{w.parts, w.slots, w.weights, static_cast<const char *>(a->residual), static_cast<char *>(a->y), a->status,
                    w.parts_row, a->residual_row, a->y_row, a->tokens, a->top_k, up->k,
                    aligned(a->residual, 8) && aligned(a->y, 8) && (a->residual_row | a->y_row) % 4 == 0};

@@ -307,14 +307,17 @@ uint64_t product_bytes(const dm_weights *w, uint32_t rows, uint32_t gated, RowsA
     return std::max<uint64_t>(s.x_bytes + s.part_bytes, 1);
 }
 
-cudaError_t launch_product(const dm_weights *w, const ProductArgs &from, void *work, cudaStream_t st) {
+cudaError_t launch_product(const dm_weights *w, const ProductArgs &from, void *work, uint64_t work_bytes, cudaStream_t st) {
     ProductArgs p = from;
     const Kernels k = kernels_of(w, p.rows);
+    WideShape s{};
+    if (k != kFew) s = wide_shape(w, p.rows, p.gated, p.x_halves ? kHalves : p.sources ? kGathered : kPlain);
+    if (s.x_bytes + s.part_bytes > work_bytes) return cudaErrorInvalidValue;
     p.most = k == kBoth ? kMostFew : 0;
     const auto few = w->dtype == DM_BF16 ? launch_few<__nv_bfloat16> : w->dtype == DM_F16 ? launch_few<__half> : launch_few<int8_t>;
     if (k != kWide) DM_TRY(few(p, st));
     if (k == kFew) return cudaSuccess;
-    return launch_product_wide(w, p, wide_shape(w, p.rows, p.gated, p.x_halves ? kHalves : p.sources ? kGathered : kPlain), work, st);
+    return launch_product_wide(w, p, s, work, st);
 }
 
 }  // namespace dm
@@ -341,5 +344,5 @@ extern "C" dm_status dm_product(const dm_weights *w, const dm_product_args *a, v
     if (a->y_row > (1ull << 32) || (a->rows > 1 && a->y_row < n)) return DM_ERR_INVALID_ARG;
     if (w->dtype == DM_I8 && (!a->x_scale || !aligned(a->x_scale, 4))) return DM_ERR_INVALID_ARG;
     if (!aligned(a->offsets, 4) || !aligned(a->sources, 4)) return DM_ERR_INVALID_ARG;
-    return status_of(launch_product(w, product_args(w, a), a->work, static_cast<cudaStream_t>(stream)));
+    return status_of(launch_product(w, product_args(w, a), a->work, a->work ? a->work_bytes : 0, static_cast<cudaStream_t>(stream)));
 }

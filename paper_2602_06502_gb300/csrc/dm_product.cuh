@@ -99,10 +99,16 @@ uint64_t product_bytes(const dm_weights *w, uint32_t rows, uint32_t gated, RowsA
 bool takes_raw(const dm_weights *w, uint32_t rows);   // a projection quantises its rows within the product
 cudaError_t launch_product_raw(const ProductArgs &p, uint32_t dtype, cudaStream_t st);
 bool takes_halves(const dm_weights *w, uint32_t rows);   // 8-bit values as halves are worth having
+// Where the rows of a layer's or a projection's product are: their quantising kernel
+// writes halves where they are worth having, and bytes else.  What a product
+// lays out in its work buffer follows from this, for its size and its launch.
+inline RowsAre rows_are(const dm_weights *w, uint32_t rows, bool gathered) {
+    return takes_halves(w, rows) ? kHalves : gathered ? kGathered : kPlain;
+}
 cudaError_t launch_product_wide(const dm_weights *w, const ProductArgs &p, const WideShape &s, void *work, cudaStream_t st);
 
-// A product of the layer's own, whose arguments are known to be right.
-cudaError_t launch_product(const dm_weights *w, const ProductArgs &p, void *work, cudaStream_t st);
+// A product whose arguments are known to be right; a work buffer that is too small is refused.
+cudaError_t launch_product(const dm_weights *w, const ProductArgs &p, void *work, uint64_t work_bytes, cudaStream_t st);
 ProductArgs product_args(const dm_weights *w, const dm_product_args *a);
 
 }  // namespace dm
