@@ -93,7 +93,7 @@ __global__ void __launch_bounds__(kLanes == 32 ? 256 : kLanes, (kHeld <= 2 ? 6 :
         }
         float scale;
         const RowStep step = row_step<T>(bits, scale);
-        if constexpr (kNorm) scale *= rsqrtf(sum / (float)p.k + p.eps);
+        if constexpr (kNorm) scale = normed(scale, bits, sum / (float)p.k, p.eps);
         if (lane == 0) p.scale[r] = scale;
         auto put = [&](const uint4 &v, uint32_t at) {
             uint32_t n[8];

@@ -128,11 +128,12 @@ __global__ void __launch_bounds__(kFewT, kM * kTiles <= 2 ? 3 : 2) k_product_few
 #pragma unroll
             for (int d = 16; d; d /= 2) sum += __shfl_xor_sync(~0u, sum, d);
             float scale;
-            const RowStep mine = row_step<X>(__reduce_max_sync(~0u, max(tops & 0xFFFFu, tops >> 16)), scale);
+            const uint32_t bits = __reduce_max_sync(~0u, max(tops & 0xFFFFu, tops >> 16));
+            const RowStep mine = row_step<X>(bits, scale);
             __syncthreads();   // the tile before has been read
             if (lane == 0) {
                 s_step[wid] = mine;
-                s_scale[wid] = p.eps >= 0.f ? scale * rsqrtf(sum / (float)p.k + p.eps) : scale;
+                s_scale[wid] = p.eps >= 0.f ? normed(scale, bits, sum / (float)p.k, p.eps) : scale;
             }
             __syncthreads();
             step = s_step[g];

@@ -70,6 +70,10 @@ __device__ __forceinline__ RowStep row_step(uint32_t bits, float &scale) {
     return s;
 }
 
+// The scale of a row that is divided by the root of `mean`, of its squares, plus
+// eps.  A row of zeros keeps 0, also where that root is 0.
+__device__ __forceinline__ float normed(float scale, uint32_t bits, float mean, float eps) { return bits ? scale * rsqrtf(mean + eps) : 0.f; }
+
 // kRound + the steps of eight values, as bits.
 template <class T>
 __device__ __forceinline__ void steps8(uint4 v, const RowStep &s, uint32_t *n) {
