@@ -93,7 +93,32 @@ __global__ void __launch_bounds__(kLanes == 32 ? 256 : kLanes, (kHeld <= 2 ? 6 :
         }
         float scale;
         const RowStep step = row_step<T>(bits, scale);
-        if constexpr (kNorm) scale = normed(scale, bits, sum / (float)p.k, p.eps);
+        if constexpr (kNorm) {
+            const float shift = norm_shift<T>(bits);
+            if (shift != 1.f) {   // the same for the whole row, which is read again: registers are for what is common
+                sum = 0.f;
+#pragma unroll 1
+                for (uint32_t at = lane * 8; at < p.k; at += kLanes * 8) {
+                    uint4 v = load(at);
+                    cut(v, at);
+                    float f[8];
+                    unpack<T>(v, f);
+#pragma unroll
+                    for (int i = 0; i < 8; ++i) sum += f[i] * shift * (f[i] * shift);
+                }
+#pragma unroll
+                for (int d = 16; d; d /= 2) sum += __shfl_xor_sync(~0u, sum, d);
+                if constexpr (kLanes > 32) {
+                    __syncthreads();   // the sums before have been read
+                    if (lane % 32 == 0) s_sum[lane / 32] = sum;
+                    __syncthreads();
+                    sum = 0.f;
+#pragma unroll
+                    for (uint32_t i = 0; i < kLanes / 32; ++i) sum += s_sum[i];
+                }
+            }
+            scale = normed(scale, bits, shift, sum / (float)p.k, p.eps);
+        }
         if (lane == 0) p.scale[r] = scale;
         auto put = [&](const uint4 &v, uint32_t at) {
             uint32_t n[8];
