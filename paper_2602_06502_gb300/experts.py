@@ -22,6 +22,7 @@ from . import dualmap as D
 
 TYPES = {torch.bfloat16: D.DM_BF16, torch.float16: D.DM_F16}
 SCORES = {torch.bfloat16: D.DM_BF16, torch.float16: D.DM_F16, torch.float32: D.DM_F32}
+_MOST = (1 << 31) - 1   # of rows and of a row's elements; ctypes would cut larger numbers off
 _sizes = {}   # of work buffers, by device and shape
 
 
@@ -64,6 +65,8 @@ def _matrix(name, x, dtypes, device, n=None, k=None):
     rows, width = x.shape
     if (n is not None and rows != n) or (k is not None and width != k):
         raise ValueError(f"{name}: shape {(rows, width)}, wanted {(n, k)}")
+    if rows > _MOST or width > _MOST:
+        raise ValueError(f"{name}: at most 2^31 - 1 rows and as many columns")
     row, one = x.stride()
     if one != 1 and width > 1:
         raise ValueError(f"{name}: its last dimension is contiguous")
@@ -133,6 +136,8 @@ class Weights:
     def __init__(self, w, scale=None, *, status=None):
         if w.dim() not in (2, 3) or w.numel() == 0 or w.shape[-1] > 1 and w.stride(-1) != 1:
             raise ValueError("weights are [n, k] or [experts, n, k], not empty, the last dimension contiguous")
+        if max(w.shape) > _MOST:
+            raise ValueError("weights have at most 2^31 - 1 of each dimension")
         if (w.dtype is torch.int8) != (scale is not None) or (scale is None and w.dtype not in TYPES):
             raise ValueError("weights are bfloat16 or float16, or int8 with a scale")
         if w.device.type != "cuda":
@@ -207,8 +212,8 @@ def product(x, weights, offsets=None, *, x_scale=None, sources=None, per_source=
     n = x.shape[0] if sources is None else sources.shape[0]
     if gated and w.n % 2:
         raise ValueError("a gated product has an even number of channels")
-    if per_source < 1:
-        raise ValueError("per_source is at least 1")
+    if not 1 <= per_source < 1 << 32:
+        raise ValueError("per_source is 1 to 2^32 - 1")
     width = w.n // 2 if gated else w.n
     if out is None:
         out = torch.empty(n, width, dtype=dtype or (torch.bfloat16 if w.scale is not None else w.dtype), device=device)
@@ -241,6 +246,8 @@ def choose(logits, top_k, *, renormalize=True):
     device = logits.device
     xp, row = _matrix("logits", logits, SCORES, device)
     tokens, experts = logits.shape
+    if top_k > _MOST:
+        raise D.DualMapError(D.DM_ERR_INVALID_ARG, "dm_choose_bytes")
     size = _size("dm_choose_bytes", device, (tokens, experts, top_k), tokens, experts, top_k)
     ids = torch.empty(tokens, top_k, dtype=torch.int32, device=device)
     weights = torch.empty(tokens, top_k, dtype=torch.float32, device=device)
