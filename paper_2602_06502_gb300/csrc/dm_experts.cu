@@ -580,7 +580,7 @@ bool linear_ok(const dm_weights *w, uint32_t rows) { return weights_ok(w) && w->
 }  // namespace dm
 
 extern "C" dm_status dm_products_last_error(uint32_t *status, void *stream) {
-    if (!status) return DM_ERR_INVALID_ARG;
+    if (!dm::status_ok(status)) return DM_ERR_INVALID_ARG;
     const auto st = static_cast<cudaStream_t>(stream);
     uint32_t e = 0;
     if (cudaMemcpyAsync(&e, status, 4, cudaMemcpyDeviceToHost, st) != cudaSuccess || cudaStreamSynchronize(st) != cudaSuccess)
@@ -609,7 +609,7 @@ extern "C" uint64_t dm_linear_bytes(const dm_weights *w, uint32_t rows) {
 
 extern "C" dm_status dm_linear(const dm_weights *w, const dm_linear_args *a, void *stream) {
     using namespace dm;
-    if (!a || !linear_ok(w, a->rows) || !a->status || a->dtype > DM_F16 || a->y_dtype > DM_F32 || a->y_dtype == DM_I8 || !(a->eps <= 3.4e38f))
+    if (!a || !linear_ok(w, a->rows) || !status_ok(a->status) || a->dtype > DM_F16 || a->y_dtype > DM_F32 || a->y_dtype == DM_I8 || !(a->eps <= 3.4e38f))
         return DM_ERR_INVALID_ARG;
     LinearWork x;
     const uint64_t need = linear_work(w, a->rows, a->work, x);
@@ -666,7 +666,7 @@ extern "C" dm_status dm_experts(const dm_weights *up, const dm_weights *down, co
     using namespace dm;
     if (!a || a->reserved0 || a->renormalize > 1 || a->dtype > DM_F16 || a->logits_dtype > DM_F32 || a->logits_dtype == DM_I8)
         return DM_ERR_INVALID_ARG;
-    if (!layer_ok(up, down, a->tokens, a->top_k) || !a->status) return DM_ERR_INVALID_ARG;
+    if (!layer_ok(up, down, a->tokens, a->top_k) || !status_ok(a->status)) return DM_ERR_INVALID_ARG;
     const bool eight = up->dtype == DM_I8;
     if (!eight && up->dtype != a->dtype) return DM_ERR_INVALID_ARG;
     LayerWork w;

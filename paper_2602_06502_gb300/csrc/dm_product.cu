@@ -347,7 +347,7 @@ extern "C" dm_status dm_product(const dm_weights *w, const dm_product_args *a, v
     using namespace dm;
     if (!a) return DM_ERR_INVALID_ARG;
     const uint64_t need = dm_product_bytes(w, a->rows, a->gated, a->sources != nullptr);
-    if (!need || a->reserved0 || !a->status) return DM_ERR_INVALID_ARG;
+    if (!need || a->reserved0 || !status_ok(a->status)) return DM_ERR_INVALID_ARG;
     if (need > 1 && (a->work_bytes < need || !a->work || !aligned(a->work, 256))) return DM_ERR_INVALID_ARG;
     const uint32_t size = dtype_size(w->dtype), n = a->gated ? w->n / 2 : w->n;
     if (a->y_dtype > DM_F32 || a->y_dtype == DM_I8 || a->x_rows > 0x7FFFFFFFu) return DM_ERR_INVALID_ARG;

@@ -76,6 +76,8 @@ __device__ __forceinline__ void store_y(const ProductArgs &p, uint64_t at, float
 
 inline uint32_t dtype_size(uint32_t t) { return t == DM_I8 ? 1 : t == DM_F32 ? 4 : 2; }
 
+inline bool status_ok(const uint32_t *status) { return status && aligned(status, 4); }
+
 inline bool weights_ok(const dm_weights *w) {
     if (!w || !w->w || !aligned(w->w, 16) || w->dtype > DM_I8) return false;
     if (w->dtype == DM_I8 && (!w->scale || !aligned(w->scale, 4))) return false;
