@@ -541,8 +541,10 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(Wide<kEight>::kThrea
             }
         }
         // the last uses of all places have ended before the CTA does
-        const uint32_t uses = 2 * c;
-        for (uint32_t u = uses > W::kAs ? uses - W::kAs : 0; on && u < uses; ++u) wait(a_empty(u % W::kAs), (u / W::kAs) & 1, gave_up, a);
+        if constexpr (kEight) {
+            const uint32_t uses = 2 * c;
+            for (uint32_t u = uses > W::kAs ? uses - W::kAs : 0; on && u < uses; ++u) wait(a_empty(u % W::kAs), (u / W::kAs) & 1, gave_up, a);
+        }
     }
     fence_before();
     __syncthreads();
