@@ -94,8 +94,10 @@ __global__ void __launch_bounds__(kLanes == 32 ? 256 : kLanes, (kHeld <= 2 ? 6 :
         float scale;
         const RowStep step = row_step<T>(bits, scale);
         if constexpr (kNorm) {
-            const float shift = norm_shift<T>(bits);
-            if (shift != 1.f) {   // the same for the whole row, which is read again: registers are for what is common
+            if (plain_squares<T>(bits)) {
+                scale *= rsqrtf(sum / (float)p.k + p.eps);
+            } else if (far_squares<T>(bits)) {   // the whole row goes here, and is read again: registers are for what is common
+                const float shift = far_shift(bits);
                 sum = 0.f;
 #pragma unroll 1
                 for (uint32_t at = lane * 8; at < p.k; at += kLanes * 8) {
@@ -116,8 +118,8 @@ __global__ void __launch_bounds__(kLanes == 32 ? 256 : kLanes, (kHeld <= 2 ? 6 :
 #pragma unroll
                     for (uint32_t i = 0; i < kLanes / 32; ++i) sum += s_sum[i];
                 }
+                scale = far_scale(bits, sum / (float)p.k, p.eps);
             }
-            scale = normed(scale, bits, shift, sum / (float)p.k, p.eps);
         }
         if (lane == 0) p.scale[r] = scale;
         auto put = [&](const uint4 &v, uint32_t at) {

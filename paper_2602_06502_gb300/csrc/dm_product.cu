@@ -129,8 +129,11 @@ __global__ void __launch_bounds__(kFewT, kM * kTiles <= 2 ? 3 : 2) k_product_few
             for (int d = 16; d; d /= 2) sum += __shfl_xor_sync(~0u, sum, d);
             float scale;
             const uint32_t bits = __reduce_max_sync(~0u, max(tops & 0xFFFFu, tops >> 16));
-            const float shift = norm_shift<X>(bits);
-            if (shift != 1.f && p.eps >= 0.f) {
+            const RowStep mine = row_step<X>(bits, scale);
+            if (p.eps >= 0.f && plain_squares<X>(bits)) {
+                scale *= rsqrtf(sum / (float)p.k + p.eps);
+            } else if (p.eps >= 0.f && far_squares<X>(bits)) {
+                const float shift = far_shift(bits);
                 sum = 0.f;
                 for (uint32_t at = lane * 16; at < 2 * p.k; at += 512) {
                     uint4 v = load16_kept(row + at);
@@ -142,12 +145,12 @@ __global__ void __launch_bounds__(kFewT, kM * kTiles <= 2 ? 3 : 2) k_product_few
                 }
 #pragma unroll
                 for (int d = 16; d; d /= 2) sum += __shfl_xor_sync(~0u, sum, d);
+                scale = far_scale(bits, sum / (float)p.k, p.eps);
             }
-            const RowStep mine = row_step<X>(bits, scale);
             __syncthreads();   // the tile before has been read
             if (lane == 0) {
                 s_step[wid] = mine;
-                s_scale[wid] = p.eps >= 0.f ? normed(scale, bits, shift, sum / (float)p.k, p.eps) : scale;
+                s_scale[wid] = scale;
             }
             __syncthreads();
             step = s_step[g];

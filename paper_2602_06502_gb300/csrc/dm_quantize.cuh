@@ -70,23 +70,25 @@ __device__ __forceinline__ RowStep row_step(uint32_t bits, float &scale) {
     return s;
 }
 
-// What a row's values are multiplied by before they are squared.  Where the
-// largest is between 2^-48 and 2^50, up to 2^24 squares neither overflow nor lose
-// what counts, and it is 1: so for every half, and for nearly every row.
+// Whether a row's squares add up as they are: where its largest value is between
+// 2^-48 and 2^50, up to 2^24 of them neither overflow nor lose what counts.  So for
+// every half, and for nearly every row.
 template <class T>
-__device__ __forceinline__ float norm_shift(uint32_t bits) {
-    if (std::is_same_v<T, __half> || bits == 0 || bits >= 0x7F80) return 1.f;
-    const float top = __uint_as_float(bits << 16);
-    return top > 0x1p50f ? 0x1p-100f : top < 0x1p-48f ? 0x1p96f : 1.f;
+__device__ __forceinline__ bool plain_squares(uint32_t bits) {
+    return std::is_same_v<T, __half> ? bits != 0 : bits - 0x2780u <= 0x5880u - 0x2780u;
 }
-
-// The scale of a row that is divided by the root of `mean`, of its squares after
-// that shift, plus eps.  A row of zeros keeps 0, also where that root is 0.
-__device__ __forceinline__ float normed(float scale, uint32_t bits, float shift, float mean, float eps) {
-    if (bits == 0) return 0.f;
-    if (shift == 1.f) return scale * rsqrtf(mean + eps);
-    const float top = __fdiv_rn(__uint_as_float(bits << 16) * shift, 127.f), more = eps * shift * shift;
-    // `mean` is at most 2^96, so it does not count beside 2^124
+// Whether they add up after a shift: else the row is zeros or not finite, and its
+// scale, 0 or NaN, is the same with any norm.
+template <class T>
+__device__ __forceinline__ bool far_squares(uint32_t bits) {
+    return !std::is_same_v<T, __half> && bits != 0 && bits < 0x7F80;
+}
+// By what its values are multiplied then, and its scale: `mean` is that of the
+// squares so shifted.
+__device__ __forceinline__ float far_shift(uint32_t bits) { return bits > 0x5880 ? 0x1p-100f : 0x1p96f; }
+__device__ __forceinline__ float far_scale(uint32_t bits, float mean, float eps) {
+    const float shift = far_shift(bits), top = __fdiv_rn(__uint_as_float(bits << 16) * shift, 127.f), more = eps * shift * shift;
+    // the mean is at most 2^96, so it does not count beside 2^124
     return more < 0x1p124f ? top * rsqrtf(mean + more) : top * rsqrtf(eps) * 0x1p-96f;
 }
 
