@@ -21,9 +21,10 @@ namespace {
 // A CTA has 16 channels (gated: and their 16 partners); its eight warps share
 // out k, 64 bytes at a time, and add their sums up in the order of the warps.
 //
-// Bound: memory.  One expert of 6,144 x 4,096, 8 rows, bf16: 8.3 us, 6.1 TB/s; 64
-// of 2,048 x 2,048, 8 rows each: 89 us, 6.0 TB/s; in 8 bits, half the bytes, 7.9
-// and 64 us: a CTA's beginning and end weigh twice as much.
+// Bound: memory.  One expert of 6,144 x 4,096, 8 rows, bf16: 10.3 us, 4.9 TB/s; 64
+// of 2,048 x 2,048, 8 rows each: 88 us, 6.1 TB/s; in 8 bits, half the bytes, 7.3
+// us, 3.4 TB/s, and 64 us, 4.2: a CTA's beginning and end weigh twice as much.
+// (Sets of weights in turn, so they come from memory.)
 
 constexpr uint32_t kFewT = 256, kFewWarps = 8;
 constexpr int kFewShared = 35;   // percent of an SM's memory as shared memory
@@ -287,16 +288,22 @@ ProductArgs product_args(const dm_weights *w, const dm_product_args *a) {
 
 // Which kernel has a product.  An expert's weights are read again for every 32
 // rows by the one for few rows, and through more hands by the other.  With 64
-// experts of 2,048 x 2,048 and 16 rows each 106 and 91 us (bf16), 77 and 77 (8
-// bits), with 8 rows 89 and 89, 64 and 76; where some experts have many more
-// rows than others, an average of 16 is 140 and 88 us (8 bits).  One of 6,144 x 4,096 with 16 rows 10
-// and 12, 9 and 20, with 32 rows 18 and 13, 16 and 20 us; one of 1,536 x 1,024
-// with 64 rows 6.6 and 9.9, 6.9 and 15.
+// experts of 2,048 x 2,048 and 16 rows each 105 and 92 us (bf16), 77 and 78 (8
+// bits), with 8 rows 88 and 90, 64 and 77; where some experts have many more
+// rows than others, an average of 16 is 127 and 92, 95 and 78 us.  One of 6,144 x 4,096 with 16 rows 11.6
+// and 14.7, 8.6 and 20, with 32 rows 20 and 15, 15 and 21 us; one of 1,536 x 1,024
+// with 64 rows 7.0 and 8.1, 6.7 and 13.
 // Where many experts have few rows on average, one may yet have hundreds, which
-// the kernel for few rows takes eight at a time (64 experts of 2,048 x 2,048, bf16,
-// 512 rows: 84 us where they are even, 156 where one expert has them all).  From
-// kBothRows on the other kernel runs behind it, for experts with more than
-// kMostFew: 64 us for those 156, and 3 to 8 us where there is no such expert.
+// the kernel for few rows takes eight at a time.  From kBothRows on the other
+// kernel runs behind it, for experts with more than kMostFew.  The kernel for few
+// rows alone, both, and the other alone (us; one expert has all rows; then each
+// has as many): 2,048 rows of 256 experts of 2,048 x 2,048 410, 143, 25; 328, 332,
+// 326 in bf16, 320, 141, 39; 238, 248, 252 in 8 bits; 2,048 rows of 64 experts
+// of 512 x 512 83, 22, 14; 21, 24, 12, and 150, 25, 18; 30, 36, 17.  So both cost 3 to 10 us
+// where no expert has many rows (14 where 8-bit rows are named by sources) and
+// save much where one does; the other alone would save more in most of this range.
+// Up to kBothRows one expert may have them all: 512 rows of 64 of 2,048 x 2,048,
+// bf16, are 129 us then, 90 where they are even.
 constexpr uint32_t kMostFew = 64, kBothRows = 1024;
 enum Kernels { kFew, kBoth, kWide };
 static Kernels kernels_of(const dm_weights *w, uint32_t rows) {

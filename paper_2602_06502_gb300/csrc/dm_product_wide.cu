@@ -19,8 +19,9 @@
 // of products) is what L2 gives.
 //
 // Bound: the tensor cores and the power they may draw where there are many rows
-// (one expert, 8,191 x 6,144 x 4,096, bf16: 224 us, 1.84 PFLOP/s, 0.97 of the library's
-// rate, in 8 bits 241; 16,384 rows of 32 experts, 2 x 1,536 x 4,096, gated, bf16: 250
+// (one expert, 8,191 x 6,144 x 4,096, bf16: 240 us, 1.72 PFLOP/s, with sets of rows and
+// weights in turn, in 8 bits 265; with one set over and over 224, 0.97 of the
+// library's rate, and 241; 16,384 rows of 32 experts, 2 x 1,536 x 4,096, gated, bf16: 250
 // us, 1.65 PFLOP/s); memory where there are few
 // (64 experts of 2,048 x 2,048 with 16 rows each: 91 us, 5.9 TB/s). In 8 bits a
 // product whose first operand is in tensor memory takes about 125 cycles, however

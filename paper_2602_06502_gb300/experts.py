@@ -198,9 +198,9 @@ def product(x, weights, offsets=None, *, x_scale=None, sources=None, per_source=
     offsets: int32 [experts + 1], expert e has rows offsets[e] .. offsets[e +
     1]; without it one expert has them all.  sources: int32 [rows], row r reads
     row sources[r] // per_source of x.  out: where y goes, [rows, n] of bfloat16,
-    float16 or float32; rows outside the offsets stay as they were (in a new
-    output: whatever memory held).  dtype: of a new output (default: x's, for int8
-    bfloat16)."""
+    float16 or float32, which overlaps none of the inputs; rows outside the offsets
+    stay as they were (in a new output: whatever memory held).  dtype: of a new
+    output (default: x's, for int8 bfloat16)."""
     w, device = weights, weights.device
     xp, x_row = _matrix("x", x, (w.dtype,), device, None, w.k)
     if (x_scale is None) != (w.scale is None):
@@ -271,9 +271,9 @@ class Linear:
         self.weights = weights
 
     def __call__(self, x, *, eps=None, out=None):
-        """x [rows, k], bfloat16 or float16; y of x's type, or out.  eps (8-bit
-        weights): rows are first divided by the root of their mean square plus
-        eps, which costs nothing here."""
+        """x [rows, k], bfloat16 or float16; y of x's type, or out, which does not
+        overlap x.  eps (8-bit weights): rows are first divided by the root of their
+        mean square plus eps, which costs nothing here."""
         w = self.weights
         if w.scale is None:
             if eps is not None:
