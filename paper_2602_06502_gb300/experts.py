@@ -297,7 +297,8 @@ class Linear:
 
 class Experts:
     """A layer of experts, each down(silu(g) u) with (g, u) = up(x): up [experts,
-    2 m, k] and down [experts, k, m], both 16-bit or both int8."""
+    2 m, k] and down [experts, k, m], both 16-bit or both int8.  Errors are those
+    of up's status."""
 
     def __init__(self, up, down, top_k, *, renormalize=True):
         if not up.grouped or not down.grouped or up.device != down.device or up.dtype is not down.dtype:

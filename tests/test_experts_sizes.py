@@ -26,7 +26,7 @@ def least(D, up, down, tokens, top_k):
     return same + tokens * k + (2 if halves[1] else 1) * slots * m
 
 
-SHAPES = [(64, 8, 512, 256), (64, 8, 1024, 384), (24, 2, 256, 128), (256, 8, 7168, 2048), (160, 8, 3000 // 16 * 16, 2000),
+SHAPES = [(64, 8, 512, 256), (64, 8, 1024, 384), (24, 2, 256, 128), (256, 8, 7168, 2048), (160, 8, 2992, 2000),
           (1024, 32, 64, 16), (64, 8, 2048, 1024), (5, 2, 272, 48)]
 
 
